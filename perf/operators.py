@@ -296,7 +296,7 @@ def _page_bounds(k_pages, fill):
     some = (fill > 0)[:, None, None]
     both = torch.where(some[..., None], torch.stack([top, low], 2), 0.0)
     scale = _power_of_two(both.abs().amax((2, 3)))
-    codes = torch.ceil(both / scale[..., None, None])
+    codes = torch.ceil(both.double() / scale[..., None, None].double())  # in 32 bits a small channel next to a huge one underflows
     return codes.to(torch.int8), torch.where(some[..., 0], scale, 0.0)
 
 
