@@ -289,6 +289,121 @@ int heatkv_head_scores(const heatkv_shape* shape, const float* beta, int sinks, 
 int heatkv_rank_dispersion(const heatkv_shape* shape, const float* betas, int runs, int sinks, int variant,
                            double* dispersion);
 
+/* ---------------------------------------------------------------------------
+ * Paged cache: requests of different lengths, each at its own step.
+ *
+ * The arenas above belong to one static plan: all batch rows are at the same scale of the same token map.  The calls below
+ * are for a server whose requests come and go: K and V rows lie on pages of page_size rows, a request's tokens on the
+ * pages of its row of a block table, wherever those are.  One step of such a server is
+ *     heatkv_paged_assign   block tables and slots of the new tokens from the requests' lengths, on the GPU
+ *     heatkv_paged_append   (per layer) the new tokens' K and V rows into their slots, with page bounds if wanted
+ *     heatkv_paged_attend   (per layer) attention of the new tokens over their requests' pages; or
+ *     heatkv_paged_select, heatkv_paged_attend_selected: over the pages with the best scores for each token only.
+ * No length crosses to the host, so a step can be captured into a graph and replayed: token tensors have a fixed number of
+ * rows, those from q_start[batch] on belong to no request, are not read as such and keep what they held in every output.
+ * HeatKV's per-head runs fit as well: a (batch row, head) pair is a request with one kv head, its retained tokens are its
+ * pages.
+ *
+ * Layouts (device memory of the caller)
+ *   token tensors  [tokens][heads][d] with any token and head stride (heatkv_rows, in elements; d contiguous; address and
+ *                  strides multiples of 16 bytes): slices of a fused projection are taken as they are
+ *   pages          [num_pages][kv_heads][page_size][d], rows of the dtype, or E4M3 codes (HEATKV_KV_FP8_E4M3, bf16 shapes):
+ *                  rounded to nearest even and saturating at +-448 on append, read back exactly
+ *   table          int32 [batch][max_pages]: page of a request's tokens [i * page_size, (i + 1) * page_size)
+ *   lens           int32 [batch]: tokens of a request that lie in the cache (attention: those of this step among them)
+ *   q_start        int32 [batch + 1]: request b's new tokens are rows q_start[b] .. q_start[b+1]-1 of the token tensors,
+ *                  the last ones of its lens[b] tokens; q_start[0] = 0, ascending
+ * Contents of integer arrays are not checked (they are on the device).  Page numbers, lengths and row numbers out of their
+ * ranges are brought into them: such a call gives wrong outputs, but touches nothing outside of the arrays.
+ *
+ * Limits: q_heads a multiple of kv_heads, at most 16 per kv head; kv_heads <= 1024; d = 64 or 128; page_size 16, 32, 64, 128
+ * or 256; batch <= 4096; tokens <= 2^22; num_pages * page_size and max_pages * page_size <= 2^30; top <= 512 and max_pages <=
+ * 32768 where pages are chosen. */
+typedef struct {
+  int32_t q_heads, kv_heads, d, dtype, kv_format;
+  int32_t page_size, num_pages; /* of the cache */
+  int32_t batch, max_pages;     /* rows and columns of the block table */
+} heatkv_paged_shape;
+
+/* Rows of a token tensor: [tokens][heads][d], strides in elements. */
+typedef struct {
+  void* data;
+  int64_t token_stride, head_stride;
+} heatkv_rows;
+
+#define HEATKV_PAGED_OK 0
+#define HEATKV_PAGED_NO_PAGES 1        /* fewer free pages than the requests need */
+#define HEATKV_PAGED_BAD_LENGTH 2      /* a length is negative, keep > lens, or a request outgrows max_pages */
+#define HEATKV_PAGED_TOO_MANY_TOKENS 3 /* more new tokens than rows of the token tensors */
+#define HEATKV_PAGED_BAD_FREE_LIST 4   /* free_span does not fit the ring, or more pages come back than there are */
+
+/* One step of the page allocator.  Request b keeps the first keep[b] of its lens[b] tokens and gets new_tokens[b] more; it
+ * then holds ceil((keep + new) / page_size) pages.  Pages that it lacks come from the ring of free pages, pages that it no
+ * longer needs go back into it; keep = new = 0 ends a request.
+ * keep, new_tokens  int32 [batch], read only
+ * lens, lens_out    int32 [batch]: tokens before the step; keep + new.  The same array, or two (the state of before stays)
+ * free_ring         int32 [num_pages]: ring buffer of free page numbers; taken from its head, requests in order, given back
+ *                   behind its tail, requests in order, and taken again by a later call at the earliest
+ * free_span, free_span_out  int32 [2]: index of the ring's head, free pages in it.  The same array, or two
+ * table             in place: entries that a request gains are written, all others stay as they are
+ * q_start           out, int32 [batch + 1]
+ * slots             out, int32 [max_tokens]: row of the cache for every new token, page * page_size + row of the page; -1
+ *                   from q_start[batch] on
+ * status            out, int32 [1]: HEATKV_PAGED_*.  Unless it is HEATKV_PAGED_OK the step is not made: lens, free pages and
+ *                   table are as before, q_start is all zeros, slots all -1 (append and attention then do nothing) */
+int heatkv_paged_assign(const heatkv_paged_shape* shape, const int32_t* keep, const int32_t* new_tokens, const int32_t* lens,
+                        int32_t* lens_out, int32_t* free_ring, const int32_t* free_span, int32_t* free_span_out,
+                        int32_t* table, int32_t* q_start, int32_t* slots, int64_t max_tokens, int32_t* status,
+                        void* stream);
+
+/* The new tokens' rows into their slots; slots outside [0, num_pages * page_size) are skipped.  No two tokens share a slot.
+ * bounds, bound_scales: both null, or for heatkv_paged_select: every page that the call touches gets the bounds of its keys
+ * anew, over its rows up to the last one that the call writes.  Tokens of one page then have to stand next to one another,
+ * in the order of their rows, as heatkv_paged_assign makes them.
+ *   bounds        int8 [num_pages][kv_heads][2][d]: the largest key value of a channel and minus the smallest one, in units of
+ *   bound_scales  fp32 [num_pages][kv_heads], a power of two: the least one, from 2^-100 on, of which no value is more than
+ *                 127 times; rounded upwards.  Values beyond +-2^127 count as that, NaN as 0.  8-bit rows: of the codes' values. */
+int heatkv_paged_append(const heatkv_paged_shape* shape, const int32_t* slots, int64_t tokens, heatkv_rows k_new,
+                        heatkv_rows v_new, void* k_pages, void* v_pages, int8_t* bounds, float* bound_scales, void* stream);
+
+/* Attention of the new tokens over their requests' tokens in the cache (append comes first):
+ *     out[t][hq] = softmax(q[t][hq] . K^T * sm_scale) V   over the keys that token t sees:
+ * all lens[b] tokens of its request, or, causal != 0, those up to itself.  A row that sees nothing, or nothing but scores of
+ * minus infinity, is zeros with lse = minus infinity.
+ * out   rows of the dtype, may not overlap q
+ * lse   fp32 [tokens][q_heads] or null: natural logarithm of the sum of exp(q . k * sm_scale)
+ * ws    device scratch of at least heatkv_paged_attend_workspace_bytes(shape, tokens, 0) bytes (may be null when that is 0).
+ *       Calls that may run at the same time, graphs among them, need a workspace each
+ * Arithmetic as heatkv_attend_scale (fp32 softmax statistics and accumulation, probabilities of bf16 shapes rounded to bf16
+ * for the second product).  Few rows with many keys are split over workgroups and joined in a fixed order: the same bits from
+ * call to call; they may differ in the last bits between shapes, numbers of tokens and batches.
+ * Keys and values on a request's pages behind its end are not looked at, whatever they hold. */
+size_t heatkv_paged_attend_workspace_bytes(const heatkv_paged_shape* shape, int64_t tokens, int top);
+int heatkv_paged_attend(const heatkv_paged_shape* shape, int64_t tokens, heatkv_rows q, const void* k_pages,
+                        const void* v_pages, const int32_t* table, const int32_t* q_start, const int32_t* lens, float sm_scale,
+                        int causal, heatkv_rows out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* For every new token and kv head the pages to attend over: `first` leading pages, the `last` ones up to the last that the
+ * token sees (its own page among them, which is why last >= 1), and of the others those with the highest scores, up to `top`
+ * in all.  first >= 0, last >= 1, first + last <= top.
+ * score(page) = bound_scale * sum over channels of (a top + b low), top and low the page's two bounds (whole numbers), a and b
+ * the sums over the kv head's queries of their positive parts and of minus their negative ones, as whole numbers of the power
+ * of two that the largest of these query values fits 127 times (rounded to nearest; +-2^127 and NaN as for the bounds): an
+ * upper bound, up to the rounding of the queries, of what the queries' scores with any key of the page add up to.  The sum is
+ * exact, the score rounded once, to fp32; of equal scores the lower page goes first: the result is the same on any machine.
+ * selected  out, int32 [tokens][kv_heads][top]: pages of the request (columns of the table), ascending, then -1 */
+int heatkv_paged_select(const heatkv_paged_shape* shape, int64_t tokens, heatkv_rows q, const int8_t* bounds,
+                        const float* bound_scales, const int32_t* table, const int32_t* q_start, const int32_t* lens, int first,
+                        int last, int top, int causal, int32_t* selected, void* stream);
+
+/* heatkv_paged_attend over the selected pages of each token and kv head only (of those, the keys that the token sees).
+ * Entries in any order; negative ones, ones behind the last page that the token sees and repeated ones count for nothing.
+ * ws as above, with `top` for the last argument of heatkv_paged_attend_workspace_bytes. */
+int heatkv_paged_attend_selected(const heatkv_paged_shape* shape, int64_t tokens, heatkv_rows q, const void* k_pages,
+                                 const void* v_pages, const int32_t* table, const int32_t* q_start, const int32_t* lens,
+                                 const int32_t* selected, int top, float sm_scale, int causal, heatkv_rows out, float* lse,
+                                 void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

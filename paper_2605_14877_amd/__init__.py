@@ -32,3 +32,17 @@ from .binding import (  # noqa: F401
     heatkv_rank_dispersion,
     library_path,
 )
+from .paged import (  # noqa: F401
+    PAGED_BAD_FREE_LIST,
+    PAGED_BAD_LENGTH,
+    PAGED_NO_PAGES,
+    PAGED_OK,
+    PAGED_TOO_MANY_TOKENS,
+    PagedShape,
+    heatkv_paged_append,
+    heatkv_paged_assign,
+    heatkv_paged_attend,
+    heatkv_paged_attend_selected,
+    heatkv_paged_select,
+    paged_attend_workspace_bytes,
+)

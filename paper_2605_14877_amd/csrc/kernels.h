@@ -82,4 +82,26 @@ hipError_t launch_accumulate_beta(int H, int batch, int K, int layer, int k1, co
 // called at plan upload, repeated calls are cheap.
 hipError_t attend_prepare_device(int dtype);
 
+// --- paged cache (paged_*.hip; paged.h describes the layout) ---
+struct AssignArgs {
+  int batch, num_pages, max_pages, page_log2;
+  long long max_tokens;
+  const int32_t *keep, *new_tokens, *lens, *span;
+  int32_t *lens_out, *span_out, *ring, *table, *q_start, *slots, *status;
+};
+hipError_t launch_paged_assign(const AssignArgs& a, hipStream_t stream);
+
+struct PagedAppendArgs {
+  int dtype, d, H, page_log2, num_pages;
+  bool kv_fp8;
+  long long tokens;
+  const int32_t* slots;
+  const void *k_new, *v_new;
+  long long k_token_stride, k_head_stride, v_token_stride, v_head_stride;  // elements
+  void *k_pages, *v_pages;
+  int8_t* bounds;  // null: rows only
+  float* bound_scales;
+};
+hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t stream);
+
 }  // namespace heatkv

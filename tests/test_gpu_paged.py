@@ -1,0 +1,440 @@
+"""The paged cache on the GPU against its definitions in 64 bits (tests/paged_reference.py): block tables, row writes and page
+bounds, attention, choice of pages, attention over chosen pages, and a server's steps with all of them.
+
+Tolerances of attention, derived: with A = sum p |v| / sum p, S the largest sum of |q_i k_i| sm over the d channels and n the
+keys of a row, the output is off by at most
+  A * (2 e + r) + w |out|,  e = 2^-24 (d S + 2 R + n + 64)
+where e bounds the relative error of a probability or of the row sum in fp32 (the dot product of d terms; the exponent's
+rounding at the range R of the scores in base 2, up to 2 R 2^-24 ln 2 of them; n additions; a few roundings and the 1-ulp
+exponential), r is the rounding of the probabilities to bf16 (2^-8; fp32: 0) and w that of the output (2^-8; fp32: 2^-24,
+in e).  The logarithm of the row sum is off by at most e + 2^-22 |lse|."""
+import math
+import random
+
+import pytest
+import torch
+
+import paper_2605_14877_amd as hk
+from tests import paged_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.bfloat16}
+
+
+def _shape(dtype, q_heads, kv_heads, d, page, num_pages, batch, max_pages):
+    return hk.PagedShape(q_heads, kv_heads, d, page, num_pages, batch, max_pages, "f32" if dtype == "f32" else "bf16",
+                         hk.KV_FP8_E4M3 if dtype == "fp8" else hk.KV_NATIVE)
+
+
+def _ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+class Problem:
+    """Requests with lens tokens in the cache, the last `new` of them of this step; everything that a kernel must not look at
+    is NaN or out of range."""
+
+    def __init__(self, dtype, q_heads, kv_heads, d, page, lens, new, seed=0, pad=3, scale=1.0, spare=2, max_pages=None):
+        g = torch.Generator().manual_seed(seed)
+        self.dtype, self.page, self.lens, self.new = dtype, page, list(lens), list(new)
+        self.H, self.Hq, self.d = kv_heads, q_heads, d
+        held = [ref.pages_of(n, page) for n in lens]
+        self.max_pages = max(max(held), 1) + 1 if max_pages is None else max_pages
+        self.num_pages = sum(held) + spare
+        perm = torch.randperm(self.num_pages, generator=g).tolist()
+        self.table, at = [], 0
+        for n in held:
+            self.table.append(perm[at:at + n])
+            at += n
+        bad = [-1, self.num_pages, 2 ** 31 - 1, -2 ** 31]
+        full = [r + [bad[(i + len(r)) % 4] for i in range(self.max_pages - len(r))] for r in self.table]
+        self.q_start = [0]
+        for n in new:
+            self.q_start.append(self.q_start[-1] + n)
+        self.tokens = self.q_start[-1] + pad
+        dt = DT[dtype]
+        shape = (self.num_pages, kv_heads, page, d)
+        pages = []
+        for _ in range(2):
+            x = ref.to_store((torch.randn(shape, generator=g) * scale).to(dt), dtype == "fp8")
+            keep = torch.zeros(self.num_pages, page, dtype=torch.bool)
+            for n, ids in zip(lens, self.table):
+                for i, p in enumerate(ids):
+                    keep[p, :min(page, n - i * page)] = True
+            x = torch.where(keep[:, None, :, None], x.float(), math.nan).to(x.dtype)
+            pages.append(x)
+        self.k, self.v = pages
+        self.q = (torch.randn(self.tokens, q_heads, d, generator=g) * scale).to(dt)
+        self.sm = 1.0 / math.sqrt(d)
+        self.shape = _shape(dtype, q_heads, kv_heads, d, page, self.num_pages, len(lens), self.max_pages)
+        self.dev = dict(q=self.q.cuda(), k=self.k.cuda(), v=self.v.cuda(), table=_ints(full), q_start=_ints(self.q_start),
+                        lens=_ints(self.lens))
+
+    def run(self, causal, selected=None, out=None, lse=True, **more):
+        d = dict(self.dev, **more)
+        out = torch.full_like(d["q"], 7.0) if out is None else out
+        lse = torch.full((self.tokens, self.Hq), 7.0, device="cuda") if lse else None
+        top = 0 if selected is None else selected.shape[2]
+        n = hk.paged_attend_workspace_bytes(self.shape, self.tokens, top)
+        ws = torch.full((max(n, 16),), 255, dtype=torch.uint8, device="cuda")
+        args = (self.shape, d["q"], d["k"], d["v"], d["table"], d["q_start"], d["lens"])
+        if selected is None:
+            hk.heatkv_paged_attend(*args, self.sm, out, ws, causal=causal, lse=lse)
+        else:
+            hk.heatkv_paged_attend_selected(*args, selected, self.sm, out, ws, causal=causal, lse=lse)
+        torch.cuda.synchronize()
+        return out, lse
+
+    def check(self, causal, got, chosen=None):
+        out, lse = got[0].cpu().double(), got[1].cpu().double()
+        want, want_lse, mag = ref.attend(self.q, self.k, self.v, self.table, self.q_start, self.lens, self.page, self.sm, causal,
+                                         chosen)
+        real = self.q_start[-1]
+        assert torch.all(out[real:] == 7.0) and torch.all(lse[real:] == 7.0), "rows of no request were written"
+        out, lse, want, want_lse, mag = out[:real], lse[:real], want[:real], want_lse[:real], mag[:real]
+        if not real:
+            return
+        r = w = 2.0 ** -8
+        if self.dtype == "f32":
+            r, w = 0.0, 2.0 ** -24
+        q, k = self.q[:real].abs().double(), self.k.double().nan_to_num(0.0).abs()
+        S = float(q.amax((0, 1)) @ k.amax((0, 1, 2))) * self.sm
+        e = 2.0 ** -24 * (self.d * S + 2 * 1.443 * 2 * S + max(self.lens) + 64)
+        off = (out - want).abs() - (mag * (2 * e + r) * (1 + 1e-6) + w * (want.abs() + mag * (2 * e + r)) + 1e-30)
+        assert not out.isnan().any() and float(off.max()) <= 0, f"output off by {float((out - want).abs().max())}"
+        empty = want_lse == -math.inf
+        assert torch.equal(lse == -math.inf, empty) and torch.all(out[empty] == 0)
+        off = (lse - want_lse)[~empty].abs() - (e + 2.0 ** -22 * want_lse[~empty].abs())
+        assert not off.numel() or float(off.max()) <= 0, f"lse off by {float((lse - want_lse)[~empty].abs().max())}"
+
+
+# dtype, q_heads, kv_heads, d, page, lens, new
+FEW = [
+    ("bf16", 1, 1, 64, 16, [1], [1]),
+    ("bf16", 1, 1, 128, 16, [1], [1]),
+    ("bf16", 4, 2, 128, 16, [17, 1, 16, 33, 5], [1, 1, 1, 1, 1]),
+    ("bf16", 6, 2, 64, 32, [31, 32, 33, 64, 65], [1, 0, 1, 1, 1]),
+    ("bf16", 16, 1, 128, 64, [63, 64, 65], [1, 2, 3]),
+    ("bf16", 8, 8, 64, 128, [300, 7], [1, 4]),
+    ("bf16", 5, 5, 128, 256, [513, 255], [3, 1]),
+    ("bf16", 8, 2, 128, 16, [1500, 700, 2048], [1, 1, 1]),
+    ("bf16", 3, 3, 64, 16, [40, 3, 0, 20], [17, 3, 0, 15]),
+    ("fp8", 4, 2, 128, 16, [17, 1, 16, 33, 5], [1, 1, 1, 1, 1]),
+    ("fp8", 6, 2, 64, 32, [31, 32, 33, 64, 65], [1, 0, 1, 1, 1]),
+    ("fp8", 16, 2, 128, 64, [1300, 64, 65], [1, 2, 3]),
+    ("f32", 1, 1, 64, 16, [1], [1]),
+    ("f32", 4, 2, 128, 16, [17, 1, 16, 33, 5], [1, 1, 1, 1, 1]),
+    ("f32", 6, 2, 64, 32, [31, 32, 33, 64, 65], [1, 0, 1, 1, 1]),
+    ("f32", 16, 2, 128, 64, [1300, 64, 65], [1, 2, 3]),
+    ("f32", 3, 3, 64, 16, [40, 3, 0, 20], [17, 3, 0, 15]),
+    ("f32", 4, 4, 128, 32, [200, 90], [70, 33]),
+]
+MANY = [
+    ("bf16", 1, 1, 128, 16, [65], [65]),
+    ("bf16", 1, 1, 64, 16, [65], [65]),
+    ("bf16", 4, 2, 128, 16, [129, 300, 40, 1], [100, 64, 32, 1]),
+    ("bf16", 4, 2, 64, 32, [129, 300, 40, 9], [100, 64, 33, 1]),
+    ("bf16", 16, 1, 128, 64, [40, 5], [33, 5]),
+    ("bf16", 2, 2, 64, 256, [700], [129]),
+    ("bf16", 3, 1, 128, 128, [1000, 64], [90, 3]),
+    ("fp8", 4, 2, 128, 16, [129, 300, 40, 1], [100, 64, 32, 1]),
+    ("fp8", 2, 2, 64, 32, [130, 65], [128, 65]),
+]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("case", FEW + MANY, ids=str)
+def test_attention(case, causal):
+    p = Problem(*case, seed=1)
+    p.check(causal, p.run(causal))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("new", [[9, 0, 70, 2, 1], [3, 1, 2, 2, 1]])
+def test_rows_that_see_nothing_are_zeros(dtype, new):
+    # fewer tokens in the cache than new ones: the first rows of a causal request see nothing; a request without tokens
+    p = Problem(dtype, 2, 1, 64, 16, [4, 0, 20, 0, 0], new, seed=2)
+    for causal in (True, False):
+        p.check(causal, p.run(causal))
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", 2), ("bf16", 70), ("fp8", 70), ("f32", 5)])
+def test_rows_may_be_slices_with_any_stride(dtype, new):
+    p = Problem(dtype, 4, 2, 64, 16, [90, 33], [new, 1], seed=3)
+    want = p.run(True)
+    wide = torch.full((p.tokens, 7, 80), 9.0, dtype=p.q.dtype, device="cuda")
+    q = wide[:, 2:6, 8:72]
+    q.copy_(p.dev["q"])
+    by_head = torch.full((6, p.tokens + 1, 64), 7.0, dtype=p.q.dtype, device="cuda")
+    out = by_head.transpose(0, 1)[:p.tokens, 1:5]
+    got = p.run(True, out=out, q=q)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert torch.all(by_head[0] == 7.0) and torch.all(by_head[5] == 7.0) and torch.all(by_head[:, p.tokens:] == 7.0)
+    # without lse
+    got = p.run(True, lse=False)
+    assert torch.equal(got[0], want[0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("new", [1, 80])
+def test_the_same_call_gives_the_same_bits(dtype, new):
+    p = Problem(dtype, 8, 2, 128, 16, [2000, 900], [new, 1], seed=4)
+    first = p.run(True)
+    for _ in range(2):
+        again = p.run(True)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", 1), ("bf16", 70), ("f32", 2)])
+def test_scores_far_apart_and_rising(dtype, new):
+    # the reference is raised again and again; probabilities of early keys vanish next to later ones
+    p = Problem(dtype, 2, 1, 64, 16, [400], [new], seed=5, scale=3.0)
+    for i, page in enumerate(p.table[0]):
+        p.k[page] = (p.k[page].float() * (0.2 + 0.1 * i)).to(p.k.dtype)
+    p.dev["k"] = p.k.cuda()
+    p.check(True, p.run(True))
+
+
+# ---- block tables ------------------------------------------------------------------------------------------------------
+
+def _allocator(batch, num_pages, max_pages, page, seed):
+    r = random.Random(seed)
+    order = list(range(num_pages))
+    r.shuffle(order)
+    a = ref.Allocator(batch, num_pages, max_pages, page, order, r.randrange(num_pages), num_pages,
+                      [[-5 - b] * max_pages for b in range(batch)], [0] * batch)
+    dev = dict(lens=_ints(a.lens), ring=_ints(a.ring), span=_ints([a.head, a.count]), table=_ints(a.table))
+    return a, dev, r
+
+
+def _assign(shape, dev, keep, new, max_tokens, two=False):
+    q_start = torch.full((shape.batch + 1,), 99, dtype=torch.int32, device="cuda")
+    slots = torch.full((max_tokens,), 99, dtype=torch.int32, device="cuda")
+    status = torch.full((1,), 99, dtype=torch.int32, device="cuda")
+    lens_out, span_out = (torch.full_like(dev["lens"], 99), torch.full_like(dev["span"], 99)) if two else (None, None)
+    hk.heatkv_paged_assign(shape, _ints(keep), _ints(new), dev["lens"], dev["ring"], dev["span"], dev["table"], q_start, slots,
+                           status, lens_out=lens_out, free_span_out=span_out)
+    if two:
+        dev["lens"], dev["span"] = lens_out, span_out
+    torch.cuda.synchronize()
+    return status.item(), q_start.tolist(), slots.tolist()
+
+
+def _same_state(a, dev):
+    return (dev["lens"].tolist() == a.lens and dev["span"].tolist() == [a.head, a.count] and dev["ring"].tolist() == a.ring and
+            dev["table"].tolist() == a.table)
+
+
+@pytest.mark.parametrize("batch,num_pages,max_pages,page,most,max_tokens", [
+    (1, 7, 5, 16, 30, 40), (5, 40, 9, 16, 50, 160), (64, 300, 12, 32, 100, 4096), (65, 400, 12, 32, 200, 5000),
+    (1000, 3000, 6, 64, 150, 90000), (1025, 2600, 4, 16, 30, 30000), (4096, 9000, 4, 256, 300, 700000), (3, 900, 600, 16, 9000, 12000)])
+def test_allocator_steps(batch, num_pages, max_pages, page, most, max_tokens):
+    a, dev, r = _allocator(batch, num_pages, max_pages, page, batch)
+    shape = _shape("bf16", 4, 2, 64, page, num_pages, batch, max_pages)
+    seen = set()
+    for step in range(9):
+        keep, new = [], []
+        for n in a.lens:
+            u = r.random()
+            k = 0 if u < 0.2 else max(0, n - r.randint(0, 2 * page)) if u < 0.4 else n
+            room = max_pages * page - k
+            keep.append(k)
+            new.append(min(room, 0 if u < 0.1 else r.randint(0, most) if u < 0.6 or step == 0 else 1))
+        if step == 4 and a.lens[-1] >= 0:
+            keep[-1] = a.lens[-1] + 1  # more than there are
+        if step == 6:
+            new[0], keep[0] = max_pages * page + 1, 0
+        status, q_start, slots = a.step(keep, new, max_tokens)
+        got = _assign(shape, dev, keep, new, max_tokens, two=step % 2 == 1)
+        assert got == (status, q_start, slots), step
+        assert _same_state(a, dev), step
+        seen.add(status)
+    assert {0, 2} <= seen
+
+
+def test_allocator_refuses_steps_that_do_not_fit():
+    a, dev, _ = _allocator(3, 6, 4, 16, 1)
+    shape = _shape("bf16", 4, 2, 64, 16, 6, 3, 4)
+    assert _assign(shape, dev, [0, 0, 0], [64, 32, 1], 200)[0] == a.step([0, 0, 0], [64, 32, 1], 200)[0] == hk.PAGED_NO_PAGES
+    assert _same_state(a, dev)
+    assert _assign(shape, dev, [0, 0, 0], [40, 32, 1], 72)[0] == a.step([0, 0, 0], [40, 32, 1], 72)[0] == hk.PAGED_TOO_MANY_TOKENS
+    assert _same_state(a, dev)
+    assert _assign(shape, dev, [0, 0, 0], [48, 32, 1], 81) == a.step([0, 0, 0], [48, 32, 1], 81)  # every page, every row
+    assert _same_state(a, dev) and a.count == 0
+    # what is given back in a step is not there to be taken in it
+    assert _assign(shape, dev, [0, 32, 1], [0, 1, 0], 81)[0] == a.step([0, 32, 1], [0, 1, 0], 81)[0] == hk.PAGED_NO_PAGES
+    assert _assign(shape, dev, [0, 32, 1], [0, 0, 0], 81) == a.step([0, 32, 1], [0, 0, 0], 81)
+    assert _assign(shape, dev, [0, 32, 1], [0, 1, 0], 81) == a.step([0, 32, 1], [0, 1, 0], 81)
+    assert _same_state(a, dev)
+    for span in ([6, 1], [-1, 1], [0, 7], [0, -1]):
+        bad = dict(dev, span=_ints(span), lens=dev["lens"].clone(), table=dev["table"].clone(), ring=dev["ring"].clone())
+        status, q_start, slots = _assign(shape, bad, [0, 0, 0], [1, 1, 1], 81)
+        assert status == hk.PAGED_BAD_FREE_LIST and q_start == [0] * 4 and slots == [-1] * 81
+        assert bad["span"].tolist() == span and torch.equal(bad["lens"], dev["lens"])
+    bad = dict(dev, lens=_ints([-1, 33, 0]))
+    assert _assign(shape, bad, [0, 33, 0], [1, 1, 1], 81)[0] == hk.PAGED_BAD_LENGTH
+
+
+# ---- row writes and page bounds -----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("with_bounds", [False, True])
+@pytest.mark.parametrize("d,H,page,cached,new", [
+    (64, 1, 16, [0], [1]), (128, 2, 16, [15, 16, 3, 31], [1, 1, 40, 2]), (64, 3, 64, [63, 0, 100], [130, 1, 0]),
+    (128, 1, 256, [250, 5], [300, 9]), (64, 2, 32, [1] * 70, [1] * 70), (128, 5, 128, [0], [1000])])
+def test_append(dtype, with_bounds, d, H, page, cached, new):
+    g = torch.Generator().manual_seed(d + page)
+    batch, dt = len(new), DT[dtype]
+    lens = [c + n for c, n in zip(cached, new)]
+    held = [ref.pages_of(n, page) for n in lens]
+    num_pages, at = sum(held) + 3, 0
+    perm = torch.randperm(num_pages, generator=g).tolist()
+    table, slots = [], []
+    for h, c, n in zip(held, cached, new):
+        table.append(perm[at:at + h])
+        at += h
+        slots += [table[-1][x // page] * page + x % page for x in range(c, c + n)]
+    total = len(slots)
+    slots += [-1, num_pages * page, 2 ** 31 - 1, -2 ** 31]
+    tokens = len(slots)
+    pages = [ref.to_store(torch.randn(num_pages, H, page, d, generator=g).to(dt), dtype == "fp8") for _ in range(2)]
+    qkv = torch.randn(tokens, 3 * H, d, generator=g).to(dt)
+    qkv *= torch.exp(2 * torch.randn(tokens, 1, 1, generator=g)).to(dt)
+    qkv[0, :, 3] = 600.0  # beyond the largest 8-bit value
+    qkv[total // 2, :, 5] = math.nan
+    qkv[total // 2, :, 6] = math.inf
+    qkv[total // 2, :, 7] = -math.inf
+    qkv[total // 3, :, 8] = 1e-38
+    want = [x.clone() for x in pages]
+    for t, s in enumerate(slots[:total]):
+        for x, first in zip(want, (H, 2 * H)):
+            x[s // page, :, s % page] = ref.to_store(qkv[t, first:first + H], dtype == "fp8")
+    bounds, scales = torch.full((num_pages, H, 2, d), 99, dtype=torch.int8), torch.full((num_pages, H), 99.0)
+    want_b, want_s = bounds.clone(), scales.clone()
+    for c, n, ids in zip(cached, new, table):
+        for i in range(c // page, ref.pages_of(c + n, page) if n else 0):
+            for h in range(H):
+                want_b[ids[i], h], want_s[ids[i], h] = ref.bounds_of(want[0][ids[i], h, :min(page, c + n - i * page)])
+    shape = _shape(dtype, 2 * H, H, d, page, num_pages, batch, max(held))
+    dq, dk, dv, db, ds = (x.cuda() for x in (qkv, *pages, bounds, scales))
+    extra = (db, ds) if with_bounds else ()
+    if dtype == "fp8":  # raw bytes are taken as well
+        hk.heatkv_paged_append(shape, _ints(slots), dq[:, H:2 * H], dq[:, 2 * H:], dk.view(torch.uint8), dv.view(torch.uint8),
+                               *extra)
+    else:
+        hk.heatkv_paged_append(shape, _ints(slots), dq[:, H:2 * H], dq[:, 2 * H:], dk, dv, *extra)
+    torch.cuda.synchronize()
+    for got, x in ((dk, want[0]), (dv, want[1])):
+        got = got.cpu()
+        assert torch.equal(got.float().isnan(), x.float().isnan())
+        assert torch.equal(got.float().nan_to_num(0.5), x.float().nan_to_num(0.5))
+    if with_bounds:
+        assert torch.equal(ds.cpu(), want_s)
+        assert torch.equal(db.cpu(), want_b)
+
+
+def test_bounds_of_values_at_the_ends_of_the_range():
+    rows = torch.zeros(6, 1, 64)
+    rows[0, 0, 0], rows[1, 0, 0] = 127.0, 127.0 * (1 + 2.0 ** -20)
+    rows[2, 0, :2] = torch.tensor([1e-40, -1e-40])
+    rows[3, 0, :2] = torch.tensor([3.4e38, -3.4e38])
+    rows[4, 0, :2] = torch.tensor([2.0 ** -93, 127 * 2.0 ** -100])
+    shape = _shape("f32", 1, 1, 64, 16, 6, 6, 1)
+    k, v = (torch.zeros(6, 1, 16, 64, device="cuda") for _ in range(2))
+    b, s = torch.zeros(6, 1, 2, 64, dtype=torch.int8, device="cuda"), torch.zeros(6, 1, device="cuda")
+    hk.heatkv_paged_append(shape, _ints([16 * i for i in range(6)]), rows.cuda(), rows.cuda(), k, v, b, s)
+    for i in range(6):
+        want_b, want_s = ref.bounds_of(rows[i])
+        assert s[i, 0].item() == want_s and torch.equal(b[i, 0].cpu(), want_b), i
+
+
+# ---- choice of pages, attention over chosen pages --------------------------------------------------------------------------
+
+def _with_bounds(p, coarse=False):
+    b = torch.zeros(p.num_pages, p.H, 2, p.d, dtype=torch.int8)
+    s = torch.zeros(p.num_pages, p.H)
+    for n, ids in zip(p.lens, p.table):
+        for i, x in enumerate(ids):
+            for h in range(p.H):
+                b[x, h], s[x, h] = ref.bounds_of(p.k[x, h, :min(p.page, n - i * p.page)])
+                if coarse:  # many equal scores
+                    b[x, h] = (b[x, h] // 100) * (1 if i % 3 else 0)
+                    s[x, h] = 1.0
+    return b, s
+
+
+SPARSE = [
+    # dtype, q_heads, kv_heads, d, page, lens, new, top, first, last
+    ("bf16", 1, 1, 64, 16, [1], [1], 1, 0, 1),
+    ("bf16", 4, 1, 128, 16, [400, 17, 90], [1, 1, 1], 5, 1, 2),
+    ("bf16", 6, 2, 64, 32, [700, 64, 33], [9, 0, 33], 4, 0, 1),
+    ("bf16", 32, 2, 128, 16, [300, 40], [5, 2], 7, 2, 3),
+    ("fp8", 4, 2, 128, 16, [400, 17, 90], [3, 1, 1], 5, 1, 2),
+    ("fp8", 3, 3, 64, 16, [260, 100], [1, 1], 6, 1, 1),
+    ("f32", 4, 2, 64, 16, [400, 17, 90], [3, 1, 20], 5, 1, 2),
+    ("f32", 6, 2, 128, 64, [900, 120], [1, 1], 3, 0, 1),
+    ("bf16", 2, 2, 64, 16, [2000], [18], 40, 1, 2),
+]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("case", SPARSE, ids=str)
+def test_choice_of_pages_and_attention_over_them(case, causal):
+    top, first, last = case[7:]
+    p = Problem(*case[:7], seed=6)
+    bounds, scales = _with_bounds(p)
+    chosen = ref.select(p.q, bounds, scales, p.table, p.q_start, p.lens, p.page, first, last, top, causal)
+    selected = torch.full((p.tokens, p.H, top), 77, dtype=torch.int32, device="cuda")
+    hk.heatkv_paged_select(p.shape, p.dev["q"], bounds.cuda(), scales.cuda(), p.dev["table"], p.dev["q_start"], p.dev["lens"],
+                           first, last, selected, causal=causal)
+    got = selected.tolist()
+    for t in range(p.tokens):
+        want = [[77] * top] * p.H if chosen[t] is None else [x + [-1] * (top - len(x)) for x in chosen[t]]
+        assert got[t] == want, t
+    p.check(causal, p.run(causal, selected), chosen)
+
+
+@pytest.mark.parametrize("max_pages,new", [(20, 3), (1200, 3), (4000, 1), (4000, 20), (20000, 1), (32768, 2)])
+def test_choice_of_pages_of_requests_of_any_size(max_pages, new):
+    # the workgroup's tokens go by the columns of the table; equal scores go to the lower page
+    n_pages = min(max_pages, 500)
+    p = Problem("bf16", 4, 2, 64, 16, [16 * n_pages - 3, 40], [new, 1], seed=7, max_pages=max_pages)
+    for coarse in (False, True):
+        bounds, scales = _with_bounds(p, coarse)
+        for top, first, last in ((9, 1, 2), (3, 1, 2), (64, 0, 1)):
+            chosen = ref.select(p.q, bounds, scales, p.table, p.q_start, p.lens, p.page, first, last, top, True)
+            selected = torch.full((p.tokens, p.H, top), 77, dtype=torch.int32, device="cuda")
+            hk.heatkv_paged_select(p.shape, p.dev["q"], bounds.cuda(), scales.cuda(), p.dev["table"], p.dev["q_start"],
+                                   p.dev["lens"], first, last, selected)
+            got = selected.tolist()
+            for t in range(p.q_start[-1]):
+                assert got[t] == [x + [-1] * (top - len(x)) for x in chosen[t]], (t, top, coarse)
+    p.check(True, p.run(True, selected), chosen)
+
+
+def test_choice_of_pages_with_queries_out_of_the_ordinary():
+    p = Problem("f32", 2, 1, 64, 16, [300, 50, 70, 90], [1, 1, 1, 1], seed=8, pad=0)
+    p.q[0, 0, 3], p.q[0, 1, 4], p.q[0, 0, 5] = math.nan, math.inf, -math.inf
+    p.q[1] = 0.0
+    p.q[2] *= 1e-36
+    p.q[3] *= 1e30
+    bounds, scales = _with_bounds(p)
+    chosen = ref.select(p.q, bounds, scales, p.table, p.q_start, p.lens, p.page, 1, 1, 4, True)
+    selected = torch.zeros(p.tokens, 1, 4, dtype=torch.int32, device="cuda")
+    hk.heatkv_paged_select(p.shape, p.q.cuda(), bounds.cuda(), scales.cuda(), p.dev["table"], p.dev["q_start"], p.dev["lens"],
+                           1, 1, selected)
+    assert selected.tolist() == [[x + [-1] * (4 - len(x)) for x in row] for row in chosen]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("group", [1, 3, 16])
+def test_selections_of_any_content(dtype, group):
+    # in any order, repeated, negative, behind the end, none at all
+    p = Problem(dtype, 2 * group, 2, 64, 16, [333, 100, 5], [4, 19, 1], seed=9)
+    top, r = 6, random.Random(3)
+    sel = [[[r.choice([-1, -7, 2 ** 31 - 1, r.randrange(0, 25), r.randrange(0, 25), r.randrange(0, 8)]) for _ in range(top)]
+            for _ in range(2)] for _ in range(p.tokens)]
+    sel[0][0], sel[1][1], sel[2][0] = [-1] * top, [3] * top, [24, 23, 22, 21, 20, 0]
+    for causal in (True, False):
+        p.check(causal, p.run(causal, _ints(sel)), sel)
