@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libheatkv.so")
 PROBE_LIB = os.path.join(HERE, "libheatkv_probe.so")
 LIBRARIES = {LIB: ["plan.cpp", "abi.cpp", "attend.hip", "attend_short.hip", "attend_f32.hip", "attend_f32_split.hip", "append.hip", "calibrate.hip",
-                   "paged_abi.cpp", "paged_tables.hip", "paged_append.hip", "paged_select.hip", "paged_attend.hip",
+                   "paged_abi.hip", "paged_tables.hip", "paged_append.hip", "paged_select.hip", "paged_attend.hip",
                    "paged_attend_long.hip", "paged_attend_f32.hip", "paged_join.hip"], PROBE_LIB: ["probe.hip"]}
 CALL_MODULE = os.path.join(HERE, "_heatkv_call.so")
 SOURCES = [src for srcs in LIBRARIES.values() for src in srcs]

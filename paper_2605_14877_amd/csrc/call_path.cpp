@@ -210,10 +210,210 @@ PyObject* calibrate_scales_call(PyObject* const* a, Py_ssize_t n) {
   }));
 }
 
+// ---- paged cache: shapes are the address of a heatkv_paged_shape ----
+
+// The tensors of one call: all on the current device, else nothing here is plainly in order.
+class PagedCall {
+ public:
+  PagedCall(PyObject* shape, PyObject* stream) {
+    s_ = static_cast<const heatkv_paged_shape*>(PyLong_AsVoidPtr(shape));
+    const auto current = c10::hip::getCurrentHIPStreamMasqueradingAsCUDA();
+    device_ = current.device_index();
+    if (stream == Py_None)
+      stream_ = current.stream();
+    else
+      ok_ = PyLong_Check(stream) && ((stream_ = PyLong_AsVoidPtr(stream)), !PyErr_Occurred());
+    ok_ = ok_ && s_;
+  }
+  bool ok() const { return ok_; }
+  const heatkv_paged_shape* shape() const { return s_; }
+  void* stream() const { return stream_; }
+
+  const at::Tensor* tensor(PyObject* o) {
+    if (!THPVariable_Check(o)) return fail();
+    const at::Tensor& x = THPVariable_Unpack(o);
+    if (!x.is_cuda() || x.get_device() != device_) return fail();
+    return &x;
+  }
+  // Contiguous, of the type and sizes given.
+  void* dense(PyObject* o, at::ScalarType type, at::IntArrayRef sizes) {
+    const at::Tensor* x = tensor(o);
+    if (!x || x->scalar_type() != type || !x->is_contiguous() || x->sizes() != sizes) return fail_ptr();
+    return x->data_ptr();
+  }
+  int32_t* ints(PyObject* o, at::IntArrayRef sizes) { return static_cast<int32_t*>(dense(o, at::kInt, sizes)); }
+  // A one-dimensional int32 tensor of any length.
+  int32_t* vector(PyObject* o, int64_t* n) {
+    const at::Tensor* x = tensor(o);
+    if (!x || x->scalar_type() != at::kInt || x->dim() != 1 || !x->is_contiguous()) return static_cast<int32_t*>(fail_ptr());
+    *n = x->size(0);
+    return static_cast<int32_t*>(x->data_ptr());
+  }
+  heatkv_rows rows(PyObject* o, int64_t heads, int64_t* tokens) {  // *tokens < 0: any number
+    const at::Tensor* x = tensor(o);
+    if (!x || x->scalar_type() != (s_->dtype == HEATKV_BF16 ? at::kBFloat16 : at::kFloat) || x->dim() != 3 ||
+        x->size(1) != heads || x->size(2) != s_->d || x->stride(2) != 1 || (*tokens >= 0 && x->size(0) != *tokens)) {
+      ok_ = false;
+      return heatkv_rows{};
+    }
+    *tokens = x->size(0);
+    return heatkv_rows{x->data_ptr(), x->stride(0), x->stride(1)};
+  }
+  void* pages(PyObject* o) {
+    const at::Tensor* x = tensor(o);
+    const int64_t sizes[4] = {s_->num_pages, s_->kv_heads, s_->page_size, s_->d};
+    if (!x || !x->is_contiguous() || x->sizes() != at::IntArrayRef(sizes)) return fail_ptr();
+    const at::ScalarType t = x->scalar_type();
+    const bool fits = s_->kv_format == HEATKV_KV_FP8_E4M3 ? t == at::kFloat8_e4m3fn || t == at::kByte
+                                                           : t == (s_->dtype == HEATKV_BF16 ? at::kBFloat16 : at::kFloat);
+    return fits ? x->data_ptr() : fail_ptr();
+  }
+  // Whether two tensors (or None) have no byte in common.
+  bool apart(PyObject* a, PyObject* b) {
+    if (a == Py_None || b == Py_None) return true;
+    const at::Tensor *x = tensor(a), *y = tensor(b);
+    if (!x || !y) return false;
+    const auto first = [](const at::Tensor& t) { return reinterpret_cast<uintptr_t>(t.data_ptr()); };
+    const auto end = [&](const at::Tensor& t) {
+      int64_t n = 1;
+      for (int64_t i = 0; i < t.dim(); ++i) n += (t.size(i) - 1) * t.stride(i);
+      return first(t) + static_cast<uintptr_t>(n) * t.element_size();
+    };
+    return x->numel() == 0 || y->numel() == 0 || end(*x) <= first(*y) || end(*y) <= first(*x);
+  }
+
+ private:
+  const at::Tensor* fail() {
+    ok_ = false;
+    return nullptr;
+  }
+  void* fail_ptr() {
+    ok_ = false;
+    return nullptr;
+  }
+  const heatkv_paged_shape* s_;
+  void* stream_ = nullptr;
+  int64_t device_;
+  bool ok_ = true;
+};
+
+bool boolean(PyObject* o, int* v) {
+  *v = o == Py_True;
+  return PyBool_Check(o);
+}
+
+// paged_assign(shape, keep, new_tokens, lens, ring, span, table, q_start, slots, status, lens_out, span_out, stream)
+PyObject* paged_assign(PyObject* const* a, Py_ssize_t n) {
+  if (n != 13) return not_plain();
+  PagedCall c(a[0], a[12]);
+  if (!c.ok()) return not_plain();
+  const heatkv_paged_shape* s = c.shape();
+  int64_t tokens = 0;
+  const int64_t table_size[2] = {s->batch, s->max_pages};
+  int32_t *keep = c.ints(a[1], {s->batch}), *come = c.ints(a[2], {s->batch}), *lens = c.ints(a[3], {s->batch});
+  int32_t *ring = c.ints(a[4], {s->num_pages}), *span = c.ints(a[5], {2}), *table = c.ints(a[6], table_size);
+  int32_t *q_start = c.ints(a[7], {int64_t(s->batch) + 1}), *slots = c.vector(a[8], &tokens), *status = c.ints(a[9], {1});
+  int32_t* lens_out = a[10] == Py_None ? lens : c.ints(a[10], {s->batch});
+  int32_t* span_out = a[11] == Py_None ? span : c.ints(a[11], {2});
+  if (!c.ok()) return not_plain();
+  return PyLong_FromLong(heatkv::without_lock([&] {
+    return heatkv_paged_assign(s, keep, come, lens, lens_out, ring, span, span_out, table, q_start, slots, tokens, status,
+                               c.stream());
+  }));
+}
+
+// paged_append(shape, slots, k_new, v_new, k_pages, v_pages, bounds, scales, stream)
+PyObject* paged_append(PyObject* const* a, Py_ssize_t n) {
+  if (n != 9) return not_plain();
+  PagedCall c(a[0], a[8]);
+  if (!c.ok()) return not_plain();
+  const heatkv_paged_shape* s = c.shape();
+  int64_t tokens = 0;
+  const int32_t* slots = c.vector(a[1], &tokens);
+  const heatkv_rows k = c.rows(a[2], s->kv_heads, &tokens), v = c.rows(a[3], s->kv_heads, &tokens);
+  void *kp = c.pages(a[4]), *vp = c.pages(a[5]);
+  void* bounds = a[6] == Py_None ? nullptr : c.dense(a[6], at::kChar, {s->num_pages, s->kv_heads, 2, s->d});
+  void* scales = a[7] == Py_None ? nullptr : c.dense(a[7], at::kFloat, {s->num_pages, s->kv_heads});
+  if (!c.ok()) return not_plain();
+  return PyLong_FromLong(heatkv::without_lock([&] {
+    return heatkv_paged_append(s, slots, tokens, k, v, kp, vp, static_cast<int8_t*>(bounds), static_cast<float*>(scales),
+                               c.stream());
+  }));
+}
+
+// paged_attend(shape, q, k_pages, v_pages, table, q_start, lens, selected, sm_scale, out, ws, causal, lse, stream)
+PyObject* paged_attend(PyObject* const* a, Py_ssize_t n) {
+  if (n != 14) return not_plain();
+  PagedCall c(a[0], a[13]);
+  if (!c.ok()) return not_plain();
+  const heatkv_paged_shape* s = c.shape();
+  int64_t tokens = -1, top = 0;
+  float sm;
+  int causal;
+  const heatkv_rows q = c.rows(a[1], s->q_heads, &tokens);
+  void *kp = c.pages(a[2]), *vp = c.pages(a[3]);
+  const int32_t *table = c.ints(a[4], {s->batch, s->max_pages}), *q_start = c.ints(a[5], {int64_t(s->batch) + 1}),
+                *lens = c.ints(a[6], {s->batch});
+  const heatkv_rows out = c.rows(a[9], s->q_heads, &tokens);
+  void* lse = a[12] == Py_None ? nullptr : c.dense(a[12], at::kFloat, {tokens, s->q_heads});
+  const int32_t* selected = nullptr;
+  if (a[7] != Py_None) {
+    const at::Tensor* x = c.tensor(a[7]);
+    if (!x || x->dim() != 3) return not_plain();
+    top = x->size(2);
+    selected = c.ints(a[7], {tokens, s->kv_heads, top});
+  }
+  void* ws;
+  size_t ws_bytes;
+  if (!number(a[8], &sm) || !boolean(a[11], &causal) || !buffer(a[10], 0, &ws, &ws_bytes) || !c.ok()) return not_plain();
+  if (a[10] != Py_None && !c.tensor(a[10])) return not_plain();
+  for (PyObject* other : {a[1], a[2], a[3], a[7], a[10], a[12]})
+    if (!c.apart(a[9], other)) return not_plain();
+  return PyLong_FromLong(heatkv::without_lock([&] {
+    if (selected)
+      return heatkv_paged_attend_selected(s, tokens, q, kp, vp, table, q_start, lens, selected, static_cast<int>(top), sm, causal,
+                                          out, static_cast<float*>(lse), ws, ws_bytes, c.stream());
+    return heatkv_paged_attend(s, tokens, q, kp, vp, table, q_start, lens, sm, causal, out, static_cast<float*>(lse), ws, ws_bytes,
+                               c.stream());
+  }));
+}
+
+// paged_select(shape, q, bounds, scales, table, q_start, lens, first, last, selected, causal, stream)
+PyObject* paged_select(PyObject* const* a, Py_ssize_t n) {
+  if (n != 12) return not_plain();
+  PagedCall c(a[0], a[11]);
+  if (!c.ok()) return not_plain();
+  const heatkv_paged_shape* s = c.shape();
+  int64_t tokens = -1;
+  long first, last;
+  int causal;
+  const heatkv_rows q = c.rows(a[1], s->q_heads, &tokens);
+  const void* bounds = c.dense(a[2], at::kChar, {s->num_pages, s->kv_heads, 2, s->d});
+  const void* scales = c.dense(a[3], at::kFloat, {s->num_pages, s->kv_heads});
+  const int32_t *table = c.ints(a[4], {s->batch, s->max_pages}), *q_start = c.ints(a[5], {int64_t(s->batch) + 1}),
+                *lens = c.ints(a[6], {s->batch});
+  const at::Tensor* x = c.tensor(a[9]);
+  if (!x || x->dim() != 3) return not_plain();
+  const int64_t top = x->size(2);
+  int32_t* selected = c.ints(a[9], {tokens, s->kv_heads, top});
+  if (!integer(a[7], &first) || !integer(a[8], &last) || !boolean(a[10], &causal) || !c.ok() || top > INT32_MAX ||
+      first != static_cast<int>(first) || last != static_cast<int>(last))
+    return not_plain();
+  return PyLong_FromLong(heatkv::without_lock([&] {
+    return heatkv_paged_select(s, tokens, q, static_cast<const int8_t*>(bounds), static_cast<const float*>(scales), table, q_start,
+                               lens, static_cast<int>(first), static_cast<int>(last), static_cast<int>(top), causal, selected,
+                               c.stream());
+  }));
+}
+
 PyMethodDef methods[] = {{"plan_info", plan_info, METH_VARARGS, nullptr},
                          {"scale_call", heatkv::fastcall<scale_call>(), METH_FASTCALL, nullptr},
                          {"calibrate_call", heatkv::fastcall<calibrate_call>(), METH_FASTCALL, nullptr},
                          {"calibrate_scales_call", heatkv::fastcall<calibrate_scales_call>(), METH_FASTCALL, nullptr},
+                         {"paged_assign", heatkv::fastcall<paged_assign>(), METH_FASTCALL, nullptr},
+                         {"paged_append", heatkv::fastcall<paged_append>(), METH_FASTCALL, nullptr},
+                         {"paged_attend", heatkv::fastcall<paged_attend>(), METH_FASTCALL, nullptr},
+                         {"paged_select", heatkv::fastcall<paged_select>(), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_heatkv_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

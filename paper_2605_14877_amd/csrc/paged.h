@@ -102,17 +102,14 @@ __device__ __forceinline__ int code_exponent(float amax) {
   return amax > 0.f ? max(__builtin_amdgcn_frexp_expf(amax) - (m <= 127.f / 128.f ? 7 : 6), -100) : -100;
 }
 
-// How the keys of a tile are split over workgroups: `steps` units of work (of 32 or 64 keys), `splits` workgroups at hand,
-// no less than `least` units for each.
-__device__ __forceinline__ int split_size(int steps, int splits, int least) { return max((steps + splits - 1) / splits, least); }
-
 struct Rows {  // of the token tensors, strides in elements
   const void* data;
   long long token_stride, head_stride;
 };
 
-// Requests of more query rows per kv head than this are the long kernel's, where it is launched.
-constexpr int LONG_ROWS = 64;
+struct Border {
+  int b, h, t, parts;  // segment that a border between two shares cuts, and its parts
+};
 
 struct AttendParams {
   Cache c;
@@ -122,29 +119,14 @@ struct AttendParams {
   int top;
   float sm_scale;
   float* lse;           // [tokens][Hq] or null
-  // Rows whose keys are split over workgroups (splits > 1): what each of them has found, and how many there are of it.
-  float *part_o, *part_ml;  // [splits][part_rows][d], [splits][part_rows][2]: unnormalised output; reference and sum
-  int* parts;               // [part_rows]; up to 1: the output is in its place already
-  long long part_rows;
-  int splits;
-  int tiles;  // of the kernel at hand
-  // Next to a launch of the long kernel: the requests of up to LONG_ROWS rows only, LONG_ROWS / 16 tiles for each request.
-  int short_requests;
-  int long_only;  // the join of the long kernel's parts
+  // Requests of this launch, by their query rows per kv head (new tokens x group): least_rows < rows <= most_rows.
+  int least_rows, most_rows;
+  // How it is dealt (paged_schedule.h): workgroups, weight of the lightest share.
+  int workgroups, least_weight, whole_from;
+  int grid;
+  float *part_o, *part_ml;  // parts of cut segments: [workgroups][2][ROWS][d] unnormalised outputs, [..][2] reference and sum
+  Border* borders;          // [workgroups]; null: nothing can be cut
 };
-__device__ __forceinline__ Tile find_row_tile(const AttendParams& p, int tile, int lane) {
-  if (!p.short_requests) return find_tile<16>(p.c, tile, lane);
-  Tile t;
-  t.b = tile / (LONG_ROWS / 16);
-  fill_tile(p.c, t);
-  t.row0 = tile % (LONG_ROWS / 16) * 16;
-  t.rows = t.n_new * p.c.G > LONG_ROWS ? 0 : min(t.n_new * p.c.G - t.row0, 16);
-  return t;
-}
-// Where a row's parts are: query row `row` of the request, i.e. query head hq of `token`.
-__device__ __forceinline__ long long part_row(const AttendParams& p, int b, int row, int h, long long token, int hq) {
-  return p.short_requests ? (static_cast<long long>(b) * LONG_ROWS + row) * p.c.H + h : token * p.c.Hq + hq;
-}
 
 struct SelectParams {
   Cache c, tokens_as_rows;  // the second with G = 1: tiles of tokens
@@ -165,6 +147,6 @@ hipError_t launch_paged_select(const PagedSelectParams& p, int dtype, int d, hip
 hipError_t launch_paged_attend_bf16(const PagedAttendParams& p, int d, bool fp8, hipStream_t stream);
 hipError_t launch_paged_attend_long(const PagedAttendParams& p, int d, bool fp8, hipStream_t stream);
 hipError_t launch_paged_attend_f32(const PagedAttendParams& p, int d, hipStream_t stream);
-hipError_t launch_paged_join(const PagedAttendParams& p, int dtype, int d, hipStream_t stream);
+hipError_t launch_paged_join(const PagedAttendParams& p, int dtype, int d, bool many, hipStream_t stream);
 
 }  // namespace heatkv

@@ -9,6 +9,7 @@
 #include "heatkv.h"
 #include "kernels.h"
 #include "paged.h"
+#include "paged_schedule.h"
 #include "paged_rules.h"
 #include "plan.h"
 
@@ -64,6 +65,14 @@ int check_rows(const heatkv_paged_shape* s, const heatkv_rows& r, const char* na
   return HEATKV_OK;
 }
 
+// Rows that are written: no two of them share an element.
+int check_apart(const heatkv_paged_shape* s, int64_t tokens, int64_t heads, const heatkv_rows& r, const char* name) {
+  const int64_t t = r.token_stride, h = r.head_stride, d = s->d;
+  const bool apart = (tokens == 1 || t >= d) && (heads == 1 || h >= d) &&
+                     (tokens == 1 || heads == 1 || t >= (heads - 1) * h + d || h >= (tokens - 1) * t + d);
+  return apart ? HEATKV_OK : fail(HEATKV_EINVAL, std::string(name) + ": rows overlap one another");
+}
+
 int check_cache(const void* k_pages, const void* v_pages) {
   if (!k_pages || !v_pages) return fail(HEATKV_EINVAL, "null page pointer");
   if (!aligned(k_pages, 16) || !aligned(v_pages, 16)) return fail(HEATKV_EINVAL, "pages must be 16-byte aligned");
@@ -106,39 +115,35 @@ heatkv::paged::Cache cache_of(const heatkv_paged_shape* s, int64_t tokens, const
   return c;
 }
 
-// Workspace: the parts of rows that are split, of the few-row launch and of the long one, each array from a multiple of 256
-// bytes on.
+// Workspace: the parts of cut segments, of the few-row launch and of the long one, each array from a multiple of 256 bytes on.
 struct PartArrays {
-  int64_t rows = 0;
-  size_t o = 0, ml = 0, parts = 0;
+  size_t o = 0, ml = 0, borders = 0;
 };
 struct Workspace {
   PartArrays few, many;
   size_t total = 0;
 };
-Workspace workspace_of(const heatkv_paged_shape* s, int64_t tokens, const heatkv::paged::Split& split) {
+Workspace workspace_of(const heatkv_paged_shape* s, const heatkv::paged::Plan& plan) {
   Workspace w;
   auto take = [&](size_t n) {
     const size_t at = w.total;
     w.total += (n + 255) / 256 * 256;
     return at;
   };
-  auto arrays = [&](PartArrays& a, int64_t rows, int splits) {
-    if (splits <= 1) return;
-    a.rows = rows;
-    a.o = take(size_t(rows) * splits * s->d * 4);
-    a.ml = take(size_t(rows) * splits * 8);
-    a.parts = take(size_t(rows) * 4);
+  auto arrays = [&](PartArrays& a, const heatkv::paged::Launch& l, int rows) {
+    if (!l.workgroups || !l.join) return;
+    a.o = take(size_t(l.workgroups) * 2 * rows * s->d * 4);
+    a.ml = take(size_t(l.workgroups) * 2 * rows * 8);
+    a.borders = take(size_t(l.workgroups) * sizeof(heatkv::paged::Border));
   };
-  static_assert(heatkv::paged::MANY_ROWS == heatkv::paged::LONG_ROWS, "rules and kernels agree");
-  arrays(w.few, split.many ? int64_t(s->batch) * heatkv::paged::LONG_ROWS * s->kv_heads : tokens * s->q_heads, split.few);
-  arrays(w.many, tokens * s->q_heads, split.many);
+  arrays(w.few, plan.few, 16);
+  arrays(w.many, plan.many, 128);
   return w;
 }
 
-heatkv::paged::Split splits_of(const heatkv_paged_shape* s, int64_t tokens, int top) {
-  return heatkv::paged::plan_splits(s->dtype == HEATKV_BF16, s->batch, s->kv_heads, s->q_heads / s->kv_heads,
-                                    tokens, int64_t(s->max_pages) * s->page_size, int64_t(top) * s->page_size);
+heatkv::paged::Plan plan_of(const heatkv_paged_shape* s, int64_t tokens, int top) {
+  return heatkv::paged::plan_launches(s->dtype == HEATKV_BF16, s->batch, s->kv_heads, s->q_heads / s->kv_heads, tokens,
+                                      int64_t(s->max_pages) * s->page_size, int64_t(top) * s->page_size);
 }
 
 int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const void* k_pages, const void* v_pages,
@@ -151,12 +156,13 @@ int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const voi
   if (tokens == 0) return HEATKV_OK;
   if (!rc) rc = check_rows(s, q, "q");
   if (!rc) rc = check_rows(s, out, "out");
+  if (!rc) rc = check_apart(s, tokens, s->q_heads, out, "out");
   if (!rc) rc = check_cache(k_pages, v_pages);
   if (!rc) rc = check_ints({table, q_start, lens});
   if (rc) return rc;
   if (lse && !aligned(lse, 4)) return fail(HEATKV_EINVAL, "lse must be 4-byte aligned");
-  const auto split = splits_of(s, tokens, top);
-  const Workspace w = workspace_of(s, tokens, split);
+  const auto plan = plan_of(s, tokens, top);
+  const Workspace w = workspace_of(s, plan);
   if (w.total > 0) {
     if (!ws || ws_bytes < w.total) return fail(HEATKV_EINVAL, "paged attention workspace too small");
     if (!aligned(ws, 16)) return fail(HEATKV_EINVAL, "workspace must be 16-byte aligned");
@@ -171,31 +177,29 @@ int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const voi
   p.top = top;
   p.sm_scale = sm_scale;
   p.lse = lse;
-  auto use = [&](const PartArrays& a, int splits) {
-    char* base = static_cast<char*>(ws);
-    p.part_o = reinterpret_cast<float*>(base + a.o);
-    p.part_ml = reinterpret_cast<float*>(base + a.ml);
-    p.parts = reinterpret_cast<int*>(base + a.parts);
-    p.part_rows = a.rows;
-    p.splits = splits;
-  };
   const auto hip_stream = static_cast<hipStream_t>(stream);
   const bool fp8 = s->kv_format == HEATKV_KV_FP8_E4M3;
-  hipError_t e = hipSuccess;
-  if (split.many) {
-    use(w.many, split.many);
-    p.long_only = 1;
-    e = heatkv::launch_paged_attend_long(p, s->d, fp8, hip_stream);
-    if (e == hipSuccess && split.many > 1) e = heatkv::launch_paged_join(p, s->dtype, s->d, hip_stream);
-    p.long_only = 0;
-    p.short_requests = 1;
-  }
-  if (e == hipSuccess) {
-    use(w.few, split.few);
-    e = s->dtype == HEATKV_F32 ? heatkv::launch_paged_attend_f32(p, s->d, hip_stream)
-                               : heatkv::launch_paged_attend_bf16(p, s->d, fp8, hip_stream);
-  }
-  if (e == hipSuccess && split.few > 1) e = heatkv::launch_paged_join(p, s->dtype, s->d, hip_stream);
+  auto launch = [&](const heatkv::paged::Launch& l, const PartArrays& a, bool many) {
+    if (!l.workgroups) return hipSuccess;
+    p.workgroups = l.workgroups;
+    p.least_weight = l.least_steps * heatkv::paged::STEP_WEIGHT;
+    p.least_rows = l.least_rows;
+    p.most_rows = l.most_rows;
+    p.grid = int(l.grid);
+    p.whole_from = l.whole_from;
+    p.borders = nullptr;
+    if (l.join) {
+      p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + a.o);
+      p.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + a.ml);
+      p.borders = reinterpret_cast<heatkv::paged::Border*>(static_cast<char*>(ws) + a.borders);
+    }
+    hipError_t e = s->dtype == HEATKV_F32 ? heatkv::launch_paged_attend_f32(p, s->d, hip_stream)
+                   : many                 ? heatkv::launch_paged_attend_long(p, s->d, fp8, hip_stream)
+                                          : heatkv::launch_paged_attend_bf16(p, s->d, fp8, hip_stream);
+    return e == hipSuccess && l.join ? heatkv::launch_paged_join(p, s->dtype, s->d, many, hip_stream) : e;
+  };
+  hipError_t e = launch(plan.many, w.many, true);
+  if (e == hipSuccess) e = launch(plan.few, w.few, false);
   return launched(e, "paged_attend");
 }
 
@@ -275,8 +279,7 @@ int heatkv_paged_append(const heatkv_paged_shape* s, const int32_t* slots, int64
 size_t heatkv_paged_attend_workspace_bytes(const heatkv_paged_shape* s, int64_t tokens, int top) {
   if (check_shape(s) || check_tokens(tokens)) return 0;
   if (top < 0 || top > kMaxTop) return 0;
-  const auto split = splits_of(s, tokens, top);
-  return workspace_of(s, tokens, split).total;
+  return workspace_of(s, plan_of(s, tokens, top)).total;
 }
 
 int heatkv_paged_attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const void* k_pages, const void* v_pages,

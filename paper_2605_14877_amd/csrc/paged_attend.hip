@@ -1,10 +1,9 @@
 // Attention of new tokens over the paged cache, bf16 (cache rows bf16 or FP8 E4M3): few query rows per request, or a choice
 // of pages for each token.  paged_attend_long.hip: many rows over all pages; paged_attend_f32.hip: fp32.
 //
-// A workgroup takes 16 query rows (tokens x the queries that share a kv head) and a range of the keys; its four wavefronts
-// take the range's steps of 32 keys in turn, each with a running reference, row sums and accumulators of its own, merged
-// through LDS at the end.  Where a launch has few rows, several workgroups split a tile's keys and a second launch joins
-// their parts.
+// A workgroup takes its share of the launch (paged_schedule.h), segment by segment: 16 query rows (tokens x the queries that
+// share a kv head) and a range of their keys.  Its four wavefronts take the range's steps of 32 keys in turn, each with a
+// running reference, row sums and accumulators of its own, merged through LDS at the end of the segment.
 //
 // S^T = K Q^T with v_mfma_f32_16x16x32_bf16: K rows come from memory straight into the A operand (16 bytes per lane; the
 // elements of a row may be dealt to the MFMA steps in any order that Q follows, so 8-bit rows are read 16 codes a lane as
@@ -19,6 +18,7 @@
 #include "f32_mfma.h"
 #include "kernels.h"
 #include "paged.h"
+#include "paged_schedule.h"
 #include "paged_walk.h"
 
 namespace heatkv {
@@ -56,14 +56,17 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_kernel(AttendParams p
   char* const stage_all = paged_lds;                 // [WAVES] V stages, then the parked output tiles
   __shared__ float part_m[WAVES][16], part_l[WAVES][16];
 
+  __shared__ Scratch scratch;
+
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // Tile, kv head, split: the splits of a tile are far apart, its heads next to one another (one XCD per head).
-  const int per_split = p.tiles * p.c.H;
-  const int split = blockIdx.x / per_split, rest = blockIdx.x - split * per_split;
-  const int tile_no = rest / p.c.H, h = rest - tile_no * p.c.H;
-  const Tile tile = find_row_tile(p, tile_no, lane);
-  if (tile.rows <= 0) return;
+  const int w = blockIdx.x;
+  Place place = find_place<16, STEP>(p, w, scratch);
+  write_border(p, place, w);
+  Part part;
+  while (next_part<16, STEP>(p, place, part)) {
+  const Tile tile = tile_of<16>(p.c, part);
+  const int h = part.h;
 
   // This lane's query row.
   const int row = tile.row0 + min(n, tile.rows - 1);
@@ -75,10 +78,8 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_kernel(AttendParams p
 
   Walk<CHOSEN> walk(p, tile, h, j_first, j_last, limit_max, paged_lds + WAVES * stage_bytes(D), tid);
   const int steps = walk.steps();
-  const int size = split_size(steps, p.splits, LEAST_STEPS);
-  const int begin = split * size, end = min(steps, begin + size);
-  const bool alone = size >= steps;  // no other workgroup has a part of this tile
-  if (begin >= end && !(alone && split == 0)) return;
+  const int begin = steps_before(part.from, part.weight, steps), end = steps_before(part.to, part.weight, steps);
+  const bool alone = part.from == 0 && part.to == part.weight;  // no other workgroup has a part of this segment
 
   bf16x8 q[NK];
   {
@@ -246,10 +247,8 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_kernel(AttendParams p
     for (int w = 1; w < WAVES; ++w) ml = fmaxf(ml, part_m[w][tid]);
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) ll += part_l[w][tid] * fast_exp2((part_m[w][tid] - ml) * c);
-    const long long part = part_row(p, tile.b, tile.row0 + tid, h, tile.q0 + r, h * p.c.G + tile.row0 + tid - r * p.c.G);
-    if (split == 0 && p.splits > 1) p.parts[part] = (steps + size - 1) / size;
     if (!alone) {
-      float* to = p.part_ml + (split * p.part_rows + part) * 2;
+      float* to = p.part_ml + (part_rows<16>(w, part.from == 0) + tid) * 2;
       to[0] = ml;
       to[1] = ll;
     } else if (p.lse) {
@@ -268,7 +267,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_kernel(AttendParams p
     }
     const int jr = divide(tile.row0 + r, p.c.div_G), hr = h * p.c.G + tile.row0 + r - jr * p.c.G;
     if (!alone) {
-      float* to = p.part_o + (split * p.part_rows + part_row(p, tile.b, tile.row0 + r, h, tile.q0 + jr, hr)) * D + col;
+      float* to = p.part_o + (part_rows<16>(w, part.from == 0) + r) * D + col;
       *reinterpret_cast<f32x4*>(to) = x[0];
       *reinterpret_cast<f32x4*>(to + 4) = x[1];
     } else {
@@ -279,17 +278,17 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_kernel(AttendParams p
       *reinterpret_cast<bf16x8*>(to) = y;
     }
   }
+  __syncthreads();  // LDS is free for the next segment
+  }
 }
 
 template <int D, bool FP8, bool CHOSEN>
-hipError_t launch(AttendParams p, hipStream_t stream) {
-  p.tiles = p.short_requests ? p.c.batch * (LONG_ROWS / 16) : tile_count<16>(p.c.tokens, p.c.G, p.c.batch);
+hipError_t launch(const AttendParams& p, hipStream_t stream) {
   const size_t lds = WAVES * stage_bytes(D) + (CHOSEN ? walk_lds_bytes(p) : 0);
   static std::atomic<unsigned long long> allowed{0};
   if (lds > 64 * 1024)
     if (hipError_t e = allow_lds(reinterpret_cast<const void*>(&paged_attend_kernel<D, FP8, CHOSEN>), WALK_LDS, allowed)) return e;
-  hipLaunchKernelGGL((paged_attend_kernel<D, FP8, CHOSEN>), dim3(static_cast<unsigned>(p.tiles) * p.c.H * p.splits),
-                     dim3(64 * WAVES), lds, stream, p);
+  hipLaunchKernelGGL((paged_attend_kernel<D, FP8, CHOSEN>), dim3(p.grid), dim3(64 * WAVES), lds, stream, p);
   return hipGetLastError();
 }
 

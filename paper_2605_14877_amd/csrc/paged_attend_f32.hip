@@ -1,13 +1,14 @@
-// Attention of new tokens over the paged cache, fp32 (paged_attend.hip describes tiles, walks and splits; attend_f32.hip the
+// Attention of new tokens over the paged cache, fp32 (paged_attend.hip describes segments and walks; attend_f32.hip the
 // operands and the arithmetic: K through a wavefront's LDS stage, V straight into registers, 16x16x4 fp32 MFMAs).
 //
-// A workgroup takes 16 query rows; its four wavefronts take granules of 16 keys in turn.
+// A segment has 16 query rows; the workgroup's four wavefronts take granules of 16 keys in turn.
 // Bound: HBM for single tokens; the fp32 matrix instructions and the vector work that does not overlap with them otherwise.
 #include <hip/hip_runtime.h>
 
 #include "f32_mfma.h"
 #include "kernels.h"
 #include "paged.h"
+#include "paged_schedule.h"
 #include "paged_walk.h"
 
 namespace heatkv {
@@ -26,13 +27,17 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_f32_kernel(AttendPara
   static_assert(16 * PITCH * 4 == stage_bytes(D) && Stage::BYTES <= stage_bytes(D), "the parked tiles take the stages' place");
   __shared__ float part_m[WAVES][16], part_l[WAVES][16];
 
+  __shared__ Scratch scratch;
+
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int per_split = p.tiles * p.c.H;
-  const int split = blockIdx.x / per_split, rest = blockIdx.x - split * per_split;
-  const int tile_no = rest / p.c.H, h = rest - tile_no * p.c.H;
-  const Tile tile = find_tile<16>(p.c, tile_no, lane);
-  if (tile.rows <= 0) return;
+  const int w = blockIdx.x;
+  Place place = find_place<16, 2 * GRANULE>(p, w, scratch);
+  write_border(p, place, w);
+  Part part;
+  while (next_part<16, 2 * GRANULE>(p, place, part)) {
+  const Tile tile = tile_of<16>(p.c, part);
+  const int h = part.h;
 
   const int row = tile.row0 + min(n, tile.rows - 1);
   const int j = divide(row, p.c.div_G), hq = h * p.c.G + row - j * p.c.G;
@@ -42,10 +47,8 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_f32_kernel(AttendPara
 
   Walk<CHOSEN> walk(p, tile, h, j_first, j_last, limit_max, paged_f32_lds + WAVES * stage_bytes(D), tid);
   const int steps = walk.steps();
-  const int size = split_size(steps, p.splits, LEAST_STEPS);
-  const int begin = split * size, end = min(steps, begin + size);
-  const bool alone = size >= steps;
-  if (begin >= end && !(alone && split == 0)) return;
+  const int begin = steps_before(part.from, part.weight, steps), end = steps_before(part.to, part.weight, steps);
+  const bool alone = part.from == 0 && part.to == part.weight;
 
   f32m::Rows<D> q, k;
   {
@@ -141,9 +144,8 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_f32_kernel(AttendPara
     }
   if (wave == 0 && g == 0 && n < tile.rows) {
     const long long out_row = static_cast<long long>(tile.q0 + j) * p.c.Hq + hq;
-    if (split == 0 && p.splits > 1) p.parts[out_row] = (steps + size - 1) / size;
     if (!alone) {
-      float* to = p.part_ml + (split * p.part_rows + out_row) * 2;
+      float* to = p.part_ml + (part_rows<16>(w, part.from == 0) + n) * 2;
       to[0] = m_all;
       to[1] = l_all;
     } else if (p.lse) {
@@ -159,20 +161,20 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_f32_kernel(AttendPara
     const int jr = divide(tile.row0 + r, p.c.div_G), hr = h * p.c.G + tile.row0 + r - jr * p.c.G;
     float* to = alone ? static_cast<float*>(const_cast<void*>(p.out.data)) + (tile.q0 + jr) * p.out.token_stride +
                             hr * p.out.head_stride + col
-                      : p.part_o + (split * p.part_rows + static_cast<long long>(tile.q0 + jr) * p.c.Hq + hr) * D + col;
+                      : p.part_o + (part_rows<16>(w, part.from == 0) + r) * D + col;
     *reinterpret_cast<f32x4*>(to) = x;
+  }
+  __syncthreads();  // LDS is free for the next segment
   }
 }
 
 template <int D, bool CHOSEN>
-hipError_t launch(AttendParams p, hipStream_t stream) {
-  p.tiles = tile_count<16>(p.c.tokens, p.c.G, p.c.batch);
+hipError_t launch(const AttendParams& p, hipStream_t stream) {
   const size_t lds = WAVES * stage_bytes(D) + (CHOSEN ? walk_lds_bytes(p) : 0);
   static std::atomic<unsigned long long> allowed{0};
   if (lds > 64 * 1024)
     if (hipError_t e = allow_lds(reinterpret_cast<const void*>(&paged_attend_f32_kernel<D, CHOSEN>), WALK_LDS, allowed)) return e;
-  hipLaunchKernelGGL((paged_attend_f32_kernel<D, CHOSEN>), dim3(static_cast<unsigned>(p.tiles) * p.c.H * p.splits),
-                     dim3(64 * WAVES), lds, stream, p);
+  hipLaunchKernelGGL((paged_attend_f32_kernel<D, CHOSEN>), dim3(p.grid), dim3(64 * WAVES), lds, stream, p);
   return hipGetLastError();
 }
 

@@ -12,6 +12,7 @@
 
 #include "kernels.h"
 #include "paged.h"
+#include "paged_schedule.h"
 #include "paged_walk.h"
 #include "tile_lds.h"
 
@@ -22,7 +23,6 @@ namespace {
 using namespace paged;
 
 constexpr int BM = 128, BN = tile::ROWS;  // query rows of a workgroup, keys of a tile
-constexpr int LEAST_TILES = 4;            // of a workgroup, where a tile row's keys are split
 extern __shared__ __attribute__((aligned(1024))) char paged_long_lds[];
 
 __device__ __forceinline__ uint4 codes_to_chunk(unsigned lo, unsigned hi) {  // 8 E4M3 codes as bf16 (exact)
@@ -45,21 +45,21 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
   constexpr int CPL = BN * D / 16 / 256;            // 16-byte loads of a tile per lane (8-bit rows)
   char(*const lds)[2][TILE_BYTES] = reinterpret_cast<char(*)[2][TILE_BYTES]>(paged_long_lds);  // [stage][K, V]
 
+  __shared__ Scratch scratch;
+
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, hl = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // The last tiles first: with a causal limit they see the most keys.
-  const int per_split = p.tiles * p.c.H;
-  const int split = blockIdx.x / per_split, rest = blockIdx.x - split * per_split;
-  const int tile_no = p.tiles - 1 - rest / p.c.H, h = rest % p.c.H;
-  const Tile tl = find_tile<BM>(p.c, tile_no, lane);
-  if (tl.rows <= 0 || tl.n_new * p.c.G <= LONG_ROWS) return;
-
+  const int w = blockIdx.x;
+  Place place = find_place<BM, BN>(p, w, scratch);
+  write_border(p, place, w);
+  Part part;
+  while (next_part<BM, BN>(p, place, part)) {
+  const Tile tl = tile_of<BM>(p.c, part);
+  const int h = part.h;
   const int j_last = divide(tl.row0 + tl.rows - 1, p.c.div_G);
   const int steps = (visible_keys(p.c, tl, j_last) + BN - 1) / BN;
-  const int size = split_size(steps, p.splits, LEAST_TILES);
-  const int begin = split * size, end = min(steps, begin + size);
-  const bool alone = size >= steps;
-  if (begin >= end && !(alone && split == 0)) return;
+  const int begin = steps_before(part.from, part.weight, steps), end = steps_before(part.to, part.weight, steps);
+  const bool alone = part.from == 0 && part.to == part.weight;
 
   // Rows of this wavefront; one without rows still copies its share of the tiles.
   const int w_row = wave * 32;
@@ -246,22 +246,20 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
   if (it < end) step(it, std::integral_constant<int, 0>{});
 
   // Lane (n, hl) holds columns 32 i + 8 (r / 4) + 4 hl + r % 4 of query n.
-  if (!active) return;
   l = sum_halves(l);
+  if (real) {
   const long long out_row = static_cast<long long>(tl.q0 + j) * p.c.Hq + hq;
-  if (!real) return;
+  const long long part_row = part_rows<BM>(w, part.from == 0) + w_row + n;
   if (hl == 0) {
-    if (split == 0 && p.splits > 1) p.parts[out_row] = (steps + size - 1) / size;
     if (!alone) {
-      float* to = p.part_ml + (split * p.part_rows + out_row) * 2;
-      to[0] = m;
-      to[1] = l;
+      p.part_ml[part_row * 2] = m;
+      p.part_ml[part_row * 2 + 1] = l;
     } else if (p.lse) {
       p.lse[out_row] = natural_lse(m, l, p.sm_scale);
     }
   }
   if (!alone) {
-    float* to = p.part_o + (split * p.part_rows + out_row) * D + 4 * hl;
+    float* to = p.part_o + part_row * D + 4 * hl;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -281,13 +279,14 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
         *reinterpret_cast<bf16x4*>(to + 32 * i + 8 * r) = y;
       }
   }
+  }
+  __syncthreads();  // the stages are free for the next segment
+  }
 }
 
 template <int D, bool FP8>
-hipError_t launch(AttendParams p, hipStream_t stream) {
-  p.tiles = tile_count<BM>(p.c.tokens, p.c.G, p.c.batch);
-  hipLaunchKernelGGL((paged_attend_long_kernel<D, FP8>), dim3(static_cast<unsigned>(p.tiles) * p.c.H * p.splits), dim3(256),
-                     4 * BN * 2 * D, stream, p);
+hipError_t launch(const AttendParams& p, hipStream_t stream) {
+  hipLaunchKernelGGL((paged_attend_long_kernel<D, FP8>), dim3(p.grid), dim3(256), 4 * BN * 2 * D, stream, p);
   return hipGetLastError();
 }
 

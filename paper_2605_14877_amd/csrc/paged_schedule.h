@@ -1,0 +1,224 @@
+// How a launch's work is dealt to workgroups when the lengths are on the device.
+//
+// A segment is a tile of query rows of a request and kv head, and has a weight, about proportional to the keys that it walks
+// over.  All segments lie on one line: requests in order, of each the kv heads, of each the tiles.  Workgroup w takes the
+// stretch [w share, (w + 1) share) of it, so any mix of lengths is dealt evenly, with a grid that depends on nothing that the
+// host does not know.  A segment that crosses from one share into another is computed in parts (its steps in proportion to
+// the weight on either side), which a second launch joins in order; light segments are not cut, they belong to the
+// workgroup that they begin in.
+//
+// Where there are segments enough to fill the chip evenly as they come (whole_from), a workgroup takes one segment and
+// nothing is cut.
+//
+// Every workgroup finds its place by a scan over the requests (two rounds of loads, a block scan: about 2 us).
+#pragma once
+
+#include "paged.h"
+
+namespace heatkv {
+namespace paged {
+
+constexpr int STEP_WEIGHT = 32;  // of a step of KEYS keys; 2^25 steps at most: a weight is below 2^31
+
+// What a request adds to the line, for each kv head: `tiles` segments of weights w0 + t dw.
+struct Load {
+  int tiles, w0, dw;  // tiles 0: none of this launch's requests
+  __device__ __forceinline__ long long upto(int t) const {  // the first t segments
+    return static_cast<long long>(t) * w0 + static_cast<long long>(t) * (t - 1) / 2 * dw;
+  }
+  __device__ __forceinline__ long long weight(int t) const { return w0 + static_cast<long long>(t) * dw; }
+};
+template <int ROWS, int KEYS>
+__device__ __forceinline__ Load load_of(const AttendParams& p, int q0, int q1, int len) {
+  const Cache& c = p.c;
+  q0 = min(max(q0, 0), c.tokens);
+  const int n_new = min(max(q1, q0), c.tokens) - q0, rows = n_new * c.G;
+  Load l{0, STEP_WEIGHT, 0};
+  if (rows <= p.least_rows || rows > p.most_rows) return l;
+  l.tiles = (rows + ROWS - 1) / ROWS;
+  len = min(max(len, 0), c.max_pages << c.page_log2);
+  if (p.selected) {  // no more than a tile's tokens can have chosen between them
+    const int tokens = min(min(ROWS, (ROWS - 1) / c.G + 2), n_new);
+    len = min(len, tokens * p.top << c.page_log2);
+  } else if (c.causal) {  // the last row of a tile sees ROWS / G keys more than that of the tile before
+    l.dw = ROWS * STEP_WEIGHT / KEYS / c.G;
+    len = max(len - n_new + min(n_new, ROWS / c.G), 0);
+  }
+  l.w0 = max((len + KEYS - 1) / KEYS, 1) * STEP_WEIGHT;
+  return l;
+}
+
+// A number that all lanes have, in scalar registers.
+__device__ __forceinline__ long long uniform(long long x) {
+  const int lo = __builtin_amdgcn_readfirstlane(static_cast<int>(x)), hi = __builtin_amdgcn_readfirstlane(static_cast<int>(x >> 32));
+  return static_cast<long long>(hi) << 32 | static_cast<unsigned>(lo);
+}
+
+struct Place {
+  long long pos, stop, share;  // on the line; pos >= stop: nothing (more) to do
+  int b, h, t;                 // the segment at pos
+  long long off;               // pos in it
+  Load load;                   // of request b
+  bool whole;                  // one segment per workgroup: pos counts segments
+};
+struct Scratch {  // LDS
+  long long weights[4], counts[4], first;
+  int b;
+};
+
+template <int ROWS, int KEYS>
+__device__ __forceinline__ Load request_load(const AttendParams& p, int b) {
+  return load_of<ROWS, KEYS>(p, uniform_load(p.c.q_start, b), uniform_load(p.c.q_start, b + 1), uniform_load(p.c.lens, b));
+}
+
+// The place of workgroup w, by all of its 256 lanes.
+template <int ROWS, int KEYS>
+__device__ __forceinline__ Place find_place(const AttendParams& p, int w, Scratch& scratch) {
+  const Cache& c = p.c;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int per = (c.batch + 255) / 256;
+  auto load = [&](int b) { return load_of<ROWS, KEYS>(p, c.q_start[b], c.q_start[b + 1], c.lens[b]); };
+  long long weight = 0, count = 0;  // of this lane's requests, then up to and with them
+  for (int i = 0; i < per; ++i)
+    if (tid * per + i < c.batch) {
+      const Load l = load(tid * per + i);
+      weight += l.upto(l.tiles) * c.H;
+      count += static_cast<long long>(l.tiles) * c.H;
+    }
+  const long long my_weight = weight, my_count = count;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const long long u = __shfl_up(weight, d, 64), v = __shfl_up(count, d, 64);
+    if (lane >= d) {
+      weight += u;
+      count += v;
+    }
+  }
+  if (lane == 63) {
+    scratch.weights[tid >> 6] = weight;
+    scratch.counts[tid >> 6] = count;
+  }
+  __syncthreads();
+  long long total = 0, segments = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i < (tid >> 6)) {
+      weight += scratch.weights[i];
+      count += scratch.counts[i];
+    }
+    total += scratch.weights[i];
+    segments += scratch.counts[i];
+  }
+  total = uniform(total);
+  segments = uniform(segments);
+  Place at{};
+  at.whole = segments >= p.whole_from;
+  at.share = at.whole ? 1 : max((total + p.workgroups - 1) / p.workgroups, static_cast<long long>(p.least_weight));
+  at.pos = w * at.share;
+  at.stop = at.whole ? min(at.pos + 1, segments) : w < p.workgroups ? min(at.pos + at.share, total) : at.pos;
+  if (at.pos >= at.stop) return at;
+  const long long upto = at.whole ? count : weight, mine = at.whole ? my_count : my_weight;
+  if (at.pos < upto && at.pos >= upto - mine) {  // one lane
+    long long first = upto - mine;
+    for (int i = 0; i < per; ++i) {
+      const int b = tid * per + i;
+      const Load l = b < c.batch ? load(b) : Load{0, 0, 0};
+      const long long n = (at.whole ? l.tiles : l.upto(l.tiles)) * c.H;
+      if (at.pos < first + n) {
+        scratch.first = first;
+        scratch.b = b;
+        break;
+      }
+      first += n;
+    }
+  }
+  __syncthreads();
+  at.b = __builtin_amdgcn_readfirstlane(scratch.b);
+  const long long rel = at.pos - uniform(scratch.first);
+  at.load = request_load<ROWS, KEYS>(p, at.b);
+  if (at.whole) {  // the last tiles first: with a causal limit they are the heaviest
+    const int i = static_cast<int>(rel / c.H);
+    at.h = static_cast<int>(rel - static_cast<long long>(i) * c.H);
+    at.t = at.load.tiles - 1 - i;
+    return at;
+  }
+  const long long per_head = at.load.upto(at.load.tiles);
+  at.h = static_cast<int>(rel / per_head);
+  const long long in_head = rel - at.h * per_head;
+  int below = 0, above = at.load.tiles;  // the last tile that begins at in_head or before
+  while (above - below > 1) {
+    const int mid = (below + above) >> 1;
+    (at.load.upto(mid) <= in_head ? below : above) = mid;
+  }
+  at.t = below;
+  at.off = in_head - at.load.upto(below);
+  return at;
+}
+
+// The part of the segment at pos that is this workgroup's; advances the place behind it.
+struct Part {
+  int b, h, t;
+  long long from, to, weight;  // of the segment's weight; the whole segment: from == 0, to == weight
+};
+template <int ROWS, int KEYS>
+__device__ __forceinline__ bool next_part(const AttendParams& p, Place& at, Part& part) {
+  if (at.whole) {
+    part = {at.b, at.h, at.t, 0, 1, 1};
+    return at.pos++ < at.stop;
+  }
+  while (at.pos < at.stop) {
+    const long long weight = at.load.weight(at.t);
+    part = {at.b, at.h, at.t, at.off, min(weight, at.off + (at.stop - at.pos)), weight};
+    if (weight <= p.least_weight) part.to = weight;
+    at.pos += part.to - part.from;
+    at.off = 0;
+    if (part.to == weight && ++at.t == at.load.tiles) {
+      at.t = 0;
+      if (++at.h == p.c.H && at.pos < at.stop) {  // there is another request with a load
+        at.h = 0;
+        do {
+          at.load = request_load<ROWS, KEYS>(p, ++at.b);
+        } while (at.load.tiles == 0 && at.b + 1 < p.c.batch);
+      }
+    }
+    if (weight > p.least_weight || part.from == 0) return true;
+  }
+  return false;
+}
+
+// What the join has to know about the border between shares w - 1 and w: written by workgroup w, before its first part.
+// parts 0: no segment is cut there, or it was cut at an earlier border already.
+__device__ __forceinline__ void write_border(const AttendParams& p, const Place& at, int w) {
+  if (!p.borders || threadIdx.x != 0 || w >= p.workgroups) return;
+  Border x{at.b, at.h, at.t, 0};
+  if (!at.whole && at.pos < at.stop && at.off > 0 && at.off <= at.share) {
+    const long long weight = at.load.weight(at.t);
+    if (weight > p.least_weight) x.parts = 1 + static_cast<int>((weight - at.off + at.share - 1) / at.share);
+  }
+  p.borders[w] = x;
+}
+
+// Steps of a part, of the `steps` that the segment turned out to take.
+__device__ __forceinline__ int steps_before(long long weight_before, long long weight, int steps) {
+  return static_cast<int>(weight_before * steps / weight);
+}
+
+// Where a workgroup puts its parts: 0 a segment that began in an earlier share, 1 one that begins in its share and goes on
+// behind it; ROWS rows each.
+template <int ROWS>
+__device__ __forceinline__ long long part_rows(int w, bool begins) {
+  return (static_cast<long long>(w) * 2 + (begins ? 1 : 0)) * ROWS;
+}
+
+template <int ROWS>
+__device__ __forceinline__ Tile tile_of(const Cache& c, const Part& part) {
+  Tile t;
+  t.b = part.b;
+  fill_tile(c, t);
+  t.row0 = part.t * ROWS;
+  t.rows = min(t.n_new * c.G - t.row0, ROWS);
+  return t;
+}
+
+}  // namespace paged
+}  // namespace heatkv

@@ -10,7 +10,6 @@
 namespace heatkv {
 namespace paged {
 
-constexpr int LEAST_STEPS = 8;       // of a workgroup: two for each of its wavefronts
 constexpr int MAX_TOP = 512;
 constexpr size_t WALK_LDS = 144 * 1024;
 

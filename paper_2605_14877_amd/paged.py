@@ -1,7 +1,10 @@
 """Binding of the paged cache's calls (include/heatkv.h, "Paged cache"): same names, argument marshalling and checks only.
 
 Token tensors are [tokens, heads, d] with any token and head stride; pages [num_pages, kv_heads, page_size, d] in the shape's
-dtype, or E4M3 codes as torch.float8_e4m3fn or torch.uint8.  Integer arrays are int32 device tensors."""
+dtype, or E4M3 codes as torch.float8_e4m3fn or torch.uint8.  Integer arrays are int32 device tensors.
+
+Calls go through the module _heatkv_call first (csrc/call_path.cpp: the same checks without the interpreter); it declines
+whatever is not plainly in order, and the ctypes path below it names the mistake."""
 from __future__ import annotations
 
 import ctypes as C
@@ -59,9 +62,25 @@ class PagedShape:
                                      self.num_pages, self.batch, self.max_pages)
         self.pages_shape = (self.num_pages, self.kv_heads, self.page_size, self.d)
 
+        self.address = C.addressof(self.c_struct)
+
     @property
     def ref(self):
         return C.byref(self.c_struct)
+
+
+def _native(name, shape, *args):
+    """True if the module _heatkv_call has made the call; it declines whatever is not plainly in order."""
+    if type(shape) is not PagedShape:
+        return False
+    if binding._call is None:
+        lib()
+    rc = getattr(binding._call, name)(shape.address, *args)
+    if rc is None:
+        return False
+    if rc:
+        _check(rc)
+    return True
 
 
 class _Call:
@@ -146,6 +165,9 @@ def _no_alias(x, name, others):
 def heatkv_paged_assign(shape, keep, new_tokens, lens, free_ring, free_span, table, q_start, slots, status, lens_out=None,
                         free_span_out=None, stream=None):
     """One step of the page allocator.  lens_out, free_span_out: None for in place."""
+    if _native("paged_assign", shape, keep, new_tokens, lens, free_ring, free_span, table, q_start, slots, status, lens_out,
+               free_span_out, stream):
+        return
     c, sh = _Call(shape), shape
     lens_out = lens if lens_out is None else lens_out
     free_span_out = free_span if free_span_out is None else free_span_out
@@ -162,6 +184,8 @@ def heatkv_paged_assign(shape, keep, new_tokens, lens, free_ring, free_span, tab
 
 def heatkv_paged_append(shape, slots, k_new, v_new, k_pages, v_pages, bounds=None, bound_scales=None, stream=None):
     """The new tokens' rows into their slots; with bounds and bound_scales also the bounds of the pages that they touch."""
+    if _native("paged_append", shape, slots, k_new, v_new, k_pages, v_pages, bounds, bound_scales, stream):
+        return
     c, sh = _Call(shape), shape
     c.dense(slots, "slots", (c.torch.int32,))
     if slots.dim() != 1:
@@ -201,6 +225,8 @@ def _attend_operands(c, q, k_pages, v_pages, table, q_start, lens, out, ws, lse)
 def heatkv_paged_attend(shape, q, k_pages, v_pages, table, q_start, lens, sm_scale, out, ws=None, causal=True, lse=None,
                         stream=None):
     """Attention of the new tokens over all tokens of their requests, or (causal) those up to themselves."""
+    if _native("paged_attend", shape, q, k_pages, v_pages, table, q_start, lens, None, sm_scale, out, ws, causal, lse, stream):
+        return
     c = _Call(shape)
     operands, outr, lp, wp, n = _attend_operands(c, q, k_pages, v_pages, table, q_start, lens, out, ws, lse)
     _check(c.lib.heatkv_paged_attend(shape.ref, *operands, float(sm_scale), int(bool(causal)), outr, lp, wp, n, c.stream(stream)))
@@ -209,6 +235,8 @@ def heatkv_paged_attend(shape, q, k_pages, v_pages, table, q_start, lens, sm_sca
 def heatkv_paged_select(shape, q, bounds, bound_scales, table, q_start, lens, first, last, selected, causal=True, stream=None):
     """The pages with the best scores for every new token and kv head, ascending, -1 behind the last; their number is
     selected's last dimension."""
+    if _native("paged_select", shape, q, bounds, bound_scales, table, q_start, lens, first, last, selected, causal, stream):
+        return
     c, sh = _Call(shape), shape
     qr = c.rows(q, "q", None, sh.q_heads)
     tokens = q.shape[0]
@@ -224,6 +252,9 @@ def heatkv_paged_select(shape, q, bounds, bound_scales, table, q_start, lens, fi
 def heatkv_paged_attend_selected(shape, q, k_pages, v_pages, table, q_start, lens, selected, sm_scale, out, ws=None,
                                  causal=True, lse=None, stream=None):
     """heatkv_paged_attend over the pages selected [tokens, kv_heads, top] of each token only."""
+    if selected is not None and _native("paged_attend", shape, q, k_pages, v_pages, table, q_start, lens, selected, sm_scale, out,
+                                        ws, causal, lse, stream):
+        return
     c, sh = _Call(shape), shape
     operands, outr, lp, wp, n = _attend_operands(c, q, k_pages, v_pages, table, q_start, lens, out, ws, lse)
     top = selected.shape[-1] if isinstance(selected, c.torch.Tensor) and selected.dim() == 3 else 0
