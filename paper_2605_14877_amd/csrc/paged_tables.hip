@@ -5,9 +5,11 @@
 // the ring, requests in order; pages that it no longer needs go behind the ring's tail, requests in order.  What is given
 // back in a step is taken again in a later one at the earliest, so taking and giving never touch the same ring entry.
 //
-// Bound: latency, a chain of memory round trips (lengths; ring entries; table) and two block scans.  One workgroup does the
-// request part; the slots come in the same launch where they are few, otherwise from a second one with a workgroup or
-// more per request (a request's slots then need no search).
+// Bound: latency, a chain of memory round trips (lengths; ring or table entries) and a block scan.  Small steps are one
+// workgroup.  In larger ones every workgroup makes the scan for itself and moves its share of pages and slots; as lens_out
+// and span_out may be lens and span, which all of them read, these are written by a second launch, which scans once more.
+// 1024 requests, 25000 pages back, 50000 slots: 14 us; by one workgroup and a second launch for the slots 39 us (one compute
+// unit: 24 us of it for the pages, whether its lanes searched for the request of a page or its wavefronts took requests).
 #include <hip/hip_runtime.h>
 
 #include "kernels.h"
@@ -41,8 +43,11 @@ __device__ __forceinline__ int find(const int* first, int n, int x) {
   return lo;
 }
 
-__global__ __launch_bounds__(LANES) void paged_assign_kernel(AssignArgs p, int slots_here) {
-  __shared__ int take0[MAX_BATCH], give0[MAX_BATCH], q0[MAX_BATCH + 1];  // of every request: sums over those before it
+// MOVE: pages, slots, q_start and status, shared by the grid's workgroups.  COMMIT: lens_out and span_out, by workgroup 0,
+// which is the only one if there is MOVE as well.
+template <bool MOVE, bool COMMIT>
+__global__ __launch_bounds__(LANES) void paged_assign_kernel(AssignArgs p) {
+  __shared__ int take0[MOVE ? MAX_BATCH : 1], give0[MOVE ? MAX_BATCH : 1], q0[MOVE ? MAX_BATCH : 1];  // sums over the requests before
   __shared__ long long part[3][LANES / 64];
   __shared__ int any_bad;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -90,9 +95,11 @@ __global__ __launch_bounds__(LANES) void paged_assign_kernel(AssignArgs p, int s
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < 3; ++k)
+#pragma unroll
     for (int w = 0; w < LANES / 64; ++w) {
-      if (w < wave) before[k] += part[k][w];
-      all[k] += part[k][w];
+      const long long x = part[k][w];
+      if (w < wave) before[k] += x;
+      all[k] += x;
     }
   int status = HEATKV_PAGED_OK;
   if (any_bad)
@@ -104,86 +111,88 @@ __global__ __launch_bounds__(LANES) void paged_assign_kernel(AssignArgs p, int s
   else if (all[0] > count)
     status = HEATKV_PAGED_NO_PAGES;
   const bool ok = status == HEATKV_PAGED_OK;
+  const int takes = ok ? static_cast<int>(all[0]) : 0, gives = ok ? static_cast<int>(all[1]) : 0;
+  const int tokens = ok ? static_cast<int>(all[2]) : 0;
+  const bool first_group = blockIdx.x == 0;
 
-  // From here on nothing that a request's part reads is written by another one: lens_out may be lens, span_out span
-  // (both have been read by every lane in front of the barrier above).
+  // Where this workgroup is the only one, it has read lens and span to the end (the barrier above): they may be the outputs.
 #pragma unroll
   for (int i = 0; i < PER_LANE; ++i) {
     const int b = tid * per + i;
     if (i < per && b < B) {
-      take0[b] = static_cast<int>(before[0]);
-      give0[b] = static_cast<int>(before[1]);
-      q0[b] = ok ? static_cast<int>(before[2]) : 0;
-      p.q_start[b] = q0[b];
-      if (ok) {
-        p.lens_out[b] = keep[i] + come[i];
-      } else if (p.lens_out != p.lens) {
-        p.lens_out[b] = p.lens[b];
+      if constexpr (MOVE) {
+        take0[b] = static_cast<int>(before[0]);
+        give0[b] = static_cast<int>(before[1]);
+        q0[b] = static_cast<int>(before[2]);
+        if (first_group) p.q_start[b] = ok ? static_cast<int>(before[2]) : 0;
+        before[0] += max(want(i) - held(i), 0);
+        before[1] += max(held(i) - want(i), 0);
+        before[2] += come[i];
       }
-      before[0] += max(want(i) - held(i), 0);
-      before[1] += max(held(i) - want(i), 0);
-      before[2] += come[i];
+      if constexpr (COMMIT) {
+        if (ok)
+          p.lens_out[b] = keep[i] + come[i];
+        else if (p.lens_out != p.lens)
+          p.lens_out[b] = p.lens[b];
+      }
     }
   }
-  const int tokens = ok ? static_cast<int>(all[2]) : 0;
-  if (tid == 0) {
-    q0[B] = tokens;
-    p.q_start[B] = tokens;
-    p.status[0] = status;
-    p.span_out[0] = ok ? static_cast<int>((head + all[0]) % R) : head;
-    p.span_out[1] = ok ? static_cast<int>(count - all[0] + all[1]) : count;
+  if (tid == 0 && first_group) {
+    if constexpr (MOVE) {
+      p.q_start[B] = tokens;
+      p.status[0] = status;
+    }
+    if constexpr (COMMIT) {
+      const int next = head + takes;  // both below 2^26
+      p.span_out[0] = ok ? next < R ? next : next - R : head;
+      p.span_out[1] = ok ? count - takes + gives : count;
+    }
   }
+  if constexpr (!MOVE) return;
   __syncthreads();
-  // Lengths of other lanes' requests, below: from keep and new_tokens, which nothing writes, and from the sums.
-  if (ok) {
-    const int takes = static_cast<int>(all[0]), gives = static_cast<int>(all[1]);
-    auto pages_wanted = [&](int b) { return (p.keep[b] + p.new_tokens[b] + page - 1) >> lp; };
-    for (int i = tid; i < takes; i += LANES) {
-      const int b = find(take0, B, i);
-      const int n = (b + 1 < B ? take0[b + 1] : takes) - take0[b];  // that the request takes: its last n pages
-      const int entry = p.ring[(head + i) % R];
-      p.table[static_cast<long long>(b) * p.max_pages + pages_wanted(b) - n + (i - take0[b])] = entry;
-    }
-    const long long tail = static_cast<long long>(head) + count;
-    for (int i = tid; i < gives; i += LANES) {
-      const int b = find(give0, B, i);
-      p.ring[(tail + i) % R] = p.table[static_cast<long long>(b) * p.max_pages + pages_wanted(b) + (i - give0[b])];
-    }
+
+  // Requests other than the lane's own, below: from keep and new_tokens, which nothing writes, and from the sums.
+  const int at = blockIdx.x * LANES + tid, stride = gridDim.x * LANES;
+  auto wanted = [&](int b) { return (p.keep[b] + p.new_tokens[b] + page - 1) >> lp; };
+  auto row = [&](int b) { return p.table + static_cast<long long>(b) * p.max_pages; };
+  auto taken = [&](int i) { return p.ring[head + i < R ? head + i : head + i - R]; };
+  auto takes_of = [&](int b) { return (b + 1 < B ? take0[b + 1] : takes) - take0[b]; };
+  for (int i = at; i < takes; i += stride) {
+    const int b = find(take0, B, i);
+    row(b)[wanted(b) - takes_of(b) + i - take0[b]] = taken(i);  // the last pages of the request
   }
-  if (!slots_here) return;
-  __syncthreads();  // the table entries written above, by this workgroup
-  for (int t = tid; t < p.max_tokens; t += LANES) {
+  const unsigned tail = static_cast<unsigned>(head) + count;  // below 2 R, i below R
+  for (int i = at; i < gives; i += stride) {
+    const int b = find(give0, B, i);
+    unsigned to = tail + i;
+    to -= to >= static_cast<unsigned>(R) ? R : 0;
+    to -= to >= static_cast<unsigned>(R) ? R : 0;
+    p.ring[to] = row(b)[wanted(b) + i - give0[b]];
+  }
+  for (int t = at; t < p.max_tokens; t += stride) {
     int slot = -1;
     if (t < tokens) {
       const int b = find(q0, B, t);
-      const int x = p.keep[b] + t - q0[b];
-      slot = (p.table[static_cast<long long>(b) * p.max_pages + (x >> lp)] << lp) + (x & (page - 1));
+      const int x = p.keep[b] + t - q0[b], i = x >> lp, n = takes_of(b), old = wanted(b) - n;
+      // the table's new entries may be another workgroup's to write
+      const int entry = n > 0 && i >= old ? taken(take0[b] + i - old) : row(b)[i];
+      slot = (entry << lp) + (x & (page - 1));
     }
     p.slots[t] = slot;
-  }
-}
-
-// Slots of request blockIdx.x's new tokens; blockIdx.x = batch: of the tokens that belong to no request.
-__global__ __launch_bounds__(256) void paged_slots_kernel(AssignArgs p) {
-  const int b = blockIdx.x, lp = p.page_log2, first = p.q_start[b];
-  const int stop = b < p.batch ? p.q_start[b + 1] : static_cast<int>(p.max_tokens);
-  const int keep = b < p.batch ? p.keep[b] : 0;
-  for (int t = first + blockIdx.y * 256 + threadIdx.x; t < stop; t += gridDim.y * 256) {
-    const int x = keep + t - first;
-    p.slots[t] = b < p.batch ? (p.table[static_cast<long long>(b) * p.max_pages + (x >> lp)] << lp) + (x & ((1 << lp) - 1)) : -1;
   }
 }
 
 }  // namespace
 
 hipError_t launch_paged_assign(const AssignArgs& a, hipStream_t stream) {
-  const bool slots_here = a.max_tokens <= 4 * LANES;
-  hipLaunchKernelGGL(paged_assign_kernel, dim3(1), dim3(LANES), 0, stream, a, slots_here ? 1 : 0);
+  if (a.max_tokens <= 2 * LANES && a.batch <= 128) {
+    hipLaunchKernelGGL((paged_assign_kernel<true, true>), dim3(1), dim3(LANES), 0, stream, a);
+    return hipGetLastError();
+  }
+  const unsigned groups = static_cast<unsigned>(std::min<long long>((a.max_tokens + LANES - 1) / LANES + a.batch / 32, 128));
+  hipLaunchKernelGGL((paged_assign_kernel<true, false>), dim3(groups), dim3(LANES), 0, stream, a);
   if (hipError_t e = hipGetLastError()) return e;
-  if (slots_here) return hipSuccess;
-  // workgroups enough to fill the chip however the tokens are spread over the requests
-  const unsigned parts = static_cast<unsigned>(std::min<long long>((a.max_tokens + 255) / 256, std::max(1, 4096 / (a.batch + 1))));
-  hipLaunchKernelGGL(paged_slots_kernel, dim3(a.batch + 1, parts), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL((paged_assign_kernel<false, true>), dim3(1), dim3(LANES), 0, stream, a);
   return hipGetLastError();
 }
 
