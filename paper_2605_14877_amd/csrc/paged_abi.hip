@@ -44,6 +44,8 @@ int check_shape(const heatkv_paged_shape* s) {
   if (s->batch < 1 || s->batch > heatkv::paged::MAX_BATCH) return fail(HEATKV_EINVAL, "batch must be in [1, 4096]");
   if (s->num_pages < 1 || int64_t(s->num_pages) * s->page_size > kMaxPositions)
     return fail(HEATKV_EINVAL, "num_pages must be >= 1, and num_pages * page_size at most 2^30");
+  if (int64_t(s->num_pages) * s->page_size * s->kv_heads > int64_t(1) << 34)
+    return fail(HEATKV_EINVAL, "num_pages * page_size * kv_heads must be at most 2^34");
   if (s->max_pages < 1 || int64_t(s->max_pages) * s->page_size > kMaxPositions)
     return fail(HEATKV_EINVAL, "max_pages must be >= 1, and max_pages * page_size at most 2^30");
   return HEATKV_OK;

@@ -37,6 +37,29 @@ __device__ __forceinline__ uint4 codes_to_chunk(unsigned lo, unsigned hi) {  // 
   return o.u;
 }
 
+// Where the four granules of a tile lie, in granules of the cache (there are less than 2^31, check_shape()).
+struct TileRows {
+  int granule[4];
+};
+
+__device__ __forceinline__ const __attribute__((address_space(3))) char* lds_pointer(int at) {
+  return (const __attribute__((address_space(3))) char*)static_cast<size_t>(static_cast<unsigned>(at));
+}
+
+struct Shared {
+  Scratch scratch;
+  Place place;
+  Part next;
+  int more;
+};
+
+// The launch's arguments, loaded anew.
+__device__ __forceinline__ const AttendParams& arguments() {
+  auto* at = (const __attribute__((address_space(4))) AttendParams*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("; arguments" : "+s"(at));
+  return *(const AttendParams*)at;
+}
+
 template <int D, bool FP8>
 __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams p) {
   constexpr int RB = 2 * D, TILE_BYTES = BN * RB, SRC = FP8 ? D : RB;
@@ -44,249 +67,431 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
   constexpr int CPT = TILE_BYTES / 4096;            // copies of a tile per wavefront (bf16 rows)
   constexpr int CPL = BN * D / 16 / 256;            // 16-byte loads of a tile per lane (8-bit rows)
   char(*const lds)[2][TILE_BYTES] = reinterpret_cast<char(*)[2][TILE_BYTES]>(paged_long_lds);  // [stage][K, V]
-
-  __shared__ Scratch scratch;
+  // Behind the stages, which then begin at LDS address 0: all of their offsets fit into the read instructions.
+  Shared& shared = *reinterpret_cast<Shared*>(paged_long_lds + 4 * TILE_BYTES);
 
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, hl = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int w = blockIdx.x;
-  Place place = find_place<BM, BN>(p, w, scratch);
-  write_border(p, place, w);
-  Part part;
-  while (next_part<BM, BN>(p, place, part)) {
-  const Tile tl = tile_of<BM>(p.c, part);
-  const int h = part.h;
-  const int j_last = divide(tl.row0 + tl.rows - 1, p.c.div_G);
-  const int steps = (visible_keys(p.c, tl, j_last) + BN - 1) / BN;
-  const int begin = steps_before(part.from, part.weight, steps), end = steps_before(part.to, part.weight, steps);
-  const bool alone = part.from == 0 && part.to == part.weight;
-
-  // Rows of this wavefront; one without rows still copies its share of the tiles.
-  const int w_row = wave * 32;
-  const bool active = w_row < tl.rows;
-  const int row = tl.row0 + min(w_row + n, tl.rows - 1);
-  const int j = divide(row, p.c.div_G), hq = h * p.c.G + row - j * p.c.G;
-  const bool real = w_row + n < tl.rows;
-  const int limit = real ? visible_keys(p.c, tl, j) : 0;
-  const int limit_min = w_row + 32 <= tl.rows ? visible_keys(p.c, tl, divide(tl.row0 + w_row, p.c.div_G)) : 0;
-  const int limit_max = active ? visible_keys(p.c, tl, divide(tl.row0 + min(w_row + 31, tl.rows - 1), p.c.div_G)) : 0;
-
-  bf16x8 qreg[NK];
-  {
-    const bf16_t* from = static_cast<const bf16_t*>(p.q.data) + (tl.q0 + j) * p.q.token_stride + hq * p.q.head_stride + 8 * hl;
-#pragma unroll
-    for (int ks = 0; ks < NK; ++ks) qreg[ks] = *reinterpret_cast<const bf16x8*>(from + 16 * ks);
-  }
-
-  const long long table = static_cast<long long>(tl.b) * p.c.max_pages;
-  const char* const k_pages = static_cast<const char*>(p.k_pages);
-  const char* const v_pages = static_cast<const char*>(p.v_pages);
-  // Byte offset of the cache row at position x (a multiple of 16 below the request's end).
-  auto row_at = [&](int x) {
-    return (page_row(p.c, uniform_load(p.c.table, table + (x >> p.c.page_log2)), h) + (x & ((1 << p.c.page_log2) - 1))) * SRC;
-  };
-
-  const int ld_off_k = tile::loader_off_k<RB>(wave, lane), ld_off_v = tile::loader_off_v<RB>(wave, lane);
   const unsigned lds_base = static_cast<unsigned>(reinterpret_cast<unsigned long long>(
       (__attribute__((address_space(3))) char*)(paged_long_lds)));
   const unsigned lds_wave = __builtin_amdgcn_readfirstlane(lds_base + wave * 1024);
-  // bf16 rows: this wavefront's copies of tile `it` into a stage.  Copy i covers rows (64 / CPT) i + (16 / CPT) wave of the
-  // tile and on, all of one granule.
-  auto copy_tile = [&](int it, auto buf_tag) {
-    constexpr int buf = decltype(buf_tag)::value;
-    constexpr int PER = 64 / CPT;  // rows between copies of a wavefront
-#pragma unroll
-    for (int i = 0; i < CPT; ++i) {
-      const int ahead = PER == 32 ? 16 * (wave >> 1) : 0;  // rows of the lane offset that belong to the granule's place
-      const int x = it * BN + PER * i + ahead;
-      const int left = tl.len - x;
-      const long long at = (left > 0 ? row_at(x) : 0) - ahead * RB;
-      const int rows = left > 0 ? left + ahead : 0;
-      tile::copy_1k_checked(lds_wave, buf * (2 * TILE_BYTES) + 4096 * i, ld_off_k, tile::tile_descriptor<RB>(k_pages + at, rows), 0);
-      tile::copy_1k_checked(lds_wave, buf * (2 * TILE_BYTES) + TILE_BYTES + 4096 * i, ld_off_v,
-                            tile::tile_descriptor<RB>(v_pages + at, rows), 0);
-    }
-  };
-  // 8-bit rows: load i of a lane is 16 codes of one row.
-  constexpr int LPR = D / 16;  // lanes per row
-  uint4 raw_k[CPL], raw_v[CPL];
-  auto load_codes = [&](int it) {
-#pragma unroll
-    for (int i = 0; i < CPL; ++i) {
-      const int r = (tid + 256 * i) / LPR;
-      const int gr = __builtin_amdgcn_readfirstlane(r / 16);  // a wavefront's 64 / LPR rows are in one granule
-      const int x = it * BN + 16 * gr;
-      raw_k[i] = raw_v[i] = make_uint4(0, 0, 0, 0);
-      if (x < tl.len) {
-        const long long at = row_at(x) + (r % 16) * SRC + (tid % LPR) * 16;
-        if (x + r % 16 < tl.len) {
-          raw_k[i] = ldg16(k_pages + at);
-          raw_v[i] = ldg16(v_pages + at);
-        }
-      }
-    }
-  };
-  auto store_codes = [&](int buf) {
-#pragma unroll
-    for (int i = 0; i < CPL; ++i) {
-      const int r = (tid + 256 * i) / LPR, chunk = 2 * (tid % LPR);
-      const int sk = tile::swizzle_k<RB>(r & 15), sv = tile::swizzle_v<RB>(r & 15);
-      char* kt = lds[buf][0] + r * RB;
-      char* vt = lds[buf][1] + r * RB;
-      *reinterpret_cast<uint4*>(kt + ((chunk ^ sk) << 4)) = codes_to_chunk(raw_k[i].x, raw_k[i].y);
-      *reinterpret_cast<uint4*>(kt + (((chunk + 1) ^ sk) << 4)) = codes_to_chunk(raw_k[i].z, raw_k[i].w);
-      *reinterpret_cast<uint4*>(vt + ((chunk ^ sv) << 4)) = codes_to_chunk(raw_v[i].x, raw_v[i].y);
-      *reinterpret_cast<uint4*>(vt + (((chunk + 1) ^ sv) << 4)) = codes_to_chunk(raw_v[i].z, raw_v[i].w);
-    }
-  };
+  const int ld_off_k = tile::loader_off_k<RB>(wave, lane), ld_off_v = tile::loader_off_v<RB>(wave, lane);
+  // Reader offsets as LDS addresses: stage, tile and row of a read are then constants of the instruction.
   int k_off[NK], v_off[NV];
   tile::reader_off_k<RB>(lane, k_off);
   tile::reader_off_v<RB>(lane, v_off);
-
-  f32x16 o[NV];
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
+  for (int i = 0; i < NK; ++i) k_off[i] += lds_base;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+  for (int i = 0; i < NV; ++i) v_off[i] += lds_base;
+  const char* const k_pages = static_cast<const char*>(p.k_pages);
+  const char* const v_pages = static_cast<const char*>(p.v_pages);
   const float c = p.sm_scale * kLog2e;
-  float m = lowest_reference(c), l = 0.f;
-  constexpr float kSlack = 8.f;  // attend.hip
+  constexpr float kSlack = 8.f;  // the reference is raised by more than this only: attend.hip
   const float slack = kSlack / c;
 
-  auto math = [&](int it, auto buf_tag) {
-    constexpr int buf = decltype(buf_tag)::value;
-    const char* kt = lds[buf][0];
-    const char* vt = lds[buf][1];
-    f32x16 s[2];
-#pragma unroll
-    for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[cb][r] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < NK; ++ks)
-#pragma unroll
-      for (int cb = 0; cb < 2; ++cb) {
-        const bf16x8 a = *reinterpret_cast<const bf16x8*>(kt + cb * 32 * RB + k_off[ks]);
-        s[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qreg[ks], s[cb], 0, 0, 0);
-      }
-    if (it * BN + BN > limit_min) tile::mask_rows(limit - it * BN, hl, s);
-    float mx = s[0][0];
-#pragma unroll
-    for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[cb][r]);
-    mx = max_halves(mx);
-    if (__any(mx > m + slack)) {
-      const float m_new = fmaxf(m, mx);
-      const float alpha = fast_exp2((m - m_new) * c);
-      m = m_new;
-      l *= alpha;
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[i][r] *= alpha;
+  // The place on the line and the part at hand stay in LDS, and arguments are read where they are used: the tile loop has no
+  // registers to keep them in.
+  Part& next = shared.next;
+  {
+    const Place at = find_place<BM, BN>(p, w, shared.scratch);
+    write_border(p, at, w);
+    if (tid == 0) shared.place = at;
+  }
+  while (true) {
+    if (tid == 0) {
+      Place at = shared.place;
+      Part x{};
+      shared.more = next_part<BM, BN>(p, at, x);
+      next = x;
+      shared.place = at;
     }
-    const float mc = m * c;
-#pragma unroll
-    for (int chunk = 0; chunk < 4; ++chunk) {
-      union VOperand {
-        struct {
-          s16x4 lo, hi;
-        } s;
-        bf16x8 v;
-      } va[NV];
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const char* base = vt + 16 * chunk * RB + v_off[i];
-        va[i].s.lo = lds_read_tr16(reinterpret_cast<const bf16_t*>(base));
-        va[i].s.hi = lds_read_tr16(reinterpret_cast<const bf16_t*>(base + 8 * RB));
-      }
-      bf16x8 pb;  // rounded for the product; the row sum takes them as they are (its logarithm is an output, in fp32)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float e = fast_exp2(fmaf(s[chunk >> 1][8 * (chunk & 1) + i], c, -mc));
-        l += e;
-        pb[i] = static_cast<bf16_t>(e);
-      }
-#pragma unroll
-      for (int i = 0; i < NV; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[i].v, pb, o[i], 0, 0, 0);
-    }
-  };
-
-  // Stage b holds tile begin + 2 x + b.  One barrier a tile: the copies of tile `it` have landed for all, and the stage
-  // that the next copies go to has been read by all.
-  auto step = [&](int it, auto buf_tag) {
-    constexpr int buf = decltype(buf_tag)::value;
-    wait_vmcnt<0>();
     __syncthreads();
-    const bool more = it + 1 < end;
-    if (more) {
-      if constexpr (FP8)
-        load_codes(it + 1);
-      else
-        copy_tile(it + 1, std::integral_constant<int, 1 - buf>{});
-    }
-    if (active && it * BN < limit_max) math(it, buf_tag);
-    if constexpr (FP8)
-      if (more) store_codes(1 - buf);
-  };
-  if (begin < end) {
-    if constexpr (FP8) {
-      load_codes(begin);
-      store_codes(0);
-    } else {
-      copy_tile(begin, std::integral_constant<int, 0>{});
-    }
-  }
-  int it = begin;
-  for (; it + 1 < end; it += 2) {
-    step(it, std::integral_constant<int, 0>{});
-    step(it + 1, std::integral_constant<int, 1>{});
-  }
-  if (it < end) step(it, std::integral_constant<int, 0>{});
+    if (!__builtin_amdgcn_readfirstlane(shared.more)) return;
+    const AttendParams& a = arguments();
+    const Part part{__builtin_amdgcn_readfirstlane(next.b), __builtin_amdgcn_readfirstlane(next.h),
+                    __builtin_amdgcn_readfirstlane(next.t), uniform(next.from), uniform(next.to), uniform(next.weight)};
+    const Tile tl = tile_of<BM>(a.c, part);
+    const int h = part.h;
+    const int steps = (visible_keys(a.c, tl, divide(tl.row0 + tl.rows - 1, a.c.div_G)) + BN - 1) / BN;
+    const int begin = steps_before(part.from, part.weight, steps), end = steps_before(part.to, part.weight, steps);
 
-  // Lane (n, hl) holds columns 32 i + 8 (r / 4) + 4 hl + r % 4 of query n.
-  l = sum_halves(l);
-  if (real) {
-  const long long out_row = static_cast<long long>(tl.q0 + j) * p.c.Hq + hq;
-  const long long part_row = part_rows<BM>(w, part.from == 0) + w_row + n;
-  if (hl == 0) {
-    if (!alone) {
-      p.part_ml[part_row * 2] = m;
-      p.part_ml[part_row * 2 + 1] = l;
-    } else if (p.lse) {
-      p.lse[out_row] = natural_lse(m, l, p.sm_scale);
-    }
-  }
-  if (!alone) {
-    float* to = p.part_o + part_row * D + 4 * hl;
+    // Rows of this wavefront; one without rows still copies its share of the tiles.
+    const int w_row = wave * 32;
+    const bool active = w_row < tl.rows;
+    const int limit_min = w_row + 32 <= tl.rows ? visible_keys(a.c, tl, divide(tl.row0 + w_row, a.c.div_G)) : 0;
+    const int limit_max = active ? visible_keys(a.c, tl, divide(tl.row0 + min(w_row + 31, tl.rows - 1), a.c.div_G)) : 0;
+    // Tiles that this wavefront has to do with.
+    const int my_end = min(end, (limit_max + BN - 1) / BN);
+    struct Row {
+      int j, hq;  // token of the request, query head
+      bool real;
+    };
+    auto row_of = [&](const AttendParams& a) {
+      const int row = tl.row0 + min(w_row + n, tl.rows - 1), j = divide(row, a.c.div_G);
+      return Row{j, h * a.c.G + row - j * a.c.G, w_row + n < tl.rows};
+    };
+    const Row my = row_of(a);
+    const int limit = my.real ? visible_keys(a.c, tl, my.j) : 0;
+    // Table row of the request; page size in granules.
+    const int* const table = a.c.table + static_cast<long long>(tl.b) * a.c.max_pages;
+    const int per_log2 = a.c.page_log2 - 4, heads = a.c.H, last_page = a.c.num_pages - 1;
+    auto locate = [&](int it) {
+      TileRows r;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        *reinterpret_cast<f32x4*>(to + 32 * i + 8 * r) = f32x4{o[i][4 * r], o[i][4 * r + 1], o[i][4 * r + 2], o[i][4 * r + 3]};
-  } else {
-    const float f = l > 0.f ? 1.f / l : l;  // nothing seen: zeros; NaN stays
-    bf16_t* to = static_cast<bf16_t*>(const_cast<void*>(p.out.data)) + (tl.q0 + j) * p.out.token_stride +
-                 hq * p.out.head_stride + 4 * hl;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        bf16x4 y;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) y[k] = static_cast<bf16_t>(o[i][4 * r + k] * f);
-        *reinterpret_cast<bf16x4*>(to + 32 * i + 8 * r) = y;
+      for (int i = 0; i < 4; ++i) {
+        const int x = min(4 * it + i, max(tl.len - 1, 0) >> 4);  // granule of the request
+        const unsigned e = min(static_cast<unsigned>(uniform_load(table, x >> per_log2)), static_cast<unsigned>(last_page));
+        r.granule[i] = ((static_cast<int>(e) * heads + h) << per_log2) + (x & ((1 << per_log2) - 1));
       }
-  }
-  }
-  __syncthreads();  // the stages are free for the next segment
+      return r;
+    };
+
+    bf16x8 qreg[NK];
+    {
+      const bf16_t* from = static_cast<const bf16_t*>(a.q.data) + (tl.q0 + my.j) * a.q.token_stride + my.hq * a.q.head_stride + 8 * hl;
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks) qreg[ks] = *reinterpret_cast<const bf16x8*>(from + 16 * ks);
+    }
+
+    // A tile behind the part's end has no rows: its copies touch no memory.
+    const int stop = min(tl.len, end * BN);
+    // bf16 rows: copy i of this wavefront of a K or V tile covers rows (64 / CPT) i + (16 / CPT) wave and on, all of one
+    // granule; rows behind the request's end arrive as zeros (a probability of 0 does not remove an infinity).
+    auto source = [&](const char* pages, const TileRows& at, int it, int i) {
+      constexpr int PER = 64 / CPT;                        // rows between copies of a wavefront
+      const int ahead = PER == 16 ? 0 : 16 * (wave >> 1);  // rows of the lane offset that belong to the granule's place
+      const int left = stop - it * BN - PER * i;           // valid rows from those of the lane offset's row 0 on
+      const int from = PER == 16 ? at.granule[i] : wave >> 1 ? at.granule[2 * i + 1] : at.granule[2 * i];
+      return tile::tile_descriptor<RB>(pages + (static_cast<long long>(from) * 16 - ahead) * RB, left > ahead ? left : 0);
+    };
+    auto copy_k = [&](const TileRows& at, int it, auto buf_tag, int i) {
+      tile::copy_1k_checked(lds_wave, decltype(buf_tag)::value * (2 * TILE_BYTES) + 4096 * i, ld_off_k, source(k_pages, at, it, i), 0);
+    };
+    auto copy_v = [&](const TileRows& at, int it, auto buf_tag, int i) {
+      tile::copy_1k_checked(lds_wave, decltype(buf_tag)::value * (2 * TILE_BYTES) + TILE_BYTES + 4096 * i, ld_off_v,
+                            source(v_pages, at, it, i), 0);
+    };
+    // 8-bit rows: load i of a lane is 16 codes of one row, converted on the way into the stage.
+    constexpr int LPR = D / 16;  // lanes per row
+    auto load_codes = [&](const char* pages, const TileRows& at, int it, uint4 (&raw)[CPL]) {
+#pragma unroll
+      for (int i = 0; i < CPL; ++i) {
+        const int r = (tid + 256 * i) / LPR;  // a wavefront's 64 / LPR rows are of one granule
+        const int from = D == 128 ? (wave >> 1 ? at.granule[2 * i + 1] : at.granule[2 * i])
+                                  : wave >> 1 ? (wave & 1 ? at.granule[3] : at.granule[2]) : (wave & 1 ? at.granule[1] : at.granule[0]);
+        raw[i] = make_uint4(0, 0, 0, 0);
+        if (it * BN + r < stop) raw[i] = ldg16(pages + (static_cast<long long>(from) * 16 + (r & 15)) * SRC + (tid % LPR) * 16);
+      }
+    };
+    auto store_codes = [&](char* stage, const uint4 (&raw)[CPL], auto is_v) {
+#pragma unroll
+      for (int i = 0; i < CPL; ++i) {
+        const int r = (tid + 256 * i) / LPR, chunk = 2 * (tid % LPR);
+        const int swz = decltype(is_v)::value ? tile::swizzle_v<RB>(r & 15) : tile::swizzle_k<RB>(r & 15);
+        *reinterpret_cast<uint4*>(stage + r * RB + ((chunk ^ swz) << 4)) = codes_to_chunk(raw[i].x, raw[i].y);
+        *reinterpret_cast<uint4*>(stage + r * RB + (((chunk + 1) ^ swz) << 4)) = codes_to_chunk(raw[i].z, raw[i].w);
+      }
+    };
+    using Zero = std::integral_constant<int, 0>;
+    using One = std::integral_constant<int, 1>;
+
+    f32x16 o[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+    float m = lowest_reference(c), l = 0.f;
+
+    union VOperand {
+      struct {
+        s16x4 lo, hi;
+      } s;
+      bf16x8 v;
+    };
+    // Operands out of a stage: K rows 32 cb + n, step ks; V columns 32 i + .., keys 16 chunk + ..
+    auto read_k = [&](auto buf_tag, int ks, int cb) {
+      return *(const __attribute__((address_space(3))) bf16x8*)(lds_pointer(k_off[ks]) +
+                                                                (decltype(buf_tag)::value * (2 * TILE_BYTES) + cb * 32 * RB));
+    };
+    auto read_v = [&](auto buf_tag, int chunk, int i) {
+      const auto* at = lds_pointer(v_off[i]) + (decltype(buf_tag)::value * (2 * TILE_BYTES) + TILE_BYTES + 16 * chunk * RB);
+      VOperand x;
+      x.s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)at);
+      x.s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(at + 8 * RB));
+      return x.v;
+    };
+    // S^T = K Q^T of the 64 keys of a K tile.
+    auto scores = [&](f32x16 (&s)[2], auto buf_tag) {
+#pragma unroll
+      for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[cb][r] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+        for (int cb = 0; cb < 2; ++cb)
+          s[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_k(buf_tag, ks, cb), qreg[ks], s[cb], 0, 0, 0);
+    };
+    auto lane_max = [&](const f32x16 (&s)[2]) {
+      float mx = s[0][0];
+#pragma unroll
+      for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[cb][r]);
+      return mx;
+    };
+    auto raise = [&](float mx) {
+      mx = max_halves(mx);
+      if (__any(mx > m + slack)) {
+        const float m_new = fmaxf(m, mx);
+        const float alpha = fast_exp2((m - m_new) * c);
+        m = m_new;
+        l *= alpha;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[i][r] *= alpha;
+      }
+    };
+    // Masks what a row of tile `it` does not see; whether there may be such.
+    auto mask = [&](int it, f32x16 (&s)[2]) {
+      if (it * BN + BN <= limit_min) return false;
+      tile::mask_rows(limit - it * BN, hl, s);
+      return true;
+    };
+    // P^T = 2^(S^T c - m c) in bf16 and O^T += V^T P^T.  Probabilities are rounded for the product; the row sum takes them as
+    // they are (its logarithm is an output, in fp32).
+    auto accumulate = [&](const f32x16 (&s)[2], auto buf_tag) {
+      const float mc = m * c;
+#pragma unroll
+      for (int chunk = 0; chunk < 4; ++chunk) {
+        bf16x8 va[NV], pb;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) va[i] = read_v(buf_tag, chunk, i);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float e = fast_exp2(fmaf(s[chunk >> 1][8 * (chunk & 1) + i], c, -mc));
+          l += e;
+          pb[i] = static_cast<bf16_t>(e);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[i], pb, o[i], 0, 0, 0);
+      }
+    };
+    // Scores of the next tile (K stage kb1) and P V of this one (V stage vb0) together: MFMAs one by one, each with a share of
+    // the vector and LDS work behind it, in the order of attend.hip's step: S(g) a quarter of the scores, A(g) the 16 keys of
+    // chunk g; the probabilities of chunk g + 1 are formed under A(g) and S(g + 1), operands read a phase before their use.
+    auto step_math = [&](const f32x16 (&s_in)[2], f32x16 (&s_out)[2], auto kb1, auto vb0, auto&& copy_slot) {
+      constexpr int KPC = NK / 4, NS = 2 * KPC, NA = NV;  // K steps and slots of a phase S, slots of a phase A
+      static_assert(NS == NA && 8 % (NS + NA) == 0, "phases divide the vector work evenly");
+      const float mc = m * c;
+      bf16x8 kop[NK][2], vop[4][NV];
+      float e[4][8];
+      union {
+        bf16x8 v;
+        bf16x2 h[4];
+      } pb[4];
+      auto load_k = [&](int ks, int cb) { kop[ks][cb] = read_k(kb1, ks, cb); };
+      auto probability = [&](int chunk, int u) {
+        e[chunk][u] = fast_exp2(fmaf(s_in[chunk >> 1][8 * (chunk & 1) + u], c, -mc));
+        if (u & 1) {
+          pb[chunk].h[u >> 1] = bf16x2{static_cast<bf16_t>(e[chunk][u - 1]), static_cast<bf16_t>(e[chunk][u])};
+          l += e[chunk][u - 1] + e[chunk][u];
+        }
+      };
+      auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+#pragma unroll
+      for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s_out[cb][r] = 0.f;
+      load_k(0, 0);
+      load_k(0, 1);
+      float mx = -INFINITY;
+      int slot = 0;  // compile-time after unrolling
+      auto s_slot = [&](int gch, int i, int& done) {
+        const int ks = gch * KPC + (i >> 1), cb = i & 1;
+        s_out[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop[ks][cb], qreg[ks], s_out[cb], 0, 0, 0);
+        fence();
+        if (gch == 0) {
+          if (ks + 1 < KPC) load_k(ks + 1, cb);
+          vop[0][i] = read_v(vb0, 0, i);
+        }
+        if (gch < 3) load_k(ks + KPC, cb);
+        copy_slot(slot++);
+        const int share = gch == 0 ? 8 / NS : 8 / (NS + NA);
+        for (int u = 0; u < share; ++u) probability(gch, done++);
+        fence();
+      };
+      int done = 0;
+#pragma unroll
+      for (int i = 0; i < NS; ++i) s_slot(0, i, done);
+#pragma unroll
+      for (int gch = 0; gch < 4; ++gch) {
+        done = 0;
+#pragma unroll
+        for (int d = 0; d < NA; ++d) {
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop[gch][d], pb[gch].v, o[d], 0, 0, 0);
+          fence();
+          if (gch < 3) {
+            vop[gch + 1][d] = read_v(vb0, gch + 1, d);
+            copy_slot(slot++);
+#pragma unroll
+            for (int u = 0; u < 8 / (NS + NA); ++u) probability(gch + 1, done++);
+          } else {  // the new scores are complete: their maxima
+#pragma unroll
+            for (int r = d * (32 / NA); r < (d + 1) * (32 / NA); ++r) mx = fmaxf(mx, s_out[r >> 4][r & 15]);
+            asm volatile("" : "+v"(mx));  // in this slot
+          }
+          fence();
+        }
+        if (gch < 3)
+#pragma unroll
+          for (int i = 0; i < NS; ++i) s_slot(gch + 1, i, done);
+      }
+      return mx;
+    };
+
+    // Step `it`: K(it + 1) and V(it) have landed; V(it + 1) and K(it + 2) go out.  Tile t's K and V lie in stage (t - begin) % 2.
+    // `at`: where tile it + 1 lies; tile it + 2 is looked up between the two.
+    f32x16 s_a[2], s_b[2];
+    TileRows at{};
+    // `math(copy)`: what the wavefront computes in the step; it calls copy(i) for i = 0 .. 3 CPT - 1, in order.
+    auto step = [&](int it, auto kb1, auto vb0, auto&& math) {
+      wait_vmcnt<0>();
+      __syncthreads();
+      if constexpr (FP8) {
+        uint4 raw_k[CPL], raw_v[CPL];
+        load_codes(v_pages, at, it + 1, raw_v);
+        at = locate(it + 2);
+        load_codes(k_pages, at, it + 2, raw_k);
+        math([](int) {});
+        store_codes(lds[decltype(kb1)::value][1], raw_v, One{});
+        store_codes(lds[decltype(vb0)::value][0], raw_k, Zero{});
+      } else {
+        math([&](int i) {
+          if (i < CPT)
+            copy_v(at, it + 1, kb1, i);
+          else if (i == CPT)
+            at = locate(it + 2);
+          else if (i >= 2 * CPT && i < 3 * CPT)
+            copy_k(at, it + 2, vb0, i - 2 * CPT);
+        });
+      }
+    };
+    auto copies_only = [](auto&& copy) {
+#pragma unroll
+      for (int i = 0; i < 3 * CPT; ++i) copy(i);
+    };
+    auto pipe_step = [&](int it, auto kb1, auto vb0, f32x16 (&s_in)[2], f32x16 (&s_out)[2]) {
+      step(it, kb1, vb0, [&](auto&& copy) {
+        const float mx = step_math(s_in, s_out, kb1, vb0, copy);
+        raise(mask(it + 1, s_out) ? lane_max(s_out) : mx);
+      });
+    };
+    auto last_step = [&](int it, auto kb1, auto vb0, f32x16 (&s_in)[2]) {
+      step(it, kb1, vb0, copies_only);
+      accumulate(s_in, vb0);
+    };
+    if (begin < end) {
+      const int second = begin + 1 < end ? begin + 1 : begin;
+      at = locate(begin);
+      if constexpr (FP8) {
+        uint4 raw[CPL], raw2[CPL], raw3[CPL];
+        load_codes(k_pages, at, begin, raw);
+        load_codes(v_pages, at, begin, raw2);
+        at = locate(second);
+        load_codes(k_pages, at, second, raw3);
+        store_codes(lds[0][0], raw, Zero{});
+        store_codes(lds[0][1], raw2, One{});
+        store_codes(lds[1][0], raw3, Zero{});
+      } else {
+#pragma unroll
+        for (int i = 0; i < CPT; ++i) copy_k(at, begin, Zero{}, i);
+#pragma unroll
+        for (int i = 0; i < CPT; ++i) copy_v(at, begin, Zero{}, i);
+        at = locate(second);
+#pragma unroll
+        for (int i = 0; i < CPT; ++i) copy_k(at, second, One{}, i);
+        wait_vmcnt<2 * CPT>();  // K of the first tile
+      }
+      __syncthreads();
+      if (begin < my_end) {
+        scores(s_a, Zero{});
+        mask(begin, s_a);
+        raise(lane_max(s_a));
+      }
+      // Every wavefront makes all steps (the barriers are shared), those behind its last tile without arithmetic.
+      int it = begin;
+      for (; it + 2 < my_end; it += 2) {
+        pipe_step(it, One{}, Zero{}, s_a, s_b);
+        pipe_step(it + 1, Zero{}, One{}, s_b, s_a);
+      }
+      if (it + 1 < my_end) {
+        pipe_step(it, One{}, Zero{}, s_a, s_b);
+        last_step(it + 1, Zero{}, One{}, s_b);
+        it += 2;
+      } else if (it < my_end) {
+        last_step(it, One{}, Zero{}, s_a);
+        it += 1;
+      }
+      for (; it < end; ++it)
+        if ((it - begin) & 1)
+          step(it, Zero{}, One{}, copies_only);
+        else
+          step(it, One{}, Zero{}, copies_only);
+    }
+
+    // Lane (n, hl) holds columns 32 i + 8 (r / 4) + 4 hl + r % 4 of query n.
+    l = sum_halves(l);
+    const AttendParams& z = arguments();
+    const Row out = row_of(z);
+    const bool alone = uniform(next.from) == 0 && uniform(next.to) == uniform(next.weight);
+    if (out.real) {
+      const long long token = tl.q0 + out.j, out_row = token * z.c.Hq + out.hq;
+      const long long part_row = part_rows<BM>(w, uniform(next.from) == 0) + w_row + n;
+      if (hl == 0) {
+        if (!alone) {
+          z.part_ml[part_row * 2] = m;
+          z.part_ml[part_row * 2 + 1] = l;
+        } else if (z.lse) {
+          z.lse[out_row] = natural_lse(m, l, z.sm_scale);
+        }
+      }
+      if (!alone) {
+        float* to = z.part_o + part_row * D + 4 * hl;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            *reinterpret_cast<f32x4*>(to + 32 * i + 8 * r) = f32x4{o[i][4 * r], o[i][4 * r + 1], o[i][4 * r + 2], o[i][4 * r + 3]};
+      } else {
+        const float f = l > 0.f ? 1.f / l : l;  // nothing seen: zeros; NaN stays
+        bf16_t* to = static_cast<bf16_t*>(const_cast<void*>(z.out.data)) + token * z.out.token_stride +
+                     out.hq * z.out.head_stride + 4 * hl;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            bf16x4 y;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y[k] = static_cast<bf16_t>(o[i][4 * r + k] * f);
+            *reinterpret_cast<bf16x4*>(to + 32 * i + 8 * r) = y;
+          }
+      }
+    }
+    __syncthreads();  // the stages, and `next`, are free for the next segment
   }
 }
 
 template <int D, bool FP8>
 hipError_t launch(const AttendParams& p, hipStream_t stream) {
-  hipLaunchKernelGGL((paged_attend_long_kernel<D, FP8>), dim3(p.grid), dim3(256), 4 * BN * 2 * D, stream, p);
+  constexpr size_t lds = 4 * BN * 2 * D + sizeof(Shared);
+  static std::atomic<unsigned long long> allowed{0};
+  if (lds > 64 * 1024)
+    if (hipError_t e = allow_lds(reinterpret_cast<const void*>(&paged_attend_long_kernel<D, FP8>), lds, allowed)) return e;
+  hipLaunchKernelGGL((paged_attend_long_kernel<D, FP8>), dim3(p.grid), dim3(256), lds, stream, p);
   return hipGetLastError();
 }
 
