@@ -108,7 +108,7 @@ struct Rows {  // of the token tensors, strides in elements
 };
 
 struct Border {
-  int b, h, t, parts;  // segment that a border between two shares cuts, and its parts
+  int b, h, t, parts;  // a cut segment and its parts; 0: none at this workgroup
 };
 
 struct AttendParams {
@@ -121,11 +121,13 @@ struct AttendParams {
   float* lse;           // [tokens][Hq] or null
   // Requests of this launch, by their query rows per kv head (new tokens x group): least_rows < rows <= most_rows.
   int least_rows, most_rows;
-  // How it is dealt (paged_schedule.h): workgroups, weight of the lightest share.
-  int workgroups, least_weight, whole_from;
-  int grid;
-  float *part_o, *part_ml;  // parts of cut segments: [workgroups][2][ROWS][d] unnormalised outputs, [..][2] reference and sum
-  Border* borders;          // [workgroups]; null: nothing can be cut
+  // How it is dealt (paged_schedule.h): shares, workgroups, weight of the lightest share, segments from which on none is cut.
+  int workgroups, grid, least_weight, whole_from;
+  int cut_from;  // segments of up to this weight are not cut
+  // Parts of cut segments: unnormalised outputs [..][ROWS][d], reference and sum [..][ROWS][2], two for each workgroup of the
+  // line, one for each that takes a piece.
+  float *part_o, *part_ml;
+  Border* borders;  // of each workgroup; null: nothing can be cut
 };
 
 struct SelectParams {

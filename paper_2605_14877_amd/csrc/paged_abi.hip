@@ -133,10 +133,10 @@ Workspace workspace_of(const heatkv_paged_shape* s, const heatkv::paged::Plan& p
     return at;
   };
   auto arrays = [&](PartArrays& a, const heatkv::paged::Launch& l, int rows) {
-    if (!l.workgroups || !l.join) return;
-    a.o = take(size_t(l.workgroups) * 2 * rows * s->d * 4);
-    a.ml = take(size_t(l.workgroups) * 2 * rows * 8);
-    a.borders = take(size_t(l.workgroups) * sizeof(heatkv::paged::Border));
+    if (!l.parts) return;
+    a.o = take(size_t(l.parts) * rows * s->d * 4);
+    a.ml = take(size_t(l.parts) * rows * 8);
+    a.borders = take(size_t(l.grid) * sizeof(heatkv::paged::Border));
   };
   arrays(w.few, plan.few, 16);
   arrays(w.many, plan.many, 128);
@@ -185,12 +185,13 @@ int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const voi
     if (!l.workgroups) return hipSuccess;
     p.workgroups = l.workgroups;
     p.least_weight = l.least_steps * heatkv::paged::STEP_WEIGHT;
+    p.cut_from = l.parts ? p.least_weight : INT_MAX;
     p.least_rows = l.least_rows;
     p.most_rows = l.most_rows;
     p.grid = int(l.grid);
     p.whole_from = l.whole_from;
     p.borders = nullptr;
-    if (l.join) {
+    if (l.parts) {
       p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + a.o);
       p.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + a.ml);
       p.borders = reinterpret_cast<heatkv::paged::Border*>(static_cast<char*>(ws) + a.borders);
@@ -198,7 +199,7 @@ int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const voi
     hipError_t e = s->dtype == HEATKV_F32 ? heatkv::launch_paged_attend_f32(p, s->d, hip_stream)
                    : many                 ? heatkv::launch_paged_attend_long(p, s->d, fp8, hip_stream)
                                           : heatkv::launch_paged_attend_bf16(p, s->d, fp8, hip_stream);
-    return e == hipSuccess && l.join ? heatkv::launch_paged_join(p, s->dtype, s->d, many, hip_stream) : e;
+    return e == hipSuccess && l.parts ? heatkv::launch_paged_join(p, s->dtype, s->d, many, hip_stream) : e;
   };
   hipError_t e = launch(plan.many, w.many, true);
   if (e == hipSuccess) e = launch(plan.few, w.few, false);

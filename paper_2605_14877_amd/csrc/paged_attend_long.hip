@@ -48,9 +48,7 @@ __device__ __forceinline__ const __attribute__((address_space(3))) char* lds_poi
 
 struct Shared {
   Scratch scratch;
-  Place place;
-  Part next;
-  int more;
+  Part piece;
 };
 
 // The launch's arguments, loaded anew.
@@ -91,27 +89,18 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
   constexpr float kSlack = 8.f;  // the reference is raised by more than this only: attend.hip
   const float slack = kSlack / c;
 
-  // The place on the line and the part at hand stay in LDS, and arguments are read where they are used: the tile loop has no
-  // registers to keep them in.
-  Part& next = shared.next;
+  // The piece at hand stays in LDS, and arguments are read where they are used: the tile loop has no registers to keep them in.
   {
-    const Place at = find_place<BM, BN>(p, w, shared.scratch);
-    write_border(p, at, w);
-    if (tid == 0) shared.place = at;
-  }
-  while (true) {
-    if (tid == 0) {
-      Place at = shared.place;
-      Part x{};
-      shared.more = next_part<BM, BN>(p, at, x);
-      next = x;
-      shared.place = at;
-    }
+    Part part;
+    if (!find_piece<BM, BN>(p, w, shared.scratch, part)) return;
+    if (tid == 0) shared.piece = part;
     __syncthreads();
-    if (!__builtin_amdgcn_readfirstlane(shared.more)) return;
+  }
+  {
     const AttendParams& a = arguments();
-    const Part part{__builtin_amdgcn_readfirstlane(next.b), __builtin_amdgcn_readfirstlane(next.h),
-                    __builtin_amdgcn_readfirstlane(next.t), uniform(next.from), uniform(next.to), uniform(next.weight)};
+    const Part part{__builtin_amdgcn_readfirstlane(shared.piece.b), __builtin_amdgcn_readfirstlane(shared.piece.h),
+                    __builtin_amdgcn_readfirstlane(shared.piece.t), uniform(shared.piece.from), uniform(shared.piece.to),
+                    uniform(shared.piece.weight)};
     const Tile tl = tile_of<BM>(a.c, part);
     const int h = part.h;
     const int steps = (visible_keys(a.c, tl, divide(tl.row0 + tl.rows - 1, a.c.div_G)) + BN - 1) / BN;
@@ -447,10 +436,10 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     l = sum_halves(l);
     const AttendParams& z = arguments();
     const Row out = row_of(z);
-    const bool alone = uniform(next.from) == 0 && uniform(next.to) == uniform(next.weight);
+    const bool alone = uniform(shared.piece.weight) == 1;
     if (out.real) {
       const long long token = tl.q0 + out.j, out_row = token * z.c.Hq + out.hq;
-      const long long part_row = part_rows<BM>(w, uniform(next.from) == 0) + w_row + n;
+      const long long part_row = static_cast<long long>(w) * BM + w_row + n;
       if (hl == 0) {
         if (!alone) {
           z.part_ml[part_row * 2] = m;
@@ -481,7 +470,6 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
           }
       }
     }
-    __syncthreads();  // the stages, and `next`, are free for the next segment
   }
 }
 

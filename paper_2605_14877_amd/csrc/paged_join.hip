@@ -2,7 +2,8 @@
 // one border between shares and joins the segment there, if this is the first border in it: a wavefront per row, the parts in
 // order, so that the result does not depend on which workgroup was done first.
 //
-// Bound: latency (three rounds of loads, and one more for every sixteen parts), and of many rows the traffic of the parts.
+// Bound: latency (borders, lengths, parts: a round of loads each, one more for every sixteen parts), and of many rows the
+// traffic of the parts.
 #include <hip/hip_runtime.h>
 
 #include "f32_mfma.h"
@@ -20,61 +21,95 @@ using namespace paged;
 // EACH: rows of a wavefront.
 template <class T, int D, int ROWS, int EACH>
 __global__ __launch_bounds__(256) void paged_join_kernel(AttendParams p) {
-  constexpr int N = D / 32, U = 8;  // columns of a lane, parts whose loads a half wavefront has under way together
-  const int lane = threadIdx.x & 63, w = blockIdx.x + 1;
+  constexpr int N = D / 32;  // columns of a lane; either half of a wavefront has a whole row
+  constexpr bool PIECES = ROWS == 128;  // dealt by pieces, not along the line
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = (lane & 31) * N, w = blockIdx.x + (PIECES ? 0 : 1);
   const auto* border = (const __attribute__((address_space(4))) Border*)(p.borders) + w;
   const int parts = border->parts;
   if (parts == 0) return;
   const Part segment{border->b, border->h, border->t, 0, 0, 0};
   const Tile tile = tile_of<ROWS>(p.c, segment);
+  const int row0 = blockIdx.y * EACH * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // then every fourth
+  if (row0 >= tile.rows) return;
   const f32m::Exponent prob(p.sm_scale);
   const float c = p.sm_scale * kLog2e;
-  for (int i = 0; i < EACH; ++i) {
-  const int row = (blockIdx.y * EACH + i) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (row >= tile.rows) return;
-  auto place = [&](int i) { return part_rows<ROWS>(w - 1 + i, i == 0) + row; };
-  float m = -INFINITY;
-  for (int i = lane; i < parts; i += 64) m = fmaxf(m, p.part_ml[place(i) * 2]);
+  // 2^ of a difference of references.
+  auto factor = [&](float reference, float to) { return sizeof(T) == 4 ? prob(reference, to) : fast_exp2((reference - to) * c); };
+  struct One {
+    float m, l, x[N];
+  };
+  auto load = [&](int part, int row) {
+    const long long at = (PIECES ? (w + static_cast<long long>(part) * p.c.H) * ROWS : part_rows<ROWS>(w - 1 + part, part == 0)) + row;
+    One y;
+    y.m = p.part_ml[at * 2];
+    y.l = p.part_ml[at * 2 + 1];
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d, 64));
-  float l = 0.f, x[N] = {};
-  const int half = lane >> 5, col = (lane & 31) * N;
-  for (int i0 = half; i0 < parts; i0 += 2 * U) {  // the halves take turns
-    float ml[U][2], o[U][N];
+    for (int k = 0; k < N; ++k) y.x[k] = p.part_o[at * D + col + k];
+    return y;
+  };
+  // What the two halves have of a row becomes the output.
+  auto finish = [&](int row, One y) {
+    const float m = max_halves(y.m), f = factor(y.m, m);
+    const float l = sum_halves(y.l * f), g = l > 0.f ? 1.f / l : l;  // nothing seen: zeros; NaN stays
+    const int j = divide(tile.row0 + row, p.c.div_G), hq = segment.h * p.c.G + tile.row0 + row - j * p.c.G;
+    const long long t = tile.q0 + j;
+    T* to = static_cast<T*>(const_cast<void*>(p.out.data)) + t * p.out.token_stride + hq * p.out.head_stride + col;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const long long at_row = place(min(i0 + 2 * u, parts - 1));
-      ml[u][0] = p.part_ml[at_row * 2];
-      ml[u][1] = p.part_ml[at_row * 2 + 1];
-#pragma unroll
-      for (int k = 0; k < N; ++k) o[u][k] = p.part_o[at_row * D + col + k];
+    for (int k = 0; k < N; ++k) {
+      const float x = sum_halves(y.x[k] * f) * g;
+      if (half == 0) to[k] = static_cast<T>(x);
     }
+    if (p.lse && lane == 0) p.lse[t * p.c.Hq + hq] = sizeof(T) == 4 ? natural_lse_f32(m, l, prob) : natural_lse(m, l, p.sm_scale);
+  };
+  if (parts == 2) {  // the loads of all rows together
+    One y[EACH];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i0 + 2 * u >= parts) break;
-      const float f = sizeof(T) == 4 ? prob(ml[u][0], m) : fast_exp2((ml[u][0] - m) * c);
-      l += f * ml[u][1];
+    for (int i = 0; i < EACH; ++i) y[i] = load(half, min(row0 + 4 * i, tile.rows - 1));
 #pragma unroll
-      for (int k = 0; k < N; ++k) x[k] += f * o[u][k];
-    }
+    for (int i = 0; i < EACH; ++i)
+      if (row0 + 4 * i < tile.rows) finish(row0 + 4 * i, y[i]);
+    return;
   }
-  l += swap_halves(l);
+  // R rows and of each U parts have their loads under way together; the halves take turns over the parts.
+  constexpr int R = EACH < 4 ? EACH : 4, U = 8 / (R < 2 ? 1 : 2);
+  for (int r0 = row0; r0 < min(row0 + 4 * EACH, tile.rows); r0 += 4 * R) {
+    One sum[R];
 #pragma unroll
-  for (int k = 0; k < N; ++k) x[k] += swap_halves(x[k]);
-  const float f = l > 0.f ? 1.f / l : l;  // nothing seen: zeros; NaN stays
-  const int j = divide(tile.row0 + row, p.c.div_G), hq = segment.h * p.c.G + tile.row0 + row - j * p.c.G;
-  const long long t = tile.q0 + j;
-  T* to = static_cast<T*>(const_cast<void*>(p.out.data)) + t * p.out.token_stride + hq * p.out.head_stride + col;
-  if (half == 0)
+    for (int r = 0; r < R; ++r) sum[r] = One{-INFINITY, 0.f, {}};
+    for (int i0 = half; i0 - half < parts; i0 += 2 * U) {
+      One y[R][U];
 #pragma unroll
-    for (int k = 0; k < N; ++k) to[k] = static_cast<T>(x[k] * f);
-  if (p.lse && lane == 0) p.lse[t * p.c.Hq + hq] = sizeof(T) == 4 ? natural_lse_f32(m, l, prob) : natural_lse(m, l, p.sm_scale);
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int u = 0; u < U; ++u) y[r][u] = load(min(i0 + 2 * u, parts - 1), min(r0 + 4 * r, tile.rows - 1));
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float m = sum[r].m;
+#pragma unroll
+        for (int u = 0; u < U; ++u) m = fmaxf(m, y[r][u].m);
+        const float f = factor(sum[r].m, m);
+        sum[r].m = m;
+        sum[r].l *= f;
+#pragma unroll
+        for (int k = 0; k < N; ++k) sum[r].x[k] *= f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const float g = i0 + 2 * u < parts ? factor(y[r][u].m, m) : 0.f;
+          sum[r].l += g * y[r][u].l;
+#pragma unroll
+          for (int k = 0; k < N; ++k) sum[r].x[k] += g * y[r][u].x[k];
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (r0 + 4 * r < tile.rows) finish(r0 + 4 * r, sum[r]);
   }
 }
 
 template <class T, int D, int ROWS, int EACH>
 hipError_t launch(const AttendParams& p, hipStream_t stream) {
-  hipLaunchKernelGGL((paged_join_kernel<T, D, ROWS, EACH>), dim3(p.workgroups - 1, ROWS / 4 / EACH), dim3(256), 0, stream, p);
+  hipLaunchKernelGGL((paged_join_kernel<T, D, ROWS, EACH>), dim3(ROWS == 128 ? p.grid : p.workgroups - 1, ROWS / 4 / EACH), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 

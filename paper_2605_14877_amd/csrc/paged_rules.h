@@ -12,10 +12,10 @@ namespace paged {
 struct Launch {
   int workgroups = 0;              // shares that the work is cut into; 0: not launched
   int64_t grid = 0;                // workgroups launched
-  int whole_from = INT_MAX;        // segments from which on a workgroup takes one, uncut
+  int parts = 0;                   // places for parts of cut segments; 0: nothing is cut
+  int whole_from = INT_MAX;        // segments from which on none is cut
   int least_steps = 0;             // of a share
   int least_rows = 0, most_rows = INT_MAX;  // requests by their query rows per kv head: least_rows < rows <= most_rows
-  bool join = false;               // segments may be cut
 };
 struct Plan {
   Launch few, many;  // tiles of 16 rows and steps of 32 keys; of 128 and 64
@@ -28,19 +28,23 @@ constexpr int MANY_ROWS = 64;
 inline Plan plan_launches(bool bf16, int batch, int kv_heads, int group, int64_t tokens, int64_t longest, int64_t chosen) {
   Plan p;
   const int64_t rows = tokens * group;
+  // Two workgroups to a compute unit are resident.  A segment of up to 8 steps is not cut (nor are they all where none is longer).
   p.few.workgroups = 512;
   p.few.grid = 512;
   p.few.least_steps = 8;
-  p.few.join = longest > 8 * 32;
+  p.few.parts = longest > 8 * 32 ? 2 * 512 : 0;
   if (bf16 && chosen == 0 && rows > MANY_ROWS) {
     p.few.most_rows = p.many.least_rows = MANY_ROWS;
     p.many.workgroups = 512;
     p.many.least_steps = 8;
-    // Two whole segments and more for every share: dealt as workgroups come free.
+    // Two whole segments for every share and more: nothing is cut.  Fewer: the pieces are at most one more than each
+    // segment's weight is shares.
     p.many.whole_from = 1024;
-    const int64_t most = kv_heads * (rows / 128 + std::min<int64_t>(batch, rows / (MANY_ROWS + 1)));
-    p.many.grid = most >= p.many.whole_from ? most : p.many.workgroups;
-    p.many.join = longest > 8 * 64;
+    const int64_t segments = kv_heads * (rows / 128 + std::min<int64_t>(batch, rows / (MANY_ROWS + 1)));
+    const int64_t pieces = p.many.workgroups + std::min<int64_t>(segments, p.many.whole_from - 1);
+    const bool cut = longest > 8 * 64;
+    p.many.grid = cut ? std::max(segments, pieces) : segments;
+    p.many.parts = cut ? static_cast<int>(pieces) : 0;
   }
   return p;
 }

@@ -7,9 +7,6 @@
 // the weight on either side), which a second launch joins in order; light segments are not cut, they belong to the
 // workgroup that they begin in.
 //
-// Where there are segments enough to fill the chip evenly as they come (whole_from), a workgroup takes one segment and
-// nothing is cut.
-//
 // Every workgroup finds its place by a scan over the requests (two rounds of loads, a block scan: about 2 us).
 #pragma once
 
@@ -59,10 +56,9 @@ struct Place {
   int b, h, t;                 // the segment at pos
   long long off;               // pos in it
   Load load;                   // of request b
-  bool whole;                  // one segment per workgroup: pos counts segments
 };
 struct Scratch {  // LDS
-  long long weights[4], counts[4], first;
+  long long sums[4], more_sums[4], first;
   int b;
 };
 
@@ -71,78 +67,78 @@ __device__ __forceinline__ Load request_load(const AttendParams& p, int b) {
   return load_of<ROWS, KEYS>(p, uniform_load(p.c.q_start, b), uniform_load(p.c.q_start, b + 1), uniform_load(p.c.lens, b));
 }
 
+// Inclusive sums over the 256 lanes of a workgroup, and the total in `all`; `sums`: LDS, free at the next barrier but one.
+__device__ __forceinline__ long long block_scan(long long v, long long (&sums)[4], long long& all) {
+  const int tid = threadIdx.x, lane = tid & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const long long u = __shfl_up(v, d, 64);
+    if (lane >= d) v += u;
+  }
+  if (lane == 63) sums[tid >> 6] = v;
+  __syncthreads();
+  all = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const long long x = sums[i];
+    if (i < (tid >> 6)) v += x;
+    all += x;
+  }
+  all = uniform(all);
+  return v;
+}
+// The request that holds position `at` of a line on which request b takes cost(b), and where on the line it begins.  By all
+// lanes; `upto`: block_scan of the costs of this lane's requests, `mine`.
+template <class Cost>
+__device__ __forceinline__ int find_request_at(long long at, int batch, long long upto, long long mine, const Cost& cost,
+                                               Scratch& scratch, long long& first) {
+  const int per = (batch + 255) / 256;
+  if (at < upto && at >= upto - mine) {  // one lane
+    long long x = upto - mine;
+    for (int i = 0; i < per; ++i) {
+      const int b = threadIdx.x * per + i;
+      const long long n = b < batch ? cost(b) : 0;
+      if (at < x + n) {
+        scratch.first = x;
+        scratch.b = b;
+        break;
+      }
+      x += n;
+    }
+  }
+  __syncthreads();
+  first = uniform(scratch.first);
+  return __builtin_amdgcn_readfirstlane(scratch.b);
+}
+template <class Cost>
+__device__ __forceinline__ long long own_cost(int batch, const Cost& cost) {  // of this lane's requests
+  const int per = (batch + 255) / 256;
+  long long mine = 0;
+  for (int i = 0; i < per; ++i)
+    if (static_cast<int>(threadIdx.x) * per + i < batch) mine += cost(threadIdx.x * per + i);
+  return mine;
+}
+
 // The place of workgroup w, by all of its 256 lanes.
 template <int ROWS, int KEYS>
 __device__ __forceinline__ Place find_place(const AttendParams& p, int w, Scratch& scratch) {
   const Cache& c = p.c;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int per = (c.batch + 255) / 256;
-  auto load = [&](int b) { return load_of<ROWS, KEYS>(p, c.q_start[b], c.q_start[b + 1], c.lens[b]); };
-  long long weight = 0, count = 0;  // of this lane's requests, then up to and with them
-  for (int i = 0; i < per; ++i)
-    if (tid * per + i < c.batch) {
-      const Load l = load(tid * per + i);
-      weight += l.upto(l.tiles) * c.H;
-      count += static_cast<long long>(l.tiles) * c.H;
-    }
-  const long long my_weight = weight, my_count = count;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const long long u = __shfl_up(weight, d, 64), v = __shfl_up(count, d, 64);
-    if (lane >= d) {
-      weight += u;
-      count += v;
-    }
-  }
-  if (lane == 63) {
-    scratch.weights[tid >> 6] = weight;
-    scratch.counts[tid >> 6] = count;
-  }
-  __syncthreads();
-  long long total = 0, segments = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (i < (tid >> 6)) {
-      weight += scratch.weights[i];
-      count += scratch.counts[i];
-    }
-    total += scratch.weights[i];
-    segments += scratch.counts[i];
-  }
-  total = uniform(total);
-  segments = uniform(segments);
+  auto cost = [&](int b) {
+    const Load l = load_of<ROWS, KEYS>(p, c.q_start[b], c.q_start[b + 1], c.lens[b]);
+    return l.upto(l.tiles) * c.H;
+  };
+  const long long mine = own_cost(c.batch, cost);
+  long long total;
+  const long long upto = block_scan(mine, scratch.sums, total);
   Place at{};
-  at.whole = segments >= p.whole_from;
-  at.share = at.whole ? 1 : max((total + p.workgroups - 1) / p.workgroups, static_cast<long long>(p.least_weight));
+  at.share = max((total + p.workgroups - 1) / p.workgroups, static_cast<long long>(p.least_weight));
   at.pos = w * at.share;
-  at.stop = at.whole ? min(at.pos + 1, segments) : w < p.workgroups ? min(at.pos + at.share, total) : at.pos;
-  if (at.pos >= at.stop) return at;
-  const long long upto = at.whole ? count : weight, mine = at.whole ? my_count : my_weight;
-  if (at.pos < upto && at.pos >= upto - mine) {  // one lane
-    long long first = upto - mine;
-    for (int i = 0; i < per; ++i) {
-      const int b = tid * per + i;
-      const Load l = b < c.batch ? load(b) : Load{0, 0, 0};
-      const long long n = (at.whole ? l.tiles : l.upto(l.tiles)) * c.H;
-      if (at.pos < first + n) {
-        scratch.first = first;
-        scratch.b = b;
-        break;
-      }
-      first += n;
-    }
-  }
-  __syncthreads();
-  at.b = __builtin_amdgcn_readfirstlane(scratch.b);
-  const long long rel = at.pos - uniform(scratch.first);
+  at.stop = min(at.pos + at.share, total);
+  if (at.pos >= total) return at;
+  long long first;
+  at.b = find_request_at(at.pos, c.batch, upto, mine, cost, scratch, first);
   at.load = request_load<ROWS, KEYS>(p, at.b);
-  if (at.whole) {  // the last tiles first: with a causal limit they are the heaviest
-    const int i = static_cast<int>(rel / c.H);
-    at.h = static_cast<int>(rel - static_cast<long long>(i) * c.H);
-    at.t = at.load.tiles - 1 - i;
-    return at;
-  }
-  const long long per_head = at.load.upto(at.load.tiles);
+  const long long rel = at.pos - first, per_head = at.load.upto(at.load.tiles);
   at.h = static_cast<int>(rel / per_head);
   const long long in_head = rel - at.h * per_head;
   int below = 0, above = at.load.tiles;  // the last tile that begins at in_head or before
@@ -162,14 +158,10 @@ struct Part {
 };
 template <int ROWS, int KEYS>
 __device__ __forceinline__ bool next_part(const AttendParams& p, Place& at, Part& part) {
-  if (at.whole) {
-    part = {at.b, at.h, at.t, 0, 1, 1};
-    return at.pos++ < at.stop;
-  }
   while (at.pos < at.stop) {
     const long long weight = at.load.weight(at.t);
     part = {at.b, at.h, at.t, at.off, min(weight, at.off + (at.stop - at.pos)), weight};
-    if (weight <= p.least_weight) part.to = weight;
+    if (weight <= p.cut_from) part.to = weight;
     at.pos += part.to - part.from;
     at.off = 0;
     if (part.to == weight && ++at.t == at.load.tiles) {
@@ -181,7 +173,7 @@ __device__ __forceinline__ bool next_part(const AttendParams& p, Place& at, Part
         } while (at.load.tiles == 0 && at.b + 1 < p.c.batch);
       }
     }
-    if (weight > p.least_weight || part.from == 0) return true;
+    if (weight > p.cut_from || part.from == 0) return true;
   }
   return false;
 }
@@ -189,13 +181,55 @@ __device__ __forceinline__ bool next_part(const AttendParams& p, Place& at, Part
 // What the join has to know about the border between shares w - 1 and w: written by workgroup w, before its first part.
 // parts 0: no segment is cut there, or it was cut at an earlier border already.
 __device__ __forceinline__ void write_border(const AttendParams& p, const Place& at, int w) {
-  if (!p.borders || threadIdx.x != 0 || w >= p.workgroups) return;
+  if (!p.borders || threadIdx.x != 0) return;
   Border x{at.b, at.h, at.t, 0};
-  if (!at.whole && at.pos < at.stop && at.off > 0 && at.off <= at.share) {
+  if (at.pos < at.stop && at.off > 0 && at.off <= at.share) {
     const long long weight = at.load.weight(at.t);
-    if (weight > p.least_weight) x.parts = 1 + static_cast<int>((weight - at.off + at.share - 1) / at.share);
+    if (weight > p.cut_from) x.parts = 1 + static_cast<int>((weight - at.off + at.share - 1) / at.share);
   }
   p.borders[w] = x;
+}
+
+// The other way to deal, for large tiles: a workgroup takes one piece, and pieces come as workgroups become free.  A segment
+// is one piece where there are segments enough to fill the chip evenly (whole_from), otherwise as many as its request's mean
+// weight is shares (`workgroups` of them, none lighter than least_weight).  Parts are fewer than on the line, and the tile
+// loop needs no registers for a place on it.  The last tiles come first: with a causal limit they are the heaviest.
+// Pieces of a segment lie H workgroups apart.
+template <int ROWS, int KEYS>
+__device__ __forceinline__ bool find_piece(const AttendParams& p, int w, Scratch& scratch, Part& part) {
+  const Cache& c = p.c;
+  auto load = [&](int b) { return load_of<ROWS, KEYS>(p, c.q_start[b], c.q_start[b + 1], c.lens[b]); };
+  auto weight = [&](int b) {
+    const Load l = load(b);
+    return l.upto(l.tiles) * c.H;
+  };
+  auto segments = [&](int b) { return static_cast<long long>(load(b).tiles) * c.H; };
+  long long total, count;
+  block_scan(own_cost(c.batch, weight), scratch.sums, total);
+  block_scan(own_cost(c.batch, segments), scratch.more_sums, count);
+  const long long share = count >= p.whole_from || !p.borders ? total + 1 : max((total + p.workgroups - 1) / p.workgroups, static_cast<long long>(p.least_weight));
+  auto cuts = [&](const Load& l) {
+    return l.tiles ? static_cast<int>((l.upto(l.tiles) / l.tiles + share - 1) / share) : 0;
+  };
+  auto pieces = [&](int b) {
+    const Load l = load(b);
+    return static_cast<long long>(l.tiles) * cuts(l) * c.H;
+  };
+  const long long mine = own_cost(c.batch, pieces);
+  long long all, first;
+  const long long upto = block_scan(mine, scratch.sums, all);
+  if (p.borders && threadIdx.x == 0) p.borders[w].parts = 0;
+  if (w >= all) return false;
+  part.b = find_request_at(w, c.batch, upto, mine, pieces, scratch, first);
+  const Load l = request_load<ROWS, KEYS>(p, part.b);
+  const int n = cuts(l), rel = static_cast<int>(w - first), i = rel / c.H, tile = i / n;
+  part.h = rel - i * c.H;
+  part.t = l.tiles - 1 - tile;
+  part.from = i - tile * n;
+  part.to = part.from + 1;
+  part.weight = n;
+  if (p.borders && threadIdx.x == 0 && n > 1 && part.from == 0) p.borders[w] = Border{part.b, part.h, part.t, n};
+  return true;
 }
 
 // Steps of a part, of the `steps` that the segment turned out to take.
