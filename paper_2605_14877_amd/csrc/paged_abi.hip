@@ -145,7 +145,7 @@ Workspace workspace_of(const heatkv_paged_shape* s, const heatkv::paged::Plan& p
 
 heatkv::paged::Plan plan_of(const heatkv_paged_shape* s, int64_t tokens, int top) {
   return heatkv::paged::plan_launches(s->dtype == HEATKV_BF16, s->batch, s->kv_heads, s->q_heads / s->kv_heads, tokens,
-                                      int64_t(s->max_pages) * s->page_size, int64_t(top) * s->page_size);
+                                      s->max_pages, s->page_size, top);
 }
 
 int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const void* k_pages, const void* v_pages,

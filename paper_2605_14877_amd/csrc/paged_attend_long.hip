@@ -6,12 +6,15 @@
 // copies and operand layouts are those of tile_lds.h.  Rows behind the request's end arrive as zeros (range-checked
 // copies), keys that a row does not see get a score of -inf in the tiles where that can be.
 // 8-bit cache rows come through registers, converted on the way into the stage.
+// Chosen pages: the walk is over the union of the pages that the workgroup's tokens have chosen (up to 128 of them, neighbours in
+// the request, which choose alike), with a word of 32 tokens for each wavefront and page; every tile is masked.
 //
 // Bound: the matrix pipe, and the vector work of the softmax next to it.
 #include <hip/hip_runtime.h>
 
 #include "kernels.h"
 #include "paged.h"
+#include "paged_rules.h"
 #include "paged_schedule.h"
 #include "paged_walk.h"
 #include "tile_lds.h"
@@ -40,6 +43,26 @@ __device__ __forceinline__ uint4 codes_to_chunk(unsigned lo, unsigned hi) {  // 
 // Where the four granules of a tile lie, in granules of the cache (there are less than 2^31, check_shape()).
 struct TileRows {
   int granule[4];
+  int pos[4];  // chosen pages: position of the first key
+};
+
+// The union of a tile's chosen pages, in LDS behind the stages: `count`, a bit for each page of the request, how many there are
+// in the words before, and for each page of the union where it lies (granule of the cache), its first position / page size, and
+// who has chosen it.
+struct Union {
+  int* count;
+  unsigned* bits;
+  int *before, *granule, *page;
+  unsigned* who;  // [pages][4]: bit i = token i of the wavefront's tokens
+  __device__ __forceinline__ Union(char* lds, int max_pages, int capacity) {
+    const int words = (max_pages + 31) / 32;
+    count = reinterpret_cast<int*>(lds);
+    bits = reinterpret_cast<unsigned*>(lds + 16);
+    before = reinterpret_cast<int*>(bits + words);
+    granule = before + words;
+    page = granule + capacity;
+    who = reinterpret_cast<unsigned*>(page + capacity);
+  }
 };
 
 __device__ __forceinline__ const __attribute__((address_space(3))) char* lds_pointer(int at) {
@@ -50,6 +73,7 @@ struct Shared {
   Scratch scratch;
   Part piece;
 };
+constexpr size_t kUnionAt = (sizeof(Shared) + 15) / 16 * 16;  // behind the stages
 
 // The launch's arguments, loaded anew.
 __device__ __forceinline__ const AttendParams& arguments() {
@@ -58,7 +82,50 @@ __device__ __forceinline__ const AttendParams& arguments() {
   return *(const AttendParams*)at;
 }
 
-template <int D, bool FP8>
+// Fills the union, by all lanes; returns its size.  Entries of a token lie H * top apart.
+__device__ __forceinline__ int build_union(const AttendParams& a, const Tile& t, int h, int j_first, int j_last, int seen_last,
+                                           const Union& u, int capacity) {
+  const Cache& c = a.c;
+  const int tid = threadIdx.x, words = (c.max_pages + 31) / 32, per_log2 = c.page_log2 - 4;
+  for (int i = tid; i < words; i += 256) u.bits[i] = 0;
+  for (int i = tid; i < 4 * capacity; i += 256) u.who[i] = 0;
+  __syncthreads();
+  const int seen = (seen_last + (1 << c.page_log2) - 1) >> c.page_log2, entries = (j_last - j_first + 1) * a.top;
+  auto entry = [&](int i, int& token) {
+    token = i / a.top;
+    const int x = a.selected[((static_cast<long long>(t.q0) + j_first + token) * c.H + h) * a.top + i - token * a.top];
+    return x < seen ? x : -1;
+  };
+  for (int i = tid; i < entries; i += 256) {
+    int token;
+    const int x = entry(i, token);
+    if (x >= 0) atomicOr(&u.bits[x >> 5], 1u << (x & 31));
+  }
+  __syncthreads();
+  if (tid < 64) {
+    const int total = scan_bits(u.bits, u.before, words, tid);
+    if (tid == 0) *u.count = total;
+  }
+  __syncthreads();
+  for (int i = tid; i < entries; i += 256) {
+    int token;
+    const int x = entry(i, token);
+    if (x < 0) continue;
+    const int at = u.before[x >> 5] + __popc(u.bits[x >> 5] & ((1u << (x & 31)) - 1));
+    const unsigned e = min(static_cast<unsigned>(c.table[static_cast<long long>(t.b) * c.max_pages + x]),
+                           static_cast<unsigned>(c.num_pages - 1));
+    u.page[at] = x;
+    u.granule[at] = (static_cast<int>(e) * c.H + h) << per_log2;
+    // the wavefronts that have rows of the token: one, or two where the group does not divide 32
+    const int row = (j_first + token) * c.G - t.row0, first = max(row, 0) / 32, last = min(row + c.G - 1, BM - 1) / 32;
+    for (int w = first; w <= last; ++w)
+      atomicOr(&u.who[4 * at + w], 1u << (j_first + token - divide(t.row0 + 32 * w, c.div_G)));
+  }
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(*u.count);
+}
+
+template <int D, bool FP8, bool CHOSEN>
 __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams p) {
   constexpr int RB = 2 * D, TILE_BYTES = BN * RB, SRC = FP8 ? D : RB;
   constexpr int NK = D / 16, NV = D / 32;
@@ -103,7 +170,15 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
                     uniform(shared.piece.weight)};
     const Tile tl = tile_of<BM>(a.c, part);
     const int h = part.h;
-    const int steps = (visible_keys(a.c, tl, divide(tl.row0 + tl.rows - 1, a.c.div_G)) + BN - 1) / BN;
+    const int j_first = divide(tl.row0, a.c.div_G), j_last = divide(tl.row0 + tl.rows - 1, a.c.div_G);
+    const int seen_last = visible_keys(a.c, tl, j_last);
+    const int capacity = CHOSEN ? many_capacity(a.c, a.top) : 0;
+    const Union chosen(paged_long_lds + 4 * TILE_BYTES + kUnionAt, a.c.max_pages, capacity);
+    int steps = (seen_last + BN - 1) / BN, n_pages = 0;
+    if constexpr (CHOSEN) {
+      n_pages = build_union(a, tl, h, j_first, j_last, seen_last, chosen, capacity);
+      steps = ((n_pages << (a.c.page_log2 - 4)) + 3) / 4;
+    }
     const int begin = steps_before(part.from, part.weight, steps), end = steps_before(part.to, part.weight, steps);
 
     // Rows of this wavefront; one without rows still copies its share of the tiles.
@@ -112,7 +187,8 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     const int limit_min = w_row + 32 <= tl.rows ? visible_keys(a.c, tl, divide(tl.row0 + w_row, a.c.div_G)) : 0;
     const int limit_max = active ? visible_keys(a.c, tl, divide(tl.row0 + min(w_row + 31, tl.rows - 1), a.c.div_G)) : 0;
     // Tiles that this wavefront has to do with.
-    const int my_end = min(end, (limit_max + BN - 1) / BN);
+    const int my_end = CHOSEN ? (active ? end : begin) : min(end, (limit_max + BN - 1) / BN);
+    [[maybe_unused]] const int w_first = divide(tl.row0 + w_row, a.c.div_G);  // the wavefront's token 0
     struct Row {
       int j, hq;  // token of the request, query head
       bool real;
@@ -122,6 +198,7 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
       return Row{j, h * a.c.G + row - j * a.c.G, w_row + n < tl.rows};
     };
     const Row my = row_of(a);
+    [[maybe_unused]] const int token = my.j - w_first;
     const int limit = my.real ? visible_keys(a.c, tl, my.j) : 0;
     // Table row of the request; page size in granules.
     const int* const table = a.c.table + static_cast<long long>(tl.b) * a.c.max_pages;
@@ -130,6 +207,12 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
       TileRows r;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
+        if constexpr (CHOSEN) {
+          const int g = 4 * it + i, u = min(g >> per_log2, n_pages - 1), off = g & ((1 << per_log2) - 1);
+          r.granule[i] = __builtin_amdgcn_readfirstlane(chosen.granule[u]) + off;
+          r.pos[i] = (g >> per_log2) < n_pages ? ((__builtin_amdgcn_readfirstlane(chosen.page[u]) << per_log2) + off) * 16 : 1 << 30;
+          continue;
+        }
         const int x = min(4 * it + i, max(tl.len - 1, 0) >> 4);  // granule of the request
         const unsigned e = min(static_cast<unsigned>(uniform_load(table, x >> per_log2)), static_cast<unsigned>(last_page));
         r.granule[i] = ((static_cast<int>(e) * heads + h) << per_log2) + (x & ((1 << per_log2) - 1));
@@ -145,13 +228,15 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     }
 
     // A tile behind the part's end has no rows: its copies touch no memory.
-    const int stop = min(tl.len, end * BN);
+    const int stop = CHOSEN ? tl.len : min(tl.len, end * BN);
     // bf16 rows: copy i of this wavefront of a K or V tile covers rows (64 / CPT) i + (16 / CPT) wave and on, all of one
     // granule; rows behind the request's end arrive as zeros (a probability of 0 does not remove an infinity).
     auto source = [&](const char* pages, const TileRows& at, int it, int i) {
       constexpr int PER = 64 / CPT;                        // rows between copies of a wavefront
       const int ahead = PER == 16 ? 0 : 16 * (wave >> 1);  // rows of the lane offset that belong to the granule's place
-      const int left = stop - it * BN - PER * i;           // valid rows from those of the lane offset's row 0 on
+      const int gr = PER == 16 ? i : 2 * i;                // granule of the lane offset's row 0, but for `ahead`
+      const int left = CHOSEN ? (it < end ? stop + ahead - (PER == 16 ? at.pos[gr] : wave >> 1 ? at.pos[gr + 1] : at.pos[gr]) : 0)
+                              : stop - it * BN - PER * i;  // valid rows from those of the lane offset's row 0 on
       const int from = PER == 16 ? at.granule[i] : wave >> 1 ? at.granule[2 * i + 1] : at.granule[2 * i];
       return tile::tile_descriptor<RB>(pages + (static_cast<long long>(from) * 16 - ahead) * RB, left > ahead ? left : 0);
     };
@@ -171,7 +256,11 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
         const int from = D == 128 ? (wave >> 1 ? at.granule[2 * i + 1] : at.granule[2 * i])
                                   : wave >> 1 ? (wave & 1 ? at.granule[3] : at.granule[2]) : (wave & 1 ? at.granule[1] : at.granule[0]);
         raw[i] = make_uint4(0, 0, 0, 0);
-        if (it * BN + r < stop) raw[i] = ldg16(pages + (static_cast<long long>(from) * 16 + (r & 15)) * SRC + (tid % LPR) * 16);
+        const int pos = !CHOSEN ? it * BN + (r & ~15)
+                        : it >= end ? 1 << 30
+                        : D == 128  ? (wave >> 1 ? at.pos[2 * i + 1] : at.pos[2 * i])
+                                    : wave >> 1 ? (wave & 1 ? at.pos[3] : at.pos[2]) : (wave & 1 ? at.pos[1] : at.pos[0]);
+        if (pos + (r & 15) < stop) raw[i] = ldg16(pages + (static_cast<long long>(from) * 16 + (r & 15)) * SRC + (tid % LPR) * 16);
       }
     };
     auto store_codes = [&](char* stage, const uint4 (&raw)[CPL], auto is_v) {
@@ -246,6 +335,21 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     };
     // Masks what a row of tile `it` does not see; whether there may be such.
     auto mask = [&](int it, f32x16 (&s)[2]) {
+      if constexpr (CHOSEN) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {  // s[i / 2][8 (i % 2) + r] is key 8 (r / 4) + 4 hl + r % 4 of granule i
+          const int g = 4 * it + i, u = min(g >> per_log2, n_pages - 1), off = g & ((1 << per_log2) - 1);
+          const int pos = ((chosen.page[u] << per_log2) + off) * 16;
+          const bool sees = (g >> per_log2) < n_pages && (chosen.who[4 * u + wave] >> token & 1);
+          int lim = (sees ? limit - pos : 0) - 4 * hl;
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            const int at = 8 * (i & 1) + r;
+            s[i >> 1][at] = 8 * (r >> 2) + (r & 3) < lim ? s[i >> 1][at] : -INFINITY;
+          }
+        }
+        return true;
+      }
       if (it * BN + BN <= limit_min) return false;
       tile::mask_rows(limit - it * BN, hl, s);
       return true;
@@ -473,21 +577,26 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
   }
 }
 
-template <int D, bool FP8>
+template <int D, bool FP8, bool CHOSEN>
 hipError_t launch(const AttendParams& p, hipStream_t stream) {
-  constexpr size_t lds = 4 * BN * 2 * D + sizeof(Shared);
+  const size_t lds = 4 * BN * 2 * D + kUnionAt + (CHOSEN ? many_union_bytes(p.c.G, p.c.max_pages, p.top) : 0);
   static std::atomic<unsigned long long> allowed{0};
   if (lds > 64 * 1024)
-    if (hipError_t e = allow_lds(reinterpret_cast<const void*>(&paged_attend_long_kernel<D, FP8>), lds, allowed)) return e;
-  hipLaunchKernelGGL((paged_attend_long_kernel<D, FP8>), dim3(p.grid), dim3(256), lds, stream, p);
+    if (hipError_t e = allow_lds(reinterpret_cast<const void*>(&paged_attend_long_kernel<D, FP8, CHOSEN>), MANY_LDS, allowed)) return e;
+  hipLaunchKernelGGL((paged_attend_long_kernel<D, FP8, CHOSEN>), dim3(p.grid), dim3(256), lds, stream, p);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_paged_attend_long(const PagedAttendParams& p, int d, bool fp8, hipStream_t stream) {
-  if (d == 128) return fp8 ? launch<128, true>(p, stream) : launch<128, false>(p, stream);
-  return fp8 ? launch<64, true>(p, stream) : launch<64, false>(p, stream);
+  static_assert(4 * BN * 2 * 128 + kUnionAt + MANY_UNION_BYTES <= MANY_LDS, "the largest union that plan_launches() sends here fits");
+  if (p.selected) {
+    if (d == 128) return fp8 ? launch<128, true, true>(p, stream) : launch<128, false, true>(p, stream);
+    return fp8 ? launch<64, true, true>(p, stream) : launch<64, false, true>(p, stream);
+  }
+  if (d == 128) return fp8 ? launch<128, true, false>(p, stream) : launch<128, false, false>(p, stream);
+  return fp8 ? launch<64, true, false>(p, stream) : launch<64, false, false>(p, stream);
 }
 
 }  // namespace heatkv

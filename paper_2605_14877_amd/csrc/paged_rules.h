@@ -24,16 +24,25 @@ struct Plan {
 // Requests of more query rows (new tokens x queries per kv head) than this are the 128-row kernel's.
 constexpr int MANY_ROWS = 64;
 
-// `longest`: keys that a request can have at most; `chosen`: keys that a token reads at most (0: all of them).
-inline Plan plan_launches(bool bf16, int batch, int kv_heads, int group, int64_t tokens, int64_t longest, int64_t chosen) {
+// LDS of the 128-row kernel for the union of its tokens' chosen pages: a bit and a count for each word of the request's pages,
+// 24 bytes for each page that may be in it.  Larger unions are left to the 16-row kernel, whose tiles have fewer tokens.
+constexpr size_t MANY_LDS = 160 * 1024, MANY_UNION_BYTES = 92 * 1024;
+inline size_t many_union_bytes(int group, int64_t max_pages, int64_t top) {
+  const int64_t capacity = std::min<int64_t>(max_pages, std::min(128, 127 / group + 2) * top);
+  return static_cast<size_t>(16 + (max_pages + 31) / 32 * 8 + capacity * 24);
+}
+
+// `top`: pages that a token reads at most, 0: all of them.
+inline Plan plan_launches(bool bf16, int batch, int kv_heads, int group, int64_t tokens, int64_t max_pages, int page_size, int64_t top) {
   Plan p;
-  const int64_t rows = tokens * group;
+  const int64_t rows = tokens * group, longest = max_pages * page_size;
   // Two workgroups to a compute unit are resident.  A segment of up to 8 steps is not cut (nor are they all where none is longer).
   p.few.workgroups = 512;
   p.few.grid = 512;
   p.few.least_steps = 8;
   p.few.parts = longest > 8 * 32 ? 2 * 512 : 0;
-  if (bf16 && chosen == 0 && rows > MANY_ROWS) {
+  // Little more than one token for each request: taken for a decoding step, whose few padding rows are not worth a launch.
+  if (bf16 && rows > MANY_ROWS && tokens > batch + 16 && (top == 0 || many_union_bytes(group, max_pages, top) <= MANY_UNION_BYTES)) {
     p.few.most_rows = p.many.least_rows = MANY_ROWS;
     p.many.workgroups = 512;
     p.many.least_steps = 8;

@@ -275,7 +275,7 @@ hipError_t launch(PagedSelectParams p, hipStream_t stream) {
   auto lds = [&](int tw) { return static_cast<size_t>(tw) * (4 * D + 4 * static_cast<size_t>(std::max(p.pitch, 2 * D))); };
   // Single tokens: one per workgroup, all of which ranks it.  Chunks: 16 tokens share a pass over the bounds, where their
   // scores fit into the LDS; fewer otherwise.
-  if (p.c.tokens <= p.c.batch || lds(4) > PAGED_SELECT_LDS) return launch<T, D, 1, WAVES>(p, lds(1), stream);
+  if (p.c.tokens <= 2 * p.c.batch + 16 || lds(4) > PAGED_SELECT_LDS) return launch<T, D, 1, WAVES>(p, lds(1), stream);
   if (lds(16) > 80 * 1024) return launch<T, D, 4, 1>(p, lds(4), stream);
   return launch<T, D, 16, 1>(p, lds(16), stream);
 }

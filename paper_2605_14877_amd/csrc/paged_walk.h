@@ -34,6 +34,28 @@ inline size_t walk_lds_bytes(const AttendParams& p) {
   return 16 + (p.c.max_pages + 31) / 32 * 8 + static_cast<size_t>(walk_capacity(p)) * 8;
 }
 
+// before[i] = bits set in the words in front of word i; returns how many there are.  By one wavefront.
+__device__ __forceinline__ int scan_bits(const unsigned* bits, int* before, int words, int lane) {
+  int sum = 0;
+  for (int i = lane; i - lane < words; i += 64) {
+    const int n = i < words ? __popc(bits[i]) : 0;
+    int inc = n;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int u = __shfl_up(inc, d, 64);
+      if (lane >= d) inc += u;
+    }
+    if (i < words) before[i] = sum + inc - n;
+    sum += __shfl(inc, 63, 64);
+  }
+  return sum;
+}
+
+// Pages that the tokens of a tile of 128 rows can have chosen between them.
+__device__ __forceinline__ int many_capacity(const Cache& c, int top) {
+  return static_cast<int>(min(static_cast<long long>(c.max_pages), static_cast<long long>(min(128, 127 / c.G + 2)) * top));
+}
+
 template <bool CHOSEN>
 struct Walk;
 
@@ -90,19 +112,8 @@ struct Walk<true> {
     }
     __syncthreads();
     if (tid < 64) {
-      int sum = 0;
-      for (int i = tid; i - tid < words; i += 64) {
-        const int n = i < words ? __popc(bits[i]) : 0;
-        int inc = n;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-          const int u = __shfl_up(inc, d, 64);
-          if (tid >= d) inc += u;
-        }
-        if (i < words) before[i] = sum + inc - n;
-        sum += __shfl(inc, 63, 64);
-      }
-      if (tid == 0) *count = sum;
+      const int total = scan_bits(bits, before, words, tid);
+      if (tid == 0) *count = total;
     }
     __syncthreads();
     for (int i = tid; i < entries; i += 256) {

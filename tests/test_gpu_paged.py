@@ -438,3 +438,34 @@ def test_selections_of_any_content(dtype, group):
     sel[0][0], sel[1][1], sel[2][0] = [-1] * top, [3] * top, [24, 23, 22, 21, 20, 0]
     for causal in (True, False):
         p.check(causal, p.run(causal, _ints(sel)), sel)
+
+
+SPARSE_MANY = [
+    # dtype, q_heads, kv_heads, d, page, lens, new, top, first, last: tiles of 128 rows over the union of their tokens' pages
+    ("bf16", 1, 1, 128, 16, [900, 40], [200, 40], 6, 1, 2),
+    ("bf16", 6, 2, 64, 32, [700, 300, 33], [90, 64, 1], 4, 0, 1),
+    ("bf16", 32, 2, 128, 64, [1300, 70], [37, 9], 5, 1, 1),
+    ("bf16", 5, 1, 64, 256, [2100], [70], 3, 0, 1),
+    ("fp8", 4, 2, 128, 16, [400, 170], [100, 90], 5, 1, 2),
+    ("fp8", 3, 1, 64, 128, [1000, 5], [100, 5], 3, 1, 1),
+]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("case", SPARSE_MANY, ids=str)
+def test_choice_of_pages_of_chunks(case, causal):
+    test_choice_of_pages_and_attention_over_them(case, causal)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8"])
+@pytest.mark.parametrize("group,d", [(1, 64), (3, 128), (16, 64)])
+def test_selections_of_any_content_of_chunks(dtype, group, d):
+    p = Problem(dtype, 2 * group, 2, d, 16, [333, 100, 5], [150, 70, 1], seed=10)
+    top, r = 6, random.Random(4)
+    sel = [[[r.choice([-1, -7, 2 ** 31 - 1, r.randrange(0, 25), r.randrange(0, 25), r.randrange(0, 8)]) for _ in range(top)]
+            for _ in range(2)] for _ in range(p.tokens)]
+    sel[0][0], sel[1][1], sel[2][0] = [-1] * top, [3] * top, [24, 23, 22, 21, 20, 0]
+    for t in range(20, 150):
+        sel[t][1] = [-1] * top  # a tile without any page
+    for causal in (True, False):
+        p.check(causal, p.run(causal, _ints(sel)), sel)
