@@ -38,13 +38,83 @@ __device__ __forceinline__ unsigned ordered(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// The bar that `top` scores reach: those above it are taken, of those equal to it as many as are missing then, from the lowest
+// page on.  At least `top` scores are >= low, fewer are > high; count(x): how many are >= x.
+template <class Count>
+__device__ __forceinline__ unsigned bar_between(unsigned low, unsigned high, int top, const Count& count) {
+  while (low < high) {
+    const unsigned mid = low + (high - low + 1) / 2;
+    const int c = count(mid);
+    if (c == top) return mid - 1;  // exactly these
+    if (c > top)
+      low = mid;
+    else
+      high = mid - 1;
+  }
+  return low;
+}
+
 template <int TW, int D>
 constexpr int digit_bytes() { return TW * 2 * 2 * D; }
 
-template <class T>
-__device__ __forceinline__ float query_value(T x) {
-  const float y = static_cast<float>(x);
-  return y == y ? fminf(fmaxf(y, -0x1p127f), 0x1p127f) : 0.f;
+// N consecutive query values (8 or 4, a multiple of 8 bytes).
+template <class T, int N>
+__device__ __forceinline__ void query_values(const T* p, float (&x)[N]) {
+  typedef T Pack __attribute__((ext_vector_type(N)));
+  const Pack y = *reinterpret_cast<const Pack*>(p);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float z = static_cast<float>(y[i]);
+    x[i] = z == z ? fminf(fmaxf(z, -0x1p127f), 0x1p127f) : 0.f;
+  }
+}
+
+// Ranks one token by one wavefront: up to 64 R scores, which stay in registers.
+template <int R>
+__device__ __forceinline__ void rank_token(const unsigned* key, int scan, int seen, int forced, int top, int* out, int lane) {
+  unsigned k[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) k[r] = 64 * r + lane < scan ? key[64 * r + lane] : 0;
+  auto count = [&](unsigned least) {
+    int c = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) c += __popcll(__ballot(k[r] >= least));
+    return c;
+  };
+  unsigned bar = 0;
+  if (seen > top) {
+    if (forced >= top) {
+      bar = FORCED - 1;
+    } else {
+      unsigned low = FORCED, high = 0;
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (k[r] != 0 && k[r] != FORCED) {
+          low = min(low, k[r]);
+          high = max(high, k[r]);
+        }
+#pragma unroll
+      for (int m = 1; m < 64; m *= 2) {
+        low = min(low, static_cast<unsigned>(__shfl_xor(static_cast<int>(low), m, 64)));
+        high = max(high, static_cast<unsigned>(__shfl_xor(static_cast<int>(high), m, 64)));
+      }
+      low = __builtin_amdgcn_readfirstlane(low);
+      high = __builtin_amdgcn_readfirstlane(high);
+      bar = bar_between(low, high, top, count);
+    }
+  }
+  int ties = bar == 0 ? 0 : top - count(bar + 1), n = 0;
+  const unsigned long long before = (1ull << lane) - 1;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const unsigned long long equal = __ballot(k[r] == bar);
+    const bool take = k[r] > bar || (k[r] == bar && __popcll(equal & before) < ties);
+    const unsigned long long taken = __ballot(take);
+    if (take) out[n + __popcll(taken & before)] = 64 * r + lane;
+    n += __popcll(taken);
+    ties -= min(ties, static_cast<int>(__popcll(equal)));
+  }
+  for (int i = n + lane; i < top; i += 64) out[i] = -1;
 }
 
 // WPT wavefronts rank a token.
@@ -74,11 +144,13 @@ __global__ __launch_bounds__(LANES) void paged_select_kernel(PagedSelectParams p
     const bool real = token < tile.rows;
     const T* q = static_cast<const T*>(p.q.data) + (tile.q0 + tile.row0 + (real ? token : 0)) * p.q.token_stride +
                  static_cast<long long>(h) * p.c.G * p.q.head_stride + col;
-    float amax = 0.f;
+    float amax = 0.f, x[COLS];
     if (real)
-      for (int g = part; g < p.c.G; g += PARTS)
+      for (int g = part; g < p.c.G; g += PARTS) {
+        query_values(q + g * p.q.head_stride, x);
 #pragma unroll
-        for (int i = 0; i < COLS; ++i) amax = fmaxf(amax, fabsf(query_value(q[g * p.q.head_stride + i])));
+        for (int i = 0; i < COLS; ++i) amax = fmaxf(amax, fabsf(x[i]));
+      }
 #pragma unroll
     for (int m = 1; m < 16; m *= 2) amax = fmaxf(amax, __shfl_xor(amax, m, 64));
     if (tid % 16 == 0) atomicMax(&amax_bits[token], __float_as_uint(amax));  // not negative: ordered as their bits
@@ -88,13 +160,15 @@ __global__ __launch_bounds__(LANES) void paged_select_kernel(PagedSelectParams p
 #pragma unroll
     for (int i = 0; i < COLS; ++i) up[i] = down[i] = 0;
     if (real)
-      for (int g = part; g < p.c.G; g += PARTS)
+      for (int g = part; g < p.c.G; g += PARTS) {
+        query_values(q + g * p.q.head_stride, x);
 #pragma unroll
         for (int i = 0; i < COLS; ++i) {
-          const int code = static_cast<int>(rintf(ldexpf(query_value(q[g * p.q.head_stride + i]), -e)));
+          const int code = static_cast<int>(rintf(ldexpf(x[i], -e)));
           up[i] += max(code, 0);
           down[i] += max(-code, 0);
         }
+      }
 #pragma unroll
     for (int i = 0; i < COLS; ++i) {
       atomicAdd(&sums[token * 2 * D + col + i], up[i]);
@@ -163,12 +237,30 @@ __global__ __launch_bounds__(LANES) void paged_select_kernel(PagedSelectParams p
   }
   __syncthreads();
 
-  // Ranking.
+  // Ranking: a wavefront per token where the scores fit into its registers.
   const int scan = (pages_all + 15) / 16 * 16;
+  auto output = [&](int token) {
+    return p.selected + (static_cast<long long>(tile.q0 + tile.row0 + token) * p.c.H + h) * p.top;
+  };
+  auto forced_of = [&](int seen) { return min(seen, p.first) + max(0, min(p.last, seen - p.first)); };
+  if (scan <= 1024) {
+    for (int token = wave; token < tile.rows; token += WAVES) {
+      const unsigned* key = keys + token * pitch;
+      const int seen = pages_seen(token), forced = forced_of(seen);
+      if (scan <= 128)
+        rank_token<2>(key, scan, seen, forced, p.top, output(token), lane);
+      else if (scan <= 320)
+        rank_token<5>(key, scan, seen, forced, p.top, output(token), lane);
+      else if (scan <= 512)
+        rank_token<8>(key, scan, seen, forced, p.top, output(token), lane);
+      else
+        rank_token<16>(key, scan, seen, forced, p.top, output(token), lane);
+    }
+    return;
+  }
   for (int token = wave / WPT; token < tile.rows; token += WAVES / WPT) {
     const unsigned* key = keys + token * pitch;
-    const int seen = pages_seen(token);
-    const int forced = min(seen, p.first) + max(0, min(p.last, seen - p.first));
+    const int seen = pages_seen(token), forced = forced_of(seen);
     // Sum of a count over the lanes that rank this token; the same number on all of them.
     int turn = 0;
     auto total = [&](unsigned c) {
@@ -187,7 +279,6 @@ __global__ __launch_bounds__(LANES) void paged_select_kernel(PagedSelectParams p
       for (int i = sub; i - lane < scan; i += stride) c += __popcll(__ballot(i < scan && key[i] >= least));
       return total(c);
     };
-    // `bar`: keys above it are taken, those equal to it from the lowest page on until `top` are.
     unsigned bar = 0;
     if (seen > p.top) {
       if (forced >= p.top) {
@@ -219,42 +310,26 @@ __global__ __launch_bounds__(LANES) void paged_select_kernel(PagedSelectParams p
           }
           __syncthreads();
         }
-        // at least `top` keys are >= low, fewer than `top` are > high
-        while (low < high) {
-          const unsigned mid = low + (high - low + 1) / 2;
-          const int c = count_from(mid);
-          if (c == p.top) {
-            low = mid;
-            high = 0;  // exactly these: no key is equal to mid - 1 and wanted
-            break;
-          }
-          if (c > p.top)
-            low = mid;
-          else
-            high = mid - 1;
-        }
-        bar = high == 0 ? low - 1 : low;
+        bar = bar_between(low, high, p.top, count_from);
       }
     }
     // In page order, by one wavefront.
     if (WPT > 1 && wave > 0) continue;
     int above = 0;
     for (int i = lane; i - lane < scan; i += 64) above += __popcll(__ballot(i < scan && key[i] > bar));
-    int ties = p.top - above, out = 0;
-    if (bar == 0) ties = 0;
-    const long long at = (static_cast<long long>(tile.q0 + tile.row0 + token) * p.c.H + h) * p.top;
+    int ties = bar == 0 ? 0 : p.top - above, n = 0;
+    int* const out = output(token);
     const unsigned long long before = (1ull << lane) - 1;
     for (int i = lane; i - lane < scan; i += 64) {
       const unsigned k = i < scan ? key[i] : 0;
       const unsigned long long equal = __ballot(i < scan && k == bar);
       const bool take = i < scan && (k > bar || (k == bar && __popcll(equal & before) < ties));
       const unsigned long long taken = __ballot(take);
-      const int place = out + __popcll(taken & before);
-      if (take && place < p.top) p.selected[at + place] = i;
-      out += __popcll(taken);
-      ties -= min(ties, __popcll(equal));
+      if (take) out[n + __popcll(taken & before)] = i;
+      n += __popcll(taken);
+      ties -= min(ties, static_cast<int>(__popcll(equal)));
     }
-    for (int i = out + lane; i < p.top; i += 64) p.selected[at + i] = -1;
+    for (int i = n + lane; i < p.top; i += 64) out[i] = -1;
   }
 }
 
@@ -273,11 +348,15 @@ template <class T, int D>
 hipError_t launch(PagedSelectParams p, hipStream_t stream) {
   p.pitch = (p.c.max_pages + 15) / 16 * 16;
   auto lds = [&](int tw) { return static_cast<size_t>(tw) * (4 * D + 4 * static_cast<size_t>(std::max(p.pitch, 2 * D))); };
-  // Single tokens: one per workgroup, all of which ranks it.  Chunks: 16 tokens share a pass over the bounds, where their
-  // scores fit into the LDS; fewer otherwise.
-  if (p.c.tokens <= 2 * p.c.batch + 16 || lds(4) > PAGED_SELECT_LDS) return launch<T, D, 1, WAVES>(p, lds(1), stream);
-  if (lds(16) > 80 * 1024) return launch<T, D, 4, 1>(p, lds(4), stream);
-  return launch<T, D, 16, 1>(p, lds(16), stream);
+  // Tokens of a request share a pass over the bounds, as many as leave four workgroups for every compute unit, and whose scores
+  // fit into the LDS.  Little more than one token for each request: one per workgroup.  1024 tokens of 4 kv heads over 272
+  // pages, 16, 4 and 1 tokens: 47, 26 and 33 us.
+  const long long units = static_cast<long long>(p.c.tokens) * p.c.H;
+  if (p.c.tokens > 2 * p.c.batch + 16) {
+    if (units >= 16 * 1024 && lds(16) <= 80 * 1024) return launch<T, D, 16, 1>(p, lds(16), stream);
+    if (units >= 4 * 1024 && lds(4) <= PAGED_SELECT_LDS) return launch<T, D, 4, 1>(p, lds(4), stream);
+  }
+  return launch<T, D, 1, WAVES>(p, lds(1), stream);
 }
 
 }  // namespace
