@@ -130,6 +130,13 @@ struct AttendParams {
   Border* borders;  // of each workgroup; null: nothing can be cut
 };
 
+// The launch's arguments, loaded anew.
+__device__ __forceinline__ const AttendParams& arguments() {
+  auto* at = (const __attribute__((address_space(4))) AttendParams*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("; arguments" : "+s"(at));
+  return *(const AttendParams*)at;
+}
+
 struct SelectParams {
   Cache c, tokens_as_rows;  // the second with G = 1: tiles of tokens
   Rows q;

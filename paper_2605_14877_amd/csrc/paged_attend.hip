@@ -18,6 +18,7 @@
 #include "f32_mfma.h"
 #include "kernels.h"
 #include "paged.h"
+#include "paged_redo.h"
 #include "paged_schedule.h"
 #include "paged_walk.h"
 
@@ -44,7 +45,7 @@ __device__ __forceinline__ bf16x8 codes_to_bf16(unsigned lo, unsigned hi) {
 }
 
 template <int D, bool FP8, bool CHOSEN>
-__global__ __launch_bounds__(64 * WAVES) void paged_attend_kernel(AttendParams p) {
+__global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_kernel(AttendParams p) {
   constexpr int NK = D / 32, NV = D / 16;            // MFMA steps of a score, accumulator blocks of 16 columns
   constexpr int RB = 2 * D;                          // bytes of a bf16 row in the V stage
   constexpr int SRC = FP8 ? D : 2 * D;               // bytes of a cache row
@@ -56,15 +57,15 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_kernel(AttendParams p
   char* const stage_all = paged_lds;                 // [WAVES] V stages, then the parked output tiles
   __shared__ float part_m[WAVES][16], part_l[WAVES][16];
 
-  __shared__ Scratch scratch;
+  __shared__ Line line;
+  __shared__ unsigned nan_rows;
 
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int w = blockIdx.x;
-  Place place = find_place<16, STEP>(p, w, scratch);
-  write_border(p, place, w);
+  line.start<16, STEP>(p, w);
   Part part;
-  while (next_part<16, STEP>(p, place, part)) {
+  while (line.advance<16, STEP>(p, part)) {
   const Tile tile = tile_of<16>(p.c, part);
   const int h = part.h;
 
@@ -79,7 +80,6 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_kernel(AttendParams p
   Walk<CHOSEN> walk(p, tile, h, j_first, j_last, limit_max, paged_lds + WAVES * stage_bytes(D), tid);
   const int steps = walk.steps();
   const int begin = steps_before(part.from, part.weight, steps), end = steps_before(part.to, part.weight, steps);
-  const bool alone = part.from == 0 && part.to == part.weight;  // no other workgroup has a part of this segment
 
   bf16x8 q[NK];
   {
@@ -228,6 +228,10 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_kernel(AttendParams p
     part_m[wave][n] = m;
     part_l[wave][n] = l;
   }
+  if (tid == 0) nan_rows = 0;
+  const Part done = line.stored();
+  const bool alone = done.from == 0 && done.to == done.weight;  // no other workgroup has a part of this segment
+  const long long part_base = part_rows<16>(w, done.from == 0);
   __syncthreads();
   float m_all = part_m[0][n], l_all = 0.f;
 #pragma unroll
@@ -248,7 +252,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_kernel(AttendParams p
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) ll += part_l[w][tid] * fast_exp2((part_m[w][tid] - ml) * c);
     if (!alone) {
-      float* to = p.part_ml + (part_rows<16>(w, part.from == 0) + tid) * 2;
+      float* to = p.part_ml + (part_base + tid) * 2;
       to[0] = ml;
       to[1] = ll;
     } else if (p.lse) {
@@ -266,8 +270,12 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_kernel(AttendParams p
       for (int w = 1; w < WAVES; ++w) x[k] += *reinterpret_cast<const f32x4*>(park + (w * 16 + r) * PITCH + col + 4 * k);
     }
     const int jr = divide(tile.row0 + r, p.c.div_G), hr = h * p.c.G + tile.row0 + r - jr * p.c.G;
+    bool nan = false;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) nan = nan || x[k >> 2][k & 3] != x[k >> 2][k & 3];
+    if (nan) atomicOr(&nan_rows, 1u << r);
     if (!alone) {
-      float* to = p.part_o + (part_rows<16>(w, part.from == 0) + r) * D + col;
+      float* to = p.part_o + (part_base + r) * D + col;
       *reinterpret_cast<f32x4*>(to) = x[0];
       *reinterpret_cast<f32x4*>(to + 4) = x[1];
     } else {
@@ -278,7 +286,33 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_kernel(AttendParams p
       *reinterpret_cast<bf16x8*>(to) = y;
     }
   }
-  __syncthreads();  // LDS is free for the next segment
+  __syncthreads();  // outputs are written; LDS is free for the next segment
+  for (unsigned rows = nan_rows; rows;) {  // paged_redo.h
+    const int r = __builtin_ctz(rows);
+    rows &= rows - 1;
+    if (r % WAVES != wave) continue;
+    const AttendParams& z = arguments();
+    const int jr = divide(tile.row0 + r, z.c.div_G), hr = h * z.c.G + tile.row0 + r - jr * z.c.G;
+    float m_row = part_m[0][r], l_row = 0.f;
+    for (int i = 1; i < WAVES; ++i) m_row = fmaxf(m_row, part_m[i][r]);
+    for (int i = 0; i < WAVES; ++i) l_row += part_l[i][r] * fast_exp2((part_m[i][r] - m_row) * c);
+    const float norm = !alone ? 1.f : l_row > 0.f ? 1.f / l_row : l_row;
+    redo_row<bf16_t, FP8, D>(
+        z, tile.q0 + jr, hr, visible_keys(z.c, tile, jr), 2 * begin, 2 * end,
+        [&](int gr) {
+          const Granule at = walk.locate(gr);
+          return RedoGranule{at.row, at.pos, walk.sees(at, jr - j_first)};
+        },
+        [&](float score) { return fast_exp2((score - m_row) * c); },
+        [&](int col, float x) {
+          if (!alone)
+            z.part_o[(part_base + r) * D + col] = x;
+          else
+            (static_cast<bf16_t*>(const_cast<void*>(z.out.data)) + (tile.q0 + jr) * z.out.token_stride + hr * z.out.head_stride)[col] =
+                static_cast<bf16_t>(x * norm);
+        });
+  }
+  if (CHOSEN) __syncthreads();  // the walk's tables are free as well
   }
 }
 

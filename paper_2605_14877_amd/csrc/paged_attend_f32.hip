@@ -8,6 +8,7 @@
 #include "f32_mfma.h"
 #include "kernels.h"
 #include "paged.h"
+#include "paged_redo.h"
 #include "paged_schedule.h"
 #include "paged_walk.h"
 
@@ -21,21 +22,21 @@ constexpr int WAVES = 4;
 extern __shared__ __attribute__((aligned(1024))) char paged_f32_lds[];
 
 template <int D, bool CHOSEN>
-__global__ __launch_bounds__(64 * WAVES) void paged_attend_f32_kernel(AttendParams p) {
+__global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_f32_kernel(AttendParams p) {
   constexpr int NB = D / 16, PITCH = D + 4;
   using Stage = f32m::KeyStage<D>;
   static_assert(16 * PITCH * 4 == stage_bytes(D) && Stage::BYTES <= stage_bytes(D), "the parked tiles take the stages' place");
   __shared__ float part_m[WAVES][16], part_l[WAVES][16];
 
-  __shared__ Scratch scratch;
+  __shared__ Line line;
+  __shared__ unsigned nan_rows;
 
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int w = blockIdx.x;
-  Place place = find_place<16, 2 * GRANULE>(p, w, scratch);
-  write_border(p, place, w);
+  line.start<16, 2 * GRANULE>(p, w);
   Part part;
-  while (next_part<16, 2 * GRANULE>(p, place, part)) {
+  while (line.advance<16, 2 * GRANULE>(p, part)) {
   const Tile tile = tile_of<16>(p.c, part);
   const int h = part.h;
 
@@ -48,7 +49,6 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_f32_kernel(AttendPara
   Walk<CHOSEN> walk(p, tile, h, j_first, j_last, limit_max, paged_f32_lds + WAVES * stage_bytes(D), tid);
   const int steps = walk.steps();
   const int begin = steps_before(part.from, part.weight, steps), end = steps_before(part.to, part.weight, steps);
-  const bool alone = part.from == 0 && part.to == part.weight;
 
   f32m::Rows<D> q, k;
   {
@@ -126,6 +126,10 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_f32_kernel(AttendPara
     part_m[wave][n] = m;
     part_l[wave][n] = l;
   }
+  if (tid == 0) nan_rows = 0;
+  const Part done = line.stored();
+  const bool alone = done.from == 0 && done.to == done.weight;  // no other workgroup has a part of this segment
+  const long long part_base = part_rows<16>(w, done.from == 0);
   __syncthreads();
   float m_all = part_m[0][n], l_all = 0.f;
 #pragma unroll
@@ -145,7 +149,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_f32_kernel(AttendPara
   if (wave == 0 && g == 0 && n < tile.rows) {
     const long long out_row = static_cast<long long>(tile.q0 + j) * p.c.Hq + hq;
     if (!alone) {
-      float* to = p.part_ml + (part_rows<16>(w, part.from == 0) + n) * 2;
+      float* to = p.part_ml + (part_base + n) * 2;
       to[0] = m_all;
       to[1] = l_all;
     } else if (p.lse) {
@@ -161,10 +165,37 @@ __global__ __launch_bounds__(64 * WAVES) void paged_attend_f32_kernel(AttendPara
     const int jr = divide(tile.row0 + r, p.c.div_G), hr = h * p.c.G + tile.row0 + r - jr * p.c.G;
     float* to = alone ? static_cast<float*>(const_cast<void*>(p.out.data)) + (tile.q0 + jr) * p.out.token_stride +
                             hr * p.out.head_stride + col
-                      : p.part_o + (part_rows<16>(w, part.from == 0) + r) * D + col;
+                      : p.part_o + (part_base + r) * D + col;
     *reinterpret_cast<f32x4*>(to) = x;
+    if (x[0] != x[0] || x[1] != x[1] || x[2] != x[2] || x[3] != x[3]) atomicOr(&nan_rows, 1u << r);
   }
-  __syncthreads();  // LDS is free for the next segment
+  __syncthreads();  // outputs are written; LDS is free for the next segment
+  for (unsigned rows = nan_rows; rows;) {  // paged_redo.h
+    const int r = __builtin_ctz(rows);
+    rows &= rows - 1;
+    if (r % WAVES != wave) continue;
+    const AttendParams& z = arguments();
+    const int jr = divide(tile.row0 + r, z.c.div_G), hr = h * z.c.G + tile.row0 + r - jr * z.c.G;
+    float m_row = part_m[0][r], l_row = 0.f;
+    for (int i = 1; i < WAVES; ++i) m_row = fmaxf(m_row, part_m[i][r]);
+    for (int i = 0; i < WAVES; ++i) l_row += part_l[i][r] * prob(part_m[i][r], m_row);
+    const float norm = !alone ? 1.f : l_row > 0.f ? 1.f / l_row : l_row;
+    redo_row<float, false, D>(
+        z, tile.q0 + jr, hr, visible_keys(z.c, tile, jr), 2 * begin, 2 * end,
+        [&](int gr) {
+          const Granule x = walk.locate(gr);
+          return RedoGranule{x.row, x.pos, walk.sees(x, jr - j_first)};
+        },
+        [&](float score) { return prob(score * prob.c, m_row) * 0x1p-8f; },
+        [&](int col, float x) {
+          if (!alone)
+            z.part_o[(part_base + r) * D + col] = x;
+          else
+            (static_cast<float*>(const_cast<void*>(z.out.data)) + (tile.q0 + jr) * z.out.token_stride + hr * z.out.head_stride)[col] =
+                x * norm;
+        });
+  }
+  if (CHOSEN) __syncthreads();  // the walk's tables are free as well
   }
 }
 

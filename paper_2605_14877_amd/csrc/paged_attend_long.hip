@@ -14,6 +14,7 @@
 
 #include "kernels.h"
 #include "paged.h"
+#include "paged_redo.h"
 #include "paged_rules.h"
 #include "paged_schedule.h"
 #include "paged_walk.h"
@@ -74,13 +75,6 @@ struct Shared {
   Part piece;
 };
 constexpr size_t kUnionAt = (sizeof(Shared) + 15) / 16 * 16;  // behind the stages
-
-// The launch's arguments, loaded anew.
-__device__ __forceinline__ const AttendParams& arguments() {
-  auto* at = (const __attribute__((address_space(4))) AttendParams*)__builtin_amdgcn_kernarg_segment_ptr();
-  asm volatile("; arguments" : "+s"(at));
-  return *(const AttendParams*)at;
-}
 
 // Fills the union, by all lanes; returns its size.  Entries of a token lie H * top apart.
 __device__ __forceinline__ int build_union(const AttendParams& a, const Tile& t, int h, int j_first, int j_last, int seen_last,
@@ -541,6 +535,12 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     const AttendParams& z = arguments();
     const Row out = row_of(z);
     const bool alone = uniform(shared.piece.weight) == 1;
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) nan = nan || o[i][r] != o[i][r];
+    const unsigned long long nan_lanes = __ballot(nan && out.real);
     if (out.real) {
       const long long token = tl.q0 + out.j, out_row = token * z.c.Hq + out.hq;
       const long long part_row = static_cast<long long>(w) * BM + w_row + n;
@@ -573,6 +573,36 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
             *reinterpret_cast<bf16x4*>(to + 32 * i + 8 * r) = y;
           }
       }
+    }
+    for (unsigned rows = static_cast<unsigned>(nan_lanes | nan_lanes >> 32); rows;) {  // paged_redo.h
+      const int r = __builtin_ctz(rows);
+      rows &= rows - 1;
+      wait_vmcnt<0>();  // the row's outputs from above come first
+      const int j = __builtin_amdgcn_readlane(out.j, r), hq = __builtin_amdgcn_readlane(out.hq, r);
+      const float m_row = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, m), r));
+      const float l_row = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, l), r));
+      const float norm = !alone ? 1.f : l_row > 0.f ? 1.f / l_row : l_row;
+      redo_row<bf16_t, FP8, D>(
+          z, tl.q0 + j, hq, visible_keys(z.c, tl, j), 4 * begin, 4 * end,
+          [&](int g) {
+            const TileRows rows_at = locate(g >> 2);
+            const int from = g & 2 ? (g & 1 ? rows_at.granule[3] : rows_at.granule[2]) : (g & 1 ? rows_at.granule[1] : rows_at.granule[0]);
+            int pos = 16 * g;
+            bool seen = true;
+            if constexpr (CHOSEN) {
+              pos = g & 2 ? (g & 1 ? rows_at.pos[3] : rows_at.pos[2]) : (g & 1 ? rows_at.pos[1] : rows_at.pos[0]);
+              seen = chosen.who[4 * min(g >> per_log2, n_pages - 1) + wave] >> (j - w_first) & 1;
+            }
+            return RedoGranule{static_cast<long long>(from) * 16, pos, seen};
+          },
+          [&](float score) { return fast_exp2((score - m_row) * c); },
+          [&](int col, float x) {
+            if (!alone)
+              z.part_o[(static_cast<long long>(w) * BM + w_row + r) * D + col] = x;
+            else
+              (static_cast<bf16_t*>(const_cast<void*>(z.out.data)) + (tl.q0 + j) * z.out.token_stride + hq * z.out.head_stride)[col] =
+                  static_cast<bf16_t>(x * norm);
+          });
     }
   }
 }

@@ -232,6 +232,39 @@ __device__ __forceinline__ bool find_piece(const AttendParams& p, int w, Scratch
   return true;
 }
 
+// A workgroup's place on the line and the part at hand, in LDS: the tile loops have no registers to spare for them.
+struct Line {
+  Scratch scratch;
+  Place place;
+  Part next;
+  int more;
+  template <int ROWS, int KEYS>
+  __device__ __forceinline__ void start(const AttendParams& p, int w) {
+    const Place at = find_place<ROWS, KEYS>(p, w, scratch);
+    write_border(p, at, w);
+    if (threadIdx.x == 0) place = at;
+  }
+  // False: there is no further part.  Between two calls: a barrier behind the last use of the first one's part.
+  template <int ROWS, int KEYS>
+  __device__ __forceinline__ bool advance(const AttendParams& p, Part& part) {
+    if (threadIdx.x == 0) {
+      Place at = place;
+      Part x{};
+      more = next_part<ROWS, KEYS>(p, at, x);
+      next = x;
+      place = at;
+    }
+    __syncthreads();
+    if (!__builtin_amdgcn_readfirstlane(more)) return false;
+    part = stored();
+    return true;
+  }
+  __device__ __forceinline__ Part stored() const {
+    return {__builtin_amdgcn_readfirstlane(next.b), __builtin_amdgcn_readfirstlane(next.h), __builtin_amdgcn_readfirstlane(next.t),
+            uniform(next.from), uniform(next.to), uniform(next.weight)};
+  }
+};
+
 // Steps of a part, of the `steps` that the segment turned out to take.
 __device__ __forceinline__ int steps_before(long long weight_before, long long weight, int steps) {
   return static_cast<int>(weight_before * steps / weight);

@@ -469,3 +469,70 @@ def test_selections_of_any_content_of_chunks(dtype, group, d):
         sel[t][1] = [-1] * top  # a tile without any page
     for causal in (True, False):
         p.check(causal, p.run(causal, _ints(sel)), sel)
+
+
+# ---- values that are not finite -----------------------------------------------------------------------------------------
+
+def _spoil(p, seed, last_only):
+    """Infinities and NaN in K and V of some tokens; `last_only`: of each request's last token, which only its own row sees."""
+    r = random.Random(seed)
+    for n, ids in zip(p.lens, p.table):
+        for x in ([n - 1] if last_only else sorted({n - 1, n // 3, r.randrange(n)}) if n else []):
+            page, row = ids[x // p.page], x % p.page
+            for pages, bad in ((p.v, (math.inf, -math.inf, math.nan)), (p.k, (math.nan, math.inf))):
+                for h in range(p.H):
+                    value = r.choice([b for b in bad if p.dtype != "fp8" or math.isnan(b)])  # E4M3 has no infinity
+                    x32 = pages[page, h, row].float()
+                    x32[r.randrange(p.d)] = value
+                    pages[page, h, row] = x32.to(pages.dtype)
+    p.dev["k"], p.dev["v"] = p.k.cuda(), p.v.cuda()
+
+
+def _check_with_nan(p, causal, got, chosen=None):
+    """Rows without such a key: as ever.  The others: NaN, or the same infinity."""
+    out, lse = got[0].cpu().double(), got[1].cpu().double()
+    want, want_lse, mag = ref.attend(p.q, p.k, p.v, p.table, p.q_start, p.lens, p.page, p.sm, causal, chosen)
+    real = p.q_start[-1]
+    out, want, mag = out[:real], want[:real], mag[:real]
+    fine = want.isfinite()
+    assert torch.equal(out.isfinite(), fine)
+    infinite = want.isinf()
+    assert torch.equal(out.isinf(), infinite) and torch.equal(out[infinite], want[infinite])
+    # as in Problem.check, with the scores' largest sum from the finite keys
+    r = w = 2.0 ** -8 if p.dtype != "f32" else 2.0 ** -24
+    k = torch.where(p.k.double().isfinite(), p.k.double(), 0.0).abs()
+    S = float(p.q[:real].abs().double().amax((0, 1)) @ k.amax((0, 1, 2))) * p.sm
+    e = 2.0 ** -24 * (p.d * S + 2 * 1.443 * 2 * S + max(p.lens) + 64)
+    off = (out - want).abs() - (mag * (2 * e + (r if p.dtype != "f32" else 0.0)) * (1 + 1e-6) + w * (want.abs() + mag * (2 * e + r)) + 1e-30)
+    off = off[fine & mag.isfinite()]
+    assert not off.numel() or float(off.max()) <= 0
+    return fine
+
+
+@pytest.mark.parametrize("case", [("bf16", 4, 2, 128, 16, [50, 33], [20, 5]), ("bf16", 2, 1, 64, 32, [400], [90]),
+                                  ("bf16", 6, 1, 128, 64, [700, 65], [40, 30]), ("fp8", 4, 2, 128, 16, [50, 300], [20, 70]),
+                                  ("fp8", 2, 1, 64, 16, [77], [30]), ("f32", 4, 2, 128, 16, [50, 33], [20, 5]),
+                                  ("f32", 2, 2, 64, 64, [700], [3]), ("bf16", 8, 1, 128, 16, [2000], [4])], ids=str)
+def test_values_that_a_row_does_not_see_do_not_reach_it(case):
+    p = Problem(*case, seed=11)
+    _spoil(p, 1, True)
+    fine = _check_with_nan(p, True, p.run(True))
+    last = [s - 1 for s in p.q_start[1:]]
+    assert fine[[t for t in range(p.q_start[-1]) if t not in last]].all() and not fine[last].all()
+    p = Problem(*case, seed=12)
+    _spoil(p, 2, False)
+    for causal in (True, False):
+        _check_with_nan(p, causal, p.run(causal))
+
+
+@pytest.mark.parametrize("case", [("bf16", 4, 2, 128, 16, [300, 33], [6, 5]), ("bf16", 4, 1, 64, 32, [400], [90]),
+                                  ("fp8", 4, 2, 128, 16, [50, 300], [20, 70]), ("f32", 4, 2, 128, 16, [300, 33], [20, 5])], ids=str)
+def test_pages_that_a_token_has_not_chosen_do_not_reach_it(case):
+    p = Problem(*case, seed=13)
+    _spoil(p, 3, False)
+    r = random.Random(5)
+    top = 4
+    sel = [[[r.randrange(0, 20) for _ in range(top)] for _ in range(p.H)] for _ in range(p.tokens)]
+    for causal in (True, False):
+        fine = _check_with_nan(p, causal, p.run(causal, _ints(sel)), sel)
+        assert fine.any() and not fine.all()
