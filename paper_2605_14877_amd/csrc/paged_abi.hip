@@ -326,10 +326,11 @@ int heatkv_paged_attend_selected(const heatkv_paged_shape* s, int64_t tokens, he
                                  const void* v_pages, const int32_t* table, const int32_t* q_start, const int32_t* lens,
                                  const int32_t* selected, int top, float sm_scale, int causal, heatkv_rows out, float* lse,
                                  void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_shape(s);
+  if (rc) return rc;
   if (top < 1 || top > kMaxTop) return fail(HEATKV_EINVAL, "top must be in [1, 512]");
-  if (s && s->max_pages > kMaxSelectPages) return fail(HEATKV_EINVAL, "chosen pages: requests of up to 32768 pages");
-  int rc = check_ints({selected});
-  if (rc && tokens != 0) return rc;
+  if (s->max_pages > kMaxSelectPages) return fail(HEATKV_EINVAL, "chosen pages: requests of up to 32768 pages");
+  if (tokens != 0 && (rc = check_ints({selected}))) return rc;
   return attend(s, tokens, q, k_pages, v_pages, table, q_start, lens, selected, top, sm_scale, causal, out, lse, ws, ws_bytes,
                 stream);
 }

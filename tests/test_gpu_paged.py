@@ -536,3 +536,244 @@ def test_pages_that_a_token_has_not_chosen_do_not_reach_it(case):
     for causal in (True, False):
         fine = _check_with_nan(p, causal, p.run(causal, _ints(sel)), sel)
         assert fine.any() and not fine.all()
+
+
+# ---- a server's steps ----------------------------------------------------------------------------------------------------
+
+class Server:
+    """Requests that come and go, all lengths on the device; the reference keeps every request's rows in lists."""
+
+    def __init__(self, dtype, q_heads, kv_heads, d, page, batch, num_pages, max_pages, tokens, top=5):
+        self.dtype, self.page, self.H, self.Hq, self.d, self.top = dtype, page, kv_heads, q_heads, d, top
+        self.tokens = tokens
+        self.shape = _shape(dtype, q_heads, kv_heads, d, page, num_pages, batch, max_pages)
+        store = torch.float8_e4m3fn if dtype == "fp8" else DT[dtype]
+        kw = dict(device="cuda", dtype=torch.int32)
+        self.k = torch.full(self.shape.pages_shape, math.nan, device="cuda").to(store)
+        self.v = self.k.clone()
+        self.bounds = torch.zeros(num_pages, kv_heads, 2, d, dtype=torch.int8, device="cuda")
+        self.scales = torch.zeros(num_pages, kv_heads, device="cuda")
+        self.keep, self.new, self.lens = (torch.zeros(batch, **kw) for _ in range(3))
+        self.ring, self.span = torch.arange(num_pages, **kw).flip(0).contiguous(), _ints([3, num_pages])
+        self.table, self.q_start = torch.full((batch, max_pages), -1, **kw), torch.zeros(batch + 1, **kw)
+        self.slots, self.status = torch.zeros(tokens, **kw), torch.zeros(1, **kw)
+        self.qkv = torch.zeros(tokens, q_heads + 2 * kv_heads, d, dtype=DT[dtype], device="cuda")
+        self.out, self.sparse_out = (torch.zeros(tokens, q_heads, d, dtype=DT[dtype], device="cuda") for _ in range(2))
+        self.lse = torch.zeros(tokens, q_heads, device="cuda")
+        self.selected = torch.zeros(tokens, kv_heads, top, **kw)
+        n = max(hk.paged_attend_workspace_bytes(self.shape, tokens, t) for t in (0, top))
+        self.ws = torch.zeros(max(n, 16), dtype=torch.uint8, device="cuda")
+        self.sm = 1.0 / math.sqrt(d)
+        self.rows = [[] for _ in range(batch)]  # (k, v) of every token that the reference holds
+
+    def launch(self):
+        sh, q = self.shape, self.qkv[:, :self.Hq]
+        hk.heatkv_paged_assign(sh, self.keep, self.new, self.lens, self.ring, self.span, self.table, self.q_start, self.slots,
+                               self.status)
+        hk.heatkv_paged_append(sh, self.slots, self.qkv[:, self.Hq:self.Hq + self.H], self.qkv[:, self.Hq + self.H:], self.k, self.v,
+                               self.bounds, self.scales)
+        hk.heatkv_paged_attend(sh, q, self.k, self.v, self.table, self.q_start, self.lens, self.sm, self.out, self.ws, lse=self.lse)
+        hk.heatkv_paged_select(sh, q, self.bounds, self.scales, self.table, self.q_start, self.lens, 1, 2, self.selected)
+        hk.heatkv_paged_attend_selected(sh, q, self.k, self.v, self.table, self.q_start, self.lens, self.selected, self.sm,
+                                        self.sparse_out, self.ws)
+
+    def load(self, keep, new, seed):
+        g = torch.Generator().manual_seed(seed)
+        self.cpu = torch.randn(self.qkv.shape, generator=g).to(self.qkv.dtype)
+        self.now = (keep, new)
+        self.keep.copy_(torch.tensor(keep, dtype=torch.int32))
+        self.new.copy_(torch.tensor(new, dtype=torch.int32))
+        self.qkv.copy_(self.cpu)
+        self.out.fill_(7.0)
+        self.sparse_out.fill_(7.0)
+        self.lse.fill_(7.0)
+
+    def check(self):
+        keep, new = self.now
+        assert self.status.item() == 0
+        p = Problem.__new__(Problem)
+        p.dtype, p.page, p.H, p.Hq, p.d, p.sm = self.dtype, self.page, self.H, self.Hq, self.d, self.sm
+        t = 0
+        for b, (c, n) in enumerate(zip(keep, new)):
+            del self.rows[b][c:]
+            for i in range(n):
+                x = self.cpu[t + i]
+                self.rows[b].append((ref.to_store(x[self.Hq:self.Hq + self.H], self.dtype == "fp8"),
+                                     ref.to_store(x[self.Hq + self.H:], self.dtype == "fp8")))
+            t += n
+        p.new, p.lens = new, [len(r) for r in self.rows]
+        assert self.lens.tolist() == p.lens
+        p.q_start = self.q_start.tolist()
+        held = [ref.pages_of(n, self.page) for n in p.lens]
+        table = self.table.tolist()
+        p.table = [r[:n] for r, n in zip(table, held)]
+        used = [x for r in p.table for x in r]
+        assert len(set(used)) == len(used)
+        head, count = self.span.tolist()
+        ring = self.ring.tolist()
+        assert sorted(used + [ring[(head + i) % len(ring)] for i in range(count)]) == list(range(len(ring)))
+        p.k, p.v = torch.zeros(self.k.shape).to(self.k.dtype), torch.zeros(self.k.shape).to(self.k.dtype)
+        for b, r in enumerate(self.rows):
+            for i, (k, v) in enumerate(r):
+                p.k[p.table[b][i // self.page], :, i % self.page] = k
+                p.v[p.table[b][i // self.page], :, i % self.page] = v
+        p.q = self.cpu[:, :self.Hq]
+        p.check(True, (self.out, self.lse))
+        # Bounds of pages whose tokens were dropped in part stay as they were until the page is written again: what the choice
+        # was made from is what the device holds.
+        sel = self.selected.tolist()
+        chosen = ref.select(p.q, self.bounds.cpu(), self.scales.cpu(), p.table, p.q_start, p.lens, self.page, 1, 2, self.top, True)
+        for t in range(p.q_start[-1]):
+            assert sel[t] == [x + [-1] * (self.top - len(x)) for x in chosen[t]]
+        want, _, _ = ref.attend(p.q, p.k, p.v, p.table, p.q_start, p.lens, self.page, self.sm, True, chosen)
+        got = self.sparse_out.cpu().double()
+        assert torch.all(got[p.q_start[-1]:] == 7.0)
+        p.check(True, (self.sparse_out, torch.where(torch.arange(self.tokens, device="cuda")[:, None] < p.q_start[-1],
+                                                    self._sparse_lse(p, chosen).cuda(), 7.0)), chosen)
+
+    def _sparse_lse(self, p, chosen):  # the call had no lse: the reference's, so that check() looks at the outputs
+        lse = torch.full((self.tokens, self.Hq), 7.0, dtype=torch.float64)
+        lse[:p.q_start[-1]] = ref.attend(p.q, p.k, p.v, p.table, p.q_start, p.lens, self.page, self.sm, True, chosen)[1][:p.q_start[-1]]
+        return lse
+
+
+STEPS = [([0, 0, 0, 0], [40, 0, 7, 90]), ([40, 0, 7, 90], [1, 33, 1, 1]), ([41, 33, 0, 80], [1, 1, 0, 5]), ([0, 34, 0, 85], [64, 1, 3, 1]),
+         ([64, 35, 3, 86], [1, 1, 1, 1]), ([65, 20, 4, 0], [1, 80, 1, 2])]
+
+
+@pytest.mark.parametrize("dtype,page", [("bf16", 16), ("fp8", 32), ("f32", 16)])
+def test_steps_of_a_server(dtype, page):
+    s = Server(dtype, 4, 2, 64, page, 4, 40, 12, 150)
+    for i, (keep, new) in enumerate(STEPS):
+        s.load(keep, new, i)
+        s.launch()
+        torch.cuda.synchronize()
+        s.check()
+
+
+def test_steps_of_a_server_replayed_from_a_graph():
+    # one captured step serves steps of any lengths; eager work and synchronizations in between
+    s = Server("bf16", 6, 2, 128, 16, 4, 40, 12, 150)
+    s.load(*STEPS[0], 0)
+    s.launch()
+    torch.cuda.synchronize()
+    s.check()
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        s.launch()
+    for i, (keep, new) in enumerate(STEPS[1:], 1):
+        s.load(keep, new, i)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        s.check()
+        other = Problem("bf16", 2, 1, 64, 16, [90, 200], [1, 70], seed=i)
+        other.check(True, other.run(True))
+
+
+def test_two_streams_with_a_workspace_each():
+    a, b = (Problem("bf16", 8, 2, 128, 16, [1900, 900, 30], [1, n, 2], seed=n) for n in (1, 90))
+    want = [p.run(True) for p in (a, b)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    ws = [torch.empty(max(hk.paged_attend_workspace_bytes(p.shape, p.tokens), 16), dtype=torch.uint8, device="cuda") for p in (a, b)]
+    outs = [[torch.full_like(p.dev["q"], 7.0) for p in (a, b)] for _ in range(6)]
+    torch.cuda.synchronize()
+    for turn in outs:
+        for p, s, w, out in zip((a, b), streams, ws, turn):
+            d = p.dev
+            if turn is outs[0]:
+                with torch.cuda.stream(s):
+                    hk.heatkv_paged_attend(p.shape, d["q"], d["k"], d["v"], d["table"], d["q_start"], d["lens"], p.sm, out, w)
+            else:  # the stream by its handle
+                hk.heatkv_paged_attend(p.shape, d["q"], d["k"], d["v"], d["table"], d["q_start"], d["lens"], p.sm, out, w,
+                                       stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    for turn in outs:
+        for out, x in zip(turn, want):
+            assert torch.equal(out, x[0])
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+def test_runs_of_a_pruned_layer_on_pages(dtype, d):
+    # HeatKV's cache as pages: every (batch row, head) pair is a request with one kv head; what it keeps of the prior scales and
+    # the current scale are its tokens, and every query of the scale sees all of them
+    import heatkv_inputs as hi
+    from oracle import heatkv_oracle as orc
+    t0, H, nb, page = [1, 4, 9, 30, 70], 3, 2, 16
+    cfg = dict(L=1, H=H, d=d, dtype=dtype, batch=nb, sides=[(1, n) for n in t0])
+    K, c, sm = len(t0), hi.cumulative_tokens(t0), 1.0 / math.sqrt(d)
+    w = hi.head_weights(3, 1, H, K)
+    q, k, v = hi.make_qkv(3, 0, cfg, w=w)
+    plan = hk.heatkv_build_schedule(hk.Shape(1, H, d, t0, nb, dtype), hi.expected_beta_from_weights(w, t0).astype("float32"),
+                                    H * c[-2] * 2 * d * hi.elem_bytes(dtype) // 2, 1)
+    kk = K - 1
+    cur = slice(c[kk] - t0[kk], c[kk])
+    kept = [plan.retained(kk, 0, h).tolist() for h in range(H)]
+    assert len({len(x) for x in kept}) > 1  # ragged
+    lens = [len(kept[h]) + t0[kk] for _ in range(nb) for h in range(H)]
+    max_pages = max(ref.pages_of(n, page) for n in lens)
+    shape = _shape(dtype, 1, 1, d, page, nb * H * max_pages, nb * H, max_pages)
+    rows = [[torch.cat([x[b, h, kept[h]], x[b, h, cur]]) for b in range(nb) for h in range(H)] for x in (k, v)]
+    table, q_start = torch.full((nb * H, max_pages), -1, dtype=torch.int32, device="cuda"), _ints([0] * (nb * H + 1))
+    slots, status, dev_lens = _ints([0] * sum(lens)), _ints([9]), _ints([0] * (nb * H))
+    ring, span = torch.arange(shape.num_pages, dtype=torch.int32, device="cuda"), _ints([0, shape.num_pages])
+    hk.heatkv_paged_assign(shape, _ints([0] * (nb * H)), _ints(lens), dev_lens, ring, span, table, q_start, slots, status)
+    kp, vp = (torch.zeros(shape.pages_shape, dtype=DT[dtype], device="cuda") for _ in range(2))
+    hk.heatkv_paged_append(shape, slots, torch.cat(rows[0])[:, None].cuda(), torch.cat(rows[1])[:, None].cuda(), kp, vp)
+    qs = q[:, :, cur].reshape(-1, 1, d).contiguous().cuda()  # queries of one scale: t0[kk] to a request
+    out = torch.zeros_like(qs)
+    starts = _ints([t0[kk] * i for i in range(nb * H + 1)])
+    ws = torch.zeros(max(hk.paged_attend_workspace_bytes(shape, qs.shape[0]), 16), dtype=torch.uint8, device="cuda")
+    hk.heatkv_paged_attend(shape, qs, kp, vp, table, starts, dev_lens, sm, out, ws, causal=False)
+    assert status.item() == 0
+    got = out.view(nb, H, t0[kk], d).cpu().double().numpy()
+    tol = 2e-2 if dtype == "bf16" else 2e-5  # as in the parity tests of heatkv_attend_scale
+    present = [[i + 1 for i in range(kk) if any(c[i] - t0[i] <= x < c[i] for x in kept[h])] for h in range(H)]
+    for b in range(nb):
+        for h in range(H):
+            want = orc.attend_scale(q[b, h].double().numpy(), k[b, h].double().numpy(), v[b, h].double().numpy(), orc.one_based(t0),
+                                    K, present[h], sm)
+            assert abs(got[b, h] - want).max() < tol
+
+
+def test_malformed_calls_are_named():
+    p = Problem("bf16", 4, 2, 64, 16, [40, 20], [2, 1], max_pages=40)  # long enough to need a workspace
+    d, call = p.dev, hk.heatkv_paged_attend
+    out = torch.zeros_like(d["q"])
+    ws = torch.zeros(hk.paged_attend_workspace_bytes(p.shape, p.tokens) + 16, dtype=torch.uint8, device="cuda")
+    good = [p.shape, d["q"], d["k"], d["v"], d["table"], d["q_start"], d["lens"], p.sm, out, ws]
+    call(*good)
+    wide = torch.zeros(p.tokens, 4, 65, dtype=torch.bfloat16, device="cuda")
+    wrong = [(1, d["q"].float(), "dtype"), (1, d["q"][:, :3], "shape"), (1, d["q"].cpu(), "device tensor"), (1, wide[..., 1:], "16 bytes"),
+             (1, d["q"].transpose(1, 2).contiguous().transpose(1, 2), "contiguous"),
+             (2, d["k"].float(), "dtype"), (2, d["k"][:-1], "shape"), (2, d["k"].transpose(1, 2), "contiguous"), (4, d["table"].long(), "dtype"),
+             (4, d["table"][:, :-1].contiguous(), "shape"), (5, d["q_start"][:-1], "shape"), (6, d["lens"][:1], "shape"),
+             (7, 0.0, "sm_scale"), (7, math.inf, "sm_scale"), (8, d["q"], "overlaps"), (8, out[:-1], "shape"),
+             (8, torch.zeros(1, 4, 64, dtype=torch.bfloat16, device="cuda").expand(p.tokens, 4, 64), "overlap"),
+             (9, None, "workspace"), (9, ws[:64], "workspace"), (9, ws[1:], "16-byte")]
+    for i, x, message in wrong:
+        with pytest.raises((ValueError, hk.HeatKVError), match=message):
+            call(*good[:i], x, *good[i + 1:])
+    with pytest.raises(ValueError, match="shape"):
+        call(*good, lse=torch.zeros(p.tokens, 3, device="cuda"))
+    sel = torch.zeros(p.tokens, 2, 3, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="shape"):
+        hk.heatkv_paged_attend_selected(*good[:7], sel[:-1], p.sm, out, ws)
+    with pytest.raises(ValueError, match="shape"):
+        hk.heatkv_paged_attend_selected(*good[:7], sel[:, :, 0].contiguous(), p.sm, out, ws)
+    torch.cuda.synchronize()
+
+
+def test_calls_without_tokens_do_nothing():
+    p = Problem("bf16", 4, 2, 64, 16, [40, 20], [0, 0], pad=0)
+    d = p.dev
+    assert d["q"].shape[0] == 0
+    hk.heatkv_paged_attend(p.shape, d["q"], d["k"], d["v"], d["table"], d["q_start"], d["lens"], p.sm, torch.empty_like(d["q"]))
+    empty = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    before = d["k"].clone()
+    hk.heatkv_paged_append(p.shape, torch.zeros(0, dtype=torch.int32, device="cuda"), empty, empty, d["k"], d["v"])
+    p = Problem("bf16", 4, 2, 64, 16, [40, 20], [0, 0], pad=5)  # rows of no request
+    p.check(True, p.run(True))
+    assert torch.equal(before.view(torch.int16), d["k"].view(torch.int16))

@@ -1,0 +1,281 @@
+"""CPU-side checks of the paged cache: refusals of the C ABI before any GPU work, the launch rules, the compiled kernels' tile
+copies, and the reference of the GPU tests against closed forms.  No GPU needed."""
+import ctypes as C
+import math
+import os
+import subprocess
+import tempfile
+
+import pytest
+import torch
+
+import paper_2605_14877_amd as hk
+from paper_2605_14877_amd import build as hb
+from paper_2605_14877_amd import paged
+from tests import paged_reference as ref
+from tests.test_isa_hazards import scan
+
+GOOD = dict(q_heads=8, kv_heads=2, d=128, page_size=64, num_pages=100, batch=4, max_pages=30, dtype="bf16")
+
+
+def _shape(**change):
+    return hk.PagedShape(**{**GOOD, **change})
+
+
+BAD_SHAPES = [
+    (dict(q_heads=7), "multiple"), (dict(q_heads=0), ">= 1"), (dict(kv_heads=0), ">= 1"), (dict(q_heads=34), "more than 16"),
+    (dict(q_heads=2048, kv_heads=2048), "1024 kv heads"), (dict(d=96), "64 or 128"), (dict(d=256), "64 or 128"), (dict(dtype=2), "dtype"),
+    (dict(kv_format=2), "storage format"), (dict(kv_format=hk.KV_FP8_E4M3, dtype="f32"), "bf16 shape"), (dict(page_size=8), "page_size"),
+    (dict(page_size=48), "page_size"), (dict(page_size=512), "page_size"), (dict(batch=0), "batch"), (dict(batch=4097), "batch"),
+    (dict(num_pages=0), "num_pages"), (dict(num_pages=2 ** 24 + 1), "2\\^30"), (dict(max_pages=0), "max_pages"),
+    (dict(max_pages=2 ** 24 + 1), "2\\^30"), (dict(num_pages=2 ** 24, kv_heads=32, q_heads=32), "2\\^34"),
+]
+
+
+def _fail(rc, match):
+    with pytest.raises(hk.HeatKVError, match=match) as e:
+        paged._check(rc)
+    assert e.value.code == -1
+
+
+ROWS = paged._CRows(1 << 20, 1024, 128)
+
+
+def _calls(L, sh):
+    """Every call with that shape, its other arguments in order (addresses that are never followed: the shape is refused)."""
+    a = 1 << 20
+    return [lambda: L.heatkv_paged_assign(sh.ref, *[a] * 10, 4, a, None),
+            lambda: L.heatkv_paged_append(sh.ref, a, 4, ROWS, ROWS, a, a, None, None, None),
+            lambda: L.heatkv_paged_attend(sh.ref, 4, ROWS, a, a, a, a, a, 0.1, 1, ROWS, None, a, 1 << 40, None),
+            lambda: L.heatkv_paged_select(sh.ref, 4, ROWS, a, a, a, a, a, 1, 1, 4, 1, a, None),
+            lambda: L.heatkv_paged_attend_selected(sh.ref, 4, ROWS, a, a, a, a, a, a, 4, 0.1, 1, ROWS, None, a, 1 << 40, None)]
+
+
+@pytest.mark.parametrize("change,match", BAD_SHAPES, ids=str)
+def test_shapes_that_do_not_fit_are_refused(change, match):
+    L, sh = paged._lib(), _shape(**change)
+    assert hk.paged_attend_workspace_bytes(sh, 4) == 0
+    for call in _calls(L, sh):
+        _fail(call(), match)
+
+
+def test_arguments_that_do_not_fit_are_refused():
+    L, sh, a = paged._lib(), _shape(), 1 << 20
+    attend = lambda tokens=4, q=ROWS, k=a, ints=(a, a, a), sm=0.1, out=ROWS, lse=None, ws=a, n=1 << 40: L.heatkv_paged_attend(  # noqa: E731
+        sh.ref, tokens, q, k, a, *ints, sm, 1, out, lse, ws, n, None)
+    _fail(attend(tokens=-1), "tokens")
+    _fail(attend(tokens=2 ** 22 + 1), "tokens")
+    _fail(attend(q=paged._CRows(None, 1024, 128)), "q is null")
+    _fail(attend(q=paged._CRows(a + 8, 1024, 128)), "q: address")
+    _fail(attend(q=paged._CRows(a, 1020, 128)), "q: address")
+    _fail(attend(out=paged._CRows(a, 1024, 4)), "out: address")
+    _fail(attend(out=paged._CRows(a, 0, 128)), "overlap")
+    _fail(attend(out=paged._CRows(a, 512, 128)), "overlap")
+    _fail(attend(k=0), "page pointer")
+    _fail(attend(k=a + 4), "16-byte")
+    _fail(attend(ints=(a, 0, a)), "integer array")
+    _fail(attend(ints=(a, a, a + 2)), "4-byte")
+    for sm in (0.0, -1.0, math.inf, math.nan):
+        _fail(attend(sm=sm), "sm_scale")
+    _fail(attend(lse=a + 1), "lse")
+    assert hk.paged_attend_workspace_bytes(sh, 4) > 0
+    _fail(attend(ws=0), "workspace")
+    _fail(attend(n=hk.paged_attend_workspace_bytes(sh, 4) - 1), "workspace")
+    _fail(attend(ws=a + 8), "16-byte")
+    assert attend(tokens=0, q=paged._CRows(), ints=(0, 0, 0), ws=0, n=0) == 0
+
+    append = lambda slots=a, tokens=4, k=ROWS, pages=a, b=None, s=None: L.heatkv_paged_append(  # noqa: E731
+        sh.ref, slots, tokens, k, ROWS, pages, a, b, s, None)
+    _fail(append(slots=0), "integer array")
+    _fail(append(k=paged._CRows(a, 1024, 3)), "k_new")
+    _fail(append(pages=0), "page pointer")
+    _fail(append(b=a), "go together")
+    _fail(append(s=a), "go together")
+    _fail(append(b=a + 8, s=a), "16-byte")
+    assert append(tokens=0, slots=0) == 0
+
+    select = lambda sh=sh, first=1, last=1, top=4, bounds=a, out=a: L.heatkv_paged_select(  # noqa: E731
+        sh.ref, 4, ROWS, bounds, a, a, a, a, first, last, top, 1, out, None)
+    for first, last, top in ((0, 1, 0), (0, 1, 513), (-1, 1, 4), (1, 0, 4), (3, 2, 4), (2 ** 31 - 1, 2 ** 31 - 1, 4)):
+        _fail(select(first=first, last=last, top=top), "top|first")
+    _fail(select(bounds=a + 4), "bounds")
+    _fail(select(out=0), "integer array")
+    _fail(select(sh=_shape(max_pages=32769)), "32768")
+    chosen = lambda sh=sh, sel=a, top=4: L.heatkv_paged_attend_selected(  # noqa: E731
+        sh.ref, 4, ROWS, a, a, a, a, a, sel, top, 0.1, 1, ROWS, None, a, 1 << 40, None)
+    _fail(chosen(sel=0), "integer array")
+    _fail(chosen(top=0), "top")
+    _fail(chosen(top=513), "top")
+    _fail(chosen(sh=_shape(max_pages=32769)), "32768")
+
+    assign = lambda **c: L.heatkv_paged_assign(sh.ref, *[c.get(n, d) for n, d in (  # noqa: E731
+        ("keep", a), ("new", a + 64), ("lens", a + 128), ("lens_out", a + 128), ("ring", a), ("span", a), ("span_out", a), ("table", a),
+        ("q_start", a), ("slots", a), ("tokens", 4), ("status", a))], None)
+    for name in ("keep", "new", "lens", "lens_out", "ring", "span", "span_out", "table", "q_start", "slots", "status"):
+        _fail(assign(**{name: 0}), "integer array")
+    _fail(assign(tokens=-1), "tokens")
+    _fail(assign(lens_out=a + 132), "in part")
+    _fail(assign(span_out=a + 4), "in part")
+    _fail(assign(lens_out=a), "overlap")
+
+
+def test_binding_names_tensors_that_are_not_on_a_device():
+    sh = _shape()
+    q = torch.zeros(4, 8, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="device tensor"):
+        hk.heatkv_paged_attend(sh, q, q, q, q, q, q, 0.1, q)
+    with pytest.raises(ValueError, match="device tensor"):
+        hk.heatkv_paged_append(sh, torch.zeros(4, dtype=torch.int32), q, q, q, q)
+    with pytest.raises(ValueError, match="device tensor"):
+        hk.heatkv_paged_assign(sh, *[torch.zeros(4, dtype=torch.int32)] * 9)
+    with pytest.raises(ValueError, match="device tensor"):
+        hk.heatkv_paged_select(sh, q, q, q, q, q, q, 1, 1, q)
+    with pytest.raises(TypeError, match="PagedShape"):
+        hk.heatkv_paged_attend(hk.Shape(1, 1, 64, [1, 2], 1, "f32"), q, q, q, q, q, q, 0.1, q)
+    with pytest.raises(TypeError, match="torch tensor"):
+        hk.heatkv_paged_attend(sh, None, q, q, q, q, q, 0.1, q)
+
+
+RULES = r"""
+#include "paged_rules.h"
+extern "C" void plan(int bf16, int batch, int kv, int group, long long tokens, long long pages, int page, long long top, long long* out) {
+  const auto p = heatkv::paged::plan_launches(bf16, batch, kv, group, tokens, pages, page, top);
+  int i = 0;
+  for (const auto& l : {p.few, p.many}) {
+    out[i++] = l.workgroups; out[i++] = l.grid; out[i++] = l.parts; out[i++] = l.whole_from; out[i++] = l.least_steps;
+    out[i++] = l.least_rows; out[i++] = l.most_rows;
+  }
+  out[i] = static_cast<long long>(heatkv::paged::many_union_bytes(group, pages, top));
+}
+"""
+FIELDS = ("workgroups", "grid", "parts", "whole_from", "least_steps", "least_rows", "most_rows")
+
+
+@pytest.fixture(scope="module")
+def rules(tmp_path_factory):
+    d = tmp_path_factory.mktemp("rules")
+    src, lib = d / "rules.cpp", d / "librules.so"
+    src.write_text(RULES)
+    subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", "-I", hb.CSRC, str(src), "-o", str(lib)], check=True)
+    L = C.CDLL(str(lib))
+
+    def plan(bf16, batch, kv, group, tokens, pages, page, top=0):
+        out = (C.c_longlong * 15)()
+        L.plan(*[C.c_longlong(x) if i in (4, 5, 7) else C.c_int(x) for i, x in enumerate((int(bf16), batch, kv, group, tokens, pages, page, top))],
+               out)
+        return dict(zip(FIELDS, out[:7])), dict(zip(FIELDS, out[7:14])), out[14]
+    return plan
+
+
+def test_launch_rules_on_both_sides(rules):
+    few, many, _ = rules(True, 64, 8, 4, 64 + 16, 512, 16)  # a decoding step and padding
+    assert many["workgroups"] == 0 and few["most_rows"] > 10 ** 6 and few["parts"] > 0
+    few, many, _ = rules(True, 64, 8, 4, 64 + 17, 512, 16)
+    assert many["workgroups"] and few["most_rows"] == many["least_rows"] == 64
+    assert rules(False, 1, 8, 4, 5000, 512, 16)[1]["workgroups"] == 0  # fp32 has one kernel
+    assert rules(True, 1, 1, 1, 64, 512, 16)[1]["workgroups"] == 0 and rules(True, 1, 1, 1, 65, 512, 16)[1]["workgroups"]
+    assert rules(True, 1, 8, 4, 1, 16, 16)[0]["parts"] == 0 and rules(True, 1, 8, 4, 1, 17, 16)[0]["parts"] > 0
+    few, many, size = rules(True, 1, 8, 1, 4000, 32768, 16, 512)  # a union too large for the LDS
+    assert size > 92 * 1024 and many["workgroups"] == 0
+    few, many, size = rules(True, 1, 8, 4, 4000, 512, 64, 32)
+    assert size < 92 * 1024 and many["workgroups"]
+
+
+def _pieces(many, requests, heads, group, causal, top_keys):
+    """What the 128-row launch deals, as the kernel counts it, and how many places it needs."""
+    def load(n_new, length):
+        rows = n_new * group
+        if not many["least_rows"] < rows <= many["most_rows"]:
+            return 0, 0
+        tiles, dw = -(-rows // 128), 0
+        if top_keys:
+            length = min(length, top_keys)
+        elif causal:
+            dw = 128 * 32 // 64 // group
+            length = max(length - n_new + min(n_new, 128 // group), 0)
+        w0 = max(-(-length // 64), 1) * 32
+        return tiles, tiles * w0 + tiles * (tiles - 1) // 2 * dw
+    loads = [load(*r) for r in requests]
+    total, count = sum(w for _, w in loads) * heads, sum(t for t, _ in loads) * heads
+    if count >= many["whole_from"] or not many["parts"]:
+        return count, 0
+    share = max(-(-total // many["workgroups"]), many["least_steps"] * 32)
+    n = sum(t * -(-(w // t) // share) for t, w in loads if t) * heads
+    return n, n
+
+
+def test_pieces_fit_the_grid_and_the_workspace(rules):
+    import random
+    r = random.Random(2)
+    for _ in range(400):
+        group, heads, batch = r.choice([1, 2, 3, 4, 7, 16]), r.choice([1, 2, 8, 16, 64]), r.choice([1, 2, 5, 40, 300])
+        causal, longest = r.random() < 0.5, r.choice([16, 512, 513, 4096, 70000])
+        new = [r.choice([0, 1, 5, 64 // group, 64 // group + 1, r.randint(0, 3000)]) for _ in range(batch)]
+        tokens = sum(new) + r.choice([0, 3])
+        requests = [(n, r.randint(min(n, longest), longest)) for n in new]
+        few, many, _ = rules(True, batch, heads, group, tokens, -(-longest // 16), 16)
+        if not many["workgroups"]:
+            continue
+        grid, places = _pieces(many, requests, heads, group, causal, 0)
+        assert grid <= many["grid"] and places <= many["parts"]
+
+
+def test_tile_copies_do_not_depend_on_scalars_from_the_vector_alu():
+    with tempfile.TemporaryDirectory() as tmp:
+        for src in ("paged_attend_long.hip", "paged_attend_f32.hip"):
+            out = os.path.join(tmp, src + ".s")
+            subprocess.run(["hipcc", *hb.HIP_FLAGS, "-S", "--cuda-device-only", os.path.join(hb.CSRC, src), "-o", out], check=True,
+                           capture_output=True)
+            with open(out) as f:
+                copies, hazards = scan(f.read())
+            assert copies > 0 and not hazards, (src, hazards[:5])
+
+
+# ---- the reference -----------------------------------------------------------------------------------------------------
+
+def test_reference_attention_against_torch():
+    g = torch.Generator().manual_seed(1)
+    page, lens, new = 4, [13, 6], [5, 6]
+    k, v = (torch.randn(10, 2, page, 8, generator=g, dtype=torch.float64) for _ in range(2))
+    q = torch.randn(12, 4, 8, generator=g, dtype=torch.float64)
+    table, q_start = [[3, 1, 7, 0], [9, 2]], [0, 5, 11]
+    for causal in (True, False):
+        out, lse, mag = ref.attend(q, k, v, table, q_start, lens, page, 0.3, causal)
+        assert out[11].isnan().all()
+        for b in range(2):
+            ks, vs = (x[table[b]].transpose(0, 1).reshape(2, -1, 8)[:, :lens[b]].repeat_interleave(2, 0) for x in (k, v))
+            qs = q[q_start[b]:q_start[b + 1]].transpose(0, 1)
+            seen = torch.ones(new[b], lens[b], dtype=torch.bool)
+            if causal:
+                seen = seen.tril(lens[b] - new[b])
+            want = torch.nn.functional.scaled_dot_product_attention(qs, ks, vs, seen, scale=0.3)
+            assert (out[q_start[b]:q_start[b + 1]].transpose(0, 1) - want).abs().max() < 1e-12
+    assert (mag[:11] >= out[:11].abs() - 1e-12).all()
+    everything = [[list(range(4))] * 2 for _ in range(12)]
+    assert torch.equal(ref.attend(q, k, v, table, q_start, lens, page, 0.3, True, everything)[0][:11],
+                       ref.attend(q, k, v, table, q_start, lens, page, 0.3, True)[0][:11])
+
+
+def test_reference_bounds_bound_the_scores():
+    g = torch.Generator().manual_seed(2)
+    rows = torch.randn(16, 64, generator=g).bfloat16()
+    b, scale = ref.bounds_of(rows)
+    assert (b[0].double() * scale >= rows.double().amax(0)).all() and (b[1].double() * scale >= -rows.double().amin(0)).all()
+    assert math.log2(scale) == int(math.log2(scale)) and b.abs().max() <= 127
+    code = torch.randint(-127, 128, (64,), generator=g).double()  # a query on its grid
+    bound = scale * (code.clamp(min=0) @ b[0].double() + (-code).clamp(min=0) @ b[1].double())
+    assert bound >= (rows.double() @ code).max()
+
+
+def test_reference_allocator_keeps_every_page_once():
+    import random
+    r = random.Random(1)
+    a = ref.Allocator(5, 30, 8, 16, list(range(30)), 7, 30, [[-1] * 8 for _ in range(5)], [0] * 5)
+    for _ in range(200):
+        keep = [r.randint(0, n) for n in a.lens]
+        new = [r.randint(0, 40) for _ in a.lens]
+        status, q_start, slots = a.step(keep, new, 150)
+        used = [x for row, n in zip(a.table, a.lens) for x in row[:ref.pages_of(n, 16)]]
+        free = [a.ring[(a.head + i) % 30] for i in range(a.count)]
+        assert sorted(used + free) == list(range(30))
+        assert status == 0 or set(slots) == {-1}
