@@ -65,7 +65,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_kernel(AttendParam
   const int w = blockIdx.x;
   line.start<16, STEP>(p, w);
   Part part;
-  while (line.advance<16, STEP>(p, part)) {
+  for (bool first = true; line.advance<16, STEP>(p, first, part); first = false) {
   const Tile tile = tile_of<16>(p.c, part);
   const int h = part.h;
 
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_kernel(AttendParam
   if (tid == 0) nan_rows = 0;
   const Part done = line.stored();
   const bool alone = done.from == 0 && done.to == done.weight;  // no other workgroup has a part of this segment
-  const long long part_base = part_rows<16>(w, done.from == 0);
+  const long long part_base = line.part_rows<16>(w, done);
   __syncthreads();
   float m_all = part_m[0][n], l_all = 0.f;
 #pragma unroll

@@ -153,7 +153,7 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
   // The piece at hand stays in LDS, and arguments are read where they are used: the tile loop has no registers to keep them in.
   {
     Part part;
-    if (!find_piece<BM, BN>(p, w, shared.scratch, part)) return;
+    if (!only_piece<BM, BN>(p, w, shared.scratch, part)) return;
     if (tid == 0) shared.piece = part;
     __syncthreads();
   }

@@ -1,6 +1,6 @@
-// Paged attention: joins the parts of segments that lie in several workgroups' shares (paged_schedule.h).  A workgroup looks at
-// one border between shares and joins the segment there, if this is the first border in it: a wavefront per row, the parts in
-// order, so that the result does not depend on which workgroup was done first.
+// Paged attention: joins the parts of segments that several workgroups had (paged_schedule.h).  A workgroup looks at one border
+// between shares, or one piece, and joins the segment there if this is the first border in it, or its first piece: a wavefront
+// per row, the parts in order, so that the result does not depend on which workgroup was done first.
 //
 // Bound: latency (borders, lengths, parts: a round of loads each, one more for every sixteen parts), and of many rows the
 // traffic of the parts.
@@ -22,12 +22,12 @@ using namespace paged;
 template <class T, int D, int ROWS, int EACH>
 __global__ __launch_bounds__(256) void paged_join_kernel(AttendParams p) {
   constexpr int N = D / 32;  // columns of a lane; either half of a wavefront has a whole row
-  constexpr bool PIECES = ROWS == 128;  // dealt by pieces, not along the line
-  const int lane = threadIdx.x & 63, half = lane >> 5, col = (lane & 31) * N, w = blockIdx.x + (PIECES ? 0 : 1);
-  const auto* border = (const __attribute__((address_space(4))) Border*)(p.borders) + w;
-  const int parts = border->parts;
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = (lane & 31) * N, w = blockIdx.x;
+  const auto* at_border = (const __attribute__((address_space(4))) Border*)(p.borders) + w;
+  const Border border{at_border->b, at_border->h, at_border->t, at_border->parts};
+  const int parts = abs(border.parts);
   if (parts == 0) return;
-  const Part segment{border->b, border->h, border->t, 0, 0, 0};
+  const Part segment{border.b, border.h, border.t, 0, 0, 0};
   const Tile tile = tile_of<ROWS>(p.c, segment);
   const int row0 = blockIdx.y * EACH * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // then every fourth
   if (row0 >= tile.rows) return;
@@ -39,7 +39,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttendParams p) {
     float m, l, x[N];
   };
   auto load = [&](int part, int row) {
-    const long long at = (PIECES ? (w + static_cast<long long>(part) * p.c.H) * ROWS : part_rows<ROWS>(w - 1 + part, part == 0)) + row;
+    const long long at = joined_rows<ROWS>(border, w, part, p.c.H) + row;
     One y;
     y.m = p.part_ml[at * 2];
     y.l = p.part_ml[at * 2 + 1];
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttendParams p) {
 
 template <class T, int D, int ROWS, int EACH>
 hipError_t launch(const AttendParams& p, hipStream_t stream) {
-  hipLaunchKernelGGL((paged_join_kernel<T, D, ROWS, EACH>), dim3(ROWS == 128 ? p.grid : p.workgroups - 1, ROWS / 4 / EACH), dim3(256), 0, stream, p);
+  hipLaunchKernelGGL((paged_join_kernel<T, D, ROWS, EACH>), dim3(p.grid, ROWS / 4 / EACH), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 

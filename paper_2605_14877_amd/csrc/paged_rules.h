@@ -13,7 +13,7 @@ struct Launch {
   int workgroups = 0;              // shares that the work is cut into; 0: not launched
   int64_t grid = 0;                // workgroups launched
   int parts = 0;                   // places for parts of cut segments; 0: nothing is cut
-  int whole_from = INT_MAX;        // segments from which on none is cut
+  int whole_from = 0;              // segments from which on: few, they are dealt along a line; many, none is cut
   int least_steps = 0;             // of a share
   int least_rows = 0, most_rows = INT_MAX;  // requests by their query rows per kv head: least_rows < rows <= most_rows
 };
@@ -21,6 +21,8 @@ struct Plan {
   Launch few, many;  // tiles of 16 rows and steps of 32 keys; of 128 and 64
 };
 
+// Steps of a share at least: less of them than that would not pay for a part's way through memory and the join.
+constexpr int LEAST_STEPS = 8;
 // Requests of more query rows (new tokens x queries per kv head) than this are the 128-row kernel's.
 constexpr int MANY_ROWS = 64;
 
@@ -36,22 +38,25 @@ inline size_t many_union_bytes(int group, int64_t max_pages, int64_t top) {
 inline Plan plan_launches(bool bf16, int batch, int kv_heads, int group, int64_t tokens, int64_t max_pages, int page_size, int64_t top) {
   Plan p;
   const int64_t rows = tokens * group, longest = max_pages * page_size;
-  // Two workgroups to a compute unit are resident.  A segment of up to 8 steps is not cut (nor are they all where none is longer).
+  // Two workgroups to a compute unit are resident.  A segment of up to LEAST_STEPS is not cut (nor are they all where none is
+  // longer).
   p.few.workgroups = 512;
-  p.few.grid = 512;
-  p.few.least_steps = 8;
-  p.few.parts = longest > 8 * 32 ? 2 * 512 : 0;
+  // Fewer segments than half of that are dealt by pieces: up to one more than shares for each.
+  p.few.whole_from = 256;
+  p.few.grid = 512 + 256;
+  p.few.least_steps = LEAST_STEPS;
+  p.few.parts = longest > LEAST_STEPS * 32 ? 2 * 512 : 0;
   // Little more than one token for each request: taken for a decoding step, whose few padding rows are not worth a launch.
   if (bf16 && rows > MANY_ROWS && tokens > batch + 16 && (top == 0 || many_union_bytes(group, max_pages, top) <= MANY_UNION_BYTES)) {
     p.few.most_rows = p.many.least_rows = MANY_ROWS;
     p.many.workgroups = 512;
-    p.many.least_steps = 8;
+    p.many.least_steps = LEAST_STEPS;
     // Two whole segments for every share and more: nothing is cut.  Fewer: the pieces are at most one more than each
     // segment's weight is shares.
     p.many.whole_from = 1024;
     const int64_t segments = kv_heads * (rows / 128 + std::min<int64_t>(batch, rows / (MANY_ROWS + 1)));
     const int64_t pieces = p.many.workgroups + std::min<int64_t>(segments, p.many.whole_from - 1);
-    const bool cut = longest > 8 * 64;
+    const bool cut = longest > LEAST_STEPS * 64;
     p.many.grid = cut ? std::max(segments, pieces) : segments;
     p.many.parts = cut ? static_cast<int>(pieces) : 0;
   }

@@ -1,13 +1,18 @@
 // How a launch's work is dealt to workgroups when the lengths are on the device.
 //
 // A segment is a tile of query rows of a request and kv head, and has a weight, about proportional to the keys that it walks
-// over.  All segments lie on one line: requests in order, of each the kv heads, of each the tiles.  Workgroup w takes the
-// stretch [w share, (w + 1) share) of it, so any mix of lengths is dealt evenly, with a grid that depends on nothing that the
-// host does not know.  A segment that crosses from one share into another is computed in parts (its steps in proportion to
-// the weight on either side), which a second launch joins in order; light segments are not cut, they belong to the
-// workgroup that they begin in.
+// over.  A share is the weight of all segments over the workgroups that are resident at a time.  Two ways:
 //
-// Every workgroup finds its place by a scan over the requests (two rounds of loads, a block scan: about 2 us).
+// Along a line, on which all segments lie (requests in order, of each the kv heads, of each the tiles): workgroup w takes the
+// stretch [w share, (w + 1) share) of it.  Any mix of lengths is dealt evenly, with a grid that depends on nothing that the
+// host does not know.  A segment that crosses from one share into another is computed in parts.
+//
+// By pieces: a segment is cut into as many equal parts as its request's mean weight is shares, and a workgroup takes one.
+// They come as workgroups become free, the last tiles of a request first, which are the heaviest with a causal limit.  Parts
+// are fewer than on the line, and no workgroup has two things to do one after the other.
+//
+// The steps of a part are in proportion to its weight; a second launch joins parts, in order.  Light segments are not cut.
+// Every workgroup finds its part by a scan over the requests (a round of loads; for up to 64 requests within the wavefront).
 #pragma once
 
 #include "paged.h"
@@ -51,14 +56,14 @@ __device__ __forceinline__ long long uniform(long long x) {
   return static_cast<long long>(hi) << 32 | static_cast<unsigned>(lo);
 }
 
-struct Place {
-  long long pos, stop, share;  // on the line; pos >= stop: nothing (more) to do
-  int b, h, t;                 // the segment at pos
-  long long off;               // pos in it
-  Load load;                   // of request b
-};
+// n / d of numbers that are not negative: the 64-bit division takes several times the instructions of the 32-bit one.
+__device__ __forceinline__ long long quotient(long long n, long long d) {
+  if (((n | d) >> 31) == 0) return static_cast<unsigned>(n) / static_cast<unsigned>(d);
+  return n / d;
+}
+
 struct Scratch {  // LDS
-  long long sums[4], more_sums[4], first;
+  long long sums[4], first;
   int b;
 };
 
@@ -67,95 +72,197 @@ __device__ __forceinline__ Load request_load(const AttendParams& p, int b) {
   return load_of<ROWS, KEYS>(p, uniform_load(p.c.q_start, b), uniform_load(p.c.q_start, b + 1), uniform_load(p.c.lens, b));
 }
 
-// Inclusive sums over the 256 lanes of a workgroup, and the total in `all`; `sums`: LDS, free at the next barrier but one.
-__device__ __forceinline__ long long block_scan(long long v, long long (&sums)[4], long long& all) {
-  const int tid = threadIdx.x, lane = tid & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const long long u = __shfl_up(v, d, 64);
-    if (lane >= d) v += u;
+// The requests' loads, consecutive ones to each lane of the workgroup; up to 64 requests: one to each lane of every wavefront.
+template <int ROWS, int KEYS>
+struct Requests {
+  const AttendParams& p;
+  const bool narrow;
+  const int first, count;  // this lane's
+  Load own;                // of the first
+  __device__ __forceinline__ Requests(const AttendParams& params)
+      : p(params),
+        narrow(params.c.batch <= 64),
+        first(narrow ? threadIdx.x & 63 : static_cast<int>(threadIdx.x) * ((params.c.batch + 255) / 256)),
+        count(narrow ? 1 : (params.c.batch + 255) / 256) {
+    own = load(first);
   }
-  if (lane == 63) sums[tid >> 6] = v;
-  __syncthreads();
-  all = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const long long x = sums[i];
-    if (i < (tid >> 6)) v += x;
-    all += x;
+  __device__ __forceinline__ Load load(int b) const {
+    if (b >= p.c.batch) return Load{0, STEP_WEIGHT, 0};
+    return load_of<ROWS, KEYS>(p, p.c.q_start[b], p.c.q_start[b + 1], p.c.lens[b]);
   }
-  all = uniform(all);
-  return v;
-}
-// The request that holds position `at` of a line on which request b takes cost(b), and where on the line it begins.  By all
-// lanes; `upto`: block_scan of the costs of this lane's requests, `mine`.
-template <class Cost>
-__device__ __forceinline__ int find_request_at(long long at, int batch, long long upto, long long mine, const Cost& cost,
-                                               Scratch& scratch, long long& first) {
-  const int per = (batch + 255) / 256;
-  if (at < upto && at >= upto - mine) {  // one lane
-    long long x = upto - mine;
-    for (int i = 0; i < per; ++i) {
-      const int b = threadIdx.x * per + i;
-      const long long n = b < batch ? cost(b) : 0;
-      if (at < x + n) {
-        scratch.first = x;
-        scratch.b = b;
-        break;
-      }
-      x += n;
+  template <class Cost>
+  __device__ __forceinline__ long long mine(const Cost& cost) const {
+    long long sum = cost(own);
+    for (int i = 1; i < count; ++i) sum += cost(load(first + i));
+    return sum;
+  }
+  // Sum of `v` over the lanes up to this one, and over all of them.  Between two calls with the same scratch: a barrier.
+  __device__ __forceinline__ long long scan(long long v, Scratch& scratch, long long& all) const {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const long long u = __shfl_up(v, d, 64);
+      if (lane >= d) v += u;
     }
+    if (narrow) {
+      all = last_lane(v);
+      return v;
+    }
+    if (lane == 63) scratch.sums[wave] = v;
+    __syncthreads();
+    all = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const long long x = scratch.sums[i];
+      if (i < wave) v += x;
+      all += x;
+    }
+    __syncthreads();
+    all = uniform(all);
+    return v;
   }
-  __syncthreads();
-  first = uniform(scratch.first);
-  return __builtin_amdgcn_readfirstlane(scratch.b);
-}
-template <class Cost>
-__device__ __forceinline__ long long own_cost(int batch, const Cost& cost) {  // of this lane's requests
-  const int per = (batch + 255) / 256;
-  long long mine = 0;
-  for (int i = 0; i < per; ++i)
-    if (static_cast<int>(threadIdx.x) * per + i < batch) mine += cost(threadIdx.x * per + i);
-  return mine;
+  // The request that holds position `at`, and where it begins; upto, mine as above.
+  template <class Cost>
+  __device__ __forceinline__ int find(long long at, long long upto, long long mine, const Cost& cost, Scratch& scratch,
+                                      long long& begins) const {
+    if (narrow) {
+      const int b = min(static_cast<int>(__popcll(__ballot(upto <= at))), 63);
+      begins = lane_of(upto - mine, b);
+      return b;
+    }
+    if (at < upto && at >= upto - mine) {  // one lane
+      long long x = upto - mine;
+      for (int i = 0; i < count; ++i) {
+        const long long n = cost(load(first + i));
+        if (at < x + n) {
+          scratch.first = x;
+          scratch.b = first + i;
+          break;
+        }
+        x += n;
+      }
+    }
+    __syncthreads();
+    begins = uniform(scratch.first);
+    return __builtin_amdgcn_readfirstlane(scratch.b);
+  }
+  // The load of request b, as every lane's own.
+  __device__ __forceinline__ Load found(int b) const {
+    if (!narrow) return request_load<ROWS, KEYS>(p, b);
+    return Load{__builtin_amdgcn_readlane(own.tiles, b), __builtin_amdgcn_readlane(own.w0, b), __builtin_amdgcn_readlane(own.dw, b)};
+  }
+  static __device__ __forceinline__ long long lane_of(long long x, int l) {
+    const int lo = __builtin_amdgcn_readlane(static_cast<int>(x), l), hi = __builtin_amdgcn_readlane(static_cast<int>(x >> 32), l);
+    return static_cast<long long>(hi) << 32 | static_cast<unsigned>(lo);
+  }
+  static __device__ __forceinline__ long long last_lane(long long x) { return lane_of(x, 63); }
+};
+
+// A part of a segment, in units of its weight; the whole segment: from == 0, to == weight.
+struct Part {
+  int b, h, t;
+  long long from, to, weight;
+};
+
+// What the join has to know; written by every workgroup.  parts > 0: the border between its share and the one before cuts a
+// segment (and no earlier border does); parts < 0: its piece is the first of -parts; 0: neither.
+__device__ __forceinline__ void write_border(const AttendParams& p, int w, const Border& x) {
+  if (p.borders && threadIdx.x == 0) p.borders[w] = x;
 }
 
-// The place of workgroup w, by all of its 256 lanes.
+// The piece of workgroup w, by all of its 256 lanes; false: there is none.  Pieces of a segment lie H workgroups apart.
 template <int ROWS, int KEYS>
-__device__ __forceinline__ Place find_place(const AttendParams& p, int w, Scratch& scratch) {
-  const Cache& c = p.c;
-  auto cost = [&](int b) {
-    const Load l = load_of<ROWS, KEYS>(p, c.q_start[b], c.q_start[b + 1], c.lens[b]);
-    return l.upto(l.tiles) * c.H;
-  };
-  const long long mine = own_cost(c.batch, cost);
-  long long total;
-  const long long upto = block_scan(mine, scratch.sums, total);
-  Place at{};
-  at.share = max((total + p.workgroups - 1) / p.workgroups, static_cast<long long>(p.least_weight));
-  at.pos = w * at.share;
-  at.stop = min(at.pos + at.share, total);
-  if (at.pos >= total) return at;
-  long long first;
-  at.b = find_request_at(at.pos, c.batch, upto, mine, cost, scratch, first);
-  at.load = request_load<ROWS, KEYS>(p, at.b);
-  const long long rel = at.pos - first, per_head = at.load.upto(at.load.tiles);
-  at.h = static_cast<int>(rel / per_head);
-  const long long in_head = rel - at.h * per_head;
-  int below = 0, above = at.load.tiles;  // the last tile that begins at in_head or before
-  while (above - below > 1) {
-    const int mid = (below + above) >> 1;
-    (at.load.upto(mid) <= in_head ? below : above) = mid;
+__device__ __forceinline__ bool find_piece(const AttendParams& p, const Requests<ROWS, KEYS>& requests, int w, long long share,
+                                           Scratch& scratch, Part& part) {
+  auto cuts = [&](const Load& l) { return l.tiles ? static_cast<int>(quotient(quotient(l.upto(l.tiles), l.tiles) + share - 1, share)) : 0; };
+  auto cost = [&](const Load& l) { return static_cast<long long>(l.tiles) * cuts(l) * p.c.H; };
+  const long long mine = requests.mine(cost);
+  long long all, first;
+  const long long upto = requests.scan(mine, scratch, all);
+  if (w >= all) {
+    write_border(p, w, Border{0, 0, 0, 0});
+    return false;
   }
-  at.t = below;
-  at.off = in_head - at.load.upto(below);
+  part.b = requests.find(w, upto, mine, cost, scratch, first);
+  const Load l = requests.found(part.b);
+  const int n = cuts(l), rel = static_cast<int>(w - first), i = rel / p.c.H, tile = i / n;
+  part.h = rel - i * p.c.H;
+  part.t = l.tiles - 1 - tile;
+  part.from = i - tile * n;
+  part.to = part.from + 1;
+  part.weight = n;
+  write_border(p, w, Border{part.b, part.h, part.t, n > 1 && part.from == 0 ? -n : 0});
+  return true;
+}
+template <int ROWS, int KEYS>
+__device__ __forceinline__ long long total_weight(const AttendParams& p, const Requests<ROWS, KEYS>& requests, Scratch& scratch,
+                                                  long long& upto, long long& mine) {
+  mine = requests.mine([&](const Load& l) { return l.upto(l.tiles) * p.c.H; });
+  long long total;
+  upto = requests.scan(mine, scratch, total);
+  return total;
+}
+template <int ROWS, int KEYS>
+__device__ __forceinline__ long long total_segments(const AttendParams& p, const Requests<ROWS, KEYS>& requests, Scratch& scratch) {
+  long long count;
+  requests.scan(requests.mine([&](const Load& l) { return static_cast<long long>(l.tiles) * p.c.H; }), scratch, count);
+  return count;
+}
+__device__ __forceinline__ long long share_of(const AttendParams& p, long long total) {
+  return max(quotient(total + p.workgroups - 1, p.workgroups), static_cast<long long>(p.least_weight));
+}
+
+// By pieces only: whole segments from whole_from on, or where the workspace has no place for parts.
+template <int ROWS, int KEYS>
+__device__ __forceinline__ bool only_piece(const AttendParams& p, int w, Scratch& scratch, Part& part) {
+  const Requests<ROWS, KEYS> requests(p);
+  long long upto, mine;
+  const long long total = total_weight(p, requests, scratch, upto, mine);
+  const bool whole = !p.borders || total_segments(p, requests, scratch) >= p.whole_from;
+  return find_piece(p, requests, w, whole ? total + 1 : share_of(p, total), scratch, part);
+}
+
+struct Place {
+  long long pos, stop;  // on the line; pos >= stop: nothing (more) to do
+  int b, h, t;          // the segment at pos
+  long long off;        // pos in it
+  Load load;            // of request b
+};
+// The place of workgroup w on the line, by all lanes.
+template <int ROWS, int KEYS>
+__device__ __forceinline__ Place find_place(const AttendParams& p, const Requests<ROWS, KEYS>& requests, int w, long long total,
+                                            long long upto, long long mine, Scratch& scratch) {
+  const long long share = share_of(p, total);
+  Place at{};
+  at.pos = w * share;
+  at.stop = min(at.pos + share, total);
+  Border border{0, 0, 0, 0};
+  if (at.pos < total && w < p.workgroups) {
+    long long first;
+    at.b = requests.find(at.pos, upto, mine, [&](const Load& l) { return l.upto(l.tiles) * p.c.H; }, scratch, first);
+    at.load = requests.found(at.b);
+    const long long rel = at.pos - first, per_head = at.load.upto(at.load.tiles);
+    at.h = static_cast<int>(quotient(rel, per_head));
+    const long long in_head = rel - at.h * per_head;
+    int below = 0, above = at.load.tiles;  // the last tile that begins at in_head or before
+    while (above - below > 1) {
+      const int mid = (below + above) >> 1;
+      (at.load.upto(mid) <= in_head ? below : above) = mid;
+    }
+    at.t = below;
+    at.off = in_head - at.load.upto(below);
+    const long long weight = at.load.weight(at.t);
+    border = Border{at.b, at.h, at.t, 0};
+    if (at.off > 0 && at.off <= share && weight > p.cut_from)
+      border.parts = 1 + static_cast<int>(quotient(weight - at.off + share - 1, share));
+  } else {
+    at.stop = at.pos;
+  }
+  write_border(p, w, border);
   return at;
 }
 
 // The part of the segment at pos that is this workgroup's; advances the place behind it.
-struct Part {
-  int b, h, t;
-  long long from, to, weight;  // of the segment's weight; the whole segment: from == 0, to == weight
-};
 template <int ROWS, int KEYS>
 __device__ __forceinline__ bool next_part(const AttendParams& p, Place& at, Part& part) {
   while (at.pos < at.stop) {
@@ -178,81 +285,46 @@ __device__ __forceinline__ bool next_part(const AttendParams& p, Place& at, Part
   return false;
 }
 
-// What the join has to know about the border between shares w - 1 and w: written by workgroup w, before its first part.
-// parts 0: no segment is cut there, or it was cut at an earlier border already.
-__device__ __forceinline__ void write_border(const AttendParams& p, const Place& at, int w) {
-  if (!p.borders || threadIdx.x != 0) return;
-  Border x{at.b, at.h, at.t, 0};
-  if (at.pos < at.stop && at.off > 0 && at.off <= at.share) {
-    const long long weight = at.load.weight(at.t);
-    if (weight > p.cut_from) x.parts = 1 + static_cast<int>((weight - at.off + at.share - 1) / at.share);
-  }
-  p.borders[w] = x;
-}
-
-// The other way to deal, for large tiles: a workgroup takes one piece, and pieces come as workgroups become free.  A segment
-// is one piece where there are segments enough to fill the chip evenly (whole_from), otherwise as many as its request's mean
-// weight is shares (`workgroups` of them, none lighter than least_weight).  Parts are fewer than on the line, and the tile
-// loop needs no registers for a place on it.  The last tiles come first: with a causal limit they are the heaviest.
-// Pieces of a segment lie H workgroups apart.
-template <int ROWS, int KEYS>
-__device__ __forceinline__ bool find_piece(const AttendParams& p, int w, Scratch& scratch, Part& part) {
-  const Cache& c = p.c;
-  auto load = [&](int b) { return load_of<ROWS, KEYS>(p, c.q_start[b], c.q_start[b + 1], c.lens[b]); };
-  auto weight = [&](int b) {
-    const Load l = load(b);
-    return l.upto(l.tiles) * c.H;
-  };
-  auto segments = [&](int b) { return static_cast<long long>(load(b).tiles) * c.H; };
-  long long total, count;
-  block_scan(own_cost(c.batch, weight), scratch.sums, total);
-  block_scan(own_cost(c.batch, segments), scratch.more_sums, count);
-  const long long share = count >= p.whole_from || !p.borders ? total + 1 : max((total + p.workgroups - 1) / p.workgroups, static_cast<long long>(p.least_weight));
-  auto cuts = [&](const Load& l) {
-    return l.tiles ? static_cast<int>((l.upto(l.tiles) / l.tiles + share - 1) / share) : 0;
-  };
-  auto pieces = [&](int b) {
-    const Load l = load(b);
-    return static_cast<long long>(l.tiles) * cuts(l) * c.H;
-  };
-  const long long mine = own_cost(c.batch, pieces);
-  long long all, first;
-  const long long upto = block_scan(mine, scratch.sums, all);
-  if (p.borders && threadIdx.x == 0) p.borders[w].parts = 0;
-  if (w >= all) return false;
-  part.b = find_request_at(w, c.batch, upto, mine, pieces, scratch, first);
-  const Load l = request_load<ROWS, KEYS>(p, part.b);
-  const int n = cuts(l), rel = static_cast<int>(w - first), i = rel / c.H, tile = i / n;
-  part.h = rel - i * c.H;
-  part.t = l.tiles - 1 - tile;
-  part.from = i - tile * n;
-  part.to = part.from + 1;
-  part.weight = n;
-  if (p.borders && threadIdx.x == 0 && n > 1 && part.from == 0) p.borders[w] = Border{part.b, part.h, part.t, n};
-  return true;
-}
-
-// A workgroup's place on the line and the part at hand, in LDS: the tile loops have no registers to spare for them.
+// A workgroup's parts, one after the other; what they are is kept in LDS: the tile loops have no registers to spare.  Pieces
+// where there are fewer segments than half the workgroups (whole_from), the line otherwise.
 struct Line {
   Scratch scratch;
   Place place;
   Part next;
-  int more;
+  int more, pieces;
   template <int ROWS, int KEYS>
   __device__ __forceinline__ void start(const AttendParams& p, int w) {
-    const Place at = find_place<ROWS, KEYS>(p, w, scratch);
-    write_border(p, at, w);
-    if (threadIdx.x == 0) place = at;
+    const Requests<ROWS, KEYS> requests(p);
+    long long upto, mine;
+    const long long total = total_weight(p, requests, scratch, upto, mine);
+    const bool by_pieces = total_segments(p, requests, scratch) < p.whole_from;
+    Place at{};
+    Part only{};
+    bool some = false;
+    if (by_pieces)
+      some = find_piece(p, requests, w, p.borders ? share_of(p, total) : total + 1, scratch, only);
+    else
+      at = find_place(p, requests, w, total, upto, mine, scratch);
+    if (threadIdx.x == 0) {
+      pieces = by_pieces;
+      more = some;
+      next = only;
+      place = at;
+    }
   }
   // False: there is no further part.  Between two calls: a barrier behind the last use of the first one's part.
   template <int ROWS, int KEYS>
-  __device__ __forceinline__ bool advance(const AttendParams& p, Part& part) {
+  __device__ __forceinline__ bool advance(const AttendParams& p, bool first, Part& part) {
     if (threadIdx.x == 0) {
-      Place at = place;
-      Part x{};
-      more = next_part<ROWS, KEYS>(p, at, x);
-      next = x;
-      place = at;
+      if (pieces) {
+        more = more && first;
+      } else {
+        Place at = place;
+        Part x{};
+        more = next_part<ROWS, KEYS>(p, at, x);
+        next = x;
+        place = at;
+      }
     }
     __syncthreads();
     if (!__builtin_amdgcn_readfirstlane(more)) return false;
@@ -263,18 +335,22 @@ struct Line {
     return {__builtin_amdgcn_readfirstlane(next.b), __builtin_amdgcn_readfirstlane(next.h), __builtin_amdgcn_readfirstlane(next.t),
             uniform(next.from), uniform(next.to), uniform(next.weight)};
   }
+  // Where the part's rows go if it is not a whole segment: two places for each workgroup of the line, 0 for a segment that began
+  // in an earlier share, 1 for one that begins in its share and goes on behind it; one for each piece.
+  template <int ROWS>
+  __device__ __forceinline__ long long part_rows(int w, const Part& part) const {
+    return (__builtin_amdgcn_readfirstlane(pieces) ? static_cast<long long>(w) : static_cast<long long>(w) * 2 + (part.from == 0)) * ROWS;
+  }
 };
+// The same for the join: part i of the segment that `border` of workgroup w tells of.
+template <int ROWS>
+__device__ __forceinline__ long long joined_rows(const Border& border, int w, int i, int H) {
+  return (border.parts < 0 ? w + static_cast<long long>(i) * H : i == 0 ? (w - 1) * 2ll + 1 : (w - 1ll + i) * 2) * ROWS;
+}
 
 // Steps of a part, of the `steps` that the segment turned out to take.
 __device__ __forceinline__ int steps_before(long long weight_before, long long weight, int steps) {
-  return static_cast<int>(weight_before * steps / weight);
-}
-
-// Where a workgroup puts its parts: 0 a segment that began in an earlier share, 1 one that begins in its share and goes on
-// behind it; ROWS rows each.
-template <int ROWS>
-__device__ __forceinline__ long long part_rows(int w, bool begins) {
-  return (static_cast<long long>(w) * 2 + (begins ? 1 : 0)) * ROWS;
+  return static_cast<int>(quotient(weight_before * steps, weight));
 }
 
 template <int ROWS>
