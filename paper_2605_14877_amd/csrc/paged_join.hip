@@ -117,7 +117,7 @@ hipError_t launch(const AttendParams& p, hipStream_t stream) {
 
 hipError_t launch_paged_join(const PagedAttendParams& p, int dtype, int d, bool many, hipStream_t stream) {
   if (dtype == HEATKV_F32) return d == 128 ? launch<float, 128, 16, 1>(p, stream) : launch<float, 64, 16, 1>(p, stream);
-  if (many) return d == 128 ? launch<bf16_t, 128, 128, 8>(p, stream) : launch<bf16_t, 64, 128, 8>(p, stream);
+  if (many) return d == 128 ? launch<bf16_t, 128, 128, 4>(p, stream) : launch<bf16_t, 64, 128, 4>(p, stream);
   return d == 128 ? launch<bf16_t, 128, 16, 1>(p, stream) : launch<bf16_t, 64, 16, 1>(p, stream);
 }
 

@@ -191,7 +191,9 @@ __device__ __forceinline__ bool find_piece(const AttendParams& p, const Requests
   part.from = i - tile * n;
   part.to = part.from + 1;
   part.weight = n;
-  write_border(p, w, Border{part.b, part.h, part.t, n > 1 && part.from == 0 ? -n : 0});
+  // Parts behind the grid's end: of a q_start that is not ascending only.
+  const bool joins = n > 1 && part.from == 0 && w + (n - 1ll) * p.c.H < p.grid;
+  write_border(p, w, Border{part.b, part.h, part.t, joins ? -n : 0});
   return true;
 }
 template <int ROWS, int KEYS>

@@ -220,6 +220,27 @@ def test_pieces_fit_the_grid_and_the_workspace(rules):
         assert grid <= many["grid"] and places <= many["parts"]
 
 
+def test_pieces_of_the_16_row_launch_fit_the_grid_and_the_workspace(rules):
+    import random
+    r = random.Random(3)
+    some = 0
+    for _ in range(400):
+        group, heads, batch = r.choice([1, 2, 4, 16]), r.choice([1, 2, 8, 64]), r.choice([1, 2, 5, 40, 255])
+        longest = r.choice([16, 256, 257, 4096, 70000])
+        new = [r.choice([0, 1, 1, 5]) for _ in range(batch)]
+        few, many, _ = rules(True, batch, heads, group, max(sum(new), 1), -(-longest // 16), 16)
+        # segments of any weights, one row of keys each at the least
+        segments = [(-(-n * group // 16), max(-(-r.randint(1, longest) // 32), 1) * 32) for n in new if n]
+        count, total = heads * sum(t for t, _ in segments), heads * sum(t * w for t, w in segments)
+        if not few["parts"] or not 0 < count < few["whole_from"]:
+            continue
+        share = max(-(-total // few["workgroups"]), few["least_steps"] * 32)
+        pieces = heads * sum(t * -(-w // share) for t, w in segments)
+        assert pieces <= few["grid"] <= few["parts"]
+        some += 1
+    assert some > 50
+
+
 def test_tile_copies_do_not_depend_on_scalars_from_the_vector_alu():
     with tempfile.TemporaryDirectory() as tmp:
         for src in ("paged_attend_long.hip", "paged_attend_f32.hip"):
