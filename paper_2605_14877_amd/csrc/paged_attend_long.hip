@@ -243,28 +243,23 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     };
     // 8-bit rows: load i of a lane is 16 codes of one row, converted on the way into the stage.
     constexpr int LPR = D / 16;  // lanes per row
-    auto load_codes = [&](const char* pages, const TileRows& at, int it, uint4 (&raw)[CPL]) {
-#pragma unroll
-      for (int i = 0; i < CPL; ++i) {
-        const int r = (tid + 256 * i) / LPR;  // a wavefront's 64 / LPR rows are of one granule
-        const int from = D == 128 ? (wave >> 1 ? at.granule[2 * i + 1] : at.granule[2 * i])
-                                  : wave >> 1 ? (wave & 1 ? at.granule[3] : at.granule[2]) : (wave & 1 ? at.granule[1] : at.granule[0]);
-        raw[i] = make_uint4(0, 0, 0, 0);
-        const int pos = !CHOSEN ? it * BN + (r & ~15)
-                        : it >= end ? 1 << 30
-                        : D == 128  ? (wave >> 1 ? at.pos[2 * i + 1] : at.pos[2 * i])
-                                    : wave >> 1 ? (wave & 1 ? at.pos[3] : at.pos[2]) : (wave & 1 ? at.pos[1] : at.pos[0]);
-        if (pos + (r & 15) < stop) raw[i] = ldg16(pages + (static_cast<long long>(from) * 16 + (r & 15)) * SRC + (tid % LPR) * 16);
-      }
+    auto load_codes = [&](const char* pages, const TileRows& at, int it, int i) {
+      const int r = (tid + 256 * i) / LPR;  // a wavefront's 64 / LPR rows are of one granule
+      const int from = D == 128 ? (wave >> 1 ? at.granule[2 * i + 1] : at.granule[2 * i])
+                                : wave >> 1 ? (wave & 1 ? at.granule[3] : at.granule[2]) : (wave & 1 ? at.granule[1] : at.granule[0]);
+      const int pos = !CHOSEN ? it * BN + (r & ~15)
+                      : it >= end ? 1 << 30
+                      : D == 128  ? (wave >> 1 ? at.pos[2 * i + 1] : at.pos[2 * i])
+                                  : wave >> 1 ? (wave & 1 ? at.pos[3] : at.pos[2]) : (wave & 1 ? at.pos[1] : at.pos[0]);
+      uint4 raw = make_uint4(0, 0, 0, 0);
+      if (pos + (r & 15) < stop) raw = ldg16(pages + (static_cast<long long>(from) * 16 + (r & 15)) * SRC + (tid % LPR) * 16);
+      return raw;
     };
-    auto store_codes = [&](char* stage, const uint4 (&raw)[CPL], auto is_v) {
-#pragma unroll
-      for (int i = 0; i < CPL; ++i) {
-        const int r = (tid + 256 * i) / LPR, chunk = 2 * (tid % LPR);
-        const int swz = decltype(is_v)::value ? tile::swizzle_v<RB>(r & 15) : tile::swizzle_k<RB>(r & 15);
-        *reinterpret_cast<uint4*>(stage + r * RB + ((chunk ^ swz) << 4)) = codes_to_chunk(raw[i].x, raw[i].y);
-        *reinterpret_cast<uint4*>(stage + r * RB + (((chunk + 1) ^ swz) << 4)) = codes_to_chunk(raw[i].z, raw[i].w);
-      }
+    auto store_codes = [&](char* stage, const uint4& raw, int i, auto is_v) {
+      const int r = (tid + 256 * i) / LPR, chunk = 2 * (tid % LPR);
+      const int swz = decltype(is_v)::value ? tile::swizzle_v<RB>(r & 15) : tile::swizzle_k<RB>(r & 15);
+      *reinterpret_cast<uint4*>(stage + r * RB + ((chunk ^ swz) << 4)) = codes_to_chunk(raw.x, raw.y);
+      *reinterpret_cast<uint4*>(stage + r * RB + (((chunk + 1) ^ swz) << 4)) = codes_to_chunk(raw.z, raw.w);
     };
     using Zero = std::integral_constant<int, 0>;
     using One = std::integral_constant<int, 1>;
@@ -367,11 +362,14 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
         for (int i = 0; i < NV; ++i) o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[i], pb, o[i], 0, 0, 0);
       }
     };
+    constexpr int KPC = NK / 4, NS = 2 * KPC, NA = NV;  // K steps and slots of a phase S, slots of a phase A
+    constexpr int SLOTS = 4 * NS + 3 * NA;              // that a copy can go out in
     // Scores of the next tile (K stage kb1) and P V of this one (V stage vb0) together: MFMAs one by one, each with a share of
     // the vector and LDS work behind it, in the order of attend.hip's step: S(g) a quarter of the scores, A(g) the 16 keys of
-    // chunk g; the probabilities of chunk g + 1 are formed under A(g) and S(g + 1), operands read a phase before their use.
+    // chunk g; the probabilities of chunk g + 1 are formed under A(g) and S(g + 1).  K operands are read under the A before, V
+    // operands under the S before: a phase more ahead takes 16 registers, is no faster with bf16 rows (387 and 388 us, 2 x 2048
+    // tokens, d = 128), and with 8-bit rows, whose codes come through registers, makes the loop spill (436, 400 us).
     auto step_math = [&](const f32x16 (&s_in)[2], f32x16 (&s_out)[2], auto kb1, auto vb0, auto&& copy_slot) {
-      constexpr int KPC = NK / 4, NS = 2 * KPC, NA = NV;  // K steps and slots of a phase S, slots of a phase A
       static_assert(NS == NA && 8 % (NS + NA) == 0, "phases divide the vector work evenly");
       const float mc = m * c;
       bf16x8 kop[NK][2], vop[4][NV];
@@ -401,11 +399,8 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
         const int ks = gch * KPC + (i >> 1), cb = i & 1;
         s_out[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop[ks][cb], qreg[ks], s_out[cb], 0, 0, 0);
         fence();
-        if (gch == 0) {
-          if (ks + 1 < KPC) load_k(ks + 1, cb);
-          vop[0][i] = read_v(vb0, 0, i);
-        }
-        if (gch < 3) load_k(ks + KPC, cb);
+        if (gch == 0 && ks + 1 < KPC) load_k(ks + 1, cb);
+        vop[gch][i] = read_v(vb0, gch, i);
         copy_slot(slot++);
         const int share = gch == 0 ? 8 / NS : 8 / (NS + NA);
         for (int u = 0; u < share; ++u) probability(gch, done++);
@@ -422,7 +417,7 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
           o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop[gch][d], pb[gch].v, o[d], 0, 0, 0);
           fence();
           if (gch < 3) {
-            vop[gch + 1][d] = read_v(vb0, gch + 1, d);
+            load_k((gch + 1) * KPC + (d >> 1), d & 1);
             copy_slot(slot++);
 #pragma unroll
             for (int u = 0; u < 8 / (NS + NA); ++u) probability(gch + 1, done++);
@@ -444,18 +439,25 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     // `at`: where tile it + 1 lies; tile it + 2 is looked up between the two.
     f32x16 s_a[2], s_b[2];
     TileRows at{};
-    // `math(copy)`: what the wavefront computes in the step; it calls copy(i) for i = 0 .. 3 CPT - 1, in order.
+    // `math(copy)`: what the wavefront computes in the step; it calls copy(i) for i = 0 .. SLOTS - 1, in order.
     auto step = [&](int it, auto kb1, auto vb0, auto&& math) {
       wait_vmcnt<0>();
       __syncthreads();
-      if constexpr (FP8) {
-        uint4 raw_k[CPL], raw_v[CPL];
-        load_codes(v_pages, at, it + 1, raw_v);
-        at = locate(it + 2);
-        load_codes(k_pages, at, it + 2, raw_k);
-        math([](int) {});
-        store_codes(lds[decltype(kb1)::value][1], raw_v, One{});
-        store_codes(lds[decltype(vb0)::value][0], raw_k, Zero{});
+      if constexpr (FP8) {  // V's codes have the first half of the step to arrive, K's the second
+        uint4 raw[CPL];
+        math([&](int i) {
+          if (i == 0)
+#pragma unroll
+            for (int k = 0; k < CPL; ++k) raw[k] = load_codes(v_pages, at, it + 1, k);
+          else if (i == 1)
+            at = locate(it + 2);
+          else if (i >= SLOTS / 2 && i < SLOTS / 2 + CPL) {
+            store_codes(lds[decltype(kb1)::value][1], raw[i - SLOTS / 2], i - SLOTS / 2, One{});
+            raw[i - SLOTS / 2] = load_codes(k_pages, at, it + 2, i - SLOTS / 2);
+          }
+        });
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) store_codes(lds[decltype(vb0)::value][0], raw[k], k, Zero{});
       } else {
         math([&](int i) {
           if (i < CPT)
@@ -469,7 +471,7 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     };
     auto copies_only = [](auto&& copy) {
 #pragma unroll
-      for (int i = 0; i < 3 * CPT; ++i) copy(i);
+      for (int i = 0; i < SLOTS; ++i) copy(i);
     };
     auto pipe_step = [&](int it, auto kb1, auto vb0, f32x16 (&s_in)[2], f32x16 (&s_out)[2]) {
       step(it, kb1, vb0, [&](auto&& copy) {
@@ -485,14 +487,21 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
       const int second = begin + 1 < end ? begin + 1 : begin;
       at = locate(begin);
       if constexpr (FP8) {
-        uint4 raw[CPL], raw2[CPL], raw3[CPL];
-        load_codes(k_pages, at, begin, raw);
-        load_codes(v_pages, at, begin, raw2);
+        uint4 raw[3][CPL];
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) {
+          raw[0][k] = load_codes(k_pages, at, begin, k);
+          raw[1][k] = load_codes(v_pages, at, begin, k);
+        }
         at = locate(second);
-        load_codes(k_pages, at, second, raw3);
-        store_codes(lds[0][0], raw, Zero{});
-        store_codes(lds[0][1], raw2, One{});
-        store_codes(lds[1][0], raw3, Zero{});
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) raw[2][k] = load_codes(k_pages, at, second, k);
+#pragma unroll
+        for (int k = 0; k < CPL; ++k) {
+          store_codes(lds[0][0], raw[0][k], k, Zero{});
+          store_codes(lds[0][1], raw[1][k], k, One{});
+          store_codes(lds[1][0], raw[2][k], k, Zero{});
+        }
       } else {
 #pragma unroll
         for (int i = 0; i < CPT; ++i) copy_k(at, begin, Zero{}, i);
