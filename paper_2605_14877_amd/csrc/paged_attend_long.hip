@@ -7,7 +7,7 @@
 // copies), keys that a row does not see get a score of -inf in the tiles where that can be.
 // 8-bit cache rows come through registers, converted on the way into the stage.
 // Chosen pages: the walk is over the union of the pages that the workgroup's tokens have chosen (up to 128 of them, neighbours in
-// the request, which choose alike), with a word of 32 tokens for each wavefront and page; every tile is masked.
+// the request, which choose alike), with a word of 32 tokens for each wavefront and page.
 //
 // Bound: the matrix pipe, and the vector work of the softmax next to it.
 #include <hip/hip_runtime.h>
@@ -343,10 +343,28 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
       tile::mask_rows(limit - it * BN, hl, s);
       return true;
     };
+    // Masks tile `it`, of whose scores `mx` is the lane's maximum; the maximum of those that are seen.  Chosen pages: where
+    // the tile lies in one page and ends before the last key of all rows, a row sees all of it or nothing.  `open` is whether
+    // it does, and takes the scores' place: behind a closed one the probabilities are 2^(s c - inf) = 0.
+    auto seen_max = [&](int it, f32x16 (&s)[2], float mx, bool& open) {
+      if constexpr (CHOSEN) {
+        if (per_log2 >= 2) {
+          const int u = 4 * it >> per_log2, off = 4 * it & ((1 << per_log2) - 1);
+          const int pos = ((__builtin_amdgcn_readfirstlane(chosen.page[u]) << per_log2) + off) * 16;
+          if (pos + BN <= limit_min) {
+            open = __builtin_amdgcn_readfirstlane(chosen.who[4 * u + wave]) >> token & 1;
+            return open ? mx : -INFINITY;
+          }
+        }
+        open = true;
+      }
+      return mask(it, s) ? lane_max(s) : mx;
+    };
+    auto reference = [&](bool open) { return CHOSEN && !open ? INFINITY : m * c; };
     // P^T = 2^(S^T c - m c) in bf16 and O^T += V^T P^T.  Probabilities are rounded for the product; the row sum takes them as
     // they are (its logarithm is an output, in fp32).
-    auto accumulate = [&](const f32x16 (&s)[2], auto buf_tag) {
-      const float mc = m * c;
+    auto accumulate = [&](const f32x16 (&s)[2], auto buf_tag, bool open) {
+      const float mc = reference(open);
 #pragma unroll
       for (int chunk = 0; chunk < 4; ++chunk) {
         bf16x8 va[NV], pb;
@@ -369,9 +387,9 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     // chunk g; the probabilities of chunk g + 1 are formed under A(g) and S(g + 1).  K operands are read under the A before, V
     // operands under the S before: a phase more ahead takes 16 registers, is no faster with bf16 rows (387 and 388 us, 2 x 2048
     // tokens, d = 128), and with 8-bit rows, whose codes come through registers, makes the loop spill (436, 400 us).
-    auto step_math = [&](const f32x16 (&s_in)[2], f32x16 (&s_out)[2], auto kb1, auto vb0, auto&& copy_slot) {
+    auto step_math = [&](const f32x16 (&s_in)[2], bool open, f32x16 (&s_out)[2], auto kb1, auto vb0, auto&& copy_slot) {
       static_assert(NS == NA && 8 % (NS + NA) == 0, "phases divide the vector work evenly");
-      const float mc = m * c;
+      const float mc = reference(open);
       bf16x8 kop[NK][2], vop[4][NV];
       float e[4][8];
       union {
@@ -473,15 +491,16 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
 #pragma unroll
       for (int i = 0; i < SLOTS; ++i) copy(i);
     };
+    bool open = true;  // of the scores at hand
     auto pipe_step = [&](int it, auto kb1, auto vb0, f32x16 (&s_in)[2], f32x16 (&s_out)[2]) {
       step(it, kb1, vb0, [&](auto&& copy) {
-        const float mx = step_math(s_in, s_out, kb1, vb0, copy);
-        raise(mask(it + 1, s_out) ? lane_max(s_out) : mx);
+        const float mx = step_math(s_in, open, s_out, kb1, vb0, copy);
+        raise(seen_max(it + 1, s_out, mx, open));
       });
     };
     auto last_step = [&](int it, auto kb1, auto vb0, f32x16 (&s_in)[2]) {
       step(it, kb1, vb0, copies_only);
-      accumulate(s_in, vb0);
+      accumulate(s_in, vb0, open);
     };
     if (begin < end) {
       const int second = begin + 1 < end ? begin + 1 : begin;
@@ -515,8 +534,7 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
       __syncthreads();
       if (begin < my_end) {
         scores(s_a, Zero{});
-        mask(begin, s_a);
-        raise(lane_max(s_a));
+        raise(seen_max(begin, s_a, lane_max(s_a), open));
       }
       // Every wavefront makes all steps (the barriers are shared), those behind its last tile without arithmetic.
       int it = begin;
