@@ -20,7 +20,10 @@ namespace heatkv {
 namespace {
 
 constexpr int LANES = 256;
-constexpr long long FEW_PAGES = 4096;  // tokens x heads up to which a workgroup takes a page: as many as are resident at a time, twice
+// Tokens x heads up to which a workgroup takes a page, so that its rows are read by 256 lanes; a wavefront beyond.  A token each,
+// 8 heads, pages of 16, 64, 256 rows: 32 requests 4.5, 4.8, 6.7 us by workgroups, 4.7, 5.4, 10.4 by wavefronts; 128 requests
+// 6.3, 7.0, 10.9 and 4.8, 6.5, 12.2; 512 requests, pages of 64, 17.2 and 13.9.
+constexpr long long FEW_PAGES = 512;
 
 // 8 values of a row, as floats.
 template <class T>

@@ -210,8 +210,8 @@ __device__ __forceinline__ long long total_segments(const AttendParams& p, const
   requests.scan(requests.mine([&](const Load& l) { return static_cast<long long>(l.tiles) * p.c.H; }), scratch, count);
   return count;
 }
-__device__ __forceinline__ long long share_of(const AttendParams& p, long long total) {
-  return max(quotient(total + p.workgroups - 1, p.workgroups), static_cast<long long>(p.least_weight));
+__device__ __forceinline__ long long share_of(const AttendParams& p, long long total, long long shares) {
+  return max(quotient(total + shares - 1, shares), static_cast<long long>(p.least_weight));
 }
 
 // By pieces only: whole segments from whole_from on, or where the workspace has no place for parts.
@@ -221,7 +221,7 @@ __device__ __forceinline__ bool only_piece(const AttendParams& p, int w, Scratch
   long long upto, mine;
   const long long total = total_weight(p, requests, scratch, upto, mine);
   const bool whole = !p.borders || total_segments(p, requests, scratch) >= p.whole_from;
-  return find_piece(p, requests, w, whole ? total + 1 : share_of(p, total), scratch, part);
+  return find_piece(p, requests, w, whole ? total + 1 : share_of(p, total, p.workgroups), scratch, part);
 }
 
 struct Place {
@@ -234,7 +234,7 @@ struct Place {
 template <int ROWS, int KEYS>
 __device__ __forceinline__ Place find_place(const AttendParams& p, const Requests<ROWS, KEYS>& requests, int w, long long total,
                                             long long upto, long long mine, Scratch& scratch) {
-  const long long share = share_of(p, total);
+  const long long share = share_of(p, total, p.workgroups);
   Place at{};
   at.pos = w * share;
   at.stop = min(at.pos + share, total);
@@ -288,7 +288,7 @@ __device__ __forceinline__ bool next_part(const AttendParams& p, Place& at, Part
 }
 
 // A workgroup's parts, one after the other; what they are is kept in LDS: the tile loops have no registers to spare.  Pieces
-// where there are fewer segments than half the workgroups (whole_from), the line otherwise.
+// where there are few segments (whole_from), the line otherwise.
 struct Line {
   Scratch scratch;
   Place place;
@@ -299,12 +299,13 @@ struct Line {
     const Requests<ROWS, KEYS> requests(p);
     long long upto, mine;
     const long long total = total_weight(p, requests, scratch, upto, mine);
-    const bool by_pieces = total_segments(p, requests, scratch) < p.whole_from;
+    const long long segments = total_segments(p, requests, scratch);
+    const bool by_pieces = segments < p.whole_from;  // with one more for each segment they are as many as the workgroups
     Place at{};
     Part only{};
     bool some = false;
     if (by_pieces)
-      some = find_piece(p, requests, w, p.borders ? share_of(p, total) : total + 1, scratch, only);
+      some = find_piece(p, requests, w, p.borders ? share_of(p, total, p.workgroups - segments) : total + 1, scratch, only);
     else
       at = find_place(p, requests, w, total, upto, mine, scratch);
     if (threadIdx.x == 0) {

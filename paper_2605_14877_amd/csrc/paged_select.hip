@@ -228,7 +228,7 @@ __global__ __launch_bounds__(LANES) void paged_select_kernel(PagedSelectParams p
         for (int r = 0; r < 4; ++r) {
           const int x = first + 4 * g + r;
           const float score = static_cast<float>(s[r] + (t[r] << 7)) * __shfl(scale[u], 4 * g + r, 64);
-          unsigned key = x < seen ? max(ordered(score), 1u) : 0u;
+          unsigned key = x < seen ? min(max(ordered(score), 1u), FORCED - 1) : 0u;
           if (x < seen && (x < p.first || x >= seen - p.last)) key = FORCED;
           if (n < TW) keys[n * pitch + x] = key;
         }
@@ -348,13 +348,14 @@ template <class T, int D>
 hipError_t launch(PagedSelectParams p, hipStream_t stream) {
   p.pitch = (p.c.max_pages + 15) / 16 * 16;
   auto lds = [&](int tw) { return static_cast<size_t>(tw) * (4 * D + 4 * static_cast<size_t>(std::max(p.pitch, 2 * D))); };
-  // Tokens of a request share a pass over the bounds, as many as leave four workgroups for every compute unit, and whose scores
-  // fit into the LDS.  Little more than one token for each request: one per workgroup.  1024 tokens of 4 kv heads over 272
-  // pages, 16, 4 and 1 tokens: 47, 26 and 33 us.
+  // Tokens of a request share a pass over the bounds: one, four or sixteen to a workgroup, as many as leave work for half of the
+  // compute units with four, for all of them, four workgroups each, with sixteen, and whose scores fit into the LDS.  4 kv heads
+  // over 272 pages, 16, 4 and 1 tokens to a workgroup: 64 new tokens 19.1, 10.7, 9.9 us, 128 18.8, 10.5, 11.8, 768 19.9, 15.9,
+  // 44.2, 1024 19.8, 23.9, 57.4.  Little more than one token for each request: one.
   const long long units = static_cast<long long>(p.c.tokens) * p.c.H;
   if (p.c.tokens > 2 * p.c.batch + 16) {
-    if (units >= 16 * 1024 && lds(16) <= 80 * 1024) return launch<T, D, 16, 1>(p, lds(16), stream);
-    if (units >= 4 * 1024 && lds(4) <= PAGED_SELECT_LDS) return launch<T, D, 4, 1>(p, lds(4), stream);
+    if (units >= 4 * 1024 && lds(16) <= 80 * 1024) return launch<T, D, 16, 1>(p, lds(16), stream);
+    if (units >= 512 && lds(4) <= PAGED_SELECT_LDS) return launch<T, D, 4, 1>(p, lds(4), stream);
   }
   return launch<T, D, 1, WAVES>(p, lds(1), stream);
 }

@@ -168,12 +168,14 @@ def rules(tmp_path_factory):
 
 
 def test_launch_rules_on_both_sides(rules):
-    few, many, _ = rules(True, 64, 8, 4, 64 + 16, 512, 16)  # a decoding step and padding
-    assert many["workgroups"] == 0 and few["most_rows"] > 10 ** 6 and few["parts"] > 0
-    few, many, _ = rules(True, 64, 8, 4, 64 + 17, 512, 16)
-    assert many["workgroups"] and few["most_rows"] == many["least_rows"] == 64
+    for pages, top, extra, least in ((512, 0, 40, 16), (1023, 0, 40, 16), (1024, 0, 16, 16), (1024, 8, 40, 64)):
+        few, many, _ = rules(True, 64, 8, 4, 64 + extra, pages, 16, top)  # a decoding step and padding
+        assert many["workgroups"] == 0 and few["most_rows"] > 10 ** 6 and few["parts"] > 0
+        few, many, _ = rules(True, 64, 8, 4, 64 + extra + 1, pages, 16, top)
+        assert many["workgroups"] and few["most_rows"] == many["least_rows"] == least
     assert rules(False, 1, 8, 4, 5000, 512, 16)[1]["workgroups"] == 0  # fp32 has one kernel
-    assert rules(True, 1, 1, 1, 64, 512, 16)[1]["workgroups"] == 0 and rules(True, 1, 1, 1, 65, 512, 16)[1]["workgroups"]
+    assert rules(True, 1, 1, 1, 41, 512, 16)[1]["workgroups"] == 0 and rules(True, 1, 1, 1, 42, 512, 16)[1]["workgroups"]
+    assert rules(True, 1, 1, 1, 64, 512, 16, 4)[1]["workgroups"] == 0 and rules(True, 1, 1, 1, 65, 512, 16, 4)[1]["workgroups"]
     assert rules(True, 1, 8, 4, 1, 16, 16)[0]["parts"] == 0 and rules(True, 1, 8, 4, 1, 17, 16)[0]["parts"] > 0
     few, many, size = rules(True, 1, 8, 1, 4000, 32768, 16, 512)  # a union too large for the LDS
     assert size > 92 * 1024 and many["workgroups"] == 0
@@ -234,7 +236,8 @@ def test_pieces_of_the_16_row_launch_fit_the_grid_and_the_workspace(rules):
         count, total = heads * sum(t for t, _ in segments), heads * sum(t * w for t, w in segments)
         if not few["parts"] or not 0 < count < few["whole_from"]:
             continue
-        share = max(-(-total // few["workgroups"]), few["least_steps"] * 32)
+        shares = few["workgroups"] - count
+        share = max(-(-total // shares), few["least_steps"] * 32)
         pieces = heads * sum(t * -(-w // share) for t, w in segments)
         assert pieces <= few["grid"] <= few["parts"]
         some += 1
