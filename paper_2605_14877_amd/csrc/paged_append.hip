@@ -8,7 +8,8 @@
 //
 // Bound: memory traffic for prompts (rows in, rows out, 16 bytes per lane), latency for single tokens.  A page's bounds are
 // formed anew from all of its valid rows, which costs a decoding step up to a page of older rows per head, but needs no
-// running state that would have to follow when tokens are dropped or pages change owners.
+// running state that would have to follow when tokens are dropped or pages change owners.  12 prompts, 12000 tokens, 8 heads, d =
+// 128, into 8-bit pages: 73.5 MB in 21 us, 3.5 TB/s; the rows alone take 13.5 us.
 #include <type_traits>
 
 #include "copy_rows.h"

@@ -10,7 +10,6 @@
 namespace heatkv {
 namespace paged {
 
-constexpr int MAX_TOP = 512;
 constexpr size_t WALK_LDS = 144 * 1024;
 
 // Where 16 consecutive keys lie.  pos: position of the first one; `row`, in rows of the cache, is in range also for granules
