@@ -317,8 +317,8 @@ int heatkv_rank_dispersion(const heatkv_shape* shape, const float* betas, int ru
  * ranges are brought into them: such a call gives wrong outputs, but touches nothing outside of the arrays.
  *
  * Limits: q_heads a multiple of kv_heads, at most 16 per kv head; kv_heads <= 1024; d = 64 or 128; page_size 16, 32, 64, 128
- * or 256; batch <= 4096; tokens <= 2^22; num_pages * page_size and max_pages * page_size <= 2^30, num_pages * page_size *
- * kv_heads <= 2^34; top <= 512 and max_pages <= 32768 where pages are chosen. */
+ * or 256; batch <= 4096; tokens <= 2^22, tokens * kv_heads <= 2^23; num_pages * page_size and max_pages * page_size <= 2^30,
+ * num_pages * page_size * kv_heads <= 2^34; top <= 512 and max_pages <= 32768 where pages are chosen. */
 typedef struct {
   int32_t q_heads, kv_heads, d, dtype, kv_format;
   int32_t page_size, num_pages; /* of the cache */

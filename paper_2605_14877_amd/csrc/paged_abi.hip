@@ -18,6 +18,7 @@ using heatkv::fail;
 namespace {
 
 constexpr int64_t kMaxTokens = int64_t(1) << 22;      // rows of the token tensors
+constexpr int64_t kMaxTokenHeads = int64_t(1) << 23;  // times kv heads
 constexpr int64_t kMaxPositions = int64_t(1) << 30;   // keys of a request, rows of the cache per kv head
 constexpr int kMaxGroup = 16, kMaxTop = 512, kMaxSelectPages = 32768;
 
@@ -53,6 +54,13 @@ int check_shape(const heatkv_paged_shape* s) {
 
 int check_tokens(int64_t tokens) {
   if (tokens < 0 || tokens > kMaxTokens) return fail(HEATKV_EINVAL, "tokens must be in [0, 2^22]");
+  return HEATKV_OK;
+}
+
+// Of calls whose work is by tokens and kv heads: a launch has less than 2^32 lanes, up to 256 for each of them.
+int check_tokens(const heatkv_paged_shape* s, int64_t tokens) {
+  if (int rc = check_tokens(tokens)) return rc;
+  if (tokens * s->kv_heads > kMaxTokenHeads) return fail(HEATKV_EINVAL, "tokens * kv_heads must be at most 2^23");
   return HEATKV_OK;
 }
 
@@ -152,7 +160,7 @@ int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const voi
            const int32_t* table, const int32_t* q_start, const int32_t* lens, const int32_t* selected, int top, float sm_scale,
            int causal, heatkv_rows out, float* lse, void* ws, size_t ws_bytes, void* stream) {
   int rc = check_shape(s);
-  if (!rc) rc = check_tokens(tokens);
+  if (!rc) rc = check_tokens(s, tokens);
   if (rc) return rc;
   if (!(sm_scale > 0.f) || !std::isfinite(sm_scale)) return fail(HEATKV_EINVAL, "sm_scale must be positive and finite");
   if (tokens == 0) return HEATKV_OK;
@@ -247,7 +255,7 @@ int heatkv_paged_assign(const heatkv_paged_shape* s, const int32_t* keep, const 
 int heatkv_paged_append(const heatkv_paged_shape* s, const int32_t* slots, int64_t tokens, heatkv_rows k_new, heatkv_rows v_new,
                         void* k_pages, void* v_pages, int8_t* bounds, float* bound_scales, void* stream) {
   int rc = check_shape(s);
-  if (!rc) rc = check_tokens(tokens);
+  if (!rc) rc = check_tokens(s, tokens);
   if (rc || tokens == 0) return rc;
   rc = check_ints({slots});
   if (!rc) rc = check_rows(s, k_new, "k_new");
@@ -280,7 +288,7 @@ int heatkv_paged_append(const heatkv_paged_shape* s, const int32_t* slots, int64
 }
 
 size_t heatkv_paged_attend_workspace_bytes(const heatkv_paged_shape* s, int64_t tokens, int top) {
-  if (check_shape(s) || check_tokens(tokens)) return 0;
+  if (check_shape(s) || check_tokens(s, tokens)) return 0;
   if (top < 0 || top > kMaxTop) return 0;
   return workspace_of(s, plan_of(s, tokens, top)).total;
 }
@@ -296,7 +304,7 @@ int heatkv_paged_select(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows
                         const float* bound_scales, const int32_t* table, const int32_t* q_start, const int32_t* lens, int first,
                         int last, int top, int causal, int32_t* selected, void* stream) {
   int rc = check_shape(s);
-  if (!rc) rc = check_tokens(tokens);
+  if (!rc) rc = check_tokens(s, tokens);
   if (rc) return rc;
   if (top < 1 || top > kMaxTop) return fail(HEATKV_EINVAL, "top must be in [1, 512]");
   if (first < 0 || last < 1 || int64_t(first) + last > top)

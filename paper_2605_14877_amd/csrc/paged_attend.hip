@@ -306,7 +306,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_kernel(AttendParam
             return RedoGranule{at.row, at.pos, walk.sees(at, jr - j_first)};
           },
           [&](float score) { return fast_exp2((score - m_row) * c); },
-          [&](int col, float x) {
+          [&](int col, float x, float) {
             if (!alone)
               z.part_o[(part_base + r) * D + col] = x;
             else

@@ -188,7 +188,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_f32_kernel(AttendP
             return RedoGranule{x.row, x.pos, walk.sees(x, jr - j_first)};
           },
           [&](float score) { return prob(score * prob.c, m_row) * 0x1p-8f; },
-          [&](int col, float x) {
+          [&](int col, float x, float) {
             if (!alone)
               z.part_o[(part_base + r) * D + col] = x;
             else

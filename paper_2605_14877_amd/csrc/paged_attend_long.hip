@@ -348,7 +348,8 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
   };
   // Masks tile `it`, of whose scores `mx` is the lane's maximum; the maximum of those that are seen.  Chosen pages: where
   // the tile lies in one page and ends before the last key of all rows, a row sees all of it or nothing.  `open` is whether
-  // it does, and takes the scores' place: behind a closed one the probabilities are 2^(s c - inf) = 0.
+  // it does, and takes the scores' place: behind a closed one the probabilities are 2^(s c - inf) = 0, or NaN where s is not
+  // finite; the row is then done anew (paged_redo.h).
   auto seen_max = [&](int it, f32x16 (&s)[2], float mx, bool& open) {
     if constexpr (CHOSEN) {
       if (per_log2 >= 2) {
@@ -611,7 +612,7 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     const int j = __builtin_amdgcn_readlane(out.j, r), hq = __builtin_amdgcn_readlane(out.hq, r);
     const float m_row = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, m), r));
     const float l_row = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, l), r));
-    const float norm = !alone ? 1.f : l_row > 0.f ? 1.f / l_row : l_row;
+    const bool lost = CHOSEN && l_row != l_row;  // a score that is not finite, of a page that other rows have chosen or this one
     redo_row<bf16_t, FP8, D>(
         z, tl.q0 + j, hq, visible_keys(z.c, tl, j), 4 * begin, 4 * end,
         [&](int g) {
@@ -626,9 +627,17 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
           return RedoGranule{static_cast<long long>(from) * 16, pos, seen};
         },
         [&](float score) { return fast_exp2((score - m_row) * c); },
-        [&](int col, float x) {
+        [&](int col, float x, float sum) {
+          const long long part_row = static_cast<long long>(w) * BM + w_row + r;
+          const float l_seen = lost ? sum : l_row, norm = l_seen > 0.f ? 1.f / l_seen : l_seen;
+          if (lost && col == 0) {
+            if (!alone)
+              z.part_ml[part_row * 2 + 1] = sum;
+            else if (z.lse)
+              z.lse[(tl.q0 + j) * static_cast<long long>(z.c.Hq) + hq] = natural_lse(m_row, sum, z.sm_scale);
+          }
           if (!alone)
-            z.part_o[(static_cast<long long>(w) * BM + w_row + r) * D + col] = x;
+            z.part_o[part_row * D + col] = x;
           else
             (static_cast<bf16_t*>(const_cast<void*>(z.out.data)) + (tl.q0 + j) * z.out.token_stride + hq * z.out.head_stride)[col] =
                 static_cast<bf16_t>(x * norm);

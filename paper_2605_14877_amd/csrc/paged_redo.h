@@ -21,13 +21,13 @@ __device__ __forceinline__ float cache_value(const void* pages, long long at) {
 
 // Query head hq of `token` over the granules [begin, end): locate(g) gives {row, pos, whether the row sees the granule's page}, keys
 // from `limit` on are not seen.  probability(s): of a raw score, relative to the reference that the row's sum was formed with.
-// store(column, value) gets the unnormalised sums, two columns or one per lane.
+// store(column, value, sum of the probabilities) gets the unnormalised sums, two columns or one per lane.
 template <class T, bool FP8, int D, class Locate, class Probability, class Store>
 __device__ __forceinline__ void redo_row(const AttendParams& p, long long token, int hq, int limit, int begin, int end,
                                          const Locate& locate, const Probability& probability, const Store& store) {
   const int lane = threadIdx.x & 63, key = lane >> 2, quarter = lane & 3;
   const T* q = static_cast<const T*>(p.q.data) + token * p.q.token_stride + hq * p.q.head_stride;
-  float x[D / 64] = {};
+  float x[D / 64] = {}, sum = 0.f;
   for (int g = begin; g < end; ++g) {
     const auto at = locate(g);
     if (!at.seen || at.pos >= limit) continue;
@@ -39,13 +39,15 @@ __device__ __forceinline__ void redo_row(const AttendParams& p, long long token,
     const float e = at.pos + key < limit ? probability(s) : -1.f;
     for (int k = 0; k < 16; ++k) {
       const float w = __shfl(e, 4 * k, 64);
-      if (!(w < 0.f))  // seen, whatever its probability
+      if (!(w < 0.f)) {  // seen, whatever its probability
+        sum += w;
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) x[i] += w * cache_value<T, FP8>(p.v_pages, (at.row + k) * D + 64 * i + lane);
+      }
     }
   }
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) store(64 * i + lane, x[i]);
+  for (int i = 0; i < D / 64; ++i) store(64 * i + lane, x[i], sum);
 }
 
 struct RedoGranule {

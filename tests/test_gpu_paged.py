@@ -538,6 +538,171 @@ def test_pages_that_a_token_has_not_chosen_do_not_reach_it(case):
         assert fine.any() and not fine.all()
 
 
+@pytest.mark.parametrize("case", [("bf16", 4, 1, 128, 64, [3000, 900], [90, 70]), ("bf16", 4, 2, 64, 128, [2600], [200]),
+                                  ("fp8", 4, 2, 128, 64, [1700, 300], [20, 70]), ("fp8", 2, 1, 64, 256, [6000], [100]),
+                                  ("bf16", 16, 1, 128, 64, [500, 64], [60, 40])], ids=str)
+@pytest.mark.parametrize("top", [2, 9])
+def test_large_pages_that_a_token_of_a_chunk_has_not_chosen_do_not_reach_it(case, top):
+    p = Problem(*case, seed=17)
+    _spoil(p, 4, False)
+    r = random.Random(6)
+    pages = max(p.lens) // p.page + 1
+    sel = [[[r.randrange(0, pages) for _ in range(top)] for _ in range(p.H)] for _ in range(p.tokens)]
+    for causal in (True, False):
+        out, lse = p.run(causal, _ints(sel))
+        fine = _check_with_nan(p, causal, (out, lse), sel)
+        assert fine.any() and not fine.all()
+        want = ref.attend(p.q, p.k, p.v, p.table, p.q_start, p.lens, p.page, p.sm, causal, sel)[1][:p.q_start[-1]]
+        k = torch.where(p.k.double().isfinite(), p.k.double(), 0.0).abs()
+        S = float(p.q.abs().double().amax((0, 1)) @ k.amax((0, 1, 2))) * p.sm
+        e = 2.0 ** -24 * (p.d * S + 2 * 1.443 * 2 * S + max(p.lens) + 64)
+        sure = want.isfinite()
+        assert sure.any() and torch.all((lse[:p.q_start[-1]].cpu().double() - want)[sure].abs() <= e + 2.0 ** -22 * want[sure].abs())
+
+
+# ---- many requests, many tokens, large caches, shared pages, calls at the same time -------------------------------------
+
+@pytest.mark.parametrize("case", [("bf16", 16, 1, 128, 64, [40, 5, 60], [33, 5, 20]), ("bf16", 8, 1, 64, 16, [30] * 8, [6] * 8),
+                                  ("fp8", 4, 1, 128, 32, [100, 17] * 3, [10, 17] * 3), ("fp8", 16, 1, 64, 16, [2, 70, 5], [2, 60, 2])],
+                         ids=str)
+@pytest.mark.parametrize("causal", [True, False])
+def test_chunks_of_a_few_tokens(case, causal):
+    p = Problem(*case, seed=18)
+    p.check(causal, p.run(causal))
+
+
+@pytest.mark.parametrize("dtype,heads,top", [("bf16", (4, 2), 0), ("fp8", (3, 1), 0), ("f32", (2, 2), 0), ("bf16", (4, 2), 3), ("f32", (2, 1), 3)])
+@pytest.mark.parametrize("batch", [64, 65, 300, 1000])
+def test_many_requests(dtype, heads, top, batch):
+    r = random.Random(batch)
+    new = [r.choice([0, 1, 1, 2, 9 if batch < 100 else 1]) for _ in range(batch)]
+    new[batch // 2] = 100  # a chunk among them
+    lens = [n + r.choice([0, 1, 15, 40, 150]) if n else r.choice([0, 33]) for n in new]
+    p = Problem(dtype, *heads, 64, 16, lens, new, seed=19)
+    sel = [[[r.randrange(-1, 8) for _ in range(top)] for _ in range(heads[1])] for _ in range(p.tokens)] if top else None
+    p.check(True, p.run(True, _ints(sel) if top else None), sel)
+
+
+@pytest.mark.parametrize("dtype,H,lens,new", [("bf16", 2, [300, 90], [260, 30]), ("bf16", 8, [600, 40], [520, 30]),
+                                              ("f32", 4, [200], [150]), ("f32", 64, [90, 70], [66, 20])])
+def test_choice_of_pages_of_many_tokens(dtype, H, lens, new):
+    p = Problem(dtype, 2 * H, H, 64, 16, lens, new, seed=20)
+    bounds, scales = _with_bounds(p)
+    top, first, last = 4, 1, 2
+    chosen = ref.select(p.q, bounds, scales, p.table, p.q_start, p.lens, p.page, first, last, top, True)
+    selected = torch.full((p.tokens, H, top), 77, dtype=torch.int32, device="cuda")
+    hk.heatkv_paged_select(p.shape, p.dev["q"], bounds.cuda(), scales.cuda(), p.dev["table"], p.dev["q_start"], p.dev["lens"],
+                           first, last, selected)
+    got = selected.tolist()
+    for t in range(p.q_start[-1]):
+        assert got[t] == [x + [-1] * (top - len(x)) for x in chosen[t]], t
+    assert torch.all(selected[p.q_start[-1]:] == 77)
+
+
+def test_scales_of_pages_that_are_not_numbers():
+    # of pages that no append has had: wrong choices, but no more of them than there is room for
+    p = Problem("bf16", 4, 1, 64, 16, [900, 400], [1, 1], seed=21, pad=0)
+    bounds, scales = _with_bounds(p)
+    scales.view(torch.int32)[:] = 0x7fffffff
+    room = torch.full((p.tokens + 1, 1, 5), 77, dtype=torch.int32, device="cuda")
+    hk.heatkv_paged_select(p.shape, p.dev["q"], bounds.cuda(), scales.cuda(), p.dev["table"], p.dev["q_start"], p.dev["lens"],
+                           1, 1, room[:p.tokens])
+    got = room.tolist()
+    assert got[-1] == [[77] * 5]
+    for t, n in enumerate((57, 25)):
+        assert got[t][0] == sorted(set(got[t][0])) and got[t][0][0] == 0 and got[t][0][-1] == n - 1
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", [1, 2]), ("bf16", [90, 30]), ("fp8", [90, 1]), ("f32", [20, 1])])
+def test_a_cache_of_more_than_4_gib(dtype, new):
+    # the requests' pages at both ends of a cache of 2^31 elements and more
+    p = Problem(dtype, 16, 8, 128, 256, [700, 300], new, seed=22, scale=0.5)
+    num_pages = 2 ** 31 // (8 * 256 * 128) * (2 if dtype == "fp8" else 1) + 9
+    n = p.num_pages
+    place = [0, 1] + list(range(num_pages - n + 2, num_pages))
+    shape = _shape(dtype, 16, 8, 128, 256, num_pages, 2, p.max_pages)
+    big = [torch.empty(shape.pages_shape, dtype=x.dtype, device="cuda") for x in (p.k, p.v)]
+    for x, small in zip(big, (p.k, p.v)):
+        x.view(torch.uint8)[place] = small.cuda().view(torch.uint8)
+    assert big[0].numel() * big[0].element_size() >= 2 ** 32
+    table = [[place[x] for x in row] + [0] * (p.max_pages - len(row)) for row in p.table]
+    p.shape = shape
+    p.dev.update(k=big[0], v=big[1], table=_ints(table))
+    p.check(True, p.run(True))
+    bounds, scales = _with_bounds(p)
+    big_bounds = torch.zeros(num_pages, 8, 2, 128, dtype=torch.int8, device="cuda")
+    big_scales = torch.zeros(num_pages, 8, device="cuda")
+    big_bounds[place], big_scales[place] = bounds.cuda(), scales.cuda()
+    chosen = ref.select(p.q, bounds, scales, p.table, p.q_start, p.lens, p.page, 0, 1, 2, True)
+    selected = torch.zeros(p.tokens, 8, 2, dtype=torch.int32, device="cuda")
+    hk.heatkv_paged_select(shape, p.dev["q"], big_bounds, big_scales, p.dev["table"], p.dev["q_start"], p.dev["lens"], 0, 1, selected)
+    got = selected.tolist()
+    for t in range(p.q_start[-1]):
+        assert got[t] == [x + [-1] * (2 - len(x)) for x in chosen[t]], t
+    p.check(True, p.run(True, selected), chosen)
+    # rows written there
+    slots = _ints([num_pages * 256 - 1, 5, (num_pages - 2) * 256, -1])
+    rows = torch.randn(4, 2, 8, 128, generator=torch.Generator().manual_seed(1)).to(DT[dtype]).cuda()
+    for with_bounds in (False, True):
+        for x in big:
+            for slot in slots[:3].tolist():
+                x.view(torch.uint8)[slot // 256, :, slot % 256] = 0
+        hk.heatkv_paged_append(shape, slots, rows[:, 0], rows[:, 1], *big, *((big_bounds, big_scales) if with_bounds else ()))
+        for i, slot in enumerate(slots[:3].tolist()):
+            for x, kv in zip(big, (0, 1)):
+                want = ref.to_store(rows[i, kv].cpu(), dtype == "fp8")
+                assert torch.equal(x[slot // 256, :, slot % 256].cpu().float(), want.float())
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", [1, 3, 1]), ("bf16", [60, 30, 1]), ("f32", [5, 1, 2])])
+def test_requests_may_share_pages(dtype, new):
+    p = Problem(dtype, 4, 2, 128, 16, [200, 170, 90], new, seed=23)
+    for row in p.table[1:]:
+        row[:3] = p.table[0][:3]  # a common prefix
+    full = [r + [0] * (p.max_pages - len(r)) for r in p.table]
+    p.dev["table"] = _ints(full)
+    p.check(True, p.run(True))
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", 1), ("bf16", 80), ("f32", 3)])
+def test_broadcast_queries(dtype, new):
+    # one query for all heads and tokens: strides of zero
+    p = Problem(dtype, 4, 2, 64, 16, [500, 90], [new, 1], seed=24)
+    one = p.q[:1, :1].clone()
+    p.q = one.expand(p.tokens, 4, 64)
+    p.check(True, p.run(True, q=one.cuda().expand(p.tokens, 4, 64)))
+
+
+def test_two_captured_graphs_with_a_workspace_each():
+    a, b = (Problem("bf16", 8, 2, 128, 16, [1900, 900, 30], [1, n, 2], seed=n) for n in (1, 90))
+    want = [p.run(True) for p in (a, b)]
+    graphs, outs, keep = [], [], []
+    for p in (a, b):
+        d = p.dev
+        out = torch.full_like(d["q"], 7.0)
+        ws = torch.full((max(hk.paged_attend_workspace_bytes(p.shape, p.tokens), 16),), 255, dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            hk.heatkv_paged_attend(p.shape, d["q"], d["k"], d["v"], d["table"], d["q_start"], d["lens"], p.sm, out, ws)
+        graphs.append(graph)
+        outs.append(out)
+        keep.append(ws)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for turn in range(4):
+        for out in outs:
+            out.fill_(7.0)
+        torch.cuda.synchronize()
+        for graph, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+        again = a.run(True)  # an eager call beside them
+        torch.cuda.synchronize()
+        for out, x in zip(outs, want):
+            assert torch.equal(out, x[0])
+        assert torch.equal(again[0], want[0][0])
+
+
 # ---- a server's steps ----------------------------------------------------------------------------------------------------
 
 class Server:

@@ -119,6 +119,18 @@ def test_arguments_that_do_not_fit_are_refused():
     _fail(assign(lens_out=a), "overlap")
 
 
+def test_calls_of_more_tokens_and_heads_than_a_launch_has_lanes_are_refused():
+    sh = _shape(q_heads=1024, kv_heads=1024)
+    rows, n = paged._CRows(1 << 20, 1024 * 128, 128), 2 ** 13 + 1
+    L, a = paged._lib(), 1 << 20
+    for call in (lambda: L.heatkv_paged_append(sh.ref, a, n, rows, rows, a, a, None, None, None),
+                 lambda: L.heatkv_paged_attend(sh.ref, n, rows, a, a, a, a, a, 0.1, 1, rows, None, a, 1 << 40, None),
+                 lambda: L.heatkv_paged_select(sh.ref, n, rows, a, a, a, a, a, 1, 1, 4, 1, a, None),
+                 lambda: L.heatkv_paged_attend_selected(sh.ref, n, rows, a, a, a, a, a, a, 4, 0.1, 1, rows, None, a, 1 << 40, None)):
+        _fail(call(), "2\\^23")
+    assert hk.paged_attend_workspace_bytes(sh, n) == 0 and hk.paged_attend_workspace_bytes(sh, n - 1) > 0
+
+
 def test_binding_names_tensors_that_are_not_on_a_device():
     sh = _shape()
     q = torch.zeros(4, 8, 128, dtype=torch.bfloat16)
