@@ -111,6 +111,14 @@ struct Border {
   int b, h, t, parts;  // a cut segment and its parts; 0: none at this workgroup
 };
 
+// Parts of cut segments: unnormalised outputs [..][ROWS][d], reference and sum [..][ROWS][2], two for each workgroup of the
+// line, one for each that takes a piece.
+struct Parts {
+  float *o, *ml;
+  Border* borders;  // of each workgroup; null: nothing can be cut
+  int grid;         // workgroups of the launch
+};
+
 struct AttendParams {
   Cache c;
   Rows q, out;
@@ -121,13 +129,10 @@ struct AttendParams {
   float* lse;           // [tokens][Hq] or null
   // Requests of this launch, by their query rows per kv head (new tokens x group): least_rows < rows <= most_rows.
   int least_rows, most_rows;
-  // How it is dealt (paged_schedule.h): shares, workgroups, weight of the lightest share, segments from which on none is cut.
-  int workgroups, grid, least_weight, whole_from;
+  // How it is dealt (paged_schedule.h): shares, weight of the lightest one, segments from which on it goes another way.
+  int workgroups, least_weight, whole_from;
   int cut_from;  // segments of up to this weight are not cut
-  // Parts of cut segments: unnormalised outputs [..][ROWS][d], reference and sum [..][ROWS][2], two for each workgroup of the
-  // line, one for each that takes a piece.
-  float *part_o, *part_ml;
-  Border* borders;  // of each workgroup; null: nothing can be cut
+  Parts parts;
 };
 
 // The launch's arguments, loaded anew.
@@ -151,11 +156,14 @@ constexpr size_t SELECT_LDS = 144 * 1024;  // what a workgroup may use: codes an
 
 using PagedSelectParams = paged::SelectParams;
 using PagedAttendParams = paged::AttendParams;
+using PagedParts = paged::Parts;
 constexpr size_t PAGED_SELECT_LDS = paged::SELECT_LDS;
 hipError_t launch_paged_select(const PagedSelectParams& p, int dtype, int d, hipStream_t stream);
 hipError_t launch_paged_attend_bf16(const PagedAttendParams& p, int d, bool fp8, hipStream_t stream);
 hipError_t launch_paged_attend_long(const PagedAttendParams& p, int d, bool fp8, hipStream_t stream);
 hipError_t launch_paged_attend_f32(const PagedAttendParams& p, int d, hipStream_t stream);
-hipError_t launch_paged_join(const PagedAttendParams& p, int dtype, int d, bool many, hipStream_t stream);
+// few, many: of the two attention launches, grid 0 where there is nothing to join.
+hipError_t launch_paged_join(const PagedAttendParams& p, const PagedParts& few, const PagedParts& many, int dtype, int d,
+                             hipStream_t stream);
 
 }  // namespace heatkv

@@ -189,28 +189,32 @@ int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const voi
   p.lse = lse;
   const auto hip_stream = static_cast<hipStream_t>(stream);
   const bool fp8 = s->kv_format == HEATKV_KV_FP8_E4M3;
+  hipError_t e = hipSuccess;
+  // Makes one of the two launches; its parts, with grid 0 if none can be cut.
   auto launch = [&](const heatkv::paged::Launch& l, const PartArrays& a, bool many) {
-    if (!l.workgroups) return hipSuccess;
+    heatkv::PagedParts parts{};
+    if (!l.workgroups || e != hipSuccess) return parts;
+    if (l.parts) {
+      parts.o = reinterpret_cast<float*>(static_cast<char*>(ws) + a.o);
+      parts.ml = reinterpret_cast<float*>(static_cast<char*>(ws) + a.ml);
+      parts.borders = reinterpret_cast<heatkv::paged::Border*>(static_cast<char*>(ws) + a.borders);
+    }
+    parts.grid = int(l.grid);
     p.workgroups = l.workgroups;
     p.least_weight = l.least_steps * heatkv::paged::STEP_WEIGHT;
     p.cut_from = l.parts ? p.least_weight : INT_MAX;
     p.least_rows = l.least_rows;
     p.most_rows = l.most_rows;
-    p.grid = int(l.grid);
     p.whole_from = l.whole_from;
-    p.borders = nullptr;
-    if (l.parts) {
-      p.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + a.o);
-      p.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + a.ml);
-      p.borders = reinterpret_cast<heatkv::paged::Border*>(static_cast<char*>(ws) + a.borders);
-    }
-    hipError_t e = s->dtype == HEATKV_F32 ? heatkv::launch_paged_attend_f32(p, s->d, hip_stream)
-                   : many                 ? heatkv::launch_paged_attend_long(p, s->d, fp8, hip_stream)
-                                          : heatkv::launch_paged_attend_bf16(p, s->d, fp8, hip_stream);
-    return e == hipSuccess && l.parts ? heatkv::launch_paged_join(p, s->dtype, s->d, many, hip_stream) : e;
+    p.parts = parts;
+    e = s->dtype == HEATKV_F32 ? heatkv::launch_paged_attend_f32(p, s->d, hip_stream)
+        : many                 ? heatkv::launch_paged_attend_long(p, s->d, fp8, hip_stream)
+                               : heatkv::launch_paged_attend_bf16(p, s->d, fp8, hip_stream);
+    if (!l.parts) parts.grid = 0;
+    return parts;
   };
-  hipError_t e = launch(plan.many, w.many, true);
-  if (e == hipSuccess) e = launch(plan.few, w.few, false);
+  const heatkv::PagedParts many = launch(plan.many, w.many, true), few = launch(plan.few, w.few, false);
+  if (e == hipSuccess && few.grid + many.grid > 0) e = heatkv::launch_paged_join(p, few, many, s->dtype, s->d, hip_stream);
   return launched(e, "paged_attend");
 }
 

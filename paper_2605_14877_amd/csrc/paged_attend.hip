@@ -254,7 +254,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_kernel(AttendParam
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) ll += part_l[w][tid] * fast_exp2((part_m[w][tid] - ml) * c);
       if (!alone) {
-        float* to = p.part_ml + (part_base + tid) * 2;
+        float* to = p.parts.ml + (part_base + tid) * 2;
         to[0] = ml;
         to[1] = ll;
       } else if (p.lse) {
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_kernel(AttendParam
       for (int k = 0; k < 8; ++k) nan = nan || x[k >> 2][k & 3] != x[k >> 2][k & 3];
       if (nan) atomicOr(&nan_rows, 1u << r);
       if (!alone) {
-        float* to = p.part_o + (part_base + r) * D + col;
+        float* to = p.parts.o + (part_base + r) * D + col;
         *reinterpret_cast<f32x4*>(to) = x[0];
         *reinterpret_cast<f32x4*>(to + 4) = x[1];
       } else {
@@ -308,7 +308,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_kernel(AttendParam
           [&](float score) { return fast_exp2((score - m_row) * c); },
           [&](int col, float x, float) {
             if (!alone)
-              z.part_o[(part_base + r) * D + col] = x;
+              z.parts.o[(part_base + r) * D + col] = x;
             else
               (static_cast<bf16_t*>(const_cast<void*>(z.out.data)) + (tile.q0 + jr) * z.out.token_stride + hr * z.out.head_stride)[col] =
                   static_cast<bf16_t>(x * norm);
@@ -324,7 +324,7 @@ hipError_t launch(const AttendParams& p, hipStream_t stream) {
   static std::atomic<unsigned long long> allowed{0};
   if (lds > 64 * 1024)
     if (hipError_t e = allow_lds(reinterpret_cast<const void*>(&paged_attend_kernel<D, FP8, CHOSEN>), WALK_LDS, allowed)) return e;
-  hipLaunchKernelGGL((paged_attend_kernel<D, FP8, CHOSEN>), dim3(p.grid), dim3(64 * WAVES), lds, stream, p);
+  hipLaunchKernelGGL((paged_attend_kernel<D, FP8, CHOSEN>), dim3(p.parts.grid), dim3(64 * WAVES), lds, stream, p);
   return hipGetLastError();
 }
 

@@ -150,7 +150,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_f32_kernel(AttendP
     if (wave == 0 && g == 0 && n < tile.rows) {
       const long long out_row = static_cast<long long>(tile.q0 + j) * p.c.Hq + hq;
       if (!alone) {
-        float* to = p.part_ml + (part_base + n) * 2;
+        float* to = p.parts.ml + (part_base + n) * 2;
         to[0] = m_all;
         to[1] = l_all;
       } else if (p.lse) {
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_f32_kernel(AttendP
       const int jr = divide(tile.row0 + r, p.c.div_G), hr = h * p.c.G + tile.row0 + r - jr * p.c.G;
       float* to = alone ? static_cast<float*>(const_cast<void*>(p.out.data)) + (tile.q0 + jr) * p.out.token_stride +
                               hr * p.out.head_stride + col
-                        : p.part_o + (part_base + r) * D + col;
+                        : p.parts.o + (part_base + r) * D + col;
       *reinterpret_cast<f32x4*>(to) = x;
       if (x[0] != x[0] || x[1] != x[1] || x[2] != x[2] || x[3] != x[3]) atomicOr(&nan_rows, 1u << r);
     }
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_f32_kernel(AttendP
           [&](float score) { return prob(score * prob.c, m_row) * 0x1p-8f; },
           [&](int col, float x, float) {
             if (!alone)
-              z.part_o[(part_base + r) * D + col] = x;
+              z.parts.o[(part_base + r) * D + col] = x;
             else
               (static_cast<float*>(const_cast<void*>(z.out.data)) + (tile.q0 + jr) * z.out.token_stride + hr * z.out.head_stride)[col] =
                   x * norm;
@@ -206,7 +206,7 @@ hipError_t launch(const AttendParams& p, hipStream_t stream) {
   static std::atomic<unsigned long long> allowed{0};
   if (lds > 64 * 1024)
     if (hipError_t e = allow_lds(reinterpret_cast<const void*>(&paged_attend_f32_kernel<D, CHOSEN>), WALK_LDS, allowed)) return e;
-  hipLaunchKernelGGL((paged_attend_f32_kernel<D, CHOSEN>), dim3(p.grid), dim3(64 * WAVES), lds, stream, p);
+  hipLaunchKernelGGL((paged_attend_f32_kernel<D, CHOSEN>), dim3(p.parts.grid), dim3(64 * WAVES), lds, stream, p);
   return hipGetLastError();
 }
 

@@ -577,14 +577,14 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     const long long part_row = static_cast<long long>(w) * BM + w_row + n;
     if (hl == 0) {
       if (!alone) {
-        z.part_ml[part_row * 2] = m;
-        z.part_ml[part_row * 2 + 1] = l;
+        z.parts.ml[part_row * 2] = m;
+        z.parts.ml[part_row * 2 + 1] = l;
       } else if (z.lse) {
         z.lse[out_row] = natural_lse(m, l, z.sm_scale);
       }
     }
     if (!alone) {
-      float* to = z.part_o + part_row * D + 4 * hl;
+      float* to = z.parts.o + part_row * D + 4 * hl;
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -632,12 +632,12 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
           const float l_seen = lost ? sum : l_row, norm = l_seen > 0.f ? 1.f / l_seen : l_seen;
           if (lost && col == 0) {
             if (!alone)
-              z.part_ml[part_row * 2 + 1] = sum;
+              z.parts.ml[part_row * 2 + 1] = sum;
             else if (z.lse)
               z.lse[(tl.q0 + j) * static_cast<long long>(z.c.Hq) + hq] = natural_lse(m_row, sum, z.sm_scale);
           }
           if (!alone)
-            z.part_o[part_row * D + col] = x;
+            z.parts.o[part_row * D + col] = x;
           else
             (static_cast<bf16_t*>(const_cast<void*>(z.out.data)) + (tl.q0 + j) * z.out.token_stride + hq * z.out.head_stride)[col] =
                 static_cast<bf16_t>(x * norm);
@@ -651,7 +651,7 @@ hipError_t launch(const AttendParams& p, hipStream_t stream) {
   static std::atomic<unsigned long long> allowed{0};
   if (lds > 64 * 1024)
     if (hipError_t e = allow_lds(reinterpret_cast<const void*>(&paged_attend_long_kernel<D, FP8, CHOSEN>), MANY_LDS, allowed)) return e;
-  hipLaunchKernelGGL((paged_attend_long_kernel<D, FP8, CHOSEN>), dim3(p.grid), dim3(256), lds, stream, p);
+  hipLaunchKernelGGL((paged_attend_long_kernel<D, FP8, CHOSEN>), dim3(p.parts.grid), dim3(256), lds, stream, p);
   return hipGetLastError();
 }
 

@@ -1,6 +1,7 @@
 // Paged attention: joins the parts of segments that several workgroups had (paged_schedule.h).  A workgroup looks at one border
 // between shares, or one piece, and joins the segment there if this is the first border in it, or its first piece: a wavefront
-// per row, the parts in order, so that the result does not depend on which workgroup was done first.
+// per row, the parts in order, so that the result does not depend on which workgroup was done first.  One launch for both attention
+// kernels.
 //
 // Bound: latency (borders, lengths, parts: a round of loads each, one more for every sixteen parts), and of many rows the
 // traffic of the parts.  4 to 5 us; 500 pieces of 128 rows, d = 128 (33 MB): 13 us.  Four rows to a wavefront there: with
@@ -19,18 +20,18 @@ namespace {
 
 using namespace paged;
 
-// EACH: rows of a wavefront.
+// EACH: rows of a wavefront.  `set`: which 4 EACH rows of the segment.
 template <class T, int D, int ROWS, int EACH>
-__global__ __launch_bounds__(256) void paged_join_kernel(AttendParams p) {
+__device__ __forceinline__ void join(const AttendParams& p, const Parts& from, int w, int set) {
   constexpr int N = D / 32;  // columns of a lane; either half of a wavefront has a whole row
-  const int lane = threadIdx.x & 63, half = lane >> 5, col = (lane & 31) * N, w = blockIdx.x;
-  const auto* at_border = (const __attribute__((address_space(4))) Border*)(p.borders) + w;
+  const int lane = threadIdx.x & 63, half = lane >> 5, col = (lane & 31) * N;
+  const auto* at_border = (const __attribute__((address_space(4))) Border*)(from.borders) + w;
   const Border border{at_border->b, at_border->h, at_border->t, at_border->parts};
   const int parts = abs(border.parts);
   if (parts == 0) return;
   const Part segment{border.b, border.h, border.t, 0, 0, 0};
   const Tile tile = tile_of<ROWS>(p.c, segment);
-  const int row0 = blockIdx.y * EACH * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // then every fourth
+  const int row0 = set * EACH * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // then every fourth
   if (row0 >= tile.rows) return;
   const f32m::Exponent prob(p.sm_scale);
   const float c = p.sm_scale * kLog2e;
@@ -42,10 +43,10 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttendParams p) {
   auto load = [&](int part, int row) {
     const long long at = joined_rows<ROWS>(border, w, part, p.c.H) + row;
     One y;
-    y.m = p.part_ml[at * 2];
-    y.l = p.part_ml[at * 2 + 1];
+    y.m = from.ml[at * 2];
+    y.l = from.ml[at * 2 + 1];
 #pragma unroll
-    for (int k = 0; k < N; ++k) y.x[k] = p.part_o[at * D + col + k];
+    for (int k = 0; k < N; ++k) y.x[k] = from.o[at * D + col + k];
     return y;
   };
   // What the two halves have of a row becomes the output.
@@ -108,18 +109,34 @@ __global__ __launch_bounds__(256) void paged_join_kernel(AttendParams p) {
   }
 }
 
-template <class T, int D, int ROWS, int EACH>
-hipError_t launch(const AttendParams& p, hipStream_t stream) {
-  hipLaunchKernelGGL((paged_join_kernel<T, D, ROWS, EACH>), dim3(p.grid, ROWS / 4 / EACH), dim3(256), 0, stream, p);
+constexpr int FEW_EACH = 1, FEW_SETS = 16 / 4 / FEW_EACH, MANY_EACH = 4, MANY_SETS = 128 / 4 / MANY_EACH;
+
+// 16 rows: the workgroups of one set are neighbours, so that with 8 kv heads a part is joined on the XCD that its workgroup ran on,
+// out of its L2 (16 decoding requests 53.5 us, with the sets of a segment side by side 57).  128 rows: the sets side by side (whole
+// scales 64 us, the other way 67).
+// MANY: the 128-row kernel's as well (twice the registers, which cost a decoding step of 16 requests 4 us).
+template <class T, int D, bool MANY>
+__global__ __launch_bounds__(256) void paged_join_kernel(AttendParams p, Parts few, Parts many) {
+  if constexpr (!MANY) return join<T, D, 16, FEW_EACH>(p, few, blockIdx.x, blockIdx.y);
+  const int i = blockIdx.x, j = i - few.grid * FEW_SETS;
+  if (j < 0) return join<T, D, 16, FEW_EACH>(p, few, i % few.grid, i / few.grid);
+  if constexpr (MANY) join<T, D, 128, MANY_EACH>(p, many, j / MANY_SETS, j % MANY_SETS);
+}
+
+template <class T, int D, bool MANY = false>
+hipError_t launch(const AttendParams& p, const Parts& few, const Parts& many, hipStream_t stream) {
+  const dim3 grid = MANY ? dim3(few.grid * FEW_SETS + many.grid * MANY_SETS) : dim3(few.grid, FEW_SETS);
+  hipLaunchKernelGGL((paged_join_kernel<T, D, MANY>), grid, dim3(256), 0, stream, p, few, many);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_paged_join(const PagedAttendParams& p, int dtype, int d, bool many, hipStream_t stream) {
-  if (dtype == HEATKV_F32) return d == 128 ? launch<float, 128, 16, 1>(p, stream) : launch<float, 64, 16, 1>(p, stream);
-  if (many) return d == 128 ? launch<bf16_t, 128, 128, 4>(p, stream) : launch<bf16_t, 64, 128, 4>(p, stream);
-  return d == 128 ? launch<bf16_t, 128, 16, 1>(p, stream) : launch<bf16_t, 64, 16, 1>(p, stream);
+hipError_t launch_paged_join(const PagedAttendParams& p, const PagedParts& few, const PagedParts& many, int dtype, int d,
+                             hipStream_t stream) {
+  if (dtype == HEATKV_F32) return d == 128 ? launch<float, 128>(p, few, many, stream) : launch<float, 64>(p, few, many, stream);
+  if (many.grid) return d == 128 ? launch<bf16_t, 128, true>(p, few, many, stream) : launch<bf16_t, 64, true>(p, few, many, stream);
+  return d == 128 ? launch<bf16_t, 128>(p, few, many, stream) : launch<bf16_t, 64>(p, few, many, stream);
 }
 
 }  // namespace heatkv

@@ -167,7 +167,7 @@ struct Part {
 // What the join has to know; written by every workgroup.  parts > 0: the border between its share and the one before cuts a
 // segment (and no earlier border does); parts < 0: its piece is the first of -parts; 0: neither.
 __device__ __forceinline__ void write_border(const AttendParams& p, int w, const Border& x) {
-  if (p.borders && threadIdx.x == 0) p.borders[w] = x;
+  if (p.parts.borders && threadIdx.x == 0) p.parts.borders[w] = x;
 }
 
 // The piece of workgroup w, by all of its 256 lanes; false: there is none.  Pieces of a segment lie H workgroups apart.
@@ -192,7 +192,7 @@ __device__ __forceinline__ bool find_piece(const AttendParams& p, const Requests
   part.to = part.from + 1;
   part.weight = n;
   // Parts behind the grid's end: of a q_start that is not ascending only.
-  const bool joins = n > 1 && part.from == 0 && w + (n - 1ll) * p.c.H < p.grid;
+  const bool joins = n > 1 && part.from == 0 && w + (n - 1ll) * p.c.H < p.parts.grid;
   write_border(p, w, Border{part.b, part.h, part.t, joins ? -n : 0});
   return true;
 }
@@ -220,7 +220,7 @@ __device__ __forceinline__ bool only_piece(const AttendParams& p, int w, Scratch
   const Requests<ROWS, KEYS> requests(p);
   long long upto, mine;
   const long long total = total_weight(p, requests, scratch, upto, mine);
-  const bool whole = !p.borders || total_segments(p, requests, scratch) >= p.whole_from;
+  const bool whole = !p.parts.borders || total_segments(p, requests, scratch) >= p.whole_from;
   return find_piece(p, requests, w, whole ? total + 1 : share_of(p, total, p.workgroups), scratch, part);
 }
 
@@ -305,7 +305,7 @@ struct Line {
     Part only{};
     bool some = false;
     if (by_pieces)
-      some = find_piece(p, requests, w, p.borders ? share_of(p, total, p.workgroups - segments) : total + 1, scratch, only);
+      some = find_piece(p, requests, w, p.parts.borders ? share_of(p, total, p.workgroups - segments) : total + 1, scratch, only);
     else
       at = find_place(p, requests, w, total, upto, mine, scratch);
     if (threadIdx.x == 0) {
