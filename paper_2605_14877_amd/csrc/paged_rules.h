@@ -39,8 +39,8 @@ constexpr int FEW_SEGMENTS = 128;
 constexpr int MANY_ROWS = 16, MANY_CHOSEN_ROWS = 64;
 
 // More tokens than one for each request and this: before, the call is taken for a decoding step, with padding rows or a few
-// tokens that are checked at once, and not worth the second kernel's and join's launches (10 us) to look for long requests.
-// One request, 24 tokens at 1000, 8000 and 32000 keys: 16, 31 and 79 us by the 16-row kernel alone, 25, 35 and 63 with both.
+// tokens that are checked at once, and not worth the second kernel's launch and the longer join (up to 10 us) to look for long requests.
+// One request, 24 tokens at 1000, 8000 and 32000 keys: 16, 31 and 80 us by the 16-row kernel alone, 24, 32 and 59 with both.
 constexpr int FEW_TOKENS = 40, FEW_TOKENS_LONG = 16, LONG_CACHE = 16384;
 
 // LDS of the 128-row kernel for the union of its tokens' chosen pages: a bit and a count for each word of the request's pages,
