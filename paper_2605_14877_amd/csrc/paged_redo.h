@@ -28,7 +28,7 @@ __device__ __forceinline__ void redo_row(const AttendParams& p, long long token,
   const int lane = threadIdx.x & 63, key = lane >> 2, quarter = lane & 3;
   const T* q = static_cast<const T*>(p.q.data) + token * p.q.token_stride + hq * p.q.head_stride;
   float x[D / 64] = {}, sum = 0.f;
-  for (int g = begin; g < end; ++g) {
+  for (int g = begin; g < end && sum == sum; ++g) {  // behind a probability that is NaN everything stays NaN
     const auto at = locate(g);
     if (!at.seen || at.pos >= limit) continue;
     float s = 0.f;

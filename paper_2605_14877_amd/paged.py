@@ -238,6 +238,8 @@ def heatkv_paged_select(shape, q, bounds, bound_scales, table, q_start, lens, fi
     if _native("paged_select", shape, q, bounds, bound_scales, table, q_start, lens, first, last, selected, causal, stream):
         return
     c, sh = _Call(shape), shape
+    if not 0 <= first < 2 ** 31 or not 1 <= last < 2 ** 31:
+        raise ValueError("first must be at least 0, last at least 1, both below 2^31")
     qr = c.rows(q, "q", None, sh.q_heads)
     tokens = q.shape[0]
     bp = c.dense(bounds, "bounds", (c.torch.int8,), (sh.num_pages, sh.kv_heads, 2, sh.d))

@@ -931,6 +931,25 @@ def test_malformed_calls_are_named():
     torch.cuda.synchronize()
 
 
+def test_a_choice_that_does_not_fit_is_named():
+    p = Problem("bf16", 4, 2, 64, 16, [40, 20], [2, 1])
+    d = p.dev
+    bounds = torch.zeros(p.num_pages, 2, 2, 64, dtype=torch.int8, device="cuda")
+    scales = torch.zeros(p.num_pages, 2, device="cuda")
+    selected = torch.zeros(p.tokens, 2, 4, dtype=torch.int32, device="cuda")
+    good = [p.shape, d["q"], bounds, scales, d["table"], d["q_start"], d["lens"], 1, 1, selected]
+    for i, x, message in ((7, -1, "first"), (7, 2 ** 32 + 1, "first"), (8, 0, "last"), (8, 2 ** 32 + 1, "last"), (7, 4, "top"),
+                          (2, bounds.short(), "dtype"), (2, bounds[:-1], "shape"), (3, scales.double(), "dtype"),
+                          (3, scales[:, :1], "contiguous"), (9, selected[:-1], "shape"), (9, selected.long(), "dtype"),
+                          (9, selected[..., 0], "contiguous"), (9, torch.zeros(p.tokens, 2, 513, dtype=torch.int32, device="cuda"), "top")):
+        with pytest.raises((ValueError, hk.HeatKVError), match=message):
+            hk.heatkv_paged_select(*good[:i], x, *good[i + 1:])
+    for i, x in ((1, d["q"].cpu()), (2, bounds.cpu()), (9, None)):
+        with pytest.raises((TypeError, ValueError)):
+            hk.heatkv_paged_select(*good[:i], x, *good[i + 1:])
+    torch.cuda.synchronize()
+
+
 def test_calls_without_tokens_do_nothing():
     p = Problem("bf16", 4, 2, 64, 16, [40, 20], [0, 0], pad=0)
     d = p.dev
