@@ -583,6 +583,25 @@ def test_many_requests(dtype, heads, top, batch):
     p.check(True, p.run(True, _ints(sel) if top else None), sel)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_as_many_requests_as_there_may_be(dtype):
+    r = random.Random(25)
+    new = [r.choice([0, 1, 1, 2]) for _ in range(4096)]
+    lens = [n + r.choice([0, 3, 20]) if n else 0 for n in new]
+    p = Problem(dtype, 2, 1, 64, 16, lens, new, seed=25)
+    p.check(True, p.run(True))
+
+
+@pytest.mark.parametrize("dtype,heads,max_pages,new", [("bf16", (1, 1), None, [3, 1]), ("bf16", (1, 1), None, [60, 1]),
+                                                       ("bf16", (1, 1), 32768, [60, 1]), ("fp8", (16, 1), 32768, [5, 1]),
+                                                       ("fp8", (2, 1), None, [70, 1]), ("f32", (1, 1), 32768, [20, 1])])
+def test_as_many_chosen_pages_as_there_may_be(dtype, heads, max_pages, new):
+    p = Problem(dtype, *heads, 64, 16, [9000, 30], new, seed=26, max_pages=max_pages)
+    r = random.Random(26)
+    sel = [[[r.randrange(0, 563) for _ in range(512)] for _ in range(heads[1])] for _ in range(p.tokens)]
+    p.check(True, p.run(True, _ints(sel)), sel)
+
+
 @pytest.mark.parametrize("dtype,H,lens,new", [("bf16", 2, [300, 90], [260, 30]), ("bf16", 8, [600, 40], [520, 30]),
                                               ("f32", 4, [200], [150]), ("f32", 64, [90, 70], [66, 20])])
 def test_choice_of_pages_of_many_tokens(dtype, H, lens, new):
