@@ -357,7 +357,8 @@ PyObject* paged_attend(PyObject* const* a, Py_ssize_t n) {
   const heatkv_rows out = c.rows(a[9], s->q_heads, &tokens);
   void* lse = a[12] == Py_None ? nullptr : c.dense(a[12], at::kFloat, {tokens, s->q_heads});
   const int32_t* selected = nullptr;
-  if (a[7] != Py_None) {
+  const bool chosen = a[7] != Py_None;  // a tensor without elements has a null address
+  if (chosen) {
     const at::Tensor* x = c.tensor(a[7]);
     if (!x || x->dim() != 3) return not_plain();
     top = x->size(2);
@@ -370,7 +371,7 @@ PyObject* paged_attend(PyObject* const* a, Py_ssize_t n) {
   for (PyObject* other : {a[1], a[2], a[3], a[7], a[10], a[12]})
     if (!c.apart(a[9], other)) return not_plain();
   return PyLong_FromLong(heatkv::without_lock([&] {
-    if (selected)
+    if (chosen)
       return heatkv_paged_attend_selected(s, tokens, q, kp, vp, table, q_start, lens, selected, static_cast<int>(top), sm, causal,
                                           out, static_cast<float*>(lse), ws, ws_bytes, c.stream());
     return heatkv_paged_attend(s, tokens, q, kp, vp, table, q_start, lens, sm, causal, out, static_cast<float*>(lse), ws, ws_bytes,

@@ -980,3 +980,21 @@ def test_calls_without_tokens_do_nothing():
     p = Problem("bf16", 4, 2, 64, 16, [40, 20], [0, 0], pad=5)  # rows of no request
     p.check(True, p.run(True))
     assert torch.equal(before.view(torch.int16), d["k"].view(torch.int16))
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", [2, 1]), ("bf16", [70, 1]), ("f32", [2, 1])])
+def test_a_choice_of_no_pages_is_refused(dtype, new):
+    # not the attention over all pages: a tensor without elements has a null address
+    p = Problem(dtype, 4, 2, 64, 16, [140, 20], new)
+    d = p.dev
+    selected = torch.zeros(p.tokens, 2, 3, dtype=torch.int32, device="cuda")
+    out = torch.full_like(d["q"], 7.0)
+    ws = torch.zeros(max(hk.paged_attend_workspace_bytes(p.shape, p.tokens), 16), dtype=torch.uint8, device="cuda")
+    args = (p.shape, d["q"], d["k"], d["v"], d["table"], d["q_start"], d["lens"])
+    for none in (selected[:, :, :0], selected[:, :, :0].contiguous(), torch.empty(p.tokens, 2, 0, dtype=torch.int32, device="cuda")):
+        with pytest.raises(hk.HeatKVError, match="top"):
+            hk.heatkv_paged_attend_selected(*args, none, p.sm, out, ws)
+    with pytest.raises((TypeError, ValueError)):
+        hk.heatkv_paged_attend_selected(*args, None, p.sm, out, ws)
+    torch.cuda.synchronize()
+    assert torch.all(out == 7.0)
