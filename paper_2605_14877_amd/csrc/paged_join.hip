@@ -96,10 +96,12 @@ __device__ __forceinline__ void join(const AttendParams& p, const Parts& from, i
         for (int k = 0; k < N; ++k) sum[r].x[k] *= f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const float g = i0 + 2 * u < parts ? factor(y[r][u].m, m) : 0.f;
-          sum[r].l += g * y[r][u].l;
+          // Places behind the last part hold that part again: left out, not multiplied by 0, as it may hold infinities.
+          const bool real = i0 + 2 * u < parts;
+          const float g = factor(y[r][u].m, m);
+          sum[r].l = real ? sum[r].l + g * y[r][u].l : sum[r].l;
 #pragma unroll
-          for (int k = 0; k < N; ++k) sum[r].x[k] += g * y[r][u].x[k];
+          for (int k = 0; k < N; ++k) sum[r].x[k] = real ? sum[r].x[k] + g * y[r][u].x[k] : sum[r].x[k];
         }
       }
     }

@@ -998,3 +998,58 @@ def test_a_choice_of_no_pages_is_refused(dtype, new):
         hk.heatkv_paged_attend_selected(*args, None, p.sm, out, ws)
     torch.cuda.synchronize()
     assert torch.all(out == 7.0)
+
+
+# dtype, q_heads, kv_heads, d, page, lens, new: parts of 128 keys where one request is cut (of 256 with many rows)
+CUT = [
+    ("bf16", 1, 1, 128, 16, [380], [1]), ("bf16", 4, 1, 64, 64, [640], [2]), ("bf16", 2, 2, 128, 32, [2170, 300], [1, 1]),
+    ("f32", 1, 1, 64, 16, [384], [1]), ("f32", 3, 1, 128, 32, [1900], [2]), ("bf16", 8, 8, 64, 64, [2900] * 17, [1] * 17),
+    ("bf16", 1, 1, 128, 16, [768], [70]), ("bf16", 2, 1, 64, 64, [1290, 100], [65, 1]), ("bf16", 1, 1, 64, 32, [2300], [129]),
+    ("f32", 4, 4, 64, 32, [700, 640], [33, 70]), ("bf16", 1, 1, 128, 16, [200], [1]), ("f32", 2, 1, 64, 16, [500], [1]),
+]
+
+
+def _spoil_values(p):
+    """Infinities and NaN in V alone: every row that sees them has scores as ever, and positive probabilities."""
+    for n, ids in zip(p.lens, p.table):
+        for x, column, value in ((n - 1, 3, math.inf), (0, 5, -math.inf), (n // 2, 7, math.nan), (n // 3, 9, math.inf),
+                                 (n - 2, 9, -math.inf), (n - 1, 11, math.nan), (n // 2, 13, -math.inf), (n - 1, 13, -math.inf)):
+            p.v[ids[x // p.page], :, x % p.page, column] = value
+    p.dev["v"] = p.v.cuda()
+
+
+def _check_values(p, causal, got, chosen=None):
+    """As _check_with_nan, with infinities among the values that have to be, and lse as if V were finite."""
+    want, want_lse, _ = ref.attend(p.q, p.k, p.v, p.table, p.q_start, p.lens, p.page, p.sm, causal, chosen)
+    real = p.q_start[-1]
+    assert want[:real].isinf().any() and want[:real].isnan().any()
+    _check_with_nan(p, causal, got, chosen)
+    q, k = p.q[:real].abs().double(), p.k.double().nan_to_num(0.0).abs()
+    S = float(q.amax((0, 1)) @ k.amax((0, 1, 2))) * p.sm
+    e = 2.0 ** -24 * (p.d * S + 2 * 1.443 * 2 * S + max(p.lens) + 64)
+    sure = want_lse[:real].isfinite()
+    off = (got[1][:real].cpu().double() - want_lse[:real])[sure].abs() - (e + 2.0 ** -22 * want_lse[:real][sure].abs())
+    assert sure.any() and float(off.max()) <= 0
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("case", CUT, ids=str)
+def test_infinite_values_stay_what_they_are(case, causal):
+    # whether or not a request is cut, and into however many parts
+    p = Problem(*case, seed=27)
+    _spoil_values(p)
+    _check_values(p, causal, p.run(causal))
+
+
+@pytest.mark.parametrize("case", [("bf16", 2, 1, 128, 16, [1500, 900], [1, 2]), ("f32", 4, 2, 64, 32, [1500], [3]),
+                                  ("bf16", 1, 1, 64, 64, [2600, 300], [70, 30])], ids=str)
+def test_infinite_values_of_chosen_pages_stay_what_they_are(case):
+    p = Problem(*case, seed=28)
+    _spoil_values(p)
+    r = random.Random(28)
+    some = [0] + [f(max(p.lens)) // p.page for f in (lambda n: n - 1, lambda n: n // 2, lambda n: n // 3)]
+    for top in (5, 40):
+        sel = [[[r.choice(some) if r.random() < 0.3 else r.randrange(0, max(p.lens) // p.page + 1) for _ in range(top)]
+                for _ in range(p.H)] for _ in range(p.tokens)]
+        for causal in (True, False):
+            _check_values(p, causal, p.run(causal, _ints(sel)), sel)
