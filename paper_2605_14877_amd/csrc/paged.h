@@ -116,7 +116,7 @@ struct Border {
 struct Parts {
   float *o, *ml;
   Border* borders;  // of each workgroup; null: nothing can be cut
-  int grid;         // workgroups of the launch
+  int grid;         // workgroups of the launch; for the join, those that it looks at
 };
 
 struct AttendParams {
@@ -162,7 +162,7 @@ hipError_t launch_paged_select(const PagedSelectParams& p, int dtype, int d, hip
 hipError_t launch_paged_attend_bf16(const PagedAttendParams& p, int d, bool fp8, hipStream_t stream);
 hipError_t launch_paged_attend_long(const PagedAttendParams& p, int d, bool fp8, hipStream_t stream);
 hipError_t launch_paged_attend_f32(const PagedAttendParams& p, int d, hipStream_t stream);
-// few, many: of the two attention launches, grid 0 where there is nothing to join.
+// few, many: of the two attention launches, grid: join_workgroups(), 0 where there is nothing to join.
 hipError_t launch_paged_join(const PagedAttendParams& p, const PagedParts& few, const PagedParts& many, int dtype, int d,
                              hipStream_t stream);
 

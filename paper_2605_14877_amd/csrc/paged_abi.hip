@@ -190,7 +190,7 @@ int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const voi
   const auto hip_stream = static_cast<hipStream_t>(stream);
   const bool fp8 = s->kv_format == HEATKV_KV_FP8_E4M3;
   hipError_t e = hipSuccess;
-  // Makes one of the two launches; its parts, with grid 0 if none can be cut.
+  // Makes one of the two launches; its parts, for the join.
   auto launch = [&](const heatkv::paged::Launch& l, const PartArrays& a, bool many) {
     heatkv::PagedParts parts{};
     if (!l.workgroups || e != hipSuccess) return parts;
@@ -210,7 +210,7 @@ int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const voi
     e = s->dtype == HEATKV_F32 ? heatkv::launch_paged_attend_f32(p, s->d, hip_stream)
         : many                 ? heatkv::launch_paged_attend_long(p, s->d, fp8, hip_stream)
                                : heatkv::launch_paged_attend_bf16(p, s->d, fp8, hip_stream);
-    if (!l.parts) parts.grid = 0;
+    parts.grid = heatkv::paged::join_workgroups(l);
     return parts;
   };
   const heatkv::PagedParts many = launch(plan.many, w.many, true), few = launch(plan.few, w.few, false);

@@ -21,6 +21,12 @@ struct Plan {
   Launch few, many;  // tiles of 16 rows and steps of 32 keys; of 128 and 64
 };
 
+// Workgroups of a launch that the join looks at: where segments are cut, no more have work than there are places for parts.  A
+// larger grid is one workgroup for each segment that there may be, and from whole_from segments on none is cut.  1024 kv heads of
+// 16 query heads each, 1024 requests, 8192 tokens: 2097152 workgroups, of which 1535 matter (all of them, times eight in the join,
+// would be more lanes than a launch can have).
+inline int join_workgroups(const Launch& l) { return static_cast<int>(std::min<int64_t>(l.grid, l.parts)); }
+
 // Steps of a share at least, measured with three requests of up to 740 keys (fp32, d = 128): 17.7 us with 8, 15.4 with 4, 17.4
 // with 2.  Where no cache is longer than WHOLE_STEPS nothing is cut: the halves would save less than the join's launch of about
 // 4 us.

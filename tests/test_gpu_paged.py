@@ -1053,3 +1053,20 @@ def test_infinite_values_of_chosen_pages_stay_what_they_are(case):
                 for _ in range(p.H)] for _ in range(p.tokens)]
         for causal in (True, False):
             _check_values(p, causal, p.run(causal, _ints(sel)), sel)
+
+
+def test_as_many_heads_and_rows_as_there_may_be():
+    # 2^23 tokens x kv heads, 16 queries a kv head; two requests have tokens.  All heads alike, so that one tells of all.
+    new, lens = [60, 1] + [0] * 1022, [700, 20] + [0] * 1022
+    p = Problem("bf16", 16, 1, 64, 256, lens, new, seed=32, pad=2 ** 13 - 61)
+    p.q = p.q[:, :1].expand(p.tokens, 16, 64)
+    shape = _shape("bf16", 2 ** 14, 2 ** 10, 64, 256, p.num_pages, 1024, p.max_pages)
+    q = p.dev["q"][:, :1].expand(p.tokens, 2 ** 14, 64)
+    k, v = (p.dev[x].expand(shape.pages_shape).contiguous() for x in "kv")
+    out = torch.full((p.tokens, 2 ** 14, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((p.tokens, 2 ** 14), 7.0, device="cuda")
+    ws = torch.full((hk.paged_attend_workspace_bytes(shape, p.tokens),), 255, dtype=torch.uint8, device="cuda")
+    hk.heatkv_paged_attend(shape, q, k, v, p.dev["table"], p.dev["q_start"], p.dev["lens"], p.sm, out, ws, lse=lse)
+    for h in (0, 511, 1023):
+        p.check(True, (out[:, 16 * h:16 * h + 16], lse[:, 16 * h:16 * h + 16]))
+    assert torch.equal(out[:61], out[:61, :16].repeat(1, 1024, 1)) and torch.equal(lse[:61], lse[:61, :16].repeat(1, 1024))

@@ -315,3 +315,62 @@ def test_reference_allocator_keeps_every_page_once():
         free = [a.ring[(a.head + i) % 30] for i in range(a.count)]
         assert sorted(used + free) == list(range(30))
         assert status == 0 or set(slots) == {-1}
+
+
+JOIN_RULES = r"""
+#include "paged_rules.h"
+extern "C" void launches(int bf16, int batch, int kv, int group, long long tokens, long long pages, int page, long long top, long long* out) {
+  const auto p = heatkv::paged::plan_launches(bf16, batch, kv, group, tokens, pages, page, top);
+  int i = 0;
+  for (const auto& l : {p.few, p.many}) {
+    out[i++] = l.grid;
+    out[i++] = heatkv::paged::join_workgroups(l);
+  }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def launches(tmp_path_factory):
+    d = tmp_path_factory.mktemp("launches")
+    src, lib = d / "launches.cpp", d / "liblaunches.so"
+    src.write_text(JOIN_RULES)
+    subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", "-I", hb.CSRC, str(src), "-o", str(lib)], check=True)
+    L = C.CDLL(str(lib))
+
+    def call(bf16, batch, kv, group, tokens, pages, page, top=0):
+        out = (C.c_longlong * 4)()
+        L.launches(*[C.c_longlong(x) if i in (4, 5, 7) else C.c_int(x)
+                     for i, x in enumerate((int(bf16), batch, kv, group, tokens, pages, page, top))], out)
+        return dict(zip(("few", "few_join", "many", "many_join"), out))
+    return call
+
+
+@pytest.mark.parametrize("top", [0, 4])
+@pytest.mark.parametrize("kv", [1, 3, 128, 1024])
+@pytest.mark.parametrize("batch", [1, 300, 1024, 4096])
+def test_no_launch_has_more_lanes_than_there_can_be(launches, kv, batch, top):
+    # at the limits of tokens, heads and requests; the join has 4 workgroups of 256 lanes for one of few rows, 8 for one of many
+    for group in (1, 16):
+        for tokens in {min(2 ** 22, 2 ** 23 // kv), min(2 ** 22, 2 ** 23 // kv) // 2, batch + 41}:
+            n = launches(True, batch, kv, group, tokens, 64, 256, top)
+            assert n["few"] * 256 < 2 ** 32 and n["many"] * 256 < 2 ** 32
+            assert (4 * n["few_join"] + 8 * n["many_join"]) * 256 < 2 ** 32
+
+
+def test_the_join_looks_at_every_piece(rules, launches):
+    import random
+    r, some = random.Random(4), 0
+    for _ in range(400):
+        group, heads, batch = r.choice([1, 2, 4, 16]), r.choice([1, 2, 8, 64]), r.choice([1, 2, 40, 300])
+        longest = r.choice([513, 4096, 70000])
+        new = [r.choice([0, 1, 5, 64 // group + 1, r.randint(0, 3000)]) for _ in range(batch)]
+        args = (True, batch, heads, group, sum(new), -(-longest // 16), 16)
+        many, n = rules(*args)[1], launches(*args)
+        if not many["workgroups"]:
+            continue
+        assert n["few_join"] == n["few"] and n["many_join"] <= many["parts"]
+        _, places = _pieces(many, [(x, r.randint(min(x, longest), longest)) for x in new], heads, group, True, 0)
+        assert places <= n["many_join"]
+        some += places > 0
+    assert some > 50
