@@ -315,6 +315,9 @@ int heatkv_rank_dispersion(const heatkv_shape* shape, const float* betas, int ru
  *                  the last ones of its lens[b] tokens; q_start[0] = 0, ascending
  * Contents of integer arrays are not checked (they are on the device).  Page numbers, lengths and row numbers out of their
  * ranges are brought into them: such a call gives wrong outputs, but touches nothing outside of the arrays.
+ * What a call writes has no byte in common with its other arguments, from their first byte to their last, or the call is refused.
+ * Exceptions: lens_out and free_span_out may be lens and free_span; out and q may be slices of one tensor beside each other, by
+ * the same strides; k_new and v_new may be rows of the pages of which the call writes none (a page is copied that way).
  *
  * Limits: q_heads a multiple of kv_heads, at most 16 per kv head; kv_heads <= 1024; d = 64 or 128; page_size 16, 32, 64, 128
  * or 256; batch <= 4096; tokens <= 2^22, tokens * kv_heads <= 2^23; num_pages * page_size and max_pages * page_size <= 2^30,
@@ -370,7 +373,7 @@ int heatkv_paged_append(const heatkv_paged_shape* shape, const int32_t* slots, i
  *     out[t][hq] = softmax(q[t][hq] . K^T * sm_scale) V   over the keys that token t sees:
  * all lens[b] tokens of its request, or, causal != 0, those up to itself.  A row that sees nothing, or nothing but scores of
  * minus infinity, is zeros with lse = minus infinity.
- * out   rows of the dtype, may not overlap q
+ * out   rows of the dtype, none of them in common with q
  * lse   fp32 [tokens][q_heads] or null: natural logarithm of the sum of exp(q . k * sm_scale)
  * ws    device scratch of at least heatkv_paged_attend_workspace_bytes(shape, tokens, 0) bytes (may be null when that is 0).
  *       Calls that may run at the same time, graphs among them, need a workspace each

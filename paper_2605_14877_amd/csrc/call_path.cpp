@@ -268,19 +268,6 @@ class PagedCall {
                                                            : t == (s_->dtype == HEATKV_BF16 ? at::kBFloat16 : at::kFloat);
     return fits ? x->data_ptr() : fail_ptr();
   }
-  // Whether two tensors (or None) have no byte in common.
-  bool apart(PyObject* a, PyObject* b) {
-    if (a == Py_None || b == Py_None) return true;
-    const at::Tensor *x = tensor(a), *y = tensor(b);
-    if (!x || !y) return false;
-    const auto first = [](const at::Tensor& t) { return reinterpret_cast<uintptr_t>(t.data_ptr()); };
-    const auto end = [&](const at::Tensor& t) {
-      int64_t n = 1;
-      for (int64_t i = 0; i < t.dim(); ++i) n += (t.size(i) - 1) * t.stride(i);
-      return first(t) + static_cast<uintptr_t>(n) * t.element_size();
-    };
-    return x->numel() == 0 || y->numel() == 0 || end(*x) <= first(*y) || end(*y) <= first(*x);
-  }
 
  private:
   const at::Tensor* fail() {
@@ -368,8 +355,6 @@ PyObject* paged_attend(PyObject* const* a, Py_ssize_t n) {
   size_t ws_bytes;
   if (!number(a[8], &sm) || !boolean(a[11], &causal) || !buffer(a[10], 0, &ws, &ws_bytes) || !c.ok()) return not_plain();
   if (a[10] != Py_None && !c.tensor(a[10])) return not_plain();
-  for (PyObject* other : {a[1], a[2], a[3], a[7], a[10], a[12]})
-    if (!c.apart(a[9], other)) return not_plain();
   return PyLong_FromLong(heatkv::without_lock([&] {
     if (chosen)
       return heatkv_paged_attend_selected(s, tokens, q, kp, vp, table, q_start, lens, selected, static_cast<int>(top), sm, causal,

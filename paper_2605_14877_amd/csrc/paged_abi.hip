@@ -102,6 +102,56 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return x < y + nb && y < x + na;
 }
 
+// One array of a call, from its first byte to its last.
+struct Span {
+  const char* name;
+  __int128 first, end;
+  bool written;
+};
+constexpr bool READ = false, WRITTEN = true;
+Span span_of(const char* name, const void* p, size_t bytes, bool written) {
+  const auto first = static_cast<__int128>(reinterpret_cast<uintptr_t>(p));
+  return {name, first, first + (p ? static_cast<__int128>(bytes) : 0), written};
+}
+Span span_of(const char* name, const heatkv_paged_shape* s, const heatkv_rows& r, int64_t tokens, int64_t heads, bool written) {
+  const int elem = s->dtype == HEATKV_BF16 ? 2 : 4;
+  const __int128 t = static_cast<__int128>(r.token_stride) * (tokens - 1), h = static_cast<__int128>(r.head_stride) * (heads - 1);
+  const auto at = static_cast<__int128>(reinterpret_cast<uintptr_t>(r.data));
+  return {name, at + (std::min<__int128>(t, 0) + std::min<__int128>(h, 0)) * elem,
+          at + (std::max<__int128>(t, 0) + std::max<__int128>(h, 0) + s->d) * elem, written};
+}
+// Workgroups run in any order: what a call writes, it neither reads through another argument nor writes twice.
+int check_disjoint(std::initializer_list<Span> arrays) {
+  for (const Span* a = arrays.begin(); a != arrays.end(); ++a)
+    for (const Span* b = arrays.begin(); b != a; ++b)
+      if ((a->written || b->written) && a->first < b->end && b->first < a->end && a->first < a->end && b->first < b->end)
+        return fail(HEATKV_EINVAL, std::string(b->written ? b->name : a->name) + " overlaps " + (b->written ? a->name : b->name));
+  return HEATKV_OK;
+}
+// Whether two sets of rows, of which one is written, have an element in common.  Where their ranges overlap: not if they are slices
+// of one tensor, beside each other; rows that go by different strides are taken to meet.
+bool rows_meet(const heatkv_paged_shape* s, const heatkv_rows& a, const heatkv_rows& b, int64_t tokens, int64_t heads) {
+  const Span x = span_of("", s, a, tokens, heads, WRITTEN), y = span_of("", s, b, tokens, heads, WRITTEN);
+  if (x.end <= y.first || y.end <= x.first) return false;
+  if ((tokens > 1 && a.token_stride != b.token_stride) || (heads > 1 && a.head_stride != b.head_stride)) return true;
+  const __int128 off = (y.first - x.first) / (s->dtype == HEATKV_BF16 ? 2 : 4);
+  const __int128 t = tokens > 1 ? a.token_stride < 0 ? -static_cast<__int128>(a.token_stride) : a.token_stride : 0;
+  for (int64_t dh = 1 - heads; dh < heads; ++dh) {  // heads between two rows; then the tokens that bring them nearest
+    const __int128 rest = off - static_cast<__int128>(dh) * a.head_stride;
+    __int128 dt = t ? rest / t - (rest % t < 0) : 0;
+    for (int i = 0; i < 2; ++i, ++dt) {
+      const __int128 apart = rest - dt * t;
+      if (dt < tokens && -dt < tokens && apart < s->d && -apart < s->d) return true;
+    }
+  }
+  return false;
+}
+size_t pages_bytes(const heatkv_paged_shape* s) {
+  return size_t(s->num_pages) * s->page_size * s->kv_heads * s->d *
+         (s->dtype == HEATKV_F32 ? 4 : s->kv_format == HEATKV_KV_FP8_E4M3 ? 1 : 2);
+}
+size_t table_bytes(const heatkv_paged_shape* s) { return size_t(s->batch) * s->max_pages * 4; }
+
 int launched(hipError_t e, const char* what) {
   return e == hipSuccess ? HEATKV_OK : fail(HEATKV_EHIP, std::string(what) + " launch: " + hipGetErrorString(e));
 }
@@ -177,6 +227,16 @@ int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const voi
     if (!ws || ws_bytes < w.total) return fail(HEATKV_EINVAL, "paged attention workspace too small");
     if (!aligned(ws, 16)) return fail(HEATKV_EINVAL, "workspace must be 16-byte aligned");
   }
+  const size_t requests = size_t(s->batch) * 4;
+  const Span lse_span = span_of("lse", lse, size_t(tokens) * s->q_heads * 4, WRITTEN), ws_span = span_of("ws", ws, w.total, WRITTEN);
+  rc = check_disjoint({span_of("out", s, out, tokens, s->q_heads, WRITTEN), lse_span, ws_span,
+                       span_of("k_pages", k_pages, pages_bytes(s), READ), span_of("v_pages", v_pages, pages_bytes(s), READ),
+                       span_of("table", table, table_bytes(s), READ), span_of("q_start", q_start, requests + 4, READ),
+                       span_of("lens", lens, requests, READ),
+                       span_of("selected", selected, size_t(tokens) * s->kv_heads * top * 4, READ)});
+  if (!rc) rc = check_disjoint({lse_span, ws_span, span_of("q", s, q, tokens, s->q_heads, READ)});
+  if (rc) return rc;
+  if (rows_meet(s, out, q, tokens, s->q_heads)) return fail(HEATKV_EINVAL, "out overlaps q");
   heatkv::paged::AttendParams p{};
   p.c = cache_of(s, tokens, table, q_start, lens, causal);
   p.q = {q.data, q.token_stride, q.head_stride};
@@ -236,6 +296,13 @@ int heatkv_paged_assign(const heatkv_paged_shape* s, const int32_t* keep, const 
     return fail(HEATKV_EINVAL, "free_span_out overlaps free_span in part");
   if (overlap(lens_out, row, keep, row) || overlap(lens_out, row, new_tokens, row))
     return fail(HEATKV_EINVAL, "keep and new_tokens must not overlap lens_out");
+  rc = check_disjoint({span_of("lens_out", lens_out, row, WRITTEN), span_of("free_ring", free_ring, size_t(s->num_pages) * 4, WRITTEN),
+                       span_of("free_span_out", free_span_out, 8, WRITTEN), span_of("table", table, table_bytes(s), WRITTEN),
+                       span_of("q_start", q_start, row + 4, WRITTEN), span_of("slots", slots, size_t(max_tokens) * 4, WRITTEN),
+                       span_of("status", status, 4, WRITTEN), span_of("keep", keep, row, READ),
+                       span_of("new_tokens", new_tokens, row, READ), span_of("lens", lens, lens_out == lens ? 0 : row, READ),
+                       span_of("free_span", free_span, free_span_out == free_span ? 0 : 8, READ)});
+  if (rc) return rc;
   heatkv::AssignArgs a{};
   a.batch = s->batch;
   a.num_pages = s->num_pages;
@@ -269,6 +336,16 @@ int heatkv_paged_append(const heatkv_paged_shape* s, const int32_t* slots, int64
   if ((bounds == nullptr) != (bound_scales == nullptr)) return fail(HEATKV_EINVAL, "bounds and bound_scales go together");
   if (bounds && (!aligned(bounds, 16) || !aligned(bound_scales, 4)))
     return fail(HEATKV_EINVAL, "bounds must be 16-byte aligned, bound_scales 4-byte");
+  const size_t pages_heads = size_t(s->num_pages) * s->kv_heads;
+  const Span bounds_span = span_of("bounds", bounds, pages_heads * 2 * s->d, WRITTEN),
+             scales_span = span_of("bound_scales", bound_scales, pages_heads * 4, WRITTEN);
+  rc = check_disjoint({span_of("k_pages", k_pages, pages_bytes(s), WRITTEN), span_of("v_pages", v_pages, pages_bytes(s), WRITTEN),
+                       bounds_span, scales_span, span_of("slots", slots, size_t(tokens) * 4, READ)});
+  // The new rows may be other rows of the pages: that is how a page is copied.
+  if (!rc)
+    rc = check_disjoint({bounds_span, scales_span, span_of("k_new", s, k_new, tokens, s->kv_heads, READ),
+                         span_of("v_new", s, v_new, tokens, s->kv_heads, READ)});
+  if (rc) return rc;
   heatkv::PagedAppendArgs a{};
   a.dtype = s->dtype;
   a.d = s->d;
@@ -319,6 +396,12 @@ int heatkv_paged_select(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows
   if (!rc) rc = check_ints({table, q_start, lens, selected, bound_scales});
   if (rc) return rc;
   if (!bounds || !aligned(bounds, 16)) return fail(HEATKV_EINVAL, "bounds must be 16-byte aligned and not null");
+  const size_t pages_heads = size_t(s->num_pages) * s->kv_heads, requests = size_t(s->batch) * 4;
+  rc = check_disjoint({span_of("selected", selected, size_t(tokens) * s->kv_heads * top * 4, WRITTEN),
+                       span_of("q", s, q, tokens, s->q_heads, READ), span_of("bounds", bounds, pages_heads * 2 * s->d, READ),
+                       span_of("bound_scales", bound_scales, pages_heads * 4, READ), span_of("table", table, table_bytes(s), READ),
+                       span_of("q_start", q_start, requests + 4, READ), span_of("lens", lens, requests, READ)});
+  if (rc) return rc;
   heatkv::PagedSelectParams p{};
   p.c = cache_of(s, tokens, table, q_start, lens, causal);
   p.tokens_as_rows = p.c;

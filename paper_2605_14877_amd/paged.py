@@ -85,7 +85,7 @@ def _native(name, shape, *args):
 
 class _Call:
     """Checks of one call's tensors.  The kernels trust sizes, so every operand is checked here, on the host: a wrong tensor
-    becomes a Python error, not a memory fault on the GPU."""
+    becomes a Python error, not a memory fault on the GPU.  Tensors that overlap are refused by the C entries."""
 
     def __init__(self, shape):
         if not isinstance(shape, PagedShape):
@@ -149,19 +149,6 @@ class _Call:
         return self.torch.cuda.current_stream().cuda_stream if stream is None else stream
 
 
-def _no_alias(x, name, others):
-    """Outputs that a call writes while it reads others: no shared storage range."""
-    lo = x.data_ptr()
-    hi = lo + (sum((n - 1) * s for n, s in zip(x.shape, x.stride())) + 1) * x.element_size()
-    for y, other in others:
-        if y is None or not y.numel() or not x.numel():
-            continue
-        a = y.data_ptr()
-        b = a + (sum((n - 1) * s for n, s in zip(y.shape, y.stride())) + 1) * y.element_size()
-        if lo < b and a < hi:
-            raise ValueError(f"{name} overlaps {other}")
-
-
 def heatkv_paged_assign(shape, keep, new_tokens, lens, free_ring, free_span, table, q_start, slots, status, lens_out=None,
                         free_span_out=None, stream=None):
     """One step of the page allocator.  lens_out, free_span_out: None for in place."""
@@ -211,7 +198,6 @@ def _attend_operands(c, q, k_pages, v_pages, table, q_start, lens, out, ws, lse)
     tokens = q.shape[0]
     operands = [tokens, qr, c.pages(k_pages, "k_pages"), c.pages(v_pages, "v_pages"), *c.requests(table, q_start, lens)]
     outr = c.rows(out, "out", tokens, sh.q_heads)
-    _no_alias(out, "out", ((q, "q"), (k_pages, "k_pages"), (v_pages, "v_pages"), (ws, "ws"), (lse, "lse")))
     lp = None if lse is None else c.dense(lse, "lse", (c.torch.float32,), (tokens, sh.q_heads))
     wp, ws_bytes = None, 0
     if ws is not None:
@@ -261,6 +247,5 @@ def heatkv_paged_attend_selected(shape, q, k_pages, v_pages, table, q_start, len
     operands, outr, lp, wp, n = _attend_operands(c, q, k_pages, v_pages, table, q_start, lens, out, ws, lse)
     top = selected.shape[-1] if isinstance(selected, c.torch.Tensor) and selected.dim() == 3 else 0
     sel = c.ints(selected, "selected", q.shape[0], sh.kv_heads, top)
-    _no_alias(out, "out", ((selected, "selected"),))
     _check(c.lib.heatkv_paged_attend_selected(sh.ref, *operands, sel, top, float(sm_scale), int(bool(causal)), outr, lp, wp, n,
                                               c.stream(stream)))

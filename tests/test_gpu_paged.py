@@ -1070,3 +1070,53 @@ def test_as_many_heads_and_rows_as_there_may_be():
     for h in (0, 511, 1023):
         p.check(True, (out[:, 16 * h:16 * h + 16], lse[:, 16 * h:16 * h + 16]))
     assert torch.equal(out[:61], out[:61, :16].repeat(1, 1024, 1)) and torch.equal(lse[:61], lse[:61, :16].repeat(1, 1024))
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", 2), ("bf16", 70), ("f32", 3)])
+def test_outputs_beside_the_queries(dtype, new):
+    # another slice of the tensor that holds the queries, head by head as well: no element in common
+    p = Problem(dtype, 4, 2, 64, 16, [400, 33], [new, 1], seed=29)
+    want = p.run(True)
+    for first, second in ((slice(1, 5), slice(5, 9)), (slice(5, 9), slice(1, 5))):
+        fused = torch.full((p.tokens, 10, 64), 9.0, dtype=p.q.dtype, device="cuda")
+        fused[:, first] = p.dev["q"]
+        fused[:, second] = 7.0
+        got = p.run(True, q=fused[:, first], out=fused[:, second])
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert torch.equal(fused[:, first], p.dev["q"]) and torch.all(fused[:, 0] == 9.0) and torch.all(fused[:, 9] == 9.0)
+    fused = torch.full((p.tokens, 4, 2, 64), 7.0, dtype=p.q.dtype, device="cuda")
+    fused[:, :, 0] = p.dev["q"]
+    got = p.run(True, q=fused[:, :, 0], out=fused[:, :, 1])
+    assert torch.equal(got[0], want[0]) and torch.equal(fused[:, :, 0], p.dev["q"])
+    by_head = torch.full((9, p.tokens, 64), 7.0, dtype=p.q.dtype, device="cuda")
+    by_head[:4] = p.dev["q"].transpose(0, 1)
+    got = p.run(True, q=by_head[:4].transpose(0, 1), out=by_head[5:].transpose(0, 1))
+    assert torch.equal(got[0], want[0])
+    for a, b in ((slice(1, 5), slice(1, 5)), (slice(1, 5), slice(2, 6)), (slice(2, 6), slice(1, 5))):
+        with pytest.raises((ValueError, hk.HeatKVError), match="out overlaps q"):
+            p.run(True, q=fused.view(p.tokens, 8, 64)[:, a], out=fused.view(p.tokens, 8, 64)[:, b])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pages,H", [([(2, 7)], 2), ([(2, 7), (0, 5), (3, 1)], 3), ([(i, i + 9) for i in range(9)], 8)])
+def test_pages_copied_within_the_cache(dtype, pages, H):
+    # a shared page that a request is about to write to: its rows are the new rows of another page
+    page, d, num_pages = 32, 64, 18
+    shape = _shape(dtype, H, H, d, page, num_pages, 1, 4)
+    g = torch.Generator().manual_seed(30)
+    k, v = (torch.randn(shape.pages_shape, generator=g).to(DT[dtype]).cuda() for _ in range(2))
+    bounds = torch.zeros(num_pages, H, 2, d, dtype=torch.int8, device="cuda")
+    scales = torch.zeros(num_pages, H, device="cuda")
+    every = torch.arange(num_pages * page, dtype=torch.int32, device="cuda")
+    rows = [x.transpose(1, 2).reshape(-1, H, d).contiguous() for x in (k, v)]
+    hk.heatkv_paged_append(shape, every, *rows, k, v, bounds, scales)
+    before = [x.clone() for x in (k, v, bounds, scales)]
+    for a, b in pages:
+        slots = torch.arange(b * page, (b + 1) * page, dtype=torch.int32, device="cuda")
+        hk.heatkv_paged_append(shape, slots, k[a].transpose(0, 1), v[a].transpose(0, 1), k, v, bounds, scales)
+    torch.cuda.synchronize()
+    source = list(range(num_pages))
+    for a, b in pages:
+        source[b] = a
+    for x, old in zip((k, v, bounds, scales), before):
+        assert torch.equal(x, old[source])

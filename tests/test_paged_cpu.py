@@ -374,3 +374,66 @@ def test_the_join_looks_at_every_piece(rules, launches):
         assert places <= n["many_join"]
         some += places > 0
     assert some > 50
+
+
+def test_arrays_that_overlap_are_refused():
+    # addresses are never followed: every call is refused
+    L, sh, tokens = paged._lib(), _shape(), 4
+    at = lambda i: (i + 1) << 36  # noqa: E731
+    requests, rows_bytes = 4 * sh.batch, ((tokens - 1) * 1024 + 7 * 128 + 128) * 2
+    pages = sh.num_pages * sh.page_size * sh.kv_heads * sh.d * 2
+    size = dict(q=rows_bytes, out=rows_bytes, k_new=rows_bytes // 2, v_new=rows_bytes // 2, k_pages=pages, v_pages=pages,
+                table=requests * sh.max_pages, q_start=requests + 4, lens=requests, keep=requests, new_tokens=requests,
+                lens_out=requests, free_ring=4 * sh.num_pages, free_span=8, free_span_out=8, slots=4 * tokens, status=4,
+                bounds=sh.num_pages * sh.kv_heads * 2 * sh.d, bound_scales=sh.num_pages * sh.kv_heads * 4,
+                selected=tokens * sh.kv_heads * 4 * 4, lse=tokens * sh.q_heads * 4)
+    rows = lambda a: paged._CRows(a, 1024, 128)  # noqa: E731
+    kv_rows = lambda a: paged._CRows(a, 512, 128)  # noqa: E731
+    size["k_new"] = size["v_new"] = (3 * 512 + 128 + 128) * 2
+
+    def attend(a, top=0):
+        size["ws"] = hk.paged_attend_workspace_bytes(sh, tokens, top)
+        more = (a["selected"], top) if top else ()
+        call = L.heatkv_paged_attend_selected if top else L.heatkv_paged_attend
+        return lambda: call(sh.ref, tokens, rows(a["q"]), a["k_pages"], a["v_pages"], a["table"], a["q_start"], a["lens"], *more, 0.1, 1,
+                            rows(a["out"]), a["lse"], a["ws"], 1 << 40, None)
+    calls = {
+        "assign": (("keep", "new_tokens", "lens", "lens_out", "free_ring", "free_span", "free_span_out", "table", "q_start", "slots", "status"),
+                   ("lens_out", "free_ring", "free_span_out", "table", "q_start", "slots", "status"),
+                   lambda a: lambda: L.heatkv_paged_assign(
+                       sh.ref, *[a[x] for x in ("keep", "new_tokens", "lens", "lens_out", "free_ring", "free_span", "free_span_out",
+                                                "table", "q_start", "slots")], tokens, a["status"], None), ()),
+        "append": (("slots", "k_new", "v_new", "k_pages", "v_pages", "bounds", "bound_scales"), ("k_pages", "v_pages", "bounds", "bound_scales"),
+                   lambda a: lambda: L.heatkv_paged_append(sh.ref, a["slots"], tokens, kv_rows(a["k_new"]), kv_rows(a["v_new"]),
+                                                           a["k_pages"], a["v_pages"], a["bounds"], a["bound_scales"], None),
+                   {("k_pages", "k_new"), ("k_pages", "v_new"), ("v_pages", "k_new"), ("v_pages", "v_new")}),
+        "attend": (("q", "k_pages", "v_pages", "table", "q_start", "lens", "out", "lse", "ws"), ("out", "lse", "ws"), attend, ()),
+        "attend_selected": (("q", "k_pages", "v_pages", "table", "q_start", "lens", "out", "lse", "ws", "selected"), ("out", "lse", "ws"),
+                            lambda a: attend(a, 4), ()),
+        "select": (("q", "bounds", "bound_scales", "table", "q_start", "lens", "selected"), ("selected",),
+                   lambda a: lambda: L.heatkv_paged_select(sh.ref, tokens, rows(a["q"]), a["bounds"], a["bound_scales"], a["table"],
+                                                           a["q_start"], a["lens"], 1, 1, 4, 1, a["selected"], None), ()),
+    }
+    for names, written, call, allowed in calls.values():
+        apart = {n: at(i) for i, n in enumerate((*names, "ws"))}
+        call(apart)  # sets the workspace's size; not called
+        for w in written:
+            for other in names:
+                if other == w or (w, other) in allowed or {w, other} in ({"lens_out", "lens"}, {"free_span_out", "free_span"}):
+                    continue
+                # the same first byte; the other's last 16 bytes or less; the other lies within, or begins at the last bytes
+                for where in (apart[w], apart[w] + (size[w] - 1) // 16 * 16, apart[w] - (size[other] - 1) // 16 * 16):
+                    _fail(call({**apart, other: where})(), f"{w} overlaps {other}|{other} overlaps {w}|must not overlap")
+
+
+def test_outputs_among_the_queries_are_refused():
+    L, sh, a = paged._lib(), _shape(kv_heads=2, q_heads=4, d=64), 1 << 36
+    call = lambda q, out, tokens=5: L.heatkv_paged_attend(  # noqa: E731
+        sh.ref, tokens, paged._CRows(*q), 1 << 37, 1 << 38, 1 << 39, 1 << 40, 1 << 41, 0.1, 1, paged._CRows(*out), None, 1 << 42, 1 << 40, None)
+    for q, out in (((a, 256, 64), (a, 256, 64)), ((a, 512, 64), (a + 2 * 248, 512, 64)), ((a, 512, 64), (a + 2 * (2048 + 192), 512, 64)),
+                   ((a + 2 * (2048 + 192), 512, 64), (a, 512, 64)), ((a, 64, 320), (a + 2 * 256, 64, 320)),
+                   ((a, 512, 128), (a + 2 * 8, 512, 128)), ((a, 512, 128), (a + 2 * (512 + 128), 512, 128)), ((a, 512, 64), (a + 512, 768, 64)),
+                   ((a, 0, 0), (a, 256, 64))):
+        _fail(call(q, out), "out overlaps q")
+    _fail(call((a, 1 << 61, 1 << 60), (a, 1 << 61, 1 << 60)), "overlaps")  # everything
+    _fail(call((a, 8, 64), (a, 16, 64), 1), "out overlaps q")
