@@ -299,19 +299,21 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_kernel(AttendParam
       for (int i = 1; i < WAVES; ++i) m_row = fmaxf(m_row, part_m[i][r]);
       for (int i = 0; i < WAVES; ++i) l_row += part_l[i][r] * fast_exp2((part_m[i][r] - m_row) * c);
       const float norm = !alone ? 1.f : l_row > 0.f ? 1.f / l_row : l_row;
-      redo_row<bf16_t, FP8, D>(
-          z, tile.q0 + jr, hr, visible_keys(z.c, tile, jr), 2 * begin, 2 * end,
+      float* const parts_row = z.parts.o + (part_base + r) * D;  // the part's, or not used
+      bf16_t* const out_row = static_cast<bf16_t*>(const_cast<void*>(z.out.data)) + (tile.q0 + jr) * z.out.token_stride + hr * z.out.head_stride;
+      redo_row<bf16_t, FP8, D, CHOSEN>(
+          z, tile.q0 + jr, hr, visible_keys(z.c, tile, jr), tile.len, 2 * begin, 2 * end, false,
           [&](int gr) {
             const Granule at = walk.locate(gr);
             return RedoGranule{at.row, at.pos, walk.sees(at, jr - j_first)};
           },
           [&](float score) { return fast_exp2((score - m_row) * c); },
+          [&](int col) { return alone ? static_cast<float>(out_row[col]) : parts_row[col]; },
           [&](int col, float x, float) {
             if (!alone)
-              z.parts.o[(part_base + r) * D + col] = x;
+              parts_row[col] = x;
             else
-              (static_cast<bf16_t*>(const_cast<void*>(z.out.data)) + (tile.q0 + jr) * z.out.token_stride + hr * z.out.head_stride)[col] =
-                  static_cast<bf16_t>(x * norm);
+              out_row[col] = static_cast<bf16_t>(x * norm);
           });
     }
     if (CHOSEN) __syncthreads();  // the walk's tables are free as well

@@ -181,20 +181,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_f32_kernel(AttendP
       for (int i = 1; i < WAVES; ++i) m_row = fmaxf(m_row, part_m[i][r]);
       for (int i = 0; i < WAVES; ++i) l_row += part_l[i][r] * prob(part_m[i][r], m_row);
       const float norm = !alone ? 1.f : l_row > 0.f ? 1.f / l_row : l_row;
-      redo_row<float, false, D>(
-          z, tile.q0 + jr, hr, visible_keys(z.c, tile, jr), 2 * begin, 2 * end,
+      float* const to = !alone ? z.parts.o + (part_base + r) * D
+                               : static_cast<float*>(const_cast<void*>(z.out.data)) + (tile.q0 + jr) * z.out.token_stride + hr * z.out.head_stride;
+      redo_row<float, false, D, CHOSEN>(
+          z, tile.q0 + jr, hr, visible_keys(z.c, tile, jr), tile.len, 2 * begin, 2 * end, false,
           [&](int gr) {
             const Granule x = walk.locate(gr);
             return RedoGranule{x.row, x.pos, walk.sees(x, jr - j_first)};
           },
           [&](float score) { return prob(score * prob.c, m_row) * 0x1p-8f; },
-          [&](int col, float x, float) {
-            if (!alone)
-              z.parts.o[(part_base + r) * D + col] = x;
-            else
-              (static_cast<float*>(const_cast<void*>(z.out.data)) + (tile.q0 + jr) * z.out.token_stride + hr * z.out.head_stride)[col] =
-                  x * norm;
-          });
+          [&](int col) { return to[col]; }, [&](int col, float x, float) { to[col] = x * norm; });
     }
     if (CHOSEN) __syncthreads();  // the walk's tables are free as well
   }

@@ -613,8 +613,11 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     const float m_row = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, m), r));
     const float l_row = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, l), r));
     const bool lost = CHOSEN && l_row != l_row;  // a score that is not finite, of a page that other rows have chosen or this one
-    redo_row<bf16_t, FP8, D>(
-        z, tl.q0 + j, hq, visible_keys(z.c, tl, j), 4 * begin, 4 * end,
+    const long long part_row = static_cast<long long>(w) * BM + w_row + r;
+    float* const parts_row = z.parts.o + part_row * D;  // the part's, or not used
+    bf16_t* const out_row = static_cast<bf16_t*>(const_cast<void*>(z.out.data)) + (tl.q0 + j) * z.out.token_stride + hq * z.out.head_stride;
+    const float l_seen = redo_row<bf16_t, FP8, D, CHOSEN>(
+        z, tl.q0 + j, hq, visible_keys(z.c, tl, j), tl.len, 4 * begin, 4 * end, lost,
         [&](int g) {
           const TileRows rows_at = locate(g >> 2);
           const int from = g & 2 ? (g & 1 ? rows_at.granule[3] : rows_at.granule[2]) : (g & 1 ? rows_at.granule[1] : rows_at.granule[0]);
@@ -627,21 +630,20 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
           return RedoGranule{static_cast<long long>(from) * 16, pos, seen};
         },
         [&](float score) { return fast_exp2((score - m_row) * c); },
+        [&](int col) { return alone ? static_cast<float>(out_row[col]) : parts_row[col]; },
         [&](int col, float x, float sum) {
-          const long long part_row = static_cast<long long>(w) * BM + w_row + r;
-          const float l_seen = lost ? sum : l_row, norm = l_seen > 0.f ? 1.f / l_seen : l_seen;
-          if (lost && col == 0) {
-            if (!alone)
-              z.parts.ml[part_row * 2 + 1] = sum;
-            else if (z.lse)
-              z.lse[(tl.q0 + j) * static_cast<long long>(z.c.Hq) + hq] = natural_lse(m_row, sum, z.sm_scale);
-          }
+          const float l_all = lost ? sum : l_row;
           if (!alone)
-            z.parts.o[part_row * D + col] = x;
+            parts_row[col] = x;
           else
-            (static_cast<bf16_t*>(const_cast<void*>(z.out.data)) + (tl.q0 + j) * z.out.token_stride + hq * z.out.head_stride)[col] =
-                static_cast<bf16_t>(x * norm);
+            out_row[col] = static_cast<bf16_t>(x * (l_all > 0.f ? 1.f / l_all : l_all));
         });
+    if (lost && lane == 0) {
+      if (!alone)
+        z.parts.ml[part_row * 2 + 1] = l_seen;
+      else if (z.lse)
+        z.lse[(tl.q0 + j) * static_cast<long long>(z.c.Hq) + hq] = natural_lse(m_row, l_seen, z.sm_scale);
+    }
   }
 }
 
