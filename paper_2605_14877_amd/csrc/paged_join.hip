@@ -99,9 +99,9 @@ __device__ __forceinline__ void join(const AttendParams& p, const Parts& from, i
           // Places behind the last part hold that part again: left out, not multiplied by 0, as it may hold infinities.
           const bool real = i0 + 2 * u < parts;
           const float g = factor(y[r][u].m, m);
-          sum[r].l = real ? sum[r].l + g * y[r][u].l : sum[r].l;
+          sum[r].l += g * (real ? y[r][u].l : 0.f);
 #pragma unroll
-          for (int k = 0; k < N; ++k) sum[r].x[k] = real ? sum[r].x[k] + g * y[r][u].x[k] : sum[r].x[k];
+          for (int k = 0; k < N; ++k) sum[r].x[k] += g * (real ? y[r][u].x[k] : 0.f);
         }
       }
     }
