@@ -102,39 +102,42 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return x < y + nb && y < x + na;
 }
 
-// One array of a call, from its first byte to its last.
+// One array of a call: the addresses of its first byte and of the one behind its last.
 struct Span {
   const char* name;
-  __int128 first, end;
+  uintptr_t first, end;
   bool written;
 };
 constexpr bool READ = false, WRITTEN = true;
 Span span_of(const char* name, const void* p, size_t bytes, bool written) {
-  const auto first = static_cast<__int128>(reinterpret_cast<uintptr_t>(p));
-  return {name, first, first + (p ? static_cast<__int128>(bytes) : 0), written};
+  const auto first = reinterpret_cast<uintptr_t>(p);
+  return {name, first, first + (p ? bytes : 0), written};
 }
 Span span_of(const char* name, const heatkv_paged_shape* s, const heatkv_rows& r, int64_t tokens, int64_t heads, bool written) {
   const int elem = s->dtype == HEATKV_BF16 ? 2 : 4;
   const __int128 t = static_cast<__int128>(r.token_stride) * (tokens - 1), h = static_cast<__int128>(r.head_stride) * (heads - 1);
   const auto at = static_cast<__int128>(reinterpret_cast<uintptr_t>(r.data));
-  return {name, at + (std::min<__int128>(t, 0) + std::min<__int128>(h, 0)) * elem,
-          at + (std::max<__int128>(t, 0) + std::max<__int128>(h, 0) + s->d) * elem, written};
+  const __int128 first = at + (std::min<__int128>(t, 0) + std::min<__int128>(h, 0)) * elem;
+  const __int128 end = at + (std::max<__int128>(t, 0) + std::max<__int128>(h, 0) + s->d) * elem;
+  return {name, static_cast<uintptr_t>(std::max<__int128>(first, 0)), static_cast<uintptr_t>(std::min<__int128>(end, UINTPTR_MAX)), written};
 }
-// Workgroups run in any order: what a call writes, it neither reads through another argument nor writes twice.
+bool meet(const Span& a, const Span& b) { return a.first < b.end && b.first < a.end && a.first < a.end && b.first < b.end; }
+// Workgroups run in any order: what a call writes, it neither reads through another argument nor writes twice.  Arrays that are
+// written come first.
 int check_disjoint(std::initializer_list<Span> arrays) {
-  for (const Span* a = arrays.begin(); a != arrays.end(); ++a)
-    for (const Span* b = arrays.begin(); b != a; ++b)
-      if ((a->written || b->written) && a->first < b->end && b->first < a->end && a->first < a->end && b->first < b->end)
-        return fail(HEATKV_EINVAL, std::string(b->written ? b->name : a->name) + " overlaps " + (b->written ? a->name : b->name));
+  for (const Span* a = arrays.begin(); a != arrays.end() && a->written; ++a)
+    for (const Span* b = a + 1; b != arrays.end(); ++b)
+      if (meet(*a, *b)) return fail(HEATKV_EINVAL, std::string(a->name) + " overlaps " + b->name);
   return HEATKV_OK;
 }
 // Whether two sets of rows, of which one is written, have an element in common.  Where their ranges overlap: not if they are slices
 // of one tensor, beside each other; rows that go by different strides are taken to meet.
 bool rows_meet(const heatkv_paged_shape* s, const heatkv_rows& a, const heatkv_rows& b, int64_t tokens, int64_t heads) {
-  const Span x = span_of("", s, a, tokens, heads, WRITTEN), y = span_of("", s, b, tokens, heads, WRITTEN);
-  if (x.end <= y.first || y.end <= x.first) return false;
+  const Span x = span_of("", s, a, tokens, heads, READ), y = span_of("", s, b, tokens, heads, WRITTEN);
+  if (!meet(x, y)) return false;
   if ((tokens > 1 && a.token_stride != b.token_stride) || (heads > 1 && a.head_stride != b.head_stride)) return true;
-  const __int128 off = (y.first - x.first) / (s->dtype == HEATKV_BF16 ? 2 : 4);
+  const __int128 bytes = static_cast<__int128>(reinterpret_cast<uintptr_t>(b.data)) - reinterpret_cast<uintptr_t>(a.data);
+  const __int128 off = bytes / (s->dtype == HEATKV_BF16 ? 2 : 4);
   const __int128 t = tokens > 1 ? a.token_stride < 0 ? -static_cast<__int128>(a.token_stride) : a.token_stride : 0;
   for (int64_t dh = 1 - heads; dh < heads; ++dh) {  // heads between two rows; then the tokens that bring them nearest
     const __int128 rest = off - static_cast<__int128>(dh) * a.head_stride;
