@@ -1172,3 +1172,44 @@ def test_infinite_values_of_small_probability(case):
             sees = torch.tensor([not causal or n - x + j + 1 > place for n, x in zip(p.lens, p.new) for j in range(x)], device="cuda")
             assert torch.all(out[sees, :, 3] == -math.inf) and out[~sees].isfinite().all()
             assert out[:, :, :3].isfinite().all() and out[:, :, 4:].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype,heads,d,pages,new,top", [
+    ("bf16", (4, 2), 64, 1100, 1, 40), ("bf16", (4, 2), 64, 1025, 20, 9), ("f32", (2, 2), 128, 3000, 2, 512), ("bf16", (2, 1), 64, 1500, 530, 5),
+    ("bf16", (8, 8), 64, 1030, 512, 7)])
+def test_choice_of_more_pages_than_registers_hold(dtype, heads, d, pages, new, top):
+    # more than 1024 scores: ranked out of LDS, by four wavefronts where a workgroup has one token
+    p = Problem(dtype, *heads, d, 16, [16 * pages - 5, 90], [new, 1], seed=34)
+    for coarse in (False, True):
+        bounds, scales = _with_bounds(p, coarse)
+        for first, last in ((1, 2), (0, 1)):
+            chosen = ref.select(p.q, bounds, scales, p.table, p.q_start, p.lens, p.page, first, last, top, True)
+            selected = torch.full((p.tokens, p.H, top), 77, dtype=torch.int32, device="cuda")
+            hk.heatkv_paged_select(p.shape, p.dev["q"], bounds.cuda(), scales.cuda(), p.dev["table"], p.dev["q_start"],
+                                   p.dev["lens"], first, last, selected)
+            got = selected.tolist()
+            for t in range(p.q_start[-1]):
+                assert got[t] == [x + [-1] * (top - len(x)) for x in chosen[t]], (t, coarse)
+            assert torch.all(selected[p.q_start[-1]:] == 77)
+            if heads[1] > 2 or new > 500:
+                break  # the reference takes its time
+
+
+@pytest.mark.parametrize("case,top", [(c, 0) for c in FEW[3:8] + FEW[-3:] + MANY + CUT] + [(c[:7], c[7]) for c in SPARSE + SPARSE_MANY] + [
+    (("bf16", 4, 2, 64, 16, [n for n in (900, 300, 40) for _ in range(30)], [n for n in (1, 2, 70) for _ in range(30)]), 0),
+    (("f32", 2, 1, 64, 16, [700] * 130, [1] * 130), 0), (("bf16", 8, 8, 64, 32, [2000] * 40, [1] * 40), 6)], ids=lambda x: str(x)[:50])
+def test_nothing_is_written_behind_the_workspace(case, top):
+    p = Problem(*case, seed=35)
+    d, n, guard = p.dev, hk.paged_attend_workspace_bytes(p.shape, p.tokens, top), 1 << 16
+    ws = torch.full((n + guard,), 165, dtype=torch.uint8, device="cuda")
+    out = torch.zeros_like(d["q"])
+    args = (p.shape, d["q"], d["k"], d["v"], d["table"], d["q_start"], d["lens"])
+    r = random.Random(35)
+    for causal in (True, False):
+        if top:
+            sel = _ints([[[r.randrange(0, p.max_pages) for _ in range(top)] for _ in range(p.H)] for _ in range(p.tokens)])
+            hk.heatkv_paged_attend_selected(*args, sel, p.sm, out, ws[:n], causal=causal)
+        else:
+            hk.heatkv_paged_attend(*args, p.sm, out, ws[:n], causal=causal)
+    torch.cuda.synchronize()
+    assert torch.all(ws[n:] == 165)

@@ -437,3 +437,40 @@ def test_outputs_among_the_queries_are_refused():
         _fail(call(q, out), "out overlaps q")
     _fail(call((a, 1 << 61, 1 << 60), (a, 1 << 61, 1 << 60)), "overlaps")  # everything
     _fail(call((a, 8, 64), (a, 16, 64), 1), "out overlaps q")
+
+
+def test_pieces_of_chosen_pages_fit_the_grid_and_the_workspace(rules, launches):
+    # a segment is as heavy as the pages that its tile's tokens can have chosen between them
+    import random
+    r, some = random.Random(5), {"few": 0, "many": 0}
+    for _ in range(1500):
+        group, heads, batch = r.choice([1, 2, 3, 4, 16]), r.choice([1, 2, 8, 64]), r.choice([1, 2, 5, 40, 300])
+        page, top = r.choice([16, 64, 256]), r.choice([1, 3, 32, 512])
+        longest = r.choice([16, 513, 4096, 70000])
+        new = [r.choice([0, 1, 5, 64 // group, 64 // group + 1, r.randint(0, 3000 if batch < 40 else 100)]) for _ in range(batch)]
+        requests = [(n, r.randint(min(n, longest), longest)) for n in new]
+        args = (True, batch, heads, group, sum(new) + r.choice([0, 3]), -(-longest // page), page, top)
+        few, many, _ = rules(*args)
+        for name, launch, rows, keys in (("few", few, 16, 32), ("many", many, 128, 64)):
+            if not launch["workgroups"]:
+                continue
+            loads = []
+            for n_new, length in requests:
+                if launch["least_rows"] < n_new * group <= launch["most_rows"]:
+                    tokens = min(rows, (rows - 1) // group + 2, n_new)
+                    loads.append((-(-n_new * group // rows), max(-(-min(length, tokens * top * page) // keys), 1) * 32))
+            count, total = heads * sum(t for t, _ in loads), heads * sum(t * w for t, w in loads)
+            if name == "few" and count >= launch["whole_from"]:
+                continue  # dealt along the line: two places for each workgroup
+            if name == "many" and (count >= launch["whole_from"] or not launch["parts"]):
+                assert count <= launch["grid"]
+                continue
+            if not launch["parts"]:
+                assert count <= launch["grid"]
+                continue
+            shares = launch["workgroups"] - (count if name == "few" else 0)
+            share = max(-(-total // shares), launch["least_steps"] * 32)
+            pieces = heads * sum(t * -(-w // share) for t, w in loads)
+            assert pieces <= launch["grid"] and pieces <= launch["parts"] and pieces <= launches(*args)[name + "_join"]
+            some[name] += pieces > count
+    assert min(some.values()) > 50, some
