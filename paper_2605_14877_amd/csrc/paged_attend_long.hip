@@ -608,7 +608,8 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
   for (unsigned rows = static_cast<unsigned>(nan_lanes | nan_lanes >> 32); rows;) {  // paged_redo.h
     const int r = __builtin_ctz(rows);
     rows &= rows - 1;
-    wait_vmcnt<0>();  // the row's outputs from above come first
+    wait_vmcnt<0>();  // the row's outputs from above, which other lanes have written, come first
+    __threadfence_block();
     const int j = __builtin_amdgcn_readlane(out.j, r), hq = __builtin_amdgcn_readlane(out.hq, r);
     const float m_row = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, m), r));
     const float l_row = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, l), r));
