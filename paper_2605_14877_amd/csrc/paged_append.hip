@@ -9,7 +9,7 @@
 // Bound: memory traffic for prompts (rows in, rows out, 16 bytes per lane), latency for single tokens.  A page's bounds are
 // formed anew from all of its valid rows, which costs a decoding step up to a page of older rows per head, but needs no
 // running state that would have to follow when tokens are dropped or pages change owners.  12 prompts, 12000 tokens, 8 heads, d =
-// 128, into 8-bit pages: 73.5 MB in 21 us, 3.5 TB/s; the rows alone take 13.5 us.
+// 128, into 8-bit pages: 73.5 MB in 21 us, 3.5 TB/s; the rows alone take 13 us.
 #include <type_traits>
 
 #include "copy_rows.h"
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(LANES) void paged_append_bounds_kernel(PagedAppendA
 
 // Many pages: a wavefront per page, without barriers.  It looks for owners among `chunk` tokens (at most 64) of one kv head, and
 // its first rows are under way before it knows how many count.  Rows first and the bounds by a second launch, which reads them
-// back: 13.5 + 13 us where this takes 23.
+// back, took 13.5 + 13 us; this takes 21.
 template <class T, bool FP8, int D>
 __global__ __launch_bounds__(LANES) void paged_append_pages_kernel(PagedAppendArgs p, int chunk) {
   constexpr int COLS = D / 8, ROWS = 64 / COLS, U = 4, N = sizeof(T) / 2;
@@ -456,7 +456,8 @@ hipError_t launch(const PagedAppendArgs& a, hipStream_t stream) {
       hipLaunchKernelGGL((paged_append_bounds_kernel<T, FP8, D>), dim3(static_cast<unsigned>(units)), dim3(LANES), 0, stream, a);
     } else {
       // About one owner to a wavefront: one without costs its start, one with two takes twice the chain.  12 prompts, 12000
-      // tokens, 8 heads, chunks of 12, 24, 48: pages of 32 26.0, 23.3, 26.8 us, of 64 26.2, 24.3, 20.4, of 16 28.9, 28.1, 30.0.
+      // tokens, 8 heads, d = 128, 8-bit pages, chunks of 12, 24, 48: pages of 16 22.3, 22.6, 25.8 us, of 32 25.1, 21.0, 23.7, of 64
+      // 24.8, 21.4, 25.2 (22.8 with the 46 that they get here).
       const int chunk = static_cast<int>(std::min<long long>(std::max<long long>(units / 2048, 1), std::min(64, 3 << a.page_log2 >> 2)));
       const long long groups = (a.tokens + chunk * (LANES / 64) - 1) / (chunk * (LANES / 64));
       hipLaunchKernelGGL((paged_append_pages_kernel<T, FP8, D>), dim3(static_cast<unsigned>(groups * a.H)), dim3(LANES), 0, stream, a, chunk);

@@ -7,7 +7,8 @@
 //
 // Bound: latency, a chain of memory round trips (lengths; ring or table entries) and a block scan.  Small steps are one
 // workgroup.  In larger ones every workgroup makes the scan for itself and moves its share of pages and slots; as lens_out
-// and span_out may be lens and span, which all of them read, these are written by a second launch, which scans once more.
+// and span_out may be lens and span, which all of them read, these are written by a second launch, which scans once more (also
+// where they are arrays of their own).
 // 1024 requests, finished ones replaced by new prompts: 13.7 us, by one workgroup 84; 64 decoding requests: 7.1 us by one workgroup,
 // 11 by two launches.
 #include <hip/hip_runtime.h>
