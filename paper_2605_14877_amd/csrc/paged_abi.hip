@@ -3,6 +3,7 @@
 #include <cmath>
 #include <cstdint>
 #include <string>
+#include <utility>
 
 #include <hip/hip_runtime.h>
 
@@ -130,21 +131,30 @@ int check_disjoint(std::initializer_list<Span> arrays) {
       if (meet(*a, *b)) return fail(HEATKV_EINVAL, std::string(a->name) + " overlaps " + b->name);
   return HEATKV_OK;
 }
-// Whether two sets of rows, of which one is written, have an element in common.  Where their ranges overlap: not if they are slices
-// of one tensor, beside each other; rows that go by different strides are taken to meet.
-bool rows_meet(const heatkv_paged_shape* s, const heatkv_rows& a, const heatkv_rows& b, int64_t tokens, int64_t heads) {
-  const Span x = span_of("", s, a, tokens, heads, READ), y = span_of("", s, b, tokens, heads, WRITTEN);
-  if (!meet(x, y)) return false;
-  if ((tokens > 1 && a.token_stride != b.token_stride) || (heads > 1 && a.head_stride != b.head_stride)) return true;
-  const __int128 bytes = static_cast<__int128>(reinterpret_cast<uintptr_t>(b.data)) - reinterpret_cast<uintptr_t>(a.data);
+// Whether rows that are written (check_apart() holds) have an element in common with others.  Where their ranges overlap: not if
+// they are slices of one tensor, beside each other; rows that go by different strides are taken to meet.
+bool rows_meet(const heatkv_paged_shape* s, const heatkv_rows& out, const heatkv_rows& in, int64_t tokens, int64_t heads) {
+  if (!meet(span_of("", s, out, tokens, heads, WRITTEN), span_of("", s, in, tokens, heads, READ))) return false;
+  if ((tokens > 1 && out.token_stride != in.token_stride) || (heads > 1 && out.head_stride != in.head_stride)) return true;
+  struct Axis {
+    __int128 stride, count;
+  };
+  Axis outer{out.token_stride, tokens}, inner{out.head_stride, heads};
+  if (tokens == 1 || (heads > 1 && inner.stride > outer.stride)) std::swap(outer, inner);
+  for (Axis* x : {&outer, &inner})
+    if (x->count == 1) x->stride = static_cast<__int128>(1) << 80;  // not used
+  const __int128 bytes = static_cast<__int128>(reinterpret_cast<uintptr_t>(in.data)) - reinterpret_cast<uintptr_t>(out.data);
   const __int128 off = bytes / (s->dtype == HEATKV_BF16 ? 2 : 4);
-  const __int128 t = tokens > 1 ? a.token_stride < 0 ? -static_cast<__int128>(a.token_stride) : a.token_stride : 0;
-  for (int64_t dh = 1 - heads; dh < heads; ++dh) {  // heads between two rows; then the tokens that bring them nearest
-    const __int128 rest = off - static_cast<__int128>(dh) * a.head_stride;
-    __int128 dt = t ? rest / t - (rest % t < 0) : 0;
-    for (int i = 0; i < 2; ++i, ++dt) {
-      const __int128 apart = rest - dt * t;
-      if (dt < tokens && -dt < tokens && apart < s->d && -apart < s->d) return true;
+  auto floor = [](__int128 n, __int128 d) { return n / d - (n % d < 0); };
+  // Steps of the outer axis between two rows that meet (few: the inner axis lies within one), then the nearest of the inner one.
+  const __int128 reach = (inner.count - 1) * inner.stride + s->d;
+  const __int128 last = std::min(outer.count - 1, floor(off + reach, outer.stride));
+  for (__int128 i = std::max(1 - outer.count, floor(off - reach, outer.stride)); i <= last; ++i) {
+    const __int128 rest = off - i * outer.stride;
+    __int128 j = floor(rest, inner.stride);
+    for (int near = 0; near < 2; ++near, ++j) {
+      const __int128 apart = rest - j * inner.stride;
+      if (j < inner.count && -j < inner.count && apart < s->d && -apart < s->d) return true;
     }
   }
   return false;
