@@ -620,15 +620,15 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     const float l_seen = redo_row<bf16_t, FP8, D, CHOSEN>(
         z, tl.q0 + j, hq, visible_keys(z.c, tl, j), tl.len, 4 * begin, 4 * end, lost,
         [&](int g) {
+          if constexpr (CHOSEN) {
+            const int u = g >> per_log2, off = g & ((1 << per_log2) - 1);
+            if (u >= n_pages || !(chosen.who[4 * u + wave] >> (j - w_first) & 1)) return RedoGranule{0, 0, false};
+            return RedoGranule{(static_cast<long long>(__builtin_amdgcn_readfirstlane(chosen.granule[u])) + off) * 16,
+                               ((__builtin_amdgcn_readfirstlane(chosen.page[u]) << per_log2) + off) * 16, true};
+          }
           const TileRows rows_at = locate(g >> 2);
           const int from = g & 2 ? (g & 1 ? rows_at.granule[3] : rows_at.granule[2]) : (g & 1 ? rows_at.granule[1] : rows_at.granule[0]);
-          int pos = 16 * g;
-          bool seen = true;
-          if constexpr (CHOSEN) {
-            pos = g & 2 ? (g & 1 ? rows_at.pos[3] : rows_at.pos[2]) : (g & 1 ? rows_at.pos[1] : rows_at.pos[0]);
-            seen = chosen.who[4 * min(g >> per_log2, n_pages - 1) + wave] >> (j - w_first) & 1;
-          }
-          return RedoGranule{static_cast<long long>(from) * 16, pos, seen};
+          return RedoGranule{static_cast<long long>(from) * 16, 16 * g, true};
         },
         [&](float score) { return fast_exp2((score - m_row) * c); },
         [&](int col) { return alone ? static_cast<float>(out_row[col]) : parts_row[col]; },

@@ -8,8 +8,8 @@
 // Over all pages, the keys that a row does not see follow those that it sees, within the last tiles.  Where their values are finite
 // the NaN is the row's own and stays: a few keys are read instead of all.  Otherwise, and of chosen pages always, the NaN columns
 // are computed anew from the keys that the row sees, 16 at a time, until each is NaN or the keys are through.  300 new tokens x 4
-// heads over 4096 keys, d = 128, one NaN in V: 41 us where all rows see it (36 without; 2400 with all rows done anew), 430 among
-// the new tokens, 2400 in the last one.
+// heads over 4096 keys, d = 128, one NaN in V: 41 us where all rows see it (36 without; 2400 with all rows done anew key by key),
+// 430 among the new tokens, 1000 in the last one; on a page that some of 1024 tokens have chosen: 2600 (142 without).
 #pragma once
 
 #include "paged.h"
@@ -61,18 +61,25 @@ __device__ __forceinline__ float redo_row(const AttendParams& p, long long token
   for (int g = begin; g < end && sum == sum; ++g) {  // behind a probability that is NaN everything stays NaN
     const auto at = locate(g);
     if (!at.seen || at.pos >= limit) continue;
+    float v[16][N];  // all loads of a granule under way together; of keys that the row does not see not used
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[k][i] = cache_value<T, FP8>(p.v_pages, (at.row + k) * D + 64 * i + lane);
     float s = 0.f;
-    for (int i = quarter; i < D; i += 4)
-      s = fmaf(static_cast<float>(q[i]), cache_value<T, FP8>(p.k_pages, (at.row + key) * D + i), s);
+#pragma unroll
+    for (int i = 0; i < D; i += 4)
+      s = fmaf(static_cast<float>(q[i + quarter]), cache_value<T, FP8>(p.k_pages, (at.row + key) * D + i + quarter), s);
     s += __shfl_xor(s, 1, 64);
     s += __shfl_xor(s, 2, 64);
     const float e = at.pos + key < limit ? probability(s) : -1.f;
+#pragma unroll
     for (int k = 0; k < 16; ++k) {
-      const float w = __shfl(e, 4 * k, 64);
+      const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, e), 4 * k));
       if (!(w < 0.f)) {  // seen, whatever its probability
         sum += w;
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] += w * cache_value<T, FP8>(p.v_pages, (at.row + k) * D + 64 * i + lane);
+        for (int i = 0; i < N; ++i) x[i] += w * v[k][i];
       }
     }
     bool open = with_sum;
