@@ -865,11 +865,13 @@ def _exact_pages(st):
 
 
 def exact(case, seed):
+    tables = case["what"] in ("share", "compact")
+    if tables and case["dtype"] == "fp4":
+        return None  # integers, and values that other cases form
     st = prepare(case, seed)
-    if case["what"] in ("share", "compact"):
+    if tables:
         whole = [None] * (10 if case["what"] == "share" else 8)
-        values = [None, None] if case["dtype"] == "fp4" else _exact_pages(st)
-        return whole + values + ([None, None] if case["bounds"] else [])
+        return whole + _exact_pages(st) + ([None, None] if case["bounds"] else [])
     cached, new = _lengths(case)
     page, H, G = case["page"], case["kv_heads"], case["q_heads"] // case["kv_heads"]
     if case["what"] == "append":
