@@ -74,6 +74,7 @@ extern "C" {
  * the current scale's K/V, which come from the caller's tensors, keep their precision. */
 #define HEATKV_KV_NATIVE 0
 #define HEATKV_KV_FP8_E4M3 1
+#define HEATKV_KV_FP4_E2M1 4 /* paged cache only */
 
 /* Problem shape (Sec. 3.1 notation): L layers, H heads per layer, head dimension d,
  * K scales with t[k] tokens each, `batch` independent sequences processed together. */
@@ -309,6 +310,12 @@ int heatkv_rank_dispersion(const heatkv_shape* shape, const float* betas, int ru
  *                  strides multiples of 16 bytes): slices of a fused projection are taken as they are
  *   pages          [num_pages][kv_heads][page_size][d], rows of the dtype, or E4M3 codes (HEATKV_KV_FP8_E4M3, bf16 shapes):
  *                  rounded to nearest even and saturating at +-448 on append, read back exactly
+ *   4-bit pages    (HEATKV_KV_FP4_E2M1, bf16 shapes) [num_pages][kv_heads][page_size * (d / 2 + d / 32)] bytes.  A row is d E2M1
+ *                  codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) and one E8M0 byte x for each 32 channels: value = code * 2^(x - 127),
+ *                  NaN if x = 255, and exact in bf16.  On append x - 127 is the least exponent in [-100, 125] with which no value of
+ *                  the 32 is more than 7 times the power; rounded to nearest even, saturating at 6 times the power, infinities too.
+ *                  A NaN makes all 32 channels NaN.  16 rows lie together: 16 times d / 2 bytes of codes (channel 2 i in the low
+ *                  half of byte i), then 16 times d / 32 scale bytes
  *   table          int32 [batch][max_pages]: page of a request's tokens [i * page_size, (i + 1) * page_size)
  *   lens           int32 [batch]: tokens of a request that lie in the cache (attention: those of this step among them)
  *   q_start        int32 [batch + 1]: request b's new tokens are rows q_start[b] .. q_start[b+1]-1 of the token tensors,
@@ -339,6 +346,7 @@ typedef struct {
 #define HEATKV_PAGED_BAD_LENGTH 2      /* a length is negative, keep > lens, or a request outgrows max_pages */
 #define HEATKV_PAGED_TOO_MANY_TOKENS 3 /* more new tokens than rows of the token tensors */
 #define HEATKV_PAGED_BAD_FREE_LIST 4   /* free_span does not fit the ring, or more pages come back than there are */
+#define HEATKV_PAGED_BAD_PARENT 5      /* fork: a parent is not a row of the table */
 
 /* One step of the page allocator.  Request b keeps the first keep[b] of its lens[b] tokens and gets new_tokens[b] more; it
  * then holds ceil((keep + new) / page_size) pages.  Pages that it lacks come from the ring of free pages, pages that it no
@@ -410,6 +418,61 @@ int heatkv_paged_attend_selected(const heatkv_paged_shape* shape, int64_t tokens
                                  const void* v_pages, const int32_t* table, const int32_t* q_start, const int32_t* lens,
                                  const int32_t* selected, int top, float sm_scale, int causal, heatkv_rows out, float* lse,
                                  void* ws, size_t ws_bytes, void* stream);
+
+/* Rows of the cache by their slots (as heatkv_paged_append takes them), as values of the dtype: what attention goes on with, exactly.
+ * Rows of k_out and v_out whose slot is outside of [0, num_pages * page_size) are left as they are.  k_out and v_out may be slices
+ * of one tensor beside each other, by the same strides. */
+int heatkv_paged_read(const heatkv_paged_shape* shape, const int32_t* slots, int64_t tokens, const void* k_pages,
+                      const void* v_pages, heatkv_rows k_out, heatkv_rows v_out, void* stream);
+
+/* Pages that several requests hold: beams, samples of one prompt, common prefixes; and requests that lose tokens out of their middle.
+ * holders: int32 [num_pages], how many rows of the table hold a page; 0 for free ones (all of them, before the first call).  A
+ * cache with holders has its pages taken and given back by the three calls below, and not by heatkv_paged_assign.  They read and
+ * write lens, free_ring, free_span and table as that does (lens_out and free_span_out may be lens and free_span); pages that no row
+ * holds any more go behind the ring's tail, in ascending order, and are taken again by a later call at the earliest.  Holders that
+ * do not fit the table give wrong tables, but touch nothing outside of the arrays.
+ * ws  device scratch of heatkv_paged_tables_workspace_bytes(shape) bytes, 16-byte aligned.  Calls that may run at the same time, graphs
+ *     among them, need a workspace each
+ * status as for heatkv_paged_assign: unless it is HEATKV_PAGED_OK the call has changed nothing but its lists (slots and moves are -1,
+ * q_start zeros).  batch * max_pages is at most 2^30. */
+size_t heatkv_paged_tables_workspace_bytes(const heatkv_paged_shape* shape);
+
+/* Row b of the table continues row parent[b], all of them at once, as the rows were before the call: it holds the same pages and has
+ * the same length.  parent[b] = b leaves it as it is, -1 ends it.  No row of the cache is touched: a page that the new tokens of
+ * several rows would go to is only copied once they do (heatkv_paged_assign_shared).
+ * parent  int32 [batch], read only
+ * table   in place: entries that a row gains are written, all others stay as they are */
+int heatkv_paged_fork(const heatkv_paged_shape* shape, const int32_t* parent, const int32_t* lens, int32_t* lens_out,
+                      int32_t* holders, int32_t* free_ring, const int32_t* free_span, int32_t* free_span_out, int32_t* table,
+                      int32_t* status, void* ws, size_t ws_bytes, void* stream);
+
+/* One step of the allocator, as heatkv_paged_assign, for a cache with holders.  All pages behind the last that holds one of the keep[b]
+ * tokens are let go, those for new tokens come from the ring.  Where new tokens would go onto a page that another row holds as well
+ * (the last one with kept tokens), the row takes a fresh page in its place, and the kept tokens on it are listed:
+ * copy_from, copy_to  out, int32 [batch][page_size]: slots of these rows and their new places, -1 for all else; for
+ *                     heatkv_paged_move, in every layer, before heatkv_paged_append */
+int heatkv_paged_assign_shared(const heatkv_paged_shape* shape, const int32_t* keep, const int32_t* new_tokens,
+                               const int32_t* lens, int32_t* lens_out, int32_t* holders, int32_t* free_ring,
+                               const int32_t* free_span, int32_t* free_span_out, int32_t* table, int32_t* q_start, int32_t* slots,
+                               int64_t max_tokens, int32_t* copy_from, int32_t* copy_to, int32_t* status, void* ws,
+                               size_t ws_bytes, void* stream);
+
+/* Every request keeps those of its tokens that are marked, in order.  Pages in front of the first token that goes stay as they are;
+ * behind it the kept tokens get fresh pages (so pages that other rows hold are never written), and their old ones are let go.  A
+ * request that loses only its last tokens keeps all pages that it still needs.
+ * kept       [batch][max_pages * page_size] bytes: not 0 for tokens that stay; those from lens[b] on are not looked at
+ * move_from, move_to  out, int32 [max_moves]: slots of the rows that move and their new places, requests and tokens in order, -1
+ *            behind the last; for heatkv_paged_move, in every layer.  More than max_moves: HEATKV_PAGED_TOO_MANY_TOKENS */
+int heatkv_paged_compact(const heatkv_paged_shape* shape, const uint8_t* kept, const int32_t* lens, int32_t* lens_out,
+                         int32_t* holders, int32_t* free_ring, const int32_t* free_span, int32_t* free_span_out, int32_t* table,
+                         int32_t* move_from, int32_t* move_to, int64_t max_moves, int32_t* status, void* ws, size_t ws_bytes,
+                         void* stream);
+
+/* Row move_to[i] of the cache becomes what row move_from[i] is, K and V of all kv heads, as stored.  Entries whose move_to is outside of
+ * [0, num_pages * page_size) are skipped.  No row is moved to twice, and none that is moved to is one that is moved from.
+ * bounds, bound_scales as for heatkv_paged_append, of the pages that rows are moved to. */
+int heatkv_paged_move(const heatkv_paged_shape* shape, const int32_t* move_from, const int32_t* move_to, int64_t rows,
+                      void* k_pages, void* v_pages, int8_t* bounds, float* bound_scales, void* stream);
 
 #ifdef __cplusplus
 }

@@ -7,6 +7,7 @@ memory handles and for the current HIP stream.
 """
 from .binding import (  # noqa: F401
     HeatKVError,
+    KV_FP4_E2M1,
     KV_FP8_E4M3,
     KV_NATIVE,
     Plan,
@@ -35,14 +36,21 @@ from .binding import (  # noqa: F401
 from .paged import (  # noqa: F401
     PAGED_BAD_FREE_LIST,
     PAGED_BAD_LENGTH,
+    PAGED_BAD_PARENT,
     PAGED_NO_PAGES,
     PAGED_OK,
     PAGED_TOO_MANY_TOKENS,
     PagedShape,
     heatkv_paged_append,
     heatkv_paged_assign,
+    heatkv_paged_assign_shared,
     heatkv_paged_attend,
     heatkv_paged_attend_selected,
+    heatkv_paged_compact,
+    heatkv_paged_fork,
+    heatkv_paged_move,
+    heatkv_paged_read,
     heatkv_paged_select,
     paged_attend_workspace_bytes,
+    paged_tables_workspace_bytes,
 )

@@ -17,7 +17,7 @@ _CALL_PATH = os.path.join(os.path.dirname(_LIB_PATH), "_heatkv_call.so")
 F32, BF16 = 0, 1
 VARIANT_HEATKV, VARIANT_BINARY, VARIANT_NAIVE, VARIANT_BINARY_NAIVE = 0, 1, 2, 3
 SET_G, SET_E, SET_A = 0, 1, 2
-KV_NATIVE, KV_FP8_E4M3 = 0, 1
+KV_NATIVE, KV_FP8_E4M3, KV_FP4_E2M1 = 0, 1, 4
 _DTYPES = {"f32": F32, "bf16": BF16}
 
 

@@ -226,6 +226,7 @@ class PagedCall {
     ok_ = ok_ && s_;
   }
   bool ok() const { return ok_; }
+  void refuse() { ok_ = false; }
   const heatkv_paged_shape* shape() const { return s_; }
   void* stream() const { return stream_; }
 
@@ -261,9 +262,11 @@ class PagedCall {
   }
   void* pages(PyObject* o) {
     const at::Tensor* x = tensor(o);
-    const int64_t sizes[4] = {s_->num_pages, s_->kv_heads, s_->page_size, s_->d};
-    if (!x || !x->is_contiguous() || x->sizes() != at::IntArrayRef(sizes)) return fail_ptr();
+    const bool fp4 = s_->kv_format == HEATKV_KV_FP4_E2M1;  // [num_pages][kv_heads][bytes of a page]
+    const int64_t sizes[4] = {s_->num_pages, s_->kv_heads, fp4 ? int64_t(s_->page_size) * (s_->d / 2 + s_->d / 32) : s_->page_size, s_->d};
+    if (!x || !x->is_contiguous() || x->sizes() != at::IntArrayRef(sizes, fp4 ? 3 : 4)) return fail_ptr();
     const at::ScalarType t = x->scalar_type();
+    if (fp4) return t == at::kByte ? x->data_ptr() : fail_ptr();
     const bool fits = s_->kv_format == HEATKV_KV_FP8_E4M3 ? t == at::kFloat8_e4m3fn || t == at::kByte
                                                            : t == (s_->dtype == HEATKV_BF16 ? at::kBFloat16 : at::kFloat);
     return fits ? x->data_ptr() : fail_ptr();
@@ -287,6 +290,114 @@ class PagedCall {
 bool boolean(PyObject* o, int* v) {
   *v = o == Py_True;
   return PyBool_Check(o);
+}
+
+// What the calls on shared pages have in common: a = lens, holders, ring, span, table; out = lens_out, span_out, or None.
+struct TableOperands {
+  int32_t *lens, *lens_out, *holders, *ring, *span, *span_out, *table, *status;
+  void* ws = nullptr;
+  size_t ws_bytes = 0;
+  TableOperands(PagedCall& c, PyObject* const* a, PyObject* status_o, PyObject* ws_o, PyObject* const* out) {
+    const heatkv_paged_shape* s = c.shape();
+    lens = c.ints(a[0], {s->batch});
+    holders = c.ints(a[1], {s->num_pages});
+    ring = c.ints(a[2], {s->num_pages});
+    span = c.ints(a[3], {2});
+    table = c.ints(a[4], {s->batch, s->max_pages});
+    status = c.ints(status_o, {1});
+    lens_out = out[0] == Py_None ? lens : c.ints(out[0], {s->batch});
+    span_out = out[1] == Py_None ? span : c.ints(out[1], {2});
+    const at::Tensor* x = c.tensor(ws_o);
+    if (x && buffer(ws_o, 0, &ws, &ws_bytes)) return;
+    c.refuse();
+  }
+};
+
+// paged_fork(shape, parent, lens, holders, ring, span, table, status, ws, lens_out, span_out, stream)
+PyObject* paged_fork(PyObject* const* a, Py_ssize_t n) {
+  if (n != 12) return not_plain();
+  PagedCall c(a[0], a[11]);
+  if (!c.ok()) return not_plain();
+  const heatkv_paged_shape* s = c.shape();
+  const int32_t* parent = c.ints(a[1], {s->batch});
+  const TableOperands t(c, a + 2, a[7], a[8], a + 9);
+  if (!c.ok()) return not_plain();
+  return PyLong_FromLong(heatkv::without_lock([&] {
+    return heatkv_paged_fork(s, parent, t.lens, t.lens_out, t.holders, t.ring, t.span, t.span_out, t.table, t.status, t.ws, t.ws_bytes,
+                             c.stream());
+  }));
+}
+
+// paged_assign_shared(shape, keep, new_tokens, lens, holders, ring, span, table, q_start, slots, copy_from, copy_to, status, ws,
+//                     lens_out, span_out, stream)
+PyObject* paged_assign_shared(PyObject* const* a, Py_ssize_t n) {
+  if (n != 17) return not_plain();
+  PagedCall c(a[0], a[16]);
+  if (!c.ok()) return not_plain();
+  const heatkv_paged_shape* s = c.shape();
+  int64_t tokens = 0;
+  const int32_t *keep = c.ints(a[1], {s->batch}), *come = c.ints(a[2], {s->batch});
+  const TableOperands t(c, a + 3, a[12], a[13], a + 14);
+  int32_t *q_start = c.ints(a[8], {int64_t(s->batch) + 1}), *slots = c.vector(a[9], &tokens);
+  int32_t *from = c.ints(a[10], {s->batch, s->page_size}), *to = c.ints(a[11], {s->batch, s->page_size});
+  if (!c.ok()) return not_plain();
+  return PyLong_FromLong(heatkv::without_lock([&] {
+    return heatkv_paged_assign_shared(s, keep, come, t.lens, t.lens_out, t.holders, t.ring, t.span, t.span_out, t.table, q_start, slots,
+                                      tokens, from, to, t.status, t.ws, t.ws_bytes, c.stream());
+  }));
+}
+
+// paged_compact(shape, kept, lens, holders, ring, span, table, move_from, move_to, status, ws, lens_out, span_out, stream)
+PyObject* paged_compact(PyObject* const* a, Py_ssize_t n) {
+  if (n != 14) return not_plain();
+  PagedCall c(a[0], a[13]);
+  if (!c.ok()) return not_plain();
+  const heatkv_paged_shape* s = c.shape();
+  int64_t moves = 0;
+  const at::Tensor* kept = c.tensor(a[1]);
+  if (!kept || (kept->scalar_type() != at::kBool && kept->scalar_type() != at::kByte)) return not_plain();
+  const auto* marks = static_cast<const uint8_t*>(c.dense(a[1], kept->scalar_type(), {s->batch, int64_t(s->max_pages) * s->page_size}));
+  const TableOperands t(c, a + 2, a[9], a[10], a + 11);
+  int32_t* to = c.vector(a[8], &moves);
+  int32_t* from = c.ints(a[7], {moves});
+  if (!c.ok()) return not_plain();
+  return PyLong_FromLong(heatkv::without_lock([&] {
+    return heatkv_paged_compact(s, marks, t.lens, t.lens_out, t.holders, t.ring, t.span, t.span_out, t.table, from, to, moves, t.status,
+                                t.ws, t.ws_bytes, c.stream());
+  }));
+}
+
+// paged_move(shape, move_from, move_to, k_pages, v_pages, bounds, scales, stream)
+PyObject* paged_move(PyObject* const* a, Py_ssize_t n) {
+  if (n != 8) return not_plain();
+  PagedCall c(a[0], a[7]);
+  if (!c.ok()) return not_plain();
+  const heatkv_paged_shape* s = c.shape();
+  const at::Tensor* list = c.tensor(a[2]);
+  if (!list || list->dim() < 1 || list->dim() > 2) return not_plain();
+  int32_t *to = c.ints(a[2], list->sizes()), *from = c.ints(a[1], list->sizes());
+  void *kp = c.pages(a[3]), *vp = c.pages(a[4]);
+  void* bounds = a[5] == Py_None ? nullptr : c.dense(a[5], at::kChar, {s->num_pages, s->kv_heads, 2, s->d});
+  void* scales = a[6] == Py_None ? nullptr : c.dense(a[6], at::kFloat, {s->num_pages, s->kv_heads});
+  if (!c.ok()) return not_plain();
+  const int64_t rows = list->numel();
+  return PyLong_FromLong(heatkv::without_lock([&] {
+    return heatkv_paged_move(s, from, to, rows, kp, vp, static_cast<int8_t*>(bounds), static_cast<float*>(scales), c.stream());
+  }));
+}
+
+// paged_read(shape, slots, k_pages, v_pages, k_out, v_out, stream)
+PyObject* paged_read(PyObject* const* a, Py_ssize_t n) {
+  if (n != 7) return not_plain();
+  PagedCall c(a[0], a[6]);
+  if (!c.ok()) return not_plain();
+  const heatkv_paged_shape* s = c.shape();
+  int64_t tokens = 0;
+  const int32_t* slots = c.vector(a[1], &tokens);
+  void *kp = c.pages(a[2]), *vp = c.pages(a[3]);
+  const heatkv_rows k = c.rows(a[4], s->kv_heads, &tokens), v = c.rows(a[5], s->kv_heads, &tokens);
+  if (!c.ok()) return not_plain();
+  return PyLong_FromLong(heatkv::without_lock([&] { return heatkv_paged_read(s, slots, tokens, kp, vp, k, v, c.stream()); }));
 }
 
 // paged_assign(shape, keep, new_tokens, lens, ring, span, table, q_start, slots, status, lens_out, span_out, stream)
@@ -399,6 +510,11 @@ PyMethodDef methods[] = {{"plan_info", plan_info, METH_VARARGS, nullptr},
                          {"paged_assign", heatkv::fastcall<paged_assign>(), METH_FASTCALL, nullptr},
                          {"paged_append", heatkv::fastcall<paged_append>(), METH_FASTCALL, nullptr},
                          {"paged_attend", heatkv::fastcall<paged_attend>(), METH_FASTCALL, nullptr},
+                         {"paged_read", heatkv::fastcall<paged_read>(), METH_FASTCALL, nullptr},
+                         {"paged_fork", heatkv::fastcall<paged_fork>(), METH_FASTCALL, nullptr},
+                         {"paged_assign_shared", heatkv::fastcall<paged_assign_shared>(), METH_FASTCALL, nullptr},
+                         {"paged_compact", heatkv::fastcall<paged_compact>(), METH_FASTCALL, nullptr},
+                         {"paged_move", heatkv::fastcall<paged_move>(), METH_FASTCALL, nullptr},
                          {"paged_select", heatkv::fastcall<paged_select>(), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 

@@ -93,9 +93,10 @@ hipError_t launch_paged_assign(const AssignArgs& a, hipStream_t stream);
 
 struct PagedAppendArgs {
   int dtype, d, H, page_log2, num_pages;
-  bool kv_fp8;
+  int kv_format;
   long long tokens;
   const int32_t* slots;
+  const int32_t* from;  // null, or rows of the cache instead of k_new and v_new
   const void *k_new, *v_new;
   long long k_token_stride, k_head_stride, v_token_stride, v_head_stride;  // elements
   void *k_pages, *v_pages;
@@ -103,5 +104,48 @@ struct PagedAppendArgs {
   float* bound_scales;
 };
 hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t stream);
+
+struct PagedReadArgs {
+  int dtype, d, H, page_log2, num_pages, kv_format;
+  long long tokens;
+  const int32_t* slots;
+  const void *k_pages, *v_pages;
+  void *k_out, *v_out;
+  long long k_token_stride, k_head_stride, v_token_stride, v_head_stride;  // elements
+};
+hipError_t launch_paged_read(const PagedReadArgs& a, hipStream_t stream);
+
+// Calls on pages that several rows of the table hold (paged_share.hip).
+struct TableArgs {
+  int batch, num_pages, max_pages, page_log2;
+  const int32_t *lens, *span;
+  int32_t *lens_out, *span_out, *holders, *ring, *table, *status;
+  // workspace: a few numbers, the lengths to be, a bit for each page that nobody holds any more
+  int32_t *state, *next;
+  uint32_t* gone;
+};
+struct ForkArgs {
+  TableArgs t;
+  const int32_t* parent;
+};
+struct AssignSharedArgs {
+  TableArgs t;
+  const int32_t *keep, *new_tokens;
+  int32_t *q_start, *slots, *copy_from, *copy_to;
+  long long max_tokens;
+  int32_t *take0, *touch0, *first, *copied;  // workspace, [batch + 1] each
+};
+struct CompactArgs {
+  TableArgs t;
+  const uint8_t* kept;
+  int32_t *move_from, *move_to;
+  long long max_moves;
+  int tile, tiles;  // tokens that a workgroup looks at, a multiple of 4096; how many such a row of the table may have
+  int32_t *take0, *move0, *first;  // workspace, [batch + 1] each
+  int32_t *counts, *drops;         // workspace, [batch][tiles] each
+};
+hipError_t launch_paged_fork(const ForkArgs& f, hipStream_t stream);
+hipError_t launch_paged_assign_shared(const AssignSharedArgs& a, hipStream_t stream);
+hipError_t launch_paged_compact(const CompactArgs& a, hipStream_t stream);
 
 }  // namespace heatkv

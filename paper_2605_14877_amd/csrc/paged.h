@@ -18,6 +18,15 @@ namespace paged {
 constexpr int GRANULE = 16;
 constexpr int MAX_BATCH = 4096;
 
+// How a cache row is stored: as the operands are, as E4M3 codes, or as E2M1 codes with a power of two (E8M0 byte, 255: NaN) for
+// each 32 channels.  4-bit rows of a granule lie together: 16 times d / 2 bytes of codes, then 16 times d / 32 scale bytes, so
+// that codes are read 16 bytes a lane and a granule is still one contiguous piece.
+enum Format : int { NATIVE, E4M3, E2M1 };
+template <class T, Format F>
+__host__ __device__ constexpr int row_bytes(int d) {
+  return F == E2M1 ? d / 2 + d / 32 : F == E4M3 ? d : d * static_cast<int>(sizeof(T));
+}
+
 struct Cache {
   int H, G, Hq;  // kv heads, queries per kv head, H * G
   int page_log2, num_pages, batch, max_pages;
@@ -102,6 +111,32 @@ __device__ __forceinline__ int code_exponent(float amax) {
   return amax > 0.f ? max(__builtin_amdgcn_frexp_expf(amax) - (m <= 127.f / 128.f ? 7 : 6), -100) : -100;
 }
 
+// 8 E4M3 codes, or 8 E2M1 codes times `scale`, as bf16 (exact).
+__device__ __forceinline__ bf16x8 codes_to_bf16(unsigned lo, unsigned hi) {
+  union {
+    bf16x2 h[4];
+    bf16x8 v;
+  } o;
+  o.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(lo), 1.0f, false);
+  o.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(lo), 1.0f, true);
+  o.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(hi), 1.0f, false);
+  o.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(hi), 1.0f, true);
+  return o.v;
+}
+__device__ __forceinline__ bf16x8 nibbles_to_bf16(unsigned codes, float scale) {
+  union {
+    bf16x2 h[4];
+    bf16x8 v;
+  } o;
+  o.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
+  o.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
+  o.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2);
+  o.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
+  return o.v;
+}
+// The conversion takes the exponent field as the E8M0 byte that it is: 255 gives NaN, whatever the codes.
+__device__ __forceinline__ float scale_of(unsigned byte) { return __uint_as_float(byte << 23); }
+
 struct Rows {  // of the token tensors, strides in elements
   const void* data;
   long long token_stride, head_stride;
@@ -159,8 +194,8 @@ using PagedAttendParams = paged::AttendParams;
 using PagedParts = paged::Parts;
 constexpr size_t PAGED_SELECT_LDS = paged::SELECT_LDS;
 hipError_t launch_paged_select(const PagedSelectParams& p, int dtype, int d, hipStream_t stream);
-hipError_t launch_paged_attend_bf16(const PagedAttendParams& p, int d, bool fp8, hipStream_t stream);
-hipError_t launch_paged_attend_long(const PagedAttendParams& p, int d, bool fp8, hipStream_t stream);
+hipError_t launch_paged_attend_bf16(const PagedAttendParams& p, int d, int kv_format, hipStream_t stream);
+hipError_t launch_paged_attend_long(const PagedAttendParams& p, int d, int kv_format, hipStream_t stream);
 hipError_t launch_paged_attend_f32(const PagedAttendParams& p, int d, hipStream_t stream);
 // few, many: of the two attention launches, grid: join_workgroups(), 0 where there is nothing to join.
 hipError_t launch_paged_join(const PagedAttendParams& p, const PagedParts& few, const PagedParts& many, int dtype, int d,

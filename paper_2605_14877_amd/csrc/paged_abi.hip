@@ -37,10 +37,12 @@ int check_shape(const heatkv_paged_shape* s) {
   if (s->kv_heads > 1024) return fail(HEATKV_EINVAL, "more than 1024 kv heads");
   if (s->d != 64 && s->d != 128) return fail(HEATKV_EINVAL, "head dimension must be 64 or 128");
   if (s->dtype != HEATKV_F32 && s->dtype != HEATKV_BF16) return fail(HEATKV_EINVAL, "unknown dtype");
-  if (s->kv_format != HEATKV_KV_NATIVE && s->kv_format != HEATKV_KV_FP8_E4M3)
+  if (s->kv_format != HEATKV_KV_NATIVE && s->kv_format != HEATKV_KV_FP8_E4M3 && s->kv_format != HEATKV_KV_FP4_E2M1)
     return fail(HEATKV_EINVAL, "unknown cache storage format");
   if (s->kv_format == HEATKV_KV_FP8_E4M3 && s->dtype != HEATKV_BF16)
     return fail(HEATKV_EINVAL, "HEATKV_KV_FP8_E4M3 needs a bf16 shape");
+  if (s->kv_format == HEATKV_KV_FP4_E2M1 && s->dtype != HEATKV_BF16)
+    return fail(HEATKV_EINVAL, "HEATKV_KV_FP4_E2M1 needs a bf16 shape");
   if (s->page_size < 16 || s->page_size > 256 || (s->page_size & (s->page_size - 1)) != 0)
     return fail(HEATKV_EINVAL, "page_size must be 16, 32, 64, 128 or 256");
   if (s->batch < 1 || s->batch > heatkv::paged::MAX_BATCH) return fail(HEATKV_EINVAL, "batch must be in [1, 4096]");
@@ -90,6 +92,13 @@ int check_cache(const void* k_pages, const void* v_pages) {
   return HEATKV_OK;
 }
 
+int check_bounds(const int8_t* bounds, const float* bound_scales) {
+  if ((bounds == nullptr) != (bound_scales == nullptr)) return fail(HEATKV_EINVAL, "bounds and bound_scales go together");
+  if (bounds && (!aligned(bounds, 16) || !aligned(bound_scales, 4)))
+    return fail(HEATKV_EINVAL, "bounds must be 16-byte aligned, bound_scales 4-byte");
+  return HEATKV_OK;
+}
+
 int check_ints(std::initializer_list<const void*> arrays) {
   for (const void* a : arrays) {
     if (!a) return fail(HEATKV_EINVAL, "null integer array");
@@ -125,12 +134,13 @@ Span span_of(const char* name, const heatkv_paged_shape* s, const heatkv_rows& r
 bool meet(const Span& a, const Span& b) { return a.first < b.end && b.first < a.end && a.first < a.end && b.first < b.end; }
 // Workgroups run in any order: what a call writes, it neither reads through another argument nor writes twice.  Arrays that are
 // written come first.
-int check_disjoint(std::initializer_list<Span> arrays) {
-  for (const Span* a = arrays.begin(); a != arrays.end() && a->written; ++a)
-    for (const Span* b = a + 1; b != arrays.end(); ++b)
+int check_disjoint(const Span* first, const Span* end) {
+  for (const Span* a = first; a != end && a->written; ++a)
+    for (const Span* b = a + 1; b != end; ++b)
       if (meet(*a, *b)) return fail(HEATKV_EINVAL, std::string(a->name) + " overlaps " + b->name);
   return HEATKV_OK;
 }
+int check_disjoint(std::initializer_list<Span> arrays) { return check_disjoint(arrays.begin(), arrays.end()); }
 // Whether rows that are written (check_apart() holds) have an element in common with others.  Where their ranges overlap: not if
 // they are slices of one tensor, beside each other; rows that go by different strides are taken to meet.
 bool rows_meet(const heatkv_paged_shape* s, const heatkv_rows& out, const heatkv_rows& in, int64_t tokens, int64_t heads) {
@@ -160,8 +170,10 @@ bool rows_meet(const heatkv_paged_shape* s, const heatkv_rows& out, const heatkv
   return false;
 }
 size_t pages_bytes(const heatkv_paged_shape* s) {
-  return size_t(s->num_pages) * s->page_size * s->kv_heads * s->d *
-         (s->dtype == HEATKV_F32 ? 4 : s->kv_format == HEATKV_KV_FP8_E4M3 ? 1 : 2);
+  const int row = s->kv_format == HEATKV_KV_FP4_E2M1   ? s->d / 2 + s->d / 32
+                  : s->kv_format == HEATKV_KV_FP8_E4M3 ? s->d
+                                                       : s->d * (s->dtype == HEATKV_F32 ? 4 : 2);
+  return size_t(s->num_pages) * s->page_size * s->kv_heads * row;
 }
 size_t table_bytes(const heatkv_paged_shape* s) { return size_t(s->batch) * s->max_pages * 4; }
 
@@ -261,7 +273,6 @@ int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const voi
   p.sm_scale = sm_scale;
   p.lse = lse;
   const auto hip_stream = static_cast<hipStream_t>(stream);
-  const bool fp8 = s->kv_format == HEATKV_KV_FP8_E4M3;
   hipError_t e = hipSuccess;
   // Makes one of the two launches; its parts, for the join.
   auto launch = [&](const heatkv::paged::Launch& l, const PartArrays& a, bool many) {
@@ -281,8 +292,8 @@ int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const voi
     p.whole_from = l.whole_from;
     p.parts = parts;
     e = s->dtype == HEATKV_F32 ? heatkv::launch_paged_attend_f32(p, s->d, hip_stream)
-        : many                 ? heatkv::launch_paged_attend_long(p, s->d, fp8, hip_stream)
-                               : heatkv::launch_paged_attend_bf16(p, s->d, fp8, hip_stream);
+        : many                 ? heatkv::launch_paged_attend_long(p, s->d, s->kv_format, hip_stream)
+                               : heatkv::launch_paged_attend_bf16(p, s->d, s->kv_format, hip_stream);
     parts.grid = heatkv::paged::join_workgroups(l);
     return parts;
   };
@@ -290,6 +301,92 @@ int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const voi
   if (e == hipSuccess && few.grid + many.grid > 0) e = heatkv::launch_paged_join(p, few, many, s->dtype, s->d, hip_stream);
   return launched(e, "paged_attend");
 }
+
+// Workspace of the calls on shared pages, each array from a multiple of 256 bytes on.  A workgroup of compact looks at `tile` tokens
+// of a row of the table: few enough that 256 of them are a row.
+struct TablesWorkspace {
+  size_t state, next, gone, per_row[5], counts, drops, total = 0;
+  int tile = 4096, tiles;
+};
+TablesWorkspace tables_workspace_of(const heatkv_paged_shape* s) {
+  TablesWorkspace w;
+  auto take = [&](size_t n) {
+    const size_t at = w.total;
+    w.total += (n + 255) / 256 * 256;
+    return at;
+  };
+  const int64_t longest = int64_t(s->max_pages) * s->page_size;
+  while ((longest + w.tile - 1) / w.tile > 256) w.tile *= 2;
+  w.tiles = int((longest + w.tile - 1) / w.tile);
+  w.state = take(64);
+  w.next = take(size_t(s->batch) * 4);
+  w.gone = take((size_t(s->num_pages) + 31) / 32 * 4);
+  for (size_t& at : w.per_row) at = take((size_t(s->batch) + 1) * 4);
+  w.counts = take(size_t(s->batch) * w.tiles * 4);
+  w.drops = take(size_t(s->batch) * w.tiles * 4);
+  return w;
+}
+
+// What the calls on shared pages have in common: their arrays, and how they are checked.
+struct Tables {
+  const heatkv_paged_shape* s;
+  const int32_t* lens;
+  int32_t *lens_out, *holders, *free_ring;
+  const int32_t* free_span;
+  int32_t *free_span_out, *table, *status;
+  void* ws;
+  size_t ws_bytes;
+  TablesWorkspace w{};
+
+  int check() {
+    if (int rc = check_shape(s)) return rc;
+    if (int64_t(s->batch) * s->max_pages > int64_t(1) << 30) return fail(HEATKV_EINVAL, "batch * max_pages must be at most 2^30");
+    if (int rc = check_ints({lens, lens_out, holders, free_ring, free_span, free_span_out, table, status})) return rc;
+    w = tables_workspace_of(s);
+    if (!ws || ws_bytes < w.total) return fail(HEATKV_EINVAL, "tables workspace too small");
+    if (!aligned(ws, 16)) return fail(HEATKV_EINVAL, "workspace must be 16-byte aligned");
+    return HEATKV_OK;
+  }
+  // `written`, `read`: the call's own arrays.
+  int check_apart_from(std::initializer_list<Span> written, std::initializer_list<Span> read) const {
+    const size_t row = size_t(s->batch) * 4;
+    if (lens_out != lens && overlap(lens_out, row, lens, row)) return fail(HEATKV_EINVAL, "lens_out overlaps lens in part");
+    if (free_span_out != free_span && overlap(free_span_out, 8, free_span, 8))
+      return fail(HEATKV_EINVAL, "free_span_out overlaps free_span in part");
+    Span all[24] = {span_of("lens_out", lens_out, row, WRITTEN), span_of("free_span_out", free_span_out, 8, WRITTEN),
+                    span_of("holders", holders, size_t(s->num_pages) * 4, WRITTEN),
+                    span_of("free_ring", free_ring, size_t(s->num_pages) * 4, WRITTEN),
+                    span_of("table", table, table_bytes(s), WRITTEN), span_of("status", status, 4, WRITTEN),
+                    span_of("ws", ws, w.total, WRITTEN)};
+    int n = 7;
+    for (const Span& x : written) all[n++] = x;
+    all[n++] = span_of("lens", lens, lens_out == lens ? 0 : row, READ);
+    all[n++] = span_of("free_span", free_span, free_span_out == free_span ? 0 : 8, READ);
+    for (const Span& x : read) all[n++] = x;
+    return check_disjoint(all, all + n);
+  }
+  template <class X>
+  X* at(size_t offset) const { return reinterpret_cast<X*>(static_cast<char*>(ws) + offset); }
+  heatkv::TableArgs args() const {
+    heatkv::TableArgs t{};
+    t.batch = s->batch;
+    t.num_pages = s->num_pages;
+    t.max_pages = s->max_pages;
+    t.page_log2 = log2_of(s->page_size);
+    t.lens = lens;
+    t.span = free_span;
+    t.lens_out = lens_out;
+    t.span_out = free_span_out;
+    t.holders = holders;
+    t.ring = free_ring;
+    t.table = table;
+    t.status = status;
+    t.state = at<int32_t>(w.state);
+    t.next = at<int32_t>(w.next);
+    t.gone = at<uint32_t>(w.gone);
+    return t;
+  }
+};
 
 }  // namespace
 
@@ -346,9 +443,7 @@ int heatkv_paged_append(const heatkv_paged_shape* s, const int32_t* slots, int64
   if (!rc) rc = check_rows(s, v_new, "v_new");
   if (!rc) rc = check_cache(k_pages, v_pages);
   if (rc) return rc;
-  if ((bounds == nullptr) != (bound_scales == nullptr)) return fail(HEATKV_EINVAL, "bounds and bound_scales go together");
-  if (bounds && (!aligned(bounds, 16) || !aligned(bound_scales, 4)))
-    return fail(HEATKV_EINVAL, "bounds must be 16-byte aligned, bound_scales 4-byte");
+  if ((rc = check_bounds(bounds, bound_scales))) return rc;
   const size_t pages_heads = size_t(s->num_pages) * s->kv_heads;
   const Span bounds_span = span_of("bounds", bounds, pages_heads * 2 * s->d, WRITTEN),
              scales_span = span_of("bound_scales", bound_scales, pages_heads * 4, WRITTEN);
@@ -365,7 +460,7 @@ int heatkv_paged_append(const heatkv_paged_shape* s, const int32_t* slots, int64
   a.H = s->kv_heads;
   a.page_log2 = log2_of(s->page_size);
   a.num_pages = s->num_pages;
-  a.kv_fp8 = s->kv_format == HEATKV_KV_FP8_E4M3;
+  a.kv_format = s->kv_format;
   a.tokens = tokens;
   a.slots = slots;
   a.k_new = k_new.data;
@@ -441,6 +536,152 @@ int heatkv_paged_attend_selected(const heatkv_paged_shape* s, int64_t tokens, he
   if (tokens != 0 && (rc = check_ints({selected}))) return rc;
   return attend(s, tokens, q, k_pages, v_pages, table, q_start, lens, selected, top, sm_scale, causal, out, lse, ws, ws_bytes,
                 stream);
+}
+
+int heatkv_paged_move(const heatkv_paged_shape* s, const int32_t* move_from, const int32_t* move_to, int64_t rows, void* k_pages,
+                      void* v_pages, int8_t* bounds, float* bound_scales, void* stream) {
+  int rc = check_shape(s);
+  if (!rc) rc = check_tokens(s, rows);
+  if (rc || rows == 0) return rc;
+  rc = check_ints({move_from, move_to});
+  if (!rc) rc = check_cache(k_pages, v_pages);
+  if (!rc) rc = check_bounds(bounds, bound_scales);
+  if (rc) return rc;
+  const size_t pages_heads = size_t(s->num_pages) * s->kv_heads, list = size_t(rows) * 4;
+  rc = check_disjoint({span_of("k_pages", k_pages, pages_bytes(s), WRITTEN), span_of("v_pages", v_pages, pages_bytes(s), WRITTEN),
+                       span_of("bounds", bounds, pages_heads * 2 * s->d, WRITTEN),
+                       span_of("bound_scales", bound_scales, pages_heads * 4, WRITTEN), span_of("move_from", move_from, list, READ),
+                       span_of("move_to", move_to, list, READ)});
+  if (rc) return rc;
+  heatkv::PagedAppendArgs a{};
+  a.dtype = s->dtype;
+  a.d = s->d;
+  a.H = s->kv_heads;
+  a.page_log2 = log2_of(s->page_size);
+  a.num_pages = s->num_pages;
+  a.kv_format = s->kv_format;
+  a.tokens = rows;
+  a.slots = move_to;
+  a.from = move_from;
+  a.k_pages = k_pages;
+  a.v_pages = v_pages;
+  a.bounds = bounds;
+  a.bound_scales = bound_scales;
+  return launched(heatkv::launch_paged_append(a, static_cast<hipStream_t>(stream)), "paged_move");
+}
+
+int heatkv_paged_read(const heatkv_paged_shape* s, const int32_t* slots, int64_t tokens, const void* k_pages, const void* v_pages,
+                      heatkv_rows k_out, heatkv_rows v_out, void* stream) {
+  int rc = check_shape(s);
+  if (!rc) rc = check_tokens(s, tokens);
+  if (rc || tokens == 0) return rc;
+  rc = check_ints({slots});
+  if (!rc) rc = check_cache(k_pages, v_pages);
+  if (!rc) rc = check_rows(s, k_out, "k_out");
+  if (!rc) rc = check_rows(s, v_out, "v_out");
+  if (!rc) rc = check_apart(s, tokens, s->kv_heads, k_out, "k_out");
+  if (!rc) rc = check_apart(s, tokens, s->kv_heads, v_out, "v_out");
+  if (rc) return rc;
+  for (const Span& out : {span_of("k_out", s, k_out, tokens, s->kv_heads, WRITTEN), span_of("v_out", s, v_out, tokens, s->kv_heads, WRITTEN)}) {
+    rc = check_disjoint({out, span_of("k_pages", k_pages, pages_bytes(s), READ), span_of("v_pages", v_pages, pages_bytes(s), READ),
+                         span_of("slots", slots, size_t(tokens) * 4, READ)});
+    if (rc) return rc;
+  }
+  if (rows_meet(s, k_out, v_out, tokens, s->kv_heads)) return fail(HEATKV_EINVAL, "k_out overlaps v_out");
+  heatkv::PagedReadArgs a{};
+  a.dtype = s->dtype;
+  a.d = s->d;
+  a.H = s->kv_heads;
+  a.page_log2 = log2_of(s->page_size);
+  a.num_pages = s->num_pages;
+  a.kv_format = s->kv_format;
+  a.tokens = tokens;
+  a.slots = slots;
+  a.k_pages = k_pages;
+  a.v_pages = v_pages;
+  a.k_out = k_out.data;
+  a.v_out = v_out.data;
+  a.k_token_stride = k_out.token_stride;
+  a.k_head_stride = k_out.head_stride;
+  a.v_token_stride = v_out.token_stride;
+  a.v_head_stride = v_out.head_stride;
+  return launched(heatkv::launch_paged_read(a, static_cast<hipStream_t>(stream)), "paged_read");
+}
+
+size_t heatkv_paged_tables_workspace_bytes(const heatkv_paged_shape* s) { return check_shape(s) ? 0 : tables_workspace_of(s).total; }
+
+int heatkv_paged_fork(const heatkv_paged_shape* s, const int32_t* parent, const int32_t* lens, int32_t* lens_out, int32_t* holders,
+                      int32_t* free_ring, const int32_t* free_span, int32_t* free_span_out, int32_t* table, int32_t* status,
+                      void* ws, size_t ws_bytes, void* stream) {
+  Tables t{s, lens, lens_out, holders, free_ring, free_span, free_span_out, table, status, ws, ws_bytes};
+  int rc = t.check();
+  if (!rc) rc = check_ints({parent});
+  if (!rc) rc = t.check_apart_from({}, {span_of("parent", parent, size_t(s->batch) * 4, READ)});
+  if (rc) return rc;
+  heatkv::ForkArgs f{};
+  f.t = t.args();
+  f.parent = parent;
+  return launched(heatkv::launch_paged_fork(f, static_cast<hipStream_t>(stream)), "paged_fork");
+}
+
+int heatkv_paged_assign_shared(const heatkv_paged_shape* s, const int32_t* keep, const int32_t* new_tokens, const int32_t* lens,
+                               int32_t* lens_out, int32_t* holders, int32_t* free_ring, const int32_t* free_span,
+                               int32_t* free_span_out, int32_t* table, int32_t* q_start, int32_t* slots, int64_t max_tokens,
+                               int32_t* copy_from, int32_t* copy_to, int32_t* status, void* ws, size_t ws_bytes, void* stream) {
+  Tables t{s, lens, lens_out, holders, free_ring, free_span, free_span_out, table, status, ws, ws_bytes};
+  int rc = t.check();
+  if (!rc) rc = check_tokens(max_tokens);
+  if (!rc) rc = check_ints({keep, new_tokens, q_start, copy_from, copy_to});
+  if (!rc && max_tokens > 0) rc = check_ints({slots});
+  if (rc) return rc;
+  const size_t row = size_t(s->batch) * 4, copies = row * s->page_size;
+  rc = t.check_apart_from({span_of("q_start", q_start, row + 4, WRITTEN), span_of("slots", slots, size_t(max_tokens) * 4, WRITTEN),
+                           span_of("copy_from", copy_from, copies, WRITTEN), span_of("copy_to", copy_to, copies, WRITTEN)},
+                          {span_of("keep", keep, row, READ), span_of("new_tokens", new_tokens, row, READ)});
+  if (rc) return rc;
+  heatkv::AssignSharedArgs a{};
+  a.t = t.args();
+  a.keep = keep;
+  a.new_tokens = new_tokens;
+  a.q_start = q_start;
+  a.slots = slots;
+  a.copy_from = copy_from;
+  a.copy_to = copy_to;
+  a.max_tokens = max_tokens;
+  a.take0 = t.at<int32_t>(t.w.per_row[0]);
+  a.touch0 = t.at<int32_t>(t.w.per_row[1]);
+  a.first = t.at<int32_t>(t.w.per_row[2]);
+  a.copied = t.at<int32_t>(t.w.per_row[3]);
+  return launched(heatkv::launch_paged_assign_shared(a, static_cast<hipStream_t>(stream)), "paged_assign_shared");
+}
+
+int heatkv_paged_compact(const heatkv_paged_shape* s, const uint8_t* kept, const int32_t* lens, int32_t* lens_out, int32_t* holders,
+                         int32_t* free_ring, const int32_t* free_span, int32_t* free_span_out, int32_t* table, int32_t* move_from,
+                         int32_t* move_to, int64_t max_moves, int32_t* status, void* ws, size_t ws_bytes, void* stream) {
+  Tables t{s, lens, lens_out, holders, free_ring, free_span, free_span_out, table, status, ws, ws_bytes};
+  int rc = t.check();
+  if (!rc) rc = check_tokens(max_moves);
+  if (!rc && max_moves > 0) rc = check_ints({move_from, move_to});
+  if (rc) return rc;
+  if (!kept || !aligned(kept, 16)) return fail(HEATKV_EINVAL, "kept must be 16-byte aligned and not null");
+  const size_t list = size_t(max_moves) * 4;
+  rc = t.check_apart_from({span_of("move_from", move_from, list, WRITTEN), span_of("move_to", move_to, list, WRITTEN)},
+                          {span_of("kept", kept, size_t(s->batch) * s->max_pages * s->page_size, READ)});
+  if (rc) return rc;
+  heatkv::CompactArgs a{};
+  a.t = t.args();
+  a.kept = kept;
+  a.move_from = move_from;
+  a.move_to = move_to;
+  a.max_moves = max_moves;
+  a.tile = t.w.tile;
+  a.tiles = t.w.tiles;
+  a.take0 = t.at<int32_t>(t.w.per_row[0]);
+  a.move0 = t.at<int32_t>(t.w.per_row[1]);
+  a.first = t.at<int32_t>(t.w.per_row[2]);
+  a.counts = t.at<int32_t>(t.w.counts);
+  a.drops = t.at<int32_t>(t.w.drops);
+  return launched(heatkv::launch_paged_compact(a, static_cast<hipStream_t>(stream)), "paged_compact");
 }
 
 }  // extern "C"

@@ -20,6 +20,11 @@ namespace heatkv {
 
 namespace {
 
+using paged::E2M1;
+using paged::E4M3;
+using paged::Format;
+using paged::NATIVE;
+
 constexpr int LANES = 256;
 // Tokens x heads up to which a workgroup takes a page, so that its rows are read by 256 lanes; a wavefront beyond.  A token each,
 // 8 heads, pages of 16, 64, 256 rows: 32 requests 4.5, 4.8, 6.7 us by workgroups, 4.7, 5.4, 10.4 by wavefronts; 128 requests
@@ -42,53 +47,147 @@ __device__ __forceinline__ void values8(const uint4 (&raw)[sizeof(T) / 2], float
     }
   }
 }
-__device__ __forceinline__ void decode8(uint2 w, float (&x)[8]) {  // E4M3 codes
+
+// 4-bit rows.  8 channels of a row are a lane's, so a block of 32 is four lanes next to one another, which are always all at work.
+__device__ __forceinline__ unsigned max_of_four(unsigned x) {
+  auto swapped = [](unsigned y, auto control) {
+    return static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(y), decltype(control)::value, 0xf, 0xf, true));
+  };
+  x = max(x, swapped(x, std::integral_constant<int, 0xb1>{}));  // lanes 1, 0, 3, 2
+  return max(x, swapped(x, std::integral_constant<int, 0x4e>{}));  // lanes 2, 3, 0, 1
+}
+// Codes of 8 bf16 values and the scale byte of their block: the power of two 2^e with the least e that the largest magnitude
+// fits 7 times (it is then rounded by half a step at most, as the others are), -100 <= e <= 125; 255 if there is a NaN.
+// The bits of a magnitude (1 + m / 128) 2^x are 128 (x + 127) + m: e = x - 2 up to m = 96, x - 1 beyond.
+__device__ __forceinline__ uint2 nibbles_of(const uint4& raw) {
+  const unsigned w[4] = {raw.x, raw.y, raw.z, raw.w};
+  unsigned most = 0;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int c = static_cast<int>(i ? w.y : w.x);
-    x[4 * i] = __builtin_amdgcn_cvt_f32_fp8(c, 0);
-    x[4 * i + 1] = __builtin_amdgcn_cvt_f32_fp8(c, 1);
-    x[4 * i + 2] = __builtin_amdgcn_cvt_f32_fp8(c, 2);
-    x[4 * i + 3] = __builtin_amdgcn_cvt_f32_fp8(c, 3);
+  for (int i = 0; i < 4; ++i) most = max(most, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
+  most = max_of_four(most);
+  const int byte = most > 0x7f80u ? 255 : min(max(static_cast<int>((most + 31) >> 7) - 2, 27), 252);
+  const float scale = paged::scale_of(byte);
+  unsigned c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[0]), scale, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[1]), scale, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[2]), scale, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[3]), scale, 3);
+  return make_uint2(c, byte);
+}
+
+// 8 values of a cache row as it is stored: raw[0].x, .y for 8 codes of 8 bits, for 8 of 4 bits and their scale byte.  `at`: row
+// of the cache * D + column.
+template <class T, Format F, int D>
+struct CacheEight {
+  static constexpr int N = sizeof(T) / 2;
+  uint4 raw[N];
+  struct Nibbles {
+    long long codes, scale;
+  };
+  static __device__ __forceinline__ Nibbles nibbles_at(long long at) {
+    const int r = static_cast<int>(at / D) & 15, col = static_cast<int>(at) & (D - 1);
+    const long long granule = at / (16 * D) * (16 * paged::row_bytes<T, F>(D));
+    return {granule + r * (D / 2) + col / 2, granule + 8 * D + r * (D / 32) + col / 32};
   }
+  __device__ __forceinline__ void load(const void* pages, long long at) {
+    if constexpr (F == E2M1) {
+      const Nibbles n = nibbles_at(at);
+      raw[0].x = *reinterpret_cast<const unsigned*>(static_cast<const char*>(pages) + n.codes);
+      raw[0].y = static_cast<const unsigned char*>(pages)[n.scale];
+    } else if constexpr (F == E4M3) {
+      const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const char*>(pages) + at);
+      raw[0].x = w.x;
+      raw[0].y = w.y;
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) raw[j] = ldg16(static_cast<const T*>(pages) + at + 4 * j);
+    }
+  }
+  __device__ __forceinline__ void store(void* pages, long long at) const {
+    if constexpr (F == E2M1) {
+      const Nibbles n = nibbles_at(at);
+      *reinterpret_cast<unsigned*>(static_cast<char*>(pages) + n.codes) = raw[0].x;
+      if ((at & 31) == 0) static_cast<unsigned char*>(pages)[n.scale] = static_cast<unsigned char>(raw[0].y);
+    } else if constexpr (F == E4M3) {
+      *reinterpret_cast<uint2*>(static_cast<char*>(pages) + at) = make_uint2(raw[0].x, raw[0].y);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) *reinterpret_cast<uint4*>(static_cast<T*>(pages) + at + 4 * j) = raw[j];
+    }
+  }
+  // From values as the operands have them.
+  __device__ __forceinline__ void encode() {
+    if constexpr (F == E2M1) {
+      const uint2 c = nibbles_of(raw[0]);
+      raw[0].x = c.x;
+      raw[0].y = c.y;
+    } else if constexpr (F == E4M3) {
+      const uint2 c = make_uint2(bf16x4_to_e4m3(raw[0].x, raw[0].y), bf16x4_to_e4m3(raw[0].z, raw[0].w));
+      raw[0].x = c.x;
+      raw[0].y = c.y;
+    }
+  }
+  // The values, as the operands have them.
+  __device__ __forceinline__ void decode(uint4 (&x)[N]) const {
+    if constexpr (F == E2M1)
+      x[0] = __builtin_bit_cast(uint4, paged::nibbles_to_bf16(raw[0].x, paged::scale_of(raw[0].y)));
+    else if constexpr (F == E4M3)
+      x[0] = __builtin_bit_cast(uint4, paged::codes_to_bf16(raw[0].x, raw[0].y));
+    else
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] = raw[j];
+  }
+};
+
+// Where new rows come from: the caller's token tensors, in the operands' type, or (MOVE) other rows of the cache, as they are.
+// Row t of the call, head h, columns col .. col + 7.
+template <class T, Format F, int D, bool MOVE>
+__device__ __forceinline__ void fetch_new(const PagedAppendArgs& p, long long t, int h, int col, CacheEight<T, F, D>& k,
+                                          CacheEight<T, F, D>& v) {
+  if constexpr (MOVE) {
+    const unsigned slot = min(static_cast<unsigned>(p.from[t]), static_cast<unsigned>((p.num_pages << p.page_log2) - 1));
+    const long long at = (((static_cast<long long>(slot >> p.page_log2) * p.H + h) << p.page_log2) +
+                          (slot & ((1u << p.page_log2) - 1))) * D + col;
+    k.load(p.k_pages, at);
+    v.load(p.v_pages, at);
+  } else {
+    const T* kp = static_cast<const T*>(p.k_new) + t * p.k_token_stride + h * p.k_head_stride + col;
+    const T* vp = static_cast<const T*>(p.v_new) + t * p.v_token_stride + h * p.v_head_stride + col;
+#pragma unroll
+    for (int j = 0; j < static_cast<int>(sizeof(T)) / 2; ++j) {
+      k.raw[j] = ldg16(kp + 4 * j);
+      v.raw[j] = ldg16(vp + 4 * j);
+    }
+  }
+}
+// Into the cache; k is what the cache then holds.
+template <bool MOVE, class Eight>
+__device__ __forceinline__ void write_row(const PagedAppendArgs& p, long long at, Eight& k, Eight& v) {
+  if constexpr (!MOVE) {
+    k.encode();
+    v.encode();
+  }
+  k.store(p.k_pages, at);
+  v.store(p.v_pages, at);
 }
 
 // Rows only: 8 elements of K and of V per lane.
-template <class T, bool FP8>
+template <class T, Format F, int D, bool MOVE>
 __global__ __launch_bounds__(LANES) void paged_append_kernel(PagedAppendArgs p) {
-  const int cpr = p.d / 8;
+  constexpr int COLS = D / 8;
   const long long i = static_cast<long long>(blockIdx.x) * LANES + threadIdx.x;
-  const int c = static_cast<int>(i & (cpr - 1));
-  const long long row = p.d == 128 ? i >> 4 : i >> 3;
+  const int c = static_cast<int>(i & (COLS - 1));
+  const long long row = i / COLS;
   const long long t = row / p.H;
   const int h = static_cast<int>(row - t * p.H);
   if (t >= p.tokens) return;
   const int slot = p.slots[t];
   if (slot < 0 || slot >= p.num_pages << p.page_log2) return;
-  const T* k = static_cast<const T*>(p.k_new) + t * p.k_token_stride + h * p.k_head_stride + 8 * c;
-  const T* v = static_cast<const T*>(p.v_new) + t * p.v_token_stride + h * p.v_head_stride + 8 * c;
   const long long to = ((((static_cast<long long>(slot >> p.page_log2) * p.H + h) << p.page_log2) +
-                         (slot & ((1 << p.page_log2) - 1))) * p.d + 8 * c);
-  if constexpr (FP8) {
-    const uint4 a = ldg16(k), b = ldg16(v);
-    *reinterpret_cast<uint2*>(static_cast<char*>(p.k_pages) + to) = make_uint2(bf16x4_to_e4m3(a.x, a.y), bf16x4_to_e4m3(a.z, a.w));
-    *reinterpret_cast<uint2*>(static_cast<char*>(p.v_pages) + to) = make_uint2(bf16x4_to_e4m3(b.x, b.y), bf16x4_to_e4m3(b.z, b.w));
-  } else {
-    uint4* kd = reinterpret_cast<uint4*>(static_cast<T*>(p.k_pages) + to);
-    uint4* vd = reinterpret_cast<uint4*>(static_cast<T*>(p.v_pages) + to);
-    constexpr int N = sizeof(T) / 2;
-    uint4 a[N], b[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      a[j] = ldg16(k + 4 * j);
-      b[j] = ldg16(v + 4 * j);
-    }
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      kd[j] = a[j];
-      vd[j] = b[j];
-    }
-  }
+                         (slot & ((1 << p.page_log2) - 1))) * D + 8 * c);
+  CacheEight<T, F, D> k, v;
+  fetch_new<T, F, D, MOVE>(p, t, h, 8 * c, k, v);
+  write_row<MOVE>(p, to, k, v);
 }
 
 // The first token of a call on a page is that page's owner: who has it forms the bounds over the rows up to the last one that
@@ -214,71 +313,26 @@ __device__ __forceinline__ void fold_rows(float (&top)[8], float (&low)[8]) {  /
       low[i] = fmaxf(low[i], __shfl_xor(low[i], m, 64));
     }
 }
-// 8 values of a cache row.
-template <class T, bool FP8>
-struct CacheEight {
-  uint4 raw[sizeof(T) / 2];
-  __device__ __forceinline__ void load(const void* pages, long long at) {
-    if constexpr (FP8) {
-      const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const char*>(pages) + at);
-      raw[0].x = w.x;
-      raw[0].y = w.y;
-    } else {
-#pragma unroll
-      for (int j = 0; j < static_cast<int>(sizeof(T)) / 2; ++j) raw[j] = ldg16(static_cast<const T*>(pages) + at + 4 * j);
-    }
-  }
-  __device__ __forceinline__ void values(float (&x)[8]) const {
-    if constexpr (FP8)
-      decode8(make_uint2(raw[0].x, raw[0].y), x);
-    else
-      values8<T>(raw, x);
-  }
-  __device__ __forceinline__ void add_to(Extremes<T>& e) const {
-    if constexpr (FP8) {
-      auto pair = [](unsigned w, bool high) {
-        const int c = static_cast<int>(w);
-        return __builtin_bit_cast(unsigned, high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, 1.0f, true)
-                                                 : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, 1.0f, false));
-      };
-      const uint4 w[1] = {make_uint4(pair(raw[0].x, false), pair(raw[0].x, true), pair(raw[0].y, false), pair(raw[0].y, true))};
-      e.add(w);
-    } else {
-      e.add(raw);
-    }
-  }
-};
-// 8 values of K and V of a new row into the cache; k is what the cache then holds.
-template <class T, bool FP8>
-__device__ __forceinline__ void write_row(const PagedAppendArgs& p, long long at, CacheEight<T, FP8>& k,
-                                          const uint4 (&v)[sizeof(T) / 2]) {
-  if constexpr (FP8) {
-    auto codes = [](const uint4& x) { return make_uint2(bf16x4_to_e4m3(x.x, x.y), bf16x4_to_e4m3(x.z, x.w)); };
-    const uint2 c = codes(k.raw[0]);
-    *reinterpret_cast<uint2*>(static_cast<char*>(p.k_pages) + at) = c;
-    *reinterpret_cast<uint2*>(static_cast<char*>(p.v_pages) + at) = codes(v[0]);
-    k.raw[0].x = c.x;
-    k.raw[0].y = c.y;
-  } else {
-#pragma unroll
-    for (int j = 0; j < static_cast<int>(sizeof(T)) / 2; ++j) {
-      *reinterpret_cast<uint4*>(static_cast<T*>(p.k_pages) + at + 4 * j) = k.raw[j];
-      *reinterpret_cast<uint4*>(static_cast<T*>(p.v_pages) + at + 4 * j) = v[j];
-    }
-  }
+template <class T, Format F, int D>
+__device__ __forceinline__ void add_to(Extremes<T>& e, const CacheEight<T, F, D>& x) {
+  uint4 w[sizeof(T) / 2];
+  x.decode(w);
+  e.add(w);
 }
 // The rare case: rows [r0, rows) in steps of `step`, one by one, from the cache.
-template <class T, bool FP8, int D>
+template <class T, Format F, int D>
 __device__ __forceinline__ void fold_with_nan(const void* pages, long long base, int r0, int step, int rows, float (&top)[8],
                                               float (&low)[8]) {
   float t[8], l[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) t[i] = l[i] = -INFINITY;
   for (int r = r0; r < rows; r += step) {
-    CacheEight<T, FP8> k;
+    CacheEight<T, F, D> k;
     k.load(pages, base + r * D);
+    uint4 raw[sizeof(T) / 2];
+    k.decode(raw);
     float x[8];
-    k.values(x);
+    values8<T>(raw, x);
     fold(x, t, l);
   }
 #pragma unroll
@@ -289,11 +343,10 @@ __device__ __forceinline__ void fold_with_nan(const void* pages, long long base,
 }
 
 // Few pages: a workgroup per token and head; those that own a page write its new rows and read the older ones.
-template <class T, bool FP8, int D>
+template <class T, Format F, int D, bool MOVE>
 __global__ __launch_bounds__(LANES) void paged_append_bounds_kernel(PagedAppendArgs p) {
   constexpr int COLS = D / 8, ROWS = LANES / COLS;  // lanes of a row, rows side by side
   constexpr int U = 4;                              // rows of a lane whose loads are under way together
-  constexpr int N = sizeof(T) / 2;                  // 16-byte pieces of 8 values
   __shared__ float part[LANES / 64][2][D];
   __shared__ int run_end[LANES / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -313,38 +366,31 @@ __global__ __launch_bounds__(LANES) void paged_append_bounds_kernel(PagedAppendA
   for (int w = 0; w < LANES / 64; ++w) n = min(n, run_end[w]);
   const int rows = o0 + n, col = (tid % COLS) * 8, r0 = tid / COLS;
   const long long at = static_cast<long long>(s0 >> lp) * p.H + h, base = (at << lp) * D + col;
-  const T* k_new = static_cast<const T*>(p.k_new) + h * p.k_head_stride + col;
-  const T* v_new = static_cast<const T*>(p.v_new) + h * p.v_head_stride + col;
   Extremes<T> seen;
   for (int first = r0; first < rows; first += ROWS * U) {
-    CacheEight<T, FP8> k[U];
-    uint4 v[U][N];
+    CacheEight<T, F, D> k[U], v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int r = first + ROWS * u;
       if (r >= rows) continue;
-      if (r < o0) {
+      if (r < o0)
         k[u].load(p.k_pages, base + r * D);
-      } else {
-        const T* kp = k_new + (t + r - o0) * p.k_token_stride;
-        const T* vp = v_new + (t + r - o0) * p.v_token_stride;
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          k[u].raw[j] = ldg16(kp + 4 * j);
-          v[u][j] = ldg16(vp + 4 * j);
-        }
-      }
+      else
+        fetch_new<T, F, D, MOVE>(p, t + r - o0, h, col, k[u], v[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int r = first + ROWS * u;
       if (r >= rows) continue;
-      if (r >= o0) write_row<T, FP8>(p, base + r * D, k[u], v[u]);
-      k[u].add_to(seen);
+      if (r >= o0) write_row<MOVE>(p, base + r * D, k[u], v[u]);
+      add_to(seen, k[u]);
     }
   }
   float top[8], low[8];
-  if (seen.finish(top, low)) fold_with_nan<T, FP8, D>(p.k_pages, base, r0, ROWS, rows, top, low);  // its own rows, written above
+  if (seen.finish(top, low)) {
+    if constexpr (F == E2M1) __threadfence_block();  // scale bytes that the lane next to it has written
+    fold_with_nan<T, F, D>(p.k_pages, base, r0, ROWS, rows, top, low);  // its own rows, written above
+  }
   fold_rows<COLS>(top, low);
   if (lane < COLS)
 #pragma unroll
@@ -367,9 +413,9 @@ __global__ __launch_bounds__(LANES) void paged_append_bounds_kernel(PagedAppendA
 // Many pages: a wavefront per page, without barriers.  It looks for owners among `chunk` tokens (at most 64) of one kv head, and
 // its first rows are under way before it knows how many count.  Rows first and the bounds by a second launch, which reads them
 // back, took 13.5 + 13 us; this takes 21.
-template <class T, bool FP8, int D>
+template <class T, Format F, int D, bool MOVE>
 __global__ __launch_bounds__(LANES) void paged_append_pages_kernel(PagedAppendArgs p, int chunk) {
-  constexpr int COLS = D / 8, ROWS = 64 / COLS, U = 4, N = sizeof(T) / 2;
+  constexpr int COLS = D / 8, ROWS = 64 / COLS, U = 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // the heads of a token next to one another: their rows are neighbours in memory
   const int group = blockIdx.x / p.H, h = blockIdx.x - group * p.H, lp = p.page_log2, page = 1 << lp;
@@ -388,22 +434,14 @@ __global__ __launch_bounds__(LANES) void paged_append_pages_kernel(PagedAppendAr
     const long long t = t0 + own;
     const int s0 = __builtin_amdgcn_readlane(mine, own), o0 = s0 & (page - 1);
     const long long at = static_cast<long long>(s0 >> lp) * p.H + h, base = (at << lp) * D + col;
-    const T* k_new = static_cast<const T*>(p.k_new) + h * p.k_head_stride + col;
-    const T* v_new = static_cast<const T*>(p.v_new) + h * p.v_head_stride + col;
     // New row i is row o0 + i of the page.
-    CacheEight<T, FP8> k[U];
-    uint4 v[U][N];
+    CacheEight<T, F, D> k[U], v[U];
     const long long left = min(p.tokens - t, static_cast<long long>(page - o0));
     auto fetch = [&](int first) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int i = first + ROWS * u + r0;
-        if (i >= left) continue;
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          k[u].raw[j] = ldg16(k_new + (t + i) * p.k_token_stride + 4 * j);
-          v[u][j] = ldg16(v_new + (t + i) * p.v_token_stride + 4 * j);
-        }
+        if (i < left) fetch_new<T, F, D, MOVE>(p, t + i, h, col, k[u], v[u]);
       }
     };
     fetch(0);
@@ -419,48 +457,46 @@ __global__ __launch_bounds__(LANES) void paged_append_pages_kernel(PagedAppendAr
       for (int u = 0; u < U; ++u) {
         const int i = first + ROWS * u + r0;
         if (i >= n) continue;
-        write_row<T, FP8>(p, base + (o0 + i) * D, k[u], v[u]);
-        k[u].add_to(seen);
+        write_row<MOVE>(p, base + (o0 + i) * D, k[u], v[u]);
+        add_to(seen, k[u]);
       }
     }
     for (int first = r0; first < o0; first += ROWS * U) {  // older rows
-      CacheEight<T, FP8> old[U];
+      CacheEight<T, F, D> old[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) old[u].load(p.k_pages, base + min(first + ROWS * u, o0 - 1) * D);  // some of them twice
 #pragma unroll
-      for (int u = 0; u < U; ++u) old[u].add_to(seen);
+      for (int u = 0; u < U; ++u) add_to(seen, old[u]);
     }
     const int rows = o0 + n;
     float top[8], low[8];
     if (__any(seen.finish(top, low))) {
       __threadfence_block();  // rows that other lanes have written
-      fold_with_nan<T, FP8, D>(p.k_pages, base, r0, ROWS, rows, top, low);
+      fold_with_nan<T, F, D>(p.k_pages, base, r0, ROWS, rows, top, low);
     }
     fold_rows<COLS>(top, low);
     store_bounds<D>(p, at, lane, top, low);
   }
 }
 
-template <class T, bool FP8>
+template <class T, Format F, bool MOVE>
 hipError_t launch(const PagedAppendArgs& a, hipStream_t stream) {
   const long long units = a.tokens * a.H;  // pages that the call can touch, times heads
-  if (!a.bounds) {
-    const long long lanes = units * (a.d / 8);
-    hipLaunchKernelGGL((paged_append_kernel<T, FP8>), dim3(static_cast<unsigned>((lanes + LANES - 1) / LANES)), dim3(LANES), 0,
-                       stream, a);
-    return hipGetLastError();
-  }
   auto run = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    if (units <= FEW_PAGES) {
-      hipLaunchKernelGGL((paged_append_bounds_kernel<T, FP8, D>), dim3(static_cast<unsigned>(units)), dim3(LANES), 0, stream, a);
+    if (!a.bounds) {
+      const long long lanes = units * (D / 8);
+      hipLaunchKernelGGL((paged_append_kernel<T, F, D, MOVE>), dim3(static_cast<unsigned>((lanes + LANES - 1) / LANES)), dim3(LANES), 0,
+                         stream, a);
+    } else if (units <= FEW_PAGES) {
+      hipLaunchKernelGGL((paged_append_bounds_kernel<T, F, D, MOVE>), dim3(static_cast<unsigned>(units)), dim3(LANES), 0, stream, a);
     } else {
       // About one owner to a wavefront: one without costs its start, one with two takes twice the chain.  12 prompts, 12000
       // tokens, 8 heads, d = 128, 8-bit pages, chunks of 12, 24, 48: pages of 16 22.3, 22.6, 25.8 us, of 32 25.1, 21.0, 23.7, of 64
       // 24.8, 21.4, 25.2 (22.8 with the 46 that they get here).
       const int chunk = static_cast<int>(std::min<long long>(std::max<long long>(units / 2048, 1), std::min(64, 3 << a.page_log2 >> 2)));
       const long long groups = (a.tokens + chunk * (LANES / 64) - 1) / (chunk * (LANES / 64));
-      hipLaunchKernelGGL((paged_append_pages_kernel<T, FP8, D>), dim3(static_cast<unsigned>(groups * a.H)), dim3(LANES), 0, stream, a, chunk);
+      hipLaunchKernelGGL((paged_append_pages_kernel<T, F, D, MOVE>), dim3(static_cast<unsigned>(groups * a.H)), dim3(LANES), 0, stream, a, chunk);
     }
   };
   if (a.d == 128)
@@ -470,12 +506,67 @@ hipError_t launch(const PagedAppendArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+template <bool MOVE>
+hipError_t launch(const PagedAppendArgs& a, hipStream_t stream) {
+  if (a.tokens == 0) return hipSuccess;
+  if (a.dtype == HEATKV_F32) return launch<float, NATIVE, MOVE>(a, stream);
+  return a.kv_format == HEATKV_KV_FP4_E2M1   ? launch<bf16_t, E2M1, MOVE>(a, stream)
+         : a.kv_format == HEATKV_KV_FP8_E4M3 ? launch<bf16_t, E4M3, MOVE>(a, stream)
+                                             : launch<bf16_t, NATIVE, MOVE>(a, stream);
+}
+
+// The other way: rows of the cache by their slots, as values of the operands' type.
+template <class T, Format F, int D>
+__global__ __launch_bounds__(LANES) void paged_read_kernel(PagedReadArgs p) {
+  constexpr int COLS = D / 8;
+  const long long i = static_cast<long long>(blockIdx.x) * LANES + threadIdx.x;
+  const int c = static_cast<int>(i & (COLS - 1));
+  const long long row = i / COLS;
+  const long long t = row / p.H;
+  const int h = static_cast<int>(row - t * p.H);
+  if (t >= p.tokens) return;
+  const int slot = p.slots[t];
+  if (slot < 0 || slot >= p.num_pages << p.page_log2) return;
+  const long long at = ((((static_cast<long long>(slot >> p.page_log2) * p.H + h) << p.page_log2) +
+                         (slot & ((1 << p.page_log2) - 1))) * D + 8 * c);
+  CacheEight<T, F, D> k, v;
+  k.load(p.k_pages, at);
+  v.load(p.v_pages, at);
+  uint4 x[sizeof(T) / 2], y[sizeof(T) / 2];
+  k.decode(x);
+  v.decode(y);
+  T* ko = static_cast<T*>(p.k_out) + t * p.k_token_stride + h * p.k_head_stride + 8 * c;
+  T* vo = static_cast<T*>(p.v_out) + t * p.v_token_stride + h * p.v_head_stride + 8 * c;
+#pragma unroll
+  for (int j = 0; j < static_cast<int>(sizeof(T)) / 2; ++j) {
+    *reinterpret_cast<uint4*>(ko + 4 * j) = x[j];
+    *reinterpret_cast<uint4*>(vo + 4 * j) = y[j];
+  }
+}
+
+template <class T, Format F>
+hipError_t launch_read(const PagedReadArgs& a, hipStream_t stream) {
+  const long long lanes = a.tokens * a.H * (a.d / 8);
+  const dim3 grid(static_cast<unsigned>((lanes + LANES - 1) / LANES));
+  if (a.d == 128)
+    hipLaunchKernelGGL((paged_read_kernel<T, F, 128>), grid, dim3(LANES), 0, stream, a);
+  else
+    hipLaunchKernelGGL((paged_read_kernel<T, F, 64>), grid, dim3(LANES), 0, stream, a);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t stream) {
+  return a.from ? launch<true>(a, stream) : launch<false>(a, stream);
+}
+
+hipError_t launch_paged_read(const PagedReadArgs& a, hipStream_t stream) {
   if (a.tokens == 0) return hipSuccess;
-  if (a.dtype == HEATKV_F32) return launch<float, false>(a, stream);
-  return a.kv_fp8 ? launch<bf16_t, true>(a, stream) : launch<bf16_t, false>(a, stream);
+  if (a.dtype == HEATKV_F32) return launch_read<float, NATIVE>(a, stream);
+  return a.kv_format == HEATKV_KV_FP4_E2M1   ? launch_read<bf16_t, E2M1>(a, stream)
+         : a.kv_format == HEATKV_KV_FP8_E4M3 ? launch_read<bf16_t, E4M3>(a, stream)
+                                             : launch_read<bf16_t, NATIVE>(a, stream);
 }
 
 }  // namespace heatkv

@@ -1,4 +1,4 @@
-// Attention of new tokens over the paged cache, bf16 (cache rows bf16 or FP8 E4M3): few query rows per request, or a choice
+// Attention of new tokens over the paged cache, bf16 (cache rows bf16, FP8 E4M3 or FP4 E2M1): few query rows per request, or a choice
 // of pages for each token.  paged_attend_long.hip: many rows over all pages; paged_attend_f32.hip: fp32.
 //
 // A workgroup takes its share of the launch (paged_schedule.h), segment by segment: 16 query rows (tokens x the queries that
@@ -17,6 +17,8 @@
 // of 64 keys for each of 16 requests and 8 heads as much in as long.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "f32_mfma.h"
 #include "kernels.h"
 #include "paged.h"
@@ -33,26 +35,14 @@ using namespace paged;
 constexpr int WAVES = 4, STEP = 32;  // wavefronts of a workgroup, keys of a step
 extern __shared__ __attribute__((aligned(16))) char paged_lds[];
 
-// 8 or 16 E4M3 codes as bf16 (exact).
-__device__ __forceinline__ bf16x8 codes_to_bf16(unsigned lo, unsigned hi) {
-  union {
-    bf16x2 h[4];
-    bf16x8 v;
-  } o;
-  o.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(lo), 1.0f, false);
-  o.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(lo), 1.0f, true);
-  o.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(hi), 1.0f, false);
-  o.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(hi), 1.0f, true);
-  return o.v;
-}
-
-template <int D, bool FP8, bool CHOSEN>
+template <int D, Format F, bool CHOSEN>
 __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_kernel(AttendParams p) {
   constexpr int NK = D / 32, NV = D / 16;            // MFMA steps of a score, accumulator blocks of 16 columns
   constexpr int RB = 2 * D;                          // bytes of a bf16 row in the V stage
-  constexpr int SRC = FP8 ? D : 2 * D;               // bytes of a cache row
-  constexpr int KC = SRC / 64, VC = STEP * SRC / 1024;  // 16-byte loads per lane: a granule of K, a step of V
-  constexpr int LPR = SRC / 16;                      // lanes that share a row of V
+  constexpr bool FP8 = F == E4M3, FP4 = F == E2M1;
+  constexpr int SRC = row_bytes<bf16_t, F>(D);       // bytes of a cache row
+  constexpr int KC = FP4 ? 1 : SRC / 64, VC = FP4 ? 2 : STEP * SRC / 1024;  // loads per lane: a granule of K, a step of V
+  constexpr int LPR = FP4 ? 4 : SRC / 16;            // lanes that share a row of V
   constexpr int RPL = 64 / LPR;                      // rows of V per load
   constexpr int PITCH = D + 4;                       // floats per row of a parked output tile
   static_assert(16 * PITCH * 4 == stage_bytes(D) && STEP * RB <= stage_bytes(D), "the parked tiles take the stages' place");
@@ -88,7 +78,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_kernel(AttendParam
       const bf16_t* from = static_cast<const bf16_t*>(p.q.data) + token * p.q.token_stride + hq * p.q.head_stride;
 #pragma unroll
       for (int ks = 0; ks < NK; ++ks) {
-        const int at = FP8 ? 64 * (ks / 2) + 16 * g + 8 * (ks % 2) : 32 * ks + 8 * g;
+        const int at = FP4 ? D / 4 * g + 8 * ks : FP8 ? 64 * (ks / 2) + 16 * g + 8 * (ks % 2) : 32 * ks + 8 * g;
         q[ks] = *reinterpret_cast<const bf16x8*>(from + at);
       }
     }
@@ -96,16 +86,43 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_kernel(AttendParam
     const char* const v_pages = static_cast<const char*>(p.v_pages);
     const unsigned k_off = n * SRC + 16 * g;
     const unsigned v_off = (lane / LPR) * SRC + (lane % LPR) * 16;
+    // 4-bit rows: D / 4 codes of a row to a lane, for K those of its MFMA steps; a lane's are within one block.
+    const unsigned k_codes = (4 * n + g) * (D / 8), k_scale = 8 * D + (4 * n + g) * D / 128;
+    const unsigned v_codes = lane * (D / 8), v_scale = 8 * D + lane * D / 128;
 
     uint4 k_raw[2][KC], v_raw[VC];
+    [[maybe_unused]] unsigned char k_byte[2], v_byte[2];
+    [[maybe_unused]] auto codes = [](const char* from) {
+      if constexpr (D == 128) return ldg16(from);
+      const uint2 w = *reinterpret_cast<const uint2*>(from);
+      return make_uint4(w.x, w.y, 0, 0);
+    };
     Granule at[2] = {};
     auto fetch_k = [&] {
+      if constexpr (FP4) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const char* from = k_pages + at[i].row * SRC;
+          k_raw[i][0] = codes(from + k_codes);
+          k_byte[i] = from[k_scale];
+        }
+        return;
+      }
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int c = 0; c < KC; ++c) k_raw[i][c] = ldg16(k_pages + at[i].row * SRC + k_off + 64 * c);
     };
     auto fetch_v = [&] {
+      if constexpr (FP4) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const char* from = v_pages + at[i].row * SRC;
+          v_raw[i] = codes(from + v_codes);
+          v_byte[i] = from[v_scale];
+        }
+        return;
+      }
 #pragma unroll
       for (int c = 0; c < VC; ++c) v_raw[c] = ldg16(v_pages + at[c / (VC / 2)].row * SRC + v_off + (c % (VC / 2)) * 1024);
     };
@@ -144,7 +161,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_kernel(AttendParam
 #pragma unroll
         for (int ks = 0; ks < NK; ++ks) {
           bf16x8 a;
-          if constexpr (FP8) {
+          if constexpr (FP4) {
+            const uint4& w = k_raw[i][0];
+            a = nibbles_to_bf16(ks == 0 ? w.x : ks == 1 ? w.y : ks == 2 ? w.z : w.w, scale_of(k_byte[i]));
+          } else if constexpr (FP8) {
             const uint4& w = k_raw[i][ks / 2];
             a = ks % 2 ? codes_to_bf16(w.z, w.w) : codes_to_bf16(w.x, w.y);
           } else {
@@ -156,6 +176,23 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_kernel(AttendParam
       // V into the stage; rows behind the request's end as zeros (a probability of 0 does not remove an infinity).
 #pragma unroll
       for (int cidx = 0; cidx < VC; ++cidx) {
+        if constexpr (FP4) {
+          const int r = lane / 4, row_in = 16 * cidx + r;
+          uint4 w = v_raw[cidx];
+          float scale = scale_of(v_byte[cidx]);
+          if (at[cidx].pos + GRANULE > tile.len && at[cidx].pos + r >= tile.len) {
+            w = make_uint4(0, 0, 0, 0);
+            scale = 1.f;
+          }
+#pragma unroll
+          for (int k = 0; k < D / 64; ++k) {
+            const int win = (D / 64 * (lane % 4) + k) ^ stage_swizzle<D>(row_in);
+            bf16x8* to = reinterpret_cast<bf16x8*>(stage + row_in * RB + win * 32);
+            to[0] = nibbles_to_bf16(k ? w.z : w.x, scale);
+            to[1] = nibbles_to_bf16(k ? w.w : w.y, scale);
+          }
+          continue;
+        }
         const int i = cidx / (VC / 2), r = (cidx % (VC / 2)) * RPL + lane / LPR;  // granule, row of it
         uint4 w = v_raw[cidx];
         if (at[i].pos + GRANULE > tile.len && at[i].pos + r >= tile.len) w = make_uint4(0, 0, 0, 0);
@@ -301,7 +338,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_kernel(AttendParam
       const float norm = !alone ? 1.f : l_row > 0.f ? 1.f / l_row : l_row;
       float* const parts_row = z.parts.o + (part_base + r) * D;  // the part's, or not used
       bf16_t* const out_row = static_cast<bf16_t*>(const_cast<void*>(z.out.data)) + (tile.q0 + jr) * z.out.token_stride + hr * z.out.head_stride;
-      redo_row<bf16_t, FP8, D, CHOSEN>(
+      redo_row<bf16_t, F, D, CHOSEN>(
           z, tile.q0 + jr, hr, visible_keys(z.c, tile, jr), tile.len, 2 * begin, 2 * end, false,
           [&](int gr) {
             const Granule at = walk.locate(gr);
@@ -320,25 +357,30 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_kernel(AttendParam
   }
 }
 
-template <int D, bool FP8, bool CHOSEN>
+template <int D, Format F, bool CHOSEN>
 hipError_t launch(const AttendParams& p, hipStream_t stream) {
   const size_t lds = WAVES * stage_bytes(D) + (CHOSEN ? walk_lds_bytes(p) : 0);
   static std::atomic<unsigned long long> allowed{0};
   if (lds > 64 * 1024)
-    if (hipError_t e = allow_lds(reinterpret_cast<const void*>(&paged_attend_kernel<D, FP8, CHOSEN>), WALK_LDS, allowed)) return e;
-  hipLaunchKernelGGL((paged_attend_kernel<D, FP8, CHOSEN>), dim3(p.parts.grid), dim3(64 * WAVES), lds, stream, p);
+    if (hipError_t e = allow_lds(reinterpret_cast<const void*>(&paged_attend_kernel<D, F, CHOSEN>), WALK_LDS, allowed)) return e;
+  hipLaunchKernelGGL((paged_attend_kernel<D, F, CHOSEN>), dim3(p.parts.grid), dim3(64 * WAVES), lds, stream, p);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_paged_attend_bf16(const PagedAttendParams& p, int d, bool fp8, hipStream_t stream) {
-  if (p.selected) {
-    if (d == 128) return fp8 ? launch<128, true, true>(p, stream) : launch<128, false, true>(p, stream);
-    return fp8 ? launch<64, true, true>(p, stream) : launch<64, false, true>(p, stream);
-  }
-  if (d == 128) return fp8 ? launch<128, true, false>(p, stream) : launch<128, false, false>(p, stream);
-  return fp8 ? launch<64, true, false>(p, stream) : launch<64, false, false>(p, stream);
+hipError_t launch_paged_attend_bf16(const PagedAttendParams& p, int d, int kv_format, hipStream_t stream) {
+  auto run = [&](auto d_tag, auto chosen) {
+    constexpr int D = decltype(d_tag)::value;
+    constexpr bool CHOSEN = decltype(chosen)::value;
+    return kv_format == HEATKV_KV_FP4_E2M1   ? launch<D, E2M1, CHOSEN>(p, stream)
+           : kv_format == HEATKV_KV_FP8_E4M3 ? launch<D, E4M3, CHOSEN>(p, stream)
+                                             : launch<D, NATIVE, CHOSEN>(p, stream);
+  };
+  using D128 = std::integral_constant<int, 128>;
+  using D64 = std::integral_constant<int, 64>;
+  if (p.selected) return d == 128 ? run(D128{}, std::true_type{}) : run(D64{}, std::true_type{});
+  return d == 128 ? run(D128{}, std::false_type{}) : run(D64{}, std::false_type{});
 }
 
 }  // namespace heatkv

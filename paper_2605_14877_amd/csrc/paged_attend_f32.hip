@@ -183,7 +183,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attend_f32_kernel(AttendP
       const float norm = !alone ? 1.f : l_row > 0.f ? 1.f / l_row : l_row;
       float* const to = !alone ? z.parts.o + (part_base + r) * D
                                : static_cast<float*>(const_cast<void*>(z.out.data)) + (tile.q0 + jr) * z.out.token_stride + hr * z.out.head_stride;
-      redo_row<float, false, D, CHOSEN>(
+      redo_row<float, NATIVE, D, CHOSEN>(
           z, tile.q0 + jr, hr, visible_keys(z.c, tile, jr), tile.len, 2 * begin, 2 * end, false,
           [&](int gr) {
             const Granule x = walk.locate(gr);

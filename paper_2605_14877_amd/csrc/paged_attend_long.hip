@@ -5,7 +5,7 @@
 // The request's keys are walked in tiles of 64, four granules of 16 rows, each with an address of its own; tile format,
 // copies and operand layouts are those of tile_lds.h.  Rows behind the request's end arrive as zeros (range-checked
 // copies), keys that a row does not see get a score of -inf in the tiles where that can be.
-// 8-bit cache rows come through registers, converted on the way into the stage.
+// 8-bit and 4-bit cache rows come through registers, converted on the way into the stage.
 // Chosen pages: the walk is over the union of the pages that the workgroup's tokens have chosen (up to 128 of them, neighbours in
 // the request, which choose alike), with a word of 32 tokens for each wavefront and page.
 //
@@ -15,6 +15,8 @@
 // 44 us, twice the softmax for a product and 2 pieces to a workgroup.  Chosen pages, 1024 tokens, 32 of 272 pages each, 127 in
 // the union of 32 tokens: 96 us, as much as the union's products (57 GFLOP) at 0.6 PFLOP/s.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "kernels.h"
 #include "paged.h"
@@ -32,18 +34,6 @@ using namespace paged;
 
 constexpr int BM = 128, BN = tile::ROWS;  // query rows of a workgroup, keys of a tile
 extern __shared__ __attribute__((aligned(1024))) char paged_long_lds[];
-
-__device__ __forceinline__ uint4 codes_to_chunk(unsigned lo, unsigned hi) {  // 8 E4M3 codes as bf16 (exact)
-  union {
-    bf16x2 h[4];
-    uint4 u;
-  } o;
-  o.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(lo), 1.0f, false);
-  o.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(lo), 1.0f, true);
-  o.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(hi), 1.0f, false);
-  o.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(hi), 1.0f, true);
-  return o.u;
-}
 
 // Where the four granules of a tile lie, in granules of the cache (there are less than 2^31, check_shape()).
 struct TileRows {
@@ -73,6 +63,18 @@ struct Union {
 __device__ __forceinline__ const __attribute__((address_space(3))) char* lds_pointer(int at) {
   return (const __attribute__((address_space(3))) char*)static_cast<size_t>(static_cast<unsigned>(at));
 }
+
+__device__ __forceinline__ int pick(int which, int one, int other) {
+  int x;
+  asm("s_cmp_lg_u32 %1, 0\n\ts_cselect_b32 %0, %2, %3" : "=s"(x) : "s"(which), "s"(one), "s"(other) : "scc");
+  return x;
+}
+
+// Codes of a lane's load of a 4-bit row, and their scale byte.
+struct Nibbles {
+  uint4 w;
+  unsigned char scale;
+};
 
 struct Shared {
   Scratch scratch;
@@ -123,12 +125,13 @@ __device__ __forceinline__ int build_union(const AttendParams& a, const Tile& t,
   return __builtin_amdgcn_readfirstlane(*u.count);
 }
 
-template <int D, bool FP8, bool CHOSEN>
+template <int D, Format F, bool CHOSEN>
 __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams p) {
-  constexpr int RB = 2 * D, TILE_BYTES = BN * RB, SRC = FP8 ? D : RB;
+  constexpr bool CODES = F != NATIVE, FP4 = F == E2M1;
+  constexpr int RB = 2 * D, TILE_BYTES = BN * RB, SRC = row_bytes<bf16_t, F>(D);
   constexpr int NK = D / 16, NV = D / 32;
   constexpr int CPT = TILE_BYTES / 4096;            // copies of a tile per wavefront (bf16 rows)
-  constexpr int CPL = BN * D / 16 / 256;            // 16-byte loads of a tile per lane (8-bit rows)
+  constexpr int CPL = FP4 ? 1 : BN * D / 16 / 256;  // loads of a tile per lane (8-bit rows, 16 codes; 4-bit rows, D / 4)
   char(*const lds)[2][TILE_BYTES] = reinterpret_cast<char(*)[2][TILE_BYTES]>(paged_long_lds);  // [stage][K, V]
   // Behind the stages, which then begin at LDS address 0: all of their offsets fit into the read instructions.
   Shared& shared = *reinterpret_cast<Shared*>(paged_long_lds + 4 * TILE_BYTES);
@@ -244,25 +247,54 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     tile::copy_1k_checked(lds_wave, decltype(buf_tag)::value * (2 * TILE_BYTES) + TILE_BYTES + 4096 * i, ld_off_v,
                           source(v_pages, at, it, i), 0);
   };
-  // 8-bit rows: load i of a lane is 16 codes of one row, converted on the way into the stage.
-  constexpr int LPR = D / 16;  // lanes per row
+  // Codes: load i of a lane is 16 codes of one row (4-bit: D / 4, and their scale byte), converted on the way into the stage.
+  constexpr int LPR = FP4 ? 4 : D / 16;  // lanes per row
+  using Raw = std::conditional_t<FP4, Nibbles, uint4>;
   auto load_codes = [&](const char* pages, const TileRows& at, int it, int i) {
     const int r = (tid + 256 * i) / LPR;  // a wavefront's 64 / LPR rows are of one granule
-    const int from = D == 128 ? (wave >> 1 ? at.granule[2 * i + 1] : at.granule[2 * i])
-                              : wave >> 1 ? (wave & 1 ? at.granule[3] : at.granule[2]) : (wave & 1 ? at.granule[1] : at.granule[0]);
-    const int pos = !CHOSEN ? it * BN + (r & ~15)
-                    : it >= end ? 1 << 30
-                    : D == 128  ? (wave >> 1 ? at.pos[2 * i + 1] : at.pos[2 * i])
-                                : wave >> 1 ? (wave & 1 ? at.pos[3] : at.pos[2]) : (wave & 1 ? at.pos[1] : at.pos[0]);
-    uint4 raw = make_uint4(0, 0, 0, 0);
-    if (pos + (r & 15) < stop) raw = ldg16(pages + (static_cast<long long>(from) * 16 + (r & 15)) * SRC + (tid % LPR) * 16);
-    return raw;
+    // Of the granules' places one by arithmetic on all: a choice of one in memory would keep them there.
+    auto own = [&](const int (&x)[4]) {
+      const int x0 = x[0], x1 = x[1], x2 = x[2], x3 = x[3];
+      if constexpr (FP4 || D == 64) return pick(wave >> 1, pick(wave & 1, x3, x2), pick(wave & 1, x1, x0));
+      return i ? pick(wave >> 1, x3, x2) : pick(wave >> 1, x1, x0);
+    };
+    const int from = own(at.granule);
+    const int pos = !CHOSEN ? it * BN + (r & ~15) : it >= end ? 1 << 30 : own(at.pos);
+    const bool valid = pos + (r & 15) < stop;
+    if constexpr (FP4) {
+      Raw raw{make_uint4(0, 0, 0, 0), 127};
+      if (valid) {
+        const char* const first = pages + static_cast<long long>(from) * 16 * SRC;
+        raw.scale = first[8 * D + lane * D / 128];
+        if constexpr (D == 128) {
+          raw.w = ldg16(first + lane * 16);
+        } else {
+          const uint2 w = *reinterpret_cast<const uint2*>(first + lane * 8);
+          raw.w.x = w.x;
+          raw.w.y = w.y;
+        }
+      }
+      return raw;
+    } else {
+      Raw raw = make_uint4(0, 0, 0, 0);
+      if (valid) raw = ldg16(pages + (static_cast<long long>(from) * 16 + (r & 15)) * SRC + (tid % LPR) * 16);
+      return raw;
+    }
   };
-  auto store_codes = [&](char* stage, const uint4& raw, int i, auto is_v) {
-    const int r = (tid + 256 * i) / LPR, chunk = 2 * (tid % LPR);
+  auto store_codes = [&](char* stage, const Raw& raw, int i, auto is_v) {
+    const int r = (tid + 256 * i) / LPR;
     const int swz = decltype(is_v)::value ? tile::swizzle_v<RB>(r & 15) : tile::swizzle_k<RB>(r & 15);
-    *reinterpret_cast<uint4*>(stage + r * RB + ((chunk ^ swz) << 4)) = codes_to_chunk(raw.x, raw.y);
-    *reinterpret_cast<uint4*>(stage + r * RB + (((chunk + 1) ^ swz) << 4)) = codes_to_chunk(raw.z, raw.w);
+    if constexpr (FP4) {
+      const int chunk = D / 32 * (tid % LPR);
+      const unsigned w[4] = {raw.w.x, raw.w.y, raw.w.z, raw.w.w};
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k)
+        *reinterpret_cast<bf16x8*>(stage + r * RB + (((chunk + k) ^ swz) << 4)) = nibbles_to_bf16(w[k], scale_of(raw.scale));
+    } else {
+      const int chunk = 2 * (tid % LPR);
+      *reinterpret_cast<bf16x8*>(stage + r * RB + ((chunk ^ swz) << 4)) = codes_to_bf16(raw.x, raw.y);
+      *reinterpret_cast<bf16x8*>(stage + r * RB + (((chunk + 1) ^ swz) << 4)) = codes_to_bf16(raw.z, raw.w);
+    }
   };
   using Zero = std::integral_constant<int, 0>;
   using One = std::integral_constant<int, 1>;
@@ -465,8 +497,8 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
   auto step = [&](int it, auto kb1, auto vb0, auto&& math) {
     wait_vmcnt<0>();
     __syncthreads();
-    if constexpr (FP8) {  // V's codes have the first half of the step to arrive, K's the second
-      uint4 raw[CPL];
+    if constexpr (CODES) {  // V's codes have the first half of the step to arrive, K's the second
+      Raw raw[CPL];
       math([&](int i) {
         if (i == 0)
 #pragma unroll
@@ -474,8 +506,9 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
         else if (i == 1)
           at = locate(it + 2);
         else if (i >= SLOTS / 2 && i < SLOTS / 2 + CPL) {
-          store_codes(lds[decltype(kb1)::value][1], raw[i - SLOTS / 2], i - SLOTS / 2, One{});
-          raw[i - SLOTS / 2] = load_codes(k_pages, at, it + 2, i - SLOTS / 2);
+          const int k = CPL == 1 ? 0 : i - SLOTS / 2;
+          store_codes(lds[decltype(kb1)::value][1], raw[k], k, One{});
+          raw[k] = load_codes(k_pages, at, it + 2, k);
         }
       });
 #pragma unroll
@@ -509,8 +542,8 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
   if (begin < end) {
     const int second = begin + 1 < end ? begin + 1 : begin;
     at = locate(begin);
-    if constexpr (FP8) {
-      uint4 raw[3][CPL];
+    if constexpr (CODES) {
+      Raw raw[3][CPL];
 #pragma unroll
       for (int k = 0; k < CPL; ++k) {
         raw[0][k] = load_codes(k_pages, at, begin, k);
@@ -617,7 +650,7 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     const long long part_row = static_cast<long long>(w) * BM + w_row + r;
     float* const parts_row = z.parts.o + part_row * D;  // the part's, or not used
     bf16_t* const out_row = static_cast<bf16_t*>(const_cast<void*>(z.out.data)) + (tl.q0 + j) * z.out.token_stride + hq * z.out.head_stride;
-    const float l_seen = redo_row<bf16_t, FP8, D, CHOSEN>(
+    const float l_seen = redo_row<bf16_t, F, D, CHOSEN>(
         z, tl.q0 + j, hq, visible_keys(z.c, tl, j), tl.len, 4 * begin, 4 * end, lost,
         [&](int g) {
           if constexpr (CHOSEN) {
@@ -648,26 +681,31 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
   }
 }
 
-template <int D, bool FP8, bool CHOSEN>
+template <int D, Format F, bool CHOSEN>
 hipError_t launch(const AttendParams& p, hipStream_t stream) {
   const size_t lds = 4 * BN * 2 * D + kUnionAt + (CHOSEN ? many_union_bytes(p.c.G, p.c.max_pages, p.top) : 0);
   static std::atomic<unsigned long long> allowed{0};
   if (lds > 64 * 1024)
-    if (hipError_t e = allow_lds(reinterpret_cast<const void*>(&paged_attend_long_kernel<D, FP8, CHOSEN>), MANY_LDS, allowed)) return e;
-  hipLaunchKernelGGL((paged_attend_long_kernel<D, FP8, CHOSEN>), dim3(p.parts.grid), dim3(256), lds, stream, p);
+    if (hipError_t e = allow_lds(reinterpret_cast<const void*>(&paged_attend_long_kernel<D, F, CHOSEN>), MANY_LDS, allowed)) return e;
+  hipLaunchKernelGGL((paged_attend_long_kernel<D, F, CHOSEN>), dim3(p.parts.grid), dim3(256), lds, stream, p);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_paged_attend_long(const PagedAttendParams& p, int d, bool fp8, hipStream_t stream) {
+hipError_t launch_paged_attend_long(const PagedAttendParams& p, int d, int kv_format, hipStream_t stream) {
   static_assert(4 * BN * 2 * 128 + kUnionAt + MANY_UNION_BYTES <= MANY_LDS, "the largest union that plan_launches() sends here fits");
-  if (p.selected) {
-    if (d == 128) return fp8 ? launch<128, true, true>(p, stream) : launch<128, false, true>(p, stream);
-    return fp8 ? launch<64, true, true>(p, stream) : launch<64, false, true>(p, stream);
-  }
-  if (d == 128) return fp8 ? launch<128, true, false>(p, stream) : launch<128, false, false>(p, stream);
-  return fp8 ? launch<64, true, false>(p, stream) : launch<64, false, false>(p, stream);
+  auto run = [&](auto d_tag, auto chosen) {
+    constexpr int D = decltype(d_tag)::value;
+    constexpr bool CHOSEN = decltype(chosen)::value;
+    return kv_format == HEATKV_KV_FP4_E2M1   ? launch<D, E2M1, CHOSEN>(p, stream)
+           : kv_format == HEATKV_KV_FP8_E4M3 ? launch<D, E4M3, CHOSEN>(p, stream)
+                                             : launch<D, NATIVE, CHOSEN>(p, stream);
+  };
+  using D128 = std::integral_constant<int, 128>;
+  using D64 = std::integral_constant<int, 64>;
+  if (p.selected) return d == 128 ? run(D128{}, std::true_type{}) : run(D64{}, std::true_type{});
+  return d == 128 ? run(D128{}, std::false_type{}) : run(D64{}, std::false_type{});
 }
 
 }  // namespace heatkv

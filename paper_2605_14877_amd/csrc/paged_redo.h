@@ -17,19 +17,25 @@
 namespace heatkv {
 namespace paged {
 
-template <class T, bool FP8>
-__device__ __forceinline__ float cache_value(const void* pages, long long at) {
-  if constexpr (FP8)
-    return __builtin_amdgcn_cvt_f32_fp8(static_cast<const unsigned char*>(pages)[at], 0);
-  else
-    return static_cast<float>(static_cast<const T*>(pages)[at]);
+template <class T, Format F, int D>
+__device__ __forceinline__ float cache_value(const void* pages, long long row, int col) {
+  if constexpr (F == E4M3) {
+    return __builtin_amdgcn_cvt_f32_fp8(static_cast<const unsigned char*>(pages)[row * D + col], 0);
+  } else if constexpr (F == E2M1) {
+    const int r = static_cast<int>(row) & 15;
+    const auto* at = static_cast<const unsigned char*>(pages) + (row - r) * row_bytes<T, F>(D);
+    const unsigned code = at[r * (D / 2) + col / 2] >> (col & 1 ? 4 : 0);
+    return static_cast<float>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale_of(at[8 * D + r * (D / 32) + col / 32]), 0)[0]);
+  } else {
+    return static_cast<float>(static_cast<const T*>(pages)[row * D + col]);
+  }
 }
 
 // Query head hq of `token` over the granules [begin, end): locate(g) gives {row, pos, whether the row sees the granule's page}, keys
 // from `limit` on are not seen, and none of those from `len` on was read.  probability(s): of a raw score, relative to the reference
 // that the row's sum was formed with.  stored(column): the result so far; store(column, value, sum of the probabilities) gets the
 // unnormalised sums of the columns that were NaN.  with_sum: the row's sum is wrong as well, and formed to its end; returns it.
-template <class T, bool FP8, int D, bool CHOSEN, class Locate, class Probability, class Stored, class Store>
+template <class T, Format F, int D, bool CHOSEN, class Locate, class Probability, class Stored, class Store>
 __device__ __forceinline__ float redo_row(const AttendParams& p, long long token, int hq, int limit, int len, int begin, int end,
                                           bool with_sum, const Locate& locate, const Probability& probability, const Stored& stored,
                                           const Store& store) {
@@ -49,7 +55,7 @@ __device__ __forceinline__ float redo_row(const AttendParams& p, long long token
       for (int k = max(limit - at.pos, 0); k < min(len - at.pos, 16); ++k)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const float v = cache_value<T, FP8>(p.v_pages, (at.row + k) * D + 64 * i + lane);
+          const float v = cache_value<T, F, D>(p.v_pages, at.row + k, 64 * i + lane);
           reached = reached || (nan[i] && !(fabsf(v) < INFINITY));
         }
       reached = __any(reached);
@@ -65,11 +71,11 @@ __device__ __forceinline__ float redo_row(const AttendParams& p, long long token
 #pragma unroll
     for (int k = 0; k < 16; ++k)
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[k][i] = cache_value<T, FP8>(p.v_pages, (at.row + k) * D + 64 * i + lane);
+      for (int i = 0; i < N; ++i) v[k][i] = cache_value<T, F, D>(p.v_pages, at.row + k, 64 * i + lane);
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < D; i += 4)
-      s = fmaf(static_cast<float>(q[i + quarter]), cache_value<T, FP8>(p.k_pages, (at.row + key) * D + i + quarter), s);
+      s = fmaf(static_cast<float>(q[i + quarter]), cache_value<T, F, D>(p.k_pages, at.row + key, i + quarter), s);
     s += __shfl_xor(s, 1, 64);
     s += __shfl_xor(s, 2, 64);
     const float e = at.pos + key < limit ? probability(s) : -1.f;

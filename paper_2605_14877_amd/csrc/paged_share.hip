@@ -1,0 +1,636 @@
+// Paged cache: pages that several rows of the block table hold, and rows that lose tokens out of their middle.
+//
+//   fork     row b continues row parent[b]: its entries and length become those of that row
+//   assign   a step of the allocator (paged_tables.hip) that leaves a page alone which another row holds too
+//   compact  a row keeps the marked ones of its tokens, in order; the move of their rows is listed
+//
+// holders[page]: rows of the table that hold it.  A row that gains a page counts one up, one that loses it one down; the page
+// whose count comes down to 0 is marked in a bitmap, and the last launch of a call puts the marked pages behind the ring's tail
+// in ascending order.  Counts are whole numbers and marks are bits, so the result does not depend on the order in which
+// workgroups come by.  What is gained is counted before what is lost, in a launch of its own: no count passes through 0 on
+// the way.
+//
+// Each call is a few phases that are launches of their own; `Group` says which of how many workgroups one is.
+//
+// Bound: latency, of the launches and of a few round trips to memory in each.
+#include <hip/hip_runtime.h>
+
+#include "kernels.h"
+#include "paged.h"
+
+namespace heatkv {
+
+namespace {
+
+constexpr int LANES = 1024, WAVES = LANES / 64;
+constexpr int PER_LANE = paged::MAX_BATCH / LANES;
+constexpr int FORK_LANES = 256, FORK_ENTRIES = 8192;  // lanes of a workgroup, entries of the table that it holds in LDS
+constexpr int EMIT_LANES = 256, CHUNK = 4096;         // tokens that a workgroup of compact looks at together
+
+struct Group {
+  int index, count;
+};
+__device__ __forceinline__ Group group() { return {static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x)}; }
+
+// Words of TableArgs::state.
+enum State { HEAD, COUNT, TAKEN, STATUS, MOVES };
+
+__device__ __forceinline__ int inclusive_scan(int v, int lane) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int u = __shfl_up(v, d, 64);
+    if (lane >= d) v += u;
+  }
+  return v;
+}
+__device__ __forceinline__ long long inclusive_scan(long long v, int lane) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const long long u = __shfl_up(v, d, 64);
+    if (lane >= d) v += u;
+  }
+  return v;
+}
+
+// Largest b in [0, n) with first[b] <= x; first[0] = 0, ascending.
+__device__ __forceinline__ int find(const int* first, int n, int x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    (first[mid] <= x ? lo : hi) = mid;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ bool ring_fits(const TableArgs& p, int head, int count) {
+  return head >= 0 && head < p.num_pages && count >= 0 && count <= p.num_pages;
+}
+// Entry i behind the ring's head; i below num_pages.
+__device__ __forceinline__ int ring_at(const TableArgs& p, int head, int i) {
+  const unsigned at = static_cast<unsigned>(head) + static_cast<unsigned>(i);
+  return p.ring[at < static_cast<unsigned>(p.num_pages) ? at : at - p.num_pages];
+}
+__device__ __forceinline__ int in_range(const TableArgs& p, int page) {
+  return static_cast<int>(min(static_cast<unsigned>(page), static_cast<unsigned>(p.num_pages - 1)));
+}
+__device__ __forceinline__ int pages_of(const TableArgs& p, int tokens) {
+  return static_cast<int>((static_cast<long long>(tokens) + (1 << p.page_log2) - 1) >> p.page_log2);
+}
+__device__ __forceinline__ long long most_tokens(const TableArgs& p) { return static_cast<long long>(p.max_pages) << p.page_log2; }
+
+// A row no longer holds `page`.
+__device__ __forceinline__ void let_go(const TableArgs& p, int page) {
+  page = in_range(p, page);
+  if (atomicSub(&p.holders[page], 1) == 1) atomicOr(&p.gone[page >> 5], 1u << (page & 31));
+}
+// A row holds `page`, fresh from the ring.
+__device__ __forceinline__ void take(const TableArgs& p, int page) { p.holders[in_range(p, page)] = 1; }
+
+__device__ __forceinline__ int gone_words(const TableArgs& p) { return (p.num_pages + 31) / 32; }
+__device__ __forceinline__ void clear_gone(const TableArgs& p, Group g, int lanes) {
+  for (int i = g.index * lanes + threadIdx.x; i < gone_words(p); i += g.count * lanes) p.gone[i] = 0;
+}
+
+// ---- the last phase of every call: marked pages into the ring, lengths and the ring's span ------------------------------
+
+// Workgroup g of the grid takes words [PART g, PART (g + 1)) of the bitmap, and counts those before for itself.
+constexpr int PART = 4 * LANES;
+
+__device__ __forceinline__ void give_back(const TableArgs& p, Group g) {
+  __shared__ int part[2][WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int words = gone_words(p), first = g.index * PART, R = p.num_pages;
+  const int head = p.state[HEAD], count = p.state[COUNT], taken = p.state[TAKEN];
+  int before = 0;
+  for (int i = tid; i < first; i += LANES) before += __popc(p.gone[i]);
+  // a wavefront's words are neighbours, and a lane's
+  unsigned w[4];
+  int mine = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int i = first + 4 * tid + k;
+    w[k] = i < words ? p.gone[i] : 0;
+    mine += __popc(w[k]);
+  }
+  const int inc = inclusive_scan(mine, lane), earlier = inclusive_scan(before, lane);
+  if (lane == 63) {
+    part[0][wave] = inc;
+    part[1][wave] = earlier;
+  }
+  __syncthreads();
+  int at = 0, all = 0, all_before = 0;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) {
+    all_before += part[1][i];
+    at += i < wave ? part[0][i] : 0;
+    all += part[0][i];
+  }
+  at += all_before;
+  // Pages of a lane's words, by the wavefront: 32 lanes write the pages of one word.
+  const int start = inc - mine;
+  unsigned long long todo = __ballot(mine > 0);
+  const int room = R - (count - taken);  // tables and holders that fit each other never have more to give
+  while (todo) {
+    const int from = __builtin_ctzll(todo);
+    todo &= todo - 1;
+    int nth = at + __builtin_amdgcn_readlane(start, from);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const unsigned bits = __builtin_amdgcn_readlane(w[k], from);
+      if (lane < 32 && (bits >> lane & 1)) {
+        const int i = nth + __popc(bits & ((1u << lane) - 1));
+        if (i < room) {
+          unsigned to = static_cast<unsigned>(head) + static_cast<unsigned>(count) + static_cast<unsigned>(i);  // below 3 R < 2^32
+          to -= to >= static_cast<unsigned>(R) ? R : 0;
+          to -= to >= static_cast<unsigned>(R) ? R : 0;
+          p.ring[to] = 32 * (first + 4 * (64 * wave + from) + k) + lane;
+        }
+      }
+      nth += __popc(bits);
+    }
+  }
+  if (g.index == 0)
+    for (int b = tid; b < p.batch; b += LANES) p.lens_out[b] = p.next[b];
+  if (g.index == g.count - 1 && tid == 0) {
+    const bool made = p.state[STATUS] == HEATKV_PAGED_OK;  // else the span may be anything, and stays
+    const int next = head + taken;
+    p.span_out[0] = !made || next < R ? next : next - R;
+    p.span_out[1] = made ? count - taken + min(all_before + all, room) : count;
+  }
+}
+
+// ---- fork ---------------------------------------------------------------------------------------------------------------
+
+// Counts what rows gain.  Every workgroup looks at all parents and lengths for itself.
+__device__ __forceinline__ void fork_gains(const ForkArgs& f, Group g, int columns_log2) {
+  const TableArgs& p = f.t;
+  const int tid = threadIdx.x, B = p.batch;
+  clear_gone(p, g, FORK_LANES);
+  const int head = p.span[0], count = p.span[1];
+  const long long most = most_tokens(p);
+  bool bad_parent = false, bad_length = false;
+  for (int b = tid; b < B; b += FORK_LANES) {
+    const int parent = f.parent[b], len = p.lens[b];
+    bad_parent = bad_parent || parent < -1 || parent >= B;
+    bad_length = bad_length || len < 0 || len > most;
+  }
+  const bool any_length = __syncthreads_or(bad_length), any_parent = __syncthreads_or(bad_parent);
+  const int status = any_length               ? HEATKV_PAGED_BAD_LENGTH
+                     : any_parent             ? HEATKV_PAGED_BAD_PARENT
+                     : !ring_fits(p, head, count) ? HEATKV_PAGED_BAD_FREE_LIST
+                                              : HEATKV_PAGED_OK;
+  if (g.index == 0) {
+    for (int b = tid; b < B; b += FORK_LANES) {
+      const int parent = f.parent[b];
+      p.next[b] = status ? p.lens[b] : parent < 0 ? 0 : p.lens[parent];
+    }
+    if (tid == 0) {
+      p.state[HEAD] = head;
+      p.state[COUNT] = count;
+      p.state[TAKEN] = 0;
+      p.state[STATUS] = status;
+      p.status[0] = status;
+    }
+  }
+  if (status) return;
+  const int c0 = g.index << columns_log2;
+  for (int i = tid; i < B << columns_log2; i += FORK_LANES) {
+    const int b = i >> columns_log2, c = c0 + (i & ((1 << columns_log2) - 1)), parent = f.parent[b];
+    if (parent == b || parent < 0 || c >= pages_of(p, p.lens[parent])) continue;
+    atomicAdd(&p.holders[in_range(p, p.table[static_cast<long long>(parent) * p.max_pages + c])], 1);
+  }
+}
+
+// A workgroup has some columns of all rows: it reads them before it writes any, and nobody else does either.
+__device__ __forceinline__ void fork_rows(const ForkArgs& f, Group g, int columns_log2) {
+  const TableArgs& p = f.t;
+  __shared__ int held[FORK_ENTRIES];
+  if (p.state[STATUS]) return;
+  const int tid = threadIdx.x, c0 = g.index << columns_log2, entries = p.batch << columns_log2;
+  auto row = [&](int b) { return p.table + static_cast<long long>(b) * p.max_pages; };
+  for (int i = tid; i < entries; i += FORK_LANES) {
+    const int b = i >> columns_log2, c = c0 + (i & ((1 << columns_log2) - 1)), parent = f.parent[b];
+    if (parent == b) continue;
+    if (parent >= 0 && c < pages_of(p, p.lens[parent])) held[i] = row(parent)[c];
+    if (c < pages_of(p, p.lens[b])) let_go(p, row(b)[c]);
+  }
+  __syncthreads();
+  for (int i = tid; i < entries; i += FORK_LANES) {
+    const int b = i >> columns_log2, c = c0 + (i & ((1 << columns_log2) - 1)), parent = f.parent[b];
+    if (parent != b && parent >= 0 && c < pages_of(p, p.lens[parent])) row(b)[c] = held[i];
+  }
+}
+
+__global__ __launch_bounds__(FORK_LANES) void paged_fork_gains_kernel(ForkArgs f, int columns_log2) { fork_gains(f, group(), columns_log2); }
+__global__ __launch_bounds__(FORK_LANES) void paged_fork_rows_kernel(ForkArgs f, int columns_log2) { fork_rows(f, group(), columns_log2); }
+__global__ __launch_bounds__(LANES) void paged_give_back_kernel(TableArgs p) { give_back(p, group()); }
+
+// ---- assign -------------------------------------------------------------------------------------------------------------
+
+// Sums over the requests before of N numbers that each lane has for its PER_LANE consecutive requests; `all`: of all.
+template <int N>
+__device__ __forceinline__ void scan_requests(const long long (&sum)[N], long long (&before)[N], long long (&all)[N]) {
+  __shared__ long long part[N][WAVES];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const long long inc = inclusive_scan(sum[k], lane);
+    before[k] = inc - sum[k];
+    all[k] = 0;
+    if (lane == 63) part[k][wave] = inc;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const long long x = part[k][w];
+      if (w < wave) before[k] += x;
+      all[k] += x;
+    }
+}
+
+// What each request takes and lets go.  Columns from first[b] = ceil(keep / page) on, or from the one before where the new
+// tokens would go onto a page that another row holds (copied[b]: that page, or -1): fresh pages up to ceil((keep + new) / page),
+// what the row held there is let go.
+__device__ __forceinline__ void assign_plan(const AssignSharedArgs& a, Group g) {
+  const TableArgs& p = a.t;
+  if (g.count > 1 && g.index > 0) return clear_gone(p, {g.index - 1, g.count - 1}, LANES);
+  if (g.count == 1) clear_gone(p, g, LANES);
+  const int tid = threadIdx.x, B = p.batch, page = 1 << p.page_log2;
+  const int head = p.span[0], count = p.span[1];
+  const long long most = most_tokens(p);
+  const int per = (B + LANES - 1) / LANES;
+  int first[PER_LANE], fresh[PER_LANE], touched[PER_LANE], come[PER_LANE], next[PER_LANE], old[PER_LANE];
+  long long sum[3] = {0, 0, 0}, before[3], all[3];  // pages to take, columns to look at, tokens
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < PER_LANE; ++i) {
+    const int b = tid * per + i;
+    first[i] = fresh[i] = touched[i] = come[i] = next[i] = 0;
+    old[i] = -1;
+    if (i >= per || b >= B) continue;
+    const int len = p.lens[b], keep = a.keep[b], n = a.new_tokens[b];
+    next[i] = len;
+    if (len < 0 || len > most || keep < 0 || keep > len || n < 0 || static_cast<long long>(keep) + n > most) {
+      bad = true;
+      continue;
+    }
+    first[i] = pages_of(p, keep);
+    come[i] = n;
+    next[i] = keep + n;
+    if (n > 0 && (keep & (page - 1))) {
+      const int last = in_range(p, p.table[static_cast<long long>(b) * p.max_pages + first[i] - 1]);
+      if (p.holders[last] > 1) {
+        old[i] = last;
+        --first[i];
+      }
+    }
+    const int end = pages_of(p, keep + n);
+    fresh[i] = end - first[i];
+    touched[i] = max(end, pages_of(p, len)) - first[i];
+  }
+#pragma unroll
+  for (int i = 0; i < PER_LANE; ++i) {
+    sum[0] += fresh[i];
+    sum[1] += touched[i];
+    sum[2] += come[i];
+  }
+  scan_requests(sum, before, all);
+  const bool any_bad = __syncthreads_or(bad);
+  const int status = any_bad                      ? HEATKV_PAGED_BAD_LENGTH
+                     : !ring_fits(p, head, count) ? HEATKV_PAGED_BAD_FREE_LIST
+                     : all[2] > a.max_tokens      ? HEATKV_PAGED_TOO_MANY_TOKENS
+                     : all[0] > count             ? HEATKV_PAGED_NO_PAGES
+                                                  : HEATKV_PAGED_OK;
+  const bool ok = status == HEATKV_PAGED_OK;
+#pragma unroll
+  for (int i = 0; i < PER_LANE; ++i) {
+    const int b = tid * per + i;
+    if (i >= per || b >= B) continue;
+    a.take0[b] = ok ? static_cast<int>(before[0]) : 0;
+    a.touch0[b] = ok ? static_cast<int>(before[1]) : 0;
+    a.q_start[b] = ok ? static_cast<int>(before[2]) : 0;
+    a.first[b] = first[i];
+    a.copied[b] = ok ? old[i] : -1;
+    p.next[b] = ok ? next[i] : p.lens[b];
+    before[0] += fresh[i];
+    before[1] += touched[i];
+    before[2] += come[i];
+  }
+  if (tid == 0) {
+    a.touch0[B] = ok ? static_cast<int>(all[1]) : 0;  // below 2^31: see check_tables()
+    a.q_start[B] = ok ? static_cast<int>(all[2]) : 0;
+    p.state[HEAD] = head;
+    p.state[COUNT] = count;
+    p.state[TAKEN] = ok ? static_cast<int>(all[0]) : 0;
+    p.state[STATUS] = status;
+    p.status[0] = status;
+  }
+}
+
+__device__ __forceinline__ void assign_move(const AssignSharedArgs& a, Group g) {
+  const TableArgs& p = a.t;
+  __shared__ int touch0[paged::MAX_BATCH], q0[paged::MAX_BATCH];
+  const int tid = threadIdx.x, B = p.batch, lp = p.page_log2, page = 1 << lp;
+  for (int b = tid; b < B; b += LANES) {
+    touch0[b] = a.touch0[b];
+    q0[b] = a.q_start[b];
+  }
+  const int touched = a.touch0[B], tokens = a.q_start[B], head = p.state[HEAD];
+  __syncthreads();
+  const int at = g.index * LANES + tid, stride = g.count * LANES;
+  auto row = [&](int b) { return p.table + static_cast<long long>(b) * p.max_pages; };
+  for (int i = at; i < touched; i += stride) {
+    const int b = find(touch0, B, i), nth = i - touch0[b], c = a.first[b] + nth;
+    int* const entry = row(b) + c;
+    if (c < pages_of(p, p.lens[b])) let_go(p, *entry);
+    if (c < pages_of(p, p.next[b])) {
+      const int fresh = ring_at(p, head, a.take0[b] + nth);
+      *entry = fresh;
+      take(p, fresh);
+    }
+  }
+  for (long long t = at; t < a.max_tokens; t += stride) {
+    int slot = -1;
+    if (t < tokens) {
+      const int b = find(q0, B, static_cast<int>(t));
+      const int x = a.keep[b] + static_cast<int>(t) - q0[b], c = x >> lp, first = a.first[b];
+      // a fresh entry of the table may be another workgroup's to write; those before the first are not written
+      slot = ((c >= first ? ring_at(p, head, a.take0[b] + c - first) : row(b)[c]) << lp) + (x & (page - 1));
+    }
+    a.slots[t] = slot;
+  }
+  for (int i = at; i < B << lp; i += stride) {
+    const int b = i >> lp, r = i & (page - 1), old = a.copied[b];
+    const bool copy = old >= 0 && r < (a.keep[b] & (page - 1));
+    a.copy_from[i] = copy ? (old << lp) + r : -1;
+    a.copy_to[i] = copy ? (ring_at(p, head, a.take0[b]) << lp) + r : -1;
+  }
+}
+
+__global__ __launch_bounds__(LANES) void paged_assign_plan_kernel(AssignSharedArgs a) { assign_plan(a, group()); }
+__global__ __launch_bounds__(LANES) void paged_assign_move_kernel(AssignSharedArgs a) { assign_move(a, group()); }
+
+// ---- compact ------------------------------------------------------------------------------------------------------------
+
+// The tokens of request b that workgroup g looks at: a.tile of them from `first` on, as far as the request has any.
+struct Stretch {
+  int b, tile, first, end;
+};
+__device__ __forceinline__ Stretch stretch_of(const CompactArgs& a, Group g) {
+  const int b = g.index / a.tiles, tile = g.index - b * a.tiles;
+  const long long first = static_cast<long long>(tile) * a.tile;
+  const long long len = min(static_cast<long long>(max(a.t.lens[b], 0)), most_tokens(a.t));
+  return {b, tile, static_cast<int>(min(first, len)), static_cast<int>(min(first + a.tile, len))};
+}
+
+// Of every stretch: how many tokens are kept, and the first one that is not.
+__device__ __forceinline__ void compact_count(const CompactArgs& a, Group g) {
+  const TableArgs& p = a.t;
+  __shared__ int part[2][EMIT_LANES / 64];
+  clear_gone(p, g, EMIT_LANES);
+  const Stretch s = stretch_of(a, g);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const unsigned char* const kept = a.kept + s.b * most_tokens(p);  // rows and stretches begin at multiples of 16 bytes
+  int n = 0, drop = INT_MAX;
+  for (int x = s.first + 16 * tid; x < s.end; x += 16 * EMIT_LANES) {
+    const uint4 raw = ldg16(kept + x);
+    const unsigned w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      // 0x80 in each byte that is not 0
+      unsigned any = ((w[i] & 0x7f7f7f7fu) + 0x7f7f7f7fu | w[i]) & 0x80808080u;
+      const int left = s.end - (x + 4 * i);
+      const unsigned real = left >= 4 ? 0x80808080u : left > 0 ? 0x80808080u & ((1u << 8 * left) - 1) : 0;
+      any &= real;
+      n += __popc(any);
+      const unsigned none = any ^ real;
+      if (none) drop = min(drop, x + 4 * i + (__builtin_ctz(none) >> 3));
+    }
+  }
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) {
+    n += __shfl_xor(n, m, 64);
+    drop = min(drop, __shfl_xor(drop, m, 64));
+  }
+  if (lane == 0) {
+    part[0][wave] = n;
+    part[1][wave] = drop;
+  }
+  __syncthreads();
+  if (tid == 0) {
+#pragma unroll
+    for (int i = 1; i < EMIT_LANES / 64; ++i) {
+      n += part[0][i];
+      drop = min(drop, part[1][i]);
+    }
+    a.counts[g.index] = n;
+    a.drops[g.index] = drop;
+  }
+}
+
+// Requests with kept tokens behind a dropped one take fresh pages for all from the page of that one on.
+__device__ __forceinline__ void compact_plan(const CompactArgs& a) {
+  const TableArgs& p = a.t;
+  __shared__ int totals[paged::MAX_BATCH], leads[paged::MAX_BATCH];
+  const int tid = threadIdx.x, B = p.batch;
+  const int head = p.span[0], count = p.span[1];
+  const long long most = most_tokens(p);
+  // `side` lanes to a request, which share its stretches
+  int side = 1;
+  while (side < 64 && side < a.tiles) side *= 2;
+  for (int b = tid / side; b < (B + LANES / side - 1) / (LANES / side) * (LANES / side); b += LANES / side) {
+    const int len = b < B ? p.lens[b] : 0;
+    int n = 0, drop = INT_MAX;
+    if (b < B && len > 0 && len <= most)
+      for (int i = tid % side; static_cast<long long>(i) * a.tile < len; i += side) {
+        n += a.counts[b * a.tiles + i];
+        drop = min(drop, a.drops[b * a.tiles + i]);
+      }
+    for (int m = 1; m < side; m *= 2) {
+      n += __shfl_xor(n, m, 64);
+      drop = min(drop, __shfl_xor(drop, m, 64));
+    }
+    if (b < B && tid % side == 0) {
+      totals[b] = n;
+      leads[b] = min(drop, len);
+    }
+  }
+  __syncthreads();
+  const int per = (B + LANES - 1) / LANES;
+  int first[PER_LANE], fresh[PER_LANE], moves[PER_LANE], total[PER_LANE];
+  long long sum[2] = {0, 0}, before[2], all[2];  // pages to take, rows to move
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < PER_LANE; ++i) {
+    const int b = tid * per + i;
+    first[i] = fresh[i] = moves[i] = total[i] = 0;
+    if (i >= per || b >= B) continue;
+    const int len = p.lens[b];
+    if (len < 0 || len > most) {
+      bad = true;
+      continue;
+    }
+    total[i] = totals[b];
+    const bool cut = total[i] == leads[b];  // only the last tokens go, or none
+    first[i] = cut ? pages_of(p, total[i]) : leads[b] >> p.page_log2;
+    fresh[i] = pages_of(p, total[i]) - first[i];
+    moves[i] = cut ? 0 : total[i] - (first[i] << p.page_log2);
+    sum[0] += fresh[i];
+    sum[1] += moves[i];
+  }
+  scan_requests(sum, before, all);
+  const bool any_bad = __syncthreads_or(bad);
+  const int status = any_bad                      ? HEATKV_PAGED_BAD_LENGTH
+                     : !ring_fits(p, head, count) ? HEATKV_PAGED_BAD_FREE_LIST
+                     : all[1] > a.max_moves       ? HEATKV_PAGED_TOO_MANY_TOKENS
+                     : all[0] > count             ? HEATKV_PAGED_NO_PAGES
+                                                  : HEATKV_PAGED_OK;
+  const bool ok = status == HEATKV_PAGED_OK;
+#pragma unroll
+  for (int i = 0; i < PER_LANE; ++i) {
+    const int b = tid * per + i;
+    if (i >= per || b >= B) continue;
+    a.take0[b] = ok ? static_cast<int>(before[0]) : 0;
+    a.move0[b] = ok && moves[i] > 0 ? static_cast<int>(before[1]) : -1;
+    a.first[b] = first[i];
+    p.next[b] = ok ? total[i] : p.lens[b];
+    before[0] += fresh[i];
+    before[1] += moves[i];
+  }
+  if (tid == 0) {
+    p.state[HEAD] = head;
+    p.state[COUNT] = count;
+    p.state[TAKEN] = ok ? static_cast<int>(all[0]) : 0;
+    p.state[STATUS] = status;
+    p.state[MOVES] = ok ? static_cast<int>(all[1]) : 0;
+    p.status[0] = status;
+  }
+}
+
+// Tables and the list of moves.  A workgroup reads the entries of its stretch's columns before it writes them, and nobody else
+// reads or writes these.
+__device__ __forceinline__ void compact_emit(const CompactArgs& a, Group g) {
+  const TableArgs& p = a.t;
+  __shared__ int entries[CHUNK / paged::GRANULE];
+  __shared__ int part[EMIT_LANES / 64], base_part[EMIT_LANES / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lp = p.page_log2, page = 1 << lp;
+  const int total_moves = p.state[MOVES];
+  for (long long m = total_moves + static_cast<long long>(g.index) * EMIT_LANES + tid; m < a.max_moves;
+       m += static_cast<long long>(g.count) * EMIT_LANES)
+    a.move_from[m] = a.move_to[m] = -1;
+  const Stretch s = stretch_of(a, g);
+  if (p.state[STATUS] || s.first >= s.end) return;
+  const int first = a.first[s.b], head = p.state[HEAD], take0 = a.take0[s.b], move0 = a.move0[s.b];
+  const int held = pages_of(p, p.lens[s.b]), want = pages_of(p, p.next[s.b]);
+  if ((static_cast<long long>(first) << lp) >= s.end) return;  // all of it stays where it is
+  const unsigned char* const kept = a.kept + s.b * most_tokens(p);
+  int* const row = p.table + static_cast<long long>(s.b) * p.max_pages;
+  // tokens that are kept before the stretch
+  int base = 0;
+  for (int i = tid; i < s.tile; i += EMIT_LANES) base += a.counts[g.index - s.tile + i];
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) base += __shfl_xor(base, m, 64);
+  if (lane == 0) base_part[wave] = base;
+  constexpr int ROUNDS = CHUNK / EMIT_LANES;
+  for (int x0 = s.first; x0 < s.end; x0 += CHUNK) {
+    __syncthreads();  // base_part is there; entries and part are free again
+    if (x0 == s.first) {
+      base = 0;
+#pragma unroll
+      for (int i = 0; i < EMIT_LANES / 64; ++i) base += base_part[i];
+    }
+    // a wavefront has 64 tokens a round, next to one another
+    const int w0 = x0 + wave * (CHUNK / (EMIT_LANES / 64)) + lane;
+    unsigned long long mask[ROUNDS];
+    int mine = 0;
+    unsigned char byte[ROUNDS];
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i) byte[i] = w0 + 64 * i < s.end ? kept[w0 + 64 * i] : 0;
+    const int c0 = x0 >> lp, columns = CHUNK >> lp;
+    int entry = 0;
+    const int c = c0 + tid;
+    const bool changes = tid < columns && c >= first && c < held;
+    if (changes) entries[tid] = entry = in_range(p, row[c]);
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i) {
+      mask[i] = __ballot(byte[i] != 0);
+      mine += __popcll(mask[i]);
+    }
+    if (lane == 0) part[wave] = mine;
+    __syncthreads();
+    if (changes) {
+      let_go(p, entry);
+      if (c < want) {
+        const int fresh = ring_at(p, head, take0 + c - first);
+        row[c] = fresh;
+        take(p, fresh);
+      }
+    }
+    int to = base;
+#pragma unroll
+    for (int i = 0; i < EMIT_LANES / 64; ++i) {
+      to += i < wave ? part[i] : 0;
+      base += part[i];
+    }
+    if (move0 < 0) continue;  // only its last tokens go
+#pragma unroll
+    for (int i = 0; i < ROUNDS; ++i) {
+      const int x = w0 + 64 * i;
+      if ((mask[i] >> lane & 1) && (x >> lp) >= first) {
+        const int y = to + __popcll(mask[i] & ((1ull << lane) - 1)), m = move0 + y - (first << lp);
+        a.move_from[m] = (entries[(x >> lp) - c0] << lp) + (x & (page - 1));
+        a.move_to[m] = (in_range(p, ring_at(p, head, take0 + (y >> lp) - first)) << lp) + (y & (page - 1));
+      }
+      to += __popcll(mask[i]);
+    }
+  }
+}
+
+__global__ __launch_bounds__(EMIT_LANES) void paged_compact_count_kernel(CompactArgs a) { compact_count(a, group()); }
+__global__ __launch_bounds__(LANES) void paged_compact_plan_kernel(CompactArgs a) { compact_plan(a); }
+__global__ __launch_bounds__(EMIT_LANES) void paged_compact_emit_kernel(CompactArgs a) { compact_emit(a, group()); }
+
+hipError_t launch_give_back(const TableArgs& p, hipStream_t stream) {
+  const int groups = ((p.num_pages + 31) / 32 + PART - 1) / PART;
+  hipLaunchKernelGGL(paged_give_back_kernel, dim3(groups), dim3(LANES), 0, stream, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_fork(const ForkArgs& f, hipStream_t stream) {
+  int columns_log2 = 6;
+  while (columns_log2 > 0 && f.t.batch << columns_log2 > FORK_ENTRIES) --columns_log2;
+  const unsigned groups = static_cast<unsigned>((f.t.max_pages + (1 << columns_log2) - 1) >> columns_log2);
+  hipLaunchKernelGGL(paged_fork_gains_kernel, dim3(groups), dim3(FORK_LANES), 0, stream, f, columns_log2);
+  if (hipError_t e = hipGetLastError()) return e;
+  hipLaunchKernelGGL(paged_fork_rows_kernel, dim3(groups), dim3(FORK_LANES), 0, stream, f, columns_log2);
+  if (hipError_t e = hipGetLastError()) return e;
+  return launch_give_back(f.t, stream);
+}
+
+hipError_t launch_paged_assign_shared(const AssignSharedArgs& a, hipStream_t stream) {
+  const int words = (a.t.num_pages + 31) / 32;
+  hipLaunchKernelGGL(paged_assign_plan_kernel, dim3(1 + std::min((words + LANES - 1) / LANES, 64)), dim3(LANES), 0, stream, a);
+  if (hipError_t e = hipGetLastError()) return e;
+  const long long work = std::max<long long>(a.max_tokens, static_cast<long long>(a.t.batch) << a.t.page_log2);
+  hipLaunchKernelGGL(paged_assign_move_kernel, dim3(static_cast<unsigned>(std::min<long long>((work + LANES - 1) / LANES + a.t.batch / 32, 128))),
+                     dim3(LANES), 0, stream, a);
+  if (hipError_t e = hipGetLastError()) return e;
+  return launch_give_back(a.t, stream);
+}
+
+hipError_t launch_paged_compact(const CompactArgs& a, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(a.t.batch) * a.tiles);
+  hipLaunchKernelGGL(paged_compact_count_kernel, grid, dim3(EMIT_LANES), 0, stream, a);
+  if (hipError_t e = hipGetLastError()) return e;
+  hipLaunchKernelGGL(paged_compact_plan_kernel, dim3(1), dim3(LANES), 0, stream, a);
+  if (hipError_t e = hipGetLastError()) return e;
+  hipLaunchKernelGGL(paged_compact_emit_kernel, grid, dim3(EMIT_LANES), 0, stream, a);
+  if (hipError_t e = hipGetLastError()) return e;
+  return launch_give_back(a.t, stream);
+}
+
+}  // namespace heatkv

@@ -1,7 +1,7 @@
 """Binding of the paged cache's calls (include/heatkv.h, "Paged cache"): same names, argument marshalling and checks only.
 
 Token tensors are [tokens, heads, d] with any token and head stride; pages [num_pages, kv_heads, page_size, d] in the shape's
-dtype, or E4M3 codes as torch.float8_e4m3fn or torch.uint8.  Integer arrays are int32 device tensors.
+dtype, or E4M3 codes as torch.float8_e4m3fn or torch.uint8; 4-bit pages [num_pages, kv_heads, bytes of a page] are torch.uint8.  Integer arrays are int32 device tensors.
 
 Calls go through the module _heatkv_call first (csrc/call_path.cpp: the same checks without the interpreter); it declines
 whatever is not plainly in order, and the ctypes path below it names the mistake."""
@@ -10,9 +10,9 @@ from __future__ import annotations
 import ctypes as C
 
 from . import binding
-from .binding import BF16, KV_FP8_E4M3, KV_NATIVE, _check, _DTYPES, lib
+from .binding import BF16, KV_FP4_E2M1, KV_FP8_E4M3, KV_NATIVE, _check, _DTYPES, lib
 
-PAGED_OK, PAGED_NO_PAGES, PAGED_BAD_LENGTH, PAGED_TOO_MANY_TOKENS, PAGED_BAD_FREE_LIST = 0, 1, 2, 3, 4
+PAGED_OK, PAGED_NO_PAGES, PAGED_BAD_LENGTH, PAGED_TOO_MANY_TOKENS, PAGED_BAD_FREE_LIST, PAGED_BAD_PARENT = 0, 1, 2, 3, 4, 5
 
 
 class _CPagedShape(C.Structure):
@@ -45,6 +45,19 @@ def _lib():
         L.heatkv_paged_attend_selected.restype = C.c_int
         L.heatkv_paged_attend_selected.argtypes = [sp, i64, _CRows, vp, vp, vp, vp, vp, vp, C.c_int, f32, C.c_int, _CRows, vp,
                                                    vp, C.c_size_t, vp]
+        n = C.c_size_t
+        L.heatkv_paged_read.restype = C.c_int
+        L.heatkv_paged_read.argtypes = [sp, vp, i64, vp, vp, _CRows, _CRows, vp]
+        L.heatkv_paged_tables_workspace_bytes.restype = n
+        L.heatkv_paged_tables_workspace_bytes.argtypes = [sp]
+        L.heatkv_paged_fork.restype = C.c_int
+        L.heatkv_paged_fork.argtypes = [sp] + [vp] * 10 + [n, vp]
+        L.heatkv_paged_assign_shared.restype = C.c_int
+        L.heatkv_paged_assign_shared.argtypes = [sp] + [vp] * 11 + [i64] + [vp] * 4 + [n, vp]
+        L.heatkv_paged_compact.restype = C.c_int
+        L.heatkv_paged_compact.argtypes = [sp] + [vp] * 10 + [i64] + [vp] * 2 + [n, vp]
+        L.heatkv_paged_move.restype = C.c_int
+        L.heatkv_paged_move.argtypes = [sp, vp, vp, i64] + [vp] * 5
         _bound = True
     return L
 
@@ -61,7 +74,8 @@ class PagedShape:
         self.c_struct = _CPagedShape(self.q_heads, self.kv_heads, self.d, self.dtype, self.kv_format, self.page_size,
                                      self.num_pages, self.batch, self.max_pages)
         self.pages_shape = (self.num_pages, self.kv_heads, self.page_size, self.d)
-
+        if self.kv_format == KV_FP4_E2M1:
+            self.pages_shape = (self.num_pages, self.kv_heads, self.page_size * (self.d // 2 + self.d // 32))
         self.address = C.addressof(self.c_struct)
 
     @property
@@ -134,7 +148,9 @@ class _Call:
 
     def pages(self, x, name):
         torch, sh = self.torch, self.shape
-        if sh.kv_format == KV_FP8_E4M3:
+        if sh.kv_format == KV_FP4_E2M1:
+            types = (torch.uint8,)
+        elif sh.kv_format == KV_FP8_E4M3:
             types = (torch.float8_e4m3fn, torch.uint8)
         else:
             types = (torch.bfloat16 if sh.dtype == BF16 else torch.float32,)
@@ -144,6 +160,32 @@ class _Call:
         sh = self.shape
         return (self.ints(table, "table", sh.batch, sh.max_pages), self.ints(q_start, "q_start", sh.batch + 1),
                 self.ints(lens, "lens", sh.batch))
+
+    def workspace(self, ws):
+        if ws is None:
+            return None, 0
+        self.tensor(ws, "ws")
+        if not ws.is_contiguous():
+            raise ValueError("ws: tensor must be contiguous")
+        return ws.data_ptr(), ws.numel() * ws.element_size()
+
+    def bounds(self, bounds, bound_scales):
+        sh = self.shape
+        bp = sp = None
+        if bounds is not None:
+            bp = self.dense(bounds, "bounds", (self.torch.int8,), (sh.num_pages, sh.kv_heads, 2, sh.d))
+        if bound_scales is not None:
+            sp = self.dense(bound_scales, "bound_scales", (self.torch.float32,), (sh.num_pages, sh.kv_heads))
+        return bp, sp
+
+    def tables(self, lens, lens_out, holders, free_ring, free_span, free_span_out, table):
+        """Addresses in the order of the C entries."""
+        sh = self.shape
+        return (self.ints(lens, "lens", sh.batch), self.ints(lens if lens_out is None else lens_out, "lens_out", sh.batch),
+                self.ints(holders, "holders", sh.num_pages), self.ints(free_ring, "free_ring", sh.num_pages),
+                self.ints(free_span, "free_span", 2),
+                self.ints(free_span if free_span_out is None else free_span_out, "free_span_out", 2),
+                self.ints(table, "table", sh.batch, sh.max_pages))
 
     def stream(self, stream):
         return self.torch.cuda.current_stream().cuda_stream if stream is None else stream
@@ -180,11 +222,7 @@ def heatkv_paged_append(shape, slots, k_new, v_new, k_pages, v_pages, bounds=Non
     tokens = slots.shape[0]
     k, v = c.rows(k_new, "k_new", tokens, sh.kv_heads), c.rows(v_new, "v_new", tokens, sh.kv_heads)
     kp, vp = c.pages(k_pages, "k_pages"), c.pages(v_pages, "v_pages")
-    bp = sp = None
-    if bounds is not None:
-        bp = c.dense(bounds, "bounds", (c.torch.int8,), (sh.num_pages, sh.kv_heads, 2, sh.d))
-    if bound_scales is not None:
-        sp = c.dense(bound_scales, "bound_scales", (c.torch.float32,), (sh.num_pages, sh.kv_heads))
+    bp, sp = c.bounds(bounds, bound_scales)
     _check(c.lib.heatkv_paged_append(sh.ref, slots.data_ptr(), tokens, k, v, kp, vp, bp, sp, c.stream(stream)))
 
 
@@ -199,13 +237,7 @@ def _attend_operands(c, q, k_pages, v_pages, table, q_start, lens, out, ws, lse)
     operands = [tokens, qr, c.pages(k_pages, "k_pages"), c.pages(v_pages, "v_pages"), *c.requests(table, q_start, lens)]
     outr = c.rows(out, "out", tokens, sh.q_heads)
     lp = None if lse is None else c.dense(lse, "lse", (c.torch.float32,), (tokens, sh.q_heads))
-    wp, ws_bytes = None, 0
-    if ws is not None:
-        c.tensor(ws, "ws")
-        if not ws.is_contiguous():
-            raise ValueError("ws: tensor must be contiguous")
-        wp, ws_bytes = ws.data_ptr(), ws.numel() * ws.element_size()
-    return operands, outr, lp, wp, ws_bytes
+    return operands, outr, lp, *c.workspace(ws)
 
 
 def heatkv_paged_attend(shape, q, k_pages, v_pages, table, q_start, lens, sm_scale, out, ws=None, causal=True, lse=None,
@@ -249,3 +281,83 @@ def heatkv_paged_attend_selected(shape, q, k_pages, v_pages, table, q_start, len
     sel = c.ints(selected, "selected", q.shape[0], sh.kv_heads, top)
     _check(c.lib.heatkv_paged_attend_selected(sh.ref, *operands, sel, top, float(sm_scale), int(bool(causal)), outr, lp, wp, n,
                                               c.stream(stream)))
+
+
+def heatkv_paged_read(shape, slots, k_pages, v_pages, k_out, v_out, stream=None):
+    """Rows of the cache by their slots, as values of the shape's dtype; rows of slots out of range are left as they are."""
+    if _native("paged_read", shape, slots, k_pages, v_pages, k_out, v_out, stream):
+        return
+    c, sh = _Call(shape), shape
+    c.dense(slots, "slots", (c.torch.int32,))
+    if slots.dim() != 1:
+        raise ValueError("slots: expected one dimension")
+    tokens = slots.shape[0]
+    kp, vp = c.pages(k_pages, "k_pages"), c.pages(v_pages, "v_pages")
+    k, v = c.rows(k_out, "k_out", tokens, sh.kv_heads), c.rows(v_out, "v_out", tokens, sh.kv_heads)
+    _check(c.lib.heatkv_paged_read(sh.ref, slots.data_ptr(), tokens, kp, vp, k, v, c.stream(stream)))
+
+
+def paged_tables_workspace_bytes(shape):
+    return int(_lib().heatkv_paged_tables_workspace_bytes(shape.ref))
+
+
+def heatkv_paged_fork(shape, parent, lens, holders, free_ring, free_span, table, status, ws, lens_out=None, free_span_out=None,
+                      stream=None):
+    """Row b of the table continues row parent[b]; -1 ends it.  lens_out, free_span_out: None for in place."""
+    if _native("paged_fork", shape, parent, lens, holders, free_ring, free_span, table, status, ws, lens_out, free_span_out, stream):
+        return
+    c, sh = _Call(shape), shape
+    _check(c.lib.heatkv_paged_fork(sh.ref, c.ints(parent, "parent", sh.batch),
+                                   *c.tables(lens, lens_out, holders, free_ring, free_span, free_span_out, table),
+                                   c.ints(status, "status", 1), *c.workspace(ws), c.stream(stream)))
+
+
+def heatkv_paged_assign_shared(shape, keep, new_tokens, lens, holders, free_ring, free_span, table, q_start, slots, copy_from,
+                               copy_to, status, ws, lens_out=None, free_span_out=None, stream=None):
+    """One step of the allocator that leaves pages alone which several rows hold.  copy_from, copy_to [batch, page_size] list the
+    rows of such pages for heatkv_paged_move.  lens_out, free_span_out: None for in place."""
+    if _native("paged_assign_shared", shape, keep, new_tokens, lens, holders, free_ring, free_span, table, q_start, slots, copy_from,
+               copy_to, status, ws, lens_out, free_span_out, stream):
+        return
+    c, sh = _Call(shape), shape
+    args = [c.ints(keep, "keep", sh.batch), c.ints(new_tokens, "new_tokens", sh.batch),
+            *c.tables(lens, lens_out, holders, free_ring, free_span, free_span_out, table), c.ints(q_start, "q_start", sh.batch + 1)]
+    c.dense(slots, "slots", (c.torch.int32,))
+    if slots.dim() != 1:
+        raise ValueError("slots: expected one dimension")
+    _check(c.lib.heatkv_paged_assign_shared(sh.ref, *args, slots.data_ptr(), slots.shape[0],
+                                            c.ints(copy_from, "copy_from", sh.batch, sh.page_size),
+                                            c.ints(copy_to, "copy_to", sh.batch, sh.page_size), c.ints(status, "status", 1),
+                                            *c.workspace(ws), c.stream(stream)))
+
+
+def heatkv_paged_compact(shape, kept, lens, holders, free_ring, free_span, table, move_from, move_to, status, ws, lens_out=None,
+                         free_span_out=None, stream=None):
+    """Every request keeps the tokens that are marked in kept [batch, max_pages * page_size] (bool or uint8).  move_from, move_to list
+    the rows that move for heatkv_paged_move.  lens_out, free_span_out: None for in place."""
+    if _native("paged_compact", shape, kept, lens, holders, free_ring, free_span, table, move_from, move_to, status, ws, lens_out,
+               free_span_out, stream):
+        return
+    c, sh = _Call(shape), shape
+    kp = c.dense(kept, "kept", (c.torch.bool, c.torch.uint8), (sh.batch, sh.max_pages * sh.page_size))
+    tables = c.tables(lens, lens_out, holders, free_ring, free_span, free_span_out, table)
+    c.dense(move_to, "move_to", (c.torch.int32,))
+    if move_to.dim() != 1:
+        raise ValueError("move_to: expected one dimension")
+    _check(c.lib.heatkv_paged_compact(sh.ref, kp, *tables, c.ints(move_from, "move_from", move_to.shape[0]), move_to.data_ptr(),
+                                      move_to.shape[0], c.ints(status, "status", 1), *c.workspace(ws), c.stream(stream)))
+
+
+def heatkv_paged_move(shape, move_from, move_to, k_pages, v_pages, bounds=None, bound_scales=None, stream=None):
+    """Rows move_to of the cache become what rows move_from are (int32 arrays of one shape, of one or two dimensions); with bounds
+    and bound_scales also the bounds of the pages that they touch."""
+    if _native("paged_move", shape, move_from, move_to, k_pages, v_pages, bounds, bound_scales, stream):
+        return
+    c, sh = _Call(shape), shape
+    c.dense(move_to, "move_to", (c.torch.int32,))
+    if move_to.dim() not in (1, 2):
+        raise ValueError("move_to: expected one or two dimensions")
+    fp = c.ints(move_from, "move_from", *move_to.shape)
+    kp, vp = c.pages(k_pages, "k_pages"), c.pages(v_pages, "v_pages")
+    bp, sp = c.bounds(bounds, bound_scales)
+    _check(c.lib.heatkv_paged_move(sh.ref, fp, move_to.data_ptr(), move_to.numel(), kp, vp, bp, sp, c.stream(stream)))

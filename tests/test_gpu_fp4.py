@@ -1,0 +1,328 @@
+"""4-bit cache rows (E2M1 codes, a power of two for 32 channels) on the GPU against their definitions in 64 bits: rows written, read
+back and moved, page bounds, attention, attention over chosen pages.  What the cache holds is exact in bf16, so attention has the
+tolerances of the bf16 cache (test_gpu_paged.py) against the values that are held."""
+import math
+
+import pytest
+import torch
+
+import paper_2605_14877_amd as hk
+from tests import paged_reference as ref
+from tests import share_reference as sref
+from tests.test_gpu_paged import FEW, MANY, Problem, _ints
+
+pytestmark = pytest.mark.gpu
+
+
+def _pack(x):
+    """bf16 or fp32 pages [n, H, page, d] -> 4-bit pages and the values that they hold."""
+    codes, scales = sref.fp4_encode(x)
+    return sref.fp4_pack(codes, scales), sref.fp4_decode(codes, scales)
+
+
+class Fp4Problem(Problem):
+    """Problem with 4-bit pages; k and v are the values that they hold."""
+
+    def __init__(self, q_heads, kv_heads, d, page, lens, new, **more):
+        super().__init__("bf16", q_heads, kv_heads, d, page, lens, new, **more)
+        self.shape = hk.PagedShape(q_heads, kv_heads, d, page, self.num_pages, len(lens), self.max_pages, "bf16", hk.KV_FP4_E2M1)
+        self.store()
+
+    def store(self):
+        for name in "kv":
+            pages, values = _pack(getattr(self, name))
+            setattr(self, name, values.to(torch.bfloat16))
+            assert torch.equal(getattr(self, name).double().nan_to_num(7.0), values.nan_to_num(7.0))  # bf16 has them all
+            self.dev[name] = pages.cuda()
+
+
+def _score_error(q, k, sm, keys):
+    """e of test_gpu_paged.py's tolerances."""
+    d = q.shape[-1]
+    S = float(q.abs().double().amax((0, 1)) @ k.double().nan_to_num(0.0).abs().amax((0, 1, 2))) * sm
+    return 2.0 ** -24 * (d * S + 2 * 1.443 * 2 * S + keys + 64)
+
+
+CASES = [c[1:] for c in FEW + MANY if c[0] == "bf16"]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_attention(case, causal):
+    p = Fp4Problem(*case, seed=1)
+    p.check(causal, p.run(causal))
+
+
+@pytest.mark.parametrize("new", [[9, 0, 70, 2, 1], [3, 1, 2, 2, 1]])
+def test_rows_that_see_nothing_are_zeros(new):
+    p = Fp4Problem(2, 1, 64, 16, [4, 0, 20, 0, 0], new, seed=2)
+    for causal in (True, False):
+        p.check(causal, p.run(causal))
+
+
+@pytest.mark.parametrize("new", [1, 80])
+def test_the_same_call_gives_the_same_bits_and_those_of_the_values_in_bf16(new):
+    p = Fp4Problem(8, 2, 128, 16, [2000, 900], [new, 1], seed=4)
+    first = p.run(True)
+    again = p.run(True)
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    # The same products but for the order of the channels within a score: probabilities and their sum differ by e each (as in
+    # test_gpu_paged.py), which may turn the rounding of a probability (2^-8) and of the output (a step of 2^-7).
+    q = Problem("bf16", 8, 2, 128, 16, [2000, 900], [new, 1], seed=4)
+    q.dev.update(k=p.k.cuda(), v=p.v.cuda())
+    other = q.run(True)
+    real = p.q_start[-1]
+    mag, e = float(p.v.double().nan_to_num(0.0).abs().max()), _score_error(p.q[:real], p.k, p.sm, max(p.lens))
+    assert float((first[0] - other[0])[:real].double().abs().max()) <= (2.0 ** -8 + 2.0 ** -7 + 4 * e) * mag
+    assert float((first[1] - other[1])[:real].abs().max()) <= 2 * e + 2.0 ** -22 * float(other[1][:real].abs().max())
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_scores_far_apart_and_rising(new):
+    p = Fp4Problem(2, 1, 64, 16, [400], [new], seed=5, scale=3.0)
+    for i, page in enumerate(p.table[0]):
+        p.k[page] = (p.k[page].float() * (0.2 + 0.1 * i)).to(p.k.dtype)
+    p.store()
+    p.check(True, p.run(True))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [2, 70])
+def test_blocks_of_very_different_sizes(d, new):
+    # powers of two from 2^-100 to 2^8 next to one another in a row, zeros, and V up to the largest that there is
+    p = Fp4Problem(4, 2, d, 16, [300, 40], [new, 1], seed=6)
+    g = torch.Generator().manual_seed(7)
+    n = p.k.shape
+    power = torch.exp2(torch.randint(-40, 3, (n[0], n[1], n[2], d // 32), generator=g).float()).repeat_interleave(32, -1)
+    p.k = (p.k.float() * power).to(torch.bfloat16)
+    p.k[:, :, ::3, :32] = p.k[:, :, ::3, :32] * 0.0
+    power = torch.exp2(torch.randint(-110, 100, (n[0], n[1], 1, d // 32), generator=g).float()).repeat_interleave(32, -1)
+    p.v = (p.v.float() * power).to(torch.bfloat16)
+    p.store()
+    p.check(True, p.run(True))
+
+
+@pytest.mark.parametrize("new", [1, 40, 100])
+@pytest.mark.parametrize("what", ["k", "v"])
+def test_nan_blocks_behind_what_a_row_sees_do_not_reach_it(new, what):
+    # the last tokens' blocks are NaN: rows before them do not see them, rows from them on are NaN
+    p = Fp4Problem(4, 2, 128, 32, [200, 90], [new, 1], seed=8)
+    own = getattr(p, what)
+    last = p.lens[0] - 1
+    own[p.table[0][last // 32], 1, last % 32, 64:96] = math.nan
+    p.store()
+    out, lse = p.run(True)
+    clean = Fp4Problem(4, 2, 128, 32, [200, 90], [new, 1], seed=8)
+    want = clean.run(True)
+    t = p.q_start[1] - 1  # the one token that sees it, and its heads
+    seen = torch.zeros(p.tokens, 4, dtype=torch.bool, device="cuda")
+    seen[t, 2:] = True
+    assert torch.equal(lse[~seen], want[1][~seen])
+    # A row that shares a tile with the NaN has those columns computed anew, with probabilities that are not rounded to bf16.  Either
+    # result is off by A 2 e and half a step of the output (2^-8), the clean one by A 2^-8 as well (test_gpu_paged.py), A <= max |v|.
+    e, A = _score_error(p.q, clean.k, p.sm, 200), float(clean.v.double().nan_to_num(0.0).abs().max())
+    a, b = out[~seen].double(), want[0][~seen].double()
+    assert torch.all((a - b).abs() <= A * (4 * e + 2.0 ** -8) + 2.0 ** -8 * (a.abs() + b.abs()))
+    if what == "k":
+        assert out[t, 2:].isnan().all() and lse[t, 2:].isnan().all()
+    else:
+        assert out[t, 2:, 64:96].isnan().all() and not out[t, 2:, :64].isnan().any() and not out[t, 2:, 96:].isnan().any()
+        assert torch.equal(lse, want[1])
+
+
+@pytest.mark.parametrize("d,page,G,new", [(128, 32, 4, 1), (64, 16, 3, 2), (128, 16, 2, 90), (64, 64, 4, 100)])
+def test_chosen_pages(d, page, G, new):
+    H, lens = 2, [700, 300]
+    p = Fp4Problem(G * H, H, d, page, lens, [new, 1], seed=9)
+    bounds = torch.zeros(p.num_pages, H, 2, d, dtype=torch.int8)
+    scales = torch.zeros(p.num_pages, H)
+    for n, ids in zip(lens, p.table):
+        for i, x in enumerate(ids):
+            for h in range(H):
+                b, s = ref.bounds_of(p.k[x, h, :min(page, n - i * page)])
+                bounds[x, h], scales[x, h] = b, s
+    top = 5
+    selected = torch.full((p.tokens, H, top), -7, dtype=torch.int32, device="cuda")
+    d_ = p.dev
+    hk.heatkv_paged_select(p.shape, d_["q"], bounds.cuda(), scales.cuda(), d_["table"], d_["q_start"], d_["lens"], 1, 2, selected)
+    want = ref.select(p.q, bounds, scales, p.table, p.q_start, lens, page, 1, 2, top, True)
+    got = selected.cpu()
+    for t in range(p.q_start[-1]):
+        for h in range(H):
+            assert [x for x in got[t, h].tolist() if x >= 0] == want[t][h]
+    p.check(True, p.run(True, selected=selected), chosen=got.tolist())
+
+
+# ---- rows ---------------------------------------------------------------------------------------------------------------
+
+def _values(shape, seed):
+    """bf16 values with everything that a block can have."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(shape, generator=g)
+    b = x.unflatten(-1, (-1, 32))
+    n = b.shape[:-1]
+    b *= torch.exp2(torch.randint(-20, 20, n, generator=g).float())[..., None]
+    kind = torch.randint(0, 14, n, generator=g)
+    b[kind == 0] = 0.0
+    b[kind == 1] *= 2.0 ** -110                       # under the least power
+    b[kind == 2] *= 2.0 ** 110                        # over the largest
+    b[kind == 3] = torch.round(b[kind == 3] * 4) / 4 * 0.25  # many in the middle between two codes
+    quarters = torch.randint(-28, 29, b[kind == 4].shape, generator=g).float() / 4
+    b[kind == 4] = quarters
+    k = torch.nonzero(kind == 5)
+    for i, at in enumerate(k[:40]):
+        b[tuple(at)][i % 32] = [math.inf, -math.inf, math.nan, 3.3895e38][i % 4]
+    k = torch.nonzero(kind == 6)
+    b[kind == 6] = 0.01
+    for i, at in enumerate(k):                       # around 7 times a power of two
+        b[tuple(at)][3] = [7.0, 7.03125, 6.96875, -7.0][i % 4] * 2.0 ** (i % 9 - 4)
+    return b.flatten(-2).to(torch.bfloat16)
+
+
+def _cache(H, d, page, num_pages, batch=1, max_pages=1):
+    shape = hk.PagedShape(H, H, d, page, num_pages, batch, max_pages, "bf16", hk.KV_FP4_E2M1)
+    k, v = (torch.randint(0, 200, shape.pages_shape, dtype=torch.uint8, generator=torch.Generator().manual_seed(i)).cuda() for i in (1, 2))
+    return shape, k, v
+
+
+def _same(got, want):
+    return torch.equal(got.double().cpu().nan_to_num(7e300), want.nan_to_num(7e300)) and torch.equal(got.isnan().cpu(), want.isnan())
+
+
+@pytest.mark.parametrize("bounds", [False, True])
+@pytest.mark.parametrize("H,d,page,tokens", [(1, 64, 16, 1), (3, 128, 16, 70), (2, 64, 32, 300), (2, 128, 256, 400), (5, 64, 128, 999),
+                                             (8, 128, 64, 700)])
+def test_rows_are_written_and_read_back(H, d, page, tokens, bounds):
+    num_pages = ref.pages_of(tokens, page) + 2
+    shape, k, v = _cache(H, d, page, num_pages)
+    before = [k.cpu().clone(), v.cpu().clone()]
+    order = torch.randperm(num_pages, generator=torch.Generator().manual_seed(5)).tolist()
+    start = 5 if tokens > 5 else 0  # the first page's older rows stay, and are in its bounds
+    slots = [order[x // page] * page + x % page for x in range(start, start + tokens)]
+    qkv = _values((tokens + 3, 2 * H + 1, d), seed=tokens)
+    dev = qkv.cuda()
+    b = torch.full((num_pages, H, 2, d), 77, dtype=torch.int8, device="cuda") if bounds else None
+    s = torch.full((num_pages, H), 77.0, device="cuda") if bounds else None
+    ids = _ints(slots + [-1, num_pages * page, -5])
+    hk.heatkv_paged_append(shape, ids, dev[:, :H], dev[:, H:2 * H], k, v, b, s)
+    want = []
+    for name, pages, x in (("k", before[0], qkv[:tokens, :H]), ("v", before[1], qkv[:tokens, H:2 * H])):
+        codes, scales = sref.fp4_unpack(pages, page, d)
+        c, e = sref.fp4_encode(x)
+        at, r = torch.tensor(slots) // page, torch.tensor(slots) % page
+        codes[at, :, r], scales[at, :, r] = c, e
+        got_c, got_e = sref.fp4_unpack((k if name == "k" else v).cpu(), page, d)
+        assert torch.equal(got_e, scales)
+        number = (scales != 255).repeat_interleave(32, -1)
+        assert torch.equal(got_c[number], codes[number])
+        want.append(sref.fp4_decode(codes, scales))
+    out = torch.full((tokens + 3, 2 * H + 1, d), 5.0, dtype=torch.bfloat16, device="cuda")
+    hk.heatkv_paged_read(shape, ids, k, v, out[:, :H], out[:, H:2 * H])
+    at, r = torch.tensor(slots) // page, torch.tensor(slots) % page
+    assert _same(out[:tokens, :H], want[0][at, :, r]) and _same(out[:tokens, H:2 * H], want[1][at, :, r])
+    assert torch.all(out[tokens:] == 5.0) and torch.all(out[:, 2 * H:] == 5.0)
+    if bounds:
+        b, s = b.cpu(), s.cpu()
+        last = {}
+        for x in slots:
+            last[x // page] = max(last.get(x // page, 0), x % page + 1)
+        for p in range(num_pages):
+            for h in range(H):
+                if p not in last:
+                    assert torch.all(b[p, h] == 77) and s[p, h] == 77
+                    continue
+                codes, scale = ref.bounds_of(want[0][p, h, :last[p]])
+                assert torch.equal(b[p, h], codes) and s[p, h] == scale, (p, h)
+
+
+@pytest.mark.parametrize("dtype,fmt", [("f32", "NATIVE"), ("bf16", "NATIVE"), ("bf16", "FP8_E4M3"), ("bf16", "FP4_E2M1")])
+@pytest.mark.parametrize("d,page,bounds", [(64, 16, False), (128, 32, False), (64, 32, True), (128, 256, True), (128, 16, True)])
+def test_rows_are_moved_as_they_are(dtype, fmt, d, page, bounds):
+    H, num_pages = 3, 40
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    shape = hk.PagedShape(H, H, d, page, num_pages, 1, 1, dtype, getattr(hk, "KV_" + fmt))
+    g = torch.Generator().manual_seed(3)
+    store = t if fmt == "NATIVE" else torch.uint8
+    bytes_ = torch.randint(0, 120, (*shape.pages_shape[:-1], shape.pages_shape[-1] * (t.itemsize if store is t else 1)),
+                           dtype=torch.uint8, generator=g)
+    k = bytes_.view(store).cuda().contiguous()
+    v = bytes_.flip(0).contiguous().view(store).cuda()
+    # runs of rows, single rows, whole pages, in the order of their new places
+    half = num_pages // 2 * page
+    to, frm = [], []
+    for p in range(num_pages // 2, num_pages, 2):
+        n = [1, page, page // 2 + 1, 3][p // 2 % 4]
+        to += [p * page + i for i in range(n)]
+        frm += torch.randint(0, half, (n,), generator=g).tolist()
+    to += [-1, num_pages * page, -9]
+    frm += [0, 1, 2]
+    b = torch.full((num_pages, H, 2, d), 77, dtype=torch.int8, device="cuda") if bounds else None
+    s = torch.full((num_pages, H), 77.0, device="cuda") if bounds else None
+    read = [torch.zeros(num_pages * page, H, d, dtype=t, device="cuda") for _ in range(2)]
+    every = torch.arange(num_pages * page, dtype=torch.int32, device="cuda")
+    hk.heatkv_paged_read(shape, every, k, v, *read)
+    want = [x.clone() for x in read]
+    for x in want:
+        x[to[:-3]] = x[frm[:-3]]
+    hk.heatkv_paged_move(shape, _ints(frm), _ints(to), k, v, b, s)
+    hk.heatkv_paged_read(shape, every, k, v, *read)
+    for x, y in zip(read, want):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    if bounds:
+        values = want[0].cpu().view(num_pages, page, H, d)
+        last = {}
+        for x in to[:-3]:
+            last[x // page] = max(last.get(x // page, 0), x % page + 1)
+        for p in range(num_pages):
+            for h in range(H):
+                if p in last:
+                    codes, scale = ref.bounds_of(values[p, :last[p], h])
+                    assert torch.equal(b[p, h].cpu(), codes) and s[p, h] == scale, (p, h)
+                else:
+                    assert torch.all(b[p, h] == 77) and s[p, h] == 77
+
+
+@pytest.mark.parametrize("dtype,fmt", [("f32", "NATIVE"), ("bf16", "FP8_E4M3")])
+def test_rows_of_other_formats_are_read_as_values(dtype, fmt):
+    H, d, page, n = 2, 64, 32, 3
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    shape = hk.PagedShape(H, H, d, page, n, 1, 1, dtype, getattr(hk, "KV_" + fmt))
+    x = torch.randn(shape.pages_shape, generator=torch.Generator().manual_seed(1)).to(t)
+    pages = ref.to_store(x, fmt != "NATIVE")
+    out = torch.zeros(n * page, 2, H, d, dtype=t, device="cuda")
+    ids = torch.randperm(n * page, generator=torch.Generator().manual_seed(2)).to(torch.int32)
+    hk.heatkv_paged_read(shape, ids.cuda(), pages.cuda(), pages.cuda(), out[:, 0], out[:, 1])
+    want = pages.to(t).transpose(1, 2).reshape(n * page, H, d)[ids.long()]
+    assert torch.equal(out[:, 0].cpu(), want) and torch.equal(out[:, 1].cpu(), want)
+
+
+def test_addresses_beyond_32_bits():
+    # 4-bit pages of more than 4 GiB each; the request's tokens on the last of them
+    H, d, page = 8, 128, 256
+    num_pages = (1 << 32) // (H * page * 68) + 40
+    shape = hk.PagedShape(H, H, d, page, num_pages, 1, 4, "bf16", hk.KV_FP4_E2M1)
+    k, v = (torch.zeros(shape.pages_shape, dtype=torch.uint8, device="cuda") for _ in range(2))
+    assert k.numel() > 1 << 32
+    n = 700
+    x = torch.randn(2, n, H, d, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    ids = [num_pages - 1, num_pages - 9, num_pages - 4]
+    slots = _ints([ids[i // page] * page + i % page for i in range(n)])
+    hk.heatkv_paged_append(shape, slots, x[0].cuda(), x[1].cuda(), k, v)
+    got = torch.zeros(2, n, H, d, dtype=torch.bfloat16, device="cuda")
+    hk.heatkv_paged_read(shape, slots, k, v, got[0], got[1])
+    held = [sref.fp4_decode(*sref.fp4_encode(y)) for y in x]
+    assert _same(got[0], held[0]) and _same(got[1], held[1])
+    small = [torch.zeros(3 * page, H, d).index_copy_(0, torch.arange(n), y.float()).view(3, page, H, d).transpose(1, 2) for y in held]
+    for new in (1, 90):
+        q = torch.randn(new, H, d, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16)
+        out = torch.zeros(new, H, d, dtype=torch.bfloat16, device="cuda")
+        ws = torch.zeros(max(hk.paged_attend_workspace_bytes(shape, new), 16), dtype=torch.uint8, device="cuda")
+        hk.heatkv_paged_attend(shape, q.cuda(), k, v, _ints([ids + [0]]), _ints([0, new]), _ints([n]), 0.09, out, ws)
+        want, _, mag = ref.attend(q, *small, [[0, 1, 2]], [0, new], [n], page, 0.09, True)
+        r = 2.0 ** -8 + 2 * _score_error(q, small[0], 0.09, n)
+        off = (out.cpu().double() - want).abs() - (mag * r * (1 + 1e-6) + 2.0 ** -8 * (want.abs() + mag * r))
+        assert float(off.max()) <= 0
+    frm, to = slots[:3], _ints([5, 6, 7])
+    hk.heatkv_paged_move(shape, frm, to, k, v)
+    hk.heatkv_paged_read(shape, to, k, v, got[0, :3], got[1, :3])
+    assert _same(got[0, :3], held[0][:3]) and _same(got[1, :3], held[1][:3])
