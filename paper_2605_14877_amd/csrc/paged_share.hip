@@ -24,7 +24,8 @@ namespace {
 
 constexpr int LANES = 1024, WAVES = LANES / 64;
 constexpr int PER_LANE = paged::MAX_BATCH / LANES;
-constexpr int FORK_LANES = 256, FORK_ENTRIES = 8192;  // lanes of a workgroup, entries of the table that it holds in LDS
+constexpr int FORK_LANES = 256, FORK_ENTRIES = paged::MAX_BATCH;  // lanes of a workgroup, entries of the table that it may have
+constexpr int FORK_TARGET = 1024;                                // entries that it has if the batch is not larger
 constexpr int EMIT_LANES = 256, CHUNK = 4096;         // tokens that a workgroup of compact looks at together
 
 struct Group {
@@ -35,20 +36,16 @@ __device__ __forceinline__ Group group() { return {static_cast<int>(blockIdx.x),
 // Words of TableArgs::state.
 enum State { HEAD, COUNT, TAKEN, STATUS, MOVES };
 
-__device__ __forceinline__ int inclusive_scan(int v, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int u = __shfl_up(v, d, 64);
-    if (lane >= d) v += u;
-  }
-  return v;
-}
-__device__ __forceinline__ long long inclusive_scan(long long v, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const long long u = __shfl_up(v, d, 64);
-    if (lane >= d) v += u;
-  }
+// Sum over the lanes up to this one: within rows of 16 lanes, then from row to row.
+__device__ __forceinline__ int inclusive_scan(int v) {
+#define HEATKV_STEP(control, rows) v += __builtin_amdgcn_update_dpp(0, v, control, rows, 0xf, false)
+  HEATKV_STEP(0x111, 0xf);  // one lane up, then 2, 4 and 8
+  HEATKV_STEP(0x112, 0xf);
+  HEATKV_STEP(0x114, 0xf);
+  HEATKV_STEP(0x118, 0xf);
+  HEATKV_STEP(0x142, 0xa);  // lane 15 of a row to the next row: rows 1 and 3
+  HEATKV_STEP(0x143, 0xc);  // lane 31 to rows 2 and 3
+#undef HEATKV_STEP
   return v;
 }
 
@@ -93,26 +90,27 @@ __device__ __forceinline__ void clear_gone(const TableArgs& p, Group g, int lane
 
 // ---- the last phase of every call: marked pages into the ring, lengths and the ring's span ------------------------------
 
-// Workgroup g of the grid takes words [PART g, PART (g + 1)) of the bitmap, and counts those before for itself.
-constexpr int PART = 4 * LANES;
+// Workgroup g of the grid takes words [PART g, PART (g + 1)) of the bitmap, and counts those before for itself.  Its words are dealt
+// to its wavefronts in equal stretches: marked pages are often next to one another.
+constexpr int PART_LOG2 = 12, PART = 1 << PART_LOG2, PER_WAVE = PART / WAVES / 64;
 
 __device__ __forceinline__ void give_back(const TableArgs& p, Group g) {
   __shared__ int part[2][WAVES];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int words = gone_words(p), first = g.index * PART, R = p.num_pages;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int first = g.index << PART_LOG2, words = min(gone_words(p) - first, PART), R = p.num_pages;
   const int head = p.state[HEAD], count = p.state[COUNT], taken = p.state[TAKEN];
   int before = 0;
   for (int i = tid; i < first; i += LANES) before += __popc(p.gone[i]);
-  // a wavefront's words are neighbours, and a lane's
-  unsigned w[4];
+  const int each = (words + WAVES - 1) / WAVES, w0 = wave * each, w1 = min(w0 + each, words);
+  unsigned w[PER_WAVE];
   int mine = 0;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int i = first + 4 * tid + k;
-    w[k] = i < words ? p.gone[i] : 0;
+  for (int k = 0; k < PER_WAVE; ++k) {
+    const int i = w0 + 64 * k + lane;
+    w[k] = i < w1 ? p.gone[first + i] : 0;
     mine += __popc(w[k]);
   }
-  const int inc = inclusive_scan(mine, lane), earlier = inclusive_scan(before, lane);
+  const int inc = inclusive_scan(mine), earlier = inclusive_scan(before);
   if (lane == 63) {
     part[0][wave] = inc;
     part[1][wave] = earlier;
@@ -126,27 +124,23 @@ __device__ __forceinline__ void give_back(const TableArgs& p, Group g) {
     all += part[0][i];
   }
   at += all_before;
-  // Pages of a lane's words, by the wavefront: 32 lanes write the pages of one word.
-  const int start = inc - mine;
-  unsigned long long todo = __ballot(mine > 0);
   const int room = R - (count - taken);  // tables and holders that fit each other never have more to give
-  while (todo) {
-    const int from = __builtin_ctzll(todo);
-    todo &= todo - 1;
-    int nth = at + __builtin_amdgcn_readlane(start, from);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const unsigned bits = __builtin_amdgcn_readlane(w[k], from);
-      if (lane < 32 && (bits >> lane & 1)) {
-        const int i = nth + __popc(bits & ((1u << lane) - 1));
-        if (i < room) {
-          unsigned to = static_cast<unsigned>(head) + static_cast<unsigned>(count) + static_cast<unsigned>(i);  // below 3 R < 2^32
-          to -= to >= static_cast<unsigned>(R) ? R : 0;
-          to -= to >= static_cast<unsigned>(R) ? R : 0;
-          p.ring[to] = 32 * (first + 4 * (64 * wave + from) + k) + lane;
-        }
+  for (int k = 0; k < PER_WAVE; ++k) {
+    unsigned long long todo = __ballot(w[k] != 0);
+    while (todo) {  // two words, 64 pages, at a time
+      const int from = __builtin_ctzll(todo) & ~1;
+      todo &= ~(3ull << from);
+      const unsigned long long bits = static_cast<unsigned>(__builtin_amdgcn_readlane(w[k], from)) |
+                                      static_cast<unsigned long long>(static_cast<unsigned>(__builtin_amdgcn_readlane(w[k], from + 1))) << 32;
+      const int i = at + __popcll(bits & ((1ull << lane) - 1));
+      if ((bits >> lane & 1) && i < room) {
+        unsigned to = static_cast<unsigned>(head) + static_cast<unsigned>(count) + static_cast<unsigned>(i);  // below 3 R < 2^32
+        to -= to >= static_cast<unsigned>(R) ? R : 0;
+        to -= to >= static_cast<unsigned>(R) ? R : 0;
+        p.ring[to] = 32 * (first + w0 + 64 * k + from) + lane;
       }
-      nth += __popc(bits);
+      at += __popcll(bits);
     }
   }
   if (g.index == 0)
@@ -161,29 +155,51 @@ __device__ __forceinline__ void give_back(const TableArgs& p, Group g) {
 
 // ---- fork ---------------------------------------------------------------------------------------------------------------
 
-// Counts what rows gain.  Every workgroup looks at all parents and lengths for itself.
-__device__ __forceinline__ void fork_gains(const ForkArgs& f, Group g, int columns_log2) {
+// Parents, pages held and pages to be, of all rows, into LDS; every workgroup looks at all of them for itself.
+struct ForkRows {
+  short parent[paged::MAX_BATCH];
+  int held[paged::MAX_BATCH];
+};
+__device__ __forceinline__ int fork_load(const ForkArgs& f, ForkRows& r) {
   const TableArgs& p = f.t;
   const int tid = threadIdx.x, B = p.batch;
-  clear_gone(p, g, FORK_LANES);
-  const int head = p.span[0], count = p.span[1];
   const long long most = most_tokens(p);
   bool bad_parent = false, bad_length = false;
   for (int b = tid; b < B; b += FORK_LANES) {
     const int parent = f.parent[b], len = p.lens[b];
     bad_parent = bad_parent || parent < -1 || parent >= B;
     bad_length = bad_length || len < 0 || len > most;
+    r.parent[b] = static_cast<short>(parent);
+    r.held[b] = pages_of(p, len);
   }
   const bool any_length = __syncthreads_or(bad_length), any_parent = __syncthreads_or(bad_parent);
-  const int status = any_length               ? HEATKV_PAGED_BAD_LENGTH
-                     : any_parent             ? HEATKV_PAGED_BAD_PARENT
-                     : !ring_fits(p, head, count) ? HEATKV_PAGED_BAD_FREE_LIST
-                                              : HEATKV_PAGED_OK;
+  return any_length ? HEATKV_PAGED_BAD_LENGTH : any_parent ? HEATKV_PAGED_BAD_PARENT : HEATKV_PAGED_OK;
+}
+// A row's entry in a column before and after; -1: none.  Where they are equal nothing changes: most of what beams have in common.
+struct Change {
+  int before, after;
+};
+__device__ __forceinline__ Change fork_change(const TableArgs& p, const ForkRows& r, int b, int c) {
+  const int parent = r.parent[b];
+  Change x{-1, -1};
+  if (parent == b) return x;
+  if (c < r.held[b]) x.before = in_range(p, p.table[static_cast<long long>(b) * p.max_pages + c]);
+  if (parent >= 0 && c < r.held[parent]) x.after = in_range(p, p.table[static_cast<long long>(parent) * p.max_pages + c]);
+  if (x.before == x.after) x.before = x.after = -1;
+  return x;
+}
+
+// Counts what rows gain.
+__device__ __forceinline__ void fork_gains(const ForkArgs& f, Group g, int columns_log2) {
+  const TableArgs& p = f.t;
+  __shared__ ForkRows r;
+  const int tid = threadIdx.x, B = p.batch;
+  clear_gone(p, g, FORK_LANES);
+  const int head = p.span[0], count = p.span[1];
+  int status = fork_load(f, r);
+  if (status == HEATKV_PAGED_OK && !ring_fits(p, head, count)) status = HEATKV_PAGED_BAD_FREE_LIST;
   if (g.index == 0) {
-    for (int b = tid; b < B; b += FORK_LANES) {
-      const int parent = f.parent[b];
-      p.next[b] = status ? p.lens[b] : parent < 0 ? 0 : p.lens[parent];
-    }
+    for (int b = tid; b < B; b += FORK_LANES) p.next[b] = status ? p.lens[b] : r.parent[b] < 0 ? 0 : p.lens[r.parent[b]];
     if (tid == 0) {
       p.state[HEAD] = head;
       p.state[COUNT] = count;
@@ -193,32 +209,29 @@ __device__ __forceinline__ void fork_gains(const ForkArgs& f, Group g, int colum
     }
   }
   if (status) return;
-  const int c0 = g.index << columns_log2;
   for (int i = tid; i < B << columns_log2; i += FORK_LANES) {
-    const int b = i >> columns_log2, c = c0 + (i & ((1 << columns_log2) - 1)), parent = f.parent[b];
-    if (parent == b || parent < 0 || c >= pages_of(p, p.lens[parent])) continue;
-    atomicAdd(&p.holders[in_range(p, p.table[static_cast<long long>(parent) * p.max_pages + c])], 1);
+    const Change x = fork_change(p, r, i >> columns_log2, (g.index << columns_log2) + (i & ((1 << columns_log2) - 1)));
+    if (x.after >= 0) atomicAdd(&p.holders[x.after], 1);
   }
 }
 
 // A workgroup has some columns of all rows: it reads them before it writes any, and nobody else does either.
 __device__ __forceinline__ void fork_rows(const ForkArgs& f, Group g, int columns_log2) {
   const TableArgs& p = f.t;
-  __shared__ int held[FORK_ENTRIES];
-  if (p.state[STATUS]) return;
+  __shared__ ForkRows r;
+  __shared__ int after[FORK_ENTRIES];
+  const int status = p.state[STATUS];
+  fork_load(f, r);
+  if (status) return;
   const int tid = threadIdx.x, c0 = g.index << columns_log2, entries = p.batch << columns_log2;
-  auto row = [&](int b) { return p.table + static_cast<long long>(b) * p.max_pages; };
   for (int i = tid; i < entries; i += FORK_LANES) {
-    const int b = i >> columns_log2, c = c0 + (i & ((1 << columns_log2) - 1)), parent = f.parent[b];
-    if (parent == b) continue;
-    if (parent >= 0 && c < pages_of(p, p.lens[parent])) held[i] = row(parent)[c];
-    if (c < pages_of(p, p.lens[b])) let_go(p, row(b)[c]);
+    const Change x = fork_change(p, r, i >> columns_log2, c0 + (i & ((1 << columns_log2) - 1)));
+    after[i] = x.after;
+    if (x.before >= 0) let_go(p, x.before);
   }
   __syncthreads();
-  for (int i = tid; i < entries; i += FORK_LANES) {
-    const int b = i >> columns_log2, c = c0 + (i & ((1 << columns_log2) - 1)), parent = f.parent[b];
-    if (parent != b && parent >= 0 && c < pages_of(p, p.lens[parent])) row(b)[c] = held[i];
-  }
+  for (int i = tid; i < entries; i += FORK_LANES)
+    if (after[i] >= 0) p.table[static_cast<long long>(i >> columns_log2) * p.max_pages + c0 + (i & ((1 << columns_log2) - 1))] = after[i];
 }
 
 __global__ __launch_bounds__(FORK_LANES) void paged_fork_gains_kernel(ForkArgs f, int columns_log2) { fork_gains(f, group(), columns_log2); }
@@ -227,14 +240,15 @@ __global__ __launch_bounds__(LANES) void paged_give_back_kernel(TableArgs p) { g
 
 // ---- assign -------------------------------------------------------------------------------------------------------------
 
-// Sums over the requests before of N numbers that each lane has for its PER_LANE consecutive requests; `all`: of all.
+// Sums over the requests before of N numbers that each lane has for its PER_LANE consecutive requests; `all`: of all.  Those of a
+// wavefront's lanes are below 2^31 together.
 template <int N>
-__device__ __forceinline__ void scan_requests(const long long (&sum)[N], long long (&before)[N], long long (&all)[N]) {
-  __shared__ long long part[N][WAVES];
+__device__ __forceinline__ void scan_requests(const int (&sum)[N], long long (&before)[N], long long (&all)[N]) {
+  __shared__ int part[N][WAVES];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int k = 0; k < N; ++k) {
-    const long long inc = inclusive_scan(sum[k], lane);
+    const int inc = inclusive_scan(sum[k]);
     before[k] = inc - sum[k];
     all[k] = 0;
     if (lane == 63) part[k][wave] = inc;
@@ -244,7 +258,7 @@ __device__ __forceinline__ void scan_requests(const long long (&sum)[N], long lo
   for (int k = 0; k < N; ++k)
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-      const long long x = part[k][w];
+      const int x = part[k][w];
       if (w < wave) before[k] += x;
       all[k] += x;
     }
@@ -262,8 +276,9 @@ __device__ __forceinline__ void assign_plan(const AssignSharedArgs& a, Group g) 
   const long long most = most_tokens(p);
   const int per = (B + LANES - 1) / LANES;
   int first[PER_LANE], fresh[PER_LANE], touched[PER_LANE], come[PER_LANE], next[PER_LANE], old[PER_LANE];
-  long long sum[3] = {0, 0, 0}, before[3], all[3];  // pages to take, columns to look at, tokens
-  bool bad = false;
+  int sum[3] = {0, 0, 0};  // pages to take, columns to look at, tokens
+  long long before[3], all[3];
+  bool bad = false, many = false;
 #pragma unroll
   for (int i = 0; i < PER_LANE; ++i) {
     const int b = tid * per + i;
@@ -277,7 +292,8 @@ __device__ __forceinline__ void assign_plan(const AssignSharedArgs& a, Group g) 
       continue;
     }
     first[i] = pages_of(p, keep);
-    come[i] = n;
+    many = many || n > a.max_tokens;
+    come[i] = static_cast<int>(min(static_cast<long long>(n), a.max_tokens + 1));  // 2^22 + 1 at the most: 256 of them fit an int
     next[i] = keep + n;
     if (n > 0 && (keep & (page - 1))) {
       const int last = in_range(p, p.table[static_cast<long long>(b) * p.max_pages + first[i] - 1]);
@@ -297,10 +313,10 @@ __device__ __forceinline__ void assign_plan(const AssignSharedArgs& a, Group g) 
     sum[2] += come[i];
   }
   scan_requests(sum, before, all);
-  const bool any_bad = __syncthreads_or(bad);
+  const bool any_bad = __syncthreads_or(bad), any_many = __syncthreads_or(many);
   const int status = any_bad                      ? HEATKV_PAGED_BAD_LENGTH
                      : !ring_fits(p, head, count) ? HEATKV_PAGED_BAD_FREE_LIST
-                     : all[2] > a.max_tokens      ? HEATKV_PAGED_TOO_MANY_TOKENS
+                     : any_many || all[2] > a.max_tokens ? HEATKV_PAGED_TOO_MANY_TOKENS
                      : all[0] > count             ? HEATKV_PAGED_NO_PAGES
                                                   : HEATKV_PAGED_OK;
   const bool ok = status == HEATKV_PAGED_OK;
@@ -460,7 +476,9 @@ __device__ __forceinline__ void compact_plan(const CompactArgs& a) {
   __syncthreads();
   const int per = (B + LANES - 1) / LANES;
   int first[PER_LANE], fresh[PER_LANE], moves[PER_LANE], total[PER_LANE];
-  long long sum[2] = {0, 0}, before[2], all[2];  // pages to take, rows to move
+  int sum[2] = {0, 0};  // pages to take, rows to move
+  long long before[2], all[2];
+  bool many = false;
   bool bad = false;
 #pragma unroll
   for (int i = 0; i < PER_LANE; ++i) {
@@ -477,14 +495,15 @@ __device__ __forceinline__ void compact_plan(const CompactArgs& a) {
     first[i] = cut ? pages_of(p, total[i]) : leads[b] >> p.page_log2;
     fresh[i] = pages_of(p, total[i]) - first[i];
     moves[i] = cut ? 0 : total[i] - (first[i] << p.page_log2);
+    many = many || moves[i] > a.max_moves;
     sum[0] += fresh[i];
-    sum[1] += moves[i];
+    sum[1] += static_cast<int>(min(static_cast<long long>(moves[i]), a.max_moves + 1));  // see assign_plan()
   }
   scan_requests(sum, before, all);
-  const bool any_bad = __syncthreads_or(bad);
+  const bool any_bad = __syncthreads_or(bad), any_many = __syncthreads_or(many);
   const int status = any_bad                      ? HEATKV_PAGED_BAD_LENGTH
                      : !ring_fits(p, head, count) ? HEATKV_PAGED_BAD_FREE_LIST
-                     : all[1] > a.max_moves       ? HEATKV_PAGED_TOO_MANY_TOKENS
+                     : any_many || all[1] > a.max_moves ? HEATKV_PAGED_TOO_MANY_TOKENS
                      : all[0] > count             ? HEATKV_PAGED_NO_PAGES
                                                   : HEATKV_PAGED_OK;
   const bool ok = status == HEATKV_PAGED_OK;
@@ -513,46 +532,55 @@ __device__ __forceinline__ void compact_plan(const CompactArgs& a) {
 // reads or writes these.
 __device__ __forceinline__ void compact_emit(const CompactArgs& a, Group g) {
   const TableArgs& p = a.t;
-  __shared__ int entries[CHUNK / paged::GRANULE];
-  __shared__ int part[EMIT_LANES / 64], base_part[EMIT_LANES / 64];
+  constexpr int COLUMNS = CHUNK / paged::GRANULE, GROUP_WAVES = EMIT_LANES / 64, ROUNDS = CHUNK / EMIT_LANES;
+  __shared__ int entries[COLUMNS], fresh[COLUMNS + 1];  // of the chunk's columns, of those that its tokens go to
+  __shared__ int part[GROUP_WAVES], base_part[GROUP_WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lp = p.page_log2, page = 1 << lp;
-  const int total_moves = p.state[MOVES];
+  const int total_moves = p.state[MOVES], status = p.state[STATUS], head = p.state[HEAD];
+  const Stretch s = stretch_of(a, g);
+  const int first = a.first[s.b], take0 = a.take0[s.b], move0 = a.move0[s.b];
+  const int held = pages_of(p, p.lens[s.b]), want = pages_of(p, p.next[s.b]);
   for (long long m = total_moves + static_cast<long long>(g.index) * EMIT_LANES + tid; m < a.max_moves;
        m += static_cast<long long>(g.count) * EMIT_LANES)
     a.move_from[m] = a.move_to[m] = -1;
-  const Stretch s = stretch_of(a, g);
-  if (p.state[STATUS] || s.first >= s.end) return;
-  const int first = a.first[s.b], head = p.state[HEAD], take0 = a.take0[s.b], move0 = a.move0[s.b];
-  const int held = pages_of(p, p.lens[s.b]), want = pages_of(p, p.next[s.b]);
+  if (status || s.first >= s.end) return;
   if ((static_cast<long long>(first) << lp) >= s.end) return;  // all of it stays where it is
   const unsigned char* const kept = a.kept + s.b * most_tokens(p);
   int* const row = p.table + static_cast<long long>(s.b) * p.max_pages;
   // tokens that are kept before the stretch
   int base = 0;
   for (int i = tid; i < s.tile; i += EMIT_LANES) base += a.counts[g.index - s.tile + i];
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) base += __shfl_xor(base, m, 64);
-  if (lane == 0) base_part[wave] = base;
-  constexpr int ROUNDS = CHUNK / EMIT_LANES;
+  base = inclusive_scan(base);
+  if (lane == 63) base_part[wave] = base;
   for (int x0 = s.first; x0 < s.end; x0 += CHUNK) {
-    __syncthreads();  // base_part is there; entries and part are free again
-    if (x0 == s.first) {
-      base = 0;
-#pragma unroll
-      for (int i = 0; i < EMIT_LANES / 64; ++i) base += base_part[i];
-    }
     // a wavefront has 64 tokens a round, next to one another
-    const int w0 = x0 + wave * (CHUNK / (EMIT_LANES / 64)) + lane;
-    unsigned long long mask[ROUNDS];
-    int mine = 0;
+    const int w0 = x0 + wave * (CHUNK / GROUP_WAVES) + lane;
     unsigned char byte[ROUNDS];
 #pragma unroll
     for (int i = 0; i < ROUNDS; ++i) byte[i] = w0 + 64 * i < s.end ? kept[w0 + 64 * i] : 0;
-    const int c0 = x0 >> lp, columns = CHUNK >> lp;
-    int entry = 0;
-    const int c = c0 + tid;
+    const int c0 = x0 >> lp, columns = CHUNK >> lp, c = c0 + tid;
     const bool changes = tid < columns && c >= first && c < held;
-    if (changes) entries[tid] = entry = in_range(p, row[c]);
+    const int entry = changes ? in_range(p, row[c]) : 0;
+    __syncthreads();  // base_part is there; the arrays are free again
+    if (x0 == s.first) {
+      base = 0;
+#pragma unroll
+      for (int i = 0; i < GROUP_WAVES; ++i) base += base_part[i];
+    }
+    const int to0 = max(base >> lp, first);  // column of the chunk's first token that moves
+    for (int i = tid; i <= columns; i += EMIT_LANES)
+      if (to0 + i < want) fresh[i] = in_range(p, ring_at(p, head, take0 + to0 + i - first));
+    if (changes) {
+      entries[tid] = entry;
+      let_go(p, entry);
+      if (c < want) {
+        const int mine = ring_at(p, head, take0 + c - first);
+        row[c] = mine;
+        take(p, mine);
+      }
+    }
+    unsigned long long mask[ROUNDS];
+    int mine = 0;
 #pragma unroll
     for (int i = 0; i < ROUNDS; ++i) {
       mask[i] = __ballot(byte[i] != 0);
@@ -560,17 +588,9 @@ __device__ __forceinline__ void compact_emit(const CompactArgs& a, Group g) {
     }
     if (lane == 0) part[wave] = mine;
     __syncthreads();
-    if (changes) {
-      let_go(p, entry);
-      if (c < want) {
-        const int fresh = ring_at(p, head, take0 + c - first);
-        row[c] = fresh;
-        take(p, fresh);
-      }
-    }
     int to = base;
 #pragma unroll
-    for (int i = 0; i < EMIT_LANES / 64; ++i) {
+    for (int i = 0; i < GROUP_WAVES; ++i) {
       to += i < wave ? part[i] : 0;
       base += part[i];
     }
@@ -581,7 +601,7 @@ __device__ __forceinline__ void compact_emit(const CompactArgs& a, Group g) {
       if ((mask[i] >> lane & 1) && (x >> lp) >= first) {
         const int y = to + __popcll(mask[i] & ((1ull << lane) - 1)), m = move0 + y - (first << lp);
         a.move_from[m] = (entries[(x >> lp) - c0] << lp) + (x & (page - 1));
-        a.move_to[m] = (in_range(p, ring_at(p, head, take0 + (y >> lp) - first)) << lp) + (y & (page - 1));
+        a.move_to[m] = (fresh[(y >> lp) - to0] << lp) + (y & (page - 1));
       }
       to += __popcll(mask[i]);
     }
@@ -602,7 +622,7 @@ hipError_t launch_give_back(const TableArgs& p, hipStream_t stream) {
 
 hipError_t launch_paged_fork(const ForkArgs& f, hipStream_t stream) {
   int columns_log2 = 6;
-  while (columns_log2 > 0 && f.t.batch << columns_log2 > FORK_ENTRIES) --columns_log2;
+  while (columns_log2 > 0 && f.t.batch << columns_log2 > FORK_TARGET) --columns_log2;
   const unsigned groups = static_cast<unsigned>((f.t.max_pages + (1 << columns_log2) - 1) >> columns_log2);
   hipLaunchKernelGGL(paged_fork_gains_kernel, dim3(groups), dim3(FORK_LANES), 0, stream, f, columns_log2);
   if (hipError_t e = hipGetLastError()) return e;
