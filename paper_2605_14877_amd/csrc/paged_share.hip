@@ -153,6 +153,19 @@ __device__ __forceinline__ void give_back(const TableArgs& p, Group g) {
   }
 }
 
+// Small calls are one workgroup and one launch, which has the workspace in LDS.
+constexpr int SMALL_BATCH = 1024, SMALL_PAGES = 32 * PART;
+template <int BATCH, int PAGES>
+struct Small {
+  int state[8], next[BATCH];
+  uint32_t gone[PAGES / 32];
+  __device__ __forceinline__ void lend(TableArgs& p) {
+    p.state = state;
+    p.next = next;
+    p.gone = gone;
+  }
+};
+
 // ---- fork ---------------------------------------------------------------------------------------------------------------
 
 // Parents, pages held and pages to be, of all rows, into LDS; every workgroup looks at all of them for itself.
@@ -236,6 +249,72 @@ __device__ __forceinline__ void fork_rows(const ForkArgs& f, Group g, int column
 
 __global__ __launch_bounds__(FORK_LANES) void paged_fork_gains_kernel(ForkArgs f, int columns_log2) { fork_gains(f, group(), columns_log2); }
 __global__ __launch_bounds__(FORK_LANES) void paged_fork_rows_kernel(ForkArgs f, int columns_log2) { fork_rows(f, group(), columns_log2); }
+// All phases by one workgroup, whose lanes have up to SMALL_EACH entries of the table each.
+constexpr int SMALL_EACH = 16;
+__global__ __launch_bounds__(LANES) void paged_fork_small_kernel(ForkArgs f) {
+  __shared__ Small<SMALL_BATCH, SMALL_PAGES> s;
+  __shared__ short parents[SMALL_BATCH];
+  __shared__ int lens[SMALL_BATCH];
+  s.lend(f.t);
+  const TableArgs& p = f.t;
+  const int tid = threadIdx.x, B = p.batch;
+  const int head = p.span[0], count = p.span[1];
+  clear_gone(p, {0, 1}, LANES);
+  bool bad_parent = false, bad_length = false;
+  if (tid < B) {
+    const int parent = f.parent[tid], len = p.lens[tid];
+    bad_parent = parent < -1 || parent >= B;
+    bad_length = len < 0 || len > most_tokens(p);
+    parents[tid] = static_cast<short>(parent);
+    lens[tid] = len;
+  }
+  const bool any_length = __syncthreads_or(bad_length), any_parent = __syncthreads_or(bad_parent);
+  const int status = any_length                   ? HEATKV_PAGED_BAD_LENGTH
+                     : any_parent                 ? HEATKV_PAGED_BAD_PARENT
+                     : !ring_fits(p, head, count) ? HEATKV_PAGED_BAD_FREE_LIST
+                                                  : HEATKV_PAGED_OK;
+  if (tid < B) p.next[tid] = status ? lens[tid] : parents[tid] < 0 ? 0 : lens[parents[tid]];
+  if (tid == 0) {
+    p.state[HEAD] = head;
+    p.state[COUNT] = count;
+    p.state[TAKEN] = 0;
+    p.state[STATUS] = status;
+    p.status[0] = status;
+  }
+  if (!status) {
+    int before[SMALL_EACH], after[SMALL_EACH];
+    const int entries = B * p.max_pages;
+#pragma unroll
+    for (int k = 0; k < SMALL_EACH; ++k) {
+      const int i = k * LANES + tid;
+      before[k] = after[k] = -1;
+      if (i >= entries) continue;
+      const int b = i / p.max_pages, c = i - b * p.max_pages, parent = parents[b];
+      if (parent == b) continue;
+      if (c < pages_of(p, lens[b])) before[k] = p.table[i];
+      if (parent >= 0 && c < pages_of(p, lens[parent])) after[k] = p.table[parent * p.max_pages + c];
+    }
+#pragma unroll
+    for (int k = 0; k < SMALL_EACH; ++k) {
+      const int i = k * LANES + tid, b = i / p.max_pages, c = i - b * p.max_pages;
+      const bool has = i < entries && parents[b] != b;
+      before[k] = has && c < pages_of(p, lens[b]) ? in_range(p, before[k]) : -1;
+      after[k] = has && parents[b] >= 0 && c < pages_of(p, lens[parents[b]]) ? in_range(p, after[k]) : -1;
+      if (before[k] == after[k]) before[k] = after[k] = -1;
+      if (after[k] >= 0) atomicAdd(&p.holders[after[k]], 1);
+    }
+    wait_vmcnt<0>();  // counted, before anything is counted down; and all entries have been read
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < SMALL_EACH; ++k) {
+      if (before[k] >= 0) let_go(p, before[k]);
+      if (after[k] >= 0) p.table[k * LANES + tid] = after[k];
+    }
+  }
+  __syncthreads();
+  give_back(p, {0, 1});
+}
+
 __global__ __launch_bounds__(LANES) void paged_give_back_kernel(TableArgs p) { give_back(p, group()); }
 
 // ---- assign -------------------------------------------------------------------------------------------------------------
@@ -345,16 +424,11 @@ __device__ __forceinline__ void assign_plan(const AssignSharedArgs& a, Group g) 
   }
 }
 
-__device__ __forceinline__ void assign_move(const AssignSharedArgs& a, Group g) {
+// touch0, q0: those of `a`, in LDS.
+__device__ __forceinline__ void assign_move(const AssignSharedArgs& a, Group g, const int* touch0, const int* q0) {
   const TableArgs& p = a.t;
-  __shared__ int touch0[paged::MAX_BATCH], q0[paged::MAX_BATCH];
   const int tid = threadIdx.x, B = p.batch, lp = p.page_log2, page = 1 << lp;
-  for (int b = tid; b < B; b += LANES) {
-    touch0[b] = a.touch0[b];
-    q0[b] = a.q_start[b];
-  }
   const int touched = a.touch0[B], tokens = a.q_start[B], head = p.state[HEAD];
-  __syncthreads();
   const int at = g.index * LANES + tid, stride = g.count * LANES;
   auto row = [&](int b) { return p.table + static_cast<long long>(b) * p.max_pages; };
   for (int i = at; i < touched; i += stride) {
@@ -386,7 +460,34 @@ __device__ __forceinline__ void assign_move(const AssignSharedArgs& a, Group g) 
 }
 
 __global__ __launch_bounds__(LANES) void paged_assign_plan_kernel(AssignSharedArgs a) { assign_plan(a, group()); }
-__global__ __launch_bounds__(LANES) void paged_assign_move_kernel(AssignSharedArgs a) { assign_move(a, group()); }
+__global__ __launch_bounds__(LANES) void paged_assign_move_kernel(AssignSharedArgs a) {
+  __shared__ int touch0[paged::MAX_BATCH], q0[paged::MAX_BATCH];
+  for (int b = threadIdx.x; b < a.t.batch; b += LANES) {
+    touch0[b] = a.touch0[b];
+    q0[b] = a.q_start[b];
+  }
+  __syncthreads();
+  assign_move(a, group(), touch0, q0);
+}
+
+// All phases by one workgroup, what passes between them in LDS.
+__global__ __launch_bounds__(LANES) void paged_assign_small_kernel(AssignSharedArgs a) {
+  __shared__ Small<SMALL_BATCH, SMALL_PAGES> s;
+  __shared__ int take0[SMALL_BATCH], touch0[SMALL_BATCH + 1], first[SMALL_BATCH], copied[SMALL_BATCH], q0[SMALL_BATCH + 1];
+  int* const q_start = a.q_start;
+  s.lend(a.t);
+  a.take0 = take0;
+  a.touch0 = touch0;
+  a.first = first;
+  a.copied = copied;
+  a.q_start = q0;
+  assign_plan(a, {0, 1});
+  __syncthreads();
+  for (int b = threadIdx.x; b <= a.t.batch; b += LANES) q_start[b] = q0[b];
+  assign_move(a, {0, 1}, touch0, q0);
+  __syncthreads();
+  give_back(a.t, {0, 1});
+}
 
 // ---- compact ------------------------------------------------------------------------------------------------------------
 
@@ -612,15 +713,129 @@ __global__ __launch_bounds__(EMIT_LANES) void paged_compact_count_kernel(Compact
 __global__ __launch_bounds__(LANES) void paged_compact_plan_kernel(CompactArgs a) { compact_plan(a); }
 __global__ __launch_bounds__(EMIT_LANES) void paged_compact_emit_kernel(CompactArgs a) { compact_emit(a, group()); }
 
+// All phases by one workgroup: a lane has 16 tokens next to one another, on one page.
+constexpr int SMALL_TOKENS = 16 * LANES, THIN_BATCH = 256, THIN_PAGES = 65536;
+__global__ __launch_bounds__(LANES) void paged_compact_small_kernel(CompactArgs a) {
+  __shared__ Small<THIN_BATCH, THIN_PAGES> s;
+  __shared__ int kept_before[LANES], entries[LANES], part[WAVES];
+  __shared__ int take0[THIN_BATCH], move0[THIN_BATCH], first[THIN_BATCH], leads[THIN_BATCH];
+  __shared__ unsigned short stays[SMALL_TOKENS];  // tokens that move, by their places in `kept`
+  s.lend(a.t);
+  const TableArgs& p = a.t;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, B = p.batch, lp = p.page_log2, page = 1 << lp;
+  const int head = p.span[0], count = p.span[1], width = p.max_pages << lp;
+  clear_gone(p, {0, 1}, LANES);
+  // this lane's tokens
+  const bool real = 16 * tid < B * width;
+  const int b = real ? 16 * tid / width : 0, x0 = 16 * tid - b * width;
+  const int here = real ? min(max(max(p.lens[b], 0) - x0, 0), 16) : 0;
+  unsigned mask = 0;
+  if (here > 0) {
+    const uint4 raw = ldg16(a.kept + 16 * tid);
+    const unsigned w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mask |= (w[i >> 2] >> 8 * (i & 3) & 0xff) ? 1u << i : 0;
+    mask &= (1u << here) - 1;
+  }
+  int entry = 0;
+  if (here > 0) entry = in_range(p, p.table[b * p.max_pages + (x0 >> lp)]);
+  if (tid < B) leads[tid] = INT_MAX;
+  const int mine = __popc(mask), inc = inclusive_scan(mine);
+  if (lane == 63) part[wave] = inc;
+  __syncthreads();
+  int earlier = inc - mine, whole = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    earlier += w < wave ? part[w] : 0;
+    whole += part[w];
+  }
+  kept_before[tid] = earlier;
+  entries[tid] = entry;
+  const unsigned none = ~mask & ((1u << here) - 1);
+  if (none) atomicMin(&leads[b], x0 + __builtin_ctz(none));
+  __syncthreads();
+  // the requests, one to a lane
+  int fresh = 0, moves = 0, total = 0, from = 0;
+  bool bad = false;
+  if (tid < B) {
+    const int n = p.lens[tid], end = (tid + 1) * width / 16;
+    bad = n < 0 || n > width;
+    if (!bad) {
+      total = (end < LANES ? kept_before[end] : whole) - kept_before[tid * width / 16];
+      const int lead = min(leads[tid], n);
+      const bool cut = total == lead;
+      from = cut ? pages_of(p, total) : lead >> lp;
+      fresh = pages_of(p, total) - from;
+      moves = cut ? 0 : total - (from << lp);
+    }
+  }
+  const int sum[2] = {fresh, moves};
+  long long before[2], all[2];
+  scan_requests(sum, before, all);
+  const bool any_bad = __syncthreads_or(bad);
+  const int status = any_bad                      ? HEATKV_PAGED_BAD_LENGTH
+                     : !ring_fits(p, head, count) ? HEATKV_PAGED_BAD_FREE_LIST
+                     : all[1] > a.max_moves       ? HEATKV_PAGED_TOO_MANY_TOKENS
+                     : all[0] > count             ? HEATKV_PAGED_NO_PAGES
+                                                  : HEATKV_PAGED_OK;
+  if (tid < B) {
+    take0[tid] = static_cast<int>(before[0]);
+    move0[tid] = moves > 0 ? static_cast<int>(before[1]) : -1;
+    first[tid] = from;
+    p.next[tid] = status ? p.lens[tid] : total;
+  }
+  const int listed = status ? 0 : static_cast<int>(all[1]);
+  if (tid == 0) {
+    p.state[HEAD] = head;
+    p.state[COUNT] = count;
+    p.state[TAKEN] = status ? 0 : static_cast<int>(all[0]);
+    p.state[STATUS] = status;
+    p.status[0] = status;
+  }
+  __syncthreads();
+  const int c = x0 >> lp, start = first[b];
+  if (!status && here > 0 && c >= start) {
+    if ((x0 & (page - 1)) == 0) {
+      let_go(p, entry);
+      if (c < pages_of(p, p.next[b])) {
+        const int page_now = ring_at(p, head, take0[b] + c - start);
+        p.table[b * p.max_pages + c] = page_now;
+        take(p, page_now);
+      }
+    }
+    if (move0[b] >= 0) {
+      int m = move0[b] + earlier - kept_before[b * width / 16] - (start << lp);
+      for (unsigned bits = mask; bits; bits &= bits - 1) stays[m++] = static_cast<unsigned short>(16 * tid + __builtin_ctz(bits));
+    }
+  }
+  __syncthreads();
+  for (int m = tid; m < listed; m += LANES) {
+    const int at = stays[m], request = at / width, y = m - move0[request] + (first[request] << lp);
+    a.move_from[m] = (entries[at >> 4] << lp) + (at & (page - 1));  // `width` is a multiple of the page
+    a.move_to[m] = (in_range(p, ring_at(p, head, take0[request] + (y >> lp) - first[request])) << lp) + (y & (page - 1));
+  }
+  for (long long m = listed + tid; m < a.max_moves; m += LANES) a.move_from[m] = a.move_to[m] = -1;
+  __syncthreads();
+  give_back(p, {0, 1});
+}
+
 hipError_t launch_give_back(const TableArgs& p, hipStream_t stream) {
   const int groups = ((p.num_pages + 31) / 32 + PART - 1) / PART;
   hipLaunchKernelGGL(paged_give_back_kernel, dim3(groups), dim3(LANES), 0, stream, p);
   return hipGetLastError();
 }
 
+// Small enough for one workgroup that has the workspace in LDS.
+template <int BATCH, int PAGES>
+bool fits(const TableArgs& p) { return p.batch <= BATCH && p.num_pages <= PAGES; }
+
 }  // namespace
 
 hipError_t launch_paged_fork(const ForkArgs& f, hipStream_t stream) {
+  if (fits<SMALL_BATCH, SMALL_PAGES>(f.t) && static_cast<long long>(f.t.batch) * f.t.max_pages <= SMALL_EACH * LANES) {
+    hipLaunchKernelGGL(paged_fork_small_kernel, dim3(1), dim3(LANES), 0, stream, f);
+    return hipGetLastError();
+  }
   int columns_log2 = 6;
   while (columns_log2 > 0 && f.t.batch << columns_log2 > FORK_TARGET) --columns_log2;
   const unsigned groups = static_cast<unsigned>((f.t.max_pages + (1 << columns_log2) - 1) >> columns_log2);
@@ -632,10 +847,15 @@ hipError_t launch_paged_fork(const ForkArgs& f, hipStream_t stream) {
 }
 
 hipError_t launch_paged_assign_shared(const AssignSharedArgs& a, hipStream_t stream) {
+  const long long copies = static_cast<long long>(a.t.batch) << a.t.page_log2;
+  if (fits<SMALL_BATCH, SMALL_PAGES>(a.t) && a.max_tokens <= 4 * LANES && copies <= 8 * LANES && static_cast<long long>(a.t.batch) * a.t.max_pages <= 32 * LANES) {
+    hipLaunchKernelGGL(paged_assign_small_kernel, dim3(1), dim3(LANES), 0, stream, a);
+    return hipGetLastError();
+  }
   const int words = (a.t.num_pages + 31) / 32;
   hipLaunchKernelGGL(paged_assign_plan_kernel, dim3(1 + std::min((words + LANES - 1) / LANES, 64)), dim3(LANES), 0, stream, a);
   if (hipError_t e = hipGetLastError()) return e;
-  const long long work = std::max<long long>(a.max_tokens, static_cast<long long>(a.t.batch) << a.t.page_log2);
+  const long long work = std::max(a.max_tokens, copies);
   hipLaunchKernelGGL(paged_assign_move_kernel, dim3(static_cast<unsigned>(std::min<long long>((work + LANES - 1) / LANES + a.t.batch / 32, 128))),
                      dim3(LANES), 0, stream, a);
   if (hipError_t e = hipGetLastError()) return e;
@@ -643,6 +863,10 @@ hipError_t launch_paged_assign_shared(const AssignSharedArgs& a, hipStream_t str
 }
 
 hipError_t launch_paged_compact(const CompactArgs& a, hipStream_t stream) {
+  if (fits<THIN_BATCH, THIN_PAGES>(a.t) && (static_cast<long long>(a.t.batch) * a.t.max_pages << a.t.page_log2) <= SMALL_TOKENS) {
+    hipLaunchKernelGGL(paged_compact_small_kernel, dim3(1), dim3(LANES), 0, stream, a);
+    return hipGetLastError();
+  }
   const dim3 grid(static_cast<unsigned>(a.t.batch) * a.tiles);
   hipLaunchKernelGGL(paged_compact_count_kernel, grid, dim3(EMIT_LANES), 0, stream, a);
   if (hipError_t e = hipGetLastError()) return e;

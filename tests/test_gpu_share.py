@@ -462,3 +462,29 @@ def test_a_servers_steps(dtype, fmt, d, page):
             rows[b] = tuple(x[stay] for x in rows[b])
         check_rows()
         append(list(s.ref.lens), [1] * B)
+
+
+# ---- one workgroup or a few launches: both sides of the rules (paged_share.hip) ------------------------------------------
+
+@pytest.mark.parametrize("batch,num_pages,max_pages,page", [(64, 3000, 256, 16), (64, 3000, 257, 16), (1024, 5000, 16, 16), (1025, 5000, 15, 16),
+                                                            (4, 131072, 8, 16), (4, 131073, 8, 16), (1024, 5000, 32, 16)], ids=str)
+def test_forks_and_steps_on_both_sides_of_one_workgroup(batch, num_pages, max_pages, page):
+    s = Server(batch, num_pages, max_pages, page, seed=batch + max_pages)
+    most = min(max_pages * page, 60 if batch > 100 else 700)
+    s.assign([0] * batch, [s.rng.randint(0, most) for _ in range(batch)])
+    for tokens in (4096, 4097):
+        s.fork(s.parents())
+        keep, new = s.step_sizes(2)
+        s.assign(keep, new, tokens)
+    s.fork([-1] * batch)
+
+
+@pytest.mark.parametrize("batch,num_pages,max_pages,page", [(1, 3000, 1024, 16), (1, 3000, 1025, 16), (256, 5000, 4, 16), (257, 5000, 3, 16),
+                                                            (8, 65536, 8, 256), (8, 65537, 8, 256), (3, 5000, 21, 256), (7, 5000, 18, 128)], ids=str)
+def test_requests_thinned_out_on_both_sides_of_one_workgroup(batch, num_pages, max_pages, page):
+    s = Server(batch, num_pages, max_pages, page, seed=batch + max_pages)
+    room = max_pages * page
+    for _ in range(3):
+        s.assign(list(s.ref.lens), [s.rng.randint(0, max(0, min(room, 40000 // batch) - n)) for n in s.ref.lens])
+        s.fork([s.rng.randrange(batch) if s.rng.random() < 0.3 else b for b in range(batch)])
+        s.compact(s.marks(), sum(s.ref.lens) + 3, s.rng.choice((torch.bool, torch.uint8)))
