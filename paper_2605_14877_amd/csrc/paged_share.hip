@@ -249,23 +249,28 @@ __device__ __forceinline__ void fork_rows(const ForkArgs& f, Group g, int column
 
 __global__ __launch_bounds__(FORK_LANES) void paged_fork_gains_kernel(ForkArgs f, int columns_log2) { fork_gains(f, group(), columns_log2); }
 __global__ __launch_bounds__(FORK_LANES) void paged_fork_rows_kernel(ForkArgs f, int columns_log2) { fork_rows(f, group(), columns_log2); }
-// All phases by one workgroup, whose lanes have up to SMALL_EACH entries of the table each.
+// All phases by one workgroup.  A row's columns are dealt to 2^side_log2 lanes, up to a wavefront of them, `pieces` to each; a lane
+// has up to SMALL_EACH entries of the table.  Few instructions for each are what counts: one compute unit has them all.
 constexpr int SMALL_EACH = 16;
-__global__ __launch_bounds__(LANES) void paged_fork_small_kernel(ForkArgs f) {
+__global__ __launch_bounds__(LANES) void paged_fork_small_kernel(ForkArgs f, int side_log2, int pieces) {
   __shared__ Small<SMALL_BATCH, SMALL_PAGES> s;
-  __shared__ short parents[SMALL_BATCH];
   __shared__ int lens[SMALL_BATCH];
+  struct Row {
+    int parent, held, gets;  // a row that stays as it is holds and gets nothing
+  };
+  __shared__ Row rows[SMALL_BATCH];
   s.lend(f.t);
   const TableArgs& p = f.t;
   const int tid = threadIdx.x, B = p.batch;
   const int head = p.span[0], count = p.span[1];
   clear_gone(p, {0, 1}, LANES);
   bool bad_parent = false, bad_length = false;
+  int parent = -1, len = 0;
   if (tid < B) {
-    const int parent = f.parent[tid], len = p.lens[tid];
+    parent = f.parent[tid];
+    len = p.lens[tid];
     bad_parent = parent < -1 || parent >= B;
     bad_length = len < 0 || len > most_tokens(p);
-    parents[tid] = static_cast<short>(parent);
     lens[tid] = len;
   }
   const bool any_length = __syncthreads_or(bad_length), any_parent = __syncthreads_or(bad_parent);
@@ -273,7 +278,12 @@ __global__ __launch_bounds__(LANES) void paged_fork_small_kernel(ForkArgs f) {
                      : any_parent                 ? HEATKV_PAGED_BAD_PARENT
                      : !ring_fits(p, head, count) ? HEATKV_PAGED_BAD_FREE_LIST
                                                   : HEATKV_PAGED_OK;
-  if (tid < B) p.next[tid] = status ? lens[tid] : parents[tid] < 0 ? 0 : lens[parents[tid]];
+  if (tid < B) {
+    const int next = status ? len : parent < 0 ? 0 : lens[parent];
+    const bool changes = !status && parent != tid;
+    p.next[tid] = next;
+    rows[tid] = {max(parent, 0), changes ? pages_of(p, len) : 0, changes ? pages_of(p, next) : 0};
+  }
   if (tid == 0) {
     p.state[HEAD] = head;
     p.state[COUNT] = count;
@@ -281,35 +291,49 @@ __global__ __launch_bounds__(LANES) void paged_fork_small_kernel(ForkArgs f) {
     p.state[STATUS] = status;
     p.status[0] = status;
   }
+  __syncthreads();
   if (!status) {
+    const int step = LANES >> side_log2, first_row = tid >> side_log2, first_column = tid & ((1 << side_log2) - 1);
     int before[SMALL_EACH], after[SMALL_EACH];
-    const int entries = B * p.max_pages;
+    // Entry k of this lane, in rows row0, row0 + step, ..: visit(k, row, column, whether it exists)
+    auto entries = [&](auto&& visit) {
+      int row0 = 0, piece = 0;
 #pragma unroll
-    for (int k = 0; k < SMALL_EACH; ++k) {
-      const int i = k * LANES + tid;
-      before[k] = after[k] = -1;
-      if (i >= entries) continue;
-      const int b = i / p.max_pages, c = i - b * p.max_pages, parent = parents[b];
-      if (parent == b) continue;
-      if (c < pages_of(p, lens[b])) before[k] = p.table[i];
-      if (parent >= 0 && c < pages_of(p, lens[parent])) after[k] = p.table[parent * p.max_pages + c];
-    }
+      for (int k = 0; k < SMALL_EACH; ++k) {
+        if (row0 >= B) break;
+        visit(k, row0 + first_row, (piece << side_log2) + first_column);
+        if (++piece == pieces) {
+          piece = 0;
+          row0 += step;
+        }
+      }
+    };
 #pragma unroll
-    for (int k = 0; k < SMALL_EACH; ++k) {
-      const int i = k * LANES + tid, b = i / p.max_pages, c = i - b * p.max_pages;
-      const bool has = i < entries && parents[b] != b;
-      before[k] = has && c < pages_of(p, lens[b]) ? in_range(p, before[k]) : -1;
-      after[k] = has && parents[b] >= 0 && c < pages_of(p, lens[parents[b]]) ? in_range(p, after[k]) : -1;
+    for (int k = 0; k < SMALL_EACH; ++k) before[k] = after[k] = -1;
+    entries([&](int k, int b, int c) {
+      if (b >= B) return;
+      const Row r = rows[b];
+      if (c < r.held) before[k] = p.table[b * p.max_pages + c];
+      if (c < r.gets) after[k] = p.table[r.parent * p.max_pages + c];
+    });
+    entries([&](int k, int b, int c) {
+      if (b >= B) return;
+      const Row r = rows[b];
+      before[k] = c < r.held ? in_range(p, before[k]) : -1;
+      after[k] = c < r.gets ? in_range(p, after[k]) : -1;
       if (before[k] == after[k]) before[k] = after[k] = -1;
       if (after[k] >= 0) atomicAdd(&p.holders[after[k]], 1);
-    }
+    });
     wait_vmcnt<0>();  // counted, before anything is counted down; and all entries have been read
     __syncthreads();
+    int held_by[SMALL_EACH];
+    entries([&](int k, int b, int c) {
+      if (before[k] >= 0) held_by[k] = atomicSub(&p.holders[before[k]], 1);
+      if (after[k] >= 0) p.table[b * p.max_pages + c] = after[k];
+    });
 #pragma unroll
-    for (int k = 0; k < SMALL_EACH; ++k) {
-      if (before[k] >= 0) let_go(p, before[k]);
-      if (after[k] >= 0) p.table[k * LANES + tid] = after[k];
-    }
+    for (int k = 0; k < SMALL_EACH; ++k)
+      if (before[k] >= 0 && held_by[k] == 1) atomicOr(&p.gone[before[k] >> 5], 1u << (before[k] & 31));
   }
   __syncthreads();
   give_back(p, {0, 1});
@@ -832,8 +856,11 @@ bool fits(const TableArgs& p) { return p.batch <= BATCH && p.num_pages <= PAGES;
 }  // namespace
 
 hipError_t launch_paged_fork(const ForkArgs& f, hipStream_t stream) {
-  if (fits<SMALL_BATCH, SMALL_PAGES>(f.t) && static_cast<long long>(f.t.batch) * f.t.max_pages <= SMALL_EACH * LANES) {
-    hipLaunchKernelGGL(paged_fork_small_kernel, dim3(1), dim3(LANES), 0, stream, f);
+  int side_log2 = 0;
+  while (side_log2 < 6 && 1 << side_log2 < f.t.max_pages) ++side_log2;
+  const long long pieces = ((static_cast<long long>(f.t.max_pages) - 1) >> side_log2) + 1, step = LANES >> side_log2;
+  if (fits<SMALL_BATCH, SMALL_PAGES>(f.t) && (f.t.batch + step - 1) / step * pieces <= SMALL_EACH) {
+    hipLaunchKernelGGL(paged_fork_small_kernel, dim3(1), dim3(LANES), 0, stream, f, side_log2, static_cast<int>(pieces));
     return hipGetLastError();
   }
   int columns_log2 = 6;
