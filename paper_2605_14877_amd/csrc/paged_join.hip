@@ -78,12 +78,25 @@ __device__ __forceinline__ void join(const AttendParams& p, const Parts& from, i
     One sum[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) sum[r] = One{-INFINITY, 0.f, {}};
-    for (int i0 = half; i0 - half < parts; i0 += 2 * U) {
-      One y[R][U];
+    auto load_all = [&](One (&y)[R][U], int i0) {
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int u = 0; u < U; ++u) y[r][u] = load(min(i0 + 2 * u, parts - 1), min(r0 + 4 * r, tile.rows - 1));
+    };
+    One next[R][U];  // of few rows the next parts are under way while these are added
+    if constexpr (EACH == 1) load_all(next, half);
+    for (int i0 = half; i0 - half < parts; i0 += 2 * U) {
+      One y[R][U];
+      if constexpr (EACH == 1) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int u = 0; u < U; ++u) y[r][u] = next[r][u];
+        if (i0 - half + 2 * U < parts) load_all(next, i0 + 2 * U);
+      } else {
+        load_all(y, i0);
+      }
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         float m = sum[r].m;

@@ -56,6 +56,21 @@ __device__ __forceinline__ long long uniform(long long x) {
   return static_cast<long long>(hi) << 32 | static_cast<unsigned>(lo);
 }
 
+// Sum over the lanes up to this one: within rows of 16 lanes, then from row to row; a quarter of the time of shuffles.
+__device__ __forceinline__ long long inclusive_sum(long long v) {
+#define HEATKV_STEP(control, rows)                                                                                            \
+  v += static_cast<long long>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v >> 32), control, rows, 0xf, false)) << 32 |    \
+       static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), control, rows, 0xf, false))
+  HEATKV_STEP(0x111, 0xf);  // one lane up, then 2, 4 and 8
+  HEATKV_STEP(0x112, 0xf);
+  HEATKV_STEP(0x114, 0xf);
+  HEATKV_STEP(0x118, 0xf);
+  HEATKV_STEP(0x142, 0xa);  // lane 15 of a row to the next row: rows 1 and 3
+  HEATKV_STEP(0x143, 0xc);  // lane 31 to rows 2 and 3
+#undef HEATKV_STEP
+  return v;
+}
+
 // n / d of numbers that are not negative: the 64-bit division takes several times the instructions of the 32-bit one.
 __device__ __forceinline__ long long quotient(long long n, long long d) {
   if (((n | d) >> 31) == 0) return static_cast<unsigned>(n) / static_cast<unsigned>(d);
@@ -99,11 +114,7 @@ struct Requests {
   // Sum of `v` over the lanes up to this one, and over all of them.  Between two calls with the same scratch: a barrier.
   __device__ __forceinline__ long long scan(long long v, Scratch& scratch, long long& all) const {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const long long u = __shfl_up(v, d, 64);
-      if (lane >= d) v += u;
-    }
+    v = inclusive_sum(v);
     if (narrow) {
       all = last_lane(v);
       return v;
