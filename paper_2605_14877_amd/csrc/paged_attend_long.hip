@@ -127,11 +127,11 @@ __device__ __forceinline__ int build_union(const AttendParams& a, const Tile& t,
 
 template <int D, Format F, bool CHOSEN>
 __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams p) {
-  constexpr bool CODES = F != NATIVE, FP4 = F == E2M1;
+  constexpr bool CODES = F == E4M3, FP4 = F == E2M1;
   constexpr int RB = 2 * D, TILE_BYTES = BN * RB, SRC = row_bytes<bf16_t, F>(D);
   constexpr int NK = D / 16, NV = D / 32;
   constexpr int CPT = TILE_BYTES / 4096;            // copies of a tile per wavefront (bf16 rows)
-  constexpr int CPL = FP4 ? 1 : BN * D / 16 / 256;  // loads of a tile per lane (8-bit rows, 16 codes; 4-bit rows, D / 4)
+  constexpr int CPL = BN * D / 16 / 256;            // 16-byte loads of a tile per lane (8-bit rows)
   char(*const lds)[2][TILE_BYTES] = reinterpret_cast<char(*)[2][TILE_BYTES]>(paged_long_lds);  // [stage][K, V]
   // Behind the stages, which then begin at LDS address 0: all of their offsets fit into the read instructions.
   Shared& shared = *reinterpret_cast<Shared*>(paged_long_lds + 4 * TILE_BYTES);
@@ -203,19 +203,26 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
   // Table row of the request; page size in granules.
   const int* const table = a.c.table + static_cast<long long>(tl.b) * a.c.max_pages;
   const int per_log2 = a.c.page_log2 - 4, heads = a.c.H, last_page = a.c.num_pages - 1;
+  struct Place {
+    int granule, pos;
+  };
+  auto locate_granule = [&](int g) {  // of the walk
+    if constexpr (CHOSEN) {
+      const int u = min(g >> per_log2, n_pages - 1), off = g & ((1 << per_log2) - 1);
+      return Place{__builtin_amdgcn_readfirstlane(chosen.granule[u]) + off,
+                   (g >> per_log2) < n_pages ? ((__builtin_amdgcn_readfirstlane(chosen.page[u]) << per_log2) + off) * 16 : 1 << 30};
+    }
+    const int x = min(g, max(tl.len - 1, 0) >> 4);  // granule of the request
+    const unsigned e = min(static_cast<unsigned>(uniform_load(table, x >> per_log2)), static_cast<unsigned>(last_page));
+    return Place{((static_cast<int>(e) * heads + h) << per_log2) + (x & ((1 << per_log2) - 1)), 16 * g};
+  };
   auto locate = [&](int it) {
     TileRows r;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if constexpr (CHOSEN) {
-        const int g = 4 * it + i, u = min(g >> per_log2, n_pages - 1), off = g & ((1 << per_log2) - 1);
-        r.granule[i] = __builtin_amdgcn_readfirstlane(chosen.granule[u]) + off;
-        r.pos[i] = (g >> per_log2) < n_pages ? ((__builtin_amdgcn_readfirstlane(chosen.page[u]) << per_log2) + off) * 16 : 1 << 30;
-        continue;
-      }
-      const int x = min(4 * it + i, max(tl.len - 1, 0) >> 4);  // granule of the request
-      const unsigned e = min(static_cast<unsigned>(uniform_load(table, x >> per_log2)), static_cast<unsigned>(last_page));
-      r.granule[i] = ((static_cast<int>(e) * heads + h) << per_log2) + (x & ((1 << per_log2) - 1));
+      const Place x = locate_granule(4 * it + i);
+      r.granule[i] = x.granule;
+      r.pos[i] = x.pos;
     }
     return r;
   };
@@ -247,54 +254,61 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     tile::copy_1k_checked(lds_wave, decltype(buf_tag)::value * (2 * TILE_BYTES) + TILE_BYTES + 4096 * i, ld_off_v,
                           source(v_pages, at, it, i), 0);
   };
-  // Codes: load i of a lane is 16 codes of one row (4-bit: D / 4, and their scale byte), converted on the way into the stage.
-  constexpr int LPR = FP4 ? 4 : D / 16;  // lanes per row
-  using Raw = std::conditional_t<FP4, Nibbles, uint4>;
+  // 8-bit rows: load i of a lane is 16 codes of one row, converted on the way into the stage.
+  constexpr int LPR = D / 16;  // lanes per row
   auto load_codes = [&](const char* pages, const TileRows& at, int it, int i) {
     const int r = (tid + 256 * i) / LPR;  // a wavefront's 64 / LPR rows are of one granule
-    // Of the granules' places one by arithmetic on all: a choice of one in memory would keep them there.
-    auto own = [&](const int (&x)[4]) {
+    // By arithmetic on all four places: a choice of one in memory would keep them there.
+    auto mine = [&](const int (&x)[4]) {
       const int x0 = x[0], x1 = x[1], x2 = x[2], x3 = x[3];
-      if constexpr (FP4 || D == 64) return pick(wave >> 1, pick(wave & 1, x3, x2), pick(wave & 1, x1, x0));
+      if constexpr (D == 64) return pick(wave >> 1, pick(wave & 1, x3, x2), pick(wave & 1, x1, x0));
       return i ? pick(wave >> 1, x3, x2) : pick(wave >> 1, x1, x0);
     };
-    const int from = own(at.granule);
-    const int pos = !CHOSEN ? it * BN + (r & ~15) : it >= end ? 1 << 30 : own(at.pos);
-    const bool valid = pos + (r & 15) < stop;
-    if constexpr (FP4) {
-      Raw raw{make_uint4(0, 0, 0, 0), 127};
-      if (valid) {
-        const char* const first = pages + static_cast<long long>(from) * 16 * SRC;
-        raw.scale = first[8 * D + lane * D / 128];
-        if constexpr (D == 128) {
-          raw.w = ldg16(first + lane * 16);
-        } else {
-          const uint2 w = *reinterpret_cast<const uint2*>(first + lane * 8);
-          raw.w.x = w.x;
-          raw.w.y = w.y;
-        }
-      }
-      return raw;
-    } else {
-      Raw raw = make_uint4(0, 0, 0, 0);
-      if (valid) raw = ldg16(pages + (static_cast<long long>(from) * 16 + (r & 15)) * SRC + (tid % LPR) * 16);
-      return raw;
-    }
+    const int from = mine(at.granule);
+    const int pos = !CHOSEN ? it * BN + (r & ~15) : it >= end ? 1 << 30 : mine(at.pos);
+    uint4 raw = make_uint4(0, 0, 0, 0);
+    if (pos + (r & 15) < stop) raw = ldg16(pages + (static_cast<long long>(from) * 16 + (r & 15)) * SRC + (tid % LPR) * 16);
+    return raw;
   };
-  auto store_codes = [&](char* stage, const Raw& raw, int i, auto is_v) {
-    const int r = (tid + 256 * i) / LPR;
+  auto store_codes = [&](char* stage, const uint4& raw, int i, auto is_v) {
+    const int r = (tid + 256 * i) / LPR, chunk = 2 * (tid % LPR);
     const int swz = decltype(is_v)::value ? tile::swizzle_v<RB>(r & 15) : tile::swizzle_k<RB>(r & 15);
-    if constexpr (FP4) {
-      const int chunk = D / 32 * (tid % LPR);
-      const unsigned w[4] = {raw.w.x, raw.w.y, raw.w.z, raw.w.w};
-#pragma unroll
-      for (int k = 0; k < D / 32; ++k)
-        *reinterpret_cast<bf16x8*>(stage + r * RB + (((chunk + k) ^ swz) << 4)) = nibbles_to_bf16(w[k], scale_of(raw.scale));
+    *reinterpret_cast<bf16x8*>(stage + r * RB + ((chunk ^ swz) << 4)) = codes_to_bf16(raw.x, raw.y);
+    *reinterpret_cast<bf16x8*>(stage + r * RB + (((chunk + 1) ^ swz) << 4)) = codes_to_bf16(raw.z, raw.w);
+  };
+  // 4-bit rows: a wavefront has one granule of the tile, a lane D / 4 codes of one row and their scale byte.
+  auto locate_own = [&](int it) { return locate_granule(4 * it + wave); };
+  auto load_nibbles = [&](const char* pages, const Place& at) {
+    const char* const first = pages + static_cast<long long>(at.granule) * (16 * SRC);
+    Nibbles raw{make_uint4(0, 0, 0, 0), static_cast<unsigned char>(first[8 * D + lane * D / 128])};
+    if constexpr (D == 128) {
+      raw.w = ldg16(first + lane * 16);
     } else {
-      const int chunk = 2 * (tid % LPR);
-      *reinterpret_cast<bf16x8*>(stage + r * RB + ((chunk ^ swz) << 4)) = codes_to_bf16(raw.x, raw.y);
-      *reinterpret_cast<bf16x8*>(stage + r * RB + (((chunk + 1) ^ swz) << 4)) = codes_to_bf16(raw.z, raw.w);
+      const uint2 w = *reinterpret_cast<const uint2*>(first + lane * 8);
+      raw.w.x = w.x;
+      raw.w.y = w.y;
     }
+    return raw;
+  };
+  // K: rows that no row of queries sees may be anything, their scores are replaced.  V: rows behind the request's end have to be zeros.
+  auto load_v_nibbles = [&](const Place& at, int it) {
+    const int left = stop - (it >= end ? 1 << 30 : at.pos);
+    Nibbles raw{make_uint4(0, 0, 0, 0), 127};
+    if (left >= 16) {
+      raw = load_nibbles(v_pages, at);
+    } else if (lane / 4 < left) {
+      raw = load_nibbles(v_pages, at);
+    }
+    return raw;
+  };
+  // Chunk i of a lane's D / 32: 8 columns.  The swizzle of V leaves the chunks of a lane side by side, that of K does not.
+  const int nibble_row = 16 * wave + lane / 4, nibble_chunk = D / 32 * (lane % 4);
+  const int k_to = nibble_row * RB + ((nibble_chunk ^ tile::swizzle_k<RB>(nibble_row & 15)) << 4);
+  const int v_to = nibble_row * RB + ((nibble_chunk ^ tile::swizzle_v<RB>(nibble_row & 15)) << 4);
+  auto store_nibbles = [&](char* stage, const Nibbles& raw, int i, auto is_v) {
+    const unsigned w = i == 0 ? raw.w.x : i == 1 ? raw.w.y : i == 2 ? raw.w.z : raw.w.w;
+    const int to = decltype(is_v)::value ? v_to + 16 * i : k_to ^ 16 * i;
+    *reinterpret_cast<bf16x8*>(stage + to) = nibbles_to_bf16(w, scale_of(raw.scale));
   };
   using Zero = std::integral_constant<int, 0>;
   using One = std::integral_constant<int, 1>;
@@ -493,12 +507,32 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
   // `at`: where tile it + 1 lies; tile it + 2 is looked up between the two.
   f32x16 s_a[2], s_b[2];
   TileRows at{};
+  // 4-bit rows: codes that are on their way, and the place of the tile whose K they are.
+  [[maybe_unused]] Nibbles raw_v, raw_k;
+  [[maybe_unused]] Place own{};
   // `math(copy)`: what the wavefront computes in the step; it calls copy(i) for i = 0 .. SLOTS - 1, in order.
   auto step = [&](int it, auto kb1, auto vb0, auto&& math) {
+    if constexpr (FP4) {
+      // Codes are loaded a step before they are converted, V(it + 2) and K(it + 3) here, and a chunk of 8 columns is converted under a
+      // product.  All of a tile's in one place, behind the products of the step that had loaded them, took 382 us instead of 346 for
+      // 2 x 2048 tokens over 4096 keys (d = 128), and 80 instead of 68 for whole scales at d = 64.
+      __syncthreads();
+      constexpr int CHUNKS = D / 32, GAP = 3, K0 = SLOTS / 2;
+      math([&](int i) {
+        if (i >= 1 && i < 1 + GAP * CHUNKS && (i - 1) % GAP == 0) store_nibbles(lds[decltype(kb1)::value][1], raw_v, (i - 1) / GAP, One{});
+        if (i == 2 + GAP * (CHUNKS - 1)) {
+          raw_v = load_v_nibbles(own, it + 2);
+          own = locate_own(it + 3);
+        }
+        if (i >= K0 && i < K0 + GAP * CHUNKS && (i - K0) % GAP == 0) store_nibbles(lds[decltype(vb0)::value][0], raw_k, (i - K0) / GAP, Zero{});
+        if (i == K0 + GAP * (CHUNKS - 1) + 1) raw_k = load_nibbles(k_pages, own);
+      });
+      return;
+    }
     wait_vmcnt<0>();
     __syncthreads();
     if constexpr (CODES) {  // V's codes have the first half of the step to arrive, K's the second
-      Raw raw[CPL];
+      uint4 raw[CPL];
       math([&](int i) {
         if (i == 0)
 #pragma unroll
@@ -506,9 +540,8 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
         else if (i == 1)
           at = locate(it + 2);
         else if (i >= SLOTS / 2 && i < SLOTS / 2 + CPL) {
-          const int k = CPL == 1 ? 0 : i - SLOTS / 2;
-          store_codes(lds[decltype(kb1)::value][1], raw[k], k, One{});
-          raw[k] = load_codes(k_pages, at, it + 2, k);
+          store_codes(lds[decltype(kb1)::value][1], raw[i - SLOTS / 2], i - SLOTS / 2, One{});
+          raw[i - SLOTS / 2] = load_codes(k_pages, at, it + 2, i - SLOTS / 2);
         }
       });
 #pragma unroll
@@ -541,9 +574,24 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
   };
   if (begin < end) {
     const int second = begin + 1 < end ? begin + 1 : begin;
-    at = locate(begin);
-    if constexpr (CODES) {
-      Raw raw[3][CPL];
+    if constexpr (!FP4) at = locate(begin);
+    if constexpr (FP4) {
+      own = locate_own(begin);
+      raw_k = load_nibbles(k_pages, own);
+      raw_v = load_v_nibbles(own, begin);
+      own = locate_own(begin + 1);
+      const Nibbles next_k = load_nibbles(k_pages, own), next_v = load_v_nibbles(own, begin + 1);
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) {
+        store_nibbles(lds[0][0], raw_k, k, Zero{});
+        store_nibbles(lds[0][1], raw_v, k, One{});
+        store_nibbles(lds[1][0], next_k, k, Zero{});
+      }
+      raw_v = next_v;
+      own = locate_own(begin + 2);
+      raw_k = load_nibbles(k_pages, own);
+    } else if constexpr (CODES) {
+      uint4 raw[3][CPL];
 #pragma unroll
       for (int k = 0; k < CPL; ++k) {
         raw[0][k] = load_codes(k_pages, at, begin, k);
