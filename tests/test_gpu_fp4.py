@@ -2,6 +2,7 @@
 back and moved, page bounds, attention, attention over chosen pages.  What the cache holds is exact in bf16, so attention has the
 tolerances of the bf16 cache (test_gpu_paged.py) against the values that are held."""
 import math
+import random
 
 import pytest
 import torch
@@ -9,7 +10,7 @@ import torch
 import paper_2605_14877_amd as hk
 from tests import paged_reference as ref
 from tests import share_reference as sref
-from tests.test_gpu_paged import FEW, MANY, Problem, _ints
+from tests.test_gpu_paged import FEW, MANY, Problem, _check_with_nan, _ints, _spoil
 
 pytestmark = pytest.mark.gpu
 
@@ -326,3 +327,216 @@ def test_addresses_beyond_32_bits():
     hk.heatkv_paged_move(shape, frm, to, k, v)
     hk.heatkv_paged_read(shape, to, k, v, got[0, :3], got[1, :3])
     assert _same(got[0, :3], held[0][:3]) and _same(got[1, :3], held[1][:3])
+
+
+# ---- what tiles have in common, calls of any content, graphs ------------------------------------------------------------
+
+def _spoiled(case, seed, last_only):
+    p = Fp4Problem(*case, seed=seed)
+    p.dtype = "fp8"  # of values that are not finite only NaN: 4 bits have no infinity
+    _spoil(p, seed, last_only)
+    p.store()
+    return p
+
+
+@pytest.mark.parametrize("case", [(4, 2, 128, 16, [50, 33], [20, 5]), (2, 1, 64, 32, [400], [90]), (6, 1, 128, 64, [700, 65], [40, 30]),
+                                  (4, 2, 64, 16, [50, 300], [20, 70]), (8, 1, 128, 16, [2000], [4])], ids=str)
+def test_values_that_a_row_does_not_see_do_not_reach_it(case):
+    p = _spoiled(case, 11, True)
+    fine = _check_with_nan(p, True, p.run(True))
+    last = [s - 1 for s in p.q_start[1:]]
+    assert fine[[t for t in range(p.q_start[-1]) if t not in last]].all() and not fine[last].all()
+    p = _spoiled(case, 12, False)
+    for causal in (True, False):
+        _check_with_nan(p, causal, p.run(causal))
+
+
+@pytest.mark.parametrize("case,top", [((4, 2, 128, 16, [300, 33], [6, 5]), 4), ((4, 1, 64, 32, [400], [90]), 4),
+                                      ((4, 2, 128, 16, [50, 300], [20, 70]), 4), ((4, 1, 128, 64, [3000, 900], [90, 70]), 9),
+                                      ((4, 2, 64, 128, [2600], [200]), 2)], ids=str)
+def test_pages_that_a_token_has_not_chosen_do_not_reach_it(case, top):
+    p = _spoiled(case, 13, False)
+    r = random.Random(5)
+    pages = max(p.lens) // p.page + 1
+    sel = [[[r.randrange(0, pages) for _ in range(top)] for _ in range(p.H)] for _ in range(p.tokens)]
+    for causal in (True, False):
+        fine = _check_with_nan(p, causal, p.run(causal, _ints(sel)), sel)
+        assert fine.any() and not fine.all()
+
+
+@pytest.mark.parametrize("new", [[4, 19, 1], [150, 70, 1]])
+@pytest.mark.parametrize("group,d", [(1, 64), (3, 128), (16, 64), (16, 128)])
+def test_selections_of_any_content(group, d, new):
+    p = Fp4Problem(2 * group, 2, d, 16, [333, 100, 5], new, seed=9)
+    top, r = 6, random.Random(3)
+    sel = [[[r.choice([-1, -7, 2 ** 31 - 1, r.randrange(0, 25), r.randrange(0, 25), r.randrange(0, 8)]) for _ in range(top)]
+            for _ in range(2)] for _ in range(p.tokens)]
+    sel[0][0], sel[1][1], sel[2][0] = [-1] * top, [3] * top, [24, 23, 22, 21, 20, 0]
+    for t in range(20, min(150, p.tokens)):
+        sel[t][1] = [-1] * top  # a tile without any page
+    for causal in (True, False):
+        p.check(causal, p.run(causal, _ints(sel)), sel)
+
+
+@pytest.mark.parametrize("heads,top", [((4, 2), 0), ((3, 1), 0), ((4, 2), 3)])
+@pytest.mark.parametrize("batch", [64, 65, 1000])
+def test_many_requests(heads, top, batch):
+    r = random.Random(batch)
+    lens = [r.choice((0, 1, 15, 16, 17, 40, 90)) for _ in range(batch)]
+    new = [min(n, r.choice((0, 1, 1, 1, 20))) for n in lens]
+    p = Fp4Problem(*heads, 64, 16, lens, new, seed=batch)
+    sel = [[[r.randrange(0, 6) for _ in range(top)] for _ in range(p.H)] for _ in range(p.tokens)] if top else None
+    p.check(True, p.run(True, _ints(sel) if top else None), sel)
+
+
+@pytest.mark.parametrize("case,top", [(c, 0) for c in CASES[3:9] + CASES[-4:]] + [
+    ((4, 2, 64, 16, [n for n in (900, 300, 40) for _ in range(30)], [n for n in (1, 2, 70) for _ in range(30)]), 0),
+    ((8, 8, 64, 32, [2000] * 40, [1] * 40), 6), ((4, 2, 128, 64, [3000, 900], [90, 70]), 9)], ids=lambda x: str(x)[:50])
+def test_nothing_is_written_behind_the_workspace(case, top):
+    p = Fp4Problem(*case, seed=35)
+    d, n, guard = p.dev, hk.paged_attend_workspace_bytes(p.shape, p.tokens, top), 1 << 16
+    ws = torch.full((n + guard,), 165, dtype=torch.uint8, device="cuda")
+    out = torch.zeros_like(d["q"])
+    args = (p.shape, d["q"], d["k"], d["v"], d["table"], d["q_start"], d["lens"])
+    r = random.Random(35)
+    for causal in (True, False):
+        if top:
+            sel = _ints([[[r.randrange(0, p.max_pages) for _ in range(top)] for _ in range(p.H)] for _ in range(p.tokens)])
+            hk.heatkv_paged_attend_selected(*args, sel, p.sm, out, ws[:n], causal=causal)
+        else:
+            hk.heatkv_paged_attend(*args, p.sm, out, ws[:n], causal=causal)
+    torch.cuda.synchronize()
+    assert torch.all(ws[n:] == 165)
+
+
+@pytest.mark.parametrize("new", [2, 70])
+def test_rows_may_be_slices_with_any_stride(new):
+    p = Fp4Problem(4, 2, 64, 16, [90, 33], [new, 1], seed=3)
+    want = p.run(True)
+    wide = torch.full((p.tokens, 7, 80), 9.0, dtype=p.q.dtype, device="cuda")
+    q = wide[:, 2:6, 8:72]
+    q.copy_(p.dev["q"])
+    by_head = torch.full((6, p.tokens + 1, 64), 7.0, dtype=p.q.dtype, device="cuda")
+    got = p.run(True, out=by_head.transpose(0, 1)[:p.tokens, 1:5], q=q)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert torch.all(by_head[0] == 7.0) and torch.all(by_head[5] == 7.0) and torch.all(by_head[:, p.tokens:] == 7.0)
+
+
+@pytest.mark.parametrize("new", [1, 60])
+def test_a_captured_step_is_replayed(new):
+    """Rows in, bounds, read back, the choice, attention over all and over chosen pages, rows moved: one graph, replayed for new rows
+    with eager calls in between."""
+    p = Fp4Problem(4, 2, 128, 16, [300, 90], [new, 1], seed=20)
+    d, n = p.dev, p.q_start[-1]
+    slots = [p.table[b][x // 16] * 16 + x % 16 for b in range(2) for x in range(p.lens[b] - p.new[b], p.lens[b])]
+    slots = _ints(slots + [-1] * (p.tokens - n))
+    kv = torch.zeros(p.tokens, 4, 128, dtype=torch.bfloat16, device="cuda")
+    bounds = torch.zeros(p.num_pages, 2, 2, 128, dtype=torch.int8, device="cuda")
+    scales = torch.zeros(p.num_pages, 2, device="cuda")
+    spare = [x for x in range(p.num_pages) if not any(x in r for r in p.table)]
+    to = _ints([spare[0] * 16 + i for i in range(7)])
+
+    def state():
+        return dict(k=d["k"].clone(), v=d["v"].clone(), bounds=bounds.clone(), scales=scales.clone(),
+                    read=[torch.zeros(p.tokens, 2, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2)],
+                    sel=torch.zeros(p.tokens, 2, 5, dtype=torch.int32, device="cuda"), out=[torch.zeros_like(d["q"]) for _ in range(2)],
+                    ws=torch.zeros(max(hk.paged_attend_workspace_bytes(p.shape, p.tokens, t) for t in (0, 5)) + 16, dtype=torch.uint8,
+                                   device="cuda"))
+
+    def step(s):
+        more = (d["table"], d["q_start"], d["lens"])
+        hk.heatkv_paged_append(p.shape, slots, kv[:, :2], kv[:, 2:], s["k"], s["v"], s["bounds"], s["scales"])
+        hk.heatkv_paged_read(p.shape, slots, s["k"], s["v"], *s["read"])
+        hk.heatkv_paged_attend(p.shape, d["q"], s["k"], s["v"], *more, p.sm, s["out"][0], s["ws"])
+        hk.heatkv_paged_select(p.shape, d["q"], s["bounds"], s["scales"], *more, 1, 1, s["sel"])
+        hk.heatkv_paged_attend_selected(p.shape, d["q"], s["k"], s["v"], *more, s["sel"], p.sm, s["out"][1], s["ws"])
+        hk.heatkv_paged_move(p.shape, slots[:1].expand(7).contiguous(), to, s["k"], s["v"], s["bounds"], s["scales"])
+    captured, eager = state(), state()
+    step(eager)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        step(captured)
+    for turn in range(4):
+        kv.copy_(torch.randn(kv.shape, generator=torch.Generator().manual_seed(turn)))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        step(eager)
+        torch.cuda.synchronize()
+        for name in ("k", "v", "bounds", "scales", "sel"):
+            assert torch.equal(captured[name], eager[name]), name
+        for name in ("read", "out"):
+            assert all(torch.equal(x, y) for x, y in zip(captured[name], eager[name])), name
+
+
+def test_the_native_path_makes_the_calls(monkeypatch):
+    """Plain calls do not reach the Python checks; malformed ones do, and are named there."""
+    from paper_2605_14877_amd import paged
+    H, d, page, n, B = 2, 64, 16, 40, 3
+    shape = hk.PagedShape(2 * H, H, d, page, n, B, 8, "bf16", hk.KV_FP4_E2M1)
+    k, v = (torch.zeros(shape.pages_shape, dtype=torch.uint8, device="cuda") for _ in range(2))
+    rows = torch.zeros(4, H, d, dtype=torch.bfloat16, device="cuda")
+    out = torch.zeros(4, 2, H, d, dtype=torch.bfloat16, device="cuda")
+    q = torch.zeros(4, 2 * H, d, dtype=torch.bfloat16, device="cuda")
+    bounds, scales = torch.zeros(n, H, 2, d, dtype=torch.int8, device="cuda"), torch.zeros(n, H, device="cuda")
+    tables = [_ints([0] * B), _ints([0] * n), _ints(list(range(n))), _ints([0, n]), _ints([[0] * 8] * B)]  # lens, holders, ring, span, table
+    ws = torch.zeros(hk.paged_tables_workspace_bytes(shape), dtype=torch.uint8, device="cuda")
+    status, some, moves = _ints([0]), _ints([0] * B), _ints([-1] * 9)
+    copies = [_ints([[0] * page] * B) for _ in range(2)]
+    kept = torch.ones(B, 8 * page, dtype=torch.bool, device="cuda")
+    kept_bytes = kept.to(torch.uint8)
+    att = torch.zeros(max(hk.paged_attend_workspace_bytes(shape, 4), 16), dtype=torch.uint8, device="cuda")
+    calls = {
+        "append": lambda k=k: hk.heatkv_paged_append(shape, moves[:4], rows, rows, k, v, bounds, scales),
+        "read": lambda k=k: hk.heatkv_paged_read(shape, moves[:4], k, v, out[:, 0], out[:, 1]),
+        "attend": lambda k=k: hk.heatkv_paged_attend(shape, q, k, v, tables[4], _ints([0] * 4), tables[0], 0.1, torch.zeros_like(q), att),
+        "move": lambda k=k: hk.heatkv_paged_move(shape, moves, moves.clone(), k, v, bounds, scales),
+        "move of copies": lambda k=k: hk.heatkv_paged_move(shape, *copies, k, v),
+        "fork": lambda k=some: hk.heatkv_paged_fork(shape, k, *tables, status, ws),
+        "assign_shared": lambda k=some: hk.heatkv_paged_assign_shared(shape, some, k, *tables, _ints([0] * (B + 1)), moves.clone(), *copies, status, ws),
+        "compact": lambda k=kept: hk.heatkv_paged_compact(shape, k, *tables, moves, moves.clone(), status, ws,
+                                                          lens_out=_ints([0] * B), free_span_out=_ints([0, 0])),
+    }
+    for call in calls.values():  # by the native path or the other, they are made
+        call()
+
+    def reached(*_):
+        raise AssertionError("the call went through the Python checks")
+    monkeypatch.setattr(paged, "_Call", reached)
+    for call in calls.values():
+        call()
+    calls["compact"](kept_bytes)
+    monkeypatch.undo()
+    torch.cuda.synchronize()
+    wrong = {"append": k[:-1], "read": k.view(torch.int8), "attend": k.cpu(), "move": k.view(n, H, -1, 68), "move of copies": k[:, :1],
+             "fork": some.long(), "assign_shared": some[:2], "compact": kept[:, :-1]}
+    for name, x in wrong.items():
+        with pytest.raises((ValueError, TypeError)):
+            calls[name](x)
+
+
+def test_a_value_that_is_not_a_number_does_not_stall_a_call():
+    # NaN in V of a key that all rows see: their results are NaN as they stand (as for the other formats: test_gpu_paged.py)
+    p = Fp4Problem(4, 1, 128, 64, [4096], [300], seed=31)
+    d, out = p.dev, torch.empty_like(p.dev["q"])
+    ws = torch.zeros(max(hk.paged_attend_workspace_bytes(p.shape, p.tokens), 16), dtype=torch.uint8, device="cuda")
+    clean = d["v"]
+    p.v[p.table[0][32], :, 3, 5] = math.nan
+    p.store()
+
+    def least(v):
+        times = []
+        for _ in range(20):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            torch.cuda.synchronize()
+            a.record()
+            hk.heatkv_paged_attend(p.shape, d["q"], d["k"], v, d["table"], d["q_start"], d["lens"], p.sm, out, ws)
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+    usual = least(clean)
+    assert least(d["v"]) < 3 * usual
+    real = p.q_start[-1]
+    assert out[:real, :, :32].isnan().all() and out[:real, :, 32:].isfinite().all()
