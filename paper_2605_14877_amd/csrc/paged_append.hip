@@ -139,6 +139,26 @@ struct CacheEight {
   }
 };
 
+// A lane's token, head and place within the row, of PIECES; heads of a token are neighbours.  Tokens x heads are at most 2^23.
+struct RowPiece {
+  unsigned t;
+  int h, piece;
+};
+template <int PIECES>
+__device__ __forceinline__ RowPiece row_piece(int H) {
+  const unsigned i = blockIdx.x * LANES + threadIdx.x, row = i / PIECES, t = row / static_cast<unsigned>(H);
+  return {t, static_cast<int>(row - t * H), static_cast<int>(i % PIECES)};
+}
+// Row of the cache that slot has for head h.
+template <class Args>
+__device__ __forceinline__ long long cache_row(const Args& p, int slot, int h) {
+  return ((static_cast<long long>(slot >> p.page_log2) * p.H + h) << p.page_log2) + (slot & ((1 << p.page_log2) - 1));
+}
+template <class Args>
+__device__ __forceinline__ bool in_cache(const Args& p, int slot) {
+  return static_cast<unsigned>(slot) < static_cast<unsigned>(p.num_pages << p.page_log2);
+}
+
 // Where new rows come from: the caller's token tensors, in the operands' type, or (MOVE) other rows of the cache, as they are.
 // Row t of the call, head h, columns col .. col + 7.
 template <class T, Format F, int D, bool MOVE>
@@ -146,8 +166,7 @@ __device__ __forceinline__ void fetch_new(const PagedAppendArgs& p, long long t,
                                           CacheEight<T, F, D>& v) {
   if constexpr (MOVE) {
     const unsigned slot = min(static_cast<unsigned>(p.from[t]), static_cast<unsigned>((p.num_pages << p.page_log2) - 1));
-    const long long at = (((static_cast<long long>(slot >> p.page_log2) * p.H + h) << p.page_log2) +
-                          (slot & ((1u << p.page_log2) - 1))) * D + col;
+    const long long at = cache_row(p, static_cast<int>(slot), h) * D + col;
     k.load(p.k_pages, at);
     v.load(p.v_pages, at);
   } else {
@@ -172,22 +191,41 @@ __device__ __forceinline__ void write_row(const PagedAppendArgs& p, long long at
 }
 
 // Rows only: 8 elements of K and of V per lane.
-template <class T, Format F, int D, bool MOVE>
+template <class T, Format F, int D>
 __global__ __launch_bounds__(LANES) void paged_append_kernel(PagedAppendArgs p) {
-  constexpr int COLS = D / 8;
-  const long long i = static_cast<long long>(blockIdx.x) * LANES + threadIdx.x;
-  const int c = static_cast<int>(i & (COLS - 1));
-  const long long row = i / COLS;
-  const long long t = row / p.H;
-  const int h = static_cast<int>(row - t * p.H);
-  if (t >= p.tokens) return;
-  const int slot = p.slots[t];
-  if (slot < 0 || slot >= p.num_pages << p.page_log2) return;
-  const long long to = ((((static_cast<long long>(slot >> p.page_log2) * p.H + h) << p.page_log2) +
-                         (slot & ((1 << p.page_log2) - 1))) * D + 8 * c);
+  const RowPiece x = row_piece<D / 8>(p.H);
+  if (x.t >= p.tokens) return;
+  const int slot = p.slots[x.t];
+  if (!in_cache(p, slot)) return;
   CacheEight<T, F, D> k, v;
-  fetch_new<T, F, D, MOVE>(p, t, h, 8 * c, k, v);
-  write_row<MOVE>(p, to, k, v);
+  fetch_new<T, F, D, false>(p, x.t, x.h, 8 * x.piece, k, v);
+  write_row<false>(p, cache_row(p, slot, x.h) * D + 8 * x.piece, k, v);
+}
+
+// Rows moved as they are, without bounds: 16 bytes of K and of V per lane; of a 4-bit row the scale bytes of K by its first lane, those
+// of V by its second.
+template <class T, Format F, int D>
+__global__ __launch_bounds__(LANES) void paged_move_kernel(PagedAppendArgs p) {
+  constexpr int BYTES = F == E2M1 ? D / 2 : paged::row_bytes<T, F>(D), GRANULE_BYTES = 16 * paged::row_bytes<T, F>(D);
+  const RowPiece x = row_piece<BYTES / 16>(p.H);
+  if (x.t >= p.tokens) return;
+  const int slot = p.slots[x.t];
+  if (!in_cache(p, slot)) return;
+  const int from_slot = static_cast<int>(min(static_cast<unsigned>(p.from[x.t]), static_cast<unsigned>((p.num_pages << p.page_log2) - 1)));
+  const long long from = cache_row(p, from_slot, x.h), to = cache_row(p, slot, x.h);
+  auto at = [&](long long row) {
+    return (row >> 4) * GRANULE_BYTES + (row & 15) * BYTES + 16 * x.piece;  // codes of 16 rows lie together
+  };
+  char *const kp = static_cast<char*>(p.k_pages), *const vp = static_cast<char*>(p.v_pages);
+  const uint4 k = ldg16(kp + at(from)), v = ldg16(vp + at(from));
+  if constexpr (F == E2M1) {
+    using Scales = std::conditional_t<D == 128, unsigned, unsigned short>;
+    auto scales_at = [&](long long row) { return (row >> 4) * GRANULE_BYTES + 8 * D + (row & 15) * (D / 32); };
+    char* const pages = x.piece == 0 ? kp : vp;
+    if (x.piece < 2) *reinterpret_cast<Scales*>(pages + scales_at(to)) = *reinterpret_cast<const Scales*>(pages + scales_at(from));
+  }
+  *reinterpret_cast<uint4*>(kp + at(to)) = k;
+  *reinterpret_cast<uint4*>(vp + at(to)) = v;
 }
 
 // The first token of a call on a page is that page's owner: who has it forms the bounds over the rows up to the last one that
@@ -484,10 +522,12 @@ hipError_t launch(const PagedAppendArgs& a, hipStream_t stream) {
   const long long units = a.tokens * a.H;  // pages that the call can touch, times heads
   auto run = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    if (!a.bounds) {
-      const long long lanes = units * (D / 8);
-      hipLaunchKernelGGL((paged_append_kernel<T, F, D, MOVE>), dim3(static_cast<unsigned>((lanes + LANES - 1) / LANES)), dim3(LANES), 0,
-                         stream, a);
+    auto grid = [&](int pieces) { return dim3(static_cast<unsigned>((units * pieces + LANES - 1) / LANES)); };
+    if (!a.bounds && MOVE) {
+      const int bytes = F == E2M1 ? D / 2 : paged::row_bytes<T, F>(D);
+      hipLaunchKernelGGL((paged_move_kernel<T, F, D>), grid(bytes / 16), dim3(LANES), 0, stream, a);
+    } else if (!a.bounds) {
+      hipLaunchKernelGGL((paged_append_kernel<T, F, D>), grid(D / 8), dim3(LANES), 0, stream, a);
     } else if (units <= FEW_PAGES) {
       hipLaunchKernelGGL((paged_append_bounds_kernel<T, F, D, MOVE>), dim3(static_cast<unsigned>(units)), dim3(LANES), 0, stream, a);
     } else {
@@ -518,25 +558,19 @@ hipError_t launch(const PagedAppendArgs& a, hipStream_t stream) {
 // The other way: rows of the cache by their slots, as values of the operands' type.
 template <class T, Format F, int D>
 __global__ __launch_bounds__(LANES) void paged_read_kernel(PagedReadArgs p) {
-  constexpr int COLS = D / 8;
-  const long long i = static_cast<long long>(blockIdx.x) * LANES + threadIdx.x;
-  const int c = static_cast<int>(i & (COLS - 1));
-  const long long row = i / COLS;
-  const long long t = row / p.H;
-  const int h = static_cast<int>(row - t * p.H);
-  if (t >= p.tokens) return;
-  const int slot = p.slots[t];
-  if (slot < 0 || slot >= p.num_pages << p.page_log2) return;
-  const long long at = ((((static_cast<long long>(slot >> p.page_log2) * p.H + h) << p.page_log2) +
-                         (slot & ((1 << p.page_log2) - 1))) * D + 8 * c);
+  const RowPiece r = row_piece<D / 8>(p.H);
+  if (r.t >= p.tokens) return;
+  const int slot = p.slots[r.t];
+  if (!in_cache(p, slot)) return;
+  const long long at = cache_row(p, slot, r.h) * D + 8 * r.piece;
   CacheEight<T, F, D> k, v;
   k.load(p.k_pages, at);
   v.load(p.v_pages, at);
   uint4 x[sizeof(T) / 2], y[sizeof(T) / 2];
   k.decode(x);
   v.decode(y);
-  T* ko = static_cast<T*>(p.k_out) + t * p.k_token_stride + h * p.k_head_stride + 8 * c;
-  T* vo = static_cast<T*>(p.v_out) + t * p.v_token_stride + h * p.v_head_stride + 8 * c;
+  T* ko = static_cast<T*>(p.k_out) + r.t * p.k_token_stride + r.h * p.k_head_stride + 8 * r.piece;
+  T* vo = static_cast<T*>(p.v_out) + r.t * p.v_token_stride + r.h * p.v_head_stride + 8 * r.piece;
 #pragma unroll
   for (int j = 0; j < static_cast<int>(sizeof(T)) / 2; ++j) {
     *reinterpret_cast<uint4*>(ko + 4 * j) = x[j];
