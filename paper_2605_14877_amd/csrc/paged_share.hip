@@ -12,7 +12,9 @@
 //
 // Each call is a few phases that are launches of their own; `Group` says which of how many workgroups one is.
 //
-// Bound: latency, of the launches and of a few round trips to memory in each.
+// Bound: latency, of the launches and of a few round trips to memory in each.  A step of 64 beams (fork, assign, the rows of one layer, with
+// the copy of the tables that it starts from) takes 26 us, of 512 samples 40; one request of 3000 tokens thinned out 16 us, 32 of 8192
+// tokens 119 us, 94 of them the rows of one layer.
 #include <hip/hip_runtime.h>
 
 #include "kernels.h"
@@ -25,7 +27,7 @@ namespace {
 constexpr int LANES = 1024, WAVES = LANES / 64;
 constexpr int PER_LANE = paged::MAX_BATCH / LANES;
 constexpr int FORK_LANES = 256, FORK_ENTRIES = paged::MAX_BATCH;  // lanes of a workgroup, entries of the table that it may have
-constexpr int FORK_TARGET = 1024;                                // entries that it has if the batch is not larger
+constexpr int FORK_TARGET = 512;  // entries that it has if the batch is not larger: 512 samples 39.8 us, with 1024 42.3, with 4096 62.7
 constexpr int EMIT_LANES = 256, CHUNK = 4096;         // tokens that a workgroup of compact looks at together
 
 struct Group {
@@ -245,8 +247,10 @@ __device__ __forceinline__ void fork_rows(const ForkArgs& f, Group g, int column
 __global__ __launch_bounds__(FORK_LANES) void paged_fork_gains_kernel(ForkArgs f, int columns_log2) { fork_gains(f, group(), columns_log2); }
 __global__ __launch_bounds__(FORK_LANES) void paged_fork_rows_kernel(ForkArgs f, int columns_log2) { fork_rows(f, group(), columns_log2); }
 // All phases by one workgroup.  A row's columns are dealt to 2^side_log2 lanes, up to a wavefront of them, `pieces` to each; a lane
-// has up to SMALL_EACH entries of the table.  Few instructions for each are what counts: one compute unit has them all.
-constexpr int SMALL_EACH = 16;
+// has up to SMALL_EACH entries of the table.  Few instructions for each are what counts: one compute unit has them all.  Beams in
+// groups of four, with the copy of the tables that the measurement starts from (3.7 us), by one workgroup and by launches of many: 64 x
+// 16 entries 7.7 and 16.3 us, 64 x 64 11.0 and 16.5, 64 x 128 14.8 and 18.4, 64 x 256 21.6 and 19.6, 1024 x 16 25.3 and 21.1.
+constexpr int SMALL_EACH = 12;
 __global__ __launch_bounds__(LANES) void paged_fork_small_kernel(ForkArgs f, int side_log2, int pieces) {
   __shared__ Small<SMALL_BATCH, SMALL_PAGES> s;
   __shared__ int lens[SMALL_BATCH];
@@ -737,7 +741,8 @@ __global__ __launch_bounds__(EMIT_LANES) void paged_compact_count_kernel(Compact
 __global__ __launch_bounds__(LANES) void paged_compact_plan_kernel(CompactArgs a) { compact_plan(a); }
 __global__ __launch_bounds__(EMIT_LANES) void paged_compact_emit_kernel(CompactArgs a) { compact_emit(a, group()); }
 
-// All phases by one workgroup: a lane has 16 tokens next to one another, on one page.
+// All phases by one workgroup: a lane has 16 tokens next to one another, on one page.  Every other token goes, as above: 4 requests of up
+// to 4096 tokens 13.1 us and by launches of many 19.7, 256 of 64 tokens 13.3 and 19.1.
 constexpr int SMALL_TOKENS = 16 * LANES, THIN_BATCH = 256, THIN_PAGES = 65536;
 __global__ __launch_bounds__(LANES) void paged_compact_small_kernel(CompactArgs a) {
   __shared__ Small<THIN_BATCH, THIN_PAGES> s;
@@ -874,6 +879,8 @@ hipError_t launch_paged_fork(const ForkArgs& f, hipStream_t stream) {
 }
 
 hipError_t launch_paged_assign_shared(const AssignSharedArgs& a, hipStream_t stream) {
+  // A token each, most of them to pages that are shared, as above: 64 requests 9.4 us by one workgroup and 12.9 by launches of many, 512
+  // requests 12.3 and 15.1.  The limits are of what it goes through alone: tokens, copies, entries of the table that may all be let go.
   const long long copies = static_cast<long long>(a.t.batch) << a.t.page_log2;
   if (fits<SMALL_BATCH, SMALL_PAGES>(a.t) && a.max_tokens <= 4 * LANES && copies <= 8 * LANES && static_cast<long long>(a.t.batch) * a.t.max_pages <= 32 * LANES) {
     hipLaunchKernelGGL(paged_assign_small_kernel, dim3(1), dim3(LANES), 0, stream, a);

@@ -466,7 +466,7 @@ def test_a_servers_steps(dtype, fmt, d, page):
 
 # ---- one workgroup or a few launches: both sides of the rules (paged_share.hip) ------------------------------------------
 
-@pytest.mark.parametrize("batch,num_pages,max_pages,page", [(64, 3000, 256, 16), (64, 3000, 257, 16), (1024, 5000, 16, 16), (1025, 5000, 15, 16),
+@pytest.mark.parametrize("batch,num_pages,max_pages,page", [(64, 3000, 192, 16), (64, 3000, 193, 16), (768, 5000, 16, 16), (769, 5000, 16, 16), (1024, 5000, 8, 16), (1025, 5000, 8, 16),
                                                             (4, 131072, 8, 16), (4, 131073, 8, 16), (1024, 5000, 32, 16)], ids=str)
 def test_forks_and_steps_on_both_sides_of_one_workgroup(batch, num_pages, max_pages, page):
     s = Server(batch, num_pages, max_pages, page, seed=batch + max_pages)
