@@ -96,12 +96,12 @@ struct PagedAppendArgs {
   int kv_format;
   long long tokens;
   const int32_t* slots;
-  const int32_t* from;  // null, or rows of the cache instead of k_new and v_new
   const void *k_new, *v_new;
   long long k_token_stride, k_head_stride, v_token_stride, v_head_stride;  // elements
   void *k_pages, *v_pages;
   int8_t* bounds;  // null: rows only
   float* bound_scales;
+  const int32_t* from;  // null, or rows of the cache instead of k_new and v_new
 };
 hipError_t launch_paged_append(const PagedAppendArgs& a, hipStream_t stream);
 

@@ -159,26 +159,33 @@ __device__ __forceinline__ bool in_cache(const Args& p, int slot) {
   return static_cast<unsigned>(slot) < static_cast<unsigned>(p.num_pages << p.page_log2);
 }
 
-// Where new rows come from: the caller's token tensors, in the operands' type, or (MOVE) other rows of the cache, as they are.
-// Row t of the call, head h, columns col .. col + 7.
+// Where new rows come from, columns col .. col + 7 of head h: the caller's token tensors, in the operands' type, or (MOVE) other rows of
+// the cache, as they are.
 template <class T, Format F, int D, bool MOVE>
-__device__ __forceinline__ void fetch_new(const PagedAppendArgs& p, long long t, int h, int col, CacheEight<T, F, D>& k,
-                                          CacheEight<T, F, D>& v) {
-  if constexpr (MOVE) {
-    const unsigned slot = min(static_cast<unsigned>(p.from[t]), static_cast<unsigned>((p.num_pages << p.page_log2) - 1));
-    const long long at = cache_row(p, static_cast<int>(slot), h) * D + col;
-    k.load(p.k_pages, at);
-    v.load(p.v_pages, at);
-  } else {
-    const T* kp = static_cast<const T*>(p.k_new) + t * p.k_token_stride + h * p.k_head_stride + col;
-    const T* vp = static_cast<const T*>(p.v_new) + t * p.v_token_stride + h * p.v_head_stride + col;
+struct Incoming {
+  const PagedAppendArgs& p;
+  const int h, col;
+  const T *k_new, *v_new;
+  __device__ __forceinline__ Incoming(const PagedAppendArgs& args, int head, int column)
+      : p(args), h(head), col(column),
+        k_new(MOVE ? nullptr : static_cast<const T*>(args.k_new) + head * args.k_head_stride + column),
+        v_new(MOVE ? nullptr : static_cast<const T*>(args.v_new) + head * args.v_head_stride + column) {}
+  __device__ __forceinline__ void fetch(long long t, CacheEight<T, F, D>& k, CacheEight<T, F, D>& v) const {  // row t of the call
+    if constexpr (MOVE) {
+      const unsigned slot = min(static_cast<unsigned>(p.from[t]), static_cast<unsigned>((p.num_pages << p.page_log2) - 1));
+      const long long at = cache_row(p, static_cast<int>(slot), h) * D + col;
+      k.load(p.k_pages, at);
+      v.load(p.v_pages, at);
+    } else {
+      const T *kp = k_new + t * p.k_token_stride, *vp = v_new + t * p.v_token_stride;
 #pragma unroll
-    for (int j = 0; j < static_cast<int>(sizeof(T)) / 2; ++j) {
-      k.raw[j] = ldg16(kp + 4 * j);
-      v.raw[j] = ldg16(vp + 4 * j);
+      for (int j = 0; j < static_cast<int>(sizeof(T)) / 2; ++j) {
+        k.raw[j] = ldg16(kp + 4 * j);
+        v.raw[j] = ldg16(vp + 4 * j);
+      }
     }
   }
-}
+};
 // Into the cache; k is what the cache then holds.
 template <bool MOVE, class Eight>
 __device__ __forceinline__ void write_row(const PagedAppendArgs& p, long long at, Eight& k, Eight& v) {
@@ -198,7 +205,7 @@ __global__ __launch_bounds__(LANES) void paged_append_kernel(PagedAppendArgs p) 
   const int slot = p.slots[x.t];
   if (!in_cache(p, slot)) return;
   CacheEight<T, F, D> k, v;
-  fetch_new<T, F, D, false>(p, x.t, x.h, 8 * x.piece, k, v);
+  Incoming<T, F, D, false>(p, x.h, 8 * x.piece).fetch(x.t, k, v);
   write_row<false>(p, cache_row(p, slot, x.h) * D + 8 * x.piece, k, v);
 }
 
@@ -404,6 +411,7 @@ __global__ __launch_bounds__(LANES) void paged_append_bounds_kernel(PagedAppendA
   for (int w = 0; w < LANES / 64; ++w) n = min(n, run_end[w]);
   const int rows = o0 + n, col = (tid % COLS) * 8, r0 = tid / COLS;
   const long long at = static_cast<long long>(s0 >> lp) * p.H + h, base = (at << lp) * D + col;
+  const Incoming<T, F, D, MOVE> incoming(p, h, col);
   Extremes<T> seen;
   for (int first = r0; first < rows; first += ROWS * U) {
     CacheEight<T, F, D> k[U], v[U];
@@ -414,7 +422,7 @@ __global__ __launch_bounds__(LANES) void paged_append_bounds_kernel(PagedAppendA
       if (r < o0)
         k[u].load(p.k_pages, base + r * D);
       else
-        fetch_new<T, F, D, MOVE>(p, t + r - o0, h, col, k[u], v[u]);
+        incoming.fetch(t + r - o0, k[u], v[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -472,6 +480,7 @@ __global__ __launch_bounds__(LANES) void paged_append_pages_kernel(PagedAppendAr
     const long long t = t0 + own;
     const int s0 = __builtin_amdgcn_readlane(mine, own), o0 = s0 & (page - 1);
     const long long at = static_cast<long long>(s0 >> lp) * p.H + h, base = (at << lp) * D + col;
+    const Incoming<T, F, D, MOVE> incoming(p, h, col);
     // New row i is row o0 + i of the page.
     CacheEight<T, F, D> k[U], v[U];
     const long long left = min(p.tokens - t, static_cast<long long>(page - o0));
@@ -479,7 +488,7 @@ __global__ __launch_bounds__(LANES) void paged_append_pages_kernel(PagedAppendAr
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int i = first + ROWS * u + r0;
-        if (i < left) fetch_new<T, F, D, MOVE>(p, t + i, h, col, k[u], v[u]);
+        if (i < left) incoming.fetch(t + i, k[u], v[u]);
       }
     };
     fetch(0);
