@@ -11,7 +11,7 @@
 //
 // Bound: the matrix pipe, and the vector work of the softmax next to it.  2 x 2048 new tokens over 4096 keys before them, 32
 // heads over 8, d = 128: 344 GFLOP in 340 us, 1.0 PFLOP/s (385 us where the clock falls under the load of many in a row); 8-bit
-// rows 12 % more, for their way through registers.  Whole scales of 8 requests, 16 heads, d = 64, 11520 tile steps:
+// rows 12 % more, for their way through registers, 4-bit rows no more.  Whole scales of 8 requests, 16 heads, d = 64, 11520 tile steps:
 // 44 us, twice the softmax for a product and 2 pieces to a workgroup.  Chosen pages, 1024 tokens, 32 of 272 pages each, 127 in
 // the union of 32 tokens: 96 us, as much as the union's products (57 GFLOP) at 0.6 PFLOP/s.
 #include <hip/hip_runtime.h>
@@ -125,8 +125,11 @@ __device__ __forceinline__ int build_union(const AttendParams& a, const Tile& t,
   return __builtin_amdgcn_readfirstlane(*u.count);
 }
 
+// 4-bit rows at d = 64 take 176 registers by themselves; held to 168, three workgroups share a compute unit instead of two: whole scales of 8
+// requests 59 us instead of 68, 3000 new tokens over 4096 keys 178 instead of 206, 16 x 300 228 instead of 252; where two to a unit come
+// out even, 230 instead of 222 (2 x 2048).
 template <int D, Format F, bool CHOSEN>
-__global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams p) {
+__global__ __launch_bounds__(256, D == 64 && F == E2M1 ? 3 : 2) void paged_attend_long_kernel(AttendParams p) {
   constexpr bool CODES = F == E4M3, FP4 = F == E2M1;
   constexpr int RB = 2 * D, TILE_BYTES = BN * RB, SRC = row_bytes<bf16_t, F>(D);
   constexpr int NK = D / 16, NV = D / 32;
@@ -515,7 +518,7 @@ __global__ __launch_bounds__(256, 2) void paged_attend_long_kernel(AttendParams 
     if constexpr (FP4) {
       // Codes are loaded a step before they are converted, V(it + 2) and K(it + 3) here, and a chunk of 8 columns is converted under a
       // product.  All of a tile's in one place, behind the products of the step that had loaded them, took 382 us instead of 346 for
-      // 2 x 2048 tokens over 4096 keys (d = 128), and 80 instead of 68 for whole scales at d = 64.
+      // 2 x 2048 tokens over 4096 keys (d = 128), and 80 instead of 68 for whole scales at d = 64 (both with two workgroups to a unit).
       __syncthreads();
       constexpr int CHUNKS = D / 32, GAP = 3, K0 = SLOTS / 2;
       math([&](int i) {
