@@ -38,6 +38,15 @@ constexpr int LEAST_STEPS = 4, WHOLE_STEPS = 8;
 // and 31 requests: 23.1 and 28.3 by pieces (as many as that takes), 20.2 and 26.9 on the line.
 constexpr int FEW_SEGMENTS = 128;
 
+// Where no segment can be cut, pieces are whole segments, one to a workgroup, and further workgroups for those that are more than are
+// resident; on the line a workgroup has up to four in its share, one after the other, and other workgroups have none.  Every workgroup
+// looks for its own, which takes longer from one request to a lane on.  Decoding with up to 240 keys, 8 heads, 16 and 64 requests of
+// different lengths, 4-bit rows: 8.9 and 10.5 us by pieces, 18.0 and 22.9 on the line; of equal lengths, bf16: 9.7 and 15.8, 10.2 and
+// 16.1; 128 requests: 22.5 and 42.6, of equal lengths 31.1 and 26.6.  A prompt of 240 tokens, fp32: 12.4 and 21.3, eight of them: 49.6
+// and 60.8.  Where the 128-row kernel is launched as well there may be nothing to do for the grid of a workgroup to a segment (eight
+// prompts of 240 tokens: 22.3 us, 16.6 without).
+constexpr int WHOLE_SEGMENTS = 2560, WHOLE_BATCH = 64;
+
 // Requests of more query rows (new tokens x queries per kv head) than this are the 128-row kernel's, which reads their keys
 // once for 128 rows, and computes for 128 as well.  16 requests of 4096 keys, 4 query rows a token: 5 tokens 98 us with 16
 // rows a tile, 70 with 128, 16 tokens 174 and 83.  With chosen pages tiles of fewer tokens read fewer pages: 12 requests of
@@ -81,6 +90,11 @@ inline Plan plan_launches(bool bf16, int batch, int kv_heads, int group, int64_t
     const bool cut = longest > WHOLE_STEPS * 64;
     p.many.grid = cut ? std::max(segments, pieces) : segments;
     p.many.parts = cut ? static_cast<int>(pieces) : 0;
+  }
+  if (!p.few.parts && batch <= WHOLE_BATCH) {
+    const int64_t segments = kv_heads * (rows / 16 + std::min<int64_t>(batch, tokens));
+    if (!p.many.workgroups && segments <= WHOLE_SEGMENTS) p.few.grid = std::max(segments, p.few.grid);
+    p.few.whole_from = static_cast<int>(p.few.grid) + 1;
   }
   return p;
 }

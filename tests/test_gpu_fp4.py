@@ -389,6 +389,19 @@ def test_many_requests(heads, top, batch):
     p.check(True, p.run(True, _ints(sel) if top else None), sel)
 
 
+@pytest.mark.parametrize("dtype", ["fp4", "fp8", "bf16", "f32"])
+@pytest.mark.parametrize("batch,heads,new", [(1, 8, 240), (3, 8, 256), (10, 8, 240), (64, 8, 1), (64, 21, 1), (63, 20, 2), (64, 1, 17), (65, 8, 1),
+                                             (8, 64, 30)])
+def test_short_caches_of_many_segments(dtype, batch, heads, new):
+    # none is cut: a workgroup to a segment up to 64 requests and 2560 segments, else up to 512 of them
+    r = random.Random(batch)
+    lens = [r.randint(new, 256) for _ in range(batch)]
+    case = (2 * heads, heads, 64, 16, lens, [r.choice((new, new, max(new // 2, 1), 0)) for _ in range(batch)])
+    p = Fp4Problem(*case, seed=batch, max_pages=16) if dtype == "fp4" else Problem(dtype, *case, seed=batch, max_pages=16)
+    for causal in (True, False):
+        p.check(causal, p.run(causal))
+
+
 @pytest.mark.parametrize("case,top", [(c, 0) for c in CASES[3:9] + CASES[-4:]] + [
     ((4, 2, 64, 16, [n for n in (900, 300, 40) for _ in range(30)], [n for n in (1, 2, 70) for _ in range(30)]), 0),
     ((8, 8, 64, 32, [2000] * 40, [1] * 40), 6), ((4, 2, 128, 64, [3000, 900], [90, 70]), 9)], ids=lambda x: str(x)[:50])

@@ -9,7 +9,7 @@ import torch
 import paper_2605_14877_amd as hk
 from paper_2605_14877_amd import paged
 from tests import share_reference as sref
-from tests.test_paged_cpu import BAD_SHAPES, _fail, _shape
+from tests.test_paged_cpu import BAD_SHAPES, _fail, _shape, rules  # noqa: F401
 
 at = lambda i: (i + 1) << 36  # noqa: E731  addresses are never followed: every call is refused
 TOKENS, MOVES = 4, 9
@@ -212,3 +212,31 @@ def test_reference_tables_keep_every_page_once():
             assert sorted(free + [p for p, n in enumerate(s.holders) if n]) == list(range(R))
             for b in range(B):
                 assert [content[s.table[b][x // page] * page + x % page] for x in range(s.lens[b])] == rows[b]
+
+
+def test_short_caches_have_a_workgroup_for_each_segment(rules):  # noqa: F811
+    # where nothing is cut and there are few segments they are whole pieces: as many workgroups as segments there may be
+    for bf16, batch, heads, group, new, grid in (
+            (True, 1, 8, 4, 1, 512), (True, 16, 8, 2, 1, 512), (True, 64, 8, 2, 1, 576), (True, 64, 32, 1, 1, 2176), (True, 64, 38, 1, 1, 512), (True, 64, 20, 1, 1, 1360),
+            (True, 1, 8, 2, 40, 512), (False, 1, 8, 2, 240, 512), (False, 4, 8, 2, 240, 992), (False, 64, 1, 16, 30, 1984),
+            (False, 64, 2, 16, 30, 512), (True, 4, 8, 2, 240, 512)):
+        few, many, _ = rules(bf16, batch, heads, group, batch * new, 16, 16)
+        assert few["parts"] == 0 and few["grid"] == grid and few["whole_from"] == grid + 1
+        assert bool(many["workgroups"]) == (bf16 and new == 240)
+    for batch in (65, 300):  # more requests than lanes
+        few, _, _ = rules(True, batch, 8, 2, batch, 16, 16)
+        assert few["whole_from"] == 128 and few["grid"] == 512 and few["parts"] == 0
+    for batch in (1, 16, 64, 65, 300):  # a cache whose segments may be cut
+        few, _, _ = rules(True, batch, 8, 2, batch, 17, 16)
+        assert few["whole_from"] == 128 and few["grid"] == 512 and few["parts"] == 1024
+
+
+def test_no_segment_of_a_short_cache_is_left_out(rules):  # noqa: F811
+    import random
+    r = random.Random(4)
+    for _ in range(2000):
+        group, heads, batch = r.choice([1, 2, 3, 5, 16]), r.choice([1, 2, 8, 20, 64]), r.choice([1, 2, 5, 40, 64, 65, 300])
+        new = [r.choice([0, 1, 1, 2, 5, 16, 17, 100, 240]) if r.random() < 0.7 else 1 for _ in range(batch)]
+        few, _, _ = rules(r.random() < 0.5, batch, heads, group, sum(new) + r.choice([0, 1, 9]), 16, 16)
+        segments = heads * sum(-(-n * group // 16) for n in new if n * group <= few["most_rows"])
+        assert segments >= few["whole_from"] or segments <= few["grid"]
