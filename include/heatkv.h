@@ -373,7 +373,8 @@ int heatkv_paged_assign(const heatkv_paged_shape* shape, const int32_t* keep, co
  * in the order of their rows, as heatkv_paged_assign makes them.
  *   bounds        int8 [num_pages][kv_heads][2][d]: the largest key value of a channel and minus the smallest one, in units of
  *   bound_scales  fp32 [num_pages][kv_heads], a power of two: the least one, from 2^-100 on, of which no value is more than
- *                 127 times; rounded upwards.  Values beyond +-2^127 count as that, NaN as 0.  8-bit rows: of the codes' values. */
+ *                 127 times; rounded upwards.  Values beyond +-2^127 count as that, NaN as 0.  8-bit and 4-bit rows: of the values
+ *                 that the cache holds. */
 int heatkv_paged_append(const heatkv_paged_shape* shape, const int32_t* slots, int64_t tokens, heatkv_rows k_new,
                         heatkv_rows v_new, void* k_pages, void* v_pages, int8_t* bounds, float* bound_scales, void* stream);
 

@@ -9,7 +9,8 @@
 // Bound: memory traffic for prompts (rows in, rows out, 16 bytes per lane), latency for single tokens.  A page's bounds are
 // formed anew from all of its valid rows, which costs a decoding step up to a page of older rows per head, but needs no
 // running state that would have to follow when tokens are dropped or pages change owners.  12 prompts, 12000 tokens, 8 heads, d =
-// 128, into 8-bit pages: 73.5 MB in 21 us, 3.5 TB/s; the rows alone take 13 us.
+// 128, into 8-bit pages: 73.5 MB in 21 us, 3.5 TB/s; the rows alone take 13 us.  4-bit pages, without bounds: 11820 tokens,
+// 61 MB, 12.9 us, 4.8 TB/s, and back as values 13.3 us.  Rows moved, 65900 of bf16: 540 MB in 84 to 94 us, 5.7 to 6.4 TB/s.
 #include <type_traits>
 
 #include "copy_rows.h"

@@ -1,7 +1,8 @@
 // Attention of new tokens over the paged cache, bf16, for requests with many query rows (chunks of prompts, whole scales):
 // the tile loop of attend.hip over keys that lie on pages.
 //
-// Workgroup = 4 wavefronts x 32 query rows (row = token x query of the kv head's group), two workgroups per compute unit.
+// Workgroup = 4 wavefronts x 32 query rows (row = token x query of the kv head's group), two workgroups per compute unit (4-bit rows at
+// d = 64: three).
 // The request's keys are walked in tiles of 64, four granules of 16 rows, each with an address of its own; tile format,
 // copies and operand layouts are those of tile_lds.h.  Rows behind the request's end arrive as zeros (range-checked
 // copies), keys that a row does not see get a score of -inf in the tiles where that can be.
