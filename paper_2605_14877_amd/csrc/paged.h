@@ -170,9 +170,10 @@ struct AttendParams {
   Parts parts;
 };
 
-// The launch's arguments, loaded anew.
+// The launch's arguments, loaded anew; of a launch with several, those at place WHICH.
+template <int WHICH = 0>
 __device__ __forceinline__ const AttendParams& arguments() {
-  auto* at = (const __attribute__((address_space(4))) AttendParams*)__builtin_amdgcn_kernarg_segment_ptr();
+  auto* at = (const __attribute__((address_space(4))) AttendParams*)__builtin_amdgcn_kernarg_segment_ptr() + WHICH;
   asm volatile("; arguments" : "+s"(at));
   return *(const AttendParams*)at;
 }
@@ -195,7 +196,9 @@ using PagedParts = paged::Parts;
 constexpr size_t PAGED_SELECT_LDS = paged::SELECT_LDS;
 hipError_t launch_paged_select(const PagedSelectParams& p, int dtype, int d, hipStream_t stream);
 hipError_t launch_paged_attend_bf16(const PagedAttendParams& p, int d, int kv_format, hipStream_t stream);
-hipError_t launch_paged_attend_long(const PagedAttendParams& p, int d, int kv_format, hipStream_t stream);
+// few: of the requests with few rows, which it takes along if paged_attend_long_takes_few().
+inline bool paged_attend_long_takes_few(const PagedAttendParams& p) { return !p.selected; }
+hipError_t launch_paged_attend_long(const PagedAttendParams& p, const PagedAttendParams& few, int d, int kv_format, hipStream_t stream);
 hipError_t launch_paged_attend_f32(const PagedAttendParams& p, int d, hipStream_t stream);
 // few, many: of the two attention launches, grid: join_workgroups(), 0 where there is nothing to join.
 hipError_t launch_paged_join(const PagedAttendParams& p, const PagedParts& few, const PagedParts& many, int dtype, int d,

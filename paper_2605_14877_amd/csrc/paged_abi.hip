@@ -273,32 +273,36 @@ int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const voi
   p.sm_scale = sm_scale;
   p.lse = lse;
   const auto hip_stream = static_cast<hipStream_t>(stream);
-  hipError_t e = hipSuccess;
-  // Makes one of the two launches; its parts, for the join.
-  auto launch = [&](const heatkv::paged::Launch& l, const PartArrays& a, bool many) {
-    heatkv::PagedParts parts{};
-    if (!l.workgroups || e != hipSuccess) return parts;
+  // The arguments of one of the two kernels.
+  auto arguments = [&](const heatkv::paged::Launch& l, const PartArrays& a) {
+    heatkv::paged::AttendParams x = p;
+    if (!l.workgroups) return x;  // no grid
     if (l.parts) {
-      parts.o = reinterpret_cast<float*>(static_cast<char*>(ws) + a.o);
-      parts.ml = reinterpret_cast<float*>(static_cast<char*>(ws) + a.ml);
-      parts.borders = reinterpret_cast<heatkv::paged::Border*>(static_cast<char*>(ws) + a.borders);
+      x.parts.o = reinterpret_cast<float*>(static_cast<char*>(ws) + a.o);
+      x.parts.ml = reinterpret_cast<float*>(static_cast<char*>(ws) + a.ml);
+      x.parts.borders = reinterpret_cast<heatkv::paged::Border*>(static_cast<char*>(ws) + a.borders);
     }
-    parts.grid = int(l.grid);
-    p.workgroups = l.workgroups;
-    p.least_weight = l.least_steps * heatkv::paged::STEP_WEIGHT;
-    p.cut_from = l.parts ? p.least_weight : INT_MAX;
-    p.least_rows = l.least_rows;
-    p.most_rows = l.most_rows;
-    p.whole_from = l.whole_from;
-    p.parts = parts;
-    e = s->dtype == HEATKV_F32 ? heatkv::launch_paged_attend_f32(p, s->d, hip_stream)
-        : many                 ? heatkv::launch_paged_attend_long(p, s->d, s->kv_format, hip_stream)
-                               : heatkv::launch_paged_attend_bf16(p, s->d, s->kv_format, hip_stream);
-    parts.grid = heatkv::paged::join_workgroups(l);
-    return parts;
+    x.parts.grid = int(l.grid);
+    x.workgroups = l.workgroups;
+    x.least_weight = l.least_steps * heatkv::paged::STEP_WEIGHT;
+    x.cut_from = l.parts ? x.least_weight : INT_MAX;
+    x.least_rows = l.least_rows;
+    x.most_rows = l.most_rows;
+    x.whole_from = l.whole_from;
+    return x;
   };
-  const heatkv::PagedParts many = launch(plan.many, w.many, true), few = launch(plan.few, w.few, false);
-  if (e == hipSuccess && few.grid + many.grid > 0) e = heatkv::launch_paged_join(p, few, many, s->dtype, s->d, hip_stream);
+  heatkv::paged::AttendParams many = arguments(plan.many, w.many), few = arguments(plan.few, w.few);
+  hipError_t e = hipSuccess;
+  const bool together = many.parts.grid > 0 && heatkv::paged_attend_long_takes_few(many);
+  if (many.parts.grid > 0) e = heatkv::launch_paged_attend_long(many, few, s->d, s->kv_format, hip_stream);
+  if (e == hipSuccess && !together)
+    e = s->dtype == HEATKV_F32 ? heatkv::launch_paged_attend_f32(few, s->d, hip_stream)
+                               : heatkv::launch_paged_attend_bf16(few, s->d, s->kv_format, hip_stream);
+  // The join looks at the workgroups that may have parts.
+  many.parts.grid = many.parts.grid > 0 ? heatkv::paged::join_workgroups(plan.many) : 0;
+  few.parts.grid = heatkv::paged::join_workgroups(plan.few);
+  if (e == hipSuccess && few.parts.grid + many.parts.grid > 0)
+    e = heatkv::launch_paged_join(few, few.parts, many.parts, s->dtype, s->d, hip_stream);
   return launched(e, "paged_attend");
 }
 

@@ -1,4 +1,4 @@
-// Attention of new tokens over the paged cache, fp32 (paged_attend.hip describes segments and walks; attend_f32.hip the
+// Attention of new tokens over the paged cache, fp32 (paged_attend_few.h describes segments and walks; attend_f32.hip the
 // operands and the arithmetic: K through a wavefront's LDS stage, V straight into registers, 16x16x4 fp32 MFMAs).
 //
 // A segment has 16 query rows; the workgroup's four wavefronts take granules of 16 keys in turn.

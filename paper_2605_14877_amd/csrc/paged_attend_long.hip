@@ -1,6 +1,8 @@
 // Attention of new tokens over the paged cache, bf16, for requests with many query rows (chunks of prompts, whole scales):
 // the tile loop of attend.hip over keys that lie on pages.
 //
+// Over all pages the grid has the workgroups of the 16-row kernel as well (FEW_FIRST).
+//
 // Workgroup = 4 wavefronts x 32 query rows (row = token x query of the kv head's group), two workgroups per compute unit (4-bit rows at
 // d = 64: three).
 // The request's keys are walked in tiles of 64, four granules of 16 rows, each with an address of its own; tile format,
@@ -11,7 +13,7 @@
 // the request, which choose alike), with a word of 32 tokens for each wavefront and page.
 //
 // Bound: the matrix pipe, and the vector work of the softmax next to it.  2 x 2048 new tokens over 4096 keys before them, 32
-// heads over 8, d = 128: 344 GFLOP in 340 us, 1.0 PFLOP/s (385 us where the clock falls under the load of many in a row); 8-bit
+// heads over 8, d = 128: 344 GFLOP in 335 us, 1.0 PFLOP/s (385 us where the clock falls under the load of many in a row); 8-bit
 // rows 12 % more, for their way through registers, 4-bit rows no more.  Whole scales of 8 requests, 16 heads, d = 64, 11520 tile steps:
 // 44 us, twice the softmax for a product and 2 pieces to a workgroup.  Chosen pages, 1024 tokens, 32 of 272 pages each, 127 in
 // the union of 32 tokens: 96 us, as much as the union's products (57 GFLOP) at 0.6 PFLOP/s.
@@ -21,6 +23,7 @@
 
 #include "kernels.h"
 #include "paged.h"
+#include "paged_attend_few.h"
 #include "paged_redo.h"
 #include "paged_rules.h"
 #include "paged_schedule.h"
@@ -128,9 +131,19 @@ __device__ __forceinline__ int build_union(const AttendParams& a, const Tile& t,
 
 // 4-bit rows at d = 64 take 176 registers by themselves; held to 168, three workgroups share a compute unit instead of two: whole scales of 8
 // requests 59 us instead of 68, 3000 new tokens over 4096 keys 178 instead of 206, 16 x 300 228 instead of 252; where two to a unit come
-// out even, 230 instead of 222 (2 x 2048).
+// out even, 230 instead of 222 (2 x 2048); all with the 16-row kernel in a launch of its own.
+// few: the 16-row kernel's launch (paged_attend_few.h), whose workgroups are the grid's from few_at on, 0 or behind this kernel's own.  As a
+// launch of its own it took 4 to 8 us where it had next to nothing to do, and what it did have did not run beside this.
 template <int D, Format F, bool CHOSEN>
-__global__ __launch_bounds__(256, D == 64 && F == E2M1 ? 3 : 2) void paged_attend_long_kernel(AttendParams p) {
+__global__ __launch_bounds__(256, D == 64 && F == E2M1 ? 3 : 2) void paged_attend_long_kernel(AttendParams p, AttendParams few, int few_at) {
+  int w = blockIdx.x;
+  if constexpr (!CHOSEN) {
+    if (static_cast<unsigned>(w - few_at) < static_cast<unsigned>(few.parts.grid)) {
+      constexpr int STAGES = FEW_WAVES * stage_bytes(D);
+      return attend_few<D, F, false, 1>(few, w - few_at, *reinterpret_cast<FewShared*>(paged_long_lds + STAGES), paged_long_lds, nullptr);
+    }
+    if (few_at == 0) w -= few.parts.grid;
+  }
   constexpr bool CODES = F == E4M3, FP4 = F == E2M1;
   constexpr int RB = 2 * D, TILE_BYTES = BN * RB, SRC = row_bytes<bf16_t, F>(D);
   constexpr int NK = D / 16, NV = D / 32;
@@ -142,7 +155,6 @@ __global__ __launch_bounds__(256, D == 64 && F == E2M1 ? 3 : 2) void paged_atten
 
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, hl = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int w = blockIdx.x;
   const unsigned lds_base = static_cast<unsigned>(reinterpret_cast<unsigned long long>(
       (__attribute__((address_space(3))) char*)(paged_long_lds)));
   const unsigned lds_wave = __builtin_amdgcn_readfirstlane(lds_base + wave * 1024);
@@ -734,25 +746,27 @@ __global__ __launch_bounds__(256, D == 64 && F == E2M1 ? 3 : 2) void paged_atten
 }
 
 template <int D, Format F, bool CHOSEN>
-hipError_t launch(const AttendParams& p, hipStream_t stream) {
+hipError_t launch(const AttendParams& p, const AttendParams& few, hipStream_t stream) {
+  static_assert(FEW_WAVES * stage_bytes(D) + sizeof(FewShared) <= 4 * BN * 2 * D + kUnionAt, "the workgroups of few rows have room");
   const size_t lds = 4 * BN * 2 * D + kUnionAt + (CHOSEN ? many_union_bytes(p.c.G, p.c.max_pages, p.top) : 0);
   static std::atomic<unsigned long long> allowed{0};
   if (lds > 64 * 1024)
     if (hipError_t e = allow_lds(reinterpret_cast<const void*>(&paged_attend_long_kernel<D, F, CHOSEN>), MANY_LDS, allowed)) return e;
-  hipLaunchKernelGGL((paged_attend_long_kernel<D, F, CHOSEN>), dim3(p.parts.grid), dim3(256), lds, stream, p);
+  hipLaunchKernelGGL((paged_attend_long_kernel<D, F, CHOSEN>), dim3(p.parts.grid + (CHOSEN ? 0 : few.parts.grid)), dim3(256), lds, stream, p, few,
+                     p.c.batch > FEW_FIRST ? 0 : p.parts.grid);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_paged_attend_long(const PagedAttendParams& p, int d, int kv_format, hipStream_t stream) {
+hipError_t launch_paged_attend_long(const PagedAttendParams& p, const PagedAttendParams& few, int d, int kv_format, hipStream_t stream) {
   static_assert(4 * BN * 2 * 128 + kUnionAt + MANY_UNION_BYTES <= MANY_LDS, "the largest union that plan_launches() sends here fits");
   auto run = [&](auto d_tag, auto chosen) {
     constexpr int D = decltype(d_tag)::value;
     constexpr bool CHOSEN = decltype(chosen)::value;
-    return kv_format == HEATKV_KV_FP4_E2M1   ? launch<D, E2M1, CHOSEN>(p, stream)
-           : kv_format == HEATKV_KV_FP8_E4M3 ? launch<D, E4M3, CHOSEN>(p, stream)
-                                             : launch<D, NATIVE, CHOSEN>(p, stream);
+    return kv_format == HEATKV_KV_FP4_E2M1   ? launch<D, E2M1, CHOSEN>(p, few, stream)
+           : kv_format == HEATKV_KV_FP8_E4M3 ? launch<D, E4M3, CHOSEN>(p, few, stream)
+                                             : launch<D, NATIVE, CHOSEN>(p, few, stream);
   };
   using D128 = std::integral_constant<int, 128>;
   using D64 = std::integral_constant<int, 64>;

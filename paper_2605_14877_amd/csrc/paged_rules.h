@@ -44,7 +44,7 @@ constexpr int FEW_SEGMENTS = 128;
 // different lengths, 4-bit rows: 8.9 and 10.5 us by pieces, 18.0 and 22.9 on the line; of equal lengths, bf16: 9.7 and 15.8, 10.2 and
 // 16.1; 128 requests: 22.5 and 42.6, of equal lengths 31.1 and 26.6.  A prompt of 240 tokens, fp32: 12.4 and 21.3, eight of them: 49.6
 // and 60.8.  Where the 128-row kernel is launched as well there may be nothing to do for the grid of a workgroup to a segment (eight
-// prompts of 240 tokens: 22.3 us, 16.6 without).
+// prompts of 240 tokens: 18.0 us, 13.4 without).
 constexpr int WHOLE_SEGMENTS = 2560, WHOLE_BATCH = 64;
 
 // Requests of more query rows (new tokens x queries per kv head) than this are the 128-row kernel's, which reads their keys
@@ -54,9 +54,16 @@ constexpr int WHOLE_SEGMENTS = 2560, WHOLE_BATCH = 64;
 constexpr int MANY_ROWS = 16, MANY_CHOSEN_ROWS = 64;
 
 // More tokens than one for each request and this: before, the call is taken for a decoding step, with padding rows or a few
-// tokens that are checked at once, and not worth the second kernel's launch and the longer join (up to 10 us) to look for long requests.
-// One request, 24 tokens at 1000, 8000 and 32000 keys: 16, 31 and 80 us by the 16-row kernel alone, 24, 32 and 59 with both.
+// tokens that are checked at once, and not worth the second kernel's workgroups and the longer join (3 us) to look for long requests.
+// One request, 24 tokens at 1000, 8000 and 32000 keys: 16, 29 and 80 us by the 16-row kernel alone, 19, 26 and 48 with both.
 constexpr int FEW_TOKENS = 40, FEW_TOKENS_LONG = 16, LONG_CACHE = 16384;
+
+// Over all pages one launch has the workgroups of both kernels.  Those of many rows come first, and what few requests of few rows there
+// may be falls into the gaps at their end; from more requests than this on those of few rows come first, which read memory while the
+// others compute.  Many rows first, few rows first, two launches, bf16, d = 128: 8 requests that decode over 1000 keys and two prompts of
+// 300 tokens 27, 31, 34 us, 32 and two 39, 42, 48, 48 and two 52, 52, 59; 32 requests over 9000 keys and 1000 new tokens over 2000: 283, 260,
+// 285, 48 and those 382, 356, 386; whole scales of 8 requests, 4-bit rows, d = 64: 51, 56, 59.
+constexpr int FEW_FIRST = 32;
 
 // LDS of the 128-row kernel for the union of its tokens' chosen pages: a bit and a count for each word of the request's pages,
 // 24 bytes for each page that may be in it.  Larger unions are left to the 16-row kernel, whose tiles have fewer tokens.

@@ -389,6 +389,23 @@ def test_many_requests(heads, top, batch):
     p.check(True, p.run(True, _ints(sel) if top else None), sel)
 
 
+@pytest.mark.parametrize("dtype", ["fp4", "fp8", "bf16"])
+@pytest.mark.parametrize("d,group", [(64, 1), (128, 4)])
+@pytest.mark.parametrize("batch", [2, 32, 33, 130])
+def test_few_and_many_rows_in_one_call(dtype, d, group, batch):
+    # one launch has both, in either order (up to 32 requests and beyond): tokens that decode, drafts, prompts, requests without work
+    r = random.Random(batch)
+    lens = [r.choice((1, 30, 300, 1200)) for _ in range(batch)]
+    new = [min(n, r.choice((0, 1, 1, 1, 5, 20))) for n in lens]
+    lens[-1], new[-1] = 500, 170
+    case = (2 * group, 2, d, 16, lens, new)
+    p = Fp4Problem(*case, seed=batch) if dtype == "fp4" else Problem(dtype, *case, seed=batch)
+    for causal in (True, False):
+        first, again = p.run(causal), p.run(causal)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+        p.check(causal, first)
+
+
 @pytest.mark.parametrize("dtype", ["fp4", "fp8", "bf16", "f32"])
 @pytest.mark.parametrize("batch,heads,new", [(1, 8, 240), (3, 8, 256), (10, 8, 240), (64, 8, 1), (64, 21, 1), (63, 20, 2), (64, 1, 17), (65, 8, 1),
                                              (8, 64, 30)])
