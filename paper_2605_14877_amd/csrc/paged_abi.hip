@@ -292,12 +292,9 @@ int attend(const heatkv_paged_shape* s, int64_t tokens, heatkv_rows q, const voi
     return x;
   };
   heatkv::paged::AttendParams many = arguments(plan.many, w.many), few = arguments(plan.few, w.few);
-  hipError_t e = hipSuccess;
-  const bool together = many.parts.grid > 0 && heatkv::paged_attend_long_takes_few(many);
-  if (many.parts.grid > 0) e = heatkv::launch_paged_attend_long(many, few, s->d, s->kv_format, hip_stream);
-  if (e == hipSuccess && !together)
-    e = s->dtype == HEATKV_F32 ? heatkv::launch_paged_attend_f32(few, s->d, hip_stream)
-                               : heatkv::launch_paged_attend_bf16(few, s->d, s->kv_format, hip_stream);
+  hipError_t e = many.parts.grid > 0      ? heatkv::launch_paged_attend_long(many, few, s->d, s->kv_format, hip_stream)
+                 : s->dtype == HEATKV_F32 ? heatkv::launch_paged_attend_f32(few, s->d, hip_stream)
+                                          : heatkv::launch_paged_attend_bf16(few, s->d, s->kv_format, hip_stream);
   // The join looks at the workgroups that may have parts.
   many.parts.grid = many.parts.grid > 0 ? heatkv::paged::join_workgroups(plan.many) : 0;
   few.parts.grid = heatkv::paged::join_workgroups(plan.few);

@@ -36,6 +36,7 @@ struct FewShared {
   Line line;
   unsigned nan_rows;
 };
+constexpr int FEW_SHARED = (sizeof(FewShared) + 15) / 16 * 16;
 
 // Workgroup w of the launch; WHICH: place of `p` among the kernel's arguments.  `few_stages`: LDS, FEW_WAVES * stage_bytes(D) bytes; `few_walk`:
 // walk_lds_bytes(p) bytes with chosen pages.

@@ -1,7 +1,7 @@
 // Attention of new tokens over the paged cache, bf16, for requests with many query rows (chunks of prompts, whole scales):
 // the tile loop of attend.hip over keys that lie on pages.
 //
-// Over all pages the grid has the workgroups of the 16-row kernel as well (FEW_FIRST).
+// The grid has the workgroups of the 16-row kernel as well (FEW_FIRST).
 //
 // Workgroup = 4 wavefronts x 32 query rows (row = token x query of the kv head's group), two workgroups per compute unit (4-bit rows at
 // d = 64: three).
@@ -137,13 +137,12 @@ __device__ __forceinline__ int build_union(const AttendParams& a, const Tile& t,
 template <int D, Format F, bool CHOSEN>
 __global__ __launch_bounds__(256, D == 64 && F == E2M1 ? 3 : 2) void paged_attend_long_kernel(AttendParams p, AttendParams few, int few_at) {
   int w = blockIdx.x;
-  if constexpr (!CHOSEN) {
-    if (static_cast<unsigned>(w - few_at) < static_cast<unsigned>(few.parts.grid)) {
-      constexpr int STAGES = FEW_WAVES * stage_bytes(D);
-      return attend_few<D, F, false, 1>(few, w - few_at, *reinterpret_cast<FewShared*>(paged_long_lds + STAGES), paged_long_lds, nullptr);
-    }
-    if (few_at == 0) w -= few.parts.grid;
+  if (static_cast<unsigned>(w - few_at) < static_cast<unsigned>(few.parts.grid)) {
+    constexpr int STAGES = FEW_WAVES * stage_bytes(D);
+    return attend_few<D, F, CHOSEN, 1>(few, w - few_at, *reinterpret_cast<FewShared*>(paged_long_lds + STAGES), paged_long_lds,
+                                       paged_long_lds + STAGES + FEW_SHARED);
   }
+  if (few_at == 0) w -= few.parts.grid;
   constexpr bool CODES = F == E4M3, FP4 = F == E2M1;
   constexpr int RB = 2 * D, TILE_BYTES = BN * RB, SRC = row_bytes<bf16_t, F>(D);
   constexpr int NK = D / 16, NV = D / 32;
@@ -747,12 +746,13 @@ __global__ __launch_bounds__(256, D == 64 && F == E2M1 ? 3 : 2) void paged_atten
 
 template <int D, Format F, bool CHOSEN>
 hipError_t launch(const AttendParams& p, const AttendParams& few, hipStream_t stream) {
-  static_assert(FEW_WAVES * stage_bytes(D) + sizeof(FewShared) <= 4 * BN * 2 * D + kUnionAt, "the workgroups of few rows have room");
+  static_assert(FEW_WAVES * stage_bytes(D) + FEW_SHARED <= 4 * BN * 2 * D + kUnionAt, "the workgroups of few rows have room");
+  // With chosen pages as well: walk_lds_bytes() is for the union of no more tokens, of which each page takes 8 bytes instead of 24.
   const size_t lds = 4 * BN * 2 * D + kUnionAt + (CHOSEN ? many_union_bytes(p.c.G, p.c.max_pages, p.top) : 0);
   static std::atomic<unsigned long long> allowed{0};
   if (lds > 64 * 1024)
     if (hipError_t e = allow_lds(reinterpret_cast<const void*>(&paged_attend_long_kernel<D, F, CHOSEN>), MANY_LDS, allowed)) return e;
-  hipLaunchKernelGGL((paged_attend_long_kernel<D, F, CHOSEN>), dim3(p.parts.grid + (CHOSEN ? 0 : few.parts.grid)), dim3(256), lds, stream, p, few,
+  hipLaunchKernelGGL((paged_attend_long_kernel<D, F, CHOSEN>), dim3(p.parts.grid + few.parts.grid), dim3(256), lds, stream, p, few,
                      p.c.batch > FEW_FIRST ? 0 : p.parts.grid);
   return hipGetLastError();
 }

@@ -58,7 +58,7 @@ constexpr int MANY_ROWS = 16, MANY_CHOSEN_ROWS = 64;
 // One request, 24 tokens at 1000, 8000 and 32000 keys: 16, 29 and 80 us by the 16-row kernel alone, 19, 26 and 48 with both.
 constexpr int FEW_TOKENS = 40, FEW_TOKENS_LONG = 16, LONG_CACHE = 16384;
 
-// Over all pages one launch has the workgroups of both kernels.  Those of many rows come first, and what few requests of few rows there
+// Where both kernels have work, one launch has the workgroups of both.  Those of many rows come first, and what few requests of few rows there
 // may be falls into the gaps at their end; from more requests than this on those of few rows come first, which read memory while the
 // others compute.  Many rows first, few rows first, two launches, bf16, d = 128: 8 requests that decode over 1000 keys and two prompts of
 // 300 tokens 27, 31, 34 us, 32 and two 39, 42, 48, 48 and two 52, 52, 59; 32 requests over 9000 keys and 1000 new tokens over 2000: 283, 260,

@@ -404,6 +404,8 @@ def test_few_and_many_rows_in_one_call(dtype, d, group, batch):
         first, again = p.run(causal), p.run(causal)
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
         p.check(causal, first)
+    sel = [[[r.randrange(0, 60) for _ in range(4)] for _ in range(p.H)] for _ in range(p.tokens)]
+    p.check(True, p.run(True, _ints(sel)), sel)
 
 
 @pytest.mark.parametrize("dtype", ["fp4", "fp8", "bf16", "f32"])
