@@ -546,7 +546,8 @@ hipError_t launch(const PagedAppendArgs& a, hipStream_t stream) {
       // 24.8, 21.4, 25.2 (22.8 with the 46 that they get here).
       const int chunk = static_cast<int>(std::min<long long>(std::max<long long>(units / 2048, 1), std::min(64, 3 << a.page_log2 >> 2)));
       const long long groups = (a.tokens + chunk * (LANES / 64) - 1) / (chunk * (LANES / 64));
-      hipLaunchKernelGGL((paged_append_pages_kernel<T, F, D, MOVE>), dim3(static_cast<unsigned>(groups * a.H)), dim3(LANES), 0, stream, a, chunk);
+      hipLaunchKernelGGL((paged_append_pages_kernel<T, F, D, MOVE>), dim3(static_cast<unsigned>(groups * a.H)), dim3(LANES), 0, stream, a,
+                         chunk);
     }
   };
   if (a.d == 128)

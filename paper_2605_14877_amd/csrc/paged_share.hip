@@ -882,7 +882,8 @@ hipError_t launch_paged_assign_shared(const AssignSharedArgs& a, hipStream_t str
   // A token each, most of them to pages that are shared, as above: 64 requests 9.4 us by one workgroup and 12.9 by launches of many, 512
   // requests 12.3 and 15.1.  The limits are of what it goes through alone: tokens, copies, entries of the table that may all be let go.
   const long long copies = static_cast<long long>(a.t.batch) << a.t.page_log2;
-  if (fits<SMALL_BATCH, SMALL_PAGES>(a.t) && a.max_tokens <= 4 * LANES && copies <= 8 * LANES && static_cast<long long>(a.t.batch) * a.t.max_pages <= 32 * LANES) {
+  if (fits<SMALL_BATCH, SMALL_PAGES>(a.t) && a.max_tokens <= 4 * LANES && copies <= 8 * LANES &&
+      static_cast<long long>(a.t.batch) * a.t.max_pages <= 32 * LANES) {
     hipLaunchKernelGGL(paged_assign_small_kernel, dim3(1), dim3(LANES), 0, stream, a);
     return hipGetLastError();
   }
@@ -890,8 +891,8 @@ hipError_t launch_paged_assign_shared(const AssignSharedArgs& a, hipStream_t str
   hipLaunchKernelGGL(paged_assign_plan_kernel, dim3(1 + std::min((words + LANES - 1) / LANES, 64)), dim3(LANES), 0, stream, a);
   if (hipError_t e = hipGetLastError()) return e;
   const long long work = std::max(a.max_tokens, copies);
-  hipLaunchKernelGGL(paged_assign_move_kernel, dim3(static_cast<unsigned>(std::min<long long>((work + LANES - 1) / LANES + a.t.batch / 32, 128))),
-                     dim3(LANES), 0, stream, a);
+  const auto groups = static_cast<unsigned>(std::min<long long>((work + LANES - 1) / LANES + a.t.batch / 32, 128));
+  hipLaunchKernelGGL(paged_assign_move_kernel, dim3(groups), dim3(LANES), 0, stream, a);
   if (hipError_t e = hipGetLastError()) return e;
   return launch_give_back(a.t, stream);
 }

@@ -1,7 +1,8 @@
 """Binding of the paged cache's calls (include/heatkv.h, "Paged cache"): same names, argument marshalling and checks only.
 
 Token tensors are [tokens, heads, d] with any token and head stride; pages [num_pages, kv_heads, page_size, d] in the shape's
-dtype, or E4M3 codes as torch.float8_e4m3fn or torch.uint8; 4-bit pages [num_pages, kv_heads, bytes of a page] are torch.uint8.  Integer arrays are int32 device tensors.
+dtype, or E4M3 codes as torch.float8_e4m3fn or torch.uint8; 4-bit pages [num_pages, kv_heads, bytes of a page] are torch.uint8.
+Integer arrays are int32 device tensors.
 
 Calls go through the module _heatkv_call first (csrc/call_path.cpp: the same checks without the interpreter); it declines
 whatever is not plainly in order, and the ctypes path below it names the mistake."""
