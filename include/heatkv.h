@@ -345,8 +345,9 @@ typedef struct {
 #define HEATKV_PAGED_NO_PAGES 1        /* fewer free pages than the requests need */
 #define HEATKV_PAGED_BAD_LENGTH 2      /* a length is negative, keep > lens, or a request outgrows max_pages */
 #define HEATKV_PAGED_TOO_MANY_TOKENS 3 /* more new tokens than rows of the token tensors */
-#define HEATKV_PAGED_BAD_FREE_LIST 4   /* free_span does not fit the ring, or more pages come back than there are */
+#define HEATKV_PAGED_BAD_FREE_LIST 4   /* free_span does not fit the ring; heatkv_paged_assign: or more pages come back than there are */
 #define HEATKV_PAGED_BAD_PARENT 5      /* fork: a parent is not a row of the table */
+#define HEATKV_PAGED_BAD_HOLDERS 6     /* holders do not fit the table and the ring */
 
 /* One step of the page allocator.  Request b keeps the first keep[b] of its lens[b] tokens and gets new_tokens[b] more; it
  * then holds ceil((keep + new) / page_size) pages.  Pages that it lacks come from the ring of free pages, pages that it no
@@ -431,11 +432,12 @@ int heatkv_paged_read(const heatkv_paged_shape* shape, const int32_t* slots, int
  * cache with holders has its pages taken and given back by the three calls below, and not by heatkv_paged_assign.  They read and
  * write lens, free_ring, free_span and table as that does (lens_out and free_span_out may be lens and free_span); pages that no row
  * holds any more go behind the ring's tail, in ascending order, and are taken again by a later call at the earliest.  Holders that
- * do not fit the table give wrong tables, but touch nothing outside of the arrays.
+ * do not fit the table give wrong tables, but touch nothing outside of the arrays.  Where a count falls below 0, or more pages come
+ * back than the ring has room for, the status is HEATKV_PAGED_BAD_HOLDERS: the call has been made, pages that are free may be lost.
  * ws  device scratch of heatkv_paged_tables_workspace_bytes(shape) bytes, 16-byte aligned.  Calls that may run at the same time, graphs
  *     among them, need a workspace each
- * status as for heatkv_paged_assign: unless it is HEATKV_PAGED_OK the call has changed nothing but its lists (slots and moves are -1,
- * q_start zeros).  batch * max_pages is at most 2^30. */
+ * status as for heatkv_paged_assign: unless it is HEATKV_PAGED_OK, or HEATKV_PAGED_BAD_HOLDERS, the call has changed nothing but its
+ * lists (slots and moves are -1, q_start zeros).  batch * max_pages is at most 2^30. */
 size_t heatkv_paged_tables_workspace_bytes(const heatkv_paged_shape* shape);
 
 /* Row b of the table continues row parent[b], all of them at once, as the rows were before the call: it holds the same pages and has

@@ -35,6 +35,7 @@ from .binding import (  # noqa: F401
 )
 from .paged import (  # noqa: F401
     PAGED_BAD_FREE_LIST,
+    PAGED_BAD_HOLDERS,
     PAGED_BAD_LENGTH,
     PAGED_BAD_PARENT,
     PAGED_NO_PAGES,

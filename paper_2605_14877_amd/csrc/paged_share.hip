@@ -35,8 +35,8 @@ struct Group {
 };
 __device__ __forceinline__ Group group() { return {static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x)}; }
 
-// Words of TableArgs::state.
-enum State { HEAD, COUNT, TAKEN, STATUS, MOVES };
+// Words of TableArgs::state.  MISFIT: not 0 once a page was let go that nobody held, by its count.
+enum State { HEAD, COUNT, TAKEN, STATUS, MOVES, MISFIT };
 
 // Sum over the lanes up to this one: within rows of 16 lanes, then from row to row.
 __device__ __forceinline__ int inclusive_scan(int v) {
@@ -80,7 +80,9 @@ __device__ __forceinline__ long long most_tokens(const TableArgs& p) { return st
 // A row no longer holds `page`.
 __device__ __forceinline__ void let_go(const TableArgs& p, int page) {
   page = in_range(p, page);
-  if (atomicSub(&p.holders[page], 1) == 1) atomicOr(&p.gone[page >> 5], 1u << (page & 31));
+  const int held = atomicSub(&p.holders[page], 1);
+  if (held == 1) atomicOr(&p.gone[page >> 5], 1u << (page & 31));
+  if (held < 1) p.state[MISFIT] = 1;  // whoever finds it
 }
 // A row holds `page`, fresh from the ring.
 __device__ __forceinline__ void take(const TableArgs& p, int page) { p.holders[in_range(p, page)] = 1; }
@@ -101,7 +103,7 @@ __device__ __forceinline__ void give_back(const TableArgs& p, Group g) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int all_words = gone_words(p), each_group = (all_words + g.count - 1) / g.count;
   const int first = min(g.index * each_group, all_words), words = min(all_words - first, each_group), R = p.num_pages;
-  const int head = p.state[HEAD], count = p.state[COUNT], taken = p.state[TAKEN];
+  const int head = p.state[HEAD], count = p.state[COUNT], taken = p.state[TAKEN], misfit = p.state[MISFIT];
   int before = 0;
   for (int i = tid; i < first; i += LANES) before += __popc(p.gone[i]);
   const int each = (words + WAVES - 1) / WAVES, w0 = min(wave * each, words), w1 = min(w0 + each, words);
@@ -121,7 +123,7 @@ __device__ __forceinline__ void give_back(const TableArgs& p, Group g) {
     all += part[0][i];
   }
   at += all_before;
-  const int room = R - (count - taken);  // tables and holders that fit each other never have more to give
+  const int room = R - (count - taken);  // holders that fit the table and the ring never have more to give
   for (int k = w0; k < w1; k += 64) {
     const unsigned w = k + lane < w1 ? p.gone[first + k + lane] : 0;
     unsigned long long todo = __ballot(w != 0);
@@ -147,6 +149,7 @@ __device__ __forceinline__ void give_back(const TableArgs& p, Group g) {
     const int next = head + taken;
     p.span_out[0] = !made || next < R ? next : next - R;
     p.span_out[1] = made ? count - taken + min(all_before + all, room) : count;
+    if (made && (misfit || all_before + all > room)) p.status[0] = HEATKV_PAGED_BAD_HOLDERS;
   }
 }
 
@@ -215,6 +218,7 @@ __device__ __forceinline__ void fork_gains(const ForkArgs& f, Group g, int colum
       p.state[COUNT] = count;
       p.state[TAKEN] = 0;
       p.state[STATUS] = status;
+      p.state[MISFIT] = 0;
       p.status[0] = status;
     }
   }
@@ -288,6 +292,7 @@ __global__ __launch_bounds__(LANES) void paged_fork_small_kernel(ForkArgs f, int
     p.state[COUNT] = count;
     p.state[TAKEN] = 0;
     p.state[STATUS] = status;
+    p.state[MISFIT] = 0;
     p.status[0] = status;
   }
   __syncthreads();
@@ -330,9 +335,14 @@ __global__ __launch_bounds__(LANES) void paged_fork_small_kernel(ForkArgs f, int
       if (before[k] >= 0) held_by[k] = atomicSub(&p.holders[before[k]], 1);
       if (after[k] >= 0) p.table[b * p.max_pages + c] = after[k];
     });
+    int least = 1;
 #pragma unroll
     for (int k = 0; k < SMALL_EACH; ++k)
-      if (before[k] >= 0 && held_by[k] == 1) atomicOr(&p.gone[before[k] >> 5], 1u << (before[k] & 31));
+      if (before[k] >= 0) {
+        if (held_by[k] == 1) atomicOr(&p.gone[before[k] >> 5], 1u << (before[k] & 31));
+        least = min(least, held_by[k]);
+      }
+    if (least < 1) p.state[MISFIT] = 1;
   }
   __syncthreads();
   give_back(p, {0, 1});
@@ -443,6 +453,7 @@ __device__ __forceinline__ void assign_plan(const AssignSharedArgs& a, Group g) 
     p.state[COUNT] = count;
     p.state[TAKEN] = ok ? static_cast<int>(all[0]) : 0;
     p.state[STATUS] = status;
+    p.state[MISFIT] = 0;
     p.status[0] = status;
   }
 }
@@ -647,6 +658,7 @@ __device__ __forceinline__ void compact_plan(const CompactArgs& a) {
     p.state[COUNT] = count;
     p.state[TAKEN] = ok ? static_cast<int>(all[0]) : 0;
     p.state[STATUS] = status;
+    p.state[MISFIT] = 0;
     p.state[MOVES] = ok ? static_cast<int>(all[1]) : 0;
     p.status[0] = status;
   }
@@ -819,6 +831,7 @@ __global__ __launch_bounds__(LANES) void paged_compact_small_kernel(CompactArgs 
     p.state[COUNT] = count;
     p.state[TAKEN] = status ? 0 : static_cast<int>(all[0]);
     p.state[STATUS] = status;
+    p.state[MISFIT] = 0;
     p.status[0] = status;
   }
   __syncthreads();

@@ -13,7 +13,8 @@ import ctypes as C
 from . import binding
 from .binding import BF16, KV_FP4_E2M1, KV_FP8_E4M3, KV_NATIVE, _check, _DTYPES, lib
 
-PAGED_OK, PAGED_NO_PAGES, PAGED_BAD_LENGTH, PAGED_TOO_MANY_TOKENS, PAGED_BAD_FREE_LIST, PAGED_BAD_PARENT = 0, 1, 2, 3, 4, 5
+PAGED_OK, PAGED_NO_PAGES, PAGED_BAD_LENGTH, PAGED_TOO_MANY_TOKENS, PAGED_BAD_FREE_LIST = 0, 1, 2, 3, 4
+PAGED_BAD_PARENT, PAGED_BAD_HOLDERS = 5, 6
 
 
 class _CPagedShape(C.Structure):

@@ -257,6 +257,53 @@ def test_arrays_that_do_not_fit_touch_nothing_outside():
         assert torch.all(guard[37:] == 123456) and torch.all(table[:10] == 999) and torch.all(table[16:] == 999)
 
 
+@pytest.mark.parametrize("what", ["fork", "assign_shared", "compact"])
+@pytest.mark.parametrize("batch", [4, 1100])  # one workgroup, several launches
+def test_holders_that_do_not_fit_are_reported(batch, what):
+    def server():
+        s = Server(batch, 6 * batch, 4, 16, seed=batch)
+        s.assign([0] * batch, [20] * batch)
+        return s
+
+    def call(s, ends):
+        """Row 1 loses all of its tokens, or nothing changes."""
+        B, lens = s.batch, s.lens.tolist()
+        if what == "fork":
+            s.call("fork", _ints([-1 if b == 1 and ends else b for b in range(B)]))
+        elif what == "assign_shared":
+            copies = [torch.zeros(B, 16, dtype=torch.int32, device="cuda") for _ in range(2)]
+            s.call("assign_shared", _ints([0 if b == 1 and ends else n for b, n in enumerate(lens)]), _ints([0] * B),
+                   tail=(_ints([0] * (B + 1)), _ints([0] * 5), *copies))
+        else:
+            kept = torch.ones(B, 64, dtype=torch.bool, device="cuda")
+            kept[1] = not ends
+            s.call("compact", kept, tail=(_ints([0] * 5), _ints([0] * 5)))
+        return s.status.item(), s.lens.tolist(), s.span.tolist()
+
+    # a count below 0: the page is not given back
+    s = server()
+    head, count = s.span.tolist()
+    lost, other = s.table[1, :2].tolist()
+    s.holders[lost] = 0
+    lens = [0 if b == 1 else 20 for b in range(batch)]
+    assert call(s, True) == (hk.PAGED_BAD_HOLDERS, lens, [head, count + 1])
+    assert s.holders[lost].item() == -1 and s.ring[(head + count) % s.shape.num_pages].item() == other
+    s.holders[lost] = 0
+    assert call(s, False) == (hk.PAGED_OK, lens, [head, count + 1])  # nothing of it stays
+    # more pages than the ring has room for, by its span
+    s = server()
+    ring, full = s.ring.clone(), s.shape.num_pages - 1
+    s.span[1] = full
+    assert call(s, True) == (hk.PAGED_BAD_HOLDERS, lens, [head, full + 1])
+    first = s.ring[(head + full) % s.shape.num_pages].item()
+    ring[(head + full) % s.shape.num_pages] = first
+    assert first == min(s.table[1, :2].tolist()) and torch.equal(s.ring, ring)  # one of the two, and nothing else
+    # as many as there is room for
+    s = server()
+    s.span[1] = full - 1
+    assert call(s, True) == (hk.PAGED_OK, lens, [head, full + 1])
+
+
 def test_long_requests_and_many_of_them():
     # stretches and chunks of tokens with borders everywhere; more than one workgroup's words of the bitmap
     s = Server(3, 5000, 1700, 16, seed=7)
