@@ -312,8 +312,9 @@ int heatkv_rank_dispersion(const heatkv_shape* shape, const float* betas, int ru
  *                  rounded to nearest even and saturating at +-448 on append, read back exactly
  *   4-bit pages    (HEATKV_KV_FP4_E2M1, bf16 shapes) [num_pages][kv_heads][page_size * (d / 2 + d / 32)] bytes.  A row is d E2M1
  *                  codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) and one E8M0 byte x for each 32 channels: value = code * 2^(x - 127),
- *                  NaN if x = 255, and exact in bf16.  On append x - 127 is the least exponent in [-100, 125] with which no value of
- *                  the 32 is more than 7 times the power; rounded to nearest even, saturating at 6 times the power, infinities too.
+ *                  NaN if x = 255; exact in bf16, but for those from 2^128 on (x = 253 or 254, which append does not write), which are
+ *                  infinite.  On append x - 127 is the least exponent in [-100, 125] with which no value of the 32 is more than 7
+ *                  times the power; rounded to nearest even, saturating at 6 times the power, infinities too.
  *                  A NaN makes all 32 channels NaN.  16 rows lie together: 16 times d / 2 bytes of codes (channel 2 i in the low
  *                  half of byte i), then 16 times d / 32 scale bytes
  *   table          int32 [batch][max_pages]: page of a request's tokens [i * page_size, (i + 1) * page_size)

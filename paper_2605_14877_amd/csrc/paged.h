@@ -111,7 +111,7 @@ __device__ __forceinline__ int code_exponent(float amax) {
   return amax > 0.f ? max(__builtin_amdgcn_frexp_expf(amax) - (m <= 127.f / 128.f ? 7 : 6), -100) : -100;
 }
 
-// 8 E4M3 codes, or 8 E2M1 codes times `scale`, as bf16 (exact).
+// 8 E4M3 codes, or 8 E2M1 codes times `scale`, as bf16 (exact; products from 2^128 on are infinite).
 __device__ __forceinline__ bf16x8 codes_to_bf16(unsigned lo, unsigned hi) {
   union {
     bf16x2 h[4];

@@ -236,6 +236,32 @@ def test_rows_are_written_and_read_back(H, d, page, tokens, bounds):
                 assert torch.equal(b[p, h], codes) and s[p, h] == scale, (p, h)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [1, 60])  # the 16-row kernel, the 128-row kernel
+def test_every_code_under_every_scale_byte(d, new):
+    """Pages from elsewhere: numbers of the bf16 range are exact, its smallest ones among them, those beyond are infinite.  One key of
+    a request is seen by its first token: the output is its V."""
+    H, page, blocks = 8, 64, d // 32
+    B = 256 // (H * blocks)
+    codes = (torch.arange(d) % 16).expand(B, H, page, d).contiguous()
+    scales = torch.arange(256).view(B, H, 1, blocks).expand(B, H, page, blocks).contiguous()
+    v = sref.fp4_pack(codes, scales).cuda()
+    shape = hk.PagedShape(H, H, d, page, B, B, 1, "bf16", hk.KV_FP4_E2M1)
+    k = torch.zeros_like(v)
+    want = sref.fp4_decode(codes, scales)
+    want = torch.where(want.abs() >= 2.0 ** 128, torch.copysign(torch.tensor(math.inf, dtype=torch.float64), want), want)
+    assert torch.equal(want.to(torch.bfloat16).double().nan_to_num(7e300), want.nan_to_num(7e300))  # bf16 has them all
+    rows = [torch.zeros(B * page, H, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    hk.heatkv_paged_read(shape, _ints(list(range(B * page))), k, v, *rows)
+    assert _same(rows[1].view(B, page, H, d).transpose(1, 2), want)
+    out = torch.full((B * new, H, d), 5.0, dtype=torch.bfloat16, device="cuda")
+    ws = torch.zeros(max(hk.paged_attend_workspace_bytes(shape, B * new), 16), dtype=torch.uint8, device="cuda")
+    q = torch.randn(B * new, H, d, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+    hk.heatkv_paged_attend(shape, q, k, v, _ints([[b] for b in range(B)]), _ints([b * new for b in range(B + 1)]), _ints([new] * B), 0.1,
+                           out, ws)
+    assert _same(out.view(B, new, H, d)[:, 0], want[:, :, 0])
+
+
 @pytest.mark.parametrize("dtype,fmt", [("f32", "NATIVE"), ("bf16", "NATIVE"), ("bf16", "FP8_E4M3"), ("bf16", "FP4_E2M1")])
 @pytest.mark.parametrize("d,page,bounds", [(64, 16, False), (128, 32, False), (64, 32, True), (128, 256, True), (128, 16, True)])
 def test_rows_are_moved_as_they_are(dtype, fmt, d, page, bounds):
