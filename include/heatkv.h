@@ -474,7 +474,9 @@ int heatkv_paged_compact(const heatkv_paged_shape* shape, const uint8_t* kept, c
 
 /* Row move_to[i] of the cache becomes what row move_from[i] is, K and V of all kv heads, as stored.  Entries whose move_to is outside of
  * [0, num_pages * page_size) are skipped.  No row is moved to twice, and none that is moved to is one that is moved from.
- * bounds, bound_scales as for heatkv_paged_append, of the pages that rows are moved to. */
+ * bounds, bound_scales as for heatkv_paged_append, of the pages that rows are moved to.
+ * rows * kv_heads is at most 2^23 here as well, and the lists of the two calls above may be longer: such a list is moved in pieces, by
+ * a call for each, one after the other.  It may be cut anywhere, also between rows of one page: rows and bounds are the same. */
 int heatkv_paged_move(const heatkv_paged_shape* shape, const int32_t* move_from, const int32_t* move_to, int64_t rows,
                       void* k_pages, void* v_pages, int8_t* bounds, float* bound_scales, void* stream);
 

@@ -352,7 +352,8 @@ def heatkv_paged_compact(shape, kept, lens, holders, free_ring, free_span, table
 
 def heatkv_paged_move(shape, move_from, move_to, k_pages, v_pages, bounds=None, bound_scales=None, stream=None):
     """Rows move_to of the cache become what rows move_from are (int32 arrays of one shape, of one or two dimensions); with bounds
-    and bound_scales also the bounds of the pages that they touch."""
+    and bound_scales also the bounds of the pages that they touch.  A list of more than 2^23 / kv_heads rows is moved in pieces, by a
+    call for each: cut anywhere, rows and bounds are the same."""
     if _native("paged_move", shape, move_from, move_to, k_pages, v_pages, bounds, bound_scales, stream):
         return
     c, sh = _Call(shape), shape

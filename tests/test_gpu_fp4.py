@@ -323,6 +323,35 @@ def test_rows_of_other_formats_are_read_as_values(dtype, fmt):
     assert torch.equal(out[:, 0].cpu(), want) and torch.equal(out[:, 1].cpu(), want)
 
 
+@pytest.mark.parametrize("bounds", [False, True])
+def test_a_list_of_more_rows_than_a_call_takes_is_moved_in_pieces(bounds):
+    H, d, page, rows = 64, 64, 256, (1 << 23) // 64 + 300
+    half = ref.pages_of(rows, page)
+    shape = hk.PagedShape(H, H, d, page, 2 * half, 1, 1, "bf16", hk.KV_FP4_E2M1)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    first = [torch.randint(0, 252, shape.pages_shape, dtype=torch.uint8, device="cuda", generator=g) for _ in range(2)]
+    to = _ints(list(range(half * page, half * page + rows)))
+    frm = torch.randperm(rows, device="cuda", generator=g).int()
+
+    def moved(cuts):
+        k, v = (x.clone() for x in first)
+        b, s = (torch.full(n, 77, dtype=t, device="cuda") for n, t in (((2 * half, H, 2, d), torch.int8), ((2 * half, H), torch.float32)))
+        for i, j in zip([0, *cuts], [*cuts, rows]):
+            hk.heatkv_paged_move(shape, frm[i:j], to[i:j], k, v, *((b, s) if bounds else ()))
+        return k, v, b, s
+
+    with pytest.raises(hk.HeatKVError, match="2\\^23"):
+        moved([])
+    want = moved([half // 2 * page])  # cut between two pages
+    for cuts in ([300], [1 << 17], [half // 2 * page - 131, half // 2 * page - 126, half // 2 * page + 7]):  # within; a few rows alone
+        assert all(torch.equal(x, y) for x, y in zip(moved(cuts), want))
+    ids = torch.tensor([0, 1, 255, 256, half // 2 * page - 1, rows - 301, rows - 1], device="cuda")
+    got, old = ([torch.zeros(len(ids), H, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)] for _ in range(2))
+    hk.heatkv_paged_read(shape, to[ids], *want[:2], *got)
+    hk.heatkv_paged_read(shape, frm[ids], *first, *old)
+    assert all(torch.equal(x, y) for x, y in zip(got, old))
+
+
 def test_addresses_beyond_32_bits():
     # 4-bit pages of more than 4 GiB each; the request's tokens on the last of them
     H, d, page = 8, 128, 256
