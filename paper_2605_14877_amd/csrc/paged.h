@@ -196,7 +196,7 @@ using PagedParts = paged::Parts;
 constexpr size_t PAGED_SELECT_LDS = paged::SELECT_LDS;
 hipError_t launch_paged_select(const PagedSelectParams& p, int dtype, int d, hipStream_t stream);
 hipError_t launch_paged_attend_bf16(const PagedAttendParams& p, int d, int kv_format, hipStream_t stream);
-// few: of the requests with few rows, which it takes along.
+// few: of the requests with few rows, in the same launch or one of their own (place_of_few()).
 hipError_t launch_paged_attend_long(const PagedAttendParams& p, const PagedAttendParams& few, int d, int kv_format, hipStream_t stream);
 hipError_t launch_paged_attend_f32(const PagedAttendParams& p, int d, hipStream_t stream);
 // few, many: of the two attention launches, grid: join_workgroups(), 0 where there is nothing to join.

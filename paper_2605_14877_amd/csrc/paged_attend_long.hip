@@ -1,7 +1,7 @@
 // Attention of new tokens over the paged cache, bf16, for requests with many query rows (chunks of prompts, whole scales):
 // the tile loop of attend.hip over keys that lie on pages.
 //
-// The grid has the workgroups of the 16-row kernel as well (FEW_FIRST).
+// The grid has the workgroups of the 16-row kernel as well (place_of_few()).
 //
 // Workgroup = 4 wavefronts x 32 query rows (row = token x query of the kv head's group), two workgroups per compute unit (4-bit rows at
 // d = 64: three).
@@ -132,8 +132,8 @@ __device__ __forceinline__ int build_union(const AttendParams& a, const Tile& t,
 // 4-bit rows at d = 64 take 176 registers by themselves; held to 168, three workgroups share a compute unit instead of two: whole scales of 8
 // requests 59 us instead of 68, 3000 new tokens over 4096 keys 178 instead of 206, 16 x 300 228 instead of 252; where two to a unit come
 // out even, 230 instead of 222 (2 x 2048); all with the 16-row kernel in a launch of its own.
-// few: the 16-row kernel's launch (paged_attend_few.h), whose workgroups are the grid's from few_at on, 0 or behind this kernel's own.  As a
-// launch of its own it took 4 to 8 us where it had next to nothing to do, and what it did have did not run beside this.
+// few: the 16-row kernel's launch (paged_attend_few.h), whose workgroups are the grid's from few_at on, 0 or behind this kernel's own, or
+// none.  As a launch of its own it took 4 to 8 us where it had next to nothing to do, and what it did have did not run beside this.
 template <int D, Format F, bool CHOSEN>
 __global__ __launch_bounds__(256, D == 64 && F == E2M1 ? 3 : 2) void paged_attend_long_kernel(AttendParams p, AttendParams few, int few_at) {
   int w = blockIdx.x;
@@ -745,16 +745,20 @@ __global__ __launch_bounds__(256, D == 64 && F == E2M1 ? 3 : 2) void paged_atten
 }
 
 template <int D, Format F, bool CHOSEN>
-hipError_t launch(const AttendParams& p, const AttendParams& few, hipStream_t stream) {
+hipError_t launch(const AttendParams& p, const AttendParams& few, int kv_format, hipStream_t stream) {
   static_assert(FEW_WAVES * stage_bytes(D) + FEW_SHARED <= 4 * BN * 2 * D + kUnionAt, "the workgroups of few rows have room");
   // With chosen pages as well: walk_lds_bytes() is for the union of no more tokens, of which each page takes 8 bytes instead of 24.
   const size_t lds = 4 * BN * 2 * D + kUnionAt + (CHOSEN ? many_union_bytes(p.c.G, p.c.max_pages, p.top) : 0);
   static std::atomic<unsigned long long> allowed{0};
   if (lds > 64 * 1024)
     if (hipError_t e = allow_lds(reinterpret_cast<const void*>(&paged_attend_long_kernel<D, F, CHOSEN>), MANY_LDS, allowed)) return e;
-  hipLaunchKernelGGL((paged_attend_long_kernel<D, F, CHOSEN>), dim3(p.parts.grid + few.parts.grid), dim3(256), lds, stream, p, few,
-                     p.c.batch > FEW_FIRST ? 0 : p.parts.grid);
-  return hipGetLastError();
+  const FewRows place = place_of_few(p.c.batch, CHOSEN, lds, row_bytes<bf16_t, F>(D));
+  AttendParams along = few;
+  if (place == FewRows::APART) along.parts.grid = 0;
+  hipLaunchKernelGGL((paged_attend_long_kernel<D, F, CHOSEN>), dim3(p.parts.grid + along.parts.grid), dim3(256), lds, stream, p, along,
+                     place == FewRows::IN_FRONT ? 0 : p.parts.grid);
+  if (hipError_t e = hipGetLastError()) return e;
+  return place == FewRows::APART ? launch_paged_attend_bf16(few, D, kv_format, stream) : hipSuccess;
 }
 
 }  // namespace
@@ -764,9 +768,9 @@ hipError_t launch_paged_attend_long(const PagedAttendParams& p, const PagedAtten
   auto run = [&](auto d_tag, auto chosen) {
     constexpr int D = decltype(d_tag)::value;
     constexpr bool CHOSEN = decltype(chosen)::value;
-    return kv_format == HEATKV_KV_FP4_E2M1   ? launch<D, E2M1, CHOSEN>(p, few, stream)
-           : kv_format == HEATKV_KV_FP8_E4M3 ? launch<D, E4M3, CHOSEN>(p, few, stream)
-                                             : launch<D, NATIVE, CHOSEN>(p, few, stream);
+    return kv_format == HEATKV_KV_FP4_E2M1   ? launch<D, E2M1, CHOSEN>(p, few, kv_format, stream)
+           : kv_format == HEATKV_KV_FP8_E4M3 ? launch<D, E4M3, CHOSEN>(p, few, kv_format, stream)
+                                             : launch<D, NATIVE, CHOSEN>(p, few, kv_format, stream);
   };
   using D128 = std::integral_constant<int, 128>;
   using D64 = std::integral_constant<int, 64>;

@@ -59,18 +59,34 @@ constexpr int MANY_ROWS = 16, MANY_CHOSEN_ROWS = 64;
 constexpr int FEW_TOKENS = 40, FEW_TOKENS_LONG = 16, LONG_CACHE = 16384;
 
 // Where both kernels have work, one launch has the workgroups of both.  Those of many rows come first, and what few requests of few rows there
-// may be falls into the gaps at their end; from more requests than this on those of few rows come first, which read memory while the
+// may be falls into the gaps at their end; over all pages, from more requests than this on, those of few rows come first, which read memory while the
 // others compute.  Many rows first, few rows first, two launches, bf16, d = 128: 8 requests that decode over 1000 keys and two prompts of
 // 300 tokens 27, 31, 34 us, 32 and two 39, 42, 48, 48 and two 52, 52, 59; 32 requests over 9000 keys and 1000 new tokens over 2000: 283, 260,
 // 285, 48 and those 382, 356, 386; whole scales of 8 requests, 4-bit rows, d = 64: 51, 56, 59.
 constexpr int FEW_FIRST = 32;
 
-// LDS of the 128-row kernel for the union of its tokens' chosen pages: a bit and a count for each word of the request's pages,
+// LDS of a compute unit, and of the 128-row kernel for the union of its tokens' chosen pages: a bit and a count for each word of the request's pages,
 // 24 bytes for each page that may be in it.  Larger unions are left to the 16-row kernel, whose tiles have fewer tokens.
 constexpr size_t MANY_LDS = 160 * 1024, MANY_UNION_BYTES = 92 * 1024;
 inline size_t many_union_bytes(int group, int64_t max_pages, int64_t top) {
   const int64_t capacity = std::min<int64_t>(max_pages, std::min(128, 127 / group + 2) * top);
   return static_cast<size_t>(16 + (max_pages + 31) / 32 * 8 + capacity * 24);
+}
+
+// With chosen pages those of many rows come first: they take longer then, and the others read little.  64 requests that decode and two
+// chunks of 1000 tokens, 32 pages of 64 keys for each token, many first, few first, two launches: bf16, d = 128 and 64: 328, 340, 356 us
+// and 204, 270, 247; 8 bits: 310, 339, 348 and 225, 240, 247; 4 bits: 269, 286, 292 and 181, 199, 209.  Where the tokens of a chunk all
+// choose the same pages few first is faster at d = 128: 64 requests and 500 tokens, bf16 91 and 85, 4 bits 66 and 62 (d = 64: 53 and 57, 48
+// and 45).
+// Where the union's LDS leaves room for one workgroup on a compute unit, few rows in the same launch would have but one as well: they
+// get a launch of their own.  64 requests of 200000 keys and a chunk of 500 tokens, 80 pages each: 4 bits, d = 128 and 64: 172, 171,
+// 146 us and 142, 142, 122; 8 bits: 200, 196, 191 and 148, 147, 130; bf16, d = 64: 160, 155, 154.  Rows of 256 bytes are read as fast by one
+// workgroup to a unit (243, 228, 241).  200 requests of 64000 keys, four chunks, 26 pages: 4 bits, d = 128: 289, 289, 256; bf16: 347, 336, 343.
+enum class FewRows { BEHIND, IN_FRONT, APART };
+inline FewRows place_of_few(int batch, bool chosen, size_t lds, int row_bytes) {
+  if (!chosen) return batch > FEW_FIRST ? FewRows::IN_FRONT : FewRows::BEHIND;
+  if (2 * lds <= MANY_LDS) return FewRows::BEHIND;
+  return batch > FEW_FIRST && row_bytes >= 256 ? FewRows::IN_FRONT : FewRows::APART;
 }
 
 // `top`: pages that a token reads at most, 0: all of them.

@@ -463,6 +463,23 @@ def test_few_and_many_rows_in_one_call(dtype, d, group, batch):
     p.check(True, p.run(True, _ints(sel)), sel)
 
 
+@pytest.mark.parametrize("dtype", ["fp4", "fp8", "bf16"])
+@pytest.mark.parametrize("d,max_pages,top", [(128, 1000, 8), (64, 3000, 24)])
+@pytest.mark.parametrize("batch", [5, 40])
+def test_few_and_many_rows_beside_a_large_union(dtype, d, max_pages, top, batch):
+    # the union of a tile's pages leaves room for one workgroup on a compute unit: two launches, or one with few rows first
+    r = random.Random(batch)
+    lens = [r.choice((1, 30, 300, 1200)) for _ in range(batch)]
+    new = [min(n, r.choice((0, 1, 1, 1, 5, 20))) for n in lens]
+    lens[-1], new[-1] = 500, 170
+    case = (2, 2, d, 16, lens, new)
+    p = Fp4Problem(*case, seed=batch, max_pages=max_pages) if dtype == "fp4" else Problem(dtype, *case, seed=batch, max_pages=max_pages)
+    sel = [[[r.randrange(0, 60) for _ in range(top)] for _ in range(p.H)] for _ in range(p.tokens)]
+    first, again = p.run(True, _ints(sel)), p.run(True, _ints(sel))
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    p.check(True, first, sel)
+
+
 @pytest.mark.parametrize("dtype", ["fp4", "fp8", "bf16", "f32"])
 @pytest.mark.parametrize("batch,heads,new", [(1, 8, 240), (3, 8, 256), (10, 8, 240), (64, 8, 1), (64, 21, 1), (63, 20, 2), (64, 1, 17), (65, 8, 1),
                                              (8, 64, 30)])

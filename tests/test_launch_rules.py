@@ -60,3 +60,14 @@ def test_wavefronts_that_only_copy(rules, d, attend, copies, tiles, copiers):
 def test_two_key_streams_at_head_dimension_64(rules, attend, update, tiles, two):
     assert rules.two_key_streams(64, attend, update, tiles) == two
     assert rules.two_key_streams(128, attend, update, tiles)
+
+
+@pytest.mark.parametrize("batch,chosen,kib,row,place", [
+    # behind, in front, a launch of their own; over all pages by the number of requests
+    (32, False, 66, 256, 0), (33, False, 66, 256, 1), (2, False, 34, 36, 0), (300, False, 34, 36, 1),
+    # chosen pages: with room for two workgroups on a compute unit; for one
+    (64, True, 70, 256, 0), (64, True, 80, 68, 0), (2, True, 80, 128, 0), (300, True, 40, 36, 0),
+    (64, True, 81, 68, 2), (64, True, 81, 128, 2), (200, True, 92, 36, 2), (8, True, 90, 256, 2), (32, True, 81, 256, 2), (33, True, 81, 256, 1),
+])
+def test_where_requests_of_few_rows_go(rules, batch, chosen, kib, row, place):
+    assert rules.place_of_few(batch, int(chosen), ctypes.c_ulonglong(kib * 1024), row) == place
