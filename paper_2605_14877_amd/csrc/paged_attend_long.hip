@@ -14,7 +14,7 @@
 //
 // Bound: the matrix pipe, and the vector work of the softmax next to it.  2 x 2048 new tokens over 4096 keys before them, 32
 // heads over 8, d = 128: 344 GFLOP in 335 us, 1.0 PFLOP/s (385 us where the clock falls under the load of many in a row); 8-bit
-// rows 12 % more, for their way through registers, 4-bit rows no more.  Whole scales of 8 requests, 16 heads, d = 64, 11520 tile steps:
+// rows 3 % more, for their way through registers, 4-bit rows no more.  Whole scales of 8 requests, 16 heads, d = 64, 11520 tile steps:
 // 44 us, twice the softmax for a product and 2 pieces to a workgroup.  Chosen pages, 1024 tokens, 32 of 272 pages each, 127 in
 // the union of 32 tokens: 96 us, as much as the union's products (57 GFLOP) at 0.6 PFLOP/s.
 #include <hip/hip_runtime.h>
@@ -271,6 +271,9 @@ __global__ __launch_bounds__(256, D == 64 && F == E2M1 ? 3 : 2) void paged_atten
   };
   // 8-bit rows: load i of a lane is 16 codes of one row, converted on the way into the stage.
   constexpr int LPR = D / 16;  // lanes per row
+  // Row and place within a granule, the same for all of a lane's loads.  As an address for each load they went to scratch, and their reload
+  // waited for the load before it: 2 x 2048 tokens over 4096 keys 377 us instead of 354, 3000 tokens 347 instead of 299.
+  const int code_row = tid / LPR & 15, code_at = code_row * SRC + tid % LPR * 16;
   auto load_codes = [&](const char* pages, const TileRows& at, int it, int i) {
     const int r = (tid + 256 * i) / LPR;  // a wavefront's 64 / LPR rows are of one granule
     // By arithmetic on all four places: a choice of one in memory would keep them there.
@@ -279,10 +282,11 @@ __global__ __launch_bounds__(256, D == 64 && F == E2M1 ? 3 : 2) void paged_atten
       if constexpr (D == 64) return pick(wave >> 1, pick(wave & 1, x3, x2), pick(wave & 1, x1, x0));
       return i ? pick(wave >> 1, x3, x2) : pick(wave >> 1, x1, x0);
     };
+    [[maybe_unused]] const int here = mine(at.pos);  // for any `it`: no branch around it within the step
     const int from = mine(at.granule);
-    const int pos = !CHOSEN ? it * BN + (r & ~15) : it >= end ? 1 << 30 : mine(at.pos);
+    const int pos = !CHOSEN ? it * BN + (r & ~15) : it >= end ? 1 << 30 : here;
     uint4 raw = make_uint4(0, 0, 0, 0);
-    if (pos + (r & 15) < stop) raw = ldg16(pages + (static_cast<long long>(from) * 16 + (r & 15)) * SRC + (tid % LPR) * 16);
+    if (pos + code_row < stop) raw = ldg16(pages + static_cast<long long>(from) * (16 * SRC) + code_at);
     return raw;
   };
   auto store_codes = [&](char* stage, const uint4& raw, int i, auto is_v) {

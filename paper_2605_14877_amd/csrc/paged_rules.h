@@ -74,14 +74,14 @@ inline size_t many_union_bytes(int group, int64_t max_pages, int64_t top) {
 }
 
 // With chosen pages those of many rows come first: they take longer then, and the others read little.  64 requests that decode and two
-// chunks of 1000 tokens, 32 pages of 64 keys for each token, many first, few first, two launches: bf16, d = 128 and 64: 328, 340, 356 us
-// and 204, 270, 247; 8 bits: 310, 339, 348 and 225, 240, 247; 4 bits: 269, 286, 292 and 181, 199, 209.  Where the tokens of a chunk all
+// chunks of 1000 tokens, 32 pages of 64 keys for each token, many first, few first, two launches: bf16, d = 128 and 64: 332, 344, 356 us
+// and 205, 271, 249; 8 bits: 289, 320, 329 and 219, 235, 242; 4 bits: 265, 280, 286 and 182, 221, 209.  Where the tokens of a chunk all
 // choose the same pages few first is faster at d = 128: 64 requests and 500 tokens, bf16 91 and 85, 4 bits 66 and 62 (d = 64: 53 and 57, 48
 // and 45).
 // Where the union's LDS leaves room for one workgroup on a compute unit, few rows in the same launch would have but one as well: they
-// get a launch of their own.  64 requests of 200000 keys and a chunk of 500 tokens, 80 pages each: 4 bits, d = 128 and 64: 172, 171,
-// 146 us and 142, 142, 122; 8 bits: 200, 196, 191 and 148, 147, 130; bf16, d = 64: 160, 155, 154.  Rows of 256 bytes are read as fast by one
-// workgroup to a unit (243, 228, 241).  200 requests of 64000 keys, four chunks, 26 pages: 4 bits, d = 128: 289, 289, 256; bf16: 347, 336, 343.
+// get a launch of their own.  64 requests of 200000 keys and a chunk of 500 tokens, 80 pages each: 4 bits, d = 128 and 64: 172, 172,
+// 146 us and 142, 142, 122; 8 bits: 188, 184, 180 and 145, 145, 128; bf16, d = 64: 162, 156, 156.  Rows of 256 bytes are read as fast by one
+// workgroup to a unit (242, 228, 241).  200 requests of 64000 keys, four chunks, 26 pages: 4 bits, d = 128: 287, 287, 255; bf16: 357, 346, 352.
 enum class FewRows { BEHIND, IN_FRONT, APART };
 inline FewRows place_of_few(int batch, bool chosen, size_t lds, int row_bytes) {
   if (!chosen) return batch > FEW_FIRST ? FewRows::IN_FRONT : FewRows::BEHIND;

@@ -153,3 +153,50 @@ def test_fp32_kernels_reduce_over_lane_groups_in_registers():
             assert bodies, src
             for name, body in bodies:
                 assert "v_permlane16_swap_b32" in body and "ds_bpermute" not in body, name
+
+
+def tile_loops(body):
+    """Loops of a kernel's assembly, blocks by the innermost one: header -> [matrix instructions, scratch accesses]."""
+    loops, inside, block = {}, None, None
+    for line in body.split("\n"):
+        code, _, note = line.partition(";")
+        label = re.match(r"\.L(BB\d+_\d+):", code)
+        if label or note.startswith(" %bb."):  # a block begins; the loop that it is in stands beside it
+            block = label.group(1) if label else None
+            header = re.search(r"in Loop: Header=(BB\d+_\d+)", note)
+            inside = header.group(1) if header else None
+        if block and re.search(r"=>\s*This (?:Inner )?Loop Header", note):  # beside it, or below the loops around it
+            inside = block
+        if inside:
+            count = loops.setdefault(inside, [0, 0])
+            count[0] += code.lstrip().startswith("v_mfma")
+            count[1] += code.lstrip().startswith("scratch_")
+    return loops
+
+
+def test_tile_loops_of_the_paged_128_row_kernels_touch_no_scratch():
+    # A reload waits for every load that is under way before it, the next tile's among them.
+    planted = """
+.LBB0_1:                                ; =>This Inner Loop Header: Depth=1
+    v_mfma_f32_32x32x16_bf16 v[0:15], v[16:19], v[20:23], 0
+; %bb.2:                                ;   in Loop: Header=BB0_1 Depth=1
+    scratch_load_dwordx2 v[88:89], off, off ; 8-byte Folded Reload
+.LBB0_3:                                ;   in Loop: Header=BB0_1 Depth=1
+    s_cbranch_scc1 .LBB0_1
+; %bb.4:
+    scratch_load_dword v1, off, off
+"""
+    assert tile_loops(planted) == {"BB0_1": [1, 1]}
+    with tempfile.TemporaryDirectory() as tmp:
+        out = os.path.join(tmp, "long.s")
+        subprocess.run(["hipcc", *hb.HIP_FLAGS, "-S", "--cuda-device-only", os.path.join(hb.CSRC, "paged_attend_long.hip"), "-o", out],
+                       check=True, capture_output=True)
+        with open(out) as f:
+            bodies = re.findall(r"^(_ZN\S*paged_attend_long_kernel\S*):[^\n]*\n(.*?)^\.Lfunc_end", f.read(), re.M | re.S)
+        assert len(bodies) == 12
+        for name, body in bodies:
+            loops = [x for x in tile_loops(body).values() if x[0] >= 32]
+            assert loops, name
+            # 4-bit rows, d = 64, chosen pages, held to 168 registers: a row's last key comes back where a tile is masked
+            if "Li64ELNS_5paged6FormatE2ELb1E" not in name:
+                assert all(scratch == 0 for _, scratch in loops), (name, loops)
