@@ -415,6 +415,97 @@ def test_two_caches_on_two_streams():
         s.check(s.ref.fork(p.tolist()))
 
 
+# The same where calls are several launches, which pass what they have found through the workspace: all of them by the number of rows, or
+# of pages; fork and compact by the width of the table.
+LAUNCHES = [(1100, 9000, 12, 16), (5, 131200, 30, 16), (64, 9000, 193, 16)]
+
+
+@pytest.mark.parametrize("size", [(1100, 9000, 6, 16), (300, 6000, 60, 16), (5, 131200, 70, 16)], ids=str)
+def test_random_steps_of_several_launches_into_arrays_of_their_own(size):
+    test_random_steps(size, True)
+
+
+class Steps:
+    """Steps of a server, each a fork, an allocator's step and a compaction, without a look at any result."""
+
+    def __init__(self, size, seed, max_moves):
+        self.s = s = Server(*size, seed=seed)
+        self.width, self.max_moves = s.shape.max_pages * s.page, max_moves
+        s.assign([0] * s.batch, [s.rng.randint(1, 90) for _ in range(s.batch)])
+        B = s.batch
+        self.parent, self.keep, self.new = _ints(list(range(B))), s.lens.clone(), _ints([0] * B)
+        self.q_start, self.slots = _ints([0] * (B + 1)), _ints([0] * (4 * B + 9))
+        self.copies = [torch.zeros(B, s.page, dtype=torch.int32, device="cuda") for _ in range(2)]
+        self.kept = torch.ones(B, self.width, dtype=torch.bool, device="cuda")
+        self.moves = [_ints([0] * max_moves) for _ in range(2)]
+        self.ws = [torch.full_like(s.ws, 255) for _ in range(3)]
+        self.status = [_ints([9]) for _ in range(3)]
+
+    def draw(self):
+        """Arguments of a step into the arrays; what it comes to."""
+        s = self.s
+        parents = s.parents()
+        lens = [s.ref.lens[p] if p >= 0 else 0 for p in parents]
+        keeps = [n - min(n, s.rng.randint(0, 3)) for n in lens]
+        news = [min(self.width - k, s.rng.randint(0, 4)) for k in keeps]
+        marks = torch.rand(s.batch, self.width, generator=torch.Generator().manual_seed(sum(lens))) < 0.9
+        for x, y in ((self.parent, _ints(parents)), (self.keep, _ints(keeps)), (self.new, _ints(news)), (self.kept, marks)):
+            x.copy_(y)
+        return [s.ref.fork(parents), *s.ref.assign(keeps, news, self.slots.numel()), *s.ref.compact(marks.tolist(), self.max_moves)]
+
+    def run(self):
+        s = self.s
+        t = (s.lens, s.holders, s.ring, s.span, s.table)
+        hk.heatkv_paged_fork(s.shape, self.parent, *t, self.status[0], self.ws[0][:-64])
+        hk.heatkv_paged_assign_shared(s.shape, self.keep, self.new, *t, self.q_start, self.slots, *self.copies, self.status[1], self.ws[1][:-64])
+        hk.heatkv_paged_compact(s.shape, self.kept, *t, *self.moves, self.status[2], self.ws[2][:-64])
+
+    def check(self, want):
+        assert [x.item() for x in self.status] == [want[0], want[1], want[5]]
+        assert self.q_start.tolist() == want[2] and self.slots.tolist() == want[3]
+        assert [[tuple(x) for x in row] for row in torch.stack(self.copies, -1).tolist()] == want[4]
+        assert list(zip(*(m.tolist() for m in self.moves))) == want[6]
+        assert all(torch.all(w[-64:] == 255) for w in self.ws)
+        self.s.status.fill_(want[5])
+        self.s.check(want[5])
+
+
+@pytest.mark.parametrize("size", LAUNCHES, ids=str)
+def test_captured_steps_of_several_launches_are_replayed(size):
+    p = Steps(size, 31, max_moves=100 * size[0])
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    state = [x.clone() for x in (p.s.lens, p.s.holders, p.s.ring, p.s.span, p.s.table)]
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        p.run()
+    for x, y in zip((p.s.lens, p.s.holders, p.s.ring, p.s.span, p.s.table), state):
+        assert torch.equal(x, y)  # nothing has run
+    for i in range(6):
+        want = p.draw()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert want[0] == want[1] == want[5] == 0
+        p.check(want)
+        if i % 2:  # eager steps of the same cache and workspaces between the replays
+            want = p.draw()
+            p.run()
+            p.check(want)
+
+
+@pytest.mark.parametrize("size", LAUNCHES, ids=str)
+def test_steps_of_several_launches_on_two_streams(size):
+    pairs = [(Steps(size, 41 + i, max_moves=100 * size[0]), torch.cuda.Stream()) for i in range(2)]
+    for _ in range(3):
+        wants = [p.draw() for p, _ in pairs]
+        torch.cuda.synchronize()
+        for p, stream in pairs:
+            with torch.cuda.stream(stream):
+                p.run()
+        torch.cuda.synchronize()
+        for (p, _), want in zip(pairs, wants):
+            p.check(want)
+
+
 # ---- with the rows of the cache -----------------------------------------------------------------------------------------
 
 KINDS = [("bf16", "NATIVE", 64, 16), ("bf16", "FP8_E4M3", 128, 32), ("bf16", "FP4_E2M1", 128, 16), ("f32", "NATIVE", 128, 16),
