@@ -38,8 +38,8 @@ struct FewShared {
 };
 constexpr int FEW_SHARED = (sizeof(FewShared) + 15) / 16 * 16;
 
-// Workgroup w of the launch; WHICH: place of `p` among the kernel's arguments.  `few_stages`: LDS, FEW_WAVES * stage_bytes(D) bytes; `few_walk`:
-// walk_lds_bytes(p) bytes with chosen pages.
+// Workgroup w of the launch; WHICH: place of `p` among the kernel's arguments.  `few_stages`: LDS, FEW_WAVES * stage_bytes(D) bytes;
+// `few_walk`: walk_lds_bytes(p) bytes with chosen pages.
 template <int D, Format F, bool CHOSEN, int WHICH>
 __device__ __forceinline__ void attend_few(const AttendParams& p, int w, FewShared& s, char* few_stages, char* few_walk) {
   constexpr int NK = D / 32, NV = D / 16;            // MFMA steps of a score, accumulator blocks of 16 columns

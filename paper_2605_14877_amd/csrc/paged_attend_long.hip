@@ -12,11 +12,11 @@
 // Chosen pages: the walk is over the union of the pages that the workgroup's tokens have chosen (up to 128 of them, neighbours in
 // the request, which choose alike), with a word of 32 tokens for each wavefront and page.
 //
-// Bound: the matrix pipe, and the vector work of the softmax next to it.  2 x 2048 new tokens over 4096 keys before them, 32
-// heads over 8, d = 128: 344 GFLOP in 335 us, 1.0 PFLOP/s (385 us where the clock falls under the load of many in a row); 8-bit
-// rows 3 % more, for their way through registers, 4-bit rows no more.  Whole scales of 8 requests, 16 heads, d = 64, 11520 tile steps:
-// 44 us, twice the softmax for a product and 2 pieces to a workgroup.  Chosen pages, 1024 tokens, 32 of 272 pages each, 127 in
-// the union of 32 tokens: 96 us, as much as the union's products (57 GFLOP) at 0.6 PFLOP/s.
+// Bound: the matrix pipe, and the vector work of the softmax next to it.  2 x 2048 new tokens over 4096 keys before them, 32 heads over 8,
+// d = 128: 344 GFLOP in 335 us, 1.0 PFLOP/s (385 us where the clock falls under the load of many in a row); 8-bit rows 3 % more, for their
+// way through registers, 4-bit rows no more.  Whole scales of 8 requests, 16 heads, d = 64, 11520 tile steps: 46 us, no pipe full (4-bit
+// rows: vector work 21 %, matrix pipe 18 %, waiting 37 %, for issue 30 %), 368 tiles cut for 768 places.  Chosen pages, 1024 tokens, 32 of
+// 272 pages each, 127 in the union of 32 tokens: 96 us, as much as the union's products (57 GFLOP) at 0.6 PFLOP/s.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

@@ -58,15 +58,15 @@ constexpr int MANY_ROWS = 16, MANY_CHOSEN_ROWS = 64;
 // One request, 24 tokens at 1000, 8000 and 32000 keys: 16, 29 and 80 us by the 16-row kernel alone, 19, 26 and 48 with both.
 constexpr int FEW_TOKENS = 40, FEW_TOKENS_LONG = 16, LONG_CACHE = 16384;
 
-// Where both kernels have work, one launch has the workgroups of both.  Those of many rows come first, and what few requests of few rows there
-// may be falls into the gaps at their end; over all pages, from more requests than this on, those of few rows come first, which read memory while the
-// others compute.  Many rows first, few rows first, two launches, bf16, d = 128: 8 requests that decode over 1000 keys and two prompts of
-// 300 tokens 27, 31, 34 us, 32 and two 39, 42, 48, 48 and two 52, 52, 59; 32 requests over 9000 keys and 1000 new tokens over 2000: 283, 260,
-// 285, 48 and those 382, 356, 386; whole scales of 8 requests, 4-bit rows, d = 64: 51, 56, 59.
+// Where both kernels have work, one launch has the workgroups of both.  Those of many rows come first, and what few requests of few rows
+// there may be falls into the gaps at their end; over all pages, from more requests than this on, those of few rows come first, which read
+// memory while the others compute.  Many rows first, few rows first, two launches, bf16, d = 128: 8 requests that decode over 1000 keys and
+// two prompts of 300 tokens 27, 31, 34 us, 32 and two 39, 42, 48, 48 and two 52, 52, 59; 32 requests over 9000 keys and 1000 new tokens
+// over 2000: 283, 260, 285, 48 and those 382, 356, 386; whole scales of 8 requests, 4-bit rows, d = 64: 51, 56, 59.
 constexpr int FEW_FIRST = 32;
 
-// LDS of a compute unit, and of the 128-row kernel for the union of its tokens' chosen pages: a bit and a count for each word of the request's pages,
-// 24 bytes for each page that may be in it.  Larger unions are left to the 16-row kernel, whose tiles have fewer tokens.
+// LDS of a compute unit, and of the 128-row kernel for the union of its tokens' chosen pages: a bit and a count for each word of the
+// request's pages, 24 bytes for each page that may be in it.  Larger unions are left to the 16-row kernel, whose tiles have fewer tokens.
 constexpr size_t MANY_LDS = 160 * 1024, MANY_UNION_BYTES = 92 * 1024;
 inline size_t many_union_bytes(int group, int64_t max_pages, int64_t top) {
   const int64_t capacity = std::min<int64_t>(max_pages, std::min(128, 127 / group + 2) * top);
@@ -78,10 +78,11 @@ inline size_t many_union_bytes(int group, int64_t max_pages, int64_t top) {
 // and 205, 271, 249; 8 bits: 289, 320, 329 and 219, 235, 242; 4 bits: 265, 280, 286 and 182, 221, 209.  Where the tokens of a chunk all
 // choose the same pages few first is faster at d = 128: 64 requests and 500 tokens, bf16 91 and 85, 4 bits 66 and 62 (d = 64: 53 and 57, 48
 // and 45).
-// Where the union's LDS leaves room for one workgroup on a compute unit, few rows in the same launch would have but one as well: they
-// get a launch of their own.  64 requests of 200000 keys and a chunk of 500 tokens, 80 pages each: 4 bits, d = 128 and 64: 172, 172,
-// 146 us and 142, 142, 122; 8 bits: 188, 184, 180 and 145, 145, 128; bf16, d = 64: 162, 156, 156.  Rows of 256 bytes are read as fast by one
-// workgroup to a unit (242, 228, 241).  200 requests of 64000 keys, four chunks, 26 pages: 4 bits, d = 128: 287, 287, 255; bf16: 357, 346, 352.
+// Where the union's LDS leaves room for one workgroup on a compute unit, few rows in the same launch would have but one as well:
+// they get a launch of their own.  64 requests of 200000 keys and a chunk of 500 tokens, 80 pages each: 4 bits, d = 128 and 64: 172, 172,
+// 146 us and 142, 142, 122; 8 bits: 188, 184, 180 and 145, 145, 128; bf16, d = 64: 162, 156, 156.  Rows of 256 bytes are read as fast by
+// one workgroup to a unit (242, 228, 241).  200 requests of 64000 keys, four chunks, 26 pages: 4 bits, d = 128: 287, 287, 255; bf16: 357,
+// 346, 352.
 enum class FewRows { BEHIND, IN_FRONT, APART };
 inline FewRows place_of_few(int batch, bool chosen, size_t lds, int row_bytes) {
   if (!chosen) return batch > FEW_FIRST ? FewRows::IN_FRONT : FewRows::BEHIND;

@@ -27,7 +27,11 @@ namespace {
 constexpr int LANES = 1024, WAVES = LANES / 64;
 constexpr int PER_LANE = paged::MAX_BATCH / LANES;
 constexpr int FORK_LANES = 256, FORK_ENTRIES = paged::MAX_BATCH;  // lanes of a workgroup, entries of the table that it may have
-constexpr int FORK_TARGET = 512;  // entries that it has if the batch is not larger: 512 samples 39.8 us, with 1024 42.3, with 4096 62.7
+// Entries that it has if the batch is not larger: few, as a workgroup goes through them alone.  512 samples 39.8 us, with 1024 42.3, with
+// 4096 62.7.  Fork alone, with 512, 2048, 4096 (and the copy of the tables, 3.5): 512 rows of 128 columns 18, 30, 45 us, of 512 columns 22,
+// 32, 47, of 2048 48, 43, 54; 1024 rows of 128 24, 32, 48, of 2048 81, 76, 74.  More than 2048 rows have one column with all of them: 4096
+// rows of 128 columns 59, of 512 92, of 2048 277.
+constexpr int FORK_TARGET = 512;
 constexpr int EMIT_LANES = 256, CHUNK = 4096;         // tokens that a workgroup of compact looks at together
 
 struct Group {
